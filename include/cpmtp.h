@@ -145,7 +145,8 @@ typedef struct CUstream_st* cpmtp_stream;
  * compiles the checks out and returns -1 here. */
 int cpmtp_debug_status(void);
 
-int cpmtp_version(void);   /* major * 100 + minor * 10; 110 added the distillation entry points, 120 CPMTP_FLAG_ACCUM_GRADS */
+int cpmtp_version(void);   /* major * 100 + minor * 10; 110 added the distillation entry points, 120 CPMTP_FLAG_ACCUM_GRADS,
+                              130 the embedding, norm and optimiser entry points */
 const char* cpmtp_status_string(int status);
 
 /* Read the environment knobs listed above again (they are otherwise read once per process).  For tests
@@ -379,6 +380,159 @@ int cpmtp_forward_host(const cpmtp_shape* shape, const void* h_host, const void*
                        float* loss_host, const cpmtp_saved* saved, void* workspace,
                        size_t workspace_bytes, int32_t* dev_status, cpmtp_stream stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Around the head in a training step: where its hidden states come from and where its gradients go.
+ * The paper has no counterpart for these entry points; it trains with them unprinted (an embedding table, a
+ * pre-norm transformer trunk, AdamW).
+ *
+ * All of them: sizes of zero are allowed and enqueue nothing (outputs that are sums over nothing are
+ * written as zeros); any row width and row stride is accepted, widths, strides and addresses that
+ * allow 16-byte accesses run faster; sums are held in fp32 in a fixed order without floating-point atomics, so results are
+ * bit-reproducible; every output is rounded once.
+ */
+
+/* element types */
+enum { CPMTP_BF16 = 0, CPMTP_F32 = 1 };
+
+/* Token that stands for no token (padding of ragged sequences): looked up as a row of zeros, no gradient. */
+#define CPMTP_EMBED_PAD (-1)
+
+typedef struct cpmtp_embed_shape {
+  int32_t T;          /* tokens, 0 <= T < 2^30 */
+  int32_t V;          /* rows of the table, 1 <= V < 2^30 */
+  int32_t d;          /* row width, 1 <= d < 2^24 */
+  int32_t type;       /* CPMTP_BF16 or CPMTP_F32: type of the T rows (`out`, `dy`) */
+  int64_t ld_table;   /* elements from one row of the table to the next, >= d */
+  int64_t ld_rows;    /* the same for the T rows */
+  float scale;
+  uint32_t flags;     /* CPMTP_FLAG_ACCUM_GRADS (backward) */
+} cpmtp_embed_shape;
+
+/*
+ * Embedding lookup with scaling: out[i, :] = scale * E[x[i], :], zeros where x[i] = CPMTP_EMBED_PAD.
+ * E [V, d] bf16, x [T] int32, out [T, d] of shape->type.  Any other x[i] outside [0, V) is clamped and raises
+ * dev_status to 1.
+ */
+int cpmtp_embed_forward(const cpmtp_embed_shape* shape, const void* E, const int32_t* x, void* out,
+                        int32_t* dev_status, cpmtp_stream stream);
+
+/*
+ * Its gradient: dE[v, :] = scale * sum over {i : x[i] = v} of dy[i, :], the whole table written.  With
+ * CPMTP_FLAG_ACCUM_GRADS the sum is added to what dE holds, and only the rows that occur are touched: that is how
+ * a table that is also the head's unembedding gets both its gradients (cpmtp_backward first).
+ * dy [T, d] of shape->type, dE [V, d] bf16.  The tokens are sorted (stable radix sort), so equal tokens are
+ * summed in the order of their positions.  Workspace: cpmtp_embed_workspace_bytes.
+ */
+size_t cpmtp_embed_workspace_bytes(const cpmtp_embed_shape* shape);
+int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const int32_t* x, void* dE,
+                         void* workspace, size_t workspace_bytes, int32_t* dev_status, cpmtp_stream stream);
+
+/* Row matrix: element (i, j) is data[i * ld + j]. */
+typedef struct cpmtp_rows {
+  void* data;
+  int64_t ld;
+} cpmtp_rows;
+
+/* The gate's logits: none, one per row ([N], ld is the distance between them) or one per element ([N, d]). */
+enum { CPMTP_GATE_NONE = 0, CPMTP_GATE_ROW = 1, CPMTP_GATE_CHANNEL = 2 };
+#define CPMTP_NORM_MAX_D 8192
+
+typedef struct cpmtp_norm_args {
+  int32_t N, d;            /* rows; row width, 1 <= d <= CPMTP_NORM_MAX_D */
+  int32_t stream_type;     /* CPMTP_BF16 or CPMTP_F32: type of x, x_out, dx_out and dx; all else is bf16 */
+  int32_t gate_kind;       /* CPMTP_GATE_* */
+  uint32_t flags;          /* CPMTP_FLAG_ACCUM_GRADS (backward): dw_post and dw_pre are added to */
+  float eps;               /* > 0 */
+  float res_scale;
+  cpmtp_rows x, block, gate;         /* residual stream; block output (data NULL: none); gate logits */
+  const void *w_post, *w_pre;        /* [d] weights of the norm after / before a block; NULL: no such norm */
+  cpmtp_rows x_out, y;               /* forward: written; backward: x_out is read */
+  float *rstd_post, *rstd_pre;       /* [N] forward: written (NULL: not kept); backward: read */
+  cpmtp_rows dy, dx_out;             /* backward: gradients of y and x_out (dx_out.data NULL: zero) */
+  cpmtp_rows dx, dblock, dgate;      /* backward: written; data NULL: not wanted */
+  void *dw_post, *dw_pre;            /* [d] bf16, backward: written; NULL: not wanted */
+} cpmtp_norm_args;
+
+/*
+ * The residual addition between two blocks with the norms on both sides of it, in one pass over the rows:
+ *   u      = w_post * block * rstd_post,   rstd_post[i] = (mean_j block[i, j]^2 + eps)^(-1/2)   (w_post NULL: u = block)
+ *   x_out  = res_scale * x + sigmoid(gate) * u                                       (no gate: factor 1)
+ *   y      = w_pre * x_out * rstd_pre,     rstd_pre[i] = (mean_j x_out[i, j]^2 + eps)^(-1/2)    (w_pre NULL: no y)
+ * y is computed from x_out before its rounding.  Without a block (block.data NULL) x_out is not written and y is the
+ * norm of x: the first norm of a trunk.  The last one of a trunk makes the `h` of cpmtp_forward.  x_out may be x.
+ */
+int cpmtp_norm_forward(const cpmtp_norm_args* args, cpmtp_stream stream);
+
+/*
+ * Gradients.  With t the gradient of x_out (dx_out plus what comes through y), xh = x_out * rstd_pre and
+ * bh = block * rstd_post:
+ *   t      = dx_out + rstd_pre * (w_pre * dy - xh * mean(w_pre * dy * xh))
+ *   dx     = res_scale * t           dw_pre  = sum_i dy * xh
+ *   dgate  = t * u * g * (1 - g)     (CPMTP_GATE_ROW: summed over the row),  du = g * t
+ *   dblock = rstd_post * (w_post * du - bh * mean(w_post * du * bh))    dw_post = sum_i du * bh
+ * Without a block, x_out is the x that the forward pass was given and res_scale is 1.  dx may be dx_out.
+ * Workspace: cpmtp_norm_workspace_bytes.
+ */
+size_t cpmtp_norm_workspace_bytes(const cpmtp_norm_args* args);
+int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t workspace_bytes, cpmtp_stream stream);
+
+/* Elements of an 8-bit optimiser state that share one exponent byte. */
+#define CPMTP_ADAMW_BLOCK 256
+
+typedef struct cpmtp_adamw_tensor {
+  void* param;             /* bf16 or fp32, updated in place */
+  const void* grad;        /* bf16 or fp32; NULL: the tensor is left alone in this step */
+  float* master;           /* fp32 copy of a bf16 param that the update works on, or NULL */
+  void *m, *v;             /* moments: fp32, or one byte per element */
+  uint8_t *m_exp, *v_exp;  /* 8-bit states: [ceil(numel / CPMTP_ADAMW_BLOCK)] exponents; else unused */
+  int64_t numel;           /* >= 0 */
+  int32_t param_type, grad_type;   /* CPMTP_BF16 or CPMTP_F32 */
+  float lr_scale;          /* of the learning rate, for this tensor */
+  float decay_scale;       /* of the weight decay, for this tensor (0: none) */
+} cpmtp_adamw_tensor;
+
+typedef struct cpmtp_adamw_hyper {
+  double lr, beta1, beta2, eps, weight_decay;   /* betas in [0, 1), the others >= 0 and finite */
+  int64_t step;            /* 1 for the first step */
+  uint32_t seed;           /* of the stochastic rounding */
+  int32_t state_bits;      /* 32 or 8 */
+  const float* coef;       /* device scalar that multiplies every gradient, or NULL; NaN: the step changes nothing */
+} cpmtp_adamw_hyper;
+
+/*
+ * AdamW (decoupled weight decay) over `count` tensors in one launch per 300 tensors:
+ *   g = coef * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr wd) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * `tensors` is a HOST array, read during the call; what it points to is on the device.
+ *
+ * 8-bit states: per block of CPMTP_ADAMW_BLOCK elements one exponent byte e (that of the block's largest magnitude
+ * after room is left for one step up; 0: all zero, 255: the block held an infinity or NaN, and decodes to NaN) and one
+ * byte per element: m is sign, 4 exponent and 3 mantissa bits, v has no sign bit and 4 mantissa bits, both with gradual
+ * underflow, covering 2^17 and 2^18 below the block's largest.  The update of p uses the moments before rounding.  The
+ * moments are rounded up or down at random so that their mean is kept: rounded to nearest, v would stop following
+ * its average as soon as one step changes it by less than half a unit, which at beta2 = 0.999 is always.  Where v
+ * rounds to zero m is stored as zero too, so that no step divides a remembered m by eps alone.
+ * A bf16 param without a master copy is rounded in the same way, for the same reason.
+ * The noise is an integer hash of (seed, step, place of the element), the place counted over all tensors with each
+ * rounded up to whole blocks: the same call gives the same bits.
+ */
+int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
+                     cpmtp_stream stream);
+
+/* The values of an 8-bit state of n elements as bf16 (exactly): `second` 0 for m, 1 for v. */
+int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,
+                             cpmtp_stream stream);
+
+/*
+ * Norm of all gradients together, and the coefficient that clips it: norm = sqrt(sum over tensors of grad^2),
+ * coef = min(1, max_norm / (norm + 1e-6)), NaN if the norm is not finite.  Only `grad`, `grad_type` and `numel` of the
+ * tensors are used.  norm [1], coef [1] fp32 device (either may be NULL); max_norm > 0, infinity: no clipping.
+ * Squares and their sums per thread are fp32 (a gradient above 1.8e19 counts as infinite), across threads fp64.
+ */
+size_t cpmtp_grad_norm_workspace_bytes(const cpmtp_adamw_tensor* tensors, int32_t count);
+int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_norm, float* norm, float* coef,
+                    void* workspace, size_t workspace_bytes, cpmtp_stream stream);
+
 /*
  * Per-stage device timing, for benchmarks.  Between cpmtp_profile_begin() and
  * cpmtp_profile_end() every kernel launch of the entry points above is bracketed
@@ -407,6 +561,12 @@ enum {
   CPMTP_STAGE_DRAFT_STEP,    /* per-token selection passes of cpmtp_sample_draft */
   CPMTP_STAGE_TEACHER_LSE,   /* expert weights per token (Eq. 14); the teacher's logsumexp_V is part of the KL pass */
   CPMTP_STAGE_KL,            /* second unembedding pass: KL term of Eq. 14 */
+  CPMTP_STAGE_EMBED,         /* embedding lookup */
+  CPMTP_STAGE_EMBED_GRAD,    /* its gradient: sort, sums */
+  CPMTP_STAGE_NORM,          /* norms and gated residual addition */
+  CPMTP_STAGE_NORM_GRAD,     /* their gradient */
+  CPMTP_STAGE_GRAD_NORM,     /* norm of all gradients */
+  CPMTP_STAGE_ADAMW,         /* optimiser step */
   CPMTP_STAGE_COUNT
 };
 int cpmtp_profile_begin(void);

@@ -29,12 +29,20 @@ EXPORTS = [
     "cpmtp_profile_end", "cpmtp_score_draft_static", "cpmtp_sample_draft",
     "cpmtp_forward_full", "cpmtp_backward_full", "cpmtp_verify_draft",
     "cpmtp_distill_forward", "cpmtp_distill_backward", "cpmtp_reload_knobs", "cpmtp_debug_status",
+    "cpmtp_embed_forward", "cpmtp_embed_workspace_bytes", "cpmtp_embed_backward",
+    "cpmtp_norm_forward", "cpmtp_norm_workspace_bytes", "cpmtp_norm_backward",
+    "cpmtp_adamw_step", "cpmtp_adamw_state_values", "cpmtp_grad_norm_workspace_bytes", "cpmtp_grad_norm",
 ]
 
 STATIC_SCRATCH_BYTES = 4 << 20
+BF16, F32 = 0, 1
+EMBED_PAD = -1
+GATE_NONE, GATE_ROW, GATE_CHANNEL = 0, 1, 2
+ADAMW_BLOCK = 256
 
 STAGES = ["gate", "proj", "lse", "mixture", "finalize", "coeff", "logit_grad", "dz", "de", "de_convert",
-          "dw_head", "dh", "dw_g", "draft_step", "teacher_lse", "kl"]
+          "dw_head", "dh", "dw_g", "draft_step", "teacher_lse", "kl", "embed", "embed_grad", "norm", "norm_grad", "grad_norm",
+          "adamw"]
 
 
 class CShape(ctypes.Structure):
@@ -50,6 +58,38 @@ class CSaved(ctypes.Structure):
 class CDistillSaved(ctypes.Structure):
     _fields_ = [("lse_t", ctypes.c_void_p), ("logpi", ctypes.c_void_p), ("pm", ctypes.c_void_p),
                 ("kl", ctypes.c_void_p)]
+
+
+class CEmbedShape(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("V", ctypes.c_int32), ("d", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("ld_table", ctypes.c_int64), ("ld_rows", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("flags", ctypes.c_uint32)]
+
+
+def _rows_fields(*names):
+    return [f for n in names for f in ((n, ctypes.c_void_p), ("ld_" + n, ctypes.c_int64))]
+
+
+class CNormArgs(ctypes.Structure):
+    _fields_ = ([("N", ctypes.c_int32), ("d", ctypes.c_int32), ("stream_type", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
+                 ("flags", ctypes.c_uint32), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float)]
+                + _rows_fields("x", "block", "gate") + [("w_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p)]
+                + _rows_fields("x_out", "y") + [("rstd_post", ctypes.c_void_p), ("rstd_pre", ctypes.c_void_p)]
+                + _rows_fields("dy", "dx_out", "dx", "dblock", "dgate")
+                + [("dw_post", ctypes.c_void_p), ("dw_pre", ctypes.c_void_p)])
+
+
+class CAdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("lr_scale", ctypes.c_float),
+                ("decay_scale", ctypes.c_float)]
+
+
+class CAdamWHyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint32),
+                ("state_bits", ctypes.c_int32), ("coef", ctypes.c_void_p)]
 
 
 _lib = None
@@ -103,6 +143,27 @@ def load_library() -> ctypes.CDLL:
     lib.cpmtp_distill_backward.restype = ctypes.c_int
     lib.cpmtp_distill_backward.argtypes = [shp, vp, vp, vp, vp, i32p, vp, svp, dsp, ctypes.c_float, ctypes.c_float,
                                            fp, fp, vp, vp, vp, vp, vp, sz, i32p, vp]
+    esp, nap, atp = ctypes.POINTER(CEmbedShape), ctypes.POINTER(CNormArgs), ctypes.POINTER(CAdamWTensor)
+    lib.cpmtp_embed_forward.restype = ctypes.c_int
+    lib.cpmtp_embed_forward.argtypes = [esp, vp, i32p, vp, i32p, vp]
+    lib.cpmtp_embed_workspace_bytes.restype = sz
+    lib.cpmtp_embed_workspace_bytes.argtypes = [esp]
+    lib.cpmtp_embed_backward.restype = ctypes.c_int
+    lib.cpmtp_embed_backward.argtypes = [esp, vp, i32p, vp, vp, sz, i32p, vp]
+    lib.cpmtp_norm_forward.restype = ctypes.c_int
+    lib.cpmtp_norm_forward.argtypes = [nap, vp]
+    lib.cpmtp_norm_workspace_bytes.restype = sz
+    lib.cpmtp_norm_workspace_bytes.argtypes = [nap]
+    lib.cpmtp_norm_backward.restype = ctypes.c_int
+    lib.cpmtp_norm_backward.argtypes = [nap, vp, sz, vp]
+    lib.cpmtp_adamw_step.restype = ctypes.c_int
+    lib.cpmtp_adamw_step.argtypes = [atp, ctypes.c_int32, ctypes.POINTER(CAdamWHyper), vp]
+    lib.cpmtp_adamw_state_values.restype = ctypes.c_int
+    lib.cpmtp_adamw_state_values.argtypes = [vp, vp, ctypes.c_int64, ctypes.c_int32, vp, vp]
+    lib.cpmtp_grad_norm_workspace_bytes.restype = sz
+    lib.cpmtp_grad_norm_workspace_bytes.argtypes = [atp, ctypes.c_int32]
+    lib.cpmtp_grad_norm.restype = ctypes.c_int
+    lib.cpmtp_grad_norm.argtypes = [atp, ctypes.c_int32, ctypes.c_float, fp, fp, vp, sz, vp]
     lib.cpmtp_reload_knobs.restype = ctypes.c_int
     lib.cpmtp_debug_status.restype = ctypes.c_int
     lib.cpmtp_profile_begin.restype = ctypes.c_int
@@ -560,3 +621,349 @@ def distill_backward(h, W_head, E, W_g, x, teacher, saved: Saved, dsaved: Distil
                                     _ptr(workspace), workspace.numel(), _ptr(dev_status), _stream())
     _check(rc)
     return res
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Around the head in a training step: embedding lookup, norms with gate and residual addition, AdamW.
+
+_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise CpmtpError(f"cpmtp: {what}")
+
+
+def _on_device(ref: torch.Tensor, **tensors) -> None:
+    """Every tensor that is given lies on `ref`'s device, which is the current one (its current stream is used)."""
+    _need(ref.is_cuda and ref.device.index == torch.cuda.current_device(), "tensors must be on the current CUDA device")
+    for name, t in tensors.items():
+        _need(t is None or t.device == ref.device, f"{name} is on another device")
+
+
+def _rows(t: torch.Tensor, n: int, d: int, dtype, name: str) -> tuple:
+    """(pointer, row stride) of an [n, d] matrix whose rows are contiguous."""
+    _need(t.dim() == 2 and t.shape[0] == n and t.shape[1] == d, f"{name} must be [{n}, {d}]")
+    _need(t.dtype == dtype, f"{name} must be {dtype}")
+    ld = t.stride(0) if n > 1 else d
+    _need(d <= 1 or t.stride(1) == 1, f"{name}: the elements of a row must be contiguous")
+    _need(ld >= d, f"{name}: rows must not overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t: torch.Tensor, n: int, dtype, name: str) -> int:
+    _need(t.dim() == 1 and t.shape[0] == n and t.dtype == dtype and (n <= 1 or t.stride(0) == 1), f"{name} must be a contiguous [{n}] {dtype}")
+    return t.data_ptr()
+
+
+def _check_status(dev_status: Optional[torch.Tensor]) -> None:
+    _need(dev_status is None or (dev_status.dtype == torch.int32 and dev_status.numel() >= 1), "dev_status must be int32 [1]")
+
+
+def _check_workspace(workspace: torch.Tensor) -> torch.Tensor:
+    _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace must be contiguous uint8")
+    return workspace
+
+
+def embed_forward(E: torch.Tensor, x: torch.Tensor, *, scale: float = 1.0, out_dtype: torch.dtype = torch.bfloat16,
+                  out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """cpmtp_embed_forward: scale * E[x] for tokens x (any shape, int32, EMBED_PAD = a row of zeros); E [V, d] bf16.
+    Returns x.shape + (d,) of `out_dtype` (bf16 or fp32), or `out` ([x.numel(), d], rows may be strided)."""
+    _need(E.dim() == 2 and E.shape[0] >= 1 and E.shape[1] >= 1, "E must be [V, d]")
+    V, d = E.shape
+    T = x.numel()
+    _on_device(E, x=x, out=out, dev_status=dev_status)
+    _need(x.dtype == torch.int32 and x.is_contiguous(), "x must be contiguous int32")
+    _check_status(dev_status)
+    if out is None:
+        out = torch.empty((*x.shape, d), dtype=out_dtype, device=E.device)
+        _need(out_dtype in _TYPES, "out_dtype must be bfloat16 or float32")
+        po, ldo = out.data_ptr(), d
+    else:
+        _need(out.dtype in _TYPES, "out must be bfloat16 or float32")
+        po, ldo = _rows(out, T, d, out.dtype, "out")
+    pe, lde = _rows(E, V, d, torch.bfloat16, "E")
+    shape = CEmbedShape(T, V, d, _TYPES[out.dtype], lde, ldo, scale, 0)
+    _check(load_library().cpmtp_embed_forward(ctypes.byref(shape), pe, x.data_ptr(), po, _ptr(dev_status), _stream()))
+    return out
+
+
+def embed_backward(dy: torch.Tensor, x: torch.Tensor, V: int, *, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                   accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+                   dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """cpmtp_embed_backward: dE [V, d] bf16, the scaled sums of the rows of dy (x.shape + (d,), bf16 or fp32; a 2-D dy may
+    have strided rows) over equal tokens.  accumulate: add to `out`, touching only the rows that occur."""
+    T, d = x.numel(), dy.shape[-1]
+    _on_device(dy, x=x, out=out, dev_status=dev_status, workspace=workspace)
+    _need(x.dtype == torch.int32 and x.is_contiguous(), "x must be contiguous int32")
+    _need(dy.dtype in _TYPES, "dy must be bfloat16 or float32")
+    _check_status(dev_status)
+    if dy.dim() != 2:
+        _need(tuple(dy.shape[:-1]) == tuple(x.shape) and dy.is_contiguous(), "dy must be x.shape + (d,)")
+        dy = dy.view(T, d)
+    pd, ldd = _rows(dy, T, d, dy.dtype, "dy")
+    _need(not accumulate or out is not None, "accumulation needs the tensor to add to")
+    if out is None:
+        out = torch.empty((V, d), dtype=torch.bfloat16, device=dy.device)
+    pe, lde = _rows(out, V, d, torch.bfloat16, "out")
+    shape = CEmbedShape(T, V, d, _TYPES[dy.dtype], lde, ldd, scale, FLAG_ACCUM_GRADS if accumulate else 0)
+    lib = load_library()
+    if workspace is None:
+        workspace = alloc_workspace(int(lib.cpmtp_embed_workspace_bytes(ctypes.byref(shape))), dy.device)
+    _check_workspace(workspace)
+    _check(lib.cpmtp_embed_backward(ctypes.byref(shape), pd, x.data_ptr(), pe, workspace.data_ptr(), workspace.numel(), _ptr(dev_status),
+                                    _stream()))
+    return out
+
+
+def _norm_args(ref, w_pre, block, gate, w_post, res_scale, eps) -> CNormArgs:
+    """The inputs that both directions share; `ref` is x or x_out."""
+    _need(ref.dim() == 2 and ref.dtype in _TYPES, "the residual stream must be [N, d] bfloat16 or float32")
+    N, d = ref.shape
+    a = CNormArgs()
+    a.N, a.d, a.stream_type, a.eps, a.res_scale = N, d, _TYPES[ref.dtype], eps, res_scale
+    if w_pre is not None:
+        a.w_pre = _vector(w_pre, d, torch.bfloat16, "w_pre")
+    if w_post is not None:
+        a.w_post = _vector(w_post, d, torch.bfloat16, "w_post")
+    if block is not None:
+        a.block, a.ld_block = _rows(block, N, d, torch.bfloat16, "block")
+    if gate is not None:
+        if gate.dim() == 1:
+            _need(gate.shape[0] == N and gate.dtype == torch.bfloat16 and (N <= 1 or gate.stride(0) >= 1), f"gate must be [{N}] or [{N}, {d}] bfloat16")
+            a.gate_kind, a.gate, a.ld_gate = GATE_ROW, gate.data_ptr(), gate.stride(0) if N > 1 else 1
+        else:
+            a.gate_kind = GATE_CHANNEL
+            a.gate, a.ld_gate = _rows(gate, N, d, torch.bfloat16, "gate")
+    return a
+
+
+def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block: Optional[torch.Tensor] = None,
+                 gate: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None, res_scale: float = 1.0,
+                 eps: float = 1e-6, out: Optional[dict] = None) -> dict:
+    """cpmtp_norm_forward: x_out = res_scale * x + sigmoid(gate) * rmsnorm(block, w_post), y = rmsnorm(x_out, w_pre).
+    x [N, d] bf16 or fp32; block and gate ([N, d], or one logit per row [N]) bf16, rows may be strided (the halves of one
+    projection's output).  Without w_post the block is added as it is, without w_pre there is no y, without a block
+    x_out is x itself and y its norm.  Returns {"x_out", "y", "rstd_post", "rstd_pre"} (None where there is none);
+    tensors given in `out` are written instead of new ones (x_out may be x)."""
+    a = _norm_args(x, w_pre, block, gate, w_post, res_scale, eps)
+    N, d = x.shape
+    res = out if out is not None else {}
+    _on_device(x, w_pre=w_pre, block=block, gate=gate, w_post=w_post, **{f"out[{k}]": v for k, v in res.items()})
+    a.x, a.ld_x = _rows(x, N, d, x.dtype, "x")
+    for name, there, size, dtype in (("x_out", block is not None, (N, d), x.dtype), ("y", w_pre is not None, (N, d), torch.bfloat16),
+                                     ("rstd_post", w_post is not None, (N,), torch.float32), ("rstd_pre", w_pre is not None, (N,), torch.float32)):
+        if not there:
+            res[name] = None
+        elif res.get(name) is None:
+            res[name] = torch.empty(size, dtype=dtype, device=x.device)
+    if block is None:
+        res["x_out"] = x
+    else:
+        a.x_out, a.ld_x_out = _rows(res["x_out"], N, d, x.dtype, "x_out")
+    if w_pre is not None:
+        a.y, a.ld_y = _rows(res["y"], N, d, torch.bfloat16, "y")
+        a.rstd_pre = _vector(res["rstd_pre"], N, torch.float32, "rstd_pre")
+    if res["rstd_post"] is not None:
+        a.rstd_post = _vector(res["rstd_post"], N, torch.float32, "rstd_post")
+    _check(load_library().cpmtp_norm_forward(ctypes.byref(a), _stream()))
+    return res
+
+
+def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Optional[torch.Tensor] = None,
+                  rstd_pre: Optional[torch.Tensor] = None, *, dx_out: Optional[torch.Tensor] = None,
+                  block: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                  w_post: Optional[torch.Tensor] = None, rstd_post: Optional[torch.Tensor] = None, res_scale: float = 1.0,
+                  eps: float = 1e-6, out: Optional[dict] = None, skip: tuple = (), accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None) -> dict:
+    """cpmtp_norm_backward; x_out, rstd_pre and rstd_post as norm_forward returned them, the other inputs as it was given.
+    dy [N, d] bf16 (None: no gradient of y), dx_out [N, d] of the stream's type (None: zero).
+    Returns {"dx", "dblock", "dgate", "dw_post", "dw_pre"}: None where there is nothing to differentiate or the name is
+    in `skip`.  accumulate: dw_post and dw_pre are added to those given in `out`."""
+    a = _norm_args(x_out, w_pre, block, gate, w_post, res_scale, eps)
+    N, d = x_out.shape
+    res = out if out is not None else {}
+    _need(not accumulate or out is not None, "accumulation needs the tensors to add to")
+    _need(dy is not None or dx_out is not None, "no gradient comes in: dy and dx_out are both None")
+    _need(dy is None or (w_pre is not None and rstd_pre is not None), "dy needs w_pre and rstd_pre")
+    _need(w_post is None or rstd_post is not None, "w_post needs rstd_post")
+    _on_device(x_out, dy=dy, w_pre=w_pre, rstd_pre=rstd_pre, dx_out=dx_out, block=block, gate=gate, w_post=w_post, rstd_post=rstd_post,
+               workspace=workspace, **{f"out[{k}]": v for k, v in res.items()})
+    a.x_out, a.ld_x_out = _rows(x_out, N, d, x_out.dtype, "x_out")
+    if dy is not None:
+        a.dy, a.ld_dy = _rows(dy, N, d, torch.bfloat16, "dy")
+        a.rstd_pre = _vector(rstd_pre, N, torch.float32, "rstd_pre")
+    if dx_out is not None:
+        a.dx_out, a.ld_dx_out = _rows(dx_out, N, d, x_out.dtype, "dx_out")
+    if rstd_post is not None:
+        a.rstd_post = _vector(rstd_post, N, torch.float32, "rstd_post")
+    dev = x_out.device
+    made = dict(dx=lambda: torch.empty((N, d), dtype=x_out.dtype, device=dev))
+    if block is not None:
+        made["dblock"] = lambda: torch.empty((N, d), dtype=torch.bfloat16, device=dev)
+        if gate is not None:
+            made["dgate"] = lambda: torch.empty(gate.shape, dtype=torch.bfloat16, device=dev)
+        if w_post is not None:
+            made["dw_post"] = lambda: torch.empty(d, dtype=torch.bfloat16, device=dev)
+    if dy is not None:
+        made["dw_pre"] = lambda: torch.empty(d, dtype=torch.bfloat16, device=dev)
+    for name in ("dx", "dblock", "dgate", "dw_post", "dw_pre"):
+        if name in skip or name not in made:
+            res[name] = None
+        elif res.get(name) is None:
+            _need(not (accumulate and name.startswith("dw")), f"accumulation needs out[{name}]")
+            res[name] = made[name]()
+    if res["dx"] is not None:
+        a.dx, a.ld_dx = _rows(res["dx"], N, d, x_out.dtype, "dx")
+    if res["dblock"] is not None:
+        a.dblock, a.ld_dblock = _rows(res["dblock"], N, d, torch.bfloat16, "dblock")
+    if res["dgate"] is not None:
+        if a.gate_kind == GATE_CHANNEL:
+            a.dgate, a.ld_dgate = _rows(res["dgate"], N, d, torch.bfloat16, "dgate")
+        else:
+            g = res["dgate"]
+            _need(g.dim() == 1 and g.shape[0] == N and g.dtype == torch.bfloat16 and (N <= 1 or g.stride(0) >= 1), f"dgate must be [{N}] bfloat16")
+            a.dgate, a.ld_dgate = g.data_ptr(), g.stride(0) if N > 1 else 1
+    if res["dw_post"] is not None:
+        a.dw_post = _vector(res["dw_post"], d, torch.bfloat16, "dw_post")
+    if res["dw_pre"] is not None:
+        a.dw_pre = _vector(res["dw_pre"], d, torch.bfloat16, "dw_pre")
+    a.flags = FLAG_ACCUM_GRADS if accumulate else 0
+    lib = load_library()
+    if workspace is None:
+        workspace = alloc_workspace(int(lib.cpmtp_norm_workspace_bytes(ctypes.byref(a))), dev)
+    _check_workspace(workspace)
+    _check(lib.cpmtp_norm_backward(ctypes.byref(a), workspace.data_ptr(), workspace.numel(), _stream()))
+    return res
+
+
+def norm_workspace_bytes(N: int, d: int) -> int:
+    """Scratch bytes of norm_backward for [N, d]."""
+    a = CNormArgs(N, d, BF16, GATE_NONE, 0, 1e-6, 1.0)
+    a.w_pre = 256
+    return int(load_library().cpmtp_norm_workspace_bytes(ctypes.byref(a)))
+
+
+def embed_workspace_bytes(T: int, V: int, d: int) -> int:
+    """Scratch bytes of embed_backward for T tokens and a [V, d] table."""
+    shape = CEmbedShape(T, V, d, BF16, d, d, 1.0, 0)
+    return int(load_library().cpmtp_embed_workspace_bytes(ctypes.byref(shape)))
+
+
+def _grad_table(grads) -> ctypes.Array:
+    table = (CAdamWTensor * max(1, len(grads)))()
+    ref = next((g for g in grads if g is not None), None)
+    for c, g in zip(table, grads):
+        if g is None:
+            continue
+        _need(g.dtype in _TYPES and g.is_contiguous() and g.is_cuda and g.device == ref.device, "gradients must be contiguous bfloat16 or float32 on one device")
+        c.grad, c.numel, c.grad_type = g.data_ptr(), g.numel(), _TYPES[g.dtype]
+    return table
+
+
+def grad_norm_workspace_bytes(grads) -> int:
+    return int(load_library().cpmtp_grad_norm_workspace_bytes(_grad_table(grads), len(grads)))
+
+
+def grad_norm(grads, *, max_norm: float = float("inf"), workspace: Optional[torch.Tensor] = None, out: Optional[dict] = None) -> dict:
+    """cpmtp_grad_norm over a list of gradients (None entries are left out): {"norm", "coef"}, fp32 [1] on the device; coef
+    is what AdamW.step takes to clip to max_norm (NaN where the norm is not finite, which skips the step)."""
+    ref = next((g for g in grads if g is not None), None)
+    _need(ref is not None, "there is no gradient")
+    _on_device(ref, workspace=workspace)
+    table = _grad_table(grads)
+    lib = load_library()
+    if workspace is None:
+        workspace = alloc_workspace(int(lib.cpmtp_grad_norm_workspace_bytes(table, len(grads))), ref.device)
+    _check_workspace(workspace)
+    res = out if out is not None else {}
+    for name in ("norm", "coef"):
+        if name not in res:
+            res[name] = torch.empty(1, dtype=torch.float32, device=ref.device)
+        _need(res[name].dtype == torch.float32 and res[name].device == ref.device and res[name].numel() >= 1, f"{name} must be float32 [1]")
+    _check(lib.cpmtp_grad_norm(table, len(grads), max_norm, res["norm"].data_ptr(), res["coef"].data_ptr(), workspace.data_ptr(),
+                               workspace.numel(), _stream()))
+    return res
+
+
+class AdamW:
+    """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch.
+
+    params: contiguous bf16 or fp32 tensors, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
+    one exponent byte per ADAMW_BLOCK elements).  master: True for fp32 copies of the bf16 parameters, or a list of
+    them (None entries: none); without one a bf16 parameter is rounded stochastically.  lr_scale, decay_scale: factors per
+    tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run; new states are zero."""
+
+    def __init__(self, params, *, bits: int = 32, master=False, lr_scale=None, decay_scale=None, state: Optional[dict] = None):
+        self.params = list(params)
+        n = len(self.params)
+        _need(bits in (32, 8), "bits must be 32 or 8")
+        self.bits = bits
+        for p in self.params:
+            _need(p.dtype in _TYPES and p.is_contiguous() and p.is_cuda and p.device == self.params[0].device,
+                  "parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
+        if master is True:
+            master = [p.float() if p.dtype == torch.bfloat16 else None for p in self.params]
+        self.master = list(master) if master else [None] * n
+        state = state or {}
+        stype = torch.float32 if bits == 32 else torch.uint8
+        self.m, self.v = (self._states(state.get(k), stype, lambda p: p.numel(), k) for k in ("m", "v"))
+        self.m_exp = self.v_exp = [None] * n
+        if bits == 8:
+            self.m_exp, self.v_exp = (self._states(state.get(k), torch.uint8, lambda p: -(-p.numel() // ADAMW_BLOCK), k) for k in ("m_exp", "v_exp"))
+        for name, scales in (("lr_scale", lr_scale), ("decay_scale", decay_scale), ("master", self.master)):
+            _need(scales is None or len(scales) == n, f"{name} needs one entry per parameter")
+        self._table = (CAdamWTensor * max(1, n))()
+        for i, (c, p) in enumerate(zip(self._table, self.params)):
+            w = self.master[i]
+            _need(w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == p.numel() and w.device == p.device
+                                and p.dtype == torch.bfloat16), "a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
+            c.param, c.numel, c.param_type = p.data_ptr(), p.numel(), _TYPES[p.dtype]
+            c.master = w.data_ptr() if w is not None else None
+            c.m, c.v = self.m[i].data_ptr(), self.v[i].data_ptr()
+            if bits == 8:
+                c.m_exp, c.v_exp = self.m_exp[i].data_ptr(), self.v_exp[i].data_ptr()
+            c.lr_scale = 1.0 if lr_scale is None else float(lr_scale[i])
+            c.decay_scale = 1.0 if decay_scale is None else float(decay_scale[i])
+
+    def _states(self, given, dtype, size, name) -> list:
+        if given is None:
+            return [torch.zeros(size(p), dtype=dtype, device=p.device) for p in self.params]
+        _need(len(given) == len(self.params), f"{name} needs one entry per parameter")
+        for t, p in zip(given, self.params):
+            _need(t.dtype == dtype and t.is_contiguous() and t.numel() == size(p) and t.device == p.device, f"{name}: contiguous {dtype} of {size(p)} elements")
+        return list(given)
+
+    def step(self, grads, t: int, *, lr: float, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
+             coef: Optional[torch.Tensor] = None, seed: int = 0) -> None:
+        """Step t (1 for the first) with one gradient per parameter (bf16 or fp32, contiguous; None leaves a parameter alone).
+        coef: fp32 [1] on the device that multiplies the gradients (grad_norm's), or None."""
+        params = self.params
+        _need(len(grads) == len(params), "one gradient per parameter")
+        if not params:
+            return
+        dev = params[0].device
+        _on_device(params[0], coef=coef)
+        _need(coef is None or (coef.dtype == torch.float32 and coef.numel() >= 1), "coef must be float32 [1]")
+        for c, g in zip(self._table, grads):
+            if g is None:
+                c.grad = None
+                continue
+            _need(g.dtype in _TYPES and g.is_contiguous() and g.device == dev and g.numel() == c.numel, "a gradient is a contiguous tensor of its parameter's size")
+            c.grad, c.grad_type = g.data_ptr(), _TYPES[g.dtype]
+        hyper = CAdamWHyper(lr, betas[0], betas[1], eps, weight_decay, t, seed & 0xFFFFFFFF, self.bits,
+                            None if coef is None else coef.data_ptr())
+        _check(load_library().cpmtp_adamw_step(self._table, len(params), ctypes.byref(hyper), _stream()))
+
+
+def adamw_state_values(codes: torch.Tensor, exps: torch.Tensor, *, second: bool, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """cpmtp_adamw_state_values: the values of an 8-bit moment (second: v, else m) as bf16, exactly."""
+    n = codes.numel()
+    _on_device(codes, exps=exps, out=out)
+    _need(codes.dtype == torch.uint8 and codes.is_contiguous(), "codes must be contiguous uint8")
+    _need(exps.dtype == torch.uint8 and exps.is_contiguous() and exps.numel() == -(-n // ADAMW_BLOCK), "exps: one byte per block")
+    if out is None:
+        out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
+    _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == n, "out must be contiguous bfloat16 of codes' size")
+    _check(load_library().cpmtp_adamw_state_values(codes.data_ptr(), exps.data_ptr(), n, 1 if second else 0, out.data_ptr(), _stream()))
+    return out

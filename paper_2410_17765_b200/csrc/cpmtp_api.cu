@@ -13,6 +13,7 @@
 #include "distill_epilogues.cuh"
 #include "distill_kernels.cuh"
 #include "epilogues.cuh"
+#include "host_util.cuh"
 #include "sampler_kernels.cuh"
 #include "small_kernels.cuh"
 #include "tc_gemm.cuh"
@@ -23,7 +24,6 @@ namespace {
 
 constexpr int kBN = 256;
 constexpr int kStages = 4;
-constexpr size_t kAlign = 256;
 // Bound on the chunk of recomputed logit gradients (bf16) that the backward holds at a time.  Large on
 // purpose (the device has 180 GB): every chunk costs one read-modify-write of the fp32 dE accumulator and a
 // partly filled last wave in each of its GEMMs, so few, long chunks are cheaper than many short ones.
@@ -35,34 +35,6 @@ constexpr int kWideBM = 2 * kBM;
 using CfgKKSkinny = TileCfg<kBN, 5, false, false, 32>;   // <= 32 rows of A: bandwidth-bound draft scoring
 using WideKK = TileCfg<kBN, kWideStages, false, false, kBM, 2>;   // 256 x 256 tiles, two row blocks share B
 using CfgProj = TileCfg<kBN, kStages, false, false, kBM, 1, 2>;   // 128-row tiles, eight epilogue warps (head projection)
-
-inline size_t align_up(size_t v, size_t a = kAlign) { return (v + a - 1) / a * a; }
-
-struct DeviceInfo {
-  int sms = 0;
-  int cc_major = 0;
-  bool ok = false;
-};
-
-// One lock for the small per-process caches below (device properties, kernel attributes, tensor maps,
-// the static scratch address).  Host-side only and held for microseconds; calls from several threads are safe.
-std::mutex g_cache_mutex;
-
-// Cached per device ordinal; filled on first use with that device current.
-DeviceInfo* device_info() {
-  static DeviceInfo infos[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-  std::lock_guard<std::mutex> lock(g_cache_mutex);
-  DeviceInfo& di = infos[dev];
-  if (!di.ok) {
-    if (cudaDeviceGetAttribute(&di.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
-    if (cudaDeviceGetAttribute(&di.cc_major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess)
-      return nullptr;
-    di.ok = true;
-  }
-  return &di;
-}
 
 // Testing / tuning knobs from the environment, read once per process (and again by cpmtp_reload_knobs);
 // 0 = not set.
@@ -118,8 +90,6 @@ int validate_shape(const cpmtp_shape* s) {
   if (static_cast<double>(s->N) * s->n * s->r >= 2147483648.0) return CPMTP_ERR_SHAPE;
   return CPMTP_OK;
 }
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // Wide (256-row) tiles move a third fewer operand bytes per flop but cannot overlap their
 // epilogue with the next tile's MMAs, so they pay when the contraction is long enough to
@@ -312,31 +282,6 @@ DistillLayout distill_layout(const cpmtp_shape& s, int sms) {
   return L;
 }
 
-// Optional per-stage timing: events bracket each launch while profiling is on.
-struct Profiler {
-  bool on = false;
-  std::vector<cudaEvent_t> events;   // start/stop pairs
-  std::vector<int> stages;
-};
-Profiler g_prof;
-
-struct ProfScope {
-  cudaStream_t st;
-  bool active;
-  ProfScope(int stage, cudaStream_t stream) : st(stream), active(g_prof.on) {
-    if (!active) return;
-    cudaEvent_t a, b;
-    if (cudaEventCreate(&a) != cudaSuccess || cudaEventCreate(&b) != cudaSuccess) { active = false; return; }
-    g_prof.events.push_back(a);
-    g_prof.events.push_back(b);
-    g_prof.stages.push_back(stage);
-    cudaEventRecord(a, st);
-  }
-  ~ProfScope() {
-    if (active) cudaEventRecord(g_prof.events.back(), st);
-  }
-};
-
 // ---- full head (Eq. 6 as printed) ----
 struct FullLayout {
   size_t logw, q, wbar, lse, tgt, part_m, part_l, total;
@@ -465,24 +410,6 @@ bool cached_tmap(CUtensorMap* out, const TmapKey& key) {
   return true;
 }
 
-// Launch with programmatic stream serialization: the kernel may be scheduled while the one before it in
-// the stream drains; it calls ptx::grid_dep_wait() before it touches anything that kernel produced.
-template <class... KArgs, class... Args>
-cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
-                       Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
 template <class Cfg, class Epi>
 cudaError_t launch_gemm(const void* A, uint64_t a_rows, uint64_t a_ld, const void* B, uint64_t b_rows,
                         uint64_t b_ld, uint64_t kdim, const Sched& sched_in, const typename Epi::Params& ep,
@@ -563,11 +490,6 @@ cudaError_t gemm_auto(const void* A, uint64_t a_ld, const void* B, uint64_t b_ld
   return launch_gemm<TileCfg<kBN, kStages, A_MN, B_MN>, Epi>(A, m_rows, a_ld, B, n_cols, b_ld, kdim, sc, ep,
                                                             dev_status, sms, stream);
 }
-
-#define CPMTP_TRY(expr)                         \
-  do {                                          \
-    if ((expr) != cudaSuccess) return CPMTP_ERR_LAUNCH; \
-  } while (0)
 
 // Forward pipeline shared by cpmtp_forward and cpmtp_score_draft.
 int run_forward(const cpmtp_shape& s, const uint16_t* h, const uint16_t* W_head, const uint16_t* E,
@@ -847,7 +769,7 @@ static int backward_impl(const cpmtp_shape* shape, const void* h, const void* W_
 
 extern "C" {
 
-int cpmtp_version(void) { return 120; }   // 1.2: gradient accumulation flag, knob reload
+int cpmtp_version(void) { return 130; }   // 1.3: embedding, norms, optimiser
 
 int cpmtp_reload_knobs(void) {
   knobs();   // make sure the one-time read has happened, then read again
@@ -903,7 +825,7 @@ const char* cpmtp_status_string(int status) {
   switch (status) {
     case CPMTP_OK: return "ok";
     case CPMTP_ERR_NULL: return "a required pointer is NULL";
-    case CPMTP_ERR_SHAPE: return "shape outside the supported limits (d % 64 == 0, r <= 32, n <= 8, sizes >= 1)";
+    case CPMTP_ERR_SHAPE: return "shape or argument outside the supported limits (head: d % 64 == 0, r <= 32, n <= 8, sizes >= 1)";
     case CPMTP_ERR_ALIGN: return "a pointer is not aligned as required";
     case CPMTP_ERR_WORKSPACE: return "workspace too small";
     case CPMTP_ERR_ARCH: return "current device is not compute capability 10.x";

@@ -1,0 +1,564 @@
+// C-ABI of the operators around the head in a training step: embedding lookup and its gradient, norms with gate
+// and residual addition, AdamW and gradient clipping.  See include/cpmtp.h for the contract.
+#include "../../include/cpmtp.h"
+
+#include <cuda_runtime.h>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <type_traits>
+
+#include "adamw_kernels.cuh"
+#include "embed_kernels.cuh"
+#include "host_util.cuh"
+#include "norm_kernels.cuh"
+
+namespace cpmtp {
+namespace {
+
+using io::bf16_t;
+
+int check_device(DeviceInfo** out) {
+  DeviceInfo* di = device_info();
+  if (di == nullptr) return CPMTP_ERR_LAUNCH;
+  if (di->cc_major != 10) return CPMTP_ERR_ARCH;
+  *out = di;
+  return CPMTP_OK;
+}
+
+bool known_type(int t) { return t == CPMTP_BF16 || t == CPMTP_F32; }
+size_t type_bytes(int t) { return t == CPMTP_F32 ? 4 : 2; }
+
+// ------------------------------------------------------------------------------------------- embedding
+int check_embed(const cpmtp_embed_shape* s) {
+  if (s == nullptr) return CPMTP_ERR_NULL;
+  if (s->T < 0 || s->T >= (1 << 30) || s->V < 1 || s->V >= (1 << 30) || s->d < 1 || s->d >= (1 << 24)) return CPMTP_ERR_SHAPE;
+  if (s->ld_table < s->d || s->ld_rows < s->d || !known_type(s->type)) return CPMTP_ERR_SHAPE;
+  return CPMTP_OK;
+}
+
+struct EmbedLayout {
+  int bits, passes, blocks;      // digits of the sort; thread blocks of a pass
+  int slabs, chunks;
+  size_t hist, keys, head, tail, total;
+};
+
+EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
+  EmbedLayout L;
+  int width = 1;
+  while ((1ll << width) <= s.V) ++width;         // keys are 0 .. V
+  L.passes = (width + embed::kMaxBits - 1) / embed::kMaxBits;
+  L.bits = (width + L.passes - 1) / L.passes;
+  L.blocks = (s.T + embed::kSortKeys - 1) / embed::kSortKeys;
+  L.slabs = (s.d + embed::kSlab - 1) / embed::kSlab;
+  L.chunks = (s.T + embed::kChunk - 1) / embed::kChunk;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+  L.hist = take(3 * sizeof(int) * (static_cast<size_t>(L.blocks) << L.bits));
+  L.keys = take(2 * sizeof(uint2) * static_cast<size_t>(s.T));
+  const size_t part = L.chunks > 1 ? sizeof(float) * static_cast<size_t>(L.chunks) * L.slabs * embed::kSlab : 0;
+  L.head = take(part);
+  L.tail = take(part);
+  L.total = off;
+  return L;
+}
+
+template <class T, bool VEC>
+cudaError_t launch_embed_sum(const T* dy, const embed::SumParams& p, int zero_blocks, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(embed::embed_sum_kernel<T, VEC>, dim3(p.sum_blocks + zero_blocks), dim3(256), 0, st, dy, p);
+  if (e != cudaSuccess || p.chunks < 2) return e;
+  return launch_pdl(embed::embed_join_kernel<VEC>, dim3(p.sum_blocks), dim3(256), 0, st, p);
+}
+
+// ------------------------------------------------------------------------------------------------ norms
+struct NormLayout {
+  int W, G, threads;             // warps per row, rows per block, threads per block
+};
+
+NormLayout norm_layout(int d) {
+  NormLayout L;
+  L.W = (d + 255) / 256;
+  L.G = L.W >= 16 ? 1 : 16 / L.W;
+  L.threads = L.W * L.G * 32;
+  return L;
+}
+
+// Persistent blocks of the backward kernel.
+int norm_bwd_blocks(const cpmtp_norm_args& a, const NormLayout& L, int sms) {
+  const long long rows = (static_cast<long long>(a.N) + L.G - 1) / L.G;
+  return static_cast<int>(rows < sms ? rows : sms);
+}
+
+int check_rows(const cpmtp_rows& r, int d, size_t bytes) {
+  if (r.data == nullptr) return CPMTP_ERR_NULL;
+  if (r.ld < d) return CPMTP_ERR_SHAPE;
+  return aligned(r.data, bytes) ? CPMTP_OK : CPMTP_ERR_ALIGN;
+}
+
+int check_norm(const cpmtp_norm_args* a) {
+  if (a == nullptr) return CPMTP_ERR_NULL;
+  if (a->N < 0 || a->d < 1 || !known_type(a->stream_type)) return CPMTP_ERR_SHAPE;
+  if (a->d > CPMTP_NORM_MAX_D) return CPMTP_ERR_LIMIT;
+  if (a->gate_kind < CPMTP_GATE_NONE || a->gate_kind > CPMTP_GATE_CHANNEL) return CPMTP_ERR_SHAPE;
+  if (!(a->eps > 0.f) || !std::isfinite(a->eps) || !std::isfinite(a->res_scale)) return CPMTP_ERR_SHAPE;
+  if (a->N > 0 && a->block.data == nullptr) {      // (without rows a block may have no address)
+    // a norm alone: nothing to gate, to scale or to norm before the addition
+    if (a->gate_kind != CPMTP_GATE_NONE || a->w_post != nullptr || a->res_scale != 1.f) return CPMTP_ERR_SHAPE;
+    if (a->w_pre == nullptr) return CPMTP_ERR_NULL;
+  }
+  return CPMTP_OK;
+}
+
+int check_gate(const cpmtp_norm_args& a, const cpmtp_rows& g) {
+  if (a.gate_kind == CPMTP_GATE_CHANNEL) return check_rows(g, a.d, 2);
+  return a.gate_kind == CPMTP_GATE_ROW ? check_rows(g, 1, 2) : CPMTP_OK;
+}
+
+template <class S>
+norm::Params<S> norm_params(const cpmtp_norm_args& a, const NormLayout& L) {
+  norm::Params<S> p;
+  std::memset(&p, 0, sizeof(p));
+  p.N = a.N; p.d = a.d; p.W = L.W; p.G = L.G; p.gate_kind = a.gate_kind;
+  p.eps = a.eps; p.res_scale = a.res_scale; p.inv_d = 1.f / static_cast<float>(a.d);
+  p.x = {static_cast<const S*>(a.x.data), a.x.ld};
+  p.block = {static_cast<const bf16_t*>(a.block.data), a.block.ld};
+  p.gate = {static_cast<const bf16_t*>(a.gate.data), a.gate.ld};
+  p.w_post = static_cast<const bf16_t*>(a.w_post);
+  p.w_pre = static_cast<const bf16_t*>(a.w_pre);
+  p.x_out = {static_cast<S*>(a.x_out.data), a.x_out.ld};
+  p.y = {static_cast<bf16_t*>(a.y.data), a.y.ld};
+  p.rstd_post = a.rstd_post; p.rstd_pre = a.rstd_pre;
+  p.dy = {static_cast<const bf16_t*>(a.dy.data), a.dy.ld};
+  p.dx_out = {static_cast<const S*>(a.dx_out.data), a.dx_out.ld};
+  p.dx = {static_cast<S*>(a.dx.data), a.dx.ld};
+  p.dblock = {static_cast<bf16_t*>(a.dblock.data), a.dblock.ld};
+  p.dgate = {static_cast<bf16_t*>(a.dgate.data), a.dgate.ld};
+  return p;
+}
+
+template <class T>
+bool rows_vec(const cpmtp_rows& r, int d) { return r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d); }
+
+template <class S, int MAXT>
+cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, cudaStream_t st) {
+  const norm::Params<S> p = norm_params<S>(a, L);
+  const bool vec = rows_vec<S>(a.x, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.y, a.d) &&
+                   (a.gate_kind != CPMTP_GATE_CHANNEL || rows_vec<bf16_t>(a.gate, a.d)) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
+  const dim3 grid(static_cast<unsigned>((static_cast<long long>(a.N) + L.G - 1) / L.G));
+  if (vec) return launch_pdl(norm::norm_fwd_kernel<S, true, MAXT>, grid, dim3(L.threads), 0, st, p);
+  return launch_pdl(norm::norm_fwd_kernel<S, false, MAXT>, grid, dim3(L.threads), 0, st, p);
+}
+
+template <class S, bool VEC, int MAXT>
+cudaError_t launch_norm_bwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
+  static bool attr_set[64] = {};
+  size_t smem = L.G > 1 ? 2 * 8 * sizeof(float) * L.threads : 0;             // the block's sums; before them the rows ahead
+  const size_t ahead = static_cast<size_t>(norm::kStages) * norm::Slots<S>::kCount * 16 * L.threads;
+  if (VEC && ahead > smem) smem = ahead;
+  constexpr int most = norm::kStages * norm::Slots<S>::kCount * 16 * MAXT;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lock(g_cache_mutex);
+    if (!attr_set[dev]) {
+      const cudaError_t e = cudaFuncSetAttribute(norm::norm_bwd_kernel<S, VEC, MAXT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+      if (e != cudaSuccess) return e;
+      attr_set[dev] = true;
+    }
+  }
+  return launch_pdl(norm::norm_bwd_kernel<S, VEC, MAXT>, dim3(blocks), dim3(L.threads), smem, st, p);
+}
+
+template <class S, int MAXT>
+cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int blocks, float* part, cudaStream_t st) {
+  norm::Params<S> p = norm_params<S>(a, L);
+  p.part = part;
+  const bool channel = a.gate_kind == CPMTP_GATE_CHANNEL;
+  const bool vec = rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<bf16_t>(a.dy, a.d) && rows_vec<S>(a.dx_out, a.d) &&
+                   rows_vec<S>(a.dx, a.d) && rows_vec<bf16_t>(a.dblock, a.d) &&
+                   (!channel || (rows_vec<bf16_t>(a.gate, a.d) && rows_vec<bf16_t>(a.dgate, a.d))) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
+  if (vec) return launch_norm_bwd_as<S, true, MAXT>(p, L, blocks, st);
+  return launch_norm_bwd_as<S, false, MAXT>(p, L, blocks, st);
+}
+
+// ---------------------------------------------------------------------------------------------- optimiser
+int check_grads(const cpmtp_adamw_tensor* tensors, int32_t count) {
+  if (count < 0) return CPMTP_ERR_SHAPE;
+  if (count > 0 && tensors == nullptr) return CPMTP_ERR_NULL;
+  for (int i = 0; i < count; ++i) {
+    const cpmtp_adamw_tensor& t = tensors[i];
+    if (t.numel < 0 || t.numel >= (1ll << 40) || !known_type(t.grad_type)) return CPMTP_ERR_SHAPE;
+    if (!aligned(t.grad, type_bytes(t.grad_type))) return CPMTP_ERR_ALIGN;
+  }
+  return CPMTP_OK;
+}
+
+int check_adamw(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* h) {
+  if (h == nullptr) return CPMTP_ERR_NULL;
+  const bool betas = h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0;
+  if (!betas || !(h->lr >= 0.0) || !(h->eps >= 0.0) || !(h->weight_decay >= 0.0)) return CPMTP_ERR_SHAPE;
+  if (!std::isfinite(h->lr) || !std::isfinite(h->eps) || !std::isfinite(h->weight_decay)) return CPMTP_ERR_SHAPE;
+  if (h->step < 1 || (h->state_bits != 32 && h->state_bits != 8)) return CPMTP_ERR_SHAPE;
+  if (!aligned(h->coef, 4)) return CPMTP_ERR_ALIGN;
+  const int rc = check_grads(tensors, count);
+  if (rc != CPMTP_OK) return rc;
+  for (int i = 0; i < count; ++i) {
+    const cpmtp_adamw_tensor& t = tensors[i];
+    if (!known_type(t.param_type) || (t.master != nullptr && t.param_type != CPMTP_BF16)) return CPMTP_ERR_SHAPE;
+    if (!std::isfinite(t.lr_scale) || !std::isfinite(t.decay_scale)) return CPMTP_ERR_SHAPE;
+    if (t.grad == nullptr || t.numel == 0) continue;
+    if (!t.param || !t.m || !t.v) return CPMTP_ERR_NULL;
+    if (h->state_bits == 8 && (!t.m_exp || !t.v_exp)) return CPMTP_ERR_NULL;
+    const size_t state = h->state_bits == 8 ? 1 : 4;
+    if (!aligned(t.param, type_bytes(t.param_type)) || !aligned(t.master, 4) || !aligned(t.m, state) || !aligned(t.v, state))
+      return CPMTP_ERR_ALIGN;
+  }
+  return CPMTP_OK;
+}
+
+// Launches over tables of at most CAP tensors; `fn(table, runs)` enqueues one of them.
+template <int CAP, class Fill, class Fn>
+int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hyper& h, Fill fill, Fn fn) {
+  adamw::Table<CAP> tab;
+  tab.h = h;
+  tab.count = 0;
+  long long place = 0, runs = 0;
+  constexpr long long kMaxRuns = 1ll << 30;
+  for (int i = 0; i < count; ++i) {
+    const cpmtp_adamw_tensor& t = tensors[i];
+    const long long here = place;
+    place += (t.numel + adamw::kBlock - 1) / adamw::kBlock * adamw::kBlock;
+    if (t.grad == nullptr || t.numel == 0) continue;
+    const long long more = (t.numel + adamw::kRun - 1) / adamw::kRun;
+    if (tab.count == CAP || runs + more > kMaxRuns) {
+      const int rc = fn(tab, static_cast<int>(runs));
+      if (rc != CPMTP_OK) return rc;
+      tab.count = 0;
+      runs = 0;
+    }
+    tab.first[tab.count] = static_cast<int>(runs);
+    fill(t, here, tab.t[tab.count]);
+    ++tab.count;
+    runs += more;
+  }
+  return tab.count > 0 ? fn(tab, static_cast<int>(runs)) : CPMTP_OK;
+}
+
+template <int CAP>
+int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, cudaStream_t st) {
+  adamw::Hyper h;
+  h.b1 = static_cast<float>(hyper.beta1);
+  h.omb1 = static_cast<float>(1.0 - hyper.beta1);
+  h.b2 = static_cast<float>(hyper.beta2);
+  h.omb2 = static_cast<float>(1.0 - hyper.beta2);
+  const double t = static_cast<double>(hyper.step);
+  const double bc1 = 1.0 - std::pow(hyper.beta1, t), bc2 = 1.0 - std::pow(hyper.beta2, t);
+  h.rsqrt_bc2 = static_cast<float>(1.0 / std::sqrt(bc2));
+  h.eps = static_cast<float>(hyper.eps);
+  h.key = adamw::mix(adamw::mix(hyper.seed) ^ static_cast<uint32_t>(hyper.step));
+  h.coef = hyper.coef;
+  const size_t state = hyper.state_bits == 8 ? 8 : 32;
+  return for_tables<CAP>(
+      tensors, count, h,
+      [&](const cpmtp_adamw_tensor& in, long long place, adamw::Tensor& out) {
+        out.param = in.param; out.grad = in.grad; out.master = in.master;
+        out.m = in.m; out.v = in.v; out.m_exp = in.m_exp; out.v_exp = in.v_exp;
+        out.numel = in.numel; out.place = place;
+        out.step_size = static_cast<float>(hyper.lr * in.lr_scale / bc1);
+        out.keep = static_cast<float>(1.0 - hyper.lr * in.lr_scale * hyper.weight_decay * in.decay_scale);
+        out.param_f32 = in.param_type == CPMTP_F32; out.grad_f32 = in.grad_type == CPMTP_F32;
+        out.vec = aligned(in.param, 8 * type_bytes(in.param_type)) && aligned(in.grad, 8 * type_bytes(in.grad_type)) &&
+                  aligned(in.master, 32) && aligned(in.m, state) && aligned(in.v, state);
+      },
+      [&](const adamw::Table<CAP>& tab, int runs) -> int {
+        ProfScope prof(CPMTP_STAGE_ADAMW, st);
+        if (hyper.state_bits == 8) CPMTP_TRY(launch_pdl(adamw::adamw_kernel<8, CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
+        else CPMTP_TRY(launch_pdl(adamw::adamw_kernel<32, CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
+        return CPMTP_OK;
+      });
+}
+
+int grad_blocks(int sms) { return 4 * sms; }
+
+template <int CAP>
+int grad_squares(const cpmtp_adamw_tensor* tensors, int32_t count, int sms, double* part, int* parts, cudaStream_t st) {
+  adamw::Hyper h = {};
+  return for_tables<CAP>(
+      tensors, count, h,
+      [&](const cpmtp_adamw_tensor& in, long long, adamw::Tensor& out) {
+        std::memset(&out, 0, sizeof(out));
+        out.grad = in.grad; out.numel = in.numel; out.grad_f32 = in.grad_type == CPMTP_F32;
+        out.vec = aligned(in.grad, 8 * type_bytes(in.grad_type));
+      },
+      [&](const adamw::Table<CAP>& tab, int runs) -> int {
+        const int blocks = runs < grad_blocks(sms) ? runs : grad_blocks(sms);
+        CPMTP_TRY(launch_pdl(adamw::grad_square_kernel<CAP>, dim3(blocks), dim3(adamw::kThreads), 0, st, tab, runs, part + *parts));
+        *parts += blocks;
+        return CPMTP_OK;
+      });
+}
+
+}  // namespace
+}  // namespace cpmtp
+
+using namespace cpmtp;
+
+extern "C" {
+
+int cpmtp_embed_forward(const cpmtp_embed_shape* shape, const void* E, const int32_t* x, void* out,
+                        int32_t* dev_status, cpmtp_stream stream) {
+  const int rc = check_embed(shape);
+  if (rc != CPMTP_OK) return rc;
+  const cpmtp_embed_shape& s = *shape;
+  if (s.T == 0) return CPMTP_OK;
+  if (!E || !x || !out) return CPMTP_ERR_NULL;
+  if (!aligned(E, 2) || !aligned(x, 4) || !aligned(out, type_bytes(s.type)) || !aligned(dev_status, 4)) return CPMTP_ERR_ALIGN;
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const bf16_t* table = static_cast<const bf16_t*>(E);
+  const int slabs = (s.d + embed::kSlab - 1) / embed::kSlab;
+  const long long items = (static_cast<long long>(s.T) + embed::kFwdRows - 1) / embed::kFwdRows * slabs;
+  const long long blocks = (items + 7) / 8;
+  if (blocks > 2147483647ll) return CPMTP_ERR_LIMIT;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  ProfScope prof(CPMTP_STAGE_EMBED, st);
+  auto launch = [&](auto kernel, auto* to) {
+    return launch_pdl(kernel, grid, dim3(256), 0, st, table, s.ld_table, x, to, s.ld_rows, s.T, s.V, s.d, slabs, s.scale, dev_status);
+  };
+  const bool table_vec = io::vec_ok<bf16_t>(E, s.ld_table, s.d);
+  if (s.type == CPMTP_F32) {
+    float* to = static_cast<float*>(out);
+    if (table_vec && io::vec_ok<float>(out, s.ld_rows, s.d)) CPMTP_TRY(launch(embed::embed_fwd_kernel<float, true>, to));
+    else CPMTP_TRY(launch(embed::embed_fwd_kernel<float, false>, to));
+  } else {
+    bf16_t* to = static_cast<bf16_t*>(out);
+    if (table_vec && io::vec_ok<bf16_t>(out, s.ld_rows, s.d)) CPMTP_TRY(launch(embed::embed_fwd_kernel<bf16_t, true>, to));
+    else CPMTP_TRY(launch(embed::embed_fwd_kernel<bf16_t, false>, to));
+  }
+  return CPMTP_OK;
+}
+
+size_t cpmtp_embed_workspace_bytes(const cpmtp_embed_shape* shape) {
+  return check_embed(shape) == CPMTP_OK ? embed_layout(*shape).total : 0;
+}
+
+int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const int32_t* x, void* dE,
+                         void* workspace, size_t workspace_bytes, int32_t* dev_status, cpmtp_stream stream) {
+  const int rc = check_embed(shape);
+  if (rc != CPMTP_OK) return rc;
+  const cpmtp_embed_shape& s = *shape;
+  const bool accum = (s.flags & CPMTP_FLAG_ACCUM_GRADS) != 0;
+  if (s.T == 0 && accum) return CPMTP_OK;
+  const EmbedLayout L = embed_layout(s);
+  if (!dE || (s.T > 0 && (!dy || !x || !workspace))) return CPMTP_ERR_NULL;
+  if (!aligned(dE, 2) || !aligned(x, 4) || !aligned(dy, type_bytes(s.type)) || !aligned(workspace, kAlign) || !aligned(dev_status, 4))
+    return CPMTP_ERR_ALIGN;
+  if (s.T > 0 && workspace_bytes < L.total) return CPMTP_ERR_WORKSPACE;
+  const long long sum_blocks = (static_cast<long long>(L.chunks) * L.slabs + 7) / 8;
+  const int zero_blocks = accum ? 0 : (s.V + embed::kZeroRows - 1) / embed::kZeroRows;
+  if (sum_blocks + zero_blocks > 2147483647ll) return CPMTP_ERR_LIMIT;
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  ProfScope prof(CPMTP_STAGE_EMBED_GRAD, st);
+  const uint2* sorted = nullptr;
+  if (s.T > 0) {
+    int* hist[3];
+    for (int j = 0; j < 3; ++j) hist[j] = reinterpret_cast<int*>(ws + L.hist) + j * (static_cast<size_t>(L.blocks) << L.bits);
+    uint2* keys[2] = {reinterpret_cast<uint2*>(ws + L.keys), reinterpret_cast<uint2*>(ws + L.keys) + s.T};
+    const dim3 grid(L.blocks), threads(embed::kSortThreads);
+    CPMTP_TRY(launch_pdl(embed::embed_hist_kernel, grid, threads, 0, st, x, s.T, s.V, L.bits, hist[0], L.passes > 1 ? hist[1] : nullptr,
+                         dev_status));
+    for (int pass = 0; pass < L.passes; ++pass) {
+      int* next = pass + 1 < L.passes ? hist[(pass + 1) % 3] : nullptr;
+      int* zero = pass + 2 < L.passes ? hist[(pass + 2) % 3] : nullptr;
+      if (pass == 0)
+        CPMTP_TRY(launch_pdl(embed::embed_sort_kernel<true>, grid, threads, 0, st, x, nullptr, keys[0], s.T, s.V, L.bits, 0, hist[0], next, zero));
+      else
+        CPMTP_TRY(launch_pdl(embed::embed_sort_kernel<false>, grid, threads, 0, st, nullptr, keys[(pass + 1) % 2], keys[pass % 2], s.T, s.V,
+                             L.bits, pass * L.bits, hist[pass % 3], next, zero));
+    }
+    sorted = keys[(L.passes + 1) % 2];
+  }
+  embed::SumParams p;
+  p.sorted = sorted; p.ld = s.ld_rows; p.ld_table = s.ld_table; p.dE = static_cast<bf16_t*>(dE);
+  p.head = reinterpret_cast<float*>(ws + L.head); p.tail = reinterpret_cast<float*>(ws + L.tail);
+  p.tokens = s.T; p.V = s.V; p.d = s.d; p.slabs = L.slabs; p.chunks = L.chunks; p.accum = accum;
+  p.sum_blocks = static_cast<int>(sum_blocks); p.scale = s.scale;
+  const bool table_vec = io::vec_ok<bf16_t>(dE, s.ld_table, s.d);
+  if (s.type == CPMTP_F32) {
+    const float* from = static_cast<const float*>(dy);
+    if (table_vec && io::vec_ok<float>(dy, s.ld_rows, s.d)) CPMTP_TRY((launch_embed_sum<float, true>(from, p, zero_blocks, st)));
+    else CPMTP_TRY((launch_embed_sum<float, false>(from, p, zero_blocks, st)));
+  } else {
+    const bf16_t* from = static_cast<const bf16_t*>(dy);
+    if (table_vec && io::vec_ok<bf16_t>(dy, s.ld_rows, s.d)) CPMTP_TRY((launch_embed_sum<bf16_t, true>(from, p, zero_blocks, st)));
+    else CPMTP_TRY((launch_embed_sum<bf16_t, false>(from, p, zero_blocks, st)));
+  }
+  return CPMTP_OK;
+}
+
+int cpmtp_norm_forward(const cpmtp_norm_args* args, cpmtp_stream stream) {
+  int rc = check_norm(args);
+  if (rc != CPMTP_OK) return rc;
+  const cpmtp_norm_args& a = *args;
+  if (a.N == 0) return CPMTP_OK;
+  const size_t sb = type_bytes(a.stream_type);
+  if ((rc = check_rows(a.x, a.d, sb)) != CPMTP_OK) return rc;
+  if (a.block.data != nullptr) {
+    if ((rc = check_rows(a.block, a.d, 2)) != CPMTP_OK || (rc = check_rows(a.x_out, a.d, sb)) != CPMTP_OK || (rc = check_gate(a, a.gate)) != CPMTP_OK)
+      return rc;
+  }
+  if (a.w_pre != nullptr && (rc = check_rows(a.y, a.d, 2)) != CPMTP_OK) return rc;
+  if (!aligned(a.w_post, 2) || !aligned(a.w_pre, 2) || !aligned(a.rstd_post, 4) || !aligned(a.rstd_pre, 4)) return CPMTP_ERR_ALIGN;
+  DeviceInfo* di = nullptr;
+  if ((rc = check_device(&di)) != CPMTP_OK) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const NormLayout L = norm_layout(a.d);
+  ProfScope prof(CPMTP_STAGE_NORM, st);
+  if (L.threads > 512) {
+    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_fwd<float, 1024>(a, L, st)));
+    else CPMTP_TRY((launch_norm_fwd<bf16_t, 1024>(a, L, st)));
+  } else {
+    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_fwd<float, 512>(a, L, st)));
+    else CPMTP_TRY((launch_norm_fwd<bf16_t, 512>(a, L, st)));
+  }
+  return CPMTP_OK;
+}
+
+size_t cpmtp_norm_workspace_bytes(const cpmtp_norm_args* args) {
+  if (check_norm(args) != CPMTP_OK) return 0;
+  DeviceInfo* di = device_info();
+  const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
+  const NormLayout L = norm_layout(args->d);
+  return align_up(2 * sizeof(float) * static_cast<size_t>(norm_bwd_blocks(*args, L, sms)) * args->d + kAlign);
+}
+
+int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t workspace_bytes, cpmtp_stream stream) {
+  int rc = check_norm(args);
+  if (rc != CPMTP_OK) return rc;
+  const cpmtp_norm_args& a = *args;
+  const bool has_block = a.block.data != nullptr, has_y = a.dy.data != nullptr, has_post = has_block && a.w_post != nullptr;
+  const bool accum = (a.flags & CPMTP_FLAG_ACCUM_GRADS) != 0;
+  if (!aligned(a.w_post, 2) || !aligned(a.w_pre, 2) || !aligned(a.rstd_post, 4) || !aligned(a.rstd_pre, 4) || !aligned(a.dw_post, 2) ||
+      !aligned(a.dw_pre, 2) || !aligned(workspace, kAlign))
+    return CPMTP_ERR_ALIGN;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  DeviceInfo* di = nullptr;
+  if (a.N == 0) {
+    if (accum || (!a.dw_post && !a.dw_pre)) return CPMTP_OK;
+    if ((rc = check_device(&di)) != CPMTP_OK) return rc;
+    if (a.dw_post) CPMTP_TRY(cudaMemsetAsync(a.dw_post, 0, 2ull * a.d, st));
+    if (a.dw_pre) CPMTP_TRY(cudaMemsetAsync(a.dw_pre, 0, 2ull * a.d, st));
+    return CPMTP_OK;
+  }
+  if (!a.dx.data && !a.dblock.data && !a.dgate.data && !a.dw_post && !a.dw_pre) return CPMTP_ERR_NULL;   // nothing asked for
+  if (a.dw_post && !has_post) return CPMTP_ERR_NULL;
+  if (a.dw_pre && !has_y) return CPMTP_ERR_NULL;
+  const size_t sb = type_bytes(a.stream_type);
+  if ((rc = check_rows(a.x_out, a.d, sb)) != CPMTP_OK) return rc;
+  if (has_y && (!a.w_pre || !a.rstd_pre)) return CPMTP_ERR_NULL;
+  if (has_post && !a.rstd_post) return CPMTP_ERR_NULL;
+  if (!has_y && !a.dx_out.data) return CPMTP_ERR_NULL;          // no gradient comes in
+  if (has_y && (rc = check_rows(a.dy, a.d, 2)) != CPMTP_OK) return rc;
+  if (a.dx_out.data && (rc = check_rows(a.dx_out, a.d, sb)) != CPMTP_OK) return rc;
+  if (a.dx.data && (rc = check_rows(a.dx, a.d, sb)) != CPMTP_OK) return rc;
+  if (has_block && ((rc = check_rows(a.block, a.d, 2)) != CPMTP_OK || (rc = check_gate(a, a.gate)) != CPMTP_OK)) return rc;
+  if (a.dblock.data) {
+    if (!has_block) return CPMTP_ERR_NULL;
+    if ((rc = check_rows(a.dblock, a.d, 2)) != CPMTP_OK) return rc;
+  }
+  if (a.dgate.data) {
+    if (a.gate_kind == CPMTP_GATE_NONE) return CPMTP_ERR_NULL;
+    if ((rc = check_gate(a, a.dgate)) != CPMTP_OK) return rc;
+  }
+  if ((rc = check_device(&di)) != CPMTP_OK) return rc;
+  const NormLayout L = norm_layout(a.d);
+  const int blocks = norm_bwd_blocks(a, L, di->sms);
+  float* part = nullptr;
+  if (a.dw_post || a.dw_pre) {
+    if (!workspace) return CPMTP_ERR_NULL;
+    if (workspace_bytes < cpmtp_norm_workspace_bytes(args)) return CPMTP_ERR_WORKSPACE;
+    part = static_cast<float*>(workspace);
+  }
+  ProfScope prof(CPMTP_STAGE_NORM_GRAD, st);
+  if (L.threads > 512) {
+    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_bwd<float, 1024>(a, L, blocks, part, st)));
+    else CPMTP_TRY((launch_norm_bwd<bf16_t, 1024>(a, L, blocks, part, st)));
+  } else {
+    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_bwd<float, 512>(a, L, blocks, part, st)));
+    else CPMTP_TRY((launch_norm_bwd<bf16_t, 512>(a, L, blocks, part, st)));
+  }
+  if (part != nullptr)
+    CPMTP_TRY(launch_pdl(norm::norm_dw_kernel, dim3((a.d + 31) / 32, 2), dim3(1024), 0, st, part, blocks, a.d, static_cast<bf16_t*>(a.dw_post),
+                         static_cast<bf16_t*>(a.dw_pre), accum ? 1 : 0));
+  return CPMTP_OK;
+}
+
+int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
+                     cpmtp_stream stream) {
+  const int rc = check_adamw(tensors, count, hyper);
+  if (rc != CPMTP_OK) return rc;
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  return count <= adamw::kSmallTable ? adamw_step<adamw::kSmallTable>(tensors, count, *hyper, st)
+                                     : adamw_step<adamw::kLargeTable>(tensors, count, *hyper, st);
+}
+
+int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,
+                             cpmtp_stream stream) {
+  if (n < 0 || n >= (1ll << 40)) return CPMTP_ERR_SHAPE;
+  if (n == 0) return CPMTP_OK;
+  if (!codes || !exps || !out_bf16) return CPMTP_ERR_NULL;
+  if (!aligned(out_bf16, 2)) return CPMTP_ERR_ALIGN;
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const dim3 grid(static_cast<unsigned>((n + 8 * adamw::kBlock - 1) / (8 * adamw::kBlock)));
+  const int vec = aligned(codes, 8) && aligned(out_bf16, 16);
+  const uint8_t* c = static_cast<const uint8_t*>(codes);
+  bf16_t* out = static_cast<bf16_t*>(out_bf16);
+  ProfScope prof(CPMTP_STAGE_ADAMW, st);
+  if (second) CPMTP_TRY(launch_pdl(adamw::state_values_kernel<true>, grid, dim3(adamw::kThreads), 0, st, c, exps, n, out, vec));
+  else CPMTP_TRY(launch_pdl(adamw::state_values_kernel<false>, grid, dim3(adamw::kThreads), 0, st, c, exps, n, out, vec));
+  return CPMTP_OK;
+}
+
+size_t cpmtp_grad_norm_workspace_bytes(const cpmtp_adamw_tensor* tensors, int32_t count) {
+  if (check_grads(tensors, count) != CPMTP_OK) return 0;
+  DeviceInfo* di = device_info();
+  const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
+  const size_t launches = count <= adamw::kSmallTable ? 1 : (count + adamw::kLargeTable - 1) / adamw::kLargeTable;
+  return align_up(launches * grad_blocks(sms) * sizeof(double));
+}
+
+int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_norm, float* norm, float* coef,
+                    void* workspace, size_t workspace_bytes, cpmtp_stream stream) {
+  const int rc = check_grads(tensors, count);
+  if (rc != CPMTP_OK) return rc;
+  if (!(max_norm > 0.f)) return CPMTP_ERR_SHAPE;
+  if (!workspace || (!norm && !coef)) return CPMTP_ERR_NULL;
+  if (!aligned(workspace, kAlign) || !aligned(norm, 4) || !aligned(coef, 4)) return CPMTP_ERR_ALIGN;
+  if (workspace_bytes < cpmtp_grad_norm_workspace_bytes(tensors, count)) return CPMTP_ERR_WORKSPACE;
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  double* part = static_cast<double*>(workspace);
+  int parts = 0;
+  ProfScope prof(CPMTP_STAGE_GRAD_NORM, st);
+  const int rs = count <= adamw::kSmallTable ? grad_squares<adamw::kSmallTable>(tensors, count, di->sms, part, &parts, st)
+                                             : grad_squares<adamw::kLargeTable>(tensors, count, di->sms, part, &parts, st);
+  if (rs != CPMTP_OK) return rs;
+  CPMTP_TRY(launch_pdl(adamw::grad_norm_kernel, dim3(1), dim3(adamw::kThreads), 0, st, part, parts, max_norm, norm, coef));
+  return CPMTP_OK;
+}
+
+}  // extern "C"
