@@ -9,6 +9,8 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -143,7 +145,7 @@ def load_library() -> ctypes.CDLL:
     lib.cpmtp_distill_backward.restype = ctypes.c_int
     lib.cpmtp_distill_backward.argtypes = [shp, vp, vp, vp, vp, i32p, vp, svp, dsp, ctypes.c_float, ctypes.c_float,
                                            fp, fp, vp, vp, vp, vp, vp, sz, i32p, vp]
-    esp, nap, atp = ctypes.POINTER(CEmbedShape), ctypes.POINTER(CNormArgs), ctypes.POINTER(CAdamWTensor)
+    esp, nap, atp = ctypes.POINTER(CEmbedShape), ctypes.POINTER(CNormArgs), vp   # atp: an array's address
     lib.cpmtp_embed_forward.restype = ctypes.c_int
     lib.cpmtp_embed_forward.argtypes = [esp, vp, i32p, vp, i32p, vp]
     lib.cpmtp_embed_workspace_bytes.restype = sz
@@ -627,64 +629,86 @@ def distill_backward(h, W_head, E, W_g, x, teacher, saved: Saved, dsaved: Distil
 # Around the head in a training step: embedding lookup, norms with gate and residual addition, AdamW.
 
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_ADAMW_WORDS = ctypes.sizeof(CAdamWTensor) // 8      # a descriptor in 8-byte words: param, grad, master, m, v, m_exp, v_exp, numel, types, factors
 
+
+# The checks below run before every launch and cost a few hundred nanoseconds each, so they test first and put the
+# message together only when there is something to say.
 
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise CpmtpError(f"cpmtp: {what}")
 
 
-def _on_device(ref: torch.Tensor, **tensors) -> None:
-    """Every tensor that is given lies on `ref`'s device, which is the current one (its current stream is used)."""
-    _need(ref.is_cuda and ref.device.index == torch.cuda.current_device(), "tensors must be on the current CUDA device")
-    for name, t in tensors.items():
-        _need(t is None or t.device == ref.device, f"{name} is on another device")
+def _device(ref: torch.Tensor) -> int:
+    """Index of `ref`'s device, which has to be the current one: its current stream is used."""
+    dev = ref.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise CpmtpError("cpmtp: tensors must be on the current CUDA device")
+    return dev
 
 
-def _rows(t: torch.Tensor, n: int, d: int, dtype, name: str) -> tuple:
-    """(pointer, row stride) of an [n, d] matrix whose rows are contiguous."""
-    _need(t.dim() == 2 and t.shape[0] == n and t.shape[1] == d, f"{name} must be [{n}, {d}]")
-    _need(t.dtype == dtype, f"{name} must be {dtype}")
-    ld = t.stride(0) if n > 1 else d
-    _need(d <= 1 or t.stride(1) == 1, f"{name}: the elements of a row must be contiguous")
-    _need(ld >= d, f"{name}: rows must not overlap")
+def _raw_stream(dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _rows(t: torch.Tensor, size: tuple, dtype, dev: int, name: str) -> tuple:
+    """(pointer, row stride) of a matrix [n, d] = size whose rows are contiguous and do not overlap."""
+    if t.shape != size or t.dtype is not dtype:
+        raise CpmtpError(f"cpmtp: {name} must be {list(size)} {dtype}, not {list(t.shape)} {t.dtype}")
+    if t.get_device() != dev:
+        raise CpmtpError(f"cpmtp: {name} is on another device")
+    ld, one = t.stride()
+    n, d = size
+    if n <= 1:
+        ld = d
+    if (one != 1 and d > 1) or ld < d:
+        raise CpmtpError(f"cpmtp: {name}: the elements of a row must be contiguous and rows must not overlap")
     return t.data_ptr(), ld
 
 
-def _vector(t: torch.Tensor, n: int, dtype, name: str) -> int:
-    _need(t.dim() == 1 and t.shape[0] == n and t.dtype == dtype and (n <= 1 or t.stride(0) == 1), f"{name} must be a contiguous [{n}] {dtype}")
+def _vector(t: torch.Tensor, n: int, dtype, dev: int, name: str) -> int:
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise CpmtpError(f"cpmtp: {name} must be a contiguous [{n}] {dtype} on the same device")
     return t.data_ptr()
 
 
-def _check_status(dev_status: Optional[torch.Tensor]) -> None:
-    _need(dev_status is None or (dev_status.dtype == torch.int32 and dev_status.numel() >= 1), "dev_status must be int32 [1]")
+def _int32(t: torch.Tensor, dev: int, name: str) -> int:
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise CpmtpError(f"cpmtp: {name} must be contiguous int32 on the same device")
+    return t.data_ptr()
 
 
-def _check_workspace(workspace: torch.Tensor) -> torch.Tensor:
-    _need(workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace must be contiguous uint8")
-    return workspace
+def _workspace(t: torch.Tensor, dev: int) -> tuple:
+    if t.dtype is not torch.uint8 or t.get_device() != dev or not t.is_contiguous():
+        raise CpmtpError("cpmtp: workspace must be contiguous uint8 on the same device")
+    return t.data_ptr(), t.numel()
 
 
 def embed_forward(E: torch.Tensor, x: torch.Tensor, *, scale: float = 1.0, out_dtype: torch.dtype = torch.bfloat16,
                   out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """cpmtp_embed_forward: scale * E[x] for tokens x (any shape, int32, EMBED_PAD = a row of zeros); E [V, d] bf16.
     Returns x.shape + (d,) of `out_dtype` (bf16 or fp32), or `out` ([x.numel(), d], rows may be strided)."""
-    _need(E.dim() == 2 and E.shape[0] >= 1 and E.shape[1] >= 1, "E must be [V, d]")
-    V, d = E.shape
+    dev = _device(E)
+    size = E.shape
+    _need(len(size) == 2, "E must be [V, d]")
+    V, d = size
     T = x.numel()
-    _on_device(E, x=x, out=out, dev_status=dev_status)
-    _need(x.dtype == torch.int32 and x.is_contiguous(), "x must be contiguous int32")
-    _check_status(dev_status)
+    px = _int32(x, dev, "x")
     if out is None:
-        out = torch.empty((*x.shape, d), dtype=out_dtype, device=E.device)
         _need(out_dtype in _TYPES, "out_dtype must be bfloat16 or float32")
+        out = torch.empty((*x.shape, d), dtype=out_dtype, device=E.device)
         po, ldo = out.data_ptr(), d
     else:
-        _need(out.dtype in _TYPES, "out must be bfloat16 or float32")
-        po, ldo = _rows(out, T, d, out.dtype, "out")
-    pe, lde = _rows(E, V, d, torch.bfloat16, "E")
-    shape = CEmbedShape(T, V, d, _TYPES[out.dtype], lde, ldo, scale, 0)
-    _check(load_library().cpmtp_embed_forward(ctypes.byref(shape), pe, x.data_ptr(), po, _ptr(dev_status), _stream()))
+        out_dtype = out.dtype
+        _need(out_dtype in _TYPES, "out must be bfloat16 or float32")
+        po, ldo = _rows(out, (T, d), out_dtype, dev, "out")
+    pe, lde = _rows(E, size, torch.bfloat16, dev, "E")
+    shape = CEmbedShape(T, V, d, _TYPES[out_dtype], lde, ldo, scale, 0)
+    rc = load_library().cpmtp_embed_forward(ctypes.byref(shape), pe, px, po, None if dev_status is None else _int32(dev_status, dev, "dev_status"),
+                                            _raw_stream(dev))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -693,49 +717,64 @@ def embed_backward(dy: torch.Tensor, x: torch.Tensor, V: int, *, scale: float = 
                    dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """cpmtp_embed_backward: dE [V, d] bf16, the scaled sums of the rows of dy (x.shape + (d,), bf16 or fp32; a 2-D dy may
     have strided rows) over equal tokens.  accumulate: add to `out`, touching only the rows that occur."""
+    dev = _device(dy)
     T, d = x.numel(), dy.shape[-1]
-    _on_device(dy, x=x, out=out, dev_status=dev_status, workspace=workspace)
-    _need(x.dtype == torch.int32 and x.is_contiguous(), "x must be contiguous int32")
-    _need(dy.dtype in _TYPES, "dy must be bfloat16 or float32")
-    _check_status(dev_status)
+    px = _int32(x, dev, "x")
+    dtype = dy.dtype
+    _need(dtype in _TYPES, "dy must be bfloat16 or float32")
     if dy.dim() != 2:
-        _need(tuple(dy.shape[:-1]) == tuple(x.shape) and dy.is_contiguous(), "dy must be x.shape + (d,)")
+        _need(dy.shape[:-1] == x.shape and dy.is_contiguous(), "dy must be x.shape + (d,)")
         dy = dy.view(T, d)
-    pd, ldd = _rows(dy, T, d, dy.dtype, "dy")
-    _need(not accumulate or out is not None, "accumulation needs the tensor to add to")
+    pd, ldd = _rows(dy, (T, d), dtype, dev, "dy")
     if out is None:
+        _need(not accumulate, "accumulation needs the tensor to add to")
+        _need(V >= 1, "V must be at least 1")
         out = torch.empty((V, d), dtype=torch.bfloat16, device=dy.device)
-    pe, lde = _rows(out, V, d, torch.bfloat16, "out")
-    shape = CEmbedShape(T, V, d, _TYPES[dy.dtype], lde, ldd, scale, FLAG_ACCUM_GRADS if accumulate else 0)
-    lib = load_library()
+    pe, lde = _rows(out, (V, d), torch.bfloat16, dev, "out")
+    shape = CEmbedShape(T, V, d, _TYPES[dtype], lde, ldd, scale, FLAG_ACCUM_GRADS if accumulate else 0)
+    lib, ref = load_library(), ctypes.byref(shape)
     if workspace is None:
-        workspace = alloc_workspace(int(lib.cpmtp_embed_workspace_bytes(ctypes.byref(shape))), dy.device)
-    _check_workspace(workspace)
-    _check(lib.cpmtp_embed_backward(ctypes.byref(shape), pd, x.data_ptr(), pe, workspace.data_ptr(), workspace.numel(), _ptr(dev_status),
-                                    _stream()))
+        workspace = alloc_workspace(lib.cpmtp_embed_workspace_bytes(ref), dy.device)
+    pw, nw = _workspace(workspace, dev)
+    rc = lib.cpmtp_embed_backward(ref, pd, px, pe, pw, nw, None if dev_status is None else _int32(dev_status, dev, "dev_status"), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return out
 
 
-def _norm_args(ref, w_pre, block, gate, w_post, res_scale, eps) -> CNormArgs:
-    """The inputs that both directions share; `ref` is x or x_out."""
-    _need(ref.dim() == 2 and ref.dtype in _TYPES, "the residual stream must be [N, d] bfloat16 or float32")
-    N, d = ref.shape
-    a = CNormArgs()
-    a.N, a.d, a.stream_type, a.eps, a.res_scale = N, d, _TYPES[ref.dtype], eps, res_scale
+def embed_workspace_bytes(T: int, V: int, d: int) -> int:
+    """Scratch bytes of embed_backward for T tokens and a [V, d] table."""
+    shape = CEmbedShape(T, V, d, BF16, d, d, 1.0, 0)
+    return int(load_library().cpmtp_embed_workspace_bytes(ctypes.byref(shape)))
+
+
+def _row_gate(t: torch.Tensor, n: int, dev: int, name: str) -> tuple:
+    if t.shape != (n,) or t.dtype is not torch.bfloat16 or t.get_device() != dev or (n > 1 and t.stride(0) < 1):
+        raise CpmtpError(f"cpmtp: {name} must be [{n}] bfloat16, or have the rows' shape")
+    return t.data_ptr(), t.stride(0) if n > 1 else 1
+
+
+def _norm_args(ref, dev, w_pre, block, gate, w_post, res_scale, eps) -> tuple:
+    """The arguments that both directions share, and the rows' shape; `ref` is x or x_out."""
+    size, dtype = ref.shape, ref.dtype
+    _need(len(size) == 2 and dtype in _TYPES, "the residual stream must be [N, d] bfloat16 or float32")
+    N, d = size
+    a = CNormArgs(N, d, _TYPES[dtype], GATE_NONE, 0, eps, res_scale)
+    bf16 = torch.bfloat16
     if w_pre is not None:
-        a.w_pre = _vector(w_pre, d, torch.bfloat16, "w_pre")
+        a.w_pre = _vector(w_pre, d, bf16, dev, "w_pre")
     if w_post is not None:
-        a.w_post = _vector(w_post, d, torch.bfloat16, "w_post")
+        a.w_post = _vector(w_post, d, bf16, dev, "w_post")
     if block is not None:
-        a.block, a.ld_block = _rows(block, N, d, torch.bfloat16, "block")
+        a.block, a.ld_block = _rows(block, size, bf16, dev, "block")
     if gate is not None:
         if gate.dim() == 1:
-            _need(gate.shape[0] == N and gate.dtype == torch.bfloat16 and (N <= 1 or gate.stride(0) >= 1), f"gate must be [{N}] or [{N}, {d}] bfloat16")
-            a.gate_kind, a.gate, a.ld_gate = GATE_ROW, gate.data_ptr(), gate.stride(0) if N > 1 else 1
+            a.gate_kind = GATE_ROW
+            a.gate, a.ld_gate = _row_gate(gate, N, dev, "gate")
         else:
             a.gate_kind = GATE_CHANNEL
-            a.gate, a.ld_gate = _rows(gate, N, d, torch.bfloat16, "gate")
-    return a
+            a.gate, a.ld_gate = _rows(gate, size, bf16, dev, "gate")
+    return a, size, dtype
 
 
 def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block: Optional[torch.Tensor] = None,
@@ -746,27 +785,40 @@ def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block
     projection's output).  Without w_post the block is added as it is, without w_pre there is no y, without a block
     x_out is x itself and y its norm.  Returns {"x_out", "y", "rstd_post", "rstd_pre"} (None where there is none);
     tensors given in `out` are written instead of new ones (x_out may be x)."""
-    a = _norm_args(x, w_pre, block, gate, w_post, res_scale, eps)
-    N, d = x.shape
-    res = out if out is not None else {}
-    _on_device(x, w_pre=w_pre, block=block, gate=gate, w_post=w_post, **{f"out[{k}]": v for k, v in res.items()})
-    a.x, a.ld_x = _rows(x, N, d, x.dtype, "x")
-    for name, there, size, dtype in (("x_out", block is not None, (N, d), x.dtype), ("y", w_pre is not None, (N, d), torch.bfloat16),
-                                     ("rstd_post", w_post is not None, (N,), torch.float32), ("rstd_pre", w_pre is not None, (N,), torch.float32)):
-        if not there:
-            res[name] = None
-        elif res.get(name) is None:
-            res[name] = torch.empty(size, dtype=dtype, device=x.device)
+    dev = _device(x)
+    a, size, dtype = _norm_args(x, dev, w_pre, block, gate, w_post, res_scale, eps)
+    a.x, a.ld_x = _rows(x, size, dtype, dev, "x")
+    N = size[0]
+    res = {} if out is None else out
+    device = x.device
     if block is None:
         res["x_out"] = x
     else:
-        a.x_out, a.ld_x_out = _rows(res["x_out"], N, d, x.dtype, "x_out")
-    if w_pre is not None:
-        a.y, a.ld_y = _rows(res["y"], N, d, torch.bfloat16, "y")
-        a.rstd_pre = _vector(res["rstd_pre"], N, torch.float32, "rstd_pre")
-    if res["rstd_post"] is not None:
-        a.rstd_post = _vector(res["rstd_post"], N, torch.float32, "rstd_post")
-    _check(load_library().cpmtp_norm_forward(ctypes.byref(a), _stream()))
+        t = res.get("x_out")
+        if t is None:
+            t = res["x_out"] = torch.empty(size, dtype=dtype, device=device)
+        a.x_out, a.ld_x_out = _rows(t, size, dtype, dev, "x_out")
+    if w_pre is None:
+        res["y"] = res["rstd_pre"] = None
+    else:
+        t = res.get("y")
+        if t is None:
+            t = res["y"] = torch.empty(size, dtype=torch.bfloat16, device=device)
+        a.y, a.ld_y = _rows(t, size, torch.bfloat16, dev, "y")
+        t = res.get("rstd_pre")
+        if t is None:
+            t = res["rstd_pre"] = torch.empty(N, dtype=torch.float32, device=device)
+        a.rstd_pre = _vector(t, N, torch.float32, dev, "rstd_pre")
+    if w_post is None:
+        res["rstd_post"] = None
+    else:
+        t = res.get("rstd_post")
+        if t is None:
+            t = res["rstd_post"] = torch.empty(N, dtype=torch.float32, device=device)
+        a.rstd_post = _vector(t, N, torch.float32, dev, "rstd_post")
+    rc = load_library().cpmtp_norm_forward(ctypes.byref(a), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return res
 
 
@@ -780,60 +832,53 @@ def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Option
     dy [N, d] bf16 (None: no gradient of y), dx_out [N, d] of the stream's type (None: zero).
     Returns {"dx", "dblock", "dgate", "dw_post", "dw_pre"}: None where there is nothing to differentiate or the name is
     in `skip`.  accumulate: dw_post and dw_pre are added to those given in `out`."""
-    a = _norm_args(x_out, w_pre, block, gate, w_post, res_scale, eps)
-    N, d = x_out.shape
-    res = out if out is not None else {}
-    _need(not accumulate or out is not None, "accumulation needs the tensors to add to")
+    dev = _device(x_out)
+    a, size, dtype = _norm_args(x_out, dev, w_pre, block, gate, w_post, res_scale, eps)
+    N, d = size
+    bf16, device = torch.bfloat16, x_out.device
     _need(dy is not None or dx_out is not None, "no gradient comes in: dy and dx_out are both None")
-    _need(dy is None or (w_pre is not None and rstd_pre is not None), "dy needs w_pre and rstd_pre")
-    _need(w_post is None or rstd_post is not None, "w_post needs rstd_post")
-    _on_device(x_out, dy=dy, w_pre=w_pre, rstd_pre=rstd_pre, dx_out=dx_out, block=block, gate=gate, w_post=w_post, rstd_post=rstd_post,
-               workspace=workspace, **{f"out[{k}]": v for k, v in res.items()})
-    a.x_out, a.ld_x_out = _rows(x_out, N, d, x_out.dtype, "x_out")
+    _need(not accumulate or out is not None, "accumulation needs the tensors to add to")
+    a.x_out, a.ld_x_out = _rows(x_out, size, dtype, dev, "x_out")
     if dy is not None:
-        a.dy, a.ld_dy = _rows(dy, N, d, torch.bfloat16, "dy")
-        a.rstd_pre = _vector(rstd_pre, N, torch.float32, "rstd_pre")
+        _need(w_pre is not None and rstd_pre is not None, "dy needs w_pre and rstd_pre")
+        a.dy, a.ld_dy = _rows(dy, size, bf16, dev, "dy")
+        a.rstd_pre = _vector(rstd_pre, N, torch.float32, dev, "rstd_pre")
     if dx_out is not None:
-        a.dx_out, a.ld_dx_out = _rows(dx_out, N, d, x_out.dtype, "dx_out")
-    if rstd_post is not None:
-        a.rstd_post = _vector(rstd_post, N, torch.float32, "rstd_post")
-    dev = x_out.device
-    made = dict(dx=lambda: torch.empty((N, d), dtype=x_out.dtype, device=dev))
-    if block is not None:
-        made["dblock"] = lambda: torch.empty((N, d), dtype=torch.bfloat16, device=dev)
-        if gate is not None:
-            made["dgate"] = lambda: torch.empty(gate.shape, dtype=torch.bfloat16, device=dev)
-        if w_post is not None:
-            made["dw_post"] = lambda: torch.empty(d, dtype=torch.bfloat16, device=dev)
-    if dy is not None:
-        made["dw_pre"] = lambda: torch.empty(d, dtype=torch.bfloat16, device=dev)
-    for name in ("dx", "dblock", "dgate", "dw_post", "dw_pre"):
-        if name in skip or name not in made:
+        a.dx_out, a.ld_dx_out = _rows(dx_out, size, dtype, dev, "dx_out")
+    if w_post is not None:
+        _need(rstd_post is not None, "w_post needs rstd_post")
+        a.rstd_post = _vector(rstd_post, N, torch.float32, dev, "rstd_post")
+    res = {} if out is None else out
+
+    def want(name, there, shape, kind):
+        if not there or name in skip:
             res[name] = None
-        elif res.get(name) is None:
-            _need(not (accumulate and name.startswith("dw")), f"accumulation needs out[{name}]")
-            res[name] = made[name]()
-    if res["dx"] is not None:
-        a.dx, a.ld_dx = _rows(res["dx"], N, d, x_out.dtype, "dx")
-    if res["dblock"] is not None:
-        a.dblock, a.ld_dblock = _rows(res["dblock"], N, d, torch.bfloat16, "dblock")
-    if res["dgate"] is not None:
-        if a.gate_kind == GATE_CHANNEL:
-            a.dgate, a.ld_dgate = _rows(res["dgate"], N, d, torch.bfloat16, "dgate")
-        else:
-            g = res["dgate"]
-            _need(g.dim() == 1 and g.shape[0] == N and g.dtype == torch.bfloat16 and (N <= 1 or g.stride(0) >= 1), f"dgate must be [{N}] bfloat16")
-            a.dgate, a.ld_dgate = g.data_ptr(), g.stride(0) if N > 1 else 1
-    if res["dw_post"] is not None:
-        a.dw_post = _vector(res["dw_post"], d, torch.bfloat16, "dw_post")
-    if res["dw_pre"] is not None:
-        a.dw_pre = _vector(res["dw_pre"], d, torch.bfloat16, "dw_pre")
-    a.flags = FLAG_ACCUM_GRADS if accumulate else 0
-    lib = load_library()
+            return None
+        t = res.get(name)
+        if t is None:
+            _need(not accumulate or name[1] != "w", "accumulation needs dw_post and dw_pre in out")
+            t = res[name] = torch.empty(shape, dtype=kind, device=device)
+        return t
+
+    if (t := want("dx", True, size, dtype)) is not None:
+        a.dx, a.ld_dx = _rows(t, size, dtype, dev, "dx")
+    if (t := want("dblock", block is not None, size, bf16)) is not None:
+        a.dblock, a.ld_dblock = _rows(t, size, bf16, dev, "dblock")
+    if (t := want("dgate", gate is not None, None if gate is None else gate.shape, bf16)) is not None:
+        a.dgate, a.ld_dgate = _rows(t, size, bf16, dev, "dgate") if a.gate_kind == GATE_CHANNEL else _row_gate(t, N, dev, "dgate")
+    if (t := want("dw_post", w_post is not None, (d,), bf16)) is not None:
+        a.dw_post = _vector(t, d, bf16, dev, "dw_post")
+    if (t := want("dw_pre", dy is not None, (d,), bf16)) is not None:
+        a.dw_pre = _vector(t, d, bf16, dev, "dw_pre")
+    if accumulate:
+        a.flags = FLAG_ACCUM_GRADS
+    lib, ref = load_library(), ctypes.byref(a)
     if workspace is None:
-        workspace = alloc_workspace(int(lib.cpmtp_norm_workspace_bytes(ctypes.byref(a))), dev)
-    _check_workspace(workspace)
-    _check(lib.cpmtp_norm_backward(ctypes.byref(a), workspace.data_ptr(), workspace.numel(), _stream()))
+        workspace = alloc_workspace(lib.cpmtp_norm_workspace_bytes(ref), device)
+    pw, nw = _workspace(workspace, dev)
+    rc = lib.cpmtp_norm_backward(ref, pw, nw, _raw_stream(dev))
+    if rc:
+        _check(rc)
     return res
 
 
@@ -844,50 +889,77 @@ def norm_workspace_bytes(N: int, d: int) -> int:
     return int(load_library().cpmtp_norm_workspace_bytes(ctypes.byref(a)))
 
 
-def embed_workspace_bytes(T: int, V: int, d: int) -> int:
-    """Scratch bytes of embed_backward for T tokens and a [V, d] table."""
-    shape = CEmbedShape(T, V, d, BF16, d, d, 1.0, 0)
-    return int(load_library().cpmtp_embed_workspace_bytes(ctypes.byref(shape)))
+class _Descriptors:
+    """An array of cpmtp_adamw_tensor, written a column at a time (a step updates hundreds of them before its one launch)."""
+
+    def __init__(self, n: int):
+        self.n = n
+        self.words = array("q", bytes(8 * _ADAMW_WORDS * n))
+        self.address = self.words.buffer_info()[0]
+
+    def put(self, word: int, values) -> None:
+        if self.n:
+            self.words[word::_ADAMW_WORDS] = array("q", values)
+
+    def put_grads(self, grads, dev: int, param_types: list, numels: Optional[list] = None) -> None:
+        """Addresses and types of the gradients, one per parameter of `numels` elements; None: no address."""
+        at, types, sizes = [], [], []
+        for g, pt in zip(grads, param_types):
+            if g is None:
+                at.append(0)
+                types.append(pt)
+                sizes.append(0)
+                continue
+            t = _TYPES.get(g.dtype)
+            if t is None or g.get_device() != dev or not g.is_contiguous():
+                raise CpmtpError("cpmtp: gradients must be contiguous bfloat16 or float32 tensors on the current CUDA device")
+            at.append(g.data_ptr())
+            types.append(pt | t << 32)
+            sizes.append(g.numel())
+        if numels is None:
+            self.put(7, sizes)
+        elif sizes != numels and any(s != m and g is not None for s, m, g in zip(sizes, numels, grads)):
+            raise CpmtpError("cpmtp: a gradient must have its parameter's size")
+        self.put(1, at)
+        self.put(8, types)
 
 
-def _grad_table(grads) -> ctypes.Array:
-    table = (CAdamWTensor * max(1, len(grads)))()
+def _grad_descriptors(grads) -> tuple:
     ref = next((g for g in grads if g is not None), None)
-    for c, g in zip(table, grads):
-        if g is None:
-            continue
-        _need(g.dtype in _TYPES and g.is_contiguous() and g.is_cuda and g.device == ref.device, "gradients must be contiguous bfloat16 or float32 on one device")
-        c.grad, c.numel, c.grad_type = g.data_ptr(), g.numel(), _TYPES[g.dtype]
-    return table
+    _need(ref is not None, "there is no gradient")
+    dev = _device(ref)
+    table = _Descriptors(len(grads))
+    table.put_grads(grads, dev, [0] * len(grads))
+    return table, dev, ref.device
 
 
 def grad_norm_workspace_bytes(grads) -> int:
-    return int(load_library().cpmtp_grad_norm_workspace_bytes(_grad_table(grads), len(grads)))
+    """Scratch bytes of grad_norm for these gradients."""
+    table, _, _ = _grad_descriptors(grads)
+    return int(load_library().cpmtp_grad_norm_workspace_bytes(table.address, table.n))
 
 
 def grad_norm(grads, *, max_norm: float = float("inf"), workspace: Optional[torch.Tensor] = None, out: Optional[dict] = None) -> dict:
     """cpmtp_grad_norm over a list of gradients (None entries are left out): {"norm", "coef"}, fp32 [1] on the device; coef
     is what AdamW.step takes to clip to max_norm (NaN where the norm is not finite, which skips the step)."""
-    ref = next((g for g in grads if g is not None), None)
-    _need(ref is not None, "there is no gradient")
-    _on_device(ref, workspace=workspace)
-    table = _grad_table(grads)
+    table, dev, device = _grad_descriptors(grads)
     lib = load_library()
     if workspace is None:
-        workspace = alloc_workspace(int(lib.cpmtp_grad_norm_workspace_bytes(table, len(grads))), ref.device)
-    _check_workspace(workspace)
-    res = out if out is not None else {}
+        workspace = alloc_workspace(lib.cpmtp_grad_norm_workspace_bytes(table.address, table.n), device)
+    pw, nw = _workspace(workspace, dev)
+    res = {} if out is None else out
     for name in ("norm", "coef"):
-        if name not in res:
-            res[name] = torch.empty(1, dtype=torch.float32, device=ref.device)
-        _need(res[name].dtype == torch.float32 and res[name].device == ref.device and res[name].numel() >= 1, f"{name} must be float32 [1]")
-    _check(lib.cpmtp_grad_norm(table, len(grads), max_norm, res["norm"].data_ptr(), res["coef"].data_ptr(), workspace.data_ptr(),
-                               workspace.numel(), _stream()))
+        if res.get(name) is None:
+            res[name] = torch.empty(1, dtype=torch.float32, device=device)
+    rc = lib.cpmtp_grad_norm(table.address, table.n, max_norm, _vector(res["norm"], 1, torch.float32, dev, "norm"),
+                             _vector(res["coef"], 1, torch.float32, dev, "coef"), pw, nw, _raw_stream(dev))
+    if rc:
+        _check(rc)
     return res
 
 
 class AdamW:
-    """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch.
+    """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch per 300 tensors.
 
     params: contiguous bf16 or fp32 tensors, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
     one exponent byte per ADAMW_BLOCK elements).  master: True for fp32 copies of the bf16 parameters, or a list of
@@ -899,71 +971,69 @@ class AdamW:
         n = len(self.params)
         _need(bits in (32, 8), "bits must be 32 or 8")
         self.bits = bits
+        self._dev = _device(self.params[0]) if n else -1
         for p in self.params:
-            _need(p.dtype in _TYPES and p.is_contiguous() and p.is_cuda and p.device == self.params[0].device,
-                  "parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
+            if p.dtype not in _TYPES or not p.is_contiguous() or p.get_device() != self._dev:
+                raise CpmtpError("cpmtp: parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
+        self._numels = [p.numel() for p in self.params]
+        self._types = [_TYPES[p.dtype] for p in self.params]
         if master is True:
             master = [p.float() if p.dtype == torch.bfloat16 else None for p in self.params]
         self.master = list(master) if master else [None] * n
+        for name, given in (("master", self.master), ("lr_scale", lr_scale), ("decay_scale", decay_scale)):
+            _need(given is None or len(given) == n, f"{name} needs one entry per parameter")
+        for w, p in zip(self.master, self.params):
+            if w is not None and (p.dtype != torch.bfloat16 or w.dtype != torch.float32 or not w.is_contiguous() or w.numel() != p.numel()
+                                  or w.get_device() != self._dev):
+                raise CpmtpError("cpmtp: a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
         state = state or {}
-        stype = torch.float32 if bits == 32 else torch.uint8
-        self.m, self.v = (self._states(state.get(k), stype, lambda p: p.numel(), k) for k in ("m", "v"))
-        self.m_exp = self.v_exp = [None] * n
-        if bits == 8:
-            self.m_exp, self.v_exp = (self._states(state.get(k), torch.uint8, lambda p: -(-p.numel() // ADAMW_BLOCK), k) for k in ("m_exp", "v_exp"))
-        for name, scales in (("lr_scale", lr_scale), ("decay_scale", decay_scale), ("master", self.master)):
-            _need(scales is None or len(scales) == n, f"{name} needs one entry per parameter")
-        self._table = (CAdamWTensor * max(1, n))()
-        for i, (c, p) in enumerate(zip(self._table, self.params)):
-            w = self.master[i]
-            _need(w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == p.numel() and w.device == p.device
-                                and p.dtype == torch.bfloat16), "a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
-            c.param, c.numel, c.param_type = p.data_ptr(), p.numel(), _TYPES[p.dtype]
-            c.master = w.data_ptr() if w is not None else None
-            c.m, c.v = self.m[i].data_ptr(), self.v[i].data_ptr()
-            if bits == 8:
-                c.m_exp, c.v_exp = self.m_exp[i].data_ptr(), self.v_exp[i].data_ptr()
-            c.lr_scale = 1.0 if lr_scale is None else float(lr_scale[i])
-            c.decay_scale = 1.0 if decay_scale is None else float(decay_scale[i])
+        moment = torch.float32 if bits == 32 else torch.uint8
+        blocks = [-(-k // ADAMW_BLOCK) for k in self._numels]
+        self.m, self.v = (self._states(state.get(k), moment, self._numels, k) for k in ("m", "v"))
+        self.m_exp, self.v_exp = (self._states(state.get(k), torch.uint8, blocks, k) if bits == 8 else [None] * n for k in ("m_exp", "v_exp"))
+        self._table = _Descriptors(n)
+        for word, tensors in ((0, self.params), (2, self.master), (3, self.m), (4, self.v), (5, self.m_exp), (6, self.v_exp)):
+            self._table.put(word, [0 if t is None else t.data_ptr() for t in tensors])
+        self._table.put(7, self._numels)
+        ones = [1.0] * n
+        self._table.put(9, [struct.unpack("q", struct.pack("ff", a, b))[0] for a, b in zip(lr_scale or ones, decay_scale or ones)])
 
-    def _states(self, given, dtype, size, name) -> list:
+    def _states(self, given, dtype, sizes, name) -> list:
         if given is None:
-            return [torch.zeros(size(p), dtype=dtype, device=p.device) for p in self.params]
-        _need(len(given) == len(self.params), f"{name} needs one entry per parameter")
-        for t, p in zip(given, self.params):
-            _need(t.dtype == dtype and t.is_contiguous() and t.numel() == size(p) and t.device == p.device, f"{name}: contiguous {dtype} of {size(p)} elements")
+            return [torch.zeros(k, dtype=dtype, device=p.device) for k, p in zip(sizes, self.params)]
+        _need(len(given) == len(sizes), f"{name} needs one entry per parameter")
+        for t, k in zip(given, sizes):
+            if t.dtype != dtype or not t.is_contiguous() or t.numel() != k or t.get_device() != self._dev:
+                raise CpmtpError(f"cpmtp: {name} must be contiguous {dtype} tensors of {k} elements here")
         return list(given)
 
     def step(self, grads, t: int, *, lr: float, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
              coef: Optional[torch.Tensor] = None, seed: int = 0) -> None:
         """Step t (1 for the first) with one gradient per parameter (bf16 or fp32, contiguous; None leaves a parameter alone).
         coef: fp32 [1] on the device that multiplies the gradients (grad_norm's), or None."""
-        params = self.params
-        _need(len(grads) == len(params), "one gradient per parameter")
-        if not params:
+        n = len(self.params)
+        _need(len(grads) == n, "one gradient per parameter")
+        if n == 0:
             return
-        dev = params[0].device
-        _on_device(params[0], coef=coef)
-        _need(coef is None or (coef.dtype == torch.float32 and coef.numel() >= 1), "coef must be float32 [1]")
-        for c, g in zip(self._table, grads):
-            if g is None:
-                c.grad = None
-                continue
-            _need(g.dtype in _TYPES and g.is_contiguous() and g.device == dev and g.numel() == c.numel, "a gradient is a contiguous tensor of its parameter's size")
-            c.grad, c.grad_type = g.data_ptr(), _TYPES[g.dtype]
+        dev = _device(self.params[0])
+        self._table.put_grads(grads, dev, self._types, self._numels)
         hyper = CAdamWHyper(lr, betas[0], betas[1], eps, weight_decay, t, seed & 0xFFFFFFFF, self.bits,
-                            None if coef is None else coef.data_ptr())
-        _check(load_library().cpmtp_adamw_step(self._table, len(params), ctypes.byref(hyper), _stream()))
+                            None if coef is None else _vector(coef, 1, torch.float32, dev, "coef"))
+        rc = load_library().cpmtp_adamw_step(self._table.address, n, ctypes.byref(hyper), _raw_stream(dev))
+        if rc:
+            _check(rc)
 
 
 def adamw_state_values(codes: torch.Tensor, exps: torch.Tensor, *, second: bool, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """cpmtp_adamw_state_values: the values of an 8-bit moment (second: v, else m) as bf16, exactly."""
+    dev = _device(codes)
     n = codes.numel()
-    _on_device(codes, exps=exps, out=out)
-    _need(codes.dtype == torch.uint8 and codes.is_contiguous(), "codes must be contiguous uint8")
-    _need(exps.dtype == torch.uint8 and exps.is_contiguous() and exps.numel() == -(-n // ADAMW_BLOCK), "exps: one byte per block")
     if out is None:
         out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
-    _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == n, "out must be contiguous bfloat16 of codes' size")
-    _check(load_library().cpmtp_adamw_state_values(codes.data_ptr(), exps.data_ptr(), n, 1 if second else 0, out.data_ptr(), _stream()))
+    for name, t, dtype, size in (("codes", codes, torch.uint8, n), ("exps", exps, torch.uint8, -(-n // ADAMW_BLOCK)), ("out", out, torch.bfloat16, n)):
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() != size:
+            raise CpmtpError(f"cpmtp: {name} must be {size} contiguous {dtype} on the same device")
+    rc = load_library().cpmtp_adamw_state_values(codes.data_ptr(), exps.data_ptr(), n, 1 if second else 0, out.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return out
