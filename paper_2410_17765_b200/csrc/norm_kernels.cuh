@@ -1,14 +1,22 @@
 // Norms before and after a block, fused with its gate and the residual addition: forward and backward.
 //
-// A row is owned by W warps, eight columns to a thread, and stays in registers from its only read to its only write;
-// a block holds G rows at a time (G = 1 from 2049 columns on).
+// A row is owned by W warps, eight columns to a thread, and stays in registers from its only read to its only write; a
+// block holds G rows at a time (W G <= 16; W <= 32, G = 1 from 4097 columns on).  Blocks are persistent.  Both directions move
+// 10 to 20 bytes per element and compute some tens of operations on them, so what counts is that every SM always has tens of
+// kilobytes of reads under way: rows ahead are fetched with cp.async into a ring of kStages rows in shared memory while
+// the current row goes through its reductions.
 #pragma once
 #include "vec_io.cuh"
 
 namespace cpmtp {
 namespace norm {
 
+using io::add2;
 using io::bf16_t;
+using io::both;
+using io::f32x2;
+using io::fma2;
+using io::mul2;
 
 constexpr int kMaxWarps = 32;
 
@@ -38,241 +46,387 @@ struct Params {
   float* part;       // [blocks][2][d] sums of dw_post, dw_pre over the rows of a block; nullptr: not wanted
 };
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-
-// Sums of NV values over the W warps of a row, in every thread of them.  `red` [NV][kMaxWarps] belongs to this row
-// and to this reduction alone until the one after the next.
-template <int NV>
-__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[kMaxWarps], int W, int group, int wg, int lane) {
-#pragma unroll
-  for (int n = 0; n < NV; ++n) v[n] = io::sum_lanes(v[n]);
-  if (W == 1) return;
-  if (lane == 0) {
-#pragma unroll
-    for (int n = 0; n < NV; ++n) red[n][wg] = v[n];
-  }
-  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
-#pragma unroll
-  for (int n = 0; n < NV; ++n) v[n] = io::sum_lanes(lane < W ? red[n][lane] : 0.f);
+// 1 / (1 + 2^(-z log2 e)); the flush of results below 2^-126 keeps both steps single instructions
+__device__ __forceinline__ float rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float sigmoid(float z) { return rcp(1.f + ptx::ex2_approx(z * -1.4426950408889634f)); }
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
+  const f32x2 e = mul2(z, both(-1.4426950408889634f));
+  const f32x2 s = add2(io::pair(ptx::ex2_approx(io::lo(e)), ptx::ex2_approx(io::hi(e))), both(1.f));
+  return io::pair(rcp(io::lo(s)), rcp(io::hi(s)));
 }
 
-template <class S, bool VEC, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_fwd_kernel(const __grid_constant__ Params<S> p) {
-  __shared__ float red[2][MAXT > 512 ? 1 : 8][1][kMaxWarps];     // rows of more than one warp: at most 8 to a block
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = warp / p.W, wg = warp - group * p.W;
-  const int t = wg * 32 + lane, tg = p.W * 32;
-  const long long i = static_cast<long long>(blockIdx.x) * p.G + group;
-  ptx::grid_dep_wait();
-  if (i >= p.N) return;                          // a whole row's warps: no other row waits for them
-  const int rg = p.W == 1 ? 0 : group;
-  float x[8];
-  io::load_cols<VEC>(p.x.at(i), t, tg, p.d, x);
-  if (p.block.data != nullptr) {
-    float b[8], g[8];
-    io::load_cols<VEC>(p.block.at(i), t, tg, p.d, b);
-    if (p.gate_kind == CPMTP_GATE_CHANNEL) {
-      io::load_cols<VEC>(p.gate.at(i), t, tg, p.d, g);
+__device__ __forceinline__ void row_barrier(int W, int group) {
+  if (W == 1) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
+}
+
+// Sum over the W warps of a row, in every thread of them.  `red` is this row's and this reduction's alone until the row
+// after the next.
+__device__ __forceinline__ float row_sum(float v, float* red, int W, int group, int wg, int lane) {
+  v = io::sum_lanes(v);
+  if (W == 1) return v;
+  if (lane == 0) red[wg] = v;
+  row_barrier(W, group);
+  return io::sum_lanes(lane < W ? red[lane] : 0.f);
+}
+
+// The same for three values at once, in 12 shuffles where three single sums take 30: lanes hand over the values that
+// the other half will finish, so that each octet of lanes ends up with the sum of one of them.
+__device__ __forceinline__ void row_sum3(float (&v)[3], float (*red)[kMaxWarps], int W, int group, int wg, int lane) {
+  const bool hi = lane & 16, odd = lane & 8;
+  float a = hi ? v[2] : v[0], b = hi ? 0.f : v[1];
+  a += __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
+  b += __shfl_xor_sync(0xffffffffu, hi ? v[1] : 0.f, 16);
+  float c = odd ? b : a;
+  c += __shfl_xor_sync(0xffffffffu, odd ? a : b, 8);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] = sigmoid(g[k]);
-    } else {
-      const float one = p.gate_kind == CPMTP_GATE_ROW ? sigmoid(io::to_f(*p.gate.at(i))) : 1.f;
+  for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+  const int which = lane >> 3, j = lane & 7;
+  if (W > 1) {
+    if (j == 0 && which < 3) red[which][wg] = c;
+    row_barrier(W, group);
+    c = 0.f;
+    if (which < 3) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] = one;
+      for (int k = 0; k < kMaxWarps; k += 8)
+        if (j + k < W) c += red[which][j + k];
     }
-    if (p.w_post != nullptr) {
-      float w[8];
-      io::load_cols<VEC>(p.w_post, t, tg, p.d, w);
-      float ss[1] = {0.f};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) ss[0] = fmaf(b[k], b[k], ss[0]);
-      row_sum(ss, red[0][rg], p.W, group, wg, lane);
-      const float rb = rsqrtf(fmaf(ss[0], p.inv_d, p.eps));
-      if (t == 0 && p.rstd_post != nullptr) p.rstd_post[i] = rb;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) b[k] *= rb * w[k];
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = fmaf(p.res_scale, x[k], g[k] * b[k]);
-    io::store_cols<VEC>(p.x_out.at(i), t, tg, p.d, x);
+    for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
   }
-  if (p.w_pre != nullptr) {
-    float w[8];
-    io::load_cols<VEC>(p.w_pre, t, tg, p.d, w);
-    float ss[1] = {0.f};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) ss[0] = fmaf(x[k], x[k], ss[0]);
-    row_sum(ss, red[1][rg], p.W, group, wg, lane);
-    const float rx = rsqrtf(fmaf(ss[0], p.inv_d, p.eps));
-    if (t == 0 && p.rstd_pre != nullptr) p.rstd_pre[i] = rx;
+  for (int n = 0; n < 3; ++n) v[n] = __shfl_sync(0xffffffffu, c, 8 * n);
+}
+
+// ---- rows in shared memory ----
+// A row of d elements of T, wherever it starts, lies in at most d sizeof(T) / 16 + 1 aligned pieces of 16 bytes, and it is
+// these that are copied (the last one only as far as the row goes), so that rows of any width and stride move in whole
+// 16-byte accesses.  VEC (rows start on a piece, d = 256 W): a thread copies exactly what it will use itself, and no
+// barrier is spent on the copy.
+template <class T>
+__host__ __device__ constexpr int region_bytes(int threads) { return (threads * static_cast<int>(sizeof(T)) / 2 + 1) * 16; }
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+template <bool VEC, class T>
+__device__ __forceinline__ void fetch_row(uint32_t region, const T* row, int t, int tg, int d) {
+  constexpr int kPer = sizeof(T) / 2;                     // pieces to a thread
+  if (VEC) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= rx * w[k];
-    io::store_cols<VEC>(p.y.at(i), t, tg, p.d, x);
+    for (int k = 0; k < kPer; ++k) cp16(region + (t * kPer + k) * 16, reinterpret_cast<const char*>(row + 8 * t) + 16 * k, 16);
+  } else {
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15);
+    const char* base = reinterpret_cast<const char*>(row) - off;
+    const int end = off + d * static_cast<int>(sizeof(T));
+    for (int j = t; j * 16 < end; j += tg) cp16(region + j * 16, base + j * 16, min(16, end - j * 16));
   }
 }
 
-// Backward.  Persistent blocks: a thread keeps its eight columns' sums of dw_post and dw_pre over all rows of its
-// block.  The gradient t of x_out needs the row mean c1 = mean(w_pre dy xh); the norm after the block then needs the mean
-// of w_post du bh, which holds t.  Both come out of one reduction over the row, since t = a - rstd_pre c1 xh with
-// a = dx_out + rstd_pre w_pre dy is linear in c1:
-//   sum q t = sum q a - rstd_pre c1 sum q xh,      q = g w_post bh.
-// Rows ahead are fetched with cp.async, every thread the elements that it will itself use, so no barrier is spent on them.
-constexpr int kStages = 2;
+// This thread's eight columns of a fetched row; zeros past the row's end.
+template <bool VEC, class T>
+__device__ __forceinline__ void take8(const uint8_t* region, const T* row, int t, int tg, int d, f32x2 (&p)[4]) {
+  float v[8];
+  if (VEC) {
+    io::load8_shared(region + t * static_cast<int>(8 * sizeof(T)), v, T());
+  } else {
+    const T* s = reinterpret_cast<const T*>(region + (reinterpret_cast<uintptr_t>(row) & 15));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = t + k * tg < d ? io::to_f(s[t + k * tg]) : 0.f;
+  }
+  io::pairs(v, p);
+}
+template <bool VEC, class T>
+__device__ __forceinline__ void put8(T* row, int t, int tg, int d, const f32x2 (&p)[4]) {
+  float v[8];
+  io::singles(p, v);
+  if (VEC) io::store8(row + 8 * t, v);
+  else io::store_cols<false>(row, t, tg, d, v);
+}
+__device__ __forceinline__ void fill8(f32x2 (&p)[4], float v) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = both(v);
+}
 
-template <class S>
-struct Slots {                                   // 16-byte slots per thread and stage: dy, block, gate, x_out, dx_out
-  static constexpr int kS = sizeof(S) / 2;
-  static constexpr int kDy = 0, kBlock = 1, kGate = 2, kX = 3, kDxOut = 3 + kS, kCount = 3 + 2 * kS;
+__device__ __forceinline__ void commit_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_row() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Where a thread stands: its row's group of W warps, and its place among them.  ONE (a block holds one row at a time):
+// known to be the same for all threads, so that addresses of rows are computed once per warp.
+template <bool ONE>
+struct Place {
+  int lane, group, wg, t, tg, rg;
+  __device__ __forceinline__ explicit Place(int W) {
+    const int warp = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    group = ONE ? 0 : warp / W;
+    wg = warp - group * W;
+    t = wg * 32 + lane;
+    tg = W * 32;
+    rg = W == 1 ? 0 : group;                              // rows of one warp do not use the reductions' memory
+  }
 };
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void slot8(const uint8_t* s, int, float (&v)[8], bf16_t) {
-  io::unpack8(*reinterpret_cast<const uint4*>(s), v);
-}
-__device__ __forceinline__ void slot8(const uint8_t* s, int stride, float (&v)[8], float) {
-  const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + stride);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+// A norm's weights, or `otherwise` where there is none.
+template <bool VEC>
+__device__ __forceinline__ void load_weights(const bf16_t* w, int t, int tg, int d, float otherwise, f32x2 (&p)[4]) {
+  if (w == nullptr) {
+    fill8(p, otherwise);
+  } else {
+    float v[8];
+    if (VEC) io::load8(w + 8 * t, v);
+    else io::load_cols<false>(w, t, tg, d, v);
+    io::pairs(v, p);
+  }
 }
 
-template <class S, bool VEC, int MAXT>
+__device__ __forceinline__ float square_sum(const f32x2 (&v)[4]) {
+  f32x2 s = mul2(v[0], v[0]);
+#pragma unroll
+  for (int k = 1; k < 4; ++k) s = fma2(v[k], v[k], s);
+  return io::lo(s) + io::hi(s);
+}
+
+// One value per row, for the rows that a group of warps goes through: lane l holds that of the l-th row from here, so that a
+// row costs a shuffle and every 32nd one a load.
+template <class T>
+__device__ __forceinline__ float row_values(const T* at, long long ld, long long i, long long step, int N, int lane) {
+  const long long row = i + lane * step;
+  return row < N ? io::to_f(at[row * ld]) : 0.f;
+}
+
+// ---- forward ----
+template <class S>
+__host__ __device__ constexpr int fwd_stage_bytes(int threads) { return region_bytes<S>(threads) + 2 * region_bytes<bf16_t>(threads); }
+
+template <class S, bool VEC, int MAXT, int STAGES, bool ONE, bool ALL>
+__global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __grid_constant__ Params<S> p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float red[2][2][ONE ? 1 : 8][kMaxWarps];
+  const Place<ONE> at(p.W);
+  const int t = at.t, tg = at.tg, d = p.d;
+  const int stage_bytes = fwd_stage_bytes<S>(tg);
+  uint8_t* ring = smem + at.group * STAGES * stage_bytes;
+  const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || p.w_post != nullptr, has_y = ALL || p.w_pre != nullptr;
+  const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
+  const long long step = static_cast<long long>(gridDim.x) * (ONE ? 1 : p.G);
+  long long i = static_cast<long long>(blockIdx.x) * (ONE ? 1 : p.G) + at.group;
+  ptx::grid_dep_wait();
+  const uint32_t ring_at = ptx::smem_u32(ring);
+  auto fetch = [&](long long row, int stage) {
+    if (row < p.N) {
+      uint32_t s = ring_at + stage * stage_bytes;
+      fetch_row<VEC>(s, p.x.at(row), t, tg, d);
+      s += region_bytes<S>(tg);
+      if (has_block) fetch_row<VEC>(s, p.block.at(row), t, tg, d);
+      if (channel) fetch_row<VEC>(s + region_bytes<bf16_t>(tg), p.gate.at(row), t, tg, d);
+    }
+    commit_row();
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) fetch(i + s * step, s);
+  f32x2 w_post[4], w_pre[4];
+  load_weights<VEC>(p.w_post, t, tg, d, 0.f, w_post);
+  load_weights<VEC>(p.w_pre, t, tg, d, 0.f, w_pre);
+  float logits = 0.f;
+  int stage = 0;
+  for (int it = 0; i < p.N; i += step, ++it) {
+    float gl = 0.f;
+    if (row_gate) {
+      if ((it & 31) == 0) logits = row_values(p.gate.data, p.gate.ld, i, step, p.N, at.lane);
+      gl = __shfl_sync(0xffffffffu, logits, it & 31);
+    }
+    // the stage that this refills was read before the row barriers of the row before (one warp: before this one)
+    if (!VEC && p.W == 1) __syncwarp();
+    fetch(i + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+    wait_row<STAGES - 1>();
+    if (!VEC) row_barrier(p.W, at.group);
+    const uint8_t* s = ring + stage * stage_bytes;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    f32x2 x[4];
+    take8<VEC>(s, p.x.at(i), t, tg, d, x);
+    if (has_block) {
+      s += region_bytes<S>(tg);
+      f32x2 b[4], g[4];
+      take8<VEC>(s, p.block.at(i), t, tg, d, b);
+      if (channel) {
+        take8<VEC>(s + region_bytes<bf16_t>(tg), p.gate.at(i), t, tg, d, g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
+      } else {
+        fill8(g, row_gate ? sigmoid(gl) : 1.f);
+      }
+      if (has_post) {
+        const float rb = rsqrtf(fmaf(row_sum(square_sum(b), red[it & 1][0][at.rg], p.W, at.group, at.wg, at.lane), p.inv_d, p.eps));
+        if (t == 0 && (ALL || p.rstd_post != nullptr)) p.rstd_post[i] = rb;
+        const f32x2 rb2 = both(rb);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[k] = mul2(b[k], mul2(rb2, w_post[k]));
+      }
+      const f32x2 scale = both(p.res_scale);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = fma2(scale, x[k], mul2(g[k], b[k]));
+      put8<VEC>(p.x_out.at(i), t, tg, d, x);
+    }
+    if (has_y) {
+      const float rx = rsqrtf(fmaf(row_sum(square_sum(x), red[it & 1][1][at.rg], p.W, at.group, at.wg, at.lane), p.inv_d, p.eps));
+      if (t == 0 && (ALL || p.rstd_pre != nullptr)) p.rstd_pre[i] = rx;
+      const f32x2 rx2 = both(rx);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], mul2(rx2, w_pre[k]));
+      put8<VEC>(p.y.at(i), t, tg, d, x);
+    }
+    // without a reduction in this row nothing has yet kept the others from its stage
+    if (!VEC && !has_post && !has_y) row_barrier(p.W, at.group);
+  }
+}
+
+// ---- backward ----
+// A thread keeps its eight columns' sums of dw_post and dw_pre over all rows of its block.  The gradient t of x_out needs the
+// row mean c1 = mean(w_pre dy xh); the norm after the block then needs the mean of w_post du bh, which holds t.  Both come
+// out of one reduction over the row, since t = a - c1 rstd_pre xh with a = dx_out + rstd_pre w_pre dy is linear in c1:
+//   sum q t = sum q a - c1 rstd_pre sum q xh,      q = g w_post bh.
+// The row's two rstd are taken out of the sums and put into per-row factors, which leaves about 30 operations per element.
+template <class S>
+__host__ __device__ constexpr int bwd_stage_bytes(int threads) { return 2 * region_bytes<S>(threads) + 3 * region_bytes<bf16_t>(threads); }
+
+template <class S, bool VEC, int MAXT, int STAGES, bool ONE, bool ALL>
 __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ Params<S> p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float red[2][MAXT > 512 ? 1 : 8][3][kMaxWarps];
-  using L = Slots<S>;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = warp / p.W, wg = warp - group * p.W;
-  const int t = wg * 32 + lane, tg = p.W * 32;
-  const int rg = p.W == 1 ? 0 : group;
-  const int stride = blockDim.x * 16;            // from one slot of a thread to its next
-  const bool mine = 8 * t < p.d;
-  const long long step = static_cast<long long>(gridDim.x) * p.G;
-  const bool has_block = p.block.data != nullptr, has_post = has_block && p.w_post != nullptr;
-  const bool channel = p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = p.gate_kind == CPMTP_GATE_ROW;
-  const bool has_y = p.dy.data != nullptr, has_dx_out = p.dx_out.data != nullptr;
+  __shared__ float red[2][ONE ? 1 : 8][3][kMaxWarps];
+  const Place<ONE> at(p.W);
+  const int t = at.t, tg = at.tg, d = p.d;
+  const int rs = region_bytes<S>(tg), rb16 = region_bytes<bf16_t>(tg), stage_bytes = bwd_stage_bytes<S>(tg);
+  uint8_t* ring = smem + at.group * STAGES * stage_bytes;
+  const long long step = static_cast<long long>(gridDim.x) * (ONE ? 1 : p.G);
+  const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || (has_block && p.w_post != nullptr);
+  const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
+  const bool has_y = ALL || p.dy.data != nullptr, has_dx_out = ALL || p.dx_out.data != nullptr;
   ptx::grid_dep_wait();
-
-  auto fetch = [&](long long i, int stage) {
-    if (VEC && i < p.N && mine) {
-      const uint32_t s = ptx::smem_u32(smem) + stage * L::kCount * stride + threadIdx.x * 16;
-      if (has_y) cp16(s + L::kDy * stride, p.dy.at(i) + 8 * t);
-      if (has_block) cp16(s + L::kBlock * stride, p.block.at(i) + 8 * t);
-      if (channel) cp16(s + L::kGate * stride, p.gate.at(i) + 8 * t);
-#pragma unroll
-      for (int k = 0; k < L::kS; ++k) {
-        cp16(s + (L::kX + k) * stride, p.x_out.at(i) + 8 * t + 4 * k);
-        if (has_dx_out) cp16(s + (L::kDxOut + k) * stride, p.dx_out.at(i) + 8 * t + 4 * k);
-      }
+  long long i = static_cast<long long>(blockIdx.x) * (ONE ? 1 : p.G) + at.group;
+  const uint32_t ring_at = ptx::smem_u32(ring);
+  auto fetch = [&](long long row, int stage) {
+    if (row < p.N) {
+      uint32_t s = ring_at + stage * stage_bytes;
+      fetch_row<VEC>(s, p.x_out.at(row), t, tg, d);
+      if (has_dx_out) fetch_row<VEC>(s + rs, p.dx_out.at(row), t, tg, d);
+      s += 2 * rs;
+      if (has_y) fetch_row<VEC>(s, p.dy.at(row), t, tg, d);
+      if (has_block) fetch_row<VEC>(s + rb16, p.block.at(row), t, tg, d);
+      if (channel) fetch_row<VEC>(s + 2 * rb16, p.gate.at(row), t, tg, d);
     }
-    if (VEC) asm volatile("cp.async.commit_group;" ::: "memory");
+    commit_row();
   };
-  auto get = [&](auto rows, bool present, int slot, long long i, int stage, float (&v)[8]) {
-    using T = std::remove_cv_t<std::remove_pointer_t<decltype(rows.data)>>;
-    if (VEC ? (present && mine) : present) {
-      if (VEC) {
-        slot8(smem + (stage * L::kCount + slot) * stride + threadIdx.x * 16, stride, v, T());
-      } else {
-        io::load_cols<false>(rows.at(i), t, tg, p.d, v);
-      }
-    } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = 0.f;
-    }
-  };
-
-  float w_pre[8], w_post[8], acc_pre[8], acc_post[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) w_pre[k] = w_post[k] = acc_pre[k] = acc_post[k] = 0.f;
-  if (has_y) io::load_cols<VEC>(p.w_pre, t, tg, p.d, w_pre);
-  if (has_post) io::load_cols<VEC>(p.w_post, t, tg, p.d, w_post);
-
-  long long i = static_cast<long long>(blockIdx.x) * p.G + group;
-  for (int s = 0; s < kStages - 1; ++s) fetch(i + s * step, s);
-  float rx_next = 0.f, rb_next = 1.f, gl_next = 0.f;
-  auto scalars = [&](long long row) {
-    if (row >= p.N) return;
-    if (has_y) rx_next = p.rstd_pre[row];
-    if (has_post) rb_next = p.rstd_post[row];
-    if (row_gate) gl_next = io::to_f(*p.gate.at(row));
-  };
-  scalars(i);
+  for (int s = 0; s < STAGES - 1; ++s) fetch(i + s * step, s);
+  f32x2 w_pre[4], w_post[4], acc_pre[4], acc_post[4];
+  fill8(acc_pre, 0.f);
+  fill8(acc_post, 0.f);
+  load_weights<VEC>(has_y ? p.w_pre : nullptr, t, tg, d, 0.f, w_pre);
+  load_weights<VEC>(has_post ? p.w_post : nullptr, t, tg, d, 1.f, w_post);
+  float rstds_pre = 0.f, rstds_post = 1.f, logits = 0.f;
+  int stage = 0;
   for (int it = 0; i < p.N; i += step, ++it) {
-    const float rx = rx_next, rb = rb_next;
-    const float grow = row_gate ? sigmoid(gl_next) : 1.f;
-    scalars(i + step);
-    const int stage = it % kStages;
-    fetch(i + (kStages - 1) * step, (it + kStages - 1) % kStages);
-    if (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-    float dy[8], xh[8], a[8], bh[8], g[8];
-    get(p.dy, has_y, L::kDy, i, stage, dy);
-    get(p.x_out, true, L::kX, i, stage, xh);
-    get(p.dx_out, has_dx_out, L::kDxOut, i, stage, a);
-    get(p.block, has_block, L::kBlock, i, stage, bh);
-    get(p.gate, channel, L::kGate, i, stage, g);
-    float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      xh[k] *= rx;
-      bh[k] *= rb;
-      g[k] = channel ? sigmoid(g[k]) : 1.f;
-      const float wdy = w_pre[k] * dy[k];
-      a[k] = fmaf(rx, wdy, a[k]);
-      const float q = (has_post ? w_post[k] * bh[k] : bh[k]) * g[k];
-      s[0] = fmaf(wdy, xh[k], s[0]);
-      s[1] = fmaf(q, a[k], s[1]);
-      s[2] = fmaf(q, xh[k], s[2]);
-      acc_pre[k] = fmaf(dy[k], xh[k], acc_pre[k]);
+    if ((it & 31) == 0) {
+      if (has_y) rstds_pre = row_values(p.rstd_pre, 1, i, step, p.N, at.lane);
+      if (has_post) rstds_post = row_values(p.rstd_post, 1, i, step, p.N, at.lane);
+      if (row_gate) logits = row_values(p.gate.data, p.gate.ld, i, step, p.N, at.lane);
     }
-    row_sum(s, red[it & 1][rg], p.W, group, wg, lane);
-    const float c1 = rx * s[0] * p.inv_d;
-    const float dot = s[1] - c1 * s[2];
-    const float c2 = grow * dot * p.inv_d;
-    float dgate[8];
+    const float rx = __shfl_sync(0xffffffffu, rstds_pre, it & 31), rb = __shfl_sync(0xffffffffu, rstds_post, it & 31);
+    const float grow = row_gate ? sigmoid(__shfl_sync(0xffffffffu, logits, it & 31)) : 1.f;
+    // the stage that this refills was read before the row barrier of the row before (one warp: before this one)
+    if (!VEC && p.W == 1) __syncwarp();
+    fetch(i + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+    wait_row<STAGES - 1>();
+    if (!VEC) row_barrier(p.W, at.group);
+    const uint8_t* s = ring + stage * stage_bytes;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    f32x2 dy[4], x[4], a[4], b[4], g[4];
+    take8<VEC>(s, p.x_out.at(i), t, tg, d, x);
+    if (has_dx_out) take8<VEC>(s + rs, p.dx_out.at(i), t, tg, d, a);
+    else fill8(a, 0.f);
+    s += 2 * rs;
+    if (has_y) take8<VEC>(s, p.dy.at(i), t, tg, d, dy);
+    else fill8(dy, 0.f);
+    if (has_block) take8<VEC>(s + rb16, p.block.at(i), t, tg, d, b);
+    else fill8(b, 0.f);
+    if (channel) {
+      take8<VEC>(s + 2 * rb16, p.gate.at(i), t, tg, d, g);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float tk = fmaf(-c1, xh[k], a[k]);
-      const float du = grow * g[k] * tk;
-      const float u = has_post ? w_post[k] * bh[k] : bh[k];
-      dgate[k] = tk * u * g[k] * (1.f - g[k]);
-      acc_post[k] = fmaf(du, bh[k], acc_post[k]);
-      xh[k] = p.res_scale * tk;                                               // dx
-      a[k] = has_post ? rb * fmaf(w_post[k], du, -bh[k] * c2) : du;           // dblock
+      for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
+    } else {
+      fill8(g, 1.f);
     }
-    if (p.dx.data != nullptr) io::store_cols<VEC>(p.dx.at(i), t, tg, p.d, xh);
-    if (p.dblock.data != nullptr) io::store_cols<VEC>(p.dblock.at(i), t, tg, p.d, a);
-    if (p.dgate.data != nullptr) {
-      if (channel) io::store_cols<VEC>(p.dgate.at(i), t, tg, p.d, dgate);
+    f32x2 s0 = both(0.f), s1 = s0, s2 = s0, wb[4];
+    const f32x2 rx2 = both(rx);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x2 dyr = mul2(dy[k], rx2), wdyr = mul2(w_pre[k], dyr);
+      acc_pre[k] = fma2(dyr, x[k], acc_pre[k]);
+      a[k] = add2(a[k], wdyr);
+      wb[k] = mul2(w_post[k], b[k]);
+      const f32x2 q = mul2(wb[k], g[k]);
+      s0 = fma2(wdyr, x[k], s0);
+      s1 = fma2(q, a[k], s1);
+      s2 = fma2(q, x[k], s2);
+    }
+    float sum[3] = {io::lo(s0) + io::hi(s0), io::lo(s1) + io::hi(s1), io::lo(s2) + io::hi(s2)};
+    row_sum3(sum, red[it & 1][at.rg], p.W, at.group, at.wg, at.lane);
+    const float c1 = rx * rx * sum[0] * p.inv_d;              // t = a - c1 x
+    const float dot = rb * fmaf(-c1, sum[2], sum[1]);         // sum of t u (the row gate left out)
+    const f32x2 minus_c1 = both(-c1), grb = both(grow * rb), scale = both(p.res_scale);
+    const f32x2 minus_c2 = both(has_post ? -rb * rb * grow * dot * p.inv_d : 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x2 tk = fma2(minus_c1, x[k], a[k]);
+      const f32x2 dur = mul2(mul2(grb, g[k]), tk);            // rstd_post du
+      acc_post[k] = fma2(dur, b[k], acc_post[k]);
+      a[k] = fma2(w_post[k], dur, mul2(minus_c2, b[k]));      // dblock
+      g[k] = mul2(mul2(wb[k], dur), fma2(g[k], both(-1.f), both(1.f)));   // dgate
+      x[k] = mul2(scale, tk);                                 // dx
+    }
+    if (ALL || p.dx.data != nullptr) put8<VEC>(p.dx.at(i), t, tg, d, x);
+    if (ALL || p.dblock.data != nullptr) put8<VEC>(p.dblock.at(i), t, tg, d, a);
+    if (ALL || p.dgate.data != nullptr) {
+      if (channel) put8<VEC>(p.dgate.at(i), t, tg, d, g);
       else if (t == 0) *p.dgate.at(i) = io::from_f<bf16_t>(grow * (1.f - grow) * dot);
     }
   }
   if (p.part == nullptr) return;
-  float* out = p.part + static_cast<size_t>(blockIdx.x) * 2 * p.d;
-  if (p.G == 1) {
+  float sum_pre[8], sum_post[8];
+  io::singles(acc_pre, sum_pre);
+  io::singles(acc_post, sum_post);
+  float* out = p.part + static_cast<size_t>(blockIdx.x) * 2 * d;
+  if (ONE) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int c = io::col_of<VEC>(t, tg, k);
-      if (c < p.d) {
-        out[c] = acc_post[k];
-        out[p.d + c] = acc_pre[k];
+      if (c < d) {
+        out[c] = sum_post[k];
+        out[d + c] = sum_pre[k];
       }
     }
     return;
   }
   // the rows that the block held at a time, one after the other
-  if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  wait_row<0>();
   __syncthreads();
-  float* sums = reinterpret_cast<float*>(smem);                 // [2][G][8 tg]
+  float* sums = reinterpret_cast<float*>(smem);               // [2][G][8 tg]
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int c = io::col_of<VEC>(t, tg, k);
-    sums[group * 8 * tg + c] = acc_post[k];
-    sums[(p.G + group) * 8 * tg + c] = acc_pre[k];
+    sums[at.group * 8 * tg + c] = sum_post[k];
+    sums[(p.G + at.group) * 8 * tg + c] = sum_pre[k];
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < 2 * p.d; c += blockDim.x) {
-    const int which = c >= p.d, col = c - which * p.d;
+  for (int c = threadIdx.x; c < 2 * d; c += blockDim.x) {
+    const int which = c >= d, col = c - which * d;
     float v = 0.f;
     for (int gr = 0; gr < p.G; ++gr) v += sums[(which * p.G + gr) * 8 * tg + col];
     out[c] = v;

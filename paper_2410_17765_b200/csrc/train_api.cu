@@ -83,11 +83,21 @@ NormLayout norm_layout(int d) {
   return L;
 }
 
-// Persistent blocks of the backward kernel.
-int norm_bwd_blocks(const cpmtp_norm_args& a, const NormLayout& L, int sms) {
+// Rows kept in shared memory per row group, the current one included: as many as 227 KB hold for one block of the
+// backward kernel per SM, or half of that for two of the forward kernel.
+template <class S, int MAXT>
+constexpr int fwd_stages() { return MAXT > 512 ? (sizeof(S) == 4 ? 3 : 4) : (sizeof(S) == 4 ? 3 : 4); }
+template <class S, int MAXT>
+constexpr int bwd_stages() { return MAXT > 512 ? 2 : (sizeof(S) == 4 ? 3 : 5); }
+
+template <bool ONE>
+constexpr int kMaxGroups = ONE ? 1 : 16;
+
+int row_blocks(const cpmtp_norm_args& a, const NormLayout& L, int most) {
   const long long rows = (static_cast<long long>(a.N) + L.G - 1) / L.G;
-  return static_cast<int>(rows < sms ? rows : sms);
+  return static_cast<int>(rows < most ? rows : most);
 }
+int norm_bwd_blocks(const cpmtp_norm_args& a, const NormLayout& L, int sms) { return row_blocks(a, L, sms); }
 
 int check_rows(const cpmtp_rows& r, int d, size_t bytes) {
   if (r.data == nullptr) return CPMTP_ERR_NULL;
@@ -137,39 +147,57 @@ norm::Params<S> norm_params(const cpmtp_norm_args& a, const NormLayout& L) {
 }
 
 template <class T>
-bool rows_vec(const cpmtp_rows& r, int d) { return r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d); }
+bool rows_vec(const cpmtp_rows& r, int d) { return d % 256 == 0 && (r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d)); }
 
-template <class S, int MAXT>
-cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, cudaStream_t st) {
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+template <class K>
+cudaError_t allow_smem(K* kernel, bool (&done)[64], int bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_cache_mutex);
+  if (done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+
+template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
+cudaError_t launch_norm_fwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
+  constexpr int kStages = fwd_stages<S, MAXT>();
+  static bool done[64] = {};
+  auto* kernel = norm::norm_fwd_kernel<S, VEC, MAXT, kStages, ONE, ALL>;
+  const cudaError_t e = allow_smem(kernel, done, kStages * kMaxGroups<ONE> * norm::fwd_stage_bytes<S>(MAXT / kMaxGroups<ONE>));
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(blocks), dim3(L.threads), kStages * L.G * norm::fwd_stage_bytes<S>(L.W * 32), st, p);
+}
+
+template <class S, int MAXT, bool ONE>
+cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, int sms, cudaStream_t st) {
   const norm::Params<S> p = norm_params<S>(a, L);
   const bool vec = rows_vec<S>(a.x, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.y, a.d) &&
                    (a.gate_kind != CPMTP_GATE_CHANNEL || rows_vec<bf16_t>(a.gate, a.d)) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
-  const dim3 grid(static_cast<unsigned>((static_cast<long long>(a.N) + L.G - 1) / L.G));
-  if (vec) return launch_pdl(norm::norm_fwd_kernel<S, true, MAXT>, grid, dim3(L.threads), 0, st, p);
-  return launch_pdl(norm::norm_fwd_kernel<S, false, MAXT>, grid, dim3(L.threads), 0, st, p);
+  const int blocks = row_blocks(a, L, sms * (1024 / MAXT));
+  const bool all = a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.w_pre != nullptr && a.rstd_post != nullptr && a.rstd_pre != nullptr;
+  if (!vec) return launch_norm_fwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
+  return all ? launch_norm_fwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_fwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
+}
+template <class S>
+cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, int sms, cudaStream_t st) {
+  if (L.threads > 512) return launch_norm_fwd<S, 1024, true>(a, L, sms, st);
+  return L.G == 1 ? launch_norm_fwd<S, 512, true>(a, L, sms, st) : launch_norm_fwd<S, 512, false>(a, L, sms, st);
 }
 
-template <class S, bool VEC, int MAXT>
+template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
 cudaError_t launch_norm_bwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
-  static bool attr_set[64] = {};
-  size_t smem = L.G > 1 ? 2 * 8 * sizeof(float) * L.threads : 0;             // the block's sums; before them the rows ahead
-  const size_t ahead = static_cast<size_t>(norm::kStages) * norm::Slots<S>::kCount * 16 * L.threads;
-  if (VEC && ahead > smem) smem = ahead;
-  constexpr int most = norm::kStages * norm::Slots<S>::kCount * 16 * MAXT;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  {
-    std::lock_guard<std::mutex> lock(g_cache_mutex);
-    if (!attr_set[dev]) {
-      const cudaError_t e = cudaFuncSetAttribute(norm::norm_bwd_kernel<S, VEC, MAXT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-      if (e != cudaSuccess) return e;
-      attr_set[dev] = true;
-    }
-  }
-  return launch_pdl(norm::norm_bwd_kernel<S, VEC, MAXT>, dim3(blocks), dim3(L.threads), smem, st, p);
+  constexpr int kStages = bwd_stages<S, MAXT>();
+  static bool done[64] = {};
+  auto* kernel = norm::norm_bwd_kernel<S, VEC, MAXT, kStages, ONE, ALL>;
+  const cudaError_t e = allow_smem(kernel, done, kStages * kMaxGroups<ONE> * norm::bwd_stage_bytes<S>(MAXT / kMaxGroups<ONE>));
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(blocks), dim3(L.threads), kStages * L.G * norm::bwd_stage_bytes<S>(L.W * 32), st, p);
 }
 
-template <class S, int MAXT>
+template <class S, int MAXT, bool ONE>
 cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int blocks, float* part, cudaStream_t st) {
   norm::Params<S> p = norm_params<S>(a, L);
   p.part = part;
@@ -177,8 +205,15 @@ cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int b
   const bool vec = rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<bf16_t>(a.dy, a.d) && rows_vec<S>(a.dx_out, a.d) &&
                    rows_vec<S>(a.dx, a.d) && rows_vec<bf16_t>(a.dblock, a.d) &&
                    (!channel || (rows_vec<bf16_t>(a.gate, a.d) && rows_vec<bf16_t>(a.dgate, a.d))) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
-  if (vec) return launch_norm_bwd_as<S, true, MAXT>(p, L, blocks, st);
-  return launch_norm_bwd_as<S, false, MAXT>(p, L, blocks, st);
+  const bool all = channel && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr && a.dx.data != nullptr &&
+                   a.dblock.data != nullptr && a.dgate.data != nullptr;
+  if (!vec) return launch_norm_bwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
+  return all ? launch_norm_bwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_bwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
+}
+template <class S>
+cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int blocks, float* part, cudaStream_t st) {
+  if (L.threads > 512) return launch_norm_bwd<S, 1024, true>(a, L, blocks, part, st);
+  return L.G == 1 ? launch_norm_bwd<S, 512, true>(a, L, blocks, part, st) : launch_norm_bwd<S, 512, false>(a, L, blocks, part, st);
 }
 
 // ---------------------------------------------------------------------------------------------- optimiser
@@ -420,13 +455,8 @@ int cpmtp_norm_forward(const cpmtp_norm_args* args, cpmtp_stream stream) {
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const NormLayout L = norm_layout(a.d);
   ProfScope prof(CPMTP_STAGE_NORM, st);
-  if (L.threads > 512) {
-    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_fwd<float, 1024>(a, L, st)));
-    else CPMTP_TRY((launch_norm_fwd<bf16_t, 1024>(a, L, st)));
-  } else {
-    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_fwd<float, 512>(a, L, st)));
-    else CPMTP_TRY((launch_norm_fwd<bf16_t, 512>(a, L, st)));
-  }
+  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_fwd<float>(a, L, di->sms, st));
+  else CPMTP_TRY(launch_norm_fwd<bf16_t>(a, L, di->sms, st));
   return CPMTP_OK;
 }
 
@@ -486,13 +516,8 @@ int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t wor
     part = static_cast<float*>(workspace);
   }
   ProfScope prof(CPMTP_STAGE_NORM_GRAD, st);
-  if (L.threads > 512) {
-    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_bwd<float, 1024>(a, L, blocks, part, st)));
-    else CPMTP_TRY((launch_norm_bwd<bf16_t, 1024>(a, L, blocks, part, st)));
-  } else {
-    if (a.stream_type == CPMTP_F32) CPMTP_TRY((launch_norm_bwd<float, 512>(a, L, blocks, part, st)));
-    else CPMTP_TRY((launch_norm_bwd<bf16_t, 512>(a, L, blocks, part, st)));
-  }
+  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_bwd<float>(a, L, blocks, part, st));
+  else CPMTP_TRY(launch_norm_bwd<bf16_t>(a, L, blocks, part, st));
   if (part != nullptr)
     CPMTP_TRY(launch_pdl(norm::norm_dw_kernel, dim3((a.d + 31) / 32, 2), dim3(1024), 0, st, part, blocks, a.d, static_cast<bf16_t*>(a.dw_post),
                          static_cast<bf16_t*>(a.dw_pre), accum ? 1 : 0));

@@ -43,11 +43,57 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
                : "l"(p)
                : "memory");
 }
+// (the last argument names the type of the elements)
+__device__ __forceinline__ void load8_shared(const uint8_t* s, float (&v)[8], bf16_t) { unpack8(*reinterpret_cast<const uint4*>(s), v); }
+__device__ __forceinline__ void load8_shared(const uint8_t* s, float (&v)[8], float) {
+  const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + 16);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
 __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) { *reinterpret_cast<uint4*>(p) = pack8(v); }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
                "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
                : "memory");
+}
+
+// Two fp32 values in one register pair: sm_100 multiplies and adds pairs in one instruction, which is what counts where
+// the issue slots are what a kernel runs out of.  Each half is rounded as the single operation would be.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ f32x2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ float lo(f32x2 v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float hi(f32x2 v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Eight values, as pairs and one by one.
+__device__ __forceinline__ void pairs(const float (&v)[8], f32x2 (&p)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = pair(v[2 * k], v[2 * k + 1]);
+}
+__device__ __forceinline__ void singles(const f32x2 (&p)[4], float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = lo(p[k]);
+    v[2 * k + 1] = hi(p[k]);
+  }
 }
 
 // Whether rows of T at `p`, `ld` elements apart and `d` wide, can be read eight elements at a time.
