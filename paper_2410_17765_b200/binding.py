@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
 import os
 import struct
 from array import array
@@ -629,6 +630,7 @@ def distill_backward(h, W_head, E, W_g, x, teacher, saved: Saved, dsaved: Distil
 # Around the head in a training step: embedding lookup, norms with gate and residual addition, AdamW.
 
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_dtype_of = operator.attrgetter("dtype")
 _ADAMW_WORDS = ctypes.sizeof(CAdamWTensor) // 8      # a descriptor in 8-byte words: param, grad, master, m, v, m_exp, v_exp, numel, types, factors
 
 
@@ -790,31 +792,33 @@ def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block
     a.x, a.ld_x = _rows(x, size, dtype, dev, "x")
     N = size[0]
     res = {} if out is None else out
-    device = x.device
+    device, d = x.device, size[1]
     if block is None:
         res["x_out"] = x
+    elif (t := res.get("x_out")) is None:
+        t = res["x_out"] = torch.empty(size, dtype=dtype, device=device)
+        a.x_out, a.ld_x_out = t.data_ptr(), d
     else:
-        t = res.get("x_out")
-        if t is None:
-            t = res["x_out"] = torch.empty(size, dtype=dtype, device=device)
         a.x_out, a.ld_x_out = _rows(t, size, dtype, dev, "x_out")
     if w_pre is None:
         res["y"] = res["rstd_pre"] = None
     else:
-        t = res.get("y")
-        if t is None:
+        if (t := res.get("y")) is None:
             t = res["y"] = torch.empty(size, dtype=torch.bfloat16, device=device)
-        a.y, a.ld_y = _rows(t, size, torch.bfloat16, dev, "y")
-        t = res.get("rstd_pre")
-        if t is None:
+            a.y, a.ld_y = t.data_ptr(), d
+        else:
+            a.y, a.ld_y = _rows(t, size, torch.bfloat16, dev, "y")
+        if (t := res.get("rstd_pre")) is None:
             t = res["rstd_pre"] = torch.empty(N, dtype=torch.float32, device=device)
-        a.rstd_pre = _vector(t, N, torch.float32, dev, "rstd_pre")
+            a.rstd_pre = t.data_ptr()
+        else:
+            a.rstd_pre = _vector(t, N, torch.float32, dev, "rstd_pre")
     if w_post is None:
         res["rstd_post"] = None
+    elif (t := res.get("rstd_post")) is None:
+        t = res["rstd_post"] = torch.empty(N, dtype=torch.float32, device=device)
+        a.rstd_post = t.data_ptr()
     else:
-        t = res.get("rstd_post")
-        if t is None:
-            t = res["rstd_post"] = torch.empty(N, dtype=torch.float32, device=device)
         a.rstd_post = _vector(t, N, torch.float32, dev, "rstd_post")
     rc = load_library().cpmtp_norm_forward(ctypes.byref(a), _raw_stream(dev))
     if rc:
@@ -850,26 +854,37 @@ def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Option
         a.rstd_post = _vector(rstd_post, N, torch.float32, dev, "rstd_post")
     res = {} if out is None else out
 
-    def want(name, there, shape, kind):
+    # outputs: not there or not wanted, given, or new ones, which need no check
+    if "dx" in skip:
+        res["dx"] = None
+    elif (t := res.get("dx")) is None:
+        t = res["dx"] = torch.empty(size, dtype=dtype, device=device)
+        a.dx, a.ld_dx = t.data_ptr(), d
+    else:
+        a.dx, a.ld_dx = _rows(t, size, dtype, dev, "dx")
+    if block is None or "dblock" in skip:
+        res["dblock"] = None
+    elif (t := res.get("dblock")) is None:
+        t = res["dblock"] = torch.empty(size, dtype=bf16, device=device)
+        a.dblock, a.ld_dblock = t.data_ptr(), d
+    else:
+        a.dblock, a.ld_dblock = _rows(t, size, bf16, dev, "dblock")
+    if gate is None or "dgate" in skip:
+        res["dgate"] = None
+    elif (t := res.get("dgate")) is None:
+        t = res["dgate"] = torch.empty(gate.shape, dtype=bf16, device=device)
+        a.dgate, a.ld_dgate = t.data_ptr(), d if a.gate_kind == GATE_CHANNEL else 1
+    else:
+        a.dgate, a.ld_dgate = _rows(t, size, bf16, dev, "dgate") if a.gate_kind == GATE_CHANNEL else _row_gate(t, N, dev, "dgate")
+    for name, there in (("dw_post", w_post is not None), ("dw_pre", dy is not None)):
         if not there or name in skip:
             res[name] = None
-            return None
-        t = res.get(name)
-        if t is None:
-            _need(not accumulate or name[1] != "w", "accumulation needs dw_post and dw_pre in out")
-            t = res[name] = torch.empty(shape, dtype=kind, device=device)
-        return t
-
-    if (t := want("dx", True, size, dtype)) is not None:
-        a.dx, a.ld_dx = _rows(t, size, dtype, dev, "dx")
-    if (t := want("dblock", block is not None, size, bf16)) is not None:
-        a.dblock, a.ld_dblock = _rows(t, size, bf16, dev, "dblock")
-    if (t := want("dgate", gate is not None, None if gate is None else gate.shape, bf16)) is not None:
-        a.dgate, a.ld_dgate = _rows(t, size, bf16, dev, "dgate") if a.gate_kind == GATE_CHANNEL else _row_gate(t, N, dev, "dgate")
-    if (t := want("dw_post", w_post is not None, (d,), bf16)) is not None:
-        a.dw_post = _vector(t, d, bf16, dev, "dw_post")
-    if (t := want("dw_pre", dy is not None, (d,), bf16)) is not None:
-        a.dw_pre = _vector(t, d, bf16, dev, "dw_pre")
+        elif (t := res.get(name)) is None:
+            _need(not accumulate, "accumulation needs dw_post and dw_pre in out")
+            t = res[name] = torch.empty(d, dtype=bf16, device=device)
+            setattr(a, name, t.data_ptr())
+        else:
+            setattr(a, name, _vector(t, d, bf16, dev, name))
     if accumulate:
         a.flags = FLAG_ACCUM_GRADS
     lib, ref = load_library(), ctypes.byref(a)
@@ -901,27 +916,29 @@ class _Descriptors:
         if self.n:
             self.words[word::_ADAMW_WORDS] = array("q", values)
 
-    def put_grads(self, grads, dev: int, param_types: list, numels: Optional[list] = None) -> None:
-        """Addresses and types of the gradients, one per parameter of `numels` elements; None: no address."""
-        at, types, sizes = [], [], []
-        for g, pt in zip(grads, param_types):
-            if g is None:
-                at.append(0)
-                types.append(pt)
-                sizes.append(0)
-                continue
-            t = _TYPES.get(g.dtype)
-            if t is None or g.get_device() != dev or not g.is_contiguous():
+    def put_grads(self, grads, dev: int, param_types: Optional[list] = None, numels: Optional[list] = None) -> None:
+        """Addresses, sizes and types of the gradients, one per parameter of `numels` elements; None: no address."""
+        there = [g for g in grads if g is not None]
+        if there:
+            # one property of all of them at a time: half the cost of a loop over the tensors
+            kinds = list(map(_dtype_of, there))
+            same = kinds.count(kinds[0]) == len(kinds)
+            ok = kinds[0] in _TYPES if same else all(k in _TYPES for k in kinds)
+            if not ok or set(map(torch.Tensor.get_device, there)) != {dev} or not all(map(torch.Tensor.is_contiguous, there)):
                 raise CpmtpError("cpmtp: gradients must be contiguous bfloat16 or float32 tensors on the current CUDA device")
-            at.append(g.data_ptr())
-            types.append(pt | t << 32)
-            sizes.append(g.numel())
+            types = [_TYPES[kinds[0]] << 32] * len(kinds) if same else [_TYPES[k] << 32 for k in kinds]
+        else:
+            types = []
+        at, sizes = list(map(torch.Tensor.data_ptr, there)), list(map(torch.Tensor.numel, there))
+        if len(there) < len(grads):
+            where = [i for i, g in enumerate(grads) if g is not None]
+            at, sizes, types = ([dict(zip(where, v)).get(i, 0) for i in range(len(grads))] for v in (at, sizes, types))
         if numels is None:
             self.put(7, sizes)
-        elif sizes != numels and any(s != m and g is not None for s, m, g in zip(sizes, numels, grads)):
+        elif sizes != numels and any(g is not None and s != m for g, s, m in zip(grads, sizes, numels)):
             raise CpmtpError("cpmtp: a gradient must have its parameter's size")
         self.put(1, at)
-        self.put(8, types)
+        self.put(8, types if param_types is None else map(int.__or__, types, param_types))
 
 
 def _grad_descriptors(grads) -> tuple:
@@ -929,7 +946,7 @@ def _grad_descriptors(grads) -> tuple:
     _need(ref is not None, "there is no gradient")
     dev = _device(ref)
     table = _Descriptors(len(grads))
-    table.put_grads(grads, dev, [0] * len(grads))
+    table.put_grads(grads, dev)
     return table, dev, ref.device
 
 

@@ -6,6 +6,8 @@
 // kilobytes of reads under way: rows ahead are fetched with cp.async into a ring of kStages rows in shared memory while
 // the current row goes through its reductions.
 #pragma once
+#include <type_traits>
+
 #include "vec_io.cuh"
 
 namespace cpmtp {
@@ -24,7 +26,11 @@ template <class T>
 struct Rows {
   T* data;
   long long ld;
-  __device__ __forceinline__ T* at(long long i) const { return data + i * ld; }
+  __device__ __forceinline__ T* at(unsigned i) const { return data + i * static_cast<unsigned long long>(ld); }
+  // where in its 16-byte piece row i starts: the low bits of the address alone
+  __device__ __forceinline__ int offset(unsigned i) const {
+    return (static_cast<unsigned>(reinterpret_cast<uintptr_t>(data)) + i * static_cast<unsigned>(ld) * static_cast<unsigned>(sizeof(T))) & 15;
+  }
 };
 
 template <class S>
@@ -105,7 +111,7 @@ __device__ __forceinline__ void row_sum3(float (&v)[3], float (*red)[kMaxWarps],
 // ---- rows in shared memory ----
 // A row of d elements of T, wherever it starts, lies in at most d sizeof(T) / 16 + 1 aligned pieces of 16 bytes, and it is
 // these that are copied (the last one only as far as the row goes), so that rows of any width and stride move in whole
-// 16-byte accesses.  VEC (rows start on a piece, d = 256 W): a thread copies exactly what it will use itself, and no
+// 16-byte accesses; zeros follow up to column 256 W, so that what is read needs no bounds.  VEC (rows start on a piece, d = 256 W): a thread copies exactly what it will use itself, and no
 // barrier is spent on the copy.
 template <class T>
 __host__ __device__ constexpr int region_bytes(int threads) { return (threads * static_cast<int>(sizeof(T)) / 2 + 1) * 16; }
@@ -124,29 +130,36 @@ __device__ __forceinline__ void fetch_row(uint32_t region, const T* row, int t, 
     const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15);
     const char* base = reinterpret_cast<const char*>(row) - off;
     const int end = off + d * static_cast<int>(sizeof(T));
-    for (int j = t; j * 16 < end; j += tg) cp16(region + j * 16, base + j * 16, min(16, end - j * 16));
+    for (int j = t; j <= tg * kPer; j += tg) {
+      const int bytes = max(0, min(16, end - j * 16));    // zeros from the row's end to the region's
+      cp16(region + j * 16, bytes > 0 ? base + j * 16 : base, bytes);
+    }
   }
 }
 
-// This thread's eight columns of a fetched row; zeros past the row's end.
+// A thread's eight columns: 8t .. 8t+7 (VEC), else every 32nd of its warp's 256.
+template <bool VEC>
+__device__ __forceinline__ int col_of(int t, int k) { return VEC ? 8 * t + k : (t >> 5) * 256 + (t & 31) + 32 * k; }
+
+// This thread's columns of a fetched row; zeros past the row's end.
 template <bool VEC, class T>
-__device__ __forceinline__ void take8(const uint8_t* region, const T* row, int t, int tg, int d, f32x2 (&p)[4]) {
+__device__ __forceinline__ void take8(const uint8_t* region, const Rows<T>& rows, unsigned i, int t, f32x2 (&p)[4]) {
   float v[8];
   if (VEC) {
-    io::load8_shared(region + t * static_cast<int>(8 * sizeof(T)), v, T());
+    io::load8_shared(region + t * static_cast<int>(8 * sizeof(T)), v, std::remove_const_t<T>());
   } else {
-    const T* s = reinterpret_cast<const T*>(region + (reinterpret_cast<uintptr_t>(row) & 15));
+    const T* s = reinterpret_cast<const T*>(region + rows.offset(i)) + col_of<false>(t, 0);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = t + k * tg < d ? io::to_f(s[t + k * tg]) : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = io::to_f(s[32 * k]);
   }
   io::pairs(v, p);
 }
 template <bool VEC, class T>
-__device__ __forceinline__ void put8(T* row, int t, int tg, int d, const f32x2 (&p)[4]) {
+__device__ __forceinline__ void put8(T* row, int t, int d, const f32x2 (&p)[4]) {
   float v[8];
   io::singles(p, v);
   if (VEC) io::store8(row + 8 * t, v);
-  else io::store_cols<false>(row, t, tg, d, v);
+  else io::store_cols<false>(row + (t >> 5) * 256, t & 31, 32, d - (t >> 5) * 256, v);
 }
 __device__ __forceinline__ void fill8(f32x2 (&p)[4], float v) {
 #pragma unroll
@@ -175,13 +188,13 @@ struct Place {
 
 // A norm's weights, or `otherwise` where there is none.
 template <bool VEC>
-__device__ __forceinline__ void load_weights(const bf16_t* w, int t, int tg, int d, float otherwise, f32x2 (&p)[4]) {
+__device__ __forceinline__ void load_weights(const bf16_t* w, int t, int d, float otherwise, f32x2 (&p)[4]) {
   if (w == nullptr) {
     fill8(p, otherwise);
   } else {
     float v[8];
     if (VEC) io::load8(w + 8 * t, v);
-    else io::load_cols<false>(w, t, tg, d, v);
+    else io::load_cols<false>(w + (t >> 5) * 256, t & 31, 32, d - (t >> 5) * 256, v);
     io::pairs(v, p);
   }
 }
@@ -196,8 +209,8 @@ __device__ __forceinline__ float square_sum(const f32x2 (&v)[4]) {
 // One value per row, for the rows that a group of warps goes through: lane l holds that of the l-th row from here, so that a
 // row costs a shuffle and every 32nd one a load.
 template <class T>
-__device__ __forceinline__ float row_values(const T* at, long long ld, long long i, long long step, int N, int lane) {
-  const long long row = i + lane * step;
+__device__ __forceinline__ float row_values(const T* at, long long ld, unsigned i, unsigned step, unsigned N, int lane) {
+  const long long row = i + static_cast<long long>(lane) * step;
   return row < N ? io::to_f(at[row * ld]) : 0.f;
 }
 
@@ -215,12 +228,13 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
   uint8_t* ring = smem + at.group * STAGES * stage_bytes;
   const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || p.w_post != nullptr, has_y = ALL || p.w_pre != nullptr;
   const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
-  const long long step = static_cast<long long>(gridDim.x) * (ONE ? 1 : p.G);
-  long long i = static_cast<long long>(blockIdx.x) * (ONE ? 1 : p.G) + at.group;
+  const unsigned step = gridDim.x * (ONE ? 1 : p.G);      // rows; N < 2^31, so that a few steps past N do not wrap
+  unsigned i = blockIdx.x * (ONE ? 1 : p.G) + at.group;
   ptx::grid_dep_wait();
   const uint32_t ring_at = ptx::smem_u32(ring);
-  auto fetch = [&](long long row, int stage) {
-    if (row < p.N) {
+  const unsigned N = p.N;
+  auto fetch = [&](unsigned row, int stage) {
+    if (row < N) {
       uint32_t s = ring_at + stage * stage_bytes;
       fetch_row<VEC>(s, p.x.at(row), t, tg, d);
       s += region_bytes<S>(tg);
@@ -232,14 +246,14 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) fetch(i + s * step, s);
   f32x2 w_post[4], w_pre[4];
-  load_weights<VEC>(p.w_post, t, tg, d, 0.f, w_post);
-  load_weights<VEC>(p.w_pre, t, tg, d, 0.f, w_pre);
+  load_weights<VEC>(p.w_post, t, d, 0.f, w_post);
+  load_weights<VEC>(p.w_pre, t, d, 0.f, w_pre);
   float logits = 0.f;
   int stage = 0;
-  for (int it = 0; i < p.N; i += step, ++it) {
+  for (int it = 0; i < N; i += step, ++it) {
     float gl = 0.f;
     if (row_gate) {
-      if ((it & 31) == 0) logits = row_values(p.gate.data, p.gate.ld, i, step, p.N, at.lane);
+      if ((it & 31) == 0) logits = row_values(p.gate.data, p.gate.ld, i, step, N, at.lane);
       gl = __shfl_sync(0xffffffffu, logits, it & 31);
     }
     // the stage that this refills was read before the row barriers of the row before (one warp: before this one)
@@ -250,13 +264,13 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
     const uint8_t* s = ring + stage * stage_bytes;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     f32x2 x[4];
-    take8<VEC>(s, p.x.at(i), t, tg, d, x);
+    take8<VEC>(s, p.x, i, t, x);
     if (has_block) {
       s += region_bytes<S>(tg);
       f32x2 b[4], g[4];
-      take8<VEC>(s, p.block.at(i), t, tg, d, b);
+      take8<VEC>(s, p.block, i, t, b);
       if (channel) {
-        take8<VEC>(s + region_bytes<bf16_t>(tg), p.gate.at(i), t, tg, d, g);
+        take8<VEC>(s + region_bytes<bf16_t>(tg), p.gate, i, t, g);
 #pragma unroll
         for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
       } else {
@@ -272,7 +286,7 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
       const f32x2 scale = both(p.res_scale);
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = fma2(scale, x[k], mul2(g[k], b[k]));
-      put8<VEC>(p.x_out.at(i), t, tg, d, x);
+      put8<VEC>(p.x_out.at(i), t, d, x);
     }
     if (has_y) {
       const float rx = rsqrtf(fmaf(row_sum(square_sum(x), red[it & 1][1][at.rg], p.W, at.group, at.wg, at.lane), p.inv_d, p.eps));
@@ -280,7 +294,7 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
       const f32x2 rx2 = both(rx);
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], mul2(rx2, w_pre[k]));
-      put8<VEC>(p.y.at(i), t, tg, d, x);
+      put8<VEC>(p.y.at(i), t, d, x);
     }
     // without a reduction in this row nothing has yet kept the others from its stage
     if (!VEC && !has_post && !has_y) row_barrier(p.W, at.group);
@@ -304,15 +318,16 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   const int t = at.t, tg = at.tg, d = p.d;
   const int rs = region_bytes<S>(tg), rb16 = region_bytes<bf16_t>(tg), stage_bytes = bwd_stage_bytes<S>(tg);
   uint8_t* ring = smem + at.group * STAGES * stage_bytes;
-  const long long step = static_cast<long long>(gridDim.x) * (ONE ? 1 : p.G);
+  const unsigned step = gridDim.x * (ONE ? 1 : p.G);      // rows; N < 2^31, so that a few steps past N do not wrap
   const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || (has_block && p.w_post != nullptr);
   const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
   const bool has_y = ALL || p.dy.data != nullptr, has_dx_out = ALL || p.dx_out.data != nullptr;
   ptx::grid_dep_wait();
-  long long i = static_cast<long long>(blockIdx.x) * (ONE ? 1 : p.G) + at.group;
+  unsigned i = blockIdx.x * (ONE ? 1 : p.G) + at.group;
   const uint32_t ring_at = ptx::smem_u32(ring);
-  auto fetch = [&](long long row, int stage) {
-    if (row < p.N) {
+  const unsigned N = p.N;
+  auto fetch = [&](unsigned row, int stage) {
+    if (row < N) {
       uint32_t s = ring_at + stage * stage_bytes;
       fetch_row<VEC>(s, p.x_out.at(row), t, tg, d);
       if (has_dx_out) fetch_row<VEC>(s + rs, p.dx_out.at(row), t, tg, d);
@@ -328,15 +343,15 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   f32x2 w_pre[4], w_post[4], acc_pre[4], acc_post[4];
   fill8(acc_pre, 0.f);
   fill8(acc_post, 0.f);
-  load_weights<VEC>(has_y ? p.w_pre : nullptr, t, tg, d, 0.f, w_pre);
-  load_weights<VEC>(has_post ? p.w_post : nullptr, t, tg, d, 1.f, w_post);
+  load_weights<VEC>(has_y ? p.w_pre : nullptr, t, d, 0.f, w_pre);
+  load_weights<VEC>(has_post ? p.w_post : nullptr, t, d, 1.f, w_post);
   float rstds_pre = 0.f, rstds_post = 1.f, logits = 0.f;
   int stage = 0;
-  for (int it = 0; i < p.N; i += step, ++it) {
+  for (int it = 0; i < N; i += step, ++it) {
     if ((it & 31) == 0) {
-      if (has_y) rstds_pre = row_values(p.rstd_pre, 1, i, step, p.N, at.lane);
-      if (has_post) rstds_post = row_values(p.rstd_post, 1, i, step, p.N, at.lane);
-      if (row_gate) logits = row_values(p.gate.data, p.gate.ld, i, step, p.N, at.lane);
+      if (has_y) rstds_pre = row_values(p.rstd_pre, 1, i, step, N, at.lane);
+      if (has_post) rstds_post = row_values(p.rstd_post, 1, i, step, N, at.lane);
+      if (row_gate) logits = row_values(p.gate.data, p.gate.ld, i, step, N, at.lane);
     }
     const float rx = __shfl_sync(0xffffffffu, rstds_pre, it & 31), rb = __shfl_sync(0xffffffffu, rstds_post, it & 31);
     const float grow = row_gate ? sigmoid(__shfl_sync(0xffffffffu, logits, it & 31)) : 1.f;
@@ -348,16 +363,16 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
     const uint8_t* s = ring + stage * stage_bytes;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     f32x2 dy[4], x[4], a[4], b[4], g[4];
-    take8<VEC>(s, p.x_out.at(i), t, tg, d, x);
-    if (has_dx_out) take8<VEC>(s + rs, p.dx_out.at(i), t, tg, d, a);
+    take8<VEC>(s, p.x_out, i, t, x);
+    if (has_dx_out) take8<VEC>(s + rs, p.dx_out, i, t, a);
     else fill8(a, 0.f);
     s += 2 * rs;
-    if (has_y) take8<VEC>(s, p.dy.at(i), t, tg, d, dy);
+    if (has_y) take8<VEC>(s, p.dy, i, t, dy);
     else fill8(dy, 0.f);
-    if (has_block) take8<VEC>(s + rb16, p.block.at(i), t, tg, d, b);
+    if (has_block) take8<VEC>(s + rb16, p.block, i, t, b);
     else fill8(b, 0.f);
     if (channel) {
-      take8<VEC>(s + 2 * rb16, p.gate.at(i), t, tg, d, g);
+      take8<VEC>(s + 2 * rb16, p.gate, i, t, g);
 #pragma unroll
       for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
     } else {
@@ -391,10 +406,10 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
       g[k] = mul2(mul2(wb[k], dur), fma2(g[k], both(-1.f), both(1.f)));   // dgate
       x[k] = mul2(scale, tk);                                 // dx
     }
-    if (ALL || p.dx.data != nullptr) put8<VEC>(p.dx.at(i), t, tg, d, x);
-    if (ALL || p.dblock.data != nullptr) put8<VEC>(p.dblock.at(i), t, tg, d, a);
+    if (ALL || p.dx.data != nullptr) put8<VEC>(p.dx.at(i), t, d, x);
+    if (ALL || p.dblock.data != nullptr) put8<VEC>(p.dblock.at(i), t, d, a);
     if (ALL || p.dgate.data != nullptr) {
-      if (channel) put8<VEC>(p.dgate.at(i), t, tg, d, g);
+      if (channel) put8<VEC>(p.dgate.at(i), t, d, g);
       else if (t == 0) *p.dgate.at(i) = io::from_f<bf16_t>(grow * (1.f - grow) * dot);
     }
   }
@@ -406,7 +421,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   if (ONE) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int c = io::col_of<VEC>(t, tg, k);
+      const int c = col_of<VEC>(t, k);
       if (c < d) {
         out[c] = sum_post[k];
         out[d + c] = sum_pre[k];
@@ -420,7 +435,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   float* sums = reinterpret_cast<float*>(smem);               // [2][G][8 tg]
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int c = io::col_of<VEC>(t, tg, k);
+    const int c = col_of<VEC>(t, k);
     sums[at.group * 8 * tg + c] = sum_post[k];
     sums[(p.G + at.group) * 8 * tg + c] = sum_pre[k];
   }

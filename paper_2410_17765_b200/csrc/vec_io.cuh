@@ -104,9 +104,6 @@ inline bool vec_ok(const void* p, long long ld, long long d) {
 
 // The elements of a row of `d` that thread `t` of `threads` owns: columns 8t .. 8t+7 (VEC), else t, t + threads, ...
 // Columns past the end read as zero and are not written.
-template <bool VEC>
-__device__ __forceinline__ int col_of(int t, int threads, int k) { return VEC ? 8 * t + k : t + k * threads; }
-
 template <bool VEC, class T>
 __device__ __forceinline__ void load_cols(const T* row, int t, int threads, int d, float (&v)[8]) {
   if (VEC) {
