@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const int* __r
   __shared__ int warp_sums[kSortWarps];
   const int digits = 1 << bits, mask = digits - 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int j = threadIdx.x; j < kSortWarps * digits; j += kSortThreads) counts[j / digits][j % digits] = 0;
+  for (int j = threadIdx.x; j < kSortWarps * digits; j += kSortThreads) counts[j >> bits][j & mask] = 0;
   ptx::grid_dep_wait();
   __syncthreads();
   uint2 key[kSortRounds];
@@ -163,7 +163,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const int* __r
 // A warp takes kChunk sorted positions and one slab of columns, and adds up each run of equal tokens in it.  A run that lies
 // inside the chunk is written to the table; one that began before goes to head[chunk], one that began here and goes on to
 // tail[chunk], and embed_join_kernel adds those up.  Work per warp is the same however unequal the tokens' counts are.
+// Rows are read kAhead at a time, and with them the rows of the table that the runs ending among them are added to: a
+// warp that waited for one of those at every run's end spent three quarters of its time there.
 constexpr int kChunk = 32;
+constexpr int kAhead = 4;
 constexpr int kZeroRows = 32;     // rows of the table that a block looks at for rows without a token
 
 struct SumParams {
@@ -171,132 +174,190 @@ struct SumParams {
   long long ld, ld_table;
   bf16_t* dE;
   float *head, *tail;             // [chunks][slabs * kSlab]
-  int tokens, V, d, slabs, chunks, accum, sum_blocks;
+  int tokens, V, d, slabs, chunks, sum_blocks;
   float scale;
 };
 
-template <bool VEC>
-__device__ __forceinline__ void write_row(const SumParams& p, int row, int c0, int lane, const float (&acc)[8]) {
-  bf16_t* dst = p.dE + row * p.ld_table + c0;
+using io::f32x2;
+
+// A lane's eight columns of a slab as they were read: 8 lane .. 8 lane + 7 (VEC), else every 32nd.
+template <class T, bool VEC>
+struct Slab {
   float v[8];
-  if (p.accum) {
-    io::load_cols<VEC>(dst, lane, 32, p.d - c0, v);
+  __device__ __forceinline__ void read(const T* row, int lane, int left) { io::load_cols<VEC>(row, lane, 32, left, v); }
+  __device__ __forceinline__ void get(float (&out)[8]) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = fmaf(acc[k], p.scale, v[k]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = acc[k] * p.scale;
+    for (int k = 0; k < 8; ++k) out[k] = v[k];
   }
-  io::store_cols<VEC>(dst, lane, 32, p.d - c0, v);
+};
+template <>
+struct Slab<bf16_t, true> {       // packed until it is used: half the registers while it is on its way
+  uint4 v;
+  __device__ __forceinline__ void read(const bf16_t* row, int lane, int left) {
+    v = make_uint4(0u, 0u, 0u, 0u);
+    if (8 * lane < left) v = *reinterpret_cast<const uint4*>(row + 8 * lane);
+  }
+  __device__ __forceinline__ void get(float (&out)[8]) const { io::unpack8(v, out); }
+};
+
+template <bool VEC, bool ACCUM>
+__device__ __forceinline__ void write_slab(bf16_t* row, int lane, int left, float scale, const f32x2 (&acc)[4], const Slab<bf16_t, VEC>& before) {
+  float v[8], old[8];
+  io::singles(acc, v);
+  if (ACCUM) before.get(old);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = ACCUM ? fmaf(v[k], scale, old[k]) : v[k] * scale;
+  io::store_cols<VEC>(row, lane, 32, left, v);
 }
 
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) embed_sum_kernel(const T* __restrict__ dy, const SumParams p) {
+// Zeros for the rows of the table that no token names.
+template <bool VEC>
+__device__ __forceinline__ void zero_rows(const SumParams& p, int r0) {
+  __shared__ int present[kZeroRows];
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x < kZeroRows) present[threadIdx.x] = 0;
+  int lo = 0, hi = p.tokens;                     // first sorted position whose token is at least r0
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (static_cast<int>(p.sorted[mid].x) < r0) lo = mid + 1; else hi = mid;
+  }
+  __syncthreads();
+  for (int j = lo + threadIdx.x; j < p.tokens; j += 256) {
+    const int at = static_cast<int>(p.sorted[j].x) - r0;
+    if (at >= kZeroRows) break;
+    present[at] = 1;
+  }
+  __syncthreads();
+  const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < kZeroRows && r0 + r < p.V; ++r) {
+    if (present[r]) continue;
+    bf16_t* dst = p.dE + (r0 + r) * p.ld_table;
+    for (int c0 = (threadIdx.x >> 5) * kSlab; c0 < p.d; c0 += 8 * kSlab) io::store_cols<VEC>(dst + c0, lane, 32, p.d - c0, zeros);
+  }
+}
+
+template <class T, bool VEC, bool ACCUM>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) embed_sum_kernel(const T* __restrict__ dy, const SumParams p) {
   const int lane = threadIdx.x & 31;
   ptx::grid_dep_wait();
   if (static_cast<int>(blockIdx.x) >= p.sum_blocks) {
-    // rows without a token: zeros
-    __shared__ int present[kZeroRows];
-    const int r0 = (blockIdx.x - p.sum_blocks) * kZeroRows;
-    if (threadIdx.x < kZeroRows) present[threadIdx.x] = 0;
-    int lo = 0, hi = p.tokens;                   // first sorted position whose token is at least r0
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (static_cast<int>(p.sorted[mid].x) < r0) lo = mid + 1; else hi = mid;
-    }
-    __syncthreads();
-    for (int j = lo + threadIdx.x; j < p.tokens; j += 256) {
-      const int at = static_cast<int>(p.sorted[j].x) - r0;
-      if (at >= kZeroRows) break;
-      present[at] = 1;
-    }
-    __syncthreads();
-    const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < kZeroRows && r0 + r < p.V; ++r) {
-      if (present[r]) continue;
-      bf16_t* dst = p.dE + (r0 + r) * p.ld_table;
-      for (int c0 = (threadIdx.x >> 5) * kSlab; c0 < p.d; c0 += 8 * kSlab) io::store_cols<VEC>(dst + c0, lane, 32, p.d - c0, zeros);
-    }
+    zero_rows<VEC>(p, (blockIdx.x - p.sum_blocks) * kZeroRows);
     return;
   }
   const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   const long long chunk = item / p.slabs;
   if (chunk >= p.chunks) return;
-  const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab;
+  const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab, left = p.d - c0;
   const long long j0 = chunk * kChunk;
   uint2 kp = make_uint2(p.V, 0u);
   if (j0 + lane < p.tokens) kp = p.sorted[j0 + lane];
   const int before = j0 > 0 ? static_cast<int>(p.sorted[j0 - 1].x) : -1;
   const int after = j0 + kChunk < p.tokens ? static_cast<int>(p.sorted[j0 + kChunk].x) : -1;
-  float acc[8];
+  const int mine = static_cast<int>(kp.x);
+  int next = __shfl_down_sync(0xffffffffu, mine, 1);
+  if (lane == 31) next = after;
+  // by position: whether its run ends there; whether that run is all in this chunk and goes to the table
+  const unsigned ends = __ballot_sync(0xffffffffu, mine != next);
+  const bool first_run = mine == before;         // (only the run that the chunk begins with can have begun before)
+  const unsigned writes = __ballot_sync(0xffffffffu, mine != next && mine < p.V && !first_run);
+  const unsigned head = __ballot_sync(0xffffffffu, first_run);
+  const unsigned none = __ballot_sync(0xffffffffu, mine >= p.V);
+  const size_t part = (chunk * p.slabs + slab) * kSlab + 8 * lane;
+  f32x2 acc[4];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) acc[k] = 0.f;
-  int cur = __shfl_sync(0xffffffffu, static_cast<int>(kp.x), 0);
-  bool began_before = cur == before;
-  auto flush = [&](bool goes_on) {
-    if (cur >= p.V) return;
-    if (!began_before && !goes_on) {
-      write_row<VEC>(p, cur, c0, lane, acc);
-    } else {
-      float* to = (began_before ? p.head : p.tail) + (chunk * p.slabs + slab) * kSlab;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) to[lane * 8 + k] = acc[k];
-    }
-  };
-  constexpr int kAhead = 8;
+  for (int k = 0; k < 4; ++k) acc[k] = 0ull;
 #pragma unroll 1
   for (int k0 = 0; k0 < kChunk; k0 += kAhead) {
-    float v[kAhead][8];
+    Slab<T, VEC> rows[kAhead];
+    Slab<bf16_t, VEC> old[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int row = __shfl_sync(0xffffffffu, static_cast<int>(kp.x), k0 + u);
       const long long pos = __shfl_sync(0xffffffffu, kp.y, k0 + u);
-      if (row < p.V) {
-        io::load_cols<VEC>(dy + pos * p.ld + c0, lane, 32, p.d - c0, v[u]);
-      } else {
+      if (!((none >> (k0 + u)) & 1u)) rows[u].read(dy + pos * p.ld + c0, lane, left);
+    }
+    if (ACCUM) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[u][k] = 0.f;
+      for (int u = 0; u < kAhead; ++u) {
+        const long long row = __shfl_sync(0xffffffffu, mine, k0 + u);
+        if ((writes >> (k0 + u)) & 1u) old[u].read(p.dE + row * p.ld_table + c0, lane, left);
       }
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int row = __shfl_sync(0xffffffffu, static_cast<int>(kp.x), k0 + u);
-      if (row != cur) {
-        flush(false);
-        cur = row;
-        began_before = false;
+      const unsigned bit = 1u << (k0 + u);
+      if (none & bit) return;                    // padding sorts last
+      float v[8];
+      rows[u].get(v);
+      f32x2 add[4];
+      io::pairs(v, add);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+      for (int k = 0; k < 4; ++k) acc[k] = io::add2(acc[k], add[k]);
+      const long long row = __shfl_sync(0xffffffffu, mine, k0 + u);
+      if (ends & bit) {
+        if (writes & bit) {
+          write_slab<VEC, ACCUM>(p.dE + row * p.ld_table + c0, lane, left, p.scale, acc, old[u]);
+        } else {
+          io::singles(acc, v);
+          io::store8(p.head + part, v);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] = 0ull;
       }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] += v[u][k];
     }
   }
-  flush(cur == after);
+  if (!(ends >> 31)) {                           // the last run goes on
+    float v[8];
+    io::singles(acc, v);
+    io::store8(((head >> 31) ? p.head : p.tail) + part, v);
+  }
 }
 
 // Runs that cross a chunk's end: the warp of the chunk in which one begins adds its parts up in order.
-template <bool VEC>
+template <bool VEC, bool ACCUM>
 __global__ void __launch_bounds__(256) embed_join_kernel(const SumParams p) {
   const int lane = threadIdx.x & 31;
   const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   ptx::grid_dep_wait();
   const long long chunk = item / p.slabs;
   if (chunk + 1 >= p.chunks) return;
-  const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab;
+  const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab, left = p.d - c0;
   const long long j0 = chunk * kChunk;
-  const int row = static_cast<int>(p.sorted[j0 + kChunk - 1].x);
-  if (row >= p.V || static_cast<int>(p.sorted[j0 + kChunk].x) != row) return;
-  if (j0 > 0 && static_cast<int>(p.sorted[j0].x) == row && static_cast<int>(p.sorted[j0 - 1].x) == row) return;
+  const int row = static_cast<int>(p.sorted[j0 + kChunk - 1].x), first = static_cast<int>(p.sorted[j0].x);
+  const int before = j0 > 0 ? static_cast<int>(p.sorted[j0 - 1].x) : -1, after = static_cast<int>(p.sorted[j0 + kChunk].x);
+  if (row >= p.V || after != row || (first == row && before == row)) return;
   const size_t width = static_cast<size_t>(p.slabs) * kSlab;
-  float acc[8], v[8];
-  io::load8(p.tail + chunk * width + c0 + 8 * lane, acc);
-  for (long long c = chunk + 1; c < p.chunks && static_cast<int>(p.sorted[c * kChunk].x) == row; ++c) {
-    io::load8(p.head + c * width + c0 + 8 * lane, v);
+  const float* tail = p.tail + chunk * width + c0 + 8 * lane;
+  const float* head = p.head + (chunk + 1) * width + c0 + 8 * lane;
+  bf16_t* dst = p.dE + row * p.ld_table + c0;
+  float t[8];
+  Slab<bf16_t, VEC> old;
+  io::load8(tail, t);
+  if (ACCUM) old.read(dst, lane, left);
+  f32x2 acc[4];
+  io::pairs(t, acc);
+  // chunks that the run reaches into: 32 are looked at together, and their parts read four at a time
+  for (long long c = chunk + 1;; c += 32) {
+    const bool goes = c + lane < p.chunks && static_cast<int>(p.sorted[(c + lane) * kChunk].x) == row;
+    const unsigned mask = __ballot_sync(0xffffffffu, goes);
+    const int n = mask == 0xffffffffu ? 32 : __ffs(~mask) - 1;
+    for (int j = 0; j < n; j += 4) {
+      float v[4][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[k] += v[k];
+      for (int u = 0; u < 4; ++u)
+        if (j + u < n) io::load8(head + (j + u) * width, v[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (j + u >= n) break;
+        f32x2 add[4];
+        io::pairs(v[u], add);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] = io::add2(acc[k], add[k]);
+      }
+    }
+    if (n < 32) break;
+    head += 32 * width;
   }
-  write_row<VEC>(p, row, c0, lane, acc);
+  write_slab<VEC, ACCUM>(dst, lane, left, p.scale, acc, old);
 }
 
 }  // namespace embed

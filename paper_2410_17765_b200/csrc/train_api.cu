@@ -63,11 +63,17 @@ EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   return L;
 }
 
-template <class T, bool VEC>
-cudaError_t launch_embed_sum(const T* dy, const embed::SumParams& p, int zero_blocks, cudaStream_t st) {
-  const cudaError_t e = launch_pdl(embed::embed_sum_kernel<T, VEC>, dim3(p.sum_blocks + zero_blocks), dim3(256), 0, st, dy, p);
+template <class T, bool VEC, bool ACCUM>
+cudaError_t launch_embed_sum_as(const T* dy, const embed::SumParams& p, int zero_blocks, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(embed::embed_sum_kernel<T, VEC, ACCUM>, dim3(p.sum_blocks + zero_blocks), dim3(256), 0, st, dy, p);
   if (e != cudaSuccess || p.chunks < 2) return e;
-  return launch_pdl(embed::embed_join_kernel<VEC>, dim3(p.sum_blocks), dim3(256), 0, st, p);
+  return launch_pdl(embed::embed_join_kernel<VEC, ACCUM>, dim3(p.sum_blocks), dim3(256), 0, st, p);
+}
+template <class T>
+cudaError_t launch_embed_sum(const T* dy, const embed::SumParams& p, bool accum, int zero_blocks, cudaStream_t st) {
+  const bool vec = io::vec_ok<T>(dy, p.ld, p.d) && io::vec_ok<bf16_t>(p.dE, p.ld_table, p.d);
+  if (accum) return vec ? launch_embed_sum_as<T, true, true>(dy, p, 0, st) : launch_embed_sum_as<T, false, true>(dy, p, 0, st);
+  return vec ? launch_embed_sum_as<T, true, false>(dy, p, zero_blocks, st) : launch_embed_sum_as<T, false, false>(dy, p, zero_blocks, st);
 }
 
 // ------------------------------------------------------------------------------------------------ norms
@@ -422,18 +428,10 @@ int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const i
   embed::SumParams p;
   p.sorted = sorted; p.ld = s.ld_rows; p.ld_table = s.ld_table; p.dE = static_cast<bf16_t*>(dE);
   p.head = reinterpret_cast<float*>(ws + L.head); p.tail = reinterpret_cast<float*>(ws + L.tail);
-  p.tokens = s.T; p.V = s.V; p.d = s.d; p.slabs = L.slabs; p.chunks = L.chunks; p.accum = accum;
+  p.tokens = s.T; p.V = s.V; p.d = s.d; p.slabs = L.slabs; p.chunks = L.chunks;
   p.sum_blocks = static_cast<int>(sum_blocks); p.scale = s.scale;
-  const bool table_vec = io::vec_ok<bf16_t>(dE, s.ld_table, s.d);
-  if (s.type == CPMTP_F32) {
-    const float* from = static_cast<const float*>(dy);
-    if (table_vec && io::vec_ok<float>(dy, s.ld_rows, s.d)) CPMTP_TRY((launch_embed_sum<float, true>(from, p, zero_blocks, st)));
-    else CPMTP_TRY((launch_embed_sum<float, false>(from, p, zero_blocks, st)));
-  } else {
-    const bf16_t* from = static_cast<const bf16_t*>(dy);
-    if (table_vec && io::vec_ok<bf16_t>(dy, s.ld_rows, s.d)) CPMTP_TRY((launch_embed_sum<bf16_t, true>(from, p, zero_blocks, st)));
-    else CPMTP_TRY((launch_embed_sum<bf16_t, false>(from, p, zero_blocks, st)));
-  }
+  if (s.type == CPMTP_F32) CPMTP_TRY(launch_embed_sum(static_cast<const float*>(dy), p, accum, zero_blocks, st));
+  else CPMTP_TRY(launch_embed_sum(static_cast<const bf16_t*>(dy), p, accum, zero_blocks, st));
   return CPMTP_OK;
 }
 
