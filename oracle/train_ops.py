@@ -138,7 +138,7 @@ def encode(x, u, second):
     code = (small.astype(np.float32).view(np.uint32).astype(np.int64) + _blocks(np.asarray(u, np.int64))) >> drop
     code[(e == 0) | (e == 255)] = 0
     if not second:
-        code |= np.where(_blocks(np.asarray(x, np.float32)) < 0, 128, 0)
+        code |= np.where(np.signbit(_blocks(np.asarray(x, np.float32))), 128, 0)
     return code.reshape(-1)[:n].astype(np.uint8), e.astype(np.uint8)
 
 

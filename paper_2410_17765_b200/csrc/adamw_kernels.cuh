@@ -1,7 +1,7 @@
 // AdamW over many tensors in one launch, states in fp32 or 8 bits, and the norm of all gradients.
 //
 // The tensors' descriptors travel in the kernel's parameters (up to 32 KB), so a step is one launch with no copy to
-// the device, and can be captured.  Every block takes one run of kRun elements of one tensor; a warp takes 256 elements at a time, which
+// the device, and can be captured.  Every block takes one run of elements of one tensor; a warp takes 256 elements at a time, which
 // are also what shares an exponent in an 8-bit state.
 #pragma once
 #include "vec_io.cuh"
@@ -11,9 +11,12 @@ namespace adamw {
 
 using io::bf16_t;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kBlock = CPMTP_ADAMW_BLOCK;
-constexpr int kRun = 8192;                       // elements per thread block
+// Elements per thread block: short runs where there are few blocks, long ones for the kernel that has a ring to fill (a warp
+// of it goes through at most 32 blocks, whose exponents its lanes hold).
+constexpr int kShortRun = 2048, kRun = 8192, kLongRun = 32768;
+static_assert(kLongRun <= 32 * kWarps * kBlock, "one exponent to a lane");
 static_assert(kBlock == 32 * 8, "a warp holds one block of an 8-bit state");
 
 struct Tensor {
@@ -33,12 +36,14 @@ struct Hyper {
   float b1, omb1, b2, omb2, rsqrt_bc2, eps;
   uint32_t key;                                  // of the rounding noise: seed and step
   const float* coef;
+  float one;                                     // 1, see update_block8()
 };
 
 template <int CAP>
 struct Table {
   Hyper h;
   int count;
+  int run;                                       // elements to a thread block
   int first[CAP];                                // first run (thread block) of each tensor
   Tensor t[CAP];
 };
@@ -141,6 +146,13 @@ __device__ __forceinline__ void write_codes(uint8_t* base, int lane, int left, c
   }
 }
 
+// To a neighbouring bf16 value, the upper one with the probability that keeps the mean.  Infinities and NaN are left to
+// the conversion; the sum may carry a finite number to infinity.
+__device__ __forceinline__ float round_up_or_down(float p, uint32_t noise) {
+  const uint32_t bits = __float_as_uint(p);
+  return (bits & 0x7f800000u) == 0x7f800000u ? p : __uint_as_float((bits + ((noise >> 8) & 0xFFFFu)) & 0xFFFF0000u);
+}
+
 // One warp's 256 elements, `left` of them inside the tensor.
 template <int BITS, bool VEC>
 __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float coef, long long at, int left, int lane) {
@@ -199,7 +211,7 @@ __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float co
     for (int k = 0; k < 8; ++k) {
       cv[k] = ev > 0 && ev < 255 ? encode<kDropV>(fabsf(v[k]), to_v, noise[k] >> 13) : 0u;
       cm[k] = em > 0 && em < 255 ? encode<kDropM>(fabsf(m[k]), to_m, (noise[k] & 0xFFFFu) << 4) : 0u;
-      if (m[k] < 0.f) cm[k] |= 128u;
+      cm[k] |= (__float_as_uint(m[k]) >> 31) << 7;
       if (cv[k] == 0u) cm[k] = 0u;
     }
     write_codes<VEC>(m8, lane, left, cm);
@@ -218,60 +230,357 @@ __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float co
   } else {
     if (rounds_p) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // infinities and NaN are left to the conversion; the sum may carry a finite number to infinity
-        const uint32_t bits = __float_as_uint(p[k]);
-        if ((bits & 0x7f800000u) != 0x7f800000u) p[k] = __uint_as_float((bits + ((noise[k] >> 8) & 0xFFFFu)) & 0xFFFF0000u);
-      }
+      for (int k = 0; k < 8; ++k) p[k] = round_up_or_down(p[k], noise[k]);
     }
     write<VEC>(static_cast<bf16_t*>(t.param) + at, lane, left, p);
   }
 }
 
-template <int BITS, int CAP>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<CAP> tab) {
+// ---- 8-bit states, a whole block of a tensor that allows wide accesses ----
+// 10 bytes move per element and some 60 operations are due, which is what an SM issues in the time those bytes take: so
+// everything is counted.  Pairs are multiplied and added together (rounded as the single operations are); codes are
+// unpacked and packed in place, four to a word; and where the exponents leave room, the two powers of two of encode() and
+// decode() are one, and the decoder's goes into beta's product.  Both forms give the same bits.
+using io::add2;
+using io::both;
+using io::f32x2;
+using io::fma2;
+using io::mul2;
+
+// decode() is exact from here on up (the smallest code stays a normal number); its factors merge up to there
+constexpr int kMergeLow = 20, kMergeHigh = 141;
+__device__ __forceinline__ bool merges(int e) { return e == 0 || (e >= kMergeLow && e <= kMergeHigh); }
+// 2^(e - 15): from the code's units to values
+__device__ __forceinline__ float unit_of(int e) { return __uint_as_float(static_cast<uint32_t>(e + 112) << 23); }
+// 2^(15 - e): back
+__device__ __forceinline__ float inverse_unit_of(int e) { return __uint_as_float(static_cast<uint32_t>(142 - e) << 23); }
+
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// bytes 3 of four words, as one word
+__device__ __forceinline__ uint32_t tops(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// Blocks ahead are fetched with cp.async into a ring of kAhead blocks per warp, each lane its own share: 1.5 to 2.5 KB a
+// block is too little for a warp to have under way at a time (2.1 us of waiting per block, half of the bandwidth).
+constexpr int kAhead = 4;
+
+// Eight elements of either type as they lie in memory.
+struct Raw8 {
+  uint4 a, b;                     // b: of fp32 elements the upper four
+};
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int bytes) {
+  if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void fetch_raw(uint32_t dst, const void* p, bool f32, long long at) {
+  if (f32) {
+    copy_async(dst, static_cast<const float*>(p) + at, 16);
+    copy_async(dst + 512, static_cast<const float*>(p) + at + 4, 16);
+  } else {
+    copy_async(dst, static_cast<const bf16_t*>(p) + at, 16);
+  }
+}
+__device__ __forceinline__ Raw8 take_raw(const uint8_t* s, bool f32) {
+  Raw8 r;
+  r.a = *reinterpret_cast<const uint4*>(s);
+  if (f32) r.b = *reinterpret_cast<const uint4*>(s + 512);
+  return r;
+}
+__device__ __forceinline__ void numbers(const Raw8& r, bool f32, f32x2 (&v)[4]) {
+  if (f32) {
+    const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = io::pair(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
+  } else {
+    float f[8];
+    io::unpack8(r.a, f);
+    io::pairs(f, v);
+  }
+}
+
+struct Loaded8 {                  // a lane's share of a block as it is read
+  uint2 m, v;
+  Raw8 g, p;
+  int em, ev;
+};
+
+// A block in shared memory: m and v, 8 bytes a lane; then the gradient and what the update works on, 16 bytes a lane and
+// once more 16 for fp32.
+__host__ __device__ constexpr int stage_bytes(bool g32, bool p32) { return 512 + 512 * (2 + (g32 ? 1 : 0) + (p32 ? 1 : 0)); }
+
+__device__ __forceinline__ void fetch_block8(const Tensor& t, long long at, int lane, uint32_t stage) {
+  copy_async(stage + 8 * lane, static_cast<const uint8_t*>(t.m) + at + 8 * lane, 8);
+  copy_async(stage + 256 + 8 * lane, static_cast<const uint8_t*>(t.v) + at + 8 * lane, 8);
+  const uint32_t g = stage + 512 + 16 * lane, p = g + (t.grad_f32 ? 1024 : 512);
+  fetch_raw(g, t.grad, t.grad_f32, at + 8 * lane);
+  if (t.master != nullptr) fetch_raw(p, t.master, true, at + 8 * lane);
+  else fetch_raw(p, t.param, t.param_f32, at + 8 * lane);
+}
+__device__ __forceinline__ void take_block8(const Tensor& t, const uint8_t* stage, int lane, Loaded8& in) {
+  in.m = *reinterpret_cast<const uint2*>(stage + 8 * lane);
+  in.v = *reinterpret_cast<const uint2*>(stage + 256 + 8 * lane);
+  const uint8_t *g = stage + 512 + 16 * lane, *p = g + (t.grad_f32 ? 1024 : 512);
+  in.g = take_raw(g, t.grad_f32);
+  in.p = take_raw(p, t.param_f32 || t.master != nullptr);
+}
+
+__device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, float coef, long long at, int lane, const Loaded8& in) {
+  f32x2 g[4], m[4], v[4], p[4];
+  numbers(in.g, t.grad_f32, g);
+  numbers(in.p, t.param_f32 || t.master != nullptr, p);
+  const int em0 = in.em, ev0 = in.ev;         // the block's exponents
+  // codes to the places that encode() gives them in a number, with the sign on top for m
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t wm = k < 2 ? in.m.x : in.m.y, wv = k < 2 ? in.v.x : in.v.y;
+    const int j = 2 * (k & 1);
+    const auto place_m = [](uint32_t w, int j) {
+      return __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(w << (24 - 8 * j)) >> 4) & 0x87F00000u);
+    };
+    const auto place_v = [](uint32_t w, int j) { return __uint_as_float((j < 3 ? w << (19 - 8 * j) : w >> 5) & 0x07F80000u); };
+    m[k] = io::pair(place_m(wm, j), place_m(wm, j + 1));
+    v[k] = io::pair(place_v(wv, j), place_v(wv, j + 1));
+  }
+  if (merges(em0) && merges(ev0)) {
+    const f32x2 b1 = both(h.b1 * unit_of(em0)), b2 = both(h.b2 * unit_of(ev0));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = mul2(m[k], b1);
+      v[k] = mul2(v[k], b2);
+    }
+  } else {
+    const f32x2 huge = both(kHuge), um = both(block_unit(em0)), uv = both(block_unit(ev0)), b1 = both(h.b1), b2 = both(h.b2);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = mul2(mul2(mul2(m[k], huge), um), b1);
+      v[k] = mul2(mul2(mul2(v[k], huge), uv), b2);
+    }
+  }
+  const f32x2 coef2 = both(coef), omb1 = both(h.omb1), omb2 = both(h.omb2), step = both(-t.step_size), keep = both(t.keep);
+  const f32x2 bias = both(h.rsqrt_bc2), eps = both(h.eps);
+  // sums as products with a 1 that the compiler does not know: a packed sum of a packed product was found to come out as one
+  // operation with one rounding, for all the explicit roundings of the two
+  const f32x2 one = both(h.one);
+  float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x2 gk = mul2(g[k], coef2);
+    m[k] = fma2(m[k], one, mul2(gk, omb1));
+    v[k] = fma2(v[k], one, mul2(mul2(gk, omb2), gk));
+    top_m = max_nan(top_m, max_nan(fabsf(io::lo(m[k])), fabsf(io::hi(m[k]))));
+    top_v = max_nan(top_v, max_nan(fabsf(io::lo(v[k])), fabsf(io::hi(v[k]))));
+    const f32x2 below = fma2(io::pair(sqrt_approx(io::lo(v[k])), sqrt_approx(io::hi(v[k]))), bias, eps);
+    p[k] = fma2(p[k], keep, mul2(mul2(m[k], step), io::pair(rcp_approx(io::lo(below)), rcp_approx(io::hi(below)))));
+  }
+  const uint32_t top_mb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), top_vb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
+  const int em = min(block_exp<kDropM>(top_mb), 255), ev = min(block_exp<kDropV>(top_vb), 255);
+  // the first step of mix() for eight places that differ in their lowest three bits alone
+  const unsigned long long place = static_cast<unsigned long long>(t.place + at);
+  uint32_t base = (static_cast<uint32_t>(place) + 8 * lane) ^ h.key ^ (static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
+  base ^= base >> 16;
+  uint32_t noise[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    uint32_t x = (base ^ k) * 0x7feb352du;
+    x ^= x >> 15;
+    x *= 0x846ca68bu;
+    noise[k] = x ^ (x >> 16);
+  }
+  uint32_t cm[8], cv[8];          // codes in the words' top bytes
+  if (em >= 1 && em <= kMergeHigh && ev >= 1 && ev <= kMergeHigh) {
+    const f32x2 to_m = both(inverse_unit_of(em)), to_v = both(inverse_unit_of(ev));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x2 a = mul2(m[k], to_m), b = mul2(v[k], to_v);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t u = noise[2 * k + i];
+        const uint32_t sm = __float_as_uint(i == 0 ? io::lo(a) : io::hi(a)) + ((u & 0xFFFFu) << 4);
+        const uint32_t sv = __float_as_uint(i == 0 ? io::lo(b) : io::hi(b)) + (u >> 13);
+        cm[2 * k + i] = ((sm << 4) & 0x7F000000u) | (sm & 0x80FFFFFFu);
+        cv[2 * k + i] = sv << 5;
+      }
+    }
+  } else {
+    const float to_m = pow2(254 - min(em, 254)), to_v = pow2(254 - min(ev, 254));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float mk = (k & 1) ? io::hi(m[k / 2]) : io::lo(m[k / 2]), vk = (k & 1) ? io::hi(v[k / 2]) : io::lo(v[k / 2]);
+      cv[k] = (ev > 0 && ev < 255 ? encode<kDropV>(fabsf(vk), to_v, noise[k] >> 13) : 0u) << 24;
+      cm[k] = ((em > 0 && em < 255 ? encode<kDropM>(fabsf(mk), to_m, (noise[k] & 0xFFFFu) << 4) : 0u) | (__float_as_uint(mk) >> 31) << 7) << 24;
+    }
+  }
+  uint2 mw, vw;
+  mw.x = tops(cm[0], cm[1], cm[2], cm[3]);
+  mw.y = tops(cm[4], cm[5], cm[6], cm[7]);
+  vw.x = tops(cv[0], cv[1], cv[2], cv[3]);
+  vw.y = tops(cv[4], cv[5], cv[6], cv[7]);
+  // where v is zero m is too
+  const auto nonzero = [](uint32_t w) { return ((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) >> 7 & 0x01010101u) * 255u; };
+  mw.x &= nonzero(vw.x);
+  mw.y &= nonzero(vw.y);
+  *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.m) + at + 8 * lane) = mw;
+  *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at + 8 * lane) = vw;
+  if (lane == 0) {
+    t.m_exp[at / kBlock] = static_cast<uint8_t>(em);
+    t.v_exp[at / kBlock] = static_cast<uint8_t>(ev);
+  }
+  float q[8];
+  io::singles(p, q);
+  if (t.master != nullptr) write<true>(t.master + at, lane, kBlock, q);
+  if (t.param_f32) {
+    write<true>(static_cast<float*>(t.param) + at, lane, kBlock, q);
+  } else if (t.master != nullptr) {
+    write<true>(static_cast<bf16_t*>(t.param) + at, lane, kBlock, q);
+  } else {
+    const f32x2 sum = add2(add2(p[0], p[1]), add2(p[2], p[3]));
+    if (io::lo(sum) + io::hi(sum) == io::lo(sum) + io::hi(sum)) {
+      // no NaN among them (infinities take the noise unharmed): the rounded values are the words' upper halves
+      uint32_t w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(q[k]) + ((noise[k] >> 8) & 0xFFFFu);
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(t.param) + at + 8 * lane) =
+          make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) q[k] = round_up_or_down(q[k], noise[k]);
+      write<true>(static_cast<bf16_t*>(t.param) + at, lane, kBlock, q);
+    }
+  }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ Table<CAP> tab) {
   const int which = tensor_of(tab, blockIdx.x);
   const Tensor& t = tab.t[which];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const float coef = tab.h.coef != nullptr ? *tab.h.coef : 1.f;
   if (coef != coef) return;                      // the gradients were not finite
-  const long long start = static_cast<long long>(static_cast<int>(blockIdx.x) - tab.first[which]) * kRun;
+  const long long start = static_cast<long long>(static_cast<int>(blockIdx.x) - tab.first[which]) * tab.run;
 #pragma unroll 1
-  for (int b = warp * kBlock; b < kRun; b += kThreads / 32 * kBlock) {
+  for (int b = warp * kBlock; b < tab.run; b += kWarps * kBlock) {
     const long long at = start + b;
     if (at >= t.numel) break;
     const int left = static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock)));
-    if (t.vec) update<BITS, true>(t, tab.h, coef, at, left, lane);
-    else update<BITS, false>(t, tab.h, coef, at, left, lane);
+    if (t.vec) update<32, true>(t, tab.h, coef, at, left, lane);
+    else update<32, false>(t, tab.h, coef, at, left, lane);
   }
 }
 
+template <int CAP>
+__global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_constant__ Table<CAP> tab, const int bytes) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int which = tensor_of(tab, blockIdx.x);
+  const Tensor& t = tab.t[which];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long start = static_cast<long long>(static_cast<int>(blockIdx.x) - tab.first[which]) * tab.run;
+  const long long here = min(t.numel - start, static_cast<long long>(tab.run));
+  // blocks of this run: all, and those that are whole and go through shared memory; the warp's are warp, warp + kWarps, ...
+  const int blocks = static_cast<int>((here + kBlock - 1) / kBlock), whole = t.vec ? static_cast<int>(here / kBlock) : 0;
+  const uint8_t* ring = smem + warp * kAhead * bytes;
+  const uint32_t ring_at = ptx::smem_u32(ring);
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  const float coef = tab.h.coef != nullptr ? *tab.h.coef : 1.f;
+  // lane l: the exponents of the warp's l-th block
+  const int mine = warp + kWarps * lane;
+  int em = 0, ev = 0;
+  if (mine < whole) {
+    em = t.m_exp[start / kBlock + mine];
+    ev = t.v_exp[start / kBlock + mine];
+  }
+  const auto fetch = [&](int b, int stage) {
+    if (b < whole) fetch_block8(t, start + static_cast<long long>(b) * kBlock, lane, ring_at + stage * bytes);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < kAhead - 1; ++s) fetch(warp + s * kWarps, s);
+  if (coef != coef) {                            // the gradients were not finite: nothing changes
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    return;
+  }
+  int n = 0;
+#pragma unroll 1
+  for (int b = warp; b < whole; b += kWarps, ++n) {
+    fetch(b + (kAhead - 1) * kWarps, (n + kAhead - 1) % kAhead);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    Loaded8 in;
+    take_block8(t, ring + (n % kAhead) * bytes, lane, in);
+    in.em = __shfl_sync(0xffffffffu, em, n);
+    in.ev = __shfl_sync(0xffffffffu, ev, n);
+    update_block8(t, tab.h, coef, start + static_cast<long long>(b) * kBlock, lane, in);
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  // what is left: the tensor's last block, or all of one whose pointers do not allow wide accesses
+  for (int b = whole + (warp - whole % kWarps + kWarps) % kWarps; b < blocks; b += kWarps) {
+    const long long at = start + static_cast<long long>(b) * kBlock;
+    update<8, false>(t, tab.h, coef, at, static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock))), lane);
+  }
+}
+
+// A warp decodes kValueBlocks blocks, all read before the first is written.
+constexpr int kValueBlocks = 4;
 template <bool SECOND>
 __global__ void __launch_bounds__(kThreads) state_values_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps, long long n,
                                                                 bf16_t* __restrict__ out, int vec) {
   const int lane = threadIdx.x & 31;
-  const long long at = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kBlock;
+  const long long first = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (kValueBlocks * kBlock);
   ptx::grid_dep_wait();
-  if (at >= n) return;
-  const int left = static_cast<int>(min(n - at, static_cast<long long>(kBlock)));
-  const float unit = block_unit(exps[at / kBlock]);
-  uint32_t c[8];
-  float v[8];
-  if (vec) read_codes<true>(codes + at, lane, left, c); else read_codes<false>(codes + at, lane, left, c);
+  ptx::grid_dep_launch();
+  const auto value = [](uint32_t c, float unit) {
+    if (SECOND) return decode<kDropV>(c, unit);
+    const float a = decode<kDropM>(c & 127u, unit);
+    return c > 127u ? -a : a;
+  };
+  if (vec && first + kValueBlocks * kBlock <= n) {
+    uint2 r[kValueBlocks];
+    float unit[kValueBlocks];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    if (SECOND) {
-      v[k] = decode<kDropV>(c[k], unit);
-    } else {
-      const float a = decode<kDropM>(c[k] & 127u, unit);
-      v[k] = c[k] > 127u ? -a : a;
+    for (int j = 0; j < kValueBlocks; ++j) {
+      r[j] = *reinterpret_cast<const uint2*>(codes + first + j * kBlock + 8 * lane);
+      unit[j] = block_unit(exps[first / kBlock + j]);
     }
+#pragma unroll
+    for (int j = 0; j < kValueBlocks; ++j) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = value(((k < 4 ? r[j].x : r[j].y) >> (8 * (k & 3))) & 255u, unit[j]);
+      io::store8(out + first + j * kBlock + 8 * lane, v);
+    }
+    return;
   }
-  if (vec) write<true>(out + at, lane, left, v); else write<false>(out + at, lane, left, v);
+  for (int j = 0; j < kValueBlocks; ++j) {
+    const long long at = first + j * kBlock;
+    if (at >= n) return;
+    const int left = static_cast<int>(min(n - at, static_cast<long long>(kBlock)));
+    const float unit = block_unit(exps[at / kBlock]);
+    uint32_t c[8];
+    float v[8];
+    read_codes<false>(codes + at, lane, left, c);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = value(c[k], unit);
+    write<false>(out + at, lane, left, v);
+  }
 }
 
-// Sum of squares of every gradient: a block takes runs of kRun elements, in turn with the others.
+// Sum of squares of every gradient: a block takes runs of elements, in turn with the others.
 template <int CAP>
 __global__ void __launch_bounds__(kThreads) grad_square_kernel(const __grid_constant__ Table<CAP> tab, int runs, double* __restrict__ part) {
   __shared__ double sums[kThreads / 32];
@@ -280,12 +589,13 @@ __global__ void __launch_bounds__(kThreads) grad_square_kernel(const __grid_cons
 #pragma unroll
   for (int k = 0; k < 8; ++k) acc[k] = 0.f;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   for (int run = blockIdx.x; run < runs; run += gridDim.x) {
     const int which = tensor_of(tab, run);
     const Tensor& t = tab.t[which];
-    const long long start = static_cast<long long>(run - tab.first[which]) * kRun;
+    const long long start = static_cast<long long>(run - tab.first[which]) * tab.run;
 #pragma unroll 1
-    for (int b = warp * kBlock; b < kRun; b += kThreads / 32 * kBlock) {
+    for (int b = warp * kBlock; b < tab.run; b += kWarps * kBlock) {
       const long long at = start + b;
       if (at >= t.numel) break;
       const int left = static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock)));
@@ -313,6 +623,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* __res
   __shared__ double sums[kThreads / 32];
   double s = 0.0;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   for (int j = threadIdx.x; j < parts; j += kThreads) s += part[j];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);

@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const bf16_t* __restrict
   const long long i0 = item / slabs * kFwdRows;
   const int c0 = static_cast<int>(item % slabs) * kSlab;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   if (i0 >= tokens) return;
   int row = V;
   if (lane < kFwdRows && i0 + lane < tokens) row = row_of(x[i0 + lane], V, dev_status);
@@ -71,6 +72,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_hist_kernel(const int* __r
   const int digits = 1 << bits;
   for (int t = threadIdx.x; t < digits; t += kSortThreads) h[t] = 0;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   __syncthreads();
   for (int r = 0; r < kSortRounds; ++r) {
     const long long i = static_cast<long long>(blockIdx.x) * kSortKeys + r * kSortThreads + threadIdx.x;
@@ -95,6 +97,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const int* __r
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int j = threadIdx.x; j < kSortWarps * digits; j += kSortThreads) counts[j >> bits][j & mask] = 0;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   __syncthreads();
   uint2 key[kSortRounds];
   int rank[kSortRounds];
@@ -151,10 +154,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const int* __r
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const long long i = static_cast<long long>(blockIdx.x) * kSortKeys + warp * (32 * kSortRounds) + r * 32 + lane;
+    int next = -1;                               // where this key is counted for the next pass
     if (i < tokens) {
       const int to = counts[warp][(key[r].x >> shift) & mask] + rank[r];
       out[to] = key[r];
-      if (hist_next != nullptr) atomicAdd(&hist_next[static_cast<size_t>(to / kSortKeys) * digits + ((key[r].x >> (shift + bits)) & mask)], 1);
+      next = (to / kSortKeys << bits) + static_cast<int>(key[r].x >> (shift + bits) & mask);
+    }
+    if (hist_next != nullptr) {
+      // one atomic for the keys of a warp that count at the same place: frequent tokens have small ids, and so one digit here
+      const unsigned peers = __match_any_sync(0xffffffffu, next);
+      if (next >= 0 && lane == __ffs(peers) - 1) atomicAdd(&hist_next[next], __popc(peers));
     }
   }
 }
@@ -240,6 +249,7 @@ template <class T, bool VEC, bool ACCUM>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) embed_sum_kernel(const T* __restrict__ dy, const SumParams p) {
   const int lane = threadIdx.x & 31;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   if (static_cast<int>(blockIdx.x) >= p.sum_blocks) {
     zero_rows<VEC>(p, (blockIdx.x - p.sum_blocks) * kZeroRows);
     return;
@@ -318,6 +328,7 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const SumParams p) {
   const int lane = threadIdx.x & 31;
   const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const long long chunk = item / p.slabs;
   if (chunk + 1 >= p.chunks) return;
   const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab, left = p.d - c0;

@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
   const unsigned step = gridDim.x * (ONE ? 1 : p.G);      // rows; N < 2^31, so that a few steps past N do not wrap
   unsigned i = blockIdx.x * (ONE ? 1 : p.G) + at.group;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const uint32_t ring_at = ptx::smem_u32(ring);
   const unsigned N = p.N;
   auto fetch = [&](unsigned row, int stage) {
@@ -323,6 +324,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
   const bool has_y = ALL || p.dy.data != nullptr, has_dx_out = ALL || p.dx_out.data != nullptr;
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   unsigned i = blockIdx.x * (ONE ? 1 : p.G) + at.group;
   const uint32_t ring_at = ptx::smem_u32(ring);
   const unsigned N = p.N;
@@ -453,6 +455,7 @@ __global__ void __launch_bounds__(1024) norm_dw_kernel(const float* __restrict__
                                                        int accum) {
   __shared__ float s[32][33];
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int which = blockIdx.y, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
   bf16_t* out = which ? dw_pre : dw_post;
   if (out == nullptr) return;

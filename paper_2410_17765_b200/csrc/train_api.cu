@@ -29,6 +29,18 @@ int check_device(DeviceInfo** out) {
 bool known_type(int t) { return t == CPMTP_BF16 || t == CPMTP_F32; }
 size_t type_bytes(int t) { return t == CPMTP_F32 ? 4 : 2; }
 
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+template <class K>
+cudaError_t allow_smem(K* kernel, bool (&done)[64], int bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_cache_mutex);
+  if (done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+
 // ------------------------------------------------------------------------------------------- embedding
 int check_embed(const cpmtp_embed_shape* s) {
   if (s == nullptr) return CPMTP_ERR_NULL;
@@ -155,18 +167,6 @@ norm::Params<S> norm_params(const cpmtp_norm_args& a, const NormLayout& L) {
 template <class T>
 bool rows_vec(const cpmtp_rows& r, int d) { return d % 256 == 0 && (r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d)); }
 
-// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
-template <class K>
-cudaError_t allow_smem(K* kernel, bool (&done)[64], int bytes) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  std::lock_guard<std::mutex> lock(g_cache_mutex);
-  if (done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  done[dev] = e == cudaSuccess;
-  return e;
-}
-
 template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
 cudaError_t launch_norm_fwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
   constexpr int kStages = fwd_stages<S, MAXT>();
@@ -257,12 +257,21 @@ int check_adamw(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ad
   return CPMTP_OK;
 }
 
+// Elements per thread block: `most`, unless that leaves the SMs with few blocks each.
+int run_length(const cpmtp_adamw_tensor* tensors, int32_t count, int most, int sms) {
+  long long total = 0;
+  for (int i = 0; i < count; ++i) total += tensors[i].numel;
+  if (total >= 16ll * sms * most) return most;
+  return total >= 4ll * sms * adamw::kRun ? adamw::kRun : adamw::kShortRun;
+}
+
 // Launches over tables of at most CAP tensors; `fn(table, runs)` enqueues one of them.
 template <int CAP, class Fill, class Fn>
-int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hyper& h, Fill fill, Fn fn) {
+int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hyper& h, int run, Fill fill, Fn fn) {
   adamw::Table<CAP> tab;
   tab.h = h;
   tab.count = 0;
+  tab.run = run;
   long long place = 0, runs = 0;
   constexpr long long kMaxRuns = 1ll << 30;
   for (int i = 0; i < count; ++i) {
@@ -270,7 +279,7 @@ int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hy
     const long long here = place;
     place += (t.numel + adamw::kBlock - 1) / adamw::kBlock * adamw::kBlock;
     if (t.grad == nullptr || t.numel == 0) continue;
-    const long long more = (t.numel + adamw::kRun - 1) / adamw::kRun;
+    const long long more = (t.numel + run - 1) / run;
     if (tab.count == CAP || runs + more > kMaxRuns) {
       const int rc = fn(tab, static_cast<int>(runs));
       if (rc != CPMTP_OK) return rc;
@@ -286,7 +295,7 @@ int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hy
 }
 
 template <int CAP>
-int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, cudaStream_t st) {
+int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, int sms, cudaStream_t st) {
   adamw::Hyper h;
   h.b1 = static_cast<float>(hyper.beta1);
   h.omb1 = static_cast<float>(1.0 - hyper.beta1);
@@ -298,9 +307,10 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
   h.eps = static_cast<float>(hyper.eps);
   h.key = adamw::mix(adamw::mix(hyper.seed) ^ static_cast<uint32_t>(hyper.step));
   h.coef = hyper.coef;
+  h.one = 1.f;
   const size_t state = hyper.state_bits == 8 ? 8 : 32;
   return for_tables<CAP>(
-      tensors, count, h,
+      tensors, count, h, run_length(tensors, count, hyper.state_bits == 8 ? adamw::kLongRun : adamw::kRun, sms),
       [&](const cpmtp_adamw_tensor& in, long long place, adamw::Tensor& out) {
         out.param = in.param; out.grad = in.grad; out.master = in.master;
         out.m = in.m; out.v = in.v; out.m_exp = in.m_exp; out.v_exp = in.v_exp;
@@ -313,8 +323,20 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
       },
       [&](const adamw::Table<CAP>& tab, int runs) -> int {
         ProfScope prof(CPMTP_STAGE_ADAMW, st);
-        if (hyper.state_bits == 8) CPMTP_TRY(launch_pdl(adamw::adamw_kernel<8, CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
-        else CPMTP_TRY(launch_pdl(adamw::adamw_kernel<32, CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
+        if (hyper.state_bits != 8) {
+          CPMTP_TRY(launch_pdl(adamw::adamw32_kernel<CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
+          return CPMTP_OK;
+        }
+        bool g32 = false, p32 = false;
+        for (int i = 0; i < tab.count; ++i) {
+          g32 |= tab.t[i].grad_f32 != 0;
+          p32 |= tab.t[i].param_f32 != 0 || tab.t[i].master != nullptr;
+        }
+        constexpr int kPer = adamw::kWarps * adamw::kAhead;
+        static bool done[64] = {};
+        CPMTP_TRY(allow_smem(adamw::adamw8_kernel<CAP>, done, kPer * adamw::stage_bytes(true, true)));
+        const int bytes = adamw::stage_bytes(g32, p32);
+        CPMTP_TRY(launch_pdl(adamw::adamw8_kernel<CAP>, dim3(runs), dim3(adamw::kThreads), kPer * bytes, st, tab, bytes));
         return CPMTP_OK;
       });
 }
@@ -322,10 +344,10 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
 int grad_blocks(int sms) { return 4 * sms; }
 
 template <int CAP>
-int grad_squares(const cpmtp_adamw_tensor* tensors, int32_t count, int sms, double* part, int* parts, cudaStream_t st) {
+int grad_squares(const cpmtp_adamw_tensor* tensors, int32_t count, int sms, double* part, int most, int* parts, cudaStream_t st) {
   adamw::Hyper h = {};
   return for_tables<CAP>(
-      tensors, count, h,
+      tensors, count, h, run_length(tensors, count, adamw::kRun, sms),
       [&](const cpmtp_adamw_tensor& in, long long, adamw::Tensor& out) {
         std::memset(&out, 0, sizeof(out));
         out.grad = in.grad; out.numel = in.numel; out.grad_f32 = in.grad_type == CPMTP_F32;
@@ -333,6 +355,7 @@ int grad_squares(const cpmtp_adamw_tensor* tensors, int32_t count, int sms, doub
       },
       [&](const adamw::Table<CAP>& tab, int runs) -> int {
         const int blocks = runs < grad_blocks(sms) ? runs : grad_blocks(sms);
+        if (*parts + blocks > most) return CPMTP_ERR_LIMIT;
         CPMTP_TRY(launch_pdl(adamw::grad_square_kernel<CAP>, dim3(blocks), dim3(adamw::kThreads), 0, st, tab, runs, part + *parts));
         *parts += blocks;
         return CPMTP_OK;
@@ -530,8 +553,8 @@ int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpm
   const int rd = check_device(&di);
   if (rd != CPMTP_OK) return rd;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  return count <= adamw::kSmallTable ? adamw_step<adamw::kSmallTable>(tensors, count, *hyper, st)
-                                     : adamw_step<adamw::kLargeTable>(tensors, count, *hyper, st);
+  return count <= adamw::kSmallTable ? adamw_step<adamw::kSmallTable>(tensors, count, *hyper, di->sms, st)
+                                     : adamw_step<adamw::kLargeTable>(tensors, count, *hyper, di->sms, st);
 }
 
 int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,
@@ -544,7 +567,8 @@ int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, 
   const int rd = check_device(&di);
   if (rd != CPMTP_OK) return rd;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const dim3 grid(static_cast<unsigned>((n + 8 * adamw::kBlock - 1) / (8 * adamw::kBlock)));
+  constexpr long long kPer = 8ll * adamw::kValueBlocks * adamw::kBlock;
+  const dim3 grid(static_cast<unsigned>((n + kPer - 1) / kPer));
   const int vec = aligned(codes, 8) && aligned(out_bf16, 16);
   const uint8_t* c = static_cast<const uint8_t*>(codes);
   bf16_t* out = static_cast<bf16_t*>(out_bf16);
@@ -575,10 +599,11 @@ int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_
   if (rd != CPMTP_OK) return rd;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   double* part = static_cast<double*>(workspace);
+  const int most = static_cast<int>(workspace_bytes / sizeof(double) < (1u << 30) ? workspace_bytes / sizeof(double) : 1u << 30);
   int parts = 0;
   ProfScope prof(CPMTP_STAGE_GRAD_NORM, st);
-  const int rs = count <= adamw::kSmallTable ? grad_squares<adamw::kSmallTable>(tensors, count, di->sms, part, &parts, st)
-                                             : grad_squares<adamw::kLargeTable>(tensors, count, di->sms, part, &parts, st);
+  const int rs = count <= adamw::kSmallTable ? grad_squares<adamw::kSmallTable>(tensors, count, di->sms, part, most, &parts, st)
+                                             : grad_squares<adamw::kLargeTable>(tensors, count, di->sms, part, most, &parts, st);
   if (rs != CPMTP_OK) return rs;
   CPMTP_TRY(launch_pdl(adamw::grad_norm_kernel, dim3(1), dim3(adamw::kThreads), 0, st, part, parts, max_norm, norm, coef));
   return CPMTP_OK;
