@@ -265,9 +265,9 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // bytes 3 of four words, as one word
@@ -382,8 +382,8 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
     const f32x2 gk = mul2(g[k], coef2);
     m[k] = fma2(m[k], one, mul2(gk, omb1));
     v[k] = fma2(v[k], one, mul2(mul2(gk, omb2), gk));
-    top_m = max_nan(top_m, max_nan(fabsf(io::lo(m[k])), fabsf(io::hi(m[k]))));
-    top_v = max_nan(top_v, max_nan(fabsf(io::lo(v[k])), fabsf(io::hi(v[k]))));
+    top_m = max_nan(top_m, fabsf(io::lo(m[k])), fabsf(io::hi(m[k])));
+    top_v = max_nan(top_v, io::lo(v[k]), io::hi(v[k]));
     const f32x2 below = fma2(io::pair(sqrt_approx(io::lo(v[k])), sqrt_approx(io::hi(v[k]))), bias, eps);
     p[k] = fma2(p[k], keep, mul2(mul2(m[k], step), io::pair(rcp_approx(io::lo(below)), rcp_approx(io::hi(below)))));
   }
@@ -409,11 +409,12 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
       const f32x2 a = mul2(m[k], to_m), b = mul2(v[k], to_v);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        // encode()'s sums, moved up until the code is the top byte (what is below the noise then does not carry)
         const uint32_t u = noise[2 * k + i];
-        const uint32_t sm = __float_as_uint(i == 0 ? io::lo(a) : io::hi(a)) + ((u & 0xFFFFu) << 4);
-        const uint32_t sv = __float_as_uint(i == 0 ? io::lo(b) : io::hi(b)) + (u >> 13);
-        cm[2 * k + i] = ((sm << 4) & 0x7F000000u) | (sm & 0x80FFFFFFu);
-        cv[2 * k + i] = sv << 5;
+        const uint32_t am = __float_as_uint(i == 0 ? io::lo(a) : io::hi(a)), av = __float_as_uint(i == 0 ? io::lo(b) : io::hi(b));
+        const uint32_t sm = (am << 4) + __byte_perm(u, 0u, 0x4104);
+        cm[2 * k + i] = (sm & 0x7FFFFFFFu) | (am & 0x80000000u);
+        cv[2 * k + i] = (av << 5) + (u >> 8);
       }
     }
   } else {
@@ -453,7 +454,7 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
       // no NaN among them (infinities take the noise unharmed): the rounded values are the words' upper halves
       uint32_t w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(q[k]) + ((noise[k] >> 8) & 0xFFFFu);
+      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(q[k]) + __byte_perm(noise[k], 0u, 0x4421);
       *reinterpret_cast<uint4*>(static_cast<bf16_t*>(t.param) + at + 8 * lane) =
           make_uint4(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632), __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
     } else {
