@@ -75,6 +75,39 @@ EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   return L;
 }
 
+template <int CTAS, int KPT>
+cudaError_t sort_in_cluster_as(const int* x, uint2* out, int T, int V, const EmbedLayout& L, int* dev_status, cudaStream_t st) {
+  constexpr int kBytes = embed::cluster_sort_bytes(CTAS, KPT);
+  static bool done[64] = {};
+  auto* kernel = embed::embed_sort_cluster_kernel<CTAS, KPT>;
+  const cudaError_t e = allow_smem(kernel, done, kBytes);
+  return e != cudaSuccess ? e : launch_clusters(CTAS, kernel, dim3(CTAS), dim3(embed::kClusterThreads), kBytes, st, x, out, T, V, L.bits, L.passes, dev_status);
+}
+cudaError_t sort_in_cluster(const int* x, uint2* out, int T, int V, const EmbedLayout& L, int* dev_status, cudaStream_t st) {
+  constexpr int kOne = embed::kClusterThreads, kAll = kOne * embed::kClusterSize;
+  if (T <= kOne) return sort_in_cluster_as<1, 1>(x, out, T, V, L, dev_status, st);
+  if (T <= kAll) return sort_in_cluster_as<embed::kClusterSize, 1>(x, out, T, V, L, dev_status, st);
+  if (T <= 2 * kAll) return sort_in_cluster_as<embed::kClusterSize, 2>(x, out, T, V, L, dev_status, st);
+  if (T <= 4 * kAll) return sort_in_cluster_as<embed::kClusterSize, 4>(x, out, T, V, L, dev_status, st);
+  return sort_in_cluster_as<embed::kClusterSize, 8>(x, out, T, V, L, dev_status, st);
+}
+
+// The result is in keys[(L.passes + 1) % 2].
+cudaError_t sort_in_memory(const int* x, uint2* const (&keys)[2], int* hists, int T, int V, const EmbedLayout& L, int* dev_status, cudaStream_t st) {
+  int* hist[3];
+  for (int j = 0; j < 3; ++j) hist[j] = hists + j * (static_cast<size_t>(L.blocks) << L.bits);
+  const dim3 grid(L.blocks), threads(embed::kSortThreads);
+  cudaError_t e = launch_pdl(embed::embed_hist_kernel, grid, threads, 0, st, x, T, V, L.bits, hist[0], L.passes > 1 ? hist[1] : nullptr, dev_status);
+  for (int pass = 0; pass < L.passes && e == cudaSuccess; ++pass) {
+    int* next = pass + 1 < L.passes ? hist[(pass + 1) % 3] : nullptr;
+    int* zero = pass + 2 < L.passes ? hist[(pass + 2) % 3] : nullptr;
+    if (pass == 0) e = launch_pdl(embed::embed_sort_kernel<true>, grid, threads, 0, st, x, nullptr, keys[0], T, V, L.bits, 0, hist[0], next, zero);
+    else e = launch_pdl(embed::embed_sort_kernel<false>, grid, threads, 0, st, nullptr, keys[(pass + 1) % 2], keys[pass % 2], T, V, L.bits,
+                        pass * L.bits, hist[pass % 3], next, zero);
+  }
+  return e;
+}
+
 template <class T, bool VEC, bool ACCUM>
 cudaError_t launch_embed_sum_as(const T* dy, const embed::SumParams& p, int zero_blocks, cudaStream_t st) {
   const cudaError_t e = launch_pdl(embed::embed_sum_kernel<T, VEC, ACCUM>, dim3(p.sum_blocks + zero_blocks), dim3(256), 0, st, dy, p);
@@ -431,22 +464,14 @@ int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const i
   ProfScope prof(CPMTP_STAGE_EMBED_GRAD, st);
   const uint2* sorted = nullptr;
   if (s.T > 0) {
-    int* hist[3];
-    for (int j = 0; j < 3; ++j) hist[j] = reinterpret_cast<int*>(ws + L.hist) + j * (static_cast<size_t>(L.blocks) << L.bits);
     uint2* keys[2] = {reinterpret_cast<uint2*>(ws + L.keys), reinterpret_cast<uint2*>(ws + L.keys) + s.T};
-    const dim3 grid(L.blocks), threads(embed::kSortThreads);
-    CPMTP_TRY(launch_pdl(embed::embed_hist_kernel, grid, threads, 0, st, x, s.T, s.V, L.bits, hist[0], L.passes > 1 ? hist[1] : nullptr,
-                         dev_status));
-    for (int pass = 0; pass < L.passes; ++pass) {
-      int* next = pass + 1 < L.passes ? hist[(pass + 1) % 3] : nullptr;
-      int* zero = pass + 2 < L.passes ? hist[(pass + 2) % 3] : nullptr;
-      if (pass == 0)
-        CPMTP_TRY(launch_pdl(embed::embed_sort_kernel<true>, grid, threads, 0, st, x, nullptr, keys[0], s.T, s.V, L.bits, 0, hist[0], next, zero));
-      else
-        CPMTP_TRY(launch_pdl(embed::embed_sort_kernel<false>, grid, threads, 0, st, nullptr, keys[(pass + 1) % 2], keys[pass % 2], s.T, s.V,
-                             L.bits, pass * L.bits, hist[pass % 3], next, zero));
+    if (s.T <= embed::kClusterThreads * embed::kClusterSize * 8) {
+      sorted = keys[0];
+      CPMTP_TRY(sort_in_cluster(x, keys[0], s.T, s.V, L, dev_status, st));
+    } else {
+      sorted = keys[(L.passes + 1) % 2];
+      CPMTP_TRY(sort_in_memory(x, keys, reinterpret_cast<int*>(ws + L.hist), s.T, s.V, L, dev_status, st));
     }
-    sorted = keys[(L.passes + 1) % 2];
   }
   embed::SumParams p;
   p.sorted = sorted; p.ld = s.ld_rows; p.ld_table = s.ld_table; p.dE = static_cast<bf16_t*>(dE);

@@ -67,6 +67,19 @@ def test_gradient(n, V, d, dtype, accumulate):
         assert torch.equal(got[rest], base[rest])
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 8192, 8193, 16385, 33000, 65536, 65537, 150000])
+@pytest.mark.parametrize("V", [300, 40000, 262144])
+def test_gradient_over_the_ways_to_sort(n, V):
+    """One block, a cluster of eight with one to eight keys a thread, several launches; one to three digits."""
+    from paper_2410_17765_b200 import binding
+
+    rng = np.random.default_rng(n + V)
+    x = tokens(rng, n, V, 0.05)
+    dy = bf16(rng.normal(size=(n, 8)))
+    got = binding.embed_backward(dy, torch.from_numpy(x).cuda(), V, out=torch.full((V, 8), float("nan"), dtype=torch.bfloat16, device="cuda"))
+    check_grad(got, dy, x, V, 1.0)
+
+
 @pytest.mark.parametrize("kind", ["one token", "all padding", "two interleaved", "sorted", "every row once"])
 def test_gradient_of_extreme_token_counts(kind):
     from paper_2410_17765_b200 import binding
