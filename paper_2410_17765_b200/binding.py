@@ -750,6 +750,13 @@ def embed_workspace_bytes(T: int, V: int, d: int) -> int:
     return int(load_library().cpmtp_embed_workspace_bytes(ctypes.byref(shape)))
 
 
+def _empty(size, dtype, like: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor on like's device; a contiguous one of that size and type is the cheapest thing to copy from."""
+    if like.dtype is dtype and like.shape == size and like.is_contiguous():
+        return torch.empty_like(like)
+    return torch.empty(size, dtype=dtype, device=like.device)
+
+
 def _row_gate(t: torch.Tensor, n: int, dev: int, name: str) -> tuple:
     if t.shape != (n,) or t.dtype is not torch.bfloat16 or t.get_device() != dev or (n > 1 and t.stride(0) < 1):
         raise CpmtpError(f"cpmtp: {name} must be [{n}] bfloat16, or have the rows' shape")
@@ -796,7 +803,7 @@ def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block
     if block is None:
         res["x_out"] = x
     elif (t := res.get("x_out")) is None:
-        t = res["x_out"] = torch.empty(size, dtype=dtype, device=device)
+        t = res["x_out"] = _empty(size, dtype, x)
         a.x_out, a.ld_x_out = t.data_ptr(), d
     else:
         a.x_out, a.ld_x_out = _rows(t, size, dtype, dev, "x_out")
@@ -804,7 +811,7 @@ def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block
         res["y"] = res["rstd_pre"] = None
     else:
         if (t := res.get("y")) is None:
-            t = res["y"] = torch.empty(size, dtype=torch.bfloat16, device=device)
+            t = res["y"] = _empty(size, torch.bfloat16, x)
             a.y, a.ld_y = t.data_ptr(), d
         else:
             a.y, a.ld_y = _rows(t, size, torch.bfloat16, dev, "y")
@@ -858,21 +865,21 @@ def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Option
     if "dx" in skip:
         res["dx"] = None
     elif (t := res.get("dx")) is None:
-        t = res["dx"] = torch.empty(size, dtype=dtype, device=device)
+        t = res["dx"] = _empty(size, dtype, x_out)
         a.dx, a.ld_dx = t.data_ptr(), d
     else:
         a.dx, a.ld_dx = _rows(t, size, dtype, dev, "dx")
     if block is None or "dblock" in skip:
         res["dblock"] = None
     elif (t := res.get("dblock")) is None:
-        t = res["dblock"] = torch.empty(size, dtype=bf16, device=device)
+        t = res["dblock"] = _empty(size, bf16, x_out if dy is None else dy)
         a.dblock, a.ld_dblock = t.data_ptr(), d
     else:
         a.dblock, a.ld_dblock = _rows(t, size, bf16, dev, "dblock")
     if gate is None or "dgate" in skip:
         res["dgate"] = None
     elif (t := res.get("dgate")) is None:
-        t = res["dgate"] = torch.empty(gate.shape, dtype=bf16, device=device)
+        t = res["dgate"] = _empty(gate.shape, bf16, x_out if dy is None else dy)
         a.dgate, a.ld_dgate = t.data_ptr(), d if a.gate_kind == GATE_CHANNEL else 1
     else:
         a.dgate, a.ld_dgate = _rows(t, size, bf16, dev, "dgate") if a.gate_kind == GATE_CHANNEL else _row_gate(t, N, dev, "dgate")

@@ -17,7 +17,28 @@ __device__ __forceinline__ int row_of(int x, int V, int* dev_status) {
   return x < 0 ? 0 : V - 1;
 }
 
-// A warp copies kRowsPerWarp slabs of consecutive tokens, all read before the first is written.
+// A lane's eight columns of a slab as they lie in memory: 8 lane .. 8 lane + 7 (VEC), else every 32nd.  They become numbers
+// only when they are used, so that a warp has the loads of several rows under way.  `left`: columns from the slab's start on.
+template <class T, bool VEC>
+struct Slab {
+  T v[8];
+  __device__ __forceinline__ void read(const T* row, int lane, int left) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = row[min(lane + 32 * k, left - 1)];       // (past the end: the last one, not written)
+  }
+  __device__ __forceinline__ void get(float (&out)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) out[k] = io::to_f(v[k]);
+  }
+};
+template <class T>
+struct Slab<T, true> {
+  uint32_t v[2 * sizeof(T)];
+  __device__ __forceinline__ void read(const T* row, int lane, int left) { io::load8_raw(row + min(8 * lane, left - 8), v); }
+  __device__ __forceinline__ void get(float (&out)[8]) const { io::numbers8<T>(v, out); }
+};
+
+// A warp copies the slabs of kFwdRows consecutive tokens, all read before the first is written.
 constexpr int kFwdRows = 4;
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(const bf16_t* __restrict__ E, long long ld_table, const int* __restrict__ x,
@@ -26,34 +47,27 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const bf16_t* __restrict
   const int lane = threadIdx.x & 31;
   const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   const long long i0 = item / slabs * kFwdRows;
-  const int c0 = static_cast<int>(item % slabs) * kSlab;
+  const int c0 = static_cast<int>(item % slabs) * kSlab, left = d - c0;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   if (i0 >= tokens) return;
   int row = V;
   if (lane < kFwdRows && i0 + lane < tokens) row = row_of(x[i0 + lane], V, dev_status);
-  float v[kFwdRows][8];
+  Slab<bf16_t, VEC> in[kFwdRows];
 #pragma unroll
   for (int r = 0; r < kFwdRows; ++r) {
     const int id = __shfl_sync(0xffffffffu, row, r);
-    if (id < V) {
-      io::load_cols<VEC>(E + id * ld_table + c0, lane, 32, d - c0, v[r]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[r][k] = 0.f;
-    }
+    in[r].read(E + (id < V ? id : 0) * ld_table + c0, lane, left);
   }
 #pragma unroll
   for (int r = 0; r < kFwdRows; ++r) {
     if (i0 + r >= tokens) break;
+    float v[8];
+    in[r].get(v);
+    const bool pad = __shfl_sync(0xffffffffu, row, r) >= V;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[r][k] *= scale;
-    // the zeros of padding stay zeros whatever the scale
-    if (__shfl_sync(0xffffffffu, row, r) >= V) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[r][k] = 0.f;
-    }
-    io::store_cols<VEC>(out + (i0 + r) * ld + c0, lane, 32, d - c0, v[r]);
+    for (int k = 0; k < 8; ++k) v[k] = pad ? 0.f : v[k] * scale;      // (padding is zero whatever the scale)
+    io::store_cols<VEC>(out + (i0 + r) * ld + c0, lane, 32, left, v);
   }
 }
 
@@ -295,12 +309,14 @@ __global__ void __launch_bounds__(kClusterThreads) embed_sort_cluster_kernel(con
 }
 
 // ---- sums over equal tokens ----
-// A warp takes kChunk sorted positions and one slab of columns, and adds up each run of equal tokens in it.  A run that lies
+// A warp takes a chunk of sorted positions and one slab of columns, and adds up each run of equal tokens in it.  A run that lies
 // inside the chunk is written to the table; one that began before goes to head[chunk], one that began here and goes on to
 // tail[chunk], and embed_join_kernel adds those up.  Work per warp is the same however unequal the tokens' counts are.
 // Rows are read kAhead at a time, and with them the rows of the table that the runs ending among them are added to: a
 // warp that waited for one of those at every run's end spent three quarters of its time there.
-constexpr int kChunk = 32;
+// Chunks are kChunk long, or kShortChunk where few tokens would leave most of the GPU without a warp (736 tokens of 564
+// columns: 44 -> 16 us; at 9300 tokens of 256 the parts of a frequent token get too many, 25 -> 31 us).
+constexpr int kChunk = 32, kShortChunk = 8;
 constexpr int kAhead = 4;
 constexpr int kZeroRows = 32;     // rows of the table that a block looks at for rows without a token
 
@@ -309,31 +325,11 @@ struct SumParams {
   long long ld, ld_table;
   bf16_t* dE;
   float *head, *tail;             // [chunks][slabs * kSlab]
-  int tokens, V, d, slabs, chunks, sum_blocks;
+  int tokens, V, d, slabs, chunk, chunks, sum_blocks;
   float scale;
 };
 
 using io::f32x2;
-
-// A lane's eight columns of a slab as they were read: 8 lane .. 8 lane + 7 (VEC), else every 32nd.
-template <class T, bool VEC>
-struct Slab {
-  float v[8];
-  __device__ __forceinline__ void read(const T* row, int lane, int left) { io::load_cols<VEC>(row, lane, 32, left, v); }
-  __device__ __forceinline__ void get(float (&out)[8]) const {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) out[k] = v[k];
-  }
-};
-template <>
-struct Slab<bf16_t, true> {       // packed until it is used: half the registers while it is on its way
-  uint4 v;
-  __device__ __forceinline__ void read(const bf16_t* row, int lane, int left) {
-    v = make_uint4(0u, 0u, 0u, 0u);
-    if (8 * lane < left) v = *reinterpret_cast<const uint4*>(row + 8 * lane);
-  }
-  __device__ __forceinline__ void get(float (&out)[8]) const { io::unpack8(v, out); }
-};
 
 template <bool VEC, bool ACCUM>
 __device__ __forceinline__ void write_slab(bf16_t* row, int lane, int left, float scale, const f32x2 (&acc)[4], const Slab<bf16_t, VEC>& before) {
@@ -372,7 +368,7 @@ __device__ __forceinline__ void zero_rows(const SumParams& p, int r0) {
 }
 
 template <class T, bool VEC, bool ACCUM>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) embed_sum_kernel(const T* __restrict__ dy, const SumParams p) {
+__global__ void __launch_bounds__(256, sizeof(T) == 4 || !VEC ? 2 : 4) embed_sum_kernel(const T* __restrict__ dy, const SumParams p) {
   const int lane = threadIdx.x & 31;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
@@ -384,14 +380,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) embed_sum_kernel(
   const long long chunk = item / p.slabs;
   if (chunk >= p.chunks) return;
   const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab, left = p.d - c0;
-  const long long j0 = chunk * kChunk;
+  const long long j0 = chunk * p.chunk;
   uint2 kp = make_uint2(p.V, 0u);
-  if (j0 + lane < p.tokens) kp = p.sorted[j0 + lane];
+  if (lane < p.chunk && j0 + lane < p.tokens) kp = p.sorted[j0 + lane];
   const int before = j0 > 0 ? static_cast<int>(p.sorted[j0 - 1].x) : -1;
-  const int after = j0 + kChunk < p.tokens ? static_cast<int>(p.sorted[j0 + kChunk].x) : -1;
-  const int mine = static_cast<int>(kp.x);
+  const int after = j0 + p.chunk < p.tokens ? static_cast<int>(p.sorted[j0 + p.chunk].x) : -1;
+  const int mine = static_cast<int>(kp.x), last = p.chunk - 1;
   int next = __shfl_down_sync(0xffffffffu, mine, 1);
-  if (lane == 31) next = after;
+  if (lane == last) next = after;
   // by position: whether its run ends there; whether that run is all in this chunk and goes to the table
   const unsigned ends = __ballot_sync(0xffffffffu, mine != next);
   const bool first_run = mine == before;         // (only the run that the chunk begins with can have begun before)
@@ -403,13 +399,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) embed_sum_kernel(
 #pragma unroll
   for (int k = 0; k < 4; ++k) acc[k] = 0ull;
 #pragma unroll 1
-  for (int k0 = 0; k0 < kChunk; k0 += kAhead) {
+  for (int k0 = 0; k0 < p.chunk; k0 += kAhead) {
     Slab<T, VEC> rows[kAhead];
     Slab<bf16_t, VEC> old[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const long long pos = __shfl_sync(0xffffffffu, kp.y, k0 + u);
-      if (!((none >> (k0 + u)) & 1u)) rows[u].read(dy + pos * p.ld + c0, lane, left);
+      const long long pos = __shfl_sync(0xffffffffu, kp.y, k0 + u);      // (0 where there is none)
+      rows[u].read(dy + pos * p.ld + c0, lane, left);
     }
     if (ACCUM) {
 #pragma unroll
@@ -441,10 +437,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) embed_sum_kernel(
       }
     }
   }
-  if (!(ends >> 31)) {                           // the last run goes on
+  if (!((ends >> last) & 1u)) {                  // the last run goes on
     float v[8];
     io::singles(acc, v);
-    io::store8(((head >> 31) ? p.head : p.tail) + part, v);
+    io::store8((((head >> last) & 1u) ? p.head : p.tail) + part, v);
   }
 }
 
@@ -458,9 +454,9 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const SumParams p) {
   const long long chunk = item / p.slabs;
   if (chunk + 1 >= p.chunks) return;
   const int slab = static_cast<int>(item % p.slabs), c0 = slab * kSlab, left = p.d - c0;
-  const long long j0 = chunk * kChunk;
-  const int row = static_cast<int>(p.sorted[j0 + kChunk - 1].x), first = static_cast<int>(p.sorted[j0].x);
-  const int before = j0 > 0 ? static_cast<int>(p.sorted[j0 - 1].x) : -1, after = static_cast<int>(p.sorted[j0 + kChunk].x);
+  const long long j0 = chunk * p.chunk;
+  const int row = static_cast<int>(p.sorted[j0 + p.chunk - 1].x), first = static_cast<int>(p.sorted[j0].x);
+  const int before = j0 > 0 ? static_cast<int>(p.sorted[j0 - 1].x) : -1, after = static_cast<int>(p.sorted[j0 + p.chunk].x);
   if (row >= p.V || after != row || (first == row && before == row)) return;
   const size_t width = static_cast<size_t>(p.slabs) * kSlab;
   const float* tail = p.tail + chunk * width + c0 + 8 * lane;
@@ -475,7 +471,7 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const SumParams p) {
   // chunks that the run reaches into: 32 are looked at together, and their parts read kParts at a time
   constexpr int kParts = 8;
   for (long long c = chunk + 1;; c += 32) {
-    const bool goes = c + lane < p.chunks && static_cast<int>(p.sorted[(c + lane) * kChunk].x) == row;
+    const bool goes = c + lane < p.chunks && static_cast<int>(p.sorted[(c + lane) * p.chunk].x) == row;
     const unsigned mask = __ballot_sync(0xffffffffu, goes);
     const int n = mask == 0xffffffffu ? 32 : __ffs(~mask) - 1;
     for (int j = 0; j < n; j += kParts) {

@@ -51,9 +51,12 @@ int check_embed(const cpmtp_embed_shape* s) {
 
 struct EmbedLayout {
   int bits, passes, blocks;      // digits of the sort; thread blocks of a pass
-  int slabs, chunks;
+  int slabs, chunk, chunks;      // columns and sorted positions that the summing warps take
   size_t hist, keys, head, tail, total;
 };
+
+// Short chunks of the sums: up to this many tokens, if long ones make fewer warps than eight on each of 148 SMs.
+constexpr long long kShortTokens = 2048, kWarpsWanted = 8 * 148;
 
 EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   EmbedLayout L;
@@ -63,7 +66,8 @@ EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   L.bits = (width + L.passes - 1) / L.passes;
   L.blocks = (s.T + embed::kSortKeys - 1) / embed::kSortKeys;
   L.slabs = (s.d + embed::kSlab - 1) / embed::kSlab;
-  L.chunks = (s.T + embed::kChunk - 1) / embed::kChunk;
+  L.chunk = s.T <= kShortTokens && static_cast<long long>(s.T) * L.slabs < kWarpsWanted * embed::kChunk ? embed::kShortChunk : embed::kChunk;
+  L.chunks = (s.T + L.chunk - 1) / L.chunk;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
   L.hist = take(3 * sizeof(int) * (static_cast<size_t>(L.blocks) << L.bits));
@@ -476,7 +480,7 @@ int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const i
   embed::SumParams p;
   p.sorted = sorted; p.ld = s.ld_rows; p.ld_table = s.ld_table; p.dE = static_cast<bf16_t*>(dE);
   p.head = reinterpret_cast<float*>(ws + L.head); p.tail = reinterpret_cast<float*>(ws + L.tail);
-  p.tokens = s.T; p.V = s.V; p.d = s.d; p.slabs = L.slabs; p.chunks = L.chunks;
+  p.tokens = s.T; p.V = s.V; p.d = s.d; p.slabs = L.slabs; p.chunk = L.chunk; p.chunks = L.chunks;
   p.sum_blocks = static_cast<int>(sum_blocks); p.scale = s.scale;
   if (s.type == CPMTP_F32) CPMTP_TRY(launch_embed_sum(static_cast<const float*>(dy), p, accum, zero_blocks, st));
   else CPMTP_TRY(launch_embed_sum(static_cast<const bf16_t*>(dy), p, accum, zero_blocks, st));

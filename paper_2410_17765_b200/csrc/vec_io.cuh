@@ -43,6 +43,26 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
                : "l"(p)
                : "memory");
 }
+// The same as words, for loads whose values are wanted later.
+__device__ __forceinline__ void load8_raw(const bf16_t* p, uint32_t (&w)[4]) {
+  const uint4 r = *reinterpret_cast<const uint4*>(p);
+  w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
+}
+__device__ __forceinline__ void load8_raw(const float* p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+template <class T, int N>
+__device__ __forceinline__ void numbers8(const uint32_t (&w)[N], float (&v)[8]) {
+  if (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k % N]);
+  } else {
+    unpack8(make_uint4(w[0], w[1], w[2], w[3]), v);
+  }
+}
 // (the last argument names the type of the elements)
 __device__ __forceinline__ void load8_shared(const uint8_t* s, float (&v)[8], bf16_t) { unpack8(*reinterpret_cast<const uint4*>(s), v); }
 __device__ __forceinline__ void load8_shared(const uint8_t* s, float (&v)[8], float) {
