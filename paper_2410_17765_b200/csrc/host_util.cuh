@@ -71,7 +71,7 @@ struct ProfScope {
 // the stream drains; it calls ptx::grid_dep_wait() before it touches anything that kernel produced.
 // `cluster`: blocks to a thread-block cluster.
 template <class... KArgs, class... Args>
-cudaError_t launch_clusters(int cluster, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {
+cudaError_t launch_clusters(int cluster, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -85,11 +85,11 @@ cudaError_t launch_clusters(int cluster, void (*kernel)(KArgs...), dim3 grid, di
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 template <class... KArgs, class... Args>
 cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
-                       Args... args) {
+                       const Args&... args) {
   return launch_clusters(1, kernel, grid, block, smem, stream, args...);
 }
 

@@ -582,8 +582,9 @@ int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpm
   const int rd = check_device(&di);
   if (rd != CPMTP_OK) return rd;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  return count <= adamw::kSmallTable ? adamw_step<adamw::kSmallTable>(tensors, count, *hyper, di->sms, st)
-                                     : adamw_step<adamw::kLargeTable>(tensors, count, *hyper, di->sms, st);
+  if (count <= adamw::kSmallTable) return adamw_step<adamw::kSmallTable>(tensors, count, *hyper, di->sms, st);
+  if (count <= adamw::kMiddleTable) return adamw_step<adamw::kMiddleTable>(tensors, count, *hyper, di->sms, st);
+  return adamw_step<adamw::kLargeTable>(tensors, count, *hyper, di->sms, st);
 }
 
 int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,
@@ -611,7 +612,7 @@ size_t cpmtp_grad_norm_workspace_bytes(const cpmtp_adamw_tensor* tensors, int32_
   if (check_grads(tensors, count) != CPMTP_OK) return 0;
   DeviceInfo* di = device_info();
   const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
-  const size_t launches = count <= adamw::kSmallTable ? 1 : (count + adamw::kLargeTable - 1) / adamw::kLargeTable;
+  const size_t launches = (count + adamw::kLargeTable - 1) / adamw::kLargeTable + 1;
   return align_up(launches * grad_blocks(sms) * sizeof(double));
 }
 
@@ -631,8 +632,9 @@ int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_
   const int most = static_cast<int>(workspace_bytes / sizeof(double) < (1u << 30) ? workspace_bytes / sizeof(double) : 1u << 30);
   int parts = 0;
   ProfScope prof(CPMTP_STAGE_GRAD_NORM, st);
-  const int rs = count <= adamw::kSmallTable ? grad_squares<adamw::kSmallTable>(tensors, count, di->sms, part, most, &parts, st)
-                                             : grad_squares<adamw::kLargeTable>(tensors, count, di->sms, part, most, &parts, st);
+  const int rs = count <= adamw::kSmallTable    ? grad_squares<adamw::kSmallTable>(tensors, count, di->sms, part, most, &parts, st)
+                 : count <= adamw::kMiddleTable ? grad_squares<adamw::kMiddleTable>(tensors, count, di->sms, part, most, &parts, st)
+                                                : grad_squares<adamw::kLargeTable>(tensors, count, di->sms, part, most, &parts, st);
   if (rs != CPMTP_OK) return rs;
   CPMTP_TRY(launch_pdl(adamw::grad_norm_kernel, dim3(1), dim3(adamw::kThreads), 0, st, part, parts, max_norm, norm, coef));
   return CPMTP_OK;
