@@ -196,6 +196,7 @@ __device__ __forceinline__ void sync_ctas() {
   if (CTAS == 1) {
     __syncthreads();
   } else {
+    __syncwarp();                                             // (a warp arrives as a whole)
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }

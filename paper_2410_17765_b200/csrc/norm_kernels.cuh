@@ -65,44 +65,92 @@ __device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
   return io::pair(rcp(io::lo(s)), rcp(io::hi(s)));
 }
 
+// Barrier of the W warps of a row.  It counts warps, so a warp's lanes come together first.
+// MANY: known to be more than one.
+template <bool MANY>
 __device__ __forceinline__ void row_barrier(int W, int group) {
-  if (W == 1) __syncwarp();
-  else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
+  __syncwarp();
+  if (MANY || W > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(W * 32) : "memory");
+}
+// What crosses that barrier is written and read in assembly, so that the order of the three is the written one.
+__device__ __forceinline__ void put_shared(float* p, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(ptx::smem_u32(p)), "f"(v) : "memory"); }
+__device__ __forceinline__ float get_shared(const float* p) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(ptx::smem_u32(p)) : "memory");
+  return v;
 }
 
-// Sum over the W warps of a row, in every thread of them.  `red` is this row's and this reduction's alone until the row
-// after the next.
-__device__ __forceinline__ float row_sum(float v, float* red, int W, int group, int wg, int lane) {
-  v = io::sum_lanes(v);
-  if (W == 1) return v;
-  if (lane == 0) red[wg] = v;
-  row_barrier(W, group);
-  return io::sum_lanes(lane < W ? red[lane] : 0.f);
+// Sums over the W warps of a row, in every thread of them, in two steps: what comes between them does not wait for the other
+// warps.  `red` is this row's and this reduction's alone until the row after the next.  Two values at once take 11 shuffles
+// where two single sums take 20: half of the lanes finish the one, half the other.  No lane branches: all lanes of a half write
+// the sum that they share, and all read.  (Written under (lane & 15) == 0, red[lane >> 4] also cost correctness: the compiler
+// took that lane >> 4 for exact and used it for the reads, where it is not.)
+__device__ __forceinline__ float half_sum(float c) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+  return c;
+}
+template <bool MANY>
+__device__ __forceinline__ float begin_sum2(const float (&v)[2], float (*red)[kMaxWarps], int W, int wg, int lane) {
+  const bool hi = lane & 16;
+  float c = hi ? v[1] : v[0];
+  c += __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[1], 16);
+  c = half_sum(c);
+  if (MANY || W > 1) put_shared(&red[lane >> 4][wg], c);   // (the lanes of a half have the same sum, and no branch is taken)
+  return c;
+}
+template <bool MANY>
+__device__ __forceinline__ void end_sum2(float (&v)[2], float c, float (*red)[kMaxWarps], int W, int group, int lane) {
+  if (MANY || W > 1) {
+    row_barrier<MANY>(W, group);
+    const int j = lane & 15;
+    const float* mine = red[lane >> 4];
+    c = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxWarps; k += 16) {
+      if (k >= W) break;                     // (every lane reads; what lies past W does not count)
+      const float x = get_shared(mine + j + k);
+      c += j + k < W ? x : 0.f;
+    }
+    c = half_sum(c);
+  }
+#pragma unroll
+  for (int n = 0; n < 2; ++n) v[n] = __shfl_sync(0xffffffffu, c, 16 * n);
 }
 
-// The same for three values at once, in 12 shuffles where three single sums take 30: lanes hand over the values that
-// the other half will finish, so that each octet of lanes ends up with the sum of one of them.
-__device__ __forceinline__ void row_sum3(float (&v)[3], float (*red)[kMaxWarps], int W, int group, int wg, int lane) {
+// Three values in 12 shuffles: lanes hand over the values that the other half will finish, so that each octet of lanes ends up
+// with the sum of one of them (the last one with that of zeros).
+__device__ __forceinline__ float octet_sum(float c) {
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+  return c;
+}
+template <bool MANY>
+__device__ __forceinline__ float begin_sum3(const float (&v)[3], float (*red)[kMaxWarps], int W, int wg, int lane) {
   const bool hi = lane & 16, odd = lane & 8;
   float a = hi ? v[2] : v[0], b = hi ? 0.f : v[1];
   a += __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
   b += __shfl_xor_sync(0xffffffffu, hi ? v[1] : 0.f, 16);
   float c = odd ? b : a;
   c += __shfl_xor_sync(0xffffffffu, odd ? a : b, 8);
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-  const int which = lane >> 3, j = lane & 7;
-  if (W > 1) {
-    if (j == 0 && which < 3) red[which][wg] = c;
-    row_barrier(W, group);
+  c = octet_sum(c);
+  if (MANY || W > 1) put_shared(&red[lane >> 3][wg], c);
+  return c;
+}
+template <bool MANY>
+__device__ __forceinline__ void end_sum3(float (&v)[3], float c, float (*red)[kMaxWarps], int W, int group, int lane) {
+  if (MANY || W > 1) {
+    row_barrier<MANY>(W, group);
+    const int j = lane & 7;
+    const float* mine = red[lane >> 3];
     c = 0.f;
-    if (which < 3) {
 #pragma unroll
-      for (int k = 0; k < kMaxWarps; k += 8)
-        if (j + k < W) c += red[which][j + k];
+    for (int k = 0; k < kMaxWarps; k += 8) {
+      if (k >= W) break;                      // (every lane reads; what lies past W does not count)
+      const float x = get_shared(mine + j + k);
+      c += j + k < W ? x : 0.f;
     }
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    c = octet_sum(c);
   }
 #pragma unroll
   for (int n = 0; n < 3; ++n) v[n] = __shfl_sync(0xffffffffu, c, 8 * n);
@@ -218,13 +266,15 @@ __device__ __forceinline__ float row_values(const T* at, long long ld, unsigned 
 template <class S>
 __host__ __device__ constexpr int fwd_stage_bytes(int threads) { return region_bytes<S>(threads) + 2 * region_bytes<bf16_t>(threads); }
 
+// A row takes two sums, one after the other: of block^2, then of x_out^2.  The second one of a row and the first one of the
+// next are formed together, so that a row costs one barrier.
 template <class S, bool VEC, int MAXT, int STAGES, bool ONE, bool ALL>
 __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __grid_constant__ Params<S> p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float red[2][2][ONE ? 1 : 8][kMaxWarps];
+  __shared__ float red[2][ONE ? 1 : 8][2][kMaxWarps];
   const Place<ONE> at(p.W);
   const int t = at.t, tg = at.tg, d = p.d;
-  const int stage_bytes = fwd_stage_bytes<S>(tg);
+  const int rs = region_bytes<S>(tg), rb16 = region_bytes<bf16_t>(tg), stage_bytes = fwd_stage_bytes<S>(tg);
   uint8_t* ring = smem + at.group * STAGES * stage_bytes;
   const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || p.w_post != nullptr, has_y = ALL || p.w_pre != nullptr;
   const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
@@ -238,9 +288,8 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
     if (row < N) {
       uint32_t s = ring_at + stage * stage_bytes;
       fetch_row<VEC>(s, p.x.at(row), t, tg, d);
-      s += region_bytes<S>(tg);
-      if (has_block) fetch_row<VEC>(s, p.block.at(row), t, tg, d);
-      if (channel) fetch_row<VEC>(s + region_bytes<bf16_t>(tg), p.gate.at(row), t, tg, d);
+      if (has_block) fetch_row<VEC>(s + rs, p.block.at(row), t, tg, d);
+      if (channel) fetch_row<VEC>(s + rs + rb16, p.gate.at(row), t, tg, d);
     }
     commit_row();
   };
@@ -249,36 +298,43 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
   f32x2 w_post[4], w_pre[4];
   load_weights<VEC>(p.w_post, t, d, 0.f, w_post);
   load_weights<VEC>(p.w_pre, t, d, 0.f, w_pre);
-  float logits = 0.f;
+  float logits = 0.f, sum[2] = {0.f, 0.f};
+  // sum of block^2 over this thread's columns of the row in `stage`
+  auto block_square = [&](unsigned row, int stage) -> float {
+    if (!has_post || row >= N) return 0.f;
+    f32x2 b[4];
+    take8<VEC>(ring + stage * stage_bytes + rs, p.block, row, t, b);
+    return square_sum(b);
+  };
+  wait_row<STAGES - 2>();
+  if (!VEC) row_barrier<ONE>(p.W, at.group);
+  if (i < N) {
+    const float first[2] = {0.f, block_square(i, 0)};
+    const float c = begin_sum2<ONE>(first, red[1][at.rg], p.W, at.wg, at.lane);
+    end_sum2<ONE>(sum, c, red[1][at.rg], p.W, at.group, at.lane);
+  }
   int stage = 0;
   for (int it = 0; i < N; i += step, ++it) {
+    const float rb = rsqrtf(fmaf(sum[1], p.inv_d, p.eps));
     float gl = 0.f;
     if (row_gate) {
       if ((it & 31) == 0) logits = row_values(p.gate.data, p.gate.ld, i, step, N, at.lane);
       gl = __shfl_sync(0xffffffffu, logits, it & 31);
     }
-    // the stage that this refills was read before the row barriers of the row before (one warp: before this one)
-    if (!VEC && p.W == 1) __syncwarp();
-    fetch(i + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
-    wait_row<STAGES - 1>();
-    if (!VEC) row_barrier(p.W, at.group);
     const uint8_t* s = ring + stage * stage_bytes;
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
     f32x2 x[4];
     take8<VEC>(s, p.x, i, t, x);
     if (has_block) {
-      s += region_bytes<S>(tg);
       f32x2 b[4], g[4];
-      take8<VEC>(s, p.block, i, t, b);
+      take8<VEC>(s + rs, p.block, i, t, b);
       if (channel) {
-        take8<VEC>(s + region_bytes<bf16_t>(tg), p.gate, i, t, g);
+        take8<VEC>(s + rs + rb16, p.gate, i, t, g);
 #pragma unroll
         for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
       } else {
         fill8(g, row_gate ? sigmoid(gl) : 1.f);
       }
       if (has_post) {
-        const float rb = rsqrtf(fmaf(row_sum(square_sum(b), red[it & 1][0][at.rg], p.W, at.group, at.wg, at.lane), p.inv_d, p.eps));
         if (t == 0 && (ALL || p.rstd_post != nullptr)) p.rstd_post[i] = rb;
         const f32x2 rb2 = both(rb);
 #pragma unroll
@@ -287,18 +343,26 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
       const f32x2 scale = both(p.res_scale);
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = fma2(scale, x[k], mul2(g[k], b[k]));
-      put8<VEC>(p.x_out.at(i), t, d, x);
     }
+    // the next row is here; the one that comes STAGES - 1 after this goes into the stage before this one's, which every
+    // thread has read since the last barrier of the row before (one warp: before this one)
+    if (!VEC && p.W == 1) __syncwarp();
+    fetch(i + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+    wait_row<STAGES - 2>();
+    if (!VEC) row_barrier<ONE>(p.W, at.group);
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    const float mine[2] = {has_y ? square_sum(x) : 0.f, block_square(i + step, stage)};
+    const float c = begin_sum2<ONE>(mine, red[it & 1][at.rg], p.W, at.wg, at.lane);
+    if (has_block) put8<VEC>(p.x_out.at(i), t, d, x);
+    end_sum2<ONE>(sum, c, red[it & 1][at.rg], p.W, at.group, at.lane);
     if (has_y) {
-      const float rx = rsqrtf(fmaf(row_sum(square_sum(x), red[it & 1][1][at.rg], p.W, at.group, at.wg, at.lane), p.inv_d, p.eps));
+      const float rx = rsqrtf(fmaf(sum[0], p.inv_d, p.eps));
       if (t == 0 && (ALL || p.rstd_pre != nullptr)) p.rstd_pre[i] = rx;
       const f32x2 rx2 = both(rx);
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], mul2(rx2, w_pre[k]));
       put8<VEC>(p.y.at(i), t, d, x);
     }
-    // without a reduction in this row nothing has yet kept the others from its stage
-    if (!VEC && !has_post && !has_y) row_barrier(p.W, at.group);
   }
 }
 
@@ -314,7 +378,7 @@ __host__ __device__ constexpr int bwd_stage_bytes(int threads) { return 2 * regi
 template <class S, bool VEC, int MAXT, int STAGES, bool ONE, bool ALL>
 __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ Params<S> p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float red[2][ONE ? 1 : 8][3][kMaxWarps];
+  __shared__ float red[2][ONE ? 1 : 8][4][kMaxWarps];
   const Place<ONE> at(p.W);
   const int t = at.t, tg = at.tg, d = p.d;
   const int rs = region_bytes<S>(tg), rb16 = region_bytes<bf16_t>(tg), stage_bytes = bwd_stage_bytes<S>(tg);
@@ -349,70 +413,110 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   load_weights<VEC>(has_post ? p.w_post : nullptr, t, d, 1.f, w_post);
   float rstds_pre = 0.f, rstds_post = 1.f, logits = 0.f;
   int stage = 0;
-  for (int it = 0; i < N; i += step, ++it) {
+
+  // Row r, the it-th of this group: what comes before its sums, into `row`, and the sums as far as this warp goes.
+  struct Row {
+    f32x2 x[4], a[4], b[4], g[4];
+    float rx, rb, grow;
+  };
+  auto before_sums = [&](unsigned r, int it, Row& row) -> float {
     if ((it & 31) == 0) {
-      if (has_y) rstds_pre = row_values(p.rstd_pre, 1, i, step, N, at.lane);
-      if (has_post) rstds_post = row_values(p.rstd_post, 1, i, step, N, at.lane);
-      if (row_gate) logits = row_values(p.gate.data, p.gate.ld, i, step, N, at.lane);
+      if (has_y) rstds_pre = row_values(p.rstd_pre, 1, r, step, N, at.lane);
+      if (has_post) rstds_post = row_values(p.rstd_post, 1, r, step, N, at.lane);
+      if (row_gate) logits = row_values(p.gate.data, p.gate.ld, r, step, N, at.lane);
     }
-    const float rx = __shfl_sync(0xffffffffu, rstds_pre, it & 31), rb = __shfl_sync(0xffffffffu, rstds_post, it & 31);
-    const float grow = row_gate ? sigmoid(__shfl_sync(0xffffffffu, logits, it & 31)) : 1.f;
-    // the stage that this refills was read before the row barrier of the row before (one warp: before this one)
-    if (!VEC && p.W == 1) __syncwarp();
-    fetch(i + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
-    wait_row<STAGES - 1>();
-    if (!VEC) row_barrier(p.W, at.group);
+    row.rx = __shfl_sync(0xffffffffu, rstds_pre, it & 31);
+    row.rb = __shfl_sync(0xffffffffu, rstds_post, it & 31);
+    row.grow = row_gate ? sigmoid(__shfl_sync(0xffffffffu, logits, it & 31)) : 1.f;
+    wait_row<STAGES - 2>();
+    if (!VEC) row_barrier<ONE>(p.W, at.group);
     const uint8_t* s = ring + stage * stage_bytes;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
-    f32x2 dy[4], x[4], a[4], b[4], g[4];
-    take8<VEC>(s, p.x_out, i, t, x);
-    if (has_dx_out) take8<VEC>(s + rs, p.dx_out, i, t, a);
-    else fill8(a, 0.f);
+    f32x2 dy[4];
+    take8<VEC>(s, p.x_out, r, t, row.x);
+    if (has_dx_out) take8<VEC>(s + rs, p.dx_out, r, t, row.a);
+    else fill8(row.a, 0.f);
     s += 2 * rs;
-    if (has_y) take8<VEC>(s, p.dy, i, t, dy);
+    if (has_y) take8<VEC>(s, p.dy, r, t, dy);
     else fill8(dy, 0.f);
-    if (has_block) take8<VEC>(s + rb16, p.block, i, t, b);
-    else fill8(b, 0.f);
+    if (has_block) take8<VEC>(s + rb16, p.block, r, t, row.b);
+    else fill8(row.b, 0.f);
     if (channel) {
-      take8<VEC>(s + 2 * rb16, p.gate, i, t, g);
+      take8<VEC>(s + 2 * rb16, p.gate, r, t, row.g);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
+      for (int k = 0; k < 4; ++k) row.g[k] = sigmoid2(row.g[k]);
     } else {
-      fill8(g, 1.f);
+      fill8(row.g, 1.f);
     }
-    f32x2 s0 = both(0.f), s1 = s0, s2 = s0, wb[4];
-    const f32x2 rx2 = both(rx);
+    f32x2 s0 = both(0.f), s1 = s0, s2 = s0;
+    const f32x2 rx2 = both(row.rx);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const f32x2 dyr = mul2(dy[k], rx2), wdyr = mul2(w_pre[k], dyr);
-      acc_pre[k] = fma2(dyr, x[k], acc_pre[k]);
-      a[k] = add2(a[k], wdyr);
-      wb[k] = mul2(w_post[k], b[k]);
-      const f32x2 q = mul2(wb[k], g[k]);
-      s0 = fma2(wdyr, x[k], s0);
-      s1 = fma2(q, a[k], s1);
-      s2 = fma2(q, x[k], s2);
+      acc_pre[k] = fma2(dyr, row.x[k], acc_pre[k]);
+      row.a[k] = add2(row.a[k], wdyr);
+      const f32x2 q = mul2(mul2(w_post[k], row.b[k]), row.g[k]);
+      s0 = fma2(wdyr, row.x[k], s0);
+      s1 = fma2(q, row.a[k], s1);
+      s2 = fma2(q, row.x[k], s2);
     }
-    float sum[3] = {io::lo(s0) + io::hi(s0), io::lo(s1) + io::hi(s1), io::lo(s2) + io::hi(s2)};
-    row_sum3(sum, red[it & 1][at.rg], p.W, at.group, at.wg, at.lane);
-    const float c1 = rx * rx * sum[0] * p.inv_d;              // t = a - c1 x
-    const float dot = rb * fmaf(-c1, sum[2], sum[1]);         // sum of t u (the row gate left out)
-    const f32x2 minus_c1 = both(-c1), grb = both(grow * rb), scale = both(p.res_scale);
-    const f32x2 minus_c2 = both(has_post ? -rb * rb * grow * dot * p.inv_d : 0.f);
+    const float sum[3] = {io::lo(s0) + io::hi(s0), io::lo(s1) + io::hi(s1), io::lo(s2) + io::hi(s2)};
+    return begin_sum3<ONE>(sum, red[it & 1][at.rg], p.W, at.wg, at.lane);
+  };
+  // And what comes after them.
+  auto after_sums = [&](unsigned r, const Row& row, const float (&sum)[3]) {
+    const float c1 = row.rx * row.rx * sum[0] * p.inv_d;              // t = a - c1 x
+    const float dot = row.rb * fmaf(-c1, sum[2], sum[1]);             // sum of t u (the row gate left out)
+    const f32x2 minus_c1 = both(-c1), grb = both(row.grow * row.rb), scale = both(p.res_scale);
+    const f32x2 minus_c2 = both(has_post ? -row.rb * row.rb * row.grow * dot * p.inv_d : 0.f);
+    f32x2 dx[4], dblock[4], dgate[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const f32x2 tk = fma2(minus_c1, x[k], a[k]);
-      const f32x2 dur = mul2(mul2(grb, g[k]), tk);            // rstd_post du
-      acc_post[k] = fma2(dur, b[k], acc_post[k]);
-      a[k] = fma2(w_post[k], dur, mul2(minus_c2, b[k]));      // dblock
-      g[k] = mul2(mul2(wb[k], dur), fma2(g[k], both(-1.f), both(1.f)));   // dgate
-      x[k] = mul2(scale, tk);                                 // dx
+      const f32x2 tk = fma2(minus_c1, row.x[k], row.a[k]);
+      const f32x2 dur = mul2(mul2(grb, row.g[k]), tk);                // rstd_post du
+      acc_post[k] = fma2(dur, row.b[k], acc_post[k]);
+      dblock[k] = fma2(w_post[k], dur, mul2(minus_c2, row.b[k]));
+      dgate[k] = mul2(mul2(mul2(w_post[k], row.b[k]), dur), fma2(row.g[k], both(-1.f), both(1.f)));
+      dx[k] = mul2(scale, tk);
     }
-    if (ALL || p.dx.data != nullptr) put8<VEC>(p.dx.at(i), t, d, x);
-    if (ALL || p.dblock.data != nullptr) put8<VEC>(p.dblock.at(i), t, d, a);
+    if (ALL || p.dx.data != nullptr) put8<VEC>(p.dx.at(r), t, d, dx);
+    if (ALL || p.dblock.data != nullptr) put8<VEC>(p.dblock.at(r), t, d, dblock);
     if (ALL || p.dgate.data != nullptr) {
-      if (channel) put8<VEC>(p.dgate.at(i), t, d, g);
-      else if (t == 0) *p.dgate.at(i) = io::from_f<bf16_t>(grow * (1.f - grow) * dot);
+      if (channel) put8<VEC>(p.dgate.at(r), t, d, dgate);
+      else if (t == 0) *p.dgate.at(r) = io::from_f<bf16_t>(row.grow * (1.f - row.grow) * dot);
+    }
+  };
+
+  // the row that comes STAGES - 1 after row r goes into the stage before the one read last
+  auto fetch_after = [&](unsigned r) {
+    if (!VEC && p.W == 1) __syncwarp();
+    fetch(r + (STAGES - 1) * step, stage >= 2 ? stage - 2 : stage + STAGES - 2);
+  };
+  float sum[3];
+  if (ONE && MAXT <= 512) {
+    // A row is finished while the warps' sums of the next one are on their way: two rows are held at a time, which 128
+    // registers allow where rows' addresses are common to the block (8192 x 4096: 110 -> 101 us).
+    if (i < N) {
+      Row row;
+      end_sum3<ONE>(sum, before_sums(i, 0, row), red[0][at.rg], p.W, at.group, at.lane);
+#pragma unroll 2
+      for (int it = 1; i + step < N; i += step, ++it) {
+        fetch_after(i);
+        Row next;
+        const float c = before_sums(i + step, it, next);
+        after_sums(i, row, sum);
+        end_sum3<ONE>(sum, c, red[it & 1][at.rg], p.W, at.group, at.lane);
+        row = next;
+      }
+      after_sums(i, row, sum);
+    }
+  } else {
+    for (int it = 0; i < N; i += step, ++it) {
+      Row row;
+      const float c = before_sums(i, it, row);
+      fetch_after(i);
+      end_sum3<ONE>(sum, c, red[it & 1][at.rg], p.W, at.group, at.lane);
+      after_sums(i, row, sum);
     }
   }
   if (p.part == nullptr) return;
