@@ -581,10 +581,27 @@ __global__ void __launch_bounds__(kThreads) state_values_kernel(const uint8_t* _
   }
 }
 
-// Sum of squares of every gradient: a block takes runs of elements, in turn with the others.
+// Sum of squares of every gradient: a block takes runs of elements, in turn with the others.  A warp reads the kSquareBlocks
+// blocks of a whole run that are its own before it uses the first (one at a time it reached half of the bandwidth).
+constexpr int kSquareBlocks = kRun / (kWarps * kBlock);
+
+template <class T>
+__device__ __forceinline__ void add_squares(const T* g, int lane, float (&acc)[8]) {
+  uint32_t w[kSquareBlocks][2 * sizeof(T)];
+#pragma unroll
+  for (int j = 0; j < kSquareBlocks; ++j) io::load8_raw(g + j * kWarps * kBlock + 8 * lane, w[j]);
+#pragma unroll
+  for (int j = 0; j < kSquareBlocks; ++j) {
+    float v[8];
+    io::numbers8<T>(w[j], v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] = fmaf(v[k], v[k], acc[k]);
+  }
+}
+
 template <int CAP>
 __global__ void __launch_bounds__(kThreads) grad_square_kernel(const __grid_constant__ Table<CAP> tab, int runs, double* __restrict__ part) {
-  __shared__ double sums[kThreads / 32];
+  __shared__ double sums[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float acc[8];
 #pragma unroll
@@ -595,6 +612,12 @@ __global__ void __launch_bounds__(kThreads) grad_square_kernel(const __grid_cons
     const int which = tensor_of(tab, run);
     const Tensor& t = tab.t[which];
     const long long start = static_cast<long long>(run - tab.first[which]) * tab.run;
+    if (t.vec && tab.run == kRun && start + kRun <= t.numel) {
+      const long long at = start + warp * kBlock;
+      if (t.grad_f32) add_squares(static_cast<const float*>(t.grad) + at, lane, acc);
+      else add_squares(static_cast<const bf16_t*>(t.grad) + at, lane, acc);
+      continue;
+    }
 #pragma unroll 1
     for (int b = warp * kBlock; b < tab.run; b += kWarps * kBlock) {
       const long long at = start + b;
@@ -615,7 +638,7 @@ __global__ void __launch_bounds__(kThreads) grad_square_kernel(const __grid_cons
   if (lane == 0) sums[warp] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 32; ++w) s += sums[w];
+    for (int w = 1; w < kWarps; ++w) s += sums[w];
     part[blockIdx.x] = s;
   }
 }
