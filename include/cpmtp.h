@@ -396,6 +396,8 @@ enum { CPMTP_BF16 = 0, CPMTP_F32 = 1 };
 
 /* Token that stands for no token (padding of ragged sequences): looked up as a row of zeros, no gradient. */
 #define CPMTP_EMBED_PAD (-1)
+/* Most tokens of one gradient (the sort of more than 65536 takes a time that grows with the square of their number). */
+#define CPMTP_EMBED_MAX_GRAD_T (1 << 24)
 
 typedef struct cpmtp_embed_shape {
   int32_t T;          /* tokens, 0 <= T < 2^30 */

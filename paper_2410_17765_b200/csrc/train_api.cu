@@ -202,7 +202,7 @@ norm::Params<S> norm_params(const cpmtp_norm_args& a, const NormLayout& L) {
 }
 
 template <class T>
-bool rows_vec(const cpmtp_rows& r, int d) { return d % 256 == 0 && (r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d)); }
+bool rows_vec(const cpmtp_rows& r, int d) { return d % 8 == 0 && (r.data == nullptr || io::vec_ok<T>(r.data, r.ld, d)); }
 
 template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
 cudaError_t launch_norm_fwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
@@ -220,7 +220,7 @@ cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, int s
   const bool vec = rows_vec<S>(a.x, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.y, a.d) &&
                    (a.gate_kind != CPMTP_GATE_CHANNEL || rows_vec<bf16_t>(a.gate, a.d)) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
   const int blocks = row_blocks(a, L, sms * (1024 / MAXT));
-  const bool all = a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.w_pre != nullptr && a.rstd_post != nullptr && a.rstd_pre != nullptr;
+  const bool all = a.d % 256 == 0 && a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.w_pre != nullptr && a.rstd_post != nullptr && a.rstd_pre != nullptr;
   if (!vec) return launch_norm_fwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
   return all ? launch_norm_fwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_fwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
 }
@@ -248,7 +248,7 @@ cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int b
   const bool vec = rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<bf16_t>(a.dy, a.d) && rows_vec<S>(a.dx_out, a.d) &&
                    rows_vec<S>(a.dx, a.d) && rows_vec<bf16_t>(a.dblock, a.d) &&
                    (!channel || (rows_vec<bf16_t>(a.gate, a.d) && rows_vec<bf16_t>(a.dgate, a.d))) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
-  const bool all = channel && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr && a.dx.data != nullptr &&
+  const bool all = a.d % 256 == 0 && channel && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr && a.dx.data != nullptr &&
                    a.dblock.data != nullptr && a.dgate.data != nullptr;
   if (!vec) return launch_norm_bwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
   return all ? launch_norm_bwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_bwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
@@ -442,7 +442,7 @@ int cpmtp_embed_forward(const cpmtp_embed_shape* shape, const void* E, const int
 }
 
 size_t cpmtp_embed_workspace_bytes(const cpmtp_embed_shape* shape) {
-  return check_embed(shape) == CPMTP_OK ? embed_layout(*shape).total : 0;
+  return check_embed(shape) == CPMTP_OK && shape->T <= CPMTP_EMBED_MAX_GRAD_T ? embed_layout(*shape).total : 0;
 }
 
 int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const int32_t* x, void* dE,
@@ -452,6 +452,7 @@ int cpmtp_embed_backward(const cpmtp_embed_shape* shape, const void* dy, const i
   const cpmtp_embed_shape& s = *shape;
   const bool accum = (s.flags & CPMTP_FLAG_ACCUM_GRADS) != 0;
   if (s.T == 0 && accum) return CPMTP_OK;
+  if (s.T > CPMTP_EMBED_MAX_GRAD_T) return CPMTP_ERR_LIMIT;
   const EmbedLayout L = embed_layout(s);
   if (!dE || (s.T > 0 && (!dy || !x || !workspace))) return CPMTP_ERR_NULL;
   if (!aligned(dE, 2) || !aligned(x, 4) || !aligned(dy, type_bytes(s.type)) || !aligned(workspace, kAlign) || !aligned(dev_status, 4))

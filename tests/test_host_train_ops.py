@@ -69,6 +69,9 @@ def test_embed_arguments_are_checked(lib):
     assert lib.cpmtp_embed_backward(ctypes.byref(s), P, P, P, None, need, None, None) == -1
     assert lib.cpmtp_embed_backward(ctypes.byref(s), P, P, P, ctypes.c_void_p(4096 + 16), need, None, None) == -3
     assert lib.cpmtp_embed_backward(ctypes.byref(s), P, P, P, P, need - 1, None, None) == -4
+    many = embed(T=(1 << 24) + 1)                        # the lookup takes them, the gradient's sort does not
+    assert lib.cpmtp_embed_workspace_bytes(ctypes.byref(many)) == 0
+    assert lib.cpmtp_embed_backward(ctypes.byref(many), P, P, P, P, 1 << 40, None, None) == -7
     none = embed(T=0, flags=binding.FLAG_ACCUM_GRADS)
     assert lib.cpmtp_embed_forward(ctypes.byref(none), None, None, None, None, None) == 0
     assert lib.cpmtp_embed_backward(ctypes.byref(none), None, None, None, None, 0, None, None) == 0
