@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import operator
 import os
 import struct
@@ -631,6 +632,8 @@ def distill_backward(h, W_head, E, W_g, x, teacher, saved: Saved, dsaved: Distil
 
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _dtype_of = operator.attrgetter("dtype")
+_address_of, _size_of, _device_of, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
+_is_tensor = functools.partial(operator.is_not, None)
 _ADAMW_WORDS = ctypes.sizeof(CAdamWTensor) // 8      # a descriptor in 8-byte words: param, grad, master, m, v, m_exp, v_exp, numel, types, factors
 
 
@@ -918,6 +921,7 @@ class _Descriptors:
         self.n = n
         self.words = array("q", bytes(8 * _ADAMW_WORDS * n))
         self.address = self.words.buffer_info()[0]
+        self.grad_kind = None              # the gradients' common type as it stands in the words, if they have one
 
     def put(self, word: int, values) -> None:
         if self.n:
@@ -925,27 +929,33 @@ class _Descriptors:
 
     def put_grads(self, grads, dev: int, param_types: Optional[list] = None, numels: Optional[list] = None) -> None:
         """Addresses, sizes and types of the gradients, one per parameter of `numels` elements; None: no address."""
-        there = [g for g in grads if g is not None]
+        n = len(grads)
+        there = grads if all(map(_is_tensor, grads)) else [g for g in grads if g is not None]
         if there:
             # one property of all of them at a time: half the cost of a loop over the tensors
             kinds = list(map(_dtype_of, there))
             same = kinds.count(kinds[0]) == len(kinds)
             ok = kinds[0] in _TYPES if same else all(k in _TYPES for k in kinds)
-            if not ok or set(map(torch.Tensor.get_device, there)) != {dev} or not all(map(torch.Tensor.is_contiguous, there)):
+            devices = list(map(_device_of, there))
+            if not ok or devices.count(dev) != len(devices) or not all(map(_contiguous, there)):
                 raise CpmtpError("cpmtp: gradients must be contiguous bfloat16 or float32 tensors on the current CUDA device")
-            types = [_TYPES[kinds[0]] << 32] * len(kinds) if same else [_TYPES[k] << 32 for k in kinds]
+            kind = _TYPES[kinds[0]] << 32
+            types = [kind] * len(kinds) if same else [_TYPES[k] << 32 for k in kinds]
         else:
-            types = []
-        at, sizes = list(map(torch.Tensor.data_ptr, there)), list(map(torch.Tensor.numel, there))
-        if len(there) < len(grads):
+            kind, same, types = 0, True, []
+        at, sizes = list(map(_address_of, there)), list(map(_size_of, there))
+        if len(there) < n:
             where = [i for i, g in enumerate(grads) if g is not None]
-            at, sizes, types = ([dict(zip(where, v)).get(i, 0) for i in range(len(grads))] for v in (at, sizes, types))
+            at, sizes, types = ([dict(zip(where, v)).get(i, 0) for i in range(n)] for v in (at, sizes, types))
+            same = False
         if numels is None:
             self.put(7, sizes)
         elif sizes != numels and any(g is not None and s != m for g, s, m in zip(grads, sizes, numels)):
             raise CpmtpError("cpmtp: a gradient must have its parameter's size")
         self.put(1, at)
-        self.put(8, types if param_types is None else map(int.__or__, types, param_types))
+        if not same or kind != self.grad_kind:             # (the types seldom change from step to step)
+            self.put(8, types if param_types is None else map(operator.or_, types, param_types))
+            self.grad_kind = kind if same else None
 
 
 def _grad_descriptors(grads) -> tuple:
@@ -1052,11 +1062,14 @@ def adamw_state_values(codes: torch.Tensor, exps: torch.Tensor, *, second: bool,
     """cpmtp_adamw_state_values: the values of an 8-bit moment (second: v, else m) as bf16, exactly."""
     dev = _device(codes)
     n = codes.numel()
+    if codes.dtype is not torch.uint8 or not codes.is_contiguous():
+        raise CpmtpError("cpmtp: codes must be contiguous uint8")
+    if exps.dtype is not torch.uint8 or exps.numel() != -(-n // ADAMW_BLOCK) or exps.get_device() != dev or not exps.is_contiguous():
+        raise CpmtpError(f"cpmtp: exps must be {-(-n // ADAMW_BLOCK)} contiguous bytes on the same device")
     if out is None:
-        out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
-    for name, t, dtype, size in (("codes", codes, torch.uint8, n), ("exps", exps, torch.uint8, -(-n // ADAMW_BLOCK)), ("out", out, torch.bfloat16, n)):
-        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() != size:
-            raise CpmtpError(f"cpmtp: {name} must be {size} contiguous {dtype} on the same device")
+        out = torch.empty_like(codes, dtype=torch.bfloat16)
+    elif out.dtype is not torch.bfloat16 or out.numel() != n or out.get_device() != dev or not out.is_contiguous():
+        raise CpmtpError(f"cpmtp: out must be {n} contiguous bfloat16 on the same device")
     rc = load_library().cpmtp_adamw_state_values(codes.data_ptr(), exps.data_ptr(), n, 1 if second else 0, out.data_ptr(), _raw_stream(dev))
     if rc:
         _check(rc)
