@@ -1,7 +1,7 @@
 // Norms before and after a block, fused with its gate and the residual addition: forward and backward.
 //
 // A row is owned by W warps, eight columns to a thread, and stays in registers from its only read to its only write; a
-// block holds G rows at a time (W G <= 16; W <= 32, G = 1 from 4097 columns on).  Blocks are persistent.  Both directions move
+// block holds G rows at a time (W G <= 16, or G = 1).  Blocks are persistent.  Both directions move
 // 10 to 20 bytes per element and compute some tens of operations on them, so what counts is that every SM always has tens of
 // kilobytes of reads under way: rows ahead are fetched with cp.async into a ring of kStages rows in shared memory while
 // the current row goes through its reductions.

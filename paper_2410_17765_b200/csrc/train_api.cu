@@ -128,12 +128,18 @@ cudaError_t launch_embed_sum(const T* dy, const embed::SumParams& p, bool accum,
 // ------------------------------------------------------------------------------------------------ norms
 struct NormLayout {
   int W, G, threads;             // warps per row, rows per block, threads per block
+  int per_sm;                    // blocks that make sixteen warps on an SM
 };
 
-NormLayout norm_layout(int d) {
+// `vec`: the rows allow accesses of eight columns.  Blocks of several rows are better for those (8192 x 2048: backward 52 us
+// against 58 for blocks of one row), blocks of one row for others, whose addresses take more operations and are then common to
+// a block (8192 x 2047: 80 us against 88) -- where one row is wide enough to leave few blocks: their sums are added up afterwards.
+NormLayout norm_layout(int d, bool vec) {
   NormLayout L;
   L.W = (d + 255) / 256;
-  L.G = L.W >= 16 ? 1 : 16 / L.W;
+  const int rows = L.W >= 16 ? 1 : 16 / L.W;
+  L.G = !vec && L.W >= 4 ? 1 : rows;
+  L.per_sm = rows / L.G;
   L.threads = L.W * L.G * 32;
   return L;
 }
@@ -152,7 +158,7 @@ int row_blocks(const cpmtp_norm_args& a, const NormLayout& L, int most) {
   const long long rows = (static_cast<long long>(a.N) + L.G - 1) / L.G;
   return static_cast<int>(rows < most ? rows : most);
 }
-int norm_bwd_blocks(const cpmtp_norm_args& a, const NormLayout& L, int sms) { return row_blocks(a, L, sms); }
+int norm_bwd_blocks(const cpmtp_norm_args& a, const NormLayout& L, int sms) { return row_blocks(a, L, sms * L.per_sm); }
 
 int check_rows(const cpmtp_rows& r, int d, size_t bytes) {
   if (r.data == nullptr) return CPMTP_ERR_NULL;
@@ -215,19 +221,21 @@ cudaError_t launch_norm_fwd_as(const norm::Params<S>& p, const NormLayout& L, in
 }
 
 template <class S, int MAXT, bool ONE>
-cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, int sms, cudaStream_t st) {
+cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, bool vec, int sms, cudaStream_t st) {
   const norm::Params<S> p = norm_params<S>(a, L);
-  const bool vec = rows_vec<S>(a.x, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.y, a.d) &&
-                   (a.gate_kind != CPMTP_GATE_CHANNEL || rows_vec<bf16_t>(a.gate, a.d)) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
-  const int blocks = row_blocks(a, L, sms * (1024 / MAXT));
-  const bool all = a.d % 256 == 0 && a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.w_pre != nullptr && a.rstd_post != nullptr && a.rstd_pre != nullptr;
+  const int blocks = row_blocks(a, L, sms * (1024 / MAXT) * L.per_sm);
+  const bool all = a.d % 256 == 0 && a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.w_pre != nullptr && a.rstd_post != nullptr &&
+                   a.rstd_pre != nullptr;
   if (!vec) return launch_norm_fwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
   return all ? launch_norm_fwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_fwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
 }
 template <class S>
-cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, const NormLayout& L, int sms, cudaStream_t st) {
-  if (L.threads > 512) return launch_norm_fwd<S, 1024, true>(a, L, sms, st);
-  return L.G == 1 ? launch_norm_fwd<S, 512, true>(a, L, sms, st) : launch_norm_fwd<S, 512, false>(a, L, sms, st);
+cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, int sms, cudaStream_t st) {
+  const bool vec = rows_vec<S>(a.x, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.y, a.d) &&
+                   (a.gate_kind != CPMTP_GATE_CHANNEL || rows_vec<bf16_t>(a.gate, a.d)) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
+  const NormLayout L = norm_layout(a.d, vec);
+  if (L.threads > 512) return launch_norm_fwd<S, 1024, true>(a, L, vec, sms, st);
+  return L.G == 1 ? launch_norm_fwd<S, 512, true>(a, L, vec, sms, st) : launch_norm_fwd<S, 512, false>(a, L, vec, sms, st);
 }
 
 template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
@@ -241,22 +249,25 @@ cudaError_t launch_norm_bwd_as(const norm::Params<S>& p, const NormLayout& L, in
 }
 
 template <class S, int MAXT, bool ONE>
-cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int blocks, float* part, cudaStream_t st) {
+cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, bool vec, int blocks, float* part, cudaStream_t st) {
   norm::Params<S> p = norm_params<S>(a, L);
   p.part = part;
-  const bool channel = a.gate_kind == CPMTP_GATE_CHANNEL;
-  const bool vec = rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<bf16_t>(a.dy, a.d) && rows_vec<S>(a.dx_out, a.d) &&
-                   rows_vec<S>(a.dx, a.d) && rows_vec<bf16_t>(a.dblock, a.d) &&
-                   (!channel || (rows_vec<bf16_t>(a.gate, a.d) && rows_vec<bf16_t>(a.dgate, a.d))) && aligned(a.w_post, 16) && aligned(a.w_pre, 16);
-  const bool all = a.d % 256 == 0 && channel && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr && a.dx.data != nullptr &&
-                   a.dblock.data != nullptr && a.dgate.data != nullptr;
+  const bool all = a.d % 256 == 0 && a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr &&
+                   a.dx.data != nullptr && a.dblock.data != nullptr && a.dgate.data != nullptr;
   if (!vec) return launch_norm_bwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
   return all ? launch_norm_bwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_bwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
 }
+// Leaves the number of blocks, and so of partial sums of the weights' gradients, in `blocks`.
 template <class S>
-cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, int blocks, float* part, cudaStream_t st) {
-  if (L.threads > 512) return launch_norm_bwd<S, 1024, true>(a, L, blocks, part, st);
-  return L.G == 1 ? launch_norm_bwd<S, 512, true>(a, L, blocks, part, st) : launch_norm_bwd<S, 512, false>(a, L, blocks, part, st);
+cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, int sms, int& blocks, float* part, cudaStream_t st) {
+  const bool vec = rows_vec<S>(a.x_out, a.d) && rows_vec<bf16_t>(a.block, a.d) && rows_vec<bf16_t>(a.dy, a.d) && rows_vec<S>(a.dx_out, a.d) &&
+                   rows_vec<S>(a.dx, a.d) && rows_vec<bf16_t>(a.dblock, a.d) &&
+                   (a.gate_kind != CPMTP_GATE_CHANNEL || (rows_vec<bf16_t>(a.gate, a.d) && rows_vec<bf16_t>(a.dgate, a.d))) &&
+                   aligned(a.w_post, 16) && aligned(a.w_pre, 16);
+  const NormLayout L = norm_layout(a.d, vec);
+  blocks = norm_bwd_blocks(a, L, sms);
+  if (L.threads > 512) return launch_norm_bwd<S, 1024, true>(a, L, vec, blocks, part, st);
+  return L.G == 1 ? launch_norm_bwd<S, 512, true>(a, L, vec, blocks, part, st) : launch_norm_bwd<S, 512, false>(a, L, vec, blocks, part, st);
 }
 
 // ---------------------------------------------------------------------------------------------- optimiser
@@ -504,10 +515,9 @@ int cpmtp_norm_forward(const cpmtp_norm_args* args, cpmtp_stream stream) {
   DeviceInfo* di = nullptr;
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const NormLayout L = norm_layout(a.d);
   ProfScope prof(CPMTP_STAGE_NORM, st);
-  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_fwd<float>(a, L, di->sms, st));
-  else CPMTP_TRY(launch_norm_fwd<bf16_t>(a, L, di->sms, st));
+  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_fwd<float>(a, di->sms, st));
+  else CPMTP_TRY(launch_norm_fwd<bf16_t>(a, di->sms, st));
   return CPMTP_OK;
 }
 
@@ -515,8 +525,8 @@ size_t cpmtp_norm_workspace_bytes(const cpmtp_norm_args* args) {
   if (check_norm(args) != CPMTP_OK) return 0;
   DeviceInfo* di = device_info();
   const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
-  const NormLayout L = norm_layout(args->d);
-  return align_up(2 * sizeof(float) * static_cast<size_t>(norm_bwd_blocks(*args, L, sms)) * args->d + kAlign);
+  const int blocks[2] = {norm_bwd_blocks(*args, norm_layout(args->d, true), sms), norm_bwd_blocks(*args, norm_layout(args->d, false), sms)};
+  return align_up(2 * sizeof(float) * static_cast<size_t>(blocks[0] > blocks[1] ? blocks[0] : blocks[1]) * args->d + kAlign);
 }
 
 int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t workspace_bytes, cpmtp_stream stream) {
@@ -558,8 +568,7 @@ int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t wor
     if ((rc = check_gate(a, a.dgate)) != CPMTP_OK) return rc;
   }
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
-  const NormLayout L = norm_layout(a.d);
-  const int blocks = norm_bwd_blocks(a, L, di->sms);
+  int blocks = 0;
   float* part = nullptr;
   if (a.dw_post || a.dw_pre) {
     if (!workspace) return CPMTP_ERR_NULL;
@@ -567,8 +576,8 @@ int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t wor
     part = static_cast<float*>(workspace);
   }
   ProfScope prof(CPMTP_STAGE_NORM_GRAD, st);
-  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_bwd<float>(a, L, blocks, part, st));
-  else CPMTP_TRY(launch_norm_bwd<bf16_t>(a, L, blocks, part, st));
+  if (a.stream_type == CPMTP_F32) CPMTP_TRY(launch_norm_bwd<float>(a, di->sms, blocks, part, st));
+  else CPMTP_TRY(launch_norm_bwd<bf16_t>(a, di->sms, blocks, part, st));
   if (part != nullptr)
     CPMTP_TRY(launch_pdl(norm::norm_dw_kernel, dim3((a.d + 31) / 32, 2), dim3(1024), 0, st, part, blocks, a.d, static_cast<bf16_t*>(a.dw_post),
                          static_cast<bf16_t*>(a.dw_pre), accum ? 1 : 0));
