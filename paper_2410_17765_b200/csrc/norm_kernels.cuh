@@ -182,9 +182,16 @@ __device__ __forceinline__ void fetch_row(uint32_t region, const T* row, int t, 
     const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15);
     const char* base = reinterpret_cast<const char*>(row) - off;
     const int end = off + d * static_cast<int>(sizeof(T));
-    for (int j = t; j <= tg * kPer; j += tg) {
-      const int bytes = max(0, min(16, end - j * 16));    // zeros from the row's end to the region's
-      cp16(region + j * 16, bytes > 0 ? base + j * 16 : base, bytes);
+    const int left = end - 16 * t;
+    const char* from = base + 16 * t;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int bytes = max(0, min(16, left - 16 * k * tg));   // zeros from the row's end to the region's
+      cp16(region + (t + k * tg) * 16, bytes > 0 ? from + 16 * k * tg : base, bytes);
+    }
+    if (t == 0) {
+      const int bytes = max(0, min(16, end - 16 * kPer * tg));
+      cp16(region + kPer * tg * 16, bytes > 0 ? base + 16 * kPer * tg : base, bytes);
     }
   }
 }
