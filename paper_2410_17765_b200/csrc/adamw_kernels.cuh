@@ -47,7 +47,7 @@ struct Table {
   int first[CAP];                                // first run (thread block) of each tensor
   Tensor t[CAP];
 };
-constexpr int kSmallTable = 24, kMiddleTable = 96, kLargeTable = 300;   // a launch takes 3.4, 5 and 9 us with them
+constexpr int kSmallTable = 24, kMiddleTable = 96, kLargeTable = 300;   // a launch takes 3, 5 and up to 9 us with them
 
 // lowbias32 of Chris Wellons' hash-prospector: a bijection of 32 bits whose output bits each depend on every input bit
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {

@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   float sum[3];
   if (ONE && MAXT <= 512) {
     // A row is finished while the warps' sums of the next one are on their way: two rows are held at a time, which 128
-    // registers allow where rows' addresses are common to the block (8192 x 4096: 110 -> 101 us).
+    // registers allow where rows' addresses are common to the block (8192 x 4096: 110 -> 103 us).
     if (i < N) {
       Row row;
       end_sum3<ONE>(sum, before_sums(i, 0, row), red[0][at.rg], p.W, at.group, at.lane);
