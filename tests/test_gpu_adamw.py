@@ -92,6 +92,27 @@ def test_step(param, master, bits, offset):
     run_and_check(SIZES, param, master, bits, offset=offset)
 
 
+@pytest.mark.parametrize("scale", [1e-22, 1e-18, 1e-10, 1e6, 1e15])
+def test_eight_bit_states_far_from_one(scale):
+    """Exponents at which the powers of two of coding and decoding no longer fit into one factor, down to subnormal moments."""
+    from paper_2410_17765_b200 import binding
+
+    n = 4096 + 300
+    gen = torch.Generator().manual_seed(1)
+    p = torch.zeros(n, device="cuda")
+    opt = binding.AdamW([p], bits=8)
+    m, v = np.zeros(n, np.uint8), np.zeros(n, np.uint8)
+    me, ve = np.zeros(-(-n // 256), np.uint8), np.zeros(-(-n // 256), np.uint8)
+    for t in range(1, 5):
+        g = (torch.randn(n, generator=gen) * scale).cuda()
+        g[256:512] = 0                                     # and a block of nothing
+        opt.step([g], t, lr=1e-3, betas=HYPER["betas"], seed=3)
+        m, me, v, ve = T.adamw_states_8bit(g.cpu().numpy(), m, me, v, ve, betas=HYPER["betas"], step=t, seed=3)
+        for name, got, want in (("m", opt.m, m), ("m_exp", opt.m_exp, me), ("v", opt.v, v), ("v_exp", opt.v_exp, ve)):
+            assert (got[0].cpu().numpy() == want).all(), (name, t)
+    assert torch.isfinite(p).all()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_mixed_types_and_scaled_gradients(bits):
     run_and_check([1000, 4096], torch.bfloat16, True, bits, grad=torch.float32, coef=torch.full((1,), 0.37, device="cuda"))
