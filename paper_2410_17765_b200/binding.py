@@ -992,54 +992,96 @@ def grad_norm(grads, *, max_norm: float = float("inf"), workspace: Optional[torc
     return res
 
 
+def _state_column(name: str):
+    """An attribute of AdamW: aliases of the state tensors, in a tuple; assigning to it replaces them all."""
+
+    def read(self) -> tuple:
+        return tuple(None if t is None else t.detach() for t in self._states[name])
+
+    def write(self, tensors) -> None:
+        _need(all(t is None or isinstance(t, torch.Tensor) for t in tensors), f"{name} takes a list of tensors")
+        # Aliases, too: another tensor given to the caller's variables changes nothing here, and the memory stays theirs and ours
+        self._states[name] = [None if t is None else t.detach() for t in tensors]
+        self._at = None                    # the descriptors are out of date
+
+    return property(read, write)
+
+
 class AdamW:
     """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch per 300 tensors.
 
     params: contiguous bf16 or fp32 tensors, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
     one exponent byte per ADAMW_BLOCK elements).  master: True for fp32 copies of the bf16 parameters, or a list of
     them (None entries: none); without one a bf16 parameter is rounded stochastically.  lr_scale, decay_scale: factors per
-    tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run; new states are zero."""
+    tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run; new states are zero.
+
+    The list `params` and its tensors' memory may change between steps (`p.data = other`): every step compares their addresses
+    and sizes with those it knows, and on a difference checks all tensors again as at first.  Memory that was replaced is held until
+    then.  The states `m`, `v`, `m_exp`, `v_exp` and `master` are the memory that was given or made at first: read as tuples of
+    aliases, written in place, or replaced by assigning a whole list (`opt.m = tensors`)."""
+
+    m, v, m_exp, v_exp, master = map(_state_column, ("m", "v", "m_exp", "v_exp", "master"))
 
     def __init__(self, params, *, bits: int = 32, master=False, lr_scale=None, decay_scale=None, state: Optional[dict] = None):
         self.params = list(params)
         n = len(self.params)
         _need(bits in (32, 8), "bits must be 32 or 8")
         self.bits = bits
-        self._dev = _device(self.params[0]) if n else -1
-        for p in self.params:
-            if p.dtype not in _TYPES or not p.is_contiguous() or p.get_device() != self._dev:
-                raise CpmtpError("cpmtp: parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
-        self._numels = [p.numel() for p in self.params]
-        self._types = [_TYPES[p.dtype] for p in self.params]
+        for name, given in (("lr_scale", lr_scale), ("decay_scale", decay_scale)):
+            _need(given is None or len(given) == n, f"{name} needs one entry per parameter")
+        ones = [1.0] * n
+        self._factors = [struct.unpack("q", struct.pack("ff", a, b))[0] for a, b in zip(lr_scale or ones, decay_scale or ones)]
+        self._check_params()
         if master is True:
             master = [p.float() if p.dtype == torch.bfloat16 else None for p in self.params]
+        self._states = {}
         self.master = list(master) if master else [None] * n
-        for name, given in (("master", self.master), ("lr_scale", lr_scale), ("decay_scale", decay_scale)):
-            _need(given is None or len(given) == n, f"{name} needs one entry per parameter")
-        for w, p in zip(self.master, self.params):
-            if w is not None and (p.dtype != torch.bfloat16 or w.dtype != torch.float32 or not w.is_contiguous() or w.numel() != p.numel()
-                                  or w.get_device() != self._dev):
-                raise CpmtpError("cpmtp: a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
-        state = state or {}
-        moment = torch.float32 if bits == 32 else torch.uint8
-        blocks = [-(-k // ADAMW_BLOCK) for k in self._numels]
-        self.m, self.v = (self._states(state.get(k), moment, self._numels, k) for k in ("m", "v"))
-        self.m_exp, self.v_exp = (self._states(state.get(k), torch.uint8, blocks, k) if bits == 8 else [None] * n for k in ("m_exp", "v_exp"))
-        self._table = _Descriptors(n)
-        for word, tensors in ((0, self.params), (2, self.master), (3, self.m), (4, self.v), (5, self.m_exp), (6, self.v_exp)):
-            self._table.put(word, [0 if t is None else t.data_ptr() for t in tensors])
-        self._table.put(7, self._numels)
-        ones = [1.0] * n
-        self._table.put(9, [struct.unpack("q", struct.pack("ff", a, b))[0] for a, b in zip(lr_scale or ones, decay_scale or ones)])
+        for name, (dtype, sizes) in self._expected().items():
+            given = None if state is None else state.get(name)
+            setattr(self, name, [torch.zeros(k, dtype=dtype, device=p.device) for k, p in zip(sizes, self.params)] if given is None else given)
+        if bits == 32:
+            self.m_exp = self.v_exp = [None] * n
+        self._bind()
 
-    def _states(self, given, dtype, sizes, name) -> list:
-        if given is None:
-            return [torch.zeros(k, dtype=dtype, device=p.device) for k, p in zip(sizes, self.params)]
-        _need(len(given) == len(sizes), f"{name} needs one entry per parameter")
-        for t, k in zip(given, sizes):
-            if t.dtype != dtype or not t.is_contiguous() or t.numel() != k or t.get_device() != self._dev:
-                raise CpmtpError(f"cpmtp: {name} must be contiguous {dtype} tensors of {k} elements here")
-        return list(given)
+    def _check_params(self) -> int:
+        """Index of the parameters' device."""
+        dev = _device(self.params[0]) if self.params else -1
+        for p in self.params:
+            if p.dtype not in _TYPES or not p.is_contiguous() or p.get_device() != dev:
+                raise CpmtpError("cpmtp: parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
+        return dev
+
+    def _expected(self) -> dict:
+        """Type and lengths of the moments, by name."""
+        sizes = [p.numel() for p in self.params]
+        if self.bits == 32:
+            return dict(m=(torch.float32, sizes), v=(torch.float32, sizes))
+        blocks = [-(-k // ADAMW_BLOCK) for k in sizes]
+        return dict(m=(torch.uint8, sizes), v=(torch.uint8, sizes), m_exp=(torch.uint8, blocks), v_exp=(torch.uint8, blocks))
+
+    def _bind(self) -> None:
+        """Checks all tensors and writes them into the descriptors.  The parameters' memory, too, is held by aliases from here on: as
+        no other tensor can then come to lie at their addresses, comparing those is enough to notice a change."""
+        dev, n, states = self._check_params(), len(self.params), self._states
+        _need(len(self._factors) == n, "the number of parameters has changed")
+        _need(len(states["master"]) == n, "master needs one entry per parameter")
+        for w, p in zip(states["master"], self.params):
+            if w is not None and (p.dtype != torch.bfloat16 or w.dtype != torch.float32 or not w.is_contiguous() or w.numel() != p.numel()
+                                  or w.get_device() != dev):
+                raise CpmtpError("cpmtp: a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
+        for name, (dtype, sizes) in self._expected().items():
+            _need(len(states[name]) == n, f"{name} needs one entry per parameter")
+            for t, k in zip(states[name], sizes):
+                if t is None or t.dtype != dtype or not t.is_contiguous() or t.numel() != k or t.get_device() != dev:
+                    raise CpmtpError(f"cpmtp: {name} must be contiguous {dtype} tensors of {k} elements here")
+        table = _Descriptors(n)
+        held = [p.detach() for p in self.params]
+        for word, tensors in ((0, held), (2, states["master"]), (3, states["m"]), (4, states["v"]), (5, states["m_exp"]), (6, states["v_exp"])):
+            table.put(word, [0 if t is None else t.data_ptr() for t in tensors])
+        self._numels, self._types = [p.numel() for p in held], [_TYPES[p.dtype] for p in held]
+        table.put(7, self._numels)
+        table.put(9, self._factors)
+        self._table, self._held, self._at = table, held, [p.data_ptr() for p in held]
 
     def step(self, grads, t: int, *, lr: float, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
              coef: Optional[torch.Tensor] = None, seed: int = 0) -> None:
@@ -1050,6 +1092,8 @@ class AdamW:
         if n == 0:
             return
         dev = _device(self.params[0])
+        if list(map(_address_of, self.params)) != self._at or list(map(_size_of, self.params)) != self._numels:
+            self._bind()
         self._table.put_grads(grads, dev, self._types, self._numels)
         hyper = CAdamWHyper(lr, betas[0], betas[1], eps, weight_decay, t, seed & 0xFFFFFFFF, self.bits,
                             None if coef is None else _vector(coef, 1, torch.float32, dev, "coef"))

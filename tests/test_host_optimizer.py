@@ -1,0 +1,166 @@
+"""CPU-only checks of what the binding's optimiser hands to the library: a stand-in for the library records the descriptors."""
+import ctypes
+import gc
+
+import pytest
+import torch
+
+from paper_2410_17765_b200 import binding
+
+
+class Recorder:
+    """In the library's place: the descriptors of the last call, as a list of dicts."""
+
+    def __init__(self):
+        self.calls = []
+
+    def cpmtp_adamw_step(self, address, count, hyper, stream):
+        table = (binding.CAdamWTensor * count).from_address(address)
+        self.calls.append([{f[0]: getattr(t, f[0]) for f in t._fields_} for t in table])
+        return 0
+
+    @property
+    def last(self):
+        return self.calls[-1]
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(binding, "load_library", lambda: rec)
+    monkeypatch.setattr(binding, "_device", lambda t: t.get_device())       # (-1: the CPU, here as good as any)
+    monkeypatch.setattr(binding, "_raw_stream", lambda dev: 0)
+    return rec
+
+
+def check(lib, opt, grads):
+    """The last call named exactly the tensors that the optimiser's lists hold now."""
+    columns = dict(param=opt.params, grad=grads, master=opt.master, m=opt.m, v=opt.v)
+    if opt.bits == 8:
+        columns.update(m_exp=opt.m_exp, v_exp=opt.v_exp)
+    for i, got in enumerate(lib.last):
+        for name, tensors in columns.items():
+            assert (got[name] or 0) == (0 if tensors[i] is None else tensors[i].data_ptr()), (i, name)
+        assert got["numel"] == opt.params[i].numel()
+        assert got["param_type"] == binding._TYPES[opt.params[i].dtype]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("master", [False, True])
+def test_a_step_names_the_tensors_that_are_there_now(lib, bits, master):
+    sizes = [300, 7, 512]
+    params = [torch.zeros(n, dtype=torch.bfloat16) for n in sizes]
+    grads = [torch.zeros(n, dtype=torch.bfloat16) for n in sizes]
+    opt = binding.AdamW(params, bits=bits, master=master)
+    opt.step(grads, 1, lr=0.1)
+    check(lib, opt, grads)
+    params[1].data = torch.ones(7, dtype=torch.bfloat16)                    # what a module's .to() does
+    opt.step(grads, 2, lr=0.1)
+    check(lib, opt, grads)
+    for name in ["m", "v"] + (["m_exp", "v_exp"] if bits == 8 else []) + (["master"] if master else []):
+        setattr(opt, name, [t.clone() for t in getattr(opt, name)])         # a restored state
+        opt.step(grads, 3, lr=0.1)
+        check(lib, opt, grads)
+        with pytest.raises(TypeError):                                      # not one by one, which would go unnoticed
+            getattr(opt, name)[2] = getattr(opt, name)[2].clone()
+        getattr(opt, name)[0].data = torch.zeros(0)                         # the memory that a step writes stays what it was
+        opt.step(grads, 4, lr=0.1)
+        check(lib, opt, grads)
+        assert getattr(opt, name)[0].numel() > 0
+    if master:
+        opt.master = [None, *opt.master[1:]]
+        opt.step(grads, 5, lr=0.1)
+        check(lib, opt, grads)
+    opt.params[0] = torch.zeros(300, dtype=torch.bfloat16)
+    opt.step(grads, 6, lr=0.1)
+    check(lib, opt, grads)
+
+
+def test_memory_that_the_descriptors_name_is_held_until_they_are_renewed(lib):
+    """Else another tensor could come to lie there, with the same address and another size."""
+    p = torch.zeros(1 << 16)
+    opt = binding.AdamW([p])
+    was = [p.data_ptr(), opt.m[0].data_ptr()]
+    p.data = torch.zeros(0)
+    gc.collect()
+    fresh = [torch.zeros(1 << 16) for _ in range(16)]
+    assert all(t.data_ptr() not in was for t in fresh)
+
+
+def test_states_that_were_given_are_held_as_they_were(lib):
+    p, m = torch.zeros(300), torch.zeros(300)
+    opt = binding.AdamW([p], state=dict(m=[m], v=[torch.zeros(300)]))
+    was = m.data_ptr()
+    m.data = torch.zeros(300)
+    opt.step([torch.zeros(300)], 1, lr=0.1)
+    assert lib.last[0]["m"] == was == opt.m[0].data_ptr()
+
+
+def test_a_changed_type_is_taken_up(lib):
+    p = torch.zeros(300)
+    opt = binding.AdamW([p])
+    opt.step([torch.zeros(300)], 1, lr=0.1)
+    assert lib.last[0]["param_type"] == binding.F32
+    p.data = p.to(torch.bfloat16)
+    opt.step([torch.zeros(300)], 2, lr=0.1)
+    assert lib.last[0]["param_type"] == binding.BF16 and lib.last[0]["grad_type"] == binding.F32
+
+
+def test_tensors_that_no_longer_fit_are_refused(lib):
+    def fresh(bits=32):
+        p = [torch.zeros(64), torch.zeros(64)]
+        opt = binding.AdamW(p, bits=bits)
+        opt.step([torch.zeros(64)] * 2, 1, lr=0.1)
+        return p, opt
+
+    def replaced_by_a_shorter_one(p, opt):
+        p[0].data = torch.zeros(8)
+
+    def cut_where_it_lies(p, opt):
+        p[0].data = p[0].data[:8]
+
+    def state_of_another_size(p, opt):
+        opt.m = [torch.zeros(63), opt.m[1]]
+
+    def state_of_another_type(p, opt):
+        opt.v = [opt.v[0], torch.zeros(64, dtype=torch.float64)]
+
+    def state_gone(p, opt):
+        opt.v = [opt.v[0], None]
+
+    def another_type(p, opt):
+        p[1].data = torch.zeros(64, dtype=torch.float16)
+
+    def strided(p, opt):
+        p[1].data = torch.zeros(128)[::2]
+
+    def list_too_short(p, opt):
+        opt.m = opt.m[:1]
+
+    def master_of_fp32(p, opt):
+        opt.master = [torch.zeros(64), None]
+
+    def one_more(p, opt):
+        opt.params.append(torch.zeros(64))
+
+    for change in (replaced_by_a_shorter_one, cut_where_it_lies, state_of_another_size, state_of_another_type, state_gone, another_type, strided,
+                   list_too_short, master_of_fp32, one_more):
+        p, opt = fresh()
+        change(p, opt)
+        calls = len(lib.calls)
+        for _ in range(2):                                                  # and again: nothing of the change has stuck
+            with pytest.raises(binding.CpmtpError):
+                opt.step([torch.zeros(64)] * len(opt.params), 2, lr=0.1)
+                pytest.fail(f"{change.__name__} was accepted")
+        assert len(lib.calls) == calls
+    with pytest.raises(binding.CpmtpError):
+        opt.m = [1, 2]
+
+
+def test_nothing_changed_means_nothing_is_written_anew(lib, monkeypatch):
+    p = torch.zeros(64)
+    opt = binding.AdamW([p])
+    monkeypatch.setattr(opt, "_bind", lambda: pytest.fail("the descriptors were written anew"))
+    for t in range(1, 4):
+        p.add_(1)
+        opt.step([torch.zeros(64)], t, lr=0.1)
