@@ -505,7 +505,8 @@ typedef struct cpmtp_adamw_hyper {
  * AdamW (decoupled weight decay) over `count` tensors in one launch per 300 tensors:
  *   g = coef * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr wd) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
- * `tensors` is a HOST array, read during the call; what it points to is on the device.
+ * `tensors` is a HOST array, read during the call; what it points to is on the device.  All tensors are updated at the same
+ * time: no memory that is written may belong to two of them.
  *
  * 8-bit states: per block of CPMTP_ADAMW_BLOCK elements one exponent byte e (that of the block's largest magnitude
  * after room is left for one step up; 0: all zero, 255: the block held an infinity or NaN, and decodes to NaN) and one

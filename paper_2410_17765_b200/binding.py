@@ -1010,7 +1010,7 @@ def _state_column(name: str):
 class AdamW:
     """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch per 300 tensors.
 
-    params: contiguous bf16 or fp32 tensors, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
+    params: contiguous bf16 or fp32 tensors, each once, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
     one exponent byte per ADAMW_BLOCK elements).  master: True for fp32 copies of the bf16 parameters, or a list of
     them (None entries: none); without one a bf16 parameter is rounded stochastically.  lr_scale, decay_scale: factors per
     tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run; new states are zero.
@@ -1074,6 +1074,9 @@ class AdamW:
             for t, k in zip(states[name], sizes):
                 if t is None or t.dtype != dtype or not t.is_contiguous() or t.numel() != k or t.get_device() != dev:
                     raise CpmtpError(f"cpmtp: {name} must be contiguous {dtype} tensors of {k} elements here")
+        written = [t for t in [*self.params, *(t for column in states.values() for t in column)] if t is not None and t.numel() > 0]
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in written)
+        _need(all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "a tensor that a step writes is there twice, or overlaps another")
         table = _Descriptors(n)
         held = [p.detach() for p in self.params]
         for word, tensors in ((0, held), (2, states["master"]), (3, states["m"]), (4, states["v"]), (5, states["m_exp"]), (6, states["v_exp"])):

@@ -164,3 +164,27 @@ def test_nothing_changed_means_nothing_is_written_anew(lib, monkeypatch):
     for t in range(1, 4):
         p.add_(1)
         opt.step([torch.zeros(64)], t, lr=0.1)
+
+
+def test_memory_that_two_tensors_share_is_refused(lib):
+    """The tensors of a step are updated at the same time, in no order."""
+    flat, other = torch.zeros(600), torch.zeros(300)
+    half = [flat[:300], flat[300:]]
+    binding.AdamW(half)                                                     # next to one another is fine
+    states = dict(m=[torch.zeros(300) for _ in range(2)], v=[torch.zeros(300) for _ in range(2)])
+    binding.AdamW(half, state=states)
+    bad = [dict(params=[flat, flat]), dict(params=[flat[:300], flat[299:]]), dict(params=[flat[:300], flat[10:20], other]),
+           dict(params=half, state=dict(states, m=[other, other])), dict(params=half, state=dict(m=states["m"], v=states["m"])),
+           dict(params=half, state=dict(states, v=[other, flat[:300]])),
+           dict(params=[flat[:300].to(torch.bfloat16), flat[300:].to(torch.bfloat16)], master=[other, other])]
+    for i, kw in enumerate(bad):
+        with pytest.raises(binding.CpmtpError):
+            binding.AdamW(kw.pop("params"), **kw)
+            pytest.fail(f"case {i} was accepted")
+    empty = [torch.zeros(0), torch.zeros(0), flat]
+    binding.AdamW(empty)
+    opt = binding.AdamW(half)
+    half[1].data = flat[1:301]
+    with pytest.raises(binding.CpmtpError):
+        opt.step([torch.zeros(300)] * 2, 1, lr=0.1)
+    assert not lib.calls
