@@ -1013,7 +1013,7 @@ class AdamW:
     params: contiguous bf16 or fp32 tensors, each once, updated in place.  bits: 32 (fp32 moments) or 8 (one byte per element and
     one exponent byte per ADAMW_BLOCK elements).  master: True for fp32 copies of the bf16 parameters, or a list of
     them (None entries: none); without one a bf16 parameter is rounded stochastically.  lr_scale, decay_scale: factors per
-    tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run; new states are zero.
+    tensor.  state: {"m", "v"[, "m_exp", "v_exp"]}, lists of tensors of an earlier run, all of them; new states are zero.
 
     The list `params` and its tensors' memory may change between steps (`p.data = other`): every step compares their addresses
     and sizes with those it knows, and on a difference checks all tensors again as at first.  Memory that was replaced is held until
@@ -1036,8 +1036,11 @@ class AdamW:
             master = [p.float() if p.dtype == torch.bfloat16 else None for p in self.params]
         self._states = {}
         self.master = list(master) if master else [None] * n
-        for name, (dtype, sizes) in self._expected().items():
-            given = None if state is None else state.get(name)
+        expected = self._expected()
+        known = [k for k in expected if state is not None and state.get(k) is not None]
+        _need(len(known) in (0, len(expected)), f"a state has {', '.join(expected)}: all of them are needed")
+        for name, (dtype, sizes) in expected.items():
+            given = state[name] if known else None
             setattr(self, name, [torch.zeros(k, dtype=dtype, device=p.device) for k, p in zip(sizes, self.params)] if given is None else given)
         if bits == 32:
             self.m_exp = self.v_exp = [None] * n

@@ -188,3 +188,20 @@ def test_memory_that_two_tensors_share_is_refused(lib):
     with pytest.raises(binding.CpmtpError):
         opt.step([torch.zeros(300)] * 2, 1, lr=0.1)
     assert not lib.calls
+
+
+def test_a_state_is_given_as_a_whole(lib):
+    """8-bit codes without their exponents, or one moment without the other, are the states of no run."""
+    p = torch.zeros(600)
+    full = {32: dict(m=[torch.zeros(600)], v=[torch.zeros(600)]),
+            8: dict(m=[torch.zeros(600, dtype=torch.uint8)], v=[torch.zeros(600, dtype=torch.uint8)], m_exp=[torch.zeros(3, dtype=torch.uint8)],
+                    v_exp=[torch.zeros(3, dtype=torch.uint8)])}
+    for bits, state in full.items():
+        binding.AdamW([p], bits=bits, state=state)
+        binding.AdamW([p], bits=bits, state=dict.fromkeys(state))           # (None for all: a new run)
+        for name in state:
+            for less in ({k: t for k, t in state.items() if k != name}, dict(state, **{name: None})):
+                with pytest.raises(binding.CpmtpError):
+                    binding.AdamW([p], bits=bits, state=less)
+                    pytest.fail(f"{bits} bits without {name} were accepted")
+    binding.AdamW([p], state=dict(full[32], m_exp=None, v_exp=None))
