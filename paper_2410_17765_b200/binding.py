@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import functools
 import operator
 import os
 import struct
@@ -633,7 +632,6 @@ def distill_backward(h, W_head, E, W_g, x, teacher, saved: Saved, dsaved: Distil
 _TYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _dtype_of = operator.attrgetter("dtype")
 _address_of, _size_of, _device_of, _contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
-_is_tensor = functools.partial(operator.is_not, None)
 _ADAMW_WORDS = ctypes.sizeof(CAdamWTensor) // 8      # a descriptor in 8-byte words: param, grad, master, m, v, m_exp, v_exp, numel, types, factors
 
 
@@ -914,6 +912,14 @@ def norm_workspace_bytes(N: int, d: int) -> int:
     return int(load_library().cpmtp_norm_workspace_bytes(ctypes.byref(a)))
 
 
+def _spread(values, where: list, n: int) -> list:
+    """n zeros, and the values at their places."""
+    full = [0] * n
+    for i, v in zip(where, values):
+        full[i] = v
+    return full
+
+
 class _Descriptors:
     """An array of cpmtp_adamw_tensor, written a column at a time (a step updates hundreds of them before its one launch)."""
 
@@ -929,31 +935,33 @@ class _Descriptors:
 
     def put_grads(self, grads, dev: int, param_types: Optional[list] = None, numels: Optional[list] = None) -> None:
         """Addresses, sizes and types of the gradients, one per parameter of `numels` elements; None: no address."""
-        n = len(grads)
-        there = grads if all(map(_is_tensor, grads)) else [g for g in grads if g is not None]
-        if there:
-            # one property of all of them at a time: half the cost of a loop over the tensors
+        # one property of all of them at a time: half the cost of a loop over the tensors
+        there, where = grads, None
+        try:
             kinds = list(map(_dtype_of, there))
+        except AttributeError:                             # (None has no type)
+            where = [i for i, g in enumerate(grads) if g is not None]
+            there = [grads[i] for i in where]
+            kinds = list(map(_dtype_of, there))
+        if there:
             same = kinds.count(kinds[0]) == len(kinds)
             ok = kinds[0] in _TYPES if same else all(k in _TYPES for k in kinds)
             devices = list(map(_device_of, there))
             if not ok or devices.count(dev) != len(devices) or not all(map(_contiguous, there)):
                 raise CpmtpError("cpmtp: gradients must be contiguous bfloat16 or float32 tensors on the current CUDA device")
             kind = _TYPES[kinds[0]] << 32
-            types = [kind] * len(kinds) if same else [_TYPES[k] << 32 for k in kinds]
         else:
-            kind, same, types = 0, True, []
-        at, sizes = list(map(_address_of, there)), list(map(_size_of, there))
-        if len(there) < n:
-            where = [i for i, g in enumerate(grads) if g is not None]
-            at, sizes, types = ([dict(zip(where, v)).get(i, 0) for i in range(n)] for v in (at, sizes, types))
-            same = False
-        if numels is None:
-            self.put(7, sizes)
-        elif sizes != numels and any(g is not None and s != m for g, s, m in zip(grads, sizes, numels)):
+            kind, same = 0, True
+        at, sizes, n = list(map(_address_of, there)), list(map(_size_of, there)), len(grads)
+        if numels is not None and sizes != (numels if where is None else [numels[i] for i in where]):
             raise CpmtpError("cpmtp: a gradient must have its parameter's size")
-        self.put(1, at)
+        if numels is None:
+            self.put(7, sizes if where is None else _spread(sizes, where, n))
+        self.put(1, at if where is None else _spread(at, where, n))
         if not same or kind != self.grad_kind:             # (the types seldom change from step to step)
+            types = [_TYPES[k] << 32 for k in kinds] if not same else [kind] * n     # (a missing gradient's type does not matter)
+            if not same and where is not None:
+                types = _spread(types, where, n)
             self.put(8, types if param_types is None else map(operator.or_, types, param_types))
             self.grad_kind = kind if same else None
 
