@@ -507,6 +507,9 @@ typedef struct cpmtp_adamw_hyper {
  *   p = p (1 - lr wd) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
  * `tensors` is a HOST array, read during the call; what it points to is on the device.  All tensors are updated at the same
  * time: no memory that is written may belong to two of them.
+ * Moments are the same bits wherever an element lies.  The last bits of its parameter's update (1e-6 of the update) depend
+ * on its tensor's alignment and, with 8-bit states, on whether its block of CPMTP_ADAMW_BLOCK is a whole one.
+ * eps 0 is taken literally: an element whose second moment is 0 (no gradient yet, or none above 1e-22) then divides by 0.
  *
  * 8-bit states: per block of CPMTP_ADAMW_BLOCK elements one exponent byte e (that of the block's largest magnitude
  * after room is left for one step up; 0: all zero, 255: the block held an infinity or NaN, and decodes to NaN) and one

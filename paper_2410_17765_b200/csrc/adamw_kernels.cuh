@@ -38,7 +38,10 @@ struct Hyper {
   uint32_t key;                                  // of the rounding noise: seed and step
   const float* coef;
   float one;                                     // 1, see update_block8()
+  int small_eps;                                 // roots of subnormal second moments count beside eps
 };
+// A root below 2^-63 (of a moment below 2^-126) adds less than half a unit of fp32 to eps from here on, per unit of rsqrt_bc2.
+constexpr float kSmallEps = 1.f / 549755813888.f;                      // 2^-39
 
 template <int CAP>
 struct Table {
@@ -239,15 +242,30 @@ __device__ __forceinline__ float unit_of(int e) { return __uint_as_float(static_
 // 2^(15 - e): back
 __device__ __forceinline__ float inverse_unit_of(int e) { return __uint_as_float(static_cast<uint32_t>(142 - e) << 23); }
 
+// Root and reciprocal; FLUSH: single instructions, which take subnormal numbers for zeros (668 M bf16 parameters: the
+// question which of the two a block takes costs 0.5 %; without the flush the root of a subnormal moment stays beside a small eps).
+template <bool FLUSH>
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  if (FLUSH) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  else asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+template <bool FLUSH>
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  if (FLUSH) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  else asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+template <bool FLUSH>
+__device__ __forceinline__ void update_params(f32x2 (&p)[4], const f32x2 (&m)[4], const f32x2 (&v)[4], const Tensor& t, const Hyper& h) {
+  const f32x2 step = both(-t.step_size), keep = both(t.keep), bias = both(h.rsqrt_bc2), eps = both(h.eps);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x2 below = fma2(io::pair(sqrt_approx<FLUSH>(io::lo(v[k])), sqrt_approx<FLUSH>(io::hi(v[k]))), bias, eps);
+    p[k] = fma2(p[k], keep, mul2(mul2(m[k], step), io::pair(rcp_approx<FLUSH>(io::lo(below)), rcp_approx<FLUSH>(io::hi(below)))));
+  }
 }
 __device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
@@ -355,8 +373,7 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
       v[k] = mul2(mul2(mul2(v[k], huge), uv), b2);
     }
   }
-  const f32x2 coef2 = both(coef), omb1 = both(h.omb1), omb2 = both(h.omb2), step = both(-t.step_size), keep = both(t.keep);
-  const f32x2 bias = both(h.rsqrt_bc2), eps = both(h.eps);
+  const f32x2 coef2 = both(coef), omb1 = both(h.omb1), omb2 = both(h.omb2);
   // sums as products with a 1 that the compiler does not know: a packed sum of a packed product was found to come out as one
   // operation with one rounding, for all the explicit roundings of the two
   const f32x2 one = both(h.one);
@@ -368,9 +385,9 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
     v[k] = fma2(v[k], one, mul2(mul2(gk, omb2), gk));
     top_m = max_nan(top_m, fabsf(io::lo(m[k])), fabsf(io::hi(m[k])));
     top_v = max_nan(top_v, io::lo(v[k]), io::hi(v[k]));
-    const f32x2 below = fma2(io::pair(sqrt_approx(io::lo(v[k])), sqrt_approx(io::hi(v[k]))), bias, eps);
-    p[k] = fma2(p[k], keep, mul2(mul2(m[k], step), io::pair(rcp_approx(io::lo(below)), rcp_approx(io::hi(below)))));
   }
+  if (h.small_eps) update_params<false>(p, m, v, t, h);
+  else update_params<true>(p, m, v, t, h);
   const uint32_t top_mb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), top_vb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
   const int em = min(block_exp<kDropM>(top_mb), 255), ev = min(block_exp<kDropV>(top_vb), 255);
   // the first step of mix() for eight places that differ in their lowest three bits alone

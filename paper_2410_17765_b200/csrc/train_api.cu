@@ -356,6 +356,7 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
   h.key = adamw::mix(adamw::mix(hyper.seed) ^ static_cast<uint32_t>(hyper.step));
   h.coef = hyper.coef;
   h.one = 1.f;
+  h.small_eps = h.eps < adamw::kSmallEps * h.rsqrt_bc2;
   const size_t state = hyper.state_bits == 8 ? 8 : 32;
   return for_tables<CAP>(
       tensors, count, h, run_length(tensors, count, hyper.state_bits == 8 ? adamw::kLongRun : adamw::kRun, sms),
