@@ -41,10 +41,11 @@ def sigmoid(z):
         return 1.0 / (1.0 + np.exp(-np.asarray(z, np.float64)))
 
 
-def _gate(gate):
+def _gate(gate, sign=1):
+    """The gate; sign -1: one minus it, which the difference would lose above a logit of 37."""
     if gate is None:
         return np.ones((1, 1))
-    g = sigmoid(gate)
+    g = sigmoid(sign * np.asarray(gate, np.float64))
     return g[:, None] if g.ndim == 1 else g
 
 
@@ -92,7 +93,8 @@ def norm_backward(dy, x_out, w_pre=None, rstd_pre=None, dx_out=None, block=None,
             u = b
             r["dblock"], mag["dblock"] = du, dum
         if gate is not None:
-            dg, dgm = t * u * g * (1 - g), tm * np.abs(u) * g * (1 - g)
+            slope = g * _gate(gate, -1)
+            dg, dgm = t * u * slope, tm * np.abs(u) * slope
             row = np.ndim(gate) == 1
             r["dgate"], mag["dgate"] = (dg.sum(1), dgm.sum(1)) if row else (dg, dgm)
     r["mag"] = mag

@@ -59,11 +59,22 @@ __device__ __forceinline__ float rcp(float v) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ float sigmoid(float z) { return rcp(1.f + ptx::ex2_approx(z * -1.4426950408889634f)); }
-__device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
+__device__ __forceinline__ float exp_minus(float z) { return ptx::ex2_approx(z * -1.4426950408889634f); }
+__device__ __forceinline__ f32x2 exp_minus2(f32x2 z) {
   const f32x2 e = mul2(z, both(-1.4426950408889634f));
-  const f32x2 s = add2(io::pair(ptx::ex2_approx(io::lo(e)), ptx::ex2_approx(io::hi(e))), both(1.f));
+  return io::pair(ptx::ex2_approx(io::lo(e)), ptx::ex2_approx(io::hi(e)));
+}
+// the gate from e = exp(-z)
+__device__ __forceinline__ float gate_of(float e) { return rcp(1.f + e); }
+__device__ __forceinline__ f32x2 gate_of2(f32x2 e) {
+  const f32x2 s = add2(e, both(1.f));
   return io::pair(rcp(io::lo(s)), rcp(io::hi(s)));
+}
+// What an open gate leaves, 1 - g, as e g: the difference has no digit left at a logit of 17.  Where e is infinite and g zero, or
+// both are NaN, saturation makes the product zero; g, which everything it is multiplied with holds, says the rest.
+__device__ __forceinline__ float rest_of(float e, float g) { return __saturatef(e * g); }
+__device__ __forceinline__ f32x2 rest_of2(f32x2 e, f32x2 g) {
+  return io::pair(rest_of(io::lo(e), io::lo(g)), rest_of(io::hi(e), io::hi(g)));
 }
 
 // Barrier of the W warps of a row.  It counts warps, so a warp's lanes come together first.
@@ -343,9 +354,9 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
       if (channel) {
         take8<VEC>(s + rs + rb16, p.gate, i, t, g);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) g[k] = sigmoid2(g[k]);
+        for (int k = 0; k < 4; ++k) g[k] = gate_of2(exp_minus2(g[k]));
       } else {
-        fill8(g, row_gate ? sigmoid(gl) : 1.f);
+        fill8(g, row_gate ? gate_of(exp_minus(gl)) : 1.f);
       }
       if (has_post) {
         if (t == 0 && (ALL || p.rstd_post != nullptr)) p.rstd_post[i] = rb;
@@ -388,8 +399,13 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) norm_fwd_kernel(const __gri
 template <class S>
 __host__ __device__ constexpr int bwd_stage_bytes(int threads) { return 2 * region_bytes<S>(threads) + 3 * region_bytes<bf16_t>(threads); }
 
-template <class S, bool VEC, int MAXT, int STAGES, bool ONE, bool ALL>
+// Forms of the kernel: a gate per row or none, which leaves out all arithmetic on gates of channels (8192 x 4096, a gate per row: 89 us
+// against 113 in one form with the next); a gate per channel; and the latter with everything there (see above).
+enum { kRowGate, kChannelGate, kAll };
+
+template <class S, bool VEC, int MAXT, int STAGES, bool ONE, int FORM>
 __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ Params<S> p) {
+  constexpr bool ALL = FORM == kAll, CHANNEL = FORM != kRowGate;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float red[2][ONE ? 1 : 8][4][kMaxWarps];
   const Place<ONE> at(p.W);
@@ -398,7 +414,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   uint8_t* ring = smem + at.group * STAGES * stage_bytes;
   const unsigned step = gridDim.x * (ONE ? 1 : p.G);      // rows; N < 2^31, so that a few steps past N do not wrap
   const bool has_block = ALL || p.block.data != nullptr, has_post = ALL || (has_block && p.w_post != nullptr);
-  const bool channel = ALL || p.gate_kind == CPMTP_GATE_CHANNEL, row_gate = !ALL && p.gate_kind == CPMTP_GATE_ROW;
+  const bool row_gate = !CHANNEL && p.gate_kind == CPMTP_GATE_ROW;
   const bool has_y = ALL || p.dy.data != nullptr, has_dx_out = ALL || p.dx_out.data != nullptr;
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
@@ -413,7 +429,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
       s += 2 * rs;
       if (has_y) fetch_row<VEC, ALL>(s, p.dy.at(row), t, tg, d);
       if (has_block) fetch_row<VEC, ALL>(s + rb16, p.block.at(row), t, tg, d);
-      if (channel) fetch_row<VEC, ALL>(s + 2 * rb16, p.gate.at(row), t, tg, d);
+      if (CHANNEL) fetch_row<VEC, ALL>(s + 2 * rb16, p.gate.at(row), t, tg, d);
     }
     commit_row();
   };
@@ -428,9 +444,18 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   int stage = 0;
 
   // Row r, the it-th of this group: what comes before its sums, into `row`, and the sums as far as this warp goes.
+  // Gates are held as e = exp(-logit), from which g and 1 - g are made where they are used (holding both: 123 us against 96 at
+  // 8192 x 4096).  Where registers are short not even that: the logits are read from the ring again (16384 x 2047: 145 us
+  // against 156; 4096 x 8192, 64 registers: 127 against 146).
+  constexpr bool PIPE = ONE && MAXT <= 512, KEEP_E = ALL ? MAXT <= 512 : !ONE;
   struct Row {
-    f32x2 x[4], a[4], b[4], g[4];
-    float rx, rb, grow;
+    f32x2 x[4], a[4], b[4], e[CHANNEL && KEEP_E ? 4 : 1];
+    float rx, rb, erow;
+  };
+  auto gates = [&](unsigned r, int stage, f32x2 (&e)[4]) {
+    take8<VEC>(ring + stage * stage_bytes + 2 * rs + 2 * rb16, p.gate, r, t, e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = exp_minus2(e[k]);
   };
   auto before_sums = [&](unsigned r, int it, Row& row) -> float {
     if ((it & 31) == 0) {
@@ -440,12 +465,13 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
     }
     row.rx = __shfl_sync(0xffffffffu, rstds_pre, it & 31);
     row.rb = __shfl_sync(0xffffffffu, rstds_post, it & 31);
-    row.grow = row_gate ? sigmoid(__shfl_sync(0xffffffffu, logits, it & 31)) : 1.f;
+    row.erow = row_gate ? exp_minus(__shfl_sync(0xffffffffu, logits, it & 31)) : 0.f;
     wait_row<STAGES - 2>();
     if (!VEC) row_barrier<ONE>(p.W, at.group);
     const uint8_t* s = ring + stage * stage_bytes;
+    f32x2 dy[4], e[4];
+    if (CHANNEL) gates(r, stage, e);
     stage = stage + 1 == STAGES ? 0 : stage + 1;
-    f32x2 dy[4];
     take8<VEC>(s, p.x_out, r, t, row.x);
     if (has_dx_out) take8<VEC>(s + rs, p.dx_out, r, t, row.a);
     else fill8(row.a, 0.f);
@@ -454,13 +480,6 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
     else fill8(dy, 0.f);
     if (has_block) take8<VEC>(s + rb16, p.block, r, t, row.b);
     else fill8(row.b, 0.f);
-    if (channel) {
-      take8<VEC>(s + 2 * rb16, p.gate, r, t, row.g);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) row.g[k] = sigmoid2(row.g[k]);
-    } else {
-      fill8(row.g, 1.f);
-    }
     f32x2 s0 = both(0.f), s1 = s0, s2 = s0;
     const f32x2 rx2 = both(row.rx);
 #pragma unroll
@@ -468,7 +487,9 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
       const f32x2 dyr = mul2(dy[k], rx2), wdyr = mul2(w_pre[k], dyr);
       acc_pre[k] = fma2(dyr, row.x[k], acc_pre[k]);
       row.a[k] = add2(row.a[k], wdyr);
-      const f32x2 q = mul2(mul2(w_post[k], row.b[k]), row.g[k]);
+      f32x2 q = mul2(w_post[k], row.b[k]);
+      if (CHANNEL) q = mul2(q, gate_of2(e[k]));
+      if (CHANNEL && KEEP_E) row.e[k] = e[k];
       s0 = fma2(wdyr, row.x[k], s0);
       s1 = fma2(q, row.a[k], s1);
       s2 = fma2(q, row.x[k], s2);
@@ -476,27 +497,38 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
     const float sum[3] = {io::lo(s0) + io::hi(s0), io::lo(s1) + io::hi(s1), io::lo(s2) + io::hi(s2)};
     return begin_sum3<ONE>(sum, red[it & 1][at.rg], p.W, at.wg, at.lane);
   };
-  // And what comes after them.
-  auto after_sums = [&](unsigned r, const Row& row, const float (&sum)[3]) {
+  // And what comes after them, when `ago` rows from this one on have been read: it is still in the ring.
+  auto after_sums = [&](unsigned r, const Row& row, const float (&sum)[3], int ago) {
     const float c1 = row.rx * row.rx * sum[0] * p.inv_d;              // t = a - c1 x
     const float dot = row.rb * fmaf(-c1, sum[2], sum[1]);             // sum of t u (the row gate left out)
-    const f32x2 minus_c1 = both(-c1), grb = both(row.grow * row.rb), scale = both(p.res_scale);
-    const f32x2 minus_c2 = both(has_post ? -row.rb * row.rb * row.grow * dot * p.inv_d : 0.f);
-    f32x2 dx[4], dblock[4], dgate[4];
+    const float grow = row_gate ? gate_of(row.erow) : 1.f;
+    const f32x2 minus_c1 = both(-c1), grb = both(grow * row.rb), scale = both(p.res_scale);
+    const f32x2 minus_c2 = both(has_post ? -row.rb * row.rb * grow * dot * p.inv_d : 0.f);
+    f32x2 dx[4], dblock[4], dgate[4], e[4];
+    if (CHANNEL && !KEEP_E) gates(r, stage >= ago ? stage - ago : stage + STAGES - ago, e);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const f32x2 tk = fma2(minus_c1, row.x[k], row.a[k]);
-      const f32x2 dur = mul2(mul2(grb, row.g[k]), tk);                // rstd_post du
+      f32x2 dur = mul2(grb, tk), rest = 0ull;                         // rstd_post du
+      if (CHANNEL) {
+        if (KEEP_E) {
+          e[k] = row.e[k];
+          asm("" : "+l"(e[k]));                                       // (a new value: else g is held since before the sums)
+        }
+        const f32x2 g = gate_of2(e[k]);
+        dur = mul2(dur, g);
+        rest = rest_of2(e[k], g);
+      }
       acc_post[k] = fma2(dur, row.b[k], acc_post[k]);
       dblock[k] = fma2(w_post[k], dur, mul2(minus_c2, row.b[k]));
-      dgate[k] = mul2(mul2(mul2(w_post[k], row.b[k]), dur), fma2(row.g[k], both(-1.f), both(1.f)));
+      if (CHANNEL) dgate[k] = mul2(mul2(mul2(w_post[k], row.b[k]), dur), rest);
       dx[k] = mul2(scale, tk);
     }
     if (ALL || p.dx.data != nullptr) put8<VEC, ALL>(p.dx.at(r), t, d, dx);
     if (ALL || p.dblock.data != nullptr) put8<VEC, ALL>(p.dblock.at(r), t, d, dblock);
     if (ALL || p.dgate.data != nullptr) {
-      if (channel) put8<VEC, ALL>(p.dgate.at(r), t, d, dgate);
-      else if (t == 0) *p.dgate.at(r) = io::from_f<bf16_t>(row.grow * (1.f - row.grow) * dot);
+      if (CHANNEL) put8<VEC, ALL>(p.dgate.at(r), t, d, dgate);
+      else if (t == 0) *p.dgate.at(r) = io::from_f<bf16_t>(grow * rest_of(row.erow, grow) * dot);
     }
   };
 
@@ -506,7 +538,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
     fetch(r + (STAGES - 1) * step, stage >= 2 ? stage - 2 : stage + STAGES - 2);
   };
   float sum[3];
-  if (ONE && MAXT <= 512) {
+  if (PIPE) {
     // A row is finished while the warps' sums of the next one are on their way: two rows are held at a time, which 128
     // registers allow where rows' addresses are common to the block (8192 x 4096: 110 -> 103 us).
     if (i < N) {
@@ -517,11 +549,11 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
         fetch_after(i);
         Row next;
         const float c = before_sums(i + step, it, next);
-        after_sums(i, row, sum);
+        after_sums(i, row, sum, 2);
         end_sum3<ONE>(sum, c, red[it & 1][at.rg], p.W, at.group, at.lane);
         row = next;
       }
-      after_sums(i, row, sum);
+      after_sums(i, row, sum, 1);
     }
   } else {
     for (int it = 0; i < N; i += step, ++it) {
@@ -529,7 +561,7 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
       const float c = before_sums(i, it, row);
       fetch_after(i);
       end_sum3<ONE>(sum, c, red[it & 1][at.rg], p.W, at.group, at.lane);
-      after_sums(i, row, sum);
+      after_sums(i, row, sum, 1);
     }
   }
   if (p.part == nullptr) return;

@@ -238,11 +238,11 @@ cudaError_t launch_norm_fwd(const cpmtp_norm_args& a, int sms, cudaStream_t st) 
   return L.G == 1 ? launch_norm_fwd<S, 512, true>(a, L, vec, sms, st) : launch_norm_fwd<S, 512, false>(a, L, vec, sms, st);
 }
 
-template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
+template <class S, bool VEC, int MAXT, bool ONE, int FORM>
 cudaError_t launch_norm_bwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
   constexpr int kStages = bwd_stages<S, MAXT>();
   static bool done[64] = {};
-  auto* kernel = norm::norm_bwd_kernel<S, VEC, MAXT, kStages, ONE, ALL>;
+  auto* kernel = norm::norm_bwd_kernel<S, VEC, MAXT, kStages, ONE, FORM>;
   const cudaError_t e = allow_smem(kernel, done, kStages * kMaxGroups<ONE> * norm::bwd_stage_bytes<S>(MAXT / kMaxGroups<ONE>));
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(blocks), dim3(L.threads), kStages * L.G * norm::bwd_stage_bytes<S>(L.W * 32), st, p);
@@ -254,8 +254,12 @@ cudaError_t launch_norm_bwd(const cpmtp_norm_args& a, const NormLayout& L, bool 
   p.part = part;
   const bool all = a.d % 256 == 0 && a.gate_kind == CPMTP_GATE_CHANNEL && a.w_post != nullptr && a.dy.data != nullptr && a.dx_out.data != nullptr &&
                    a.dx.data != nullptr && a.dblock.data != nullptr && a.dgate.data != nullptr;
-  if (!vec) return launch_norm_bwd_as<S, false, MAXT, ONE, false>(p, L, blocks, st);
-  return all ? launch_norm_bwd_as<S, true, MAXT, ONE, true>(p, L, blocks, st) : launch_norm_bwd_as<S, true, MAXT, ONE, false>(p, L, blocks, st);
+  if (vec && all) return launch_norm_bwd_as<S, true, MAXT, ONE, norm::kAll>(p, L, blocks, st);
+  if (a.gate_kind == CPMTP_GATE_CHANNEL)
+    return vec ? launch_norm_bwd_as<S, true, MAXT, ONE, norm::kChannelGate>(p, L, blocks, st)
+               : launch_norm_bwd_as<S, false, MAXT, ONE, norm::kChannelGate>(p, L, blocks, st);
+  return vec ? launch_norm_bwd_as<S, true, MAXT, ONE, norm::kRowGate>(p, L, blocks, st)
+             : launch_norm_bwd_as<S, false, MAXT, ONE, norm::kRowGate>(p, L, blocks, st);
 }
 // Leaves the number of blocks, and so of partial sums of the weights' gradients, in `blocks`.
 template <class S>

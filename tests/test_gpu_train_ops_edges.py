@@ -46,3 +46,36 @@ def test_second_moments_below_the_normal_numbers(bits, n, offset, eps):
             m, v = opt.m[0].cpu().numpy(), opt.v[0].cpu().numpy()
         else:
             m, v = (T.decode(getattr(opt, k)[0].cpu().numpy(), getattr(opt, k + "_exp")[0].cpu().numpy(), k == "v") for k in ("m", "v"))
+
+
+@pytest.mark.parametrize("gate", ["row", "channel"])
+@pytest.mark.parametrize("stream", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 100, 1024, 1027, 4096, 4352, 4354])
+@pytest.mark.parametrize("whole", [True, False])
+def test_gradients_of_open_and_closed_gates(gate, stream, d, whole):
+    """g (1 - g) keeps its digits wherever it is a number at all; bounds as in the tests of the norms: 2e-5 of the terms' magnitudes, which hold the
+    factor g (1 - g), and half a unit of the output."""
+    from paper_2410_17765_b200 import binding
+
+    logits = np.array([0, 3, 6, 9, 10, 11, 12, 14, 16, 17, 20, 30, 50, 80, -10, -12, -16, -17, -30, -80], np.float32)
+    N = 40
+    gen = torch.Generator().manual_seed(d)
+
+    def draw(*shape, dtype=torch.bfloat16):
+        return torch.randn(*shape, generator=gen).to(dtype).cuda()
+
+    x, block, dy, dx_out = draw(N, d, dtype=stream), draw(N, d), draw(N, d), draw(N, d, dtype=stream)
+    w_pre, w_post = draw(d), draw(d)
+    at = np.arange(N) if gate == "row" else np.arange(N)[:, None] + np.arange(d)[None]
+    z = torch.from_numpy(logits[at % logits.size]).to(torch.bfloat16).cuda()
+    f = binding.norm_forward(x, w_pre, block=block, gate=z, w_post=w_post)
+    # with all outputs, and with the gate's gradient alone (another form of the kernel)
+    r = binding.norm_backward(dy, f["x_out"], w_pre, f["rstd_pre"], dx_out=dx_out, block=block, gate=z, w_post=w_post, rstd_post=f["rstd_post"],
+                              skip=() if whole else ("dx", "dblock", "dw_post", "dw_pre"))
+    a = [t.double().cpu().numpy() for t in (dy, f["x_out"], w_pre, f["rstd_pre"], dx_out, block, z, w_post, f["rstd_post"])]
+    want = T.norm_backward(*a)
+    for k in [k for k in want["mag"] if r[k] is not None]:
+        last = 2.0 ** -8 if r[k].dtype == torch.bfloat16 else 2.0 ** -23
+        err = np.abs(r[k].double().cpu().numpy() - want[k])
+        assert (err <= 2e-5 * want["mag"][k] + last * np.abs(want[k]) + 1e-37).all(), (k, err.max())
+    assert r["dgate"] is not None
