@@ -794,39 +794,43 @@ def norm_forward(x: torch.Tensor, w_pre: Optional[torch.Tensor] = None, *, block
     x [N, d] bf16 or fp32; block and gate ([N, d], or one logit per row [N]) bf16, rows may be strided (the halves of one
     projection's output).  Without w_post the block is added as it is, without w_pre there is no y, without a block
     x_out is x itself and y its norm.  Returns {"x_out", "y", "rstd_post", "rstd_pre"} (None where there is none);
-    tensors given in `out` are written instead of new ones (x_out may be x)."""
+    tensors given in `out` are written instead of new ones (x_out may be x), the dictionary itself is left as it is."""
     dev = _device(x)
     a, size, dtype = _norm_args(x, dev, w_pre, block, gate, w_post, res_scale, eps)
     a.x, a.ld_x = _rows(x, size, dtype, dev, "x")
     N = size[0]
-    res = {} if out is None else out
+    given, res = {} if out is None else out, {}
     device, d = x.device, size[1]
     if block is None:
         res["x_out"] = x
-    elif (t := res.get("x_out")) is None:
+    elif (t := given.get("x_out")) is None:
         t = res["x_out"] = _empty(size, dtype, x)
         a.x_out, a.ld_x_out = t.data_ptr(), d
     else:
+        res["x_out"] = t
         a.x_out, a.ld_x_out = _rows(t, size, dtype, dev, "x_out")
     if w_pre is None:
         res["y"] = res["rstd_pre"] = None
     else:
-        if (t := res.get("y")) is None:
+        if (t := given.get("y")) is None:
             t = res["y"] = _empty(size, torch.bfloat16, x)
             a.y, a.ld_y = t.data_ptr(), d
         else:
+            res["y"] = t
             a.y, a.ld_y = _rows(t, size, torch.bfloat16, dev, "y")
-        if (t := res.get("rstd_pre")) is None:
+        if (t := given.get("rstd_pre")) is None:
             t = res["rstd_pre"] = torch.empty(N, dtype=torch.float32, device=device)
             a.rstd_pre = t.data_ptr()
         else:
+            res["rstd_pre"] = t
             a.rstd_pre = _vector(t, N, torch.float32, dev, "rstd_pre")
     if w_post is None:
         res["rstd_post"] = None
-    elif (t := res.get("rstd_post")) is None:
+    elif (t := given.get("rstd_post")) is None:
         t = res["rstd_post"] = torch.empty(N, dtype=torch.float32, device=device)
         a.rstd_post = t.data_ptr()
     else:
+        res["rstd_post"] = t
         a.rstd_post = _vector(t, N, torch.float32, dev, "rstd_post")
     rc = load_library().cpmtp_norm_forward(ctypes.byref(a), _raw_stream(dev))
     if rc:
@@ -843,7 +847,7 @@ def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Option
     """cpmtp_norm_backward; x_out, rstd_pre and rstd_post as norm_forward returned them, the other inputs as it was given.
     dy [N, d] bf16 (None: no gradient of y), dx_out [N, d] of the stream's type (None: zero).
     Returns {"dx", "dblock", "dgate", "dw_post", "dw_pre"}: None where there is nothing to differentiate or the name is
-    in `skip`.  accumulate: dw_post and dw_pre are added to those given in `out`."""
+    in `skip`.  accumulate: dw_post and dw_pre are added to those given in `out`, which itself is left as it is."""
     dev = _device(x_out)
     a, size, dtype = _norm_args(x_out, dev, w_pre, block, gate, w_post, res_scale, eps)
     N, d = size
@@ -860,38 +864,42 @@ def norm_backward(dy: Optional[torch.Tensor], x_out: torch.Tensor, w_pre: Option
     if w_post is not None:
         _need(rstd_post is not None, "w_post needs rstd_post")
         a.rstd_post = _vector(rstd_post, N, torch.float32, dev, "rstd_post")
-    res = {} if out is None else out
+    given, res = {} if out is None else out, {}
 
     # outputs: not there or not wanted, given, or new ones, which need no check
     if "dx" in skip:
         res["dx"] = None
-    elif (t := res.get("dx")) is None:
+    elif (t := given.get("dx")) is None:
         t = res["dx"] = _empty(size, dtype, x_out)
         a.dx, a.ld_dx = t.data_ptr(), d
     else:
+        res["dx"] = t
         a.dx, a.ld_dx = _rows(t, size, dtype, dev, "dx")
     if block is None or "dblock" in skip:
         res["dblock"] = None
-    elif (t := res.get("dblock")) is None:
+    elif (t := given.get("dblock")) is None:
         t = res["dblock"] = _empty(size, bf16, x_out if dy is None else dy)
         a.dblock, a.ld_dblock = t.data_ptr(), d
     else:
+        res["dblock"] = t
         a.dblock, a.ld_dblock = _rows(t, size, bf16, dev, "dblock")
     if gate is None or "dgate" in skip:
         res["dgate"] = None
-    elif (t := res.get("dgate")) is None:
+    elif (t := given.get("dgate")) is None:
         t = res["dgate"] = _empty(gate.shape, bf16, x_out if dy is None else dy)
         a.dgate, a.ld_dgate = t.data_ptr(), d if a.gate_kind == GATE_CHANNEL else 1
     else:
+        res["dgate"] = t
         a.dgate, a.ld_dgate = _rows(t, size, bf16, dev, "dgate") if a.gate_kind == GATE_CHANNEL else _row_gate(t, N, dev, "dgate")
     for name, there in (("dw_post", w_post is not None), ("dw_pre", dy is not None)):
         if not there or name in skip:
             res[name] = None
-        elif (t := res.get(name)) is None:
+        elif (t := given.get(name)) is None:
             _need(not accumulate, "accumulation needs dw_post and dw_pre in out")
             t = res[name] = torch.empty(d, dtype=bf16, device=device)
             setattr(a, name, t.data_ptr())
         else:
+            res[name] = t
             setattr(a, name, _vector(t, d, bf16, dev, name))
     if accumulate:
         a.flags = FLAG_ACCUM_GRADS
