@@ -444,7 +444,7 @@ typedef struct cpmtp_norm_args {
   int32_t stream_type;     /* CPMTP_BF16 or CPMTP_F32: type of x, x_out, dx_out and dx; all else is bf16 */
   int32_t gate_kind;       /* CPMTP_GATE_* */
   uint32_t flags;          /* CPMTP_FLAG_ACCUM_GRADS (backward): dw_post and dw_pre are added to */
-  float eps;               /* > 0 */
+  float eps;               /* >= 2^-126, the smallest normal number */
   float res_scale;
   cpmtp_rows x, block, gate;         /* residual stream; block output (data NULL: none); gate logits */
   const void *w_post, *w_pre;        /* [d] weights of the norm after / before a block; NULL: no such norm */

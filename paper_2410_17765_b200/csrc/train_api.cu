@@ -3,6 +3,7 @@
 #include "../../include/cpmtp.h"
 
 #include <cuda_runtime.h>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -171,7 +172,8 @@ int check_norm(const cpmtp_norm_args* a) {
   if (a->N < 0 || a->d < 1 || !known_type(a->stream_type)) return CPMTP_ERR_SHAPE;
   if (a->d > CPMTP_NORM_MAX_D) return CPMTP_ERR_LIMIT;
   if (a->gate_kind < CPMTP_GATE_NONE || a->gate_kind > CPMTP_GATE_CHANNEL) return CPMTP_ERR_SHAPE;
-  if (!(a->eps > 0.f) || !std::isfinite(a->eps) || !std::isfinite(a->res_scale)) return CPMTP_ERR_SHAPE;
+  // (of a subnormal eps the rstd of a row of zeros would have an infinite square, which the gradient multiplies by zero)
+  if (!(a->eps >= FLT_MIN) || !std::isfinite(a->eps) || !std::isfinite(a->res_scale)) return CPMTP_ERR_SHAPE;
   if (a->N > 0 && a->block.data == nullptr) {      // (without rows a block may have no address)
     // a norm alone: nothing to gate, to scale or to norm before the addition
     if (a->gate_kind != CPMTP_GATE_NONE || a->w_post != nullptr || a->res_scale != 1.f) return CPMTP_ERR_SHAPE;

@@ -79,3 +79,36 @@ def test_gradients_of_open_and_closed_gates(gate, stream, d, whole):
         err = np.abs(r[k].double().cpu().numpy() - want[k])
         assert (err <= 2e-5 * want["mag"][k] + last * np.abs(want[k]) + 1e-37).all(), (k, err.max())
     assert r["dgate"] is not None
+
+
+@pytest.mark.parametrize("gate", ["none", "row", "channel"])
+@pytest.mark.parametrize("d", [64, 100, 4096, 4352])
+def test_rows_of_zeros_with_the_smallest_eps(gate, d):
+    """rstd is then 2^63; the gradients of rows of zeros are finite and those of the others do not notice."""
+    from paper_2410_17765_b200 import binding
+
+    eps, N = 2.0 ** -126, 24
+    gen = torch.Generator().manual_seed(d)
+
+    def draw(*shape):
+        return torch.randn(*shape, generator=gen).to(torch.bfloat16).cuda()
+
+    def check(r, *a):
+        want = T.norm_backward(*[None if t is None else t.double().cpu().numpy() for t in a])
+        for k in want["mag"]:
+            err = np.abs(r[k].double().cpu().numpy() - want[k])
+            assert (err <= 2e-5 * want["mag"][k] + 2.0 ** -8 * np.abs(want[k]) + 1e-37).all(), (k, err.max())
+
+    x, block, dy, dx_out, w_pre, w_post = draw(N, d), draw(N, d), draw(N, d), draw(N, d), draw(d), draw(d)
+    z = {"none": None, "row": draw(N), "channel": draw(N, d)}[gate]
+    block[::3] = 0
+    f = binding.norm_forward(x, w_pre, block=block, gate=z, w_post=w_post, eps=eps)
+    assert float(f["rstd_post"][0]) == 2.0 ** 63
+    r = binding.norm_backward(dy, f["x_out"], w_pre, f["rstd_pre"], dx_out=dx_out, block=block, gate=z, w_post=w_post, rstd_post=f["rstd_post"], eps=eps)
+    check(r, dy, f["x_out"], w_pre, f["rstd_pre"], dx_out, block, z, w_post, f["rstd_post"])
+    x[::2] = 0
+    f = binding.norm_forward(x, w_pre, eps=eps)
+    assert float(f["rstd_pre"][0]) == 2.0 ** 63 and not f["y"][0].any()
+    check(binding.norm_backward(dy, x, w_pre, f["rstd_pre"], dx_out=dx_out, eps=eps), dy, x, w_pre, f["rstd_pre"], dx_out)
+    with pytest.raises(binding.CpmtpError):
+        binding.norm_forward(x, w_pre, eps=1e-40)

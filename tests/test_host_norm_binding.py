@@ -72,3 +72,21 @@ def test_backward_leaves_the_dictionary_as_it_is(lib):
     empty = {}
     r = binding.norm_backward(dy, x, w, rstd, out=empty, **kw)
     assert not empty and all(lib.args[k] == r[k].data_ptr() for k in full)
+
+
+def test_eps_has_to_be_a_normal_number():
+    """The rstd of a row of zeros would have an infinite square, and the gradient of that row be NaN."""
+    import ctypes
+
+    from paper_2410_17765_b200 import build
+
+    build.build()
+    args = binding.CNormArgs(0, D, binding.BF16, binding.GATE_NONE, 0, 2.0 ** -126, 1.0)       # (no rows: nothing is enqueued)
+    args.w_pre = 4096
+    real = binding.load_library()
+    assert real.cpmtp_norm_forward(ctypes.byref(args), None) == 0
+    for eps in (1e-40, 2.0 ** -127, 0.0, -1.0):
+        args.eps = eps
+        assert real.cpmtp_norm_forward(ctypes.byref(args), None) == -2
+        assert real.cpmtp_norm_backward(ctypes.byref(args), None, 0, None) == -2
+        assert real.cpmtp_norm_workspace_bytes(ctypes.byref(args)) == 0
