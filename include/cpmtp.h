@@ -146,7 +146,7 @@ typedef struct CUstream_st* cpmtp_stream;
 int cpmtp_debug_status(void);
 
 int cpmtp_version(void);   /* major * 100 + minor * 10; 110 added the distillation entry points, 120 CPMTP_FLAG_ACCUM_GRADS,
-                              130 the embedding, norm and optimiser entry points */
+                              130 the embedding, norm and optimiser entry points, 140 optimiser steps by a clock */
 const char* cpmtp_status_string(int status);
 
 /* Read the environment knobs listed above again (they are otherwise read once per process).  For tests
@@ -524,6 +524,29 @@ typedef struct cpmtp_adamw_hyper {
  */
 int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
                      cpmtp_stream stream);
+
+/*
+ * What a captured step cannot have from the host.  cpmtp_adamw_step writes its step number, learning rate and seed into the launch:
+ * replayed from a graph it is the SAME step again, with the same bias corrections and, for every element, the same rounding noise, which
+ * then no longer keeps the mean.  A step that is to be replayed takes them from a clock in device memory.
+ */
+typedef struct cpmtp_adamw_clock {
+  int64_t step;            /* of the last step taken, 0 before the first (and whatever is below counts as 0) */
+  double lr;               /* >= 0 and finite, which is not checked */
+  uint32_t seed;
+  uint32_t key;            /* this and what follows: written by the steps */
+  double bc1;
+  float rsqrt_bc2;
+  float unused;
+} cpmtp_adamw_clock;
+
+/*
+ * cpmtp_adamw_step with step + 1, lr and seed of `clock` (device memory, 8-byte aligned) in place of those of `hyper`, which are not
+ * looked at; the clock is advanced, also where a NaN coefficient makes the step change nothing.  The results are bit for bit those of
+ * cpmtp_adamw_step with the same numbers.  Between steps the caller may write step, lr and seed, in the stream's order.
+ */
+int cpmtp_adamw_step_clocked(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
+                             cpmtp_adamw_clock* clock, cpmtp_stream stream);
 
 /* The values of an 8-bit state of n elements as bf16 (exactly): `second` 0 for m, 1 for v. */
 int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,

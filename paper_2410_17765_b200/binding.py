@@ -34,7 +34,7 @@ EXPORTS = [
     "cpmtp_distill_forward", "cpmtp_distill_backward", "cpmtp_reload_knobs", "cpmtp_debug_status",
     "cpmtp_embed_forward", "cpmtp_embed_workspace_bytes", "cpmtp_embed_backward",
     "cpmtp_norm_forward", "cpmtp_norm_workspace_bytes", "cpmtp_norm_backward",
-    "cpmtp_adamw_step", "cpmtp_adamw_state_values", "cpmtp_grad_norm_workspace_bytes", "cpmtp_grad_norm",
+    "cpmtp_adamw_step", "cpmtp_adamw_step_clocked", "cpmtp_adamw_state_values", "cpmtp_grad_norm_workspace_bytes", "cpmtp_grad_norm",
 ]
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -93,6 +93,11 @@ class CAdamWHyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint32),
                 ("state_bits", ctypes.c_int32), ("coef", ctypes.c_void_p)]
+
+
+class CAdamWClock(ctypes.Structure):
+    _fields_ = [("step", ctypes.c_int64), ("lr", ctypes.c_double), ("seed", ctypes.c_uint32), ("key", ctypes.c_uint32), ("bc1", ctypes.c_double),
+                ("rsqrt_bc2", ctypes.c_float), ("unused", ctypes.c_float)]
 
 
 _lib = None
@@ -161,6 +166,8 @@ def load_library() -> ctypes.CDLL:
     lib.cpmtp_norm_backward.argtypes = [nap, vp, sz, vp]
     lib.cpmtp_adamw_step.restype = ctypes.c_int
     lib.cpmtp_adamw_step.argtypes = [atp, ctypes.c_int32, ctypes.POINTER(CAdamWHyper), vp]
+    lib.cpmtp_adamw_step_clocked.restype = ctypes.c_int
+    lib.cpmtp_adamw_step_clocked.argtypes = [atp, ctypes.c_int32, ctypes.POINTER(CAdamWHyper), vp, vp]
     lib.cpmtp_adamw_state_values.restype = ctypes.c_int
     lib.cpmtp_adamw_state_values.argtypes = [vp, vp, ctypes.c_int64, ctypes.c_int32, vp, vp]
     lib.cpmtp_grad_norm_workspace_bytes.restype = sz
@@ -1023,6 +1030,18 @@ def _state_column(name: str):
     return property(read, write)
 
 
+class StepClock:
+    """Step number, learning rate and seed on the device (cpmtp_adamw_clock), for optimiser steps that are captured in a CUDA graph: every
+    replay is the next step.  `step` (int64 [1], of the last step taken) and `lr` (float64 [1]) are views to read, and to write between steps
+    in the stream's order, as a schedule does (`clock.lr.fill_(...)`)."""
+
+    def __init__(self, lr: float, *, step: int = 0, seed: int = 0, device="cuda"):
+        _need(step >= 0 and 0.0 <= lr < float("inf"), "a clock's step and learning rate are finite and not negative")
+        block = CAdamWClock(step=step, lr=lr, seed=seed & 0xFFFFFFFF)
+        self.block = torch.frombuffer(bytearray(block), dtype=torch.uint8).to(device)
+        self.step, self.lr = self.block[:8].view(torch.int64), self.block[8:16].view(torch.float64)
+
+
 class AdamW:
     """Parameters and their optimiser states, stepped by cpmtp_adamw_step in one launch per 300 tensors.
 
@@ -1105,10 +1124,12 @@ class AdamW:
         table.put(9, self._factors)
         self._table, self._held, self._at = table, held, [p.data_ptr() for p in held]
 
-    def step(self, grads, t: int, *, lr: float, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
+    def step(self, grads, t, *, lr: Optional[float] = None, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
              coef: Optional[torch.Tensor] = None, seed: int = 0) -> None:
         """Step t (1 for the first) with one gradient per parameter (bf16 or fp32, contiguous; None leaves a parameter alone).
-        coef: fp32 [1] on the device that multiplies the gradients (grad_norm's), or None."""
+        coef: fp32 [1] on the device that multiplies the gradients (grad_norm's), or None.
+        t may be a StepClock, which has the learning rate and the seed as well.  A step that is captured for replaying needs one: with a
+        number, each replay would be that step again, with the same bias corrections and rounding noise."""
         n = len(self.params)
         _need(len(grads) == n, "one gradient per parameter")
         if n == 0:
@@ -1117,9 +1138,16 @@ class AdamW:
         if list(map(_address_of, self.params)) != self._at or list(map(_size_of, self.params)) != self._numels:
             self._bind()
         self._table.put_grads(grads, dev, self._types, self._numels)
-        hyper = CAdamWHyper(lr, betas[0], betas[1], eps, weight_decay, t, seed & 0xFFFFFFFF, self.bits,
+        clock = t if isinstance(t, StepClock) else None
+        _need((lr is None) == (clock is not None), "a learning rate is needed, here or in the clock")
+        _need(clock is None or seed == 0, "the seed is the clock's")
+        hyper = CAdamWHyper(0.0 if clock else lr, betas[0], betas[1], eps, weight_decay, 1 if clock else t, seed & 0xFFFFFFFF, self.bits,
                             None if coef is None else _vector(coef, 1, torch.float32, dev, "coef"))
-        rc = load_library().cpmtp_adamw_step(self._table.address, n, ctypes.byref(hyper), _raw_stream(dev))
+        if clock is None:
+            rc = load_library().cpmtp_adamw_step(self._table.address, n, ctypes.byref(hyper), _raw_stream(dev))
+        else:
+            at = _vector(clock.block, ctypes.sizeof(CAdamWClock), torch.uint8, dev, "the clock")
+            rc = load_library().cpmtp_adamw_step_clocked(self._table.address, n, ctypes.byref(hyper), at, _raw_stream(dev))
         if rc:
             _check(rc)
 

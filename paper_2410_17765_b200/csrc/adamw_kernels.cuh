@@ -1,9 +1,10 @@
 // AdamW over many tensors in one launch, states in fp32 or 8 bits, and the norm of all gradients.
 //
 // The tensors' descriptors travel in the kernel's parameters (up to 32 KB), so a step is one launch with no copy to
-// the device, and can be captured.  Bound by bandwidth with fp32 states (133 M parameters with an fp32 copy, 28 bytes each: 561 us,
-// 6.6 TB/s), by instruction issue with 8-bit ones (10 bytes each: 286 us).  Every block takes one run of elements of one tensor; a warp takes 256 elements at a time, which
-// are also what shares an exponent in an 8-bit state.
+// the device, and can be captured; to be replayed as the steps that follow it takes what changes from step to step from a
+// clock in device memory, which a second, tiny launch advances.  Bound by bandwidth with fp32 states (133 M parameters with an
+// fp32 copy, 28 bytes each: 561 us, 6.6 TB/s), by instruction issue with 8-bit ones (10 bytes each: 286 us).  Every block takes one run
+// of elements of one tensor; a warp takes 256 elements at a time, which are also what shares an exponent in an 8-bit state.
 #pragma once
 #include "vec_io.cuh"
 
@@ -28,17 +29,25 @@ struct Tensor {
   uint8_t *m_exp, *v_exp;
   long long numel;
   long long place;                               // of its first element among all tensors' elements
-  float step_size, keep;                         // lr / (1 - beta1^t) and 1 - lr wd, with the tensor's factors
+  float step_size, keep;                         // see Rates; with a clock the tensor's factors of lr and wd alone
   int16_t param_f32, grad_f32;
   int32_t vec;                                   // every pointer allows accesses of eight elements
 };
 
-struct Hyper {
-  float b1, omb1, b2, omb2, rsqrt_bc2, eps;
+// What changes from step to step: of all tensors, and (the first two) of one.
+struct Rates {
+  float step_size, keep, rsqrt_bc2;              // lr / (1 - beta1^t) and 1 - lr wd, with the tensor's factors; (1 - beta2^t)^(-1/2)
   uint32_t key;                                  // of the rounding noise: seed and step
+  int small_eps;                                 // roots of subnormal second moments count beside eps
+};
+
+struct Hyper {
+  float b1, omb1, b2, omb2, eps;
+  Rates r;                                       // (no clock) but for what depends on the tensor
   const float* coef;
   float one;                                     // 1, see update_block8()
-  int small_eps;                                 // roots of subnormal second moments count beside eps
+  const cpmtp_adamw_clock* clock;                // the step's number and rate are there, nullptr: in r
+  double wd;
 };
 // A root below 2^-63 (of a moment below 2^-126) adds less than half a unit of fp32 to eps from here on, per unit of rsqrt_bc2.
 constexpr float kSmallEps = 1.f / 549755813888.f;                      // 2^-39
@@ -53,6 +62,35 @@ struct Table {
 };
 constexpr int kSmallTable = 24, kMiddleTable = 96, kLargeTable = 300;   // a launch takes 3, 5 and up to 9 us with them
 
+// Products and differences of doubles rounded one by one, so that host and device get the same bits.
+__host__ __device__ __forceinline__ double product(double a, double b) {
+#ifdef __CUDA_ARCH__
+  return __dmul_rn(a, b);
+#else
+  return a * b;
+#endif
+}
+__host__ __device__ __forceinline__ double one_minus(double a) {
+#ifdef __CUDA_ARCH__
+  return __dsub_rn(1.0, a);
+#else
+  return 1.0 - a;
+#endif
+}
+__host__ __device__ __forceinline__ double power(double base, unsigned long long n) {
+  double r = 1.0;
+  for (; n > 0; n >>= 1, base = product(base, base))
+    if (n & 1) r = product(r, base);
+  return r;
+}
+__host__ __device__ __forceinline__ float step_size_of(double lr, float factor, double bc1) { return static_cast<float>(product(lr, factor) / bc1); }
+__host__ __device__ __forceinline__ float keep_of(double lr, float factor, double wd, float decay_factor) {
+  return static_cast<float>(one_minus(product(product(product(lr, factor), wd), decay_factor)));
+}
+__host__ __device__ __forceinline__ float rsqrt_bc2_of(double beta2, unsigned long long t) {
+  return static_cast<float>(1.0 / sqrt(one_minus(power(beta2, t))));
+}
+
 // lowbias32 of Chris Wellons' hash-prospector: a bijection of 32 bits whose output bits each depend on every input bit
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x ^= x >> 16;
@@ -60,6 +98,19 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x ^= x >> 15;
   x *= 0x846ca68bu;
   return x ^ (x >> 16);
+}
+
+__host__ __device__ __forceinline__ uint32_t noise_key(uint32_t seed, unsigned long long t) { return mix(mix(seed) ^ static_cast<uint32_t>(t)); }
+
+// The clock's next step.
+__global__ void adamw_clock_kernel(cpmtp_adamw_clock* clock, double beta1, double beta2) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
+  const unsigned long long t = (clock->step > 0 ? clock->step : 0) + 1;
+  clock->step = static_cast<long long>(t);
+  clock->bc1 = one_minus(power(beta1, t));
+  clock->rsqrt_bc2 = rsqrt_bc2_of(beta2, t);
+  clock->key = noise_key(clock->seed, t);
 }
 
 // 2^(e - 127) for e in [0, 254]
@@ -141,7 +192,7 @@ __device__ __forceinline__ float round_up_or_down(float p, uint32_t noise) {
 
 // One warp's 256 elements, `left` of them inside the tensor.  8-bit states that allow wide accesses go through update_block8().
 template <int BITS, bool VEC>
-__device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float coef, long long at, int left, int lane) {
+__device__ __forceinline__ void update(const Tensor& t, const Hyper& h, const Rates& r, float coef, long long at, int left, int lane) {
   static_assert(BITS == 32 || !VEC, "see above");
   float g[8], m[8], v[8], p[8];
   read_any<VEC>(t.grad, t.grad_f32, at, lane, left, g);
@@ -172,13 +223,13 @@ __device__ __forceinline__ void update(const Tensor& t, const Hyper& h, float co
     const float gk = __fmul_rn(g[k], coef);
     m[k] = __fadd_rn(__fmul_rn(m[k], h.b1), __fmul_rn(gk, h.omb1));
     v[k] = __fadd_rn(__fmul_rn(v[k], h.b2), __fmul_rn(__fmul_rn(gk, h.omb2), gk));
-    p[k] = p[k] * t.keep - __fdividef(m[k] * t.step_size, fmaf(sqrtf(v[k]), h.rsqrt_bc2, h.eps));
+    p[k] = p[k] * r.keep - __fdividef(m[k] * r.step_size, fmaf(sqrtf(v[k]), r.rsqrt_bc2, h.eps));
   }
   const bool rounds_p = t.master == nullptr && !t.param_f32;
   uint32_t noise[8];
   if (BITS == 8 || rounds_p) {
     const unsigned long long place = static_cast<unsigned long long>(t.place + at);
-    const uint32_t key = h.key ^ (static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
+    const uint32_t key = r.key ^ (static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
 #pragma unroll
     for (int k = 0; k < 8; ++k) noise[k] = mix((static_cast<uint32_t>(place) + elem<VEC>(lane, k)) ^ key);
   }
@@ -259,8 +310,8 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return r;
 }
 template <bool FLUSH>
-__device__ __forceinline__ void update_params(f32x2 (&p)[4], const f32x2 (&m)[4], const f32x2 (&v)[4], const Tensor& t, const Hyper& h) {
-  const f32x2 step = both(-t.step_size), keep = both(t.keep), bias = both(h.rsqrt_bc2), eps = both(h.eps);
+__device__ __forceinline__ void update_params(f32x2 (&p)[4], const f32x2 (&m)[4], const f32x2 (&v)[4], const Hyper& h, const Rates& r) {
+  const f32x2 step = both(-r.step_size), keep = both(r.keep), bias = both(r.rsqrt_bc2), eps = both(h.eps);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const f32x2 below = fma2(io::pair(sqrt_approx<FLUSH>(io::lo(v[k])), sqrt_approx<FLUSH>(io::hi(v[k]))), bias, eps);
@@ -341,7 +392,7 @@ __device__ __forceinline__ void take_block8(const Tensor& t, const uint8_t* stag
   in.p = take_raw(p, t.param_f32 || t.master != nullptr);
 }
 
-__device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, float coef, long long at, int lane, const Loaded8& in) {
+__device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, const Rates& r, float coef, long long at, int lane, const Loaded8& in) {
   f32x2 g[4], m[4], v[4], p[4];
   numbers(in.g, t.grad_f32, g);
   numbers(in.p, t.param_f32 || t.master != nullptr, p);
@@ -386,13 +437,13 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
     top_m = max_nan(top_m, fabsf(io::lo(m[k])), fabsf(io::hi(m[k])));
     top_v = max_nan(top_v, io::lo(v[k]), io::hi(v[k]));
   }
-  if (h.small_eps) update_params<false>(p, m, v, t, h);
-  else update_params<true>(p, m, v, t, h);
+  if (r.small_eps) update_params<false>(p, m, v, h, r);
+  else update_params<true>(p, m, v, h, r);
   const uint32_t top_mb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), top_vb = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
   const int em = min(block_exp<kDropM>(top_mb), 255), ev = min(block_exp<kDropV>(top_vb), 255);
   // the first step of mix() for eight places that differ in their lowest three bits alone
   const unsigned long long place = static_cast<unsigned long long>(t.place + at);
-  uint32_t base = (static_cast<uint32_t>(place) + 8 * lane) ^ h.key ^ (static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
+  uint32_t base = (static_cast<uint32_t>(place) + 8 * lane) ^ r.key ^ (static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
   base ^= base >> 16;
   uint32_t noise[8];
 #pragma unroll
@@ -466,7 +517,24 @@ __device__ __forceinline__ void update_block8(const Tensor& t, const Hyper& h, f
   }
 }
 
-template <int CAP>
+// The rates of tensor t.  CLOCK: from the clock, with the operations that the host would have made.
+template <bool CLOCK>
+__device__ __forceinline__ Rates rates_of(const Tensor& t, const Hyper& h) {
+  Rates r = h.r;
+  r.step_size = t.step_size;
+  r.keep = t.keep;
+  if (CLOCK) {
+    const double lr = h.clock->lr;
+    r.step_size = step_size_of(lr, t.step_size, h.clock->bc1);
+    r.keep = keep_of(lr, t.step_size, h.wd, t.keep);
+    r.rsqrt_bc2 = h.clock->rsqrt_bc2;
+    r.key = h.clock->key;
+    r.small_eps = h.eps < kSmallEps * r.rsqrt_bc2;
+  }
+  return r;
+}
+
+template <int CAP, bool CLOCK>
 __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ Table<CAP> tab) {
   const int which = tensor_of(tab, blockIdx.x);
   const Tensor& t = tab.t[which];
@@ -475,18 +543,19 @@ __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant
   ptx::grid_dep_launch();
   const float coef = tab.h.coef != nullptr ? *tab.h.coef : 1.f;
   if (coef != coef) return;                      // the gradients were not finite
+  const Rates r = rates_of<CLOCK>(t, tab.h);
   const long long start = static_cast<long long>(static_cast<int>(blockIdx.x) - tab.first[which]) * tab.run;
 #pragma unroll 1
   for (int b = warp * kBlock; b < tab.run; b += kWarps * kBlock) {
     const long long at = start + b;
     if (at >= t.numel) break;
     const int left = static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock)));
-    if (t.vec) update<32, true>(t, tab.h, coef, at, left, lane);
-    else update<32, false>(t, tab.h, coef, at, left, lane);
+    if (t.vec) update<32, true>(t, tab.h, r, coef, at, left, lane);
+    else update<32, false>(t, tab.h, r, coef, at, left, lane);
   }
 }
 
-template <int CAP>
+template <int CAP, bool CLOCK>
 __global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_constant__ Table<CAP> tab, const int bytes) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int which = tensor_of(tab, blockIdx.x);
@@ -518,6 +587,7 @@ __global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_consta
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     return;
   }
+  const Rates r = rates_of<CLOCK>(t, tab.h);
   int n = 0;
 #pragma unroll 1
   for (int b = warp; b < whole; b += kWarps, ++n) {
@@ -527,13 +597,13 @@ __global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_consta
     take_block8(t, ring + (n % kAhead) * bytes, lane, in);
     in.em = __shfl_sync(0xffffffffu, em, n);
     in.ev = __shfl_sync(0xffffffffu, ev, n);
-    update_block8(t, tab.h, coef, start + static_cast<long long>(b) * kBlock, lane, in);
+    update_block8(t, tab.h, r, coef, start + static_cast<long long>(b) * kBlock, lane, in);
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   // what is left: the tensor's last block, or all of one whose pointers do not allow wide accesses
   for (int b = whole + (warp - whole % kWarps + kWarps) % kWarps; b < blocks; b += kWarps) {
     const long long at = start + static_cast<long long>(b) * kBlock;
-    update<8, false>(t, tab.h, coef, at, static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock))), lane);
+    update<8, false>(t, tab.h, r, coef, at, static_cast<int>(min(t.numel - at, static_cast<long long>(kBlock))), lane);
   }
 }
 

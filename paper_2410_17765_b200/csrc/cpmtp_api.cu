@@ -769,7 +769,7 @@ static int backward_impl(const cpmtp_shape* shape, const void* h, const void* W_
 
 extern "C" {
 
-int cpmtp_version(void) { return 130; }   // 1.3: embedding, norms, optimiser
+int cpmtp_version(void) { return 140; }   // 1.4: optimiser steps by a clock on the device
 
 int cpmtp_reload_knobs(void) {
   knobs();   // make sure the one-time read has happened, then read again

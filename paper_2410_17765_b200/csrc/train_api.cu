@@ -348,21 +348,24 @@ int for_tables(const cpmtp_adamw_tensor* tensors, int32_t count, const adamw::Hy
   return tab.count > 0 ? fn(tab, static_cast<int>(runs)) : CPMTP_OK;
 }
 
-template <int CAP>
-int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, int sms, cudaStream_t st) {
-  adamw::Hyper h;
+template <int CAP, bool CLOCK>
+int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, const cpmtp_adamw_clock* clock, int sms,
+               cudaStream_t st) {
+  adamw::Hyper h = {};
   h.b1 = static_cast<float>(hyper.beta1);
   h.omb1 = static_cast<float>(1.0 - hyper.beta1);
   h.b2 = static_cast<float>(hyper.beta2);
   h.omb2 = static_cast<float>(1.0 - hyper.beta2);
-  const double t = static_cast<double>(hyper.step);
-  const double bc1 = 1.0 - std::pow(hyper.beta1, t), bc2 = 1.0 - std::pow(hyper.beta2, t);
-  h.rsqrt_bc2 = static_cast<float>(1.0 / std::sqrt(bc2));
   h.eps = static_cast<float>(hyper.eps);
-  h.key = adamw::mix(adamw::mix(hyper.seed) ^ static_cast<uint32_t>(hyper.step));
+  const unsigned long long t = CLOCK ? 1 : hyper.step;
+  const double bc1 = adamw::one_minus(adamw::power(hyper.beta1, t));
+  h.r.rsqrt_bc2 = adamw::rsqrt_bc2_of(hyper.beta2, t);
+  h.r.key = adamw::noise_key(hyper.seed, t);
+  h.r.small_eps = h.eps < adamw::kSmallEps * h.r.rsqrt_bc2;
+  h.clock = clock;
+  h.wd = hyper.weight_decay;
   h.coef = hyper.coef;
   h.one = 1.f;
-  h.small_eps = h.eps < adamw::kSmallEps * h.rsqrt_bc2;
   const size_t state = hyper.state_bits == 8 ? 8 : 32;
   return for_tables<CAP>(
       tensors, count, h, run_length(tensors, count, hyper.state_bits == 8 ? adamw::kLongRun : adamw::kRun, sms),
@@ -370,8 +373,8 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
         out.param = in.param; out.grad = in.grad; out.master = in.master;
         out.m = in.m; out.v = in.v; out.m_exp = in.m_exp; out.v_exp = in.v_exp;
         out.numel = in.numel; out.place = place;
-        out.step_size = static_cast<float>(hyper.lr * in.lr_scale / bc1);
-        out.keep = static_cast<float>(1.0 - hyper.lr * in.lr_scale * hyper.weight_decay * in.decay_scale);
+        out.step_size = CLOCK ? in.lr_scale : adamw::step_size_of(hyper.lr, in.lr_scale, bc1);
+        out.keep = CLOCK ? in.decay_scale : adamw::keep_of(hyper.lr, in.lr_scale, hyper.weight_decay, in.decay_scale);
         out.param_f32 = in.param_type == CPMTP_F32; out.grad_f32 = in.grad_type == CPMTP_F32;
         out.vec = aligned(in.param, 8 * type_bytes(in.param_type)) && aligned(in.grad, 8 * type_bytes(in.grad_type)) &&
                   aligned(in.master, 32) && aligned(in.m, state) && aligned(in.v, state);
@@ -379,7 +382,7 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
       [&](const adamw::Table<CAP>& tab, int runs) -> int {
         ProfScope prof(CPMTP_STAGE_ADAMW, st);
         if (hyper.state_bits != 8) {
-          CPMTP_TRY(launch_pdl(adamw::adamw32_kernel<CAP>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
+          CPMTP_TRY(launch_pdl(adamw::adamw32_kernel<CAP, CLOCK>, dim3(runs), dim3(adamw::kThreads), 0, st, tab));
           return CPMTP_OK;
         }
         bool g32 = false, p32 = false;
@@ -389,11 +392,26 @@ int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_ada
         }
         constexpr int kPer = adamw::kWarps * adamw::kAhead;
         static bool done[64] = {};
-        CPMTP_TRY(allow_smem(adamw::adamw8_kernel<CAP>, done, kPer * adamw::stage_bytes(true, true)));
+        CPMTP_TRY(allow_smem(adamw::adamw8_kernel<CAP, CLOCK>, done, kPer * adamw::stage_bytes(true, true)));
         const int bytes = adamw::stage_bytes(g32, p32);
-        CPMTP_TRY(launch_pdl(adamw::adamw8_kernel<CAP>, dim3(runs), dim3(adamw::kThreads), kPer * bytes, st, tab, bytes));
+        CPMTP_TRY(launch_pdl(adamw::adamw8_kernel<CAP, CLOCK>, dim3(runs), dim3(adamw::kThreads), kPer * bytes, st, tab, bytes));
         return CPMTP_OK;
       });
+}
+
+template <bool CLOCK>
+int adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper& hyper, cpmtp_adamw_clock* clock, cpmtp_stream stream) {
+  DeviceInfo* di = nullptr;
+  const int rd = check_device(&di);
+  if (rd != CPMTP_OK) return rd;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (CLOCK) {
+    ProfScope prof(CPMTP_STAGE_ADAMW, st);
+    CPMTP_TRY(launch_pdl(adamw::adamw_clock_kernel, dim3(1), dim3(1), 0, st, clock, hyper.beta1, hyper.beta2));
+  }
+  if (count <= adamw::kSmallTable) return adamw_step<adamw::kSmallTable, CLOCK>(tensors, count, hyper, clock, di->sms, st);
+  if (count <= adamw::kMiddleTable) return adamw_step<adamw::kMiddleTable, CLOCK>(tensors, count, hyper, clock, di->sms, st);
+  return adamw_step<adamw::kLargeTable, CLOCK>(tensors, count, hyper, clock, di->sms, st);
 }
 
 int grad_blocks(int sms) { return 4 * sms; }
@@ -594,14 +612,17 @@ int cpmtp_norm_backward(const cpmtp_norm_args* args, void* workspace, size_t wor
 int cpmtp_adamw_step(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
                      cpmtp_stream stream) {
   const int rc = check_adamw(tensors, count, hyper);
-  if (rc != CPMTP_OK) return rc;
-  DeviceInfo* di = nullptr;
-  const int rd = check_device(&di);
-  if (rd != CPMTP_OK) return rd;
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (count <= adamw::kSmallTable) return adamw_step<adamw::kSmallTable>(tensors, count, *hyper, di->sms, st);
-  if (count <= adamw::kMiddleTable) return adamw_step<adamw::kMiddleTable>(tensors, count, *hyper, di->sms, st);
-  return adamw_step<adamw::kLargeTable>(tensors, count, *hyper, di->sms, st);
+  return rc != CPMTP_OK ? rc : adamw_step<false>(tensors, count, *hyper, nullptr, stream);
+}
+
+int cpmtp_adamw_step_clocked(const cpmtp_adamw_tensor* tensors, int32_t count, const cpmtp_adamw_hyper* hyper,
+                             cpmtp_adamw_clock* clock, cpmtp_stream stream) {
+  if (hyper == nullptr || clock == nullptr) return CPMTP_ERR_NULL;
+  if (!aligned(clock, 8)) return CPMTP_ERR_ALIGN;
+  cpmtp_adamw_hyper h = *hyper;
+  h.lr = 0.0; h.step = 1; h.seed = 0;              // (the clock's)
+  const int rc = check_adamw(tensors, count, &h);
+  return rc != CPMTP_OK ? rc : adamw_step<true>(tensors, count, h, clock, stream);
 }
 
 int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, int32_t second, void* out_bf16,

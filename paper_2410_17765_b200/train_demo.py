@@ -12,6 +12,7 @@ from __future__ import annotations
 import argparse
 import math
 from dataclasses import dataclass
+from typing import Optional
 
 import torch
 
@@ -45,7 +46,8 @@ def walk(cfg: Config, generator: torch.Generator, follow: float = 0.9) -> torch.
 
 
 class Model:
-    """Parameters, their gradients and the step.  Buffers that a step needs are made once, so that a step can be captured."""
+    """Parameters, their gradients and the step.  Buffers that a step needs are made once, so that a step can be captured in a CUDA graph; one
+    that is to be replayed as the next steps takes its number and rate from a binding.StepClock."""
 
     names = ("E", "w_in", "W_block", "w_post", "w_pre", "W_head", "W_g")
 
@@ -107,13 +109,13 @@ class Model:
                                dev_status=self.status)
         return g
 
-    def step(self, tokens: torch.Tensor, t: int, *, lr: float, max_norm: float = 1.0) -> dict:
-        """One optimiser step (the t-th, from 1): {"loss", "norm"} on the device."""
+    def step(self, tokens: torch.Tensor, t, *, lr: Optional[float] = None, max_norm: float = 1.0) -> dict:
+        """One optimiser step (the t-th, from 1, or a StepClock's next): {"loss", "norm"} on the device."""
         f = self.forward(tokens)
         g = self.backward(f)
         grads = [g[k] for k in self.names]
         clip = binding.grad_norm(grads, max_norm=max_norm, workspace=self.ws_clip)
-        self.optimizer.step(grads, t, lr=lr, coef=clip["coef"], seed=t)
+        self.optimizer.step(grads, t, lr=lr, coef=clip["coef"], seed=0 if isinstance(t, binding.StepClock) else t)
         return dict(loss=f["loss"], norm=clip["norm"])
 
 

@@ -243,3 +243,30 @@ def test_one_missing_gradient_costs_no_more_than_its_place():
         return min(times)
 
     assert best(holed) < 3 * best(full)
+
+
+def test_the_clocks_layout_and_checks():
+    import os
+    import re
+
+    from paper_2410_17765_b200 import build
+
+    build.build()
+    lib = binding.load_library()
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "cpmtp.h")).read()
+    body = re.search(r"typedef struct cpmtp_adamw_clock \{(.*?)\}", header, re.S).group(1)
+    body = re.sub(r"/\*.*?\*/", "", body, flags=re.S)
+    assert [d.split()[-1] for d in body.split(";") if d.strip()] == [f[0] for f in binding.CAdamWClock._fields_]
+    clock = binding.StepClock(0.25, step=41, seed=-1, device="cpu")
+    assert int(clock.step) == 41 and float(clock.lr) == 0.25 and clock.block.numel() == ctypes.sizeof(binding.CAdamWClock) == 40
+    clock.lr.fill_(0.5)
+    assert binding.CAdamWClock.from_buffer_copy(bytes(clock.block.tolist())).lr == 0.5
+    assert binding.CAdamWClock.from_buffer_copy(bytes(clock.block.tolist())).seed == 0xFFFFFFFF
+    hyper = binding.CAdamWHyper(0.1, 0.9, 0.95, 1e-8, 0.1, 1, 0, 32, None)
+    at = ctypes.c_void_p(4096)
+    assert lib.cpmtp_adamw_step_clocked(None, 0, ctypes.byref(hyper), None, None) == -1
+    assert lib.cpmtp_adamw_step_clocked(None, 0, None, at, None) == -1
+    assert lib.cpmtp_adamw_step_clocked(None, 0, ctypes.byref(hyper), ctypes.c_void_p(4100), None) == -3
+    assert lib.cpmtp_adamw_step_clocked(None, 1, ctypes.byref(hyper), at, None) == -1
+    hyper.beta1 = 1.0
+    assert lib.cpmtp_adamw_step_clocked(None, 0, ctypes.byref(hyper), at, None) == -2
