@@ -56,8 +56,14 @@ struct EmbedLayout {
   size_t hist, keys, head, tail, total;
 };
 
-// Short chunks of the sums: up to this many tokens, if long ones make fewer warps than eight on each of 148 SMs.
-constexpr long long kShortTokens = 2048, kWarpsWanted = 8 * 148;
+// The current device's number of SMs; without a device that of the one this is written for.
+int sm_count() {
+  const DeviceInfo* di = device_info();
+  return di != nullptr && di->sms > 0 ? di->sms : 148;
+}
+
+// Short chunks of the sums: up to this many tokens, if long ones make fewer warps than this on each SM.
+constexpr long long kShortTokens = 2048, kWarpsWanted = 8;
 
 EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   EmbedLayout L;
@@ -67,7 +73,7 @@ EmbedLayout embed_layout(const cpmtp_embed_shape& s) {
   L.bits = (width + L.passes - 1) / L.passes;
   L.blocks = (s.T + embed::kSortKeys - 1) / embed::kSortKeys;
   L.slabs = (s.d + embed::kSlab - 1) / embed::kSlab;
-  L.chunk = s.T <= kShortTokens && static_cast<long long>(s.T) * L.slabs < kWarpsWanted * embed::kChunk ? embed::kShortChunk : embed::kChunk;
+  L.chunk = s.T <= kShortTokens && static_cast<long long>(s.T) * L.slabs < kWarpsWanted * sm_count() * embed::kChunk ? embed::kShortChunk : embed::kChunk;
   L.chunks = (s.T + L.chunk - 1) / L.chunk;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
@@ -548,8 +554,7 @@ int cpmtp_norm_forward(const cpmtp_norm_args* args, cpmtp_stream stream) {
 
 size_t cpmtp_norm_workspace_bytes(const cpmtp_norm_args* args) {
   if (check_norm(args) != CPMTP_OK) return 0;
-  DeviceInfo* di = device_info();
-  const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
+  const int sms = sm_count();
   const int blocks[2] = {norm_bwd_blocks(*args, norm_layout(args->d, true), sms), norm_bwd_blocks(*args, norm_layout(args->d, false), sms)};
   return align_up(2 * sizeof(float) * static_cast<size_t>(blocks[0] > blocks[1] ? blocks[0] : blocks[1]) * args->d + kAlign);
 }
@@ -648,8 +653,7 @@ int cpmtp_adamw_state_values(const void* codes, const uint8_t* exps, int64_t n, 
 
 size_t cpmtp_grad_norm_workspace_bytes(const cpmtp_adamw_tensor* tensors, int32_t count) {
   if (check_grads(tensors, count) != CPMTP_OK) return 0;
-  DeviceInfo* di = device_info();
-  const int sms = di != nullptr && di->sms > 0 ? di->sms : 148;
+  const int sms = sm_count();
   const size_t launches = (count + adamw::kLargeTable - 1) / adamw::kLargeTable + 1;
   return align_up(launches * grad_blocks(sms) * sizeof(double));
 }
