@@ -387,8 +387,9 @@ int cpmtp_forward_host(const cpmtp_shape* shape, const void* h_host, const void*
  *
  * All of them: sizes of zero are allowed and enqueue nothing (outputs that are sums over nothing are
  * written as zeros); any row width and row stride is accepted, widths, strides and addresses that
- * allow 16-byte accesses run faster; sums are held in fp32 in a fixed order without floating-point atomics, so results are
- * bit-reproducible; every output is rounded once.
+ * allow 16-byte accesses run faster; sums are held in fp32 in a fixed order without floating-point atomics, so results
+ * are bit-reproducible; every output is rounded once.  The norms read rows that do not start on a 16-byte boundary from
+ * the boundary before on: up to 14 bytes before a matrix, in the 16 that its first element lies in, are read and not used.
  */
 
 /* element types */

@@ -153,8 +153,8 @@ NormLayout norm_layout(int d, bool vec) {
 
 // Rows kept in shared memory per row group, the current one included: as many as 227 KB hold for one block of the
 // backward kernel per SM, or half of that for two of the forward kernel.
-template <class S, int MAXT>
-constexpr int fwd_stages() { return MAXT > 512 ? (sizeof(S) == 4 ? 3 : 4) : (sizeof(S) == 4 ? 3 : 4); }
+template <class S>
+constexpr int fwd_stages() { return sizeof(S) == 4 ? 3 : 4; }
 template <class S, int MAXT>
 constexpr int bwd_stages() { return MAXT > 512 ? 2 : (sizeof(S) == 4 ? 3 : 5); }
 
@@ -220,7 +220,7 @@ bool rows_vec(const cpmtp_rows& r, int d) { return d % 8 == 0 && (r.data == null
 
 template <class S, bool VEC, int MAXT, bool ONE, bool ALL>
 cudaError_t launch_norm_fwd_as(const norm::Params<S>& p, const NormLayout& L, int blocks, cudaStream_t st) {
-  constexpr int kStages = fwd_stages<S, MAXT>();
+  constexpr int kStages = fwd_stages<S>();
   static bool done[64] = {};
   auto* kernel = norm::norm_fwd_kernel<S, VEC, MAXT, kStages, ONE, ALL>;
   const cudaError_t e = allow_smem(kernel, done, kStages * kMaxGroups<ONE> * norm::fwd_stage_bytes<S>(MAXT / kMaxGroups<ONE>));
