@@ -445,9 +445,14 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
 
   // Row r, the it-th of this group: what comes before its sums, into `row`, and the sums as far as this warp goes.
   // Gates are held as e = exp(-logit), from which g and 1 - g are made where they are used (holding both: 123 us against 96 at
-  // 8192 x 4096).  Where registers are short not even that: the logits are read from the ring again (16384 x 2047: 145 us
-  // against 156; 4096 x 8192, 64 registers: 127 against 146).
-  constexpr bool PIPE = ONE && MAXT <= 512, KEEP_E = ALL ? MAXT <= 512 : !ONE;
+  // 8192 x 4096).  Where registers are short not even that, the logits are read from the ring again: two ragged rows at a time
+  // (16384 x 2047: 145 us against 156), 64 registers (4096 x 8192: 127 against 146); elsewhere e is better kept (8192 x 4096: 99 against 106).
+  constexpr bool KEEP_E = MAXT <= 512 && (VEC || !ONE);
+  // A row is finished while the warps' sums of the next one are on their way: two rows are held at a time, which 128 registers
+  // allow where rows' addresses are common to the block.  It pays where a row is short of other work to wait with, bf16 with
+  // everything there (8192 x 4096: 94 us against 96) and ragged rows (16384 x 2047, 1023: 144 and 60 us against 147 and 63); it does not
+  // with fewer arrays or an fp32 stream (8192 x 4096: row gates 89 us against 82, fp32 129 against 125).
+  constexpr bool PIPE = ONE && MAXT <= 512 && (!VEC || (ALL && sizeof(S) == 2));
   struct Row {
     f32x2 x[4], a[4], b[4], e[CHANNEL && KEEP_E ? 4 : 1];
     float rx, rb, erow;
@@ -539,8 +544,6 @@ __global__ void __launch_bounds__(MAXT) norm_bwd_kernel(const __grid_constant__ 
   };
   float sum[3];
   if (PIPE) {
-    // A row is finished while the warps' sums of the next one are on their way: two rows are held at a time, which 128
-    // registers allow where rows' addresses are common to the block (8192 x 4096: 110 -> 103 us).
     if (i < N) {
       Row row;
       end_sum3<ONE>(sum, before_sums(i, 0, row), red[0][at.rg], p.W, at.group, at.lane);
