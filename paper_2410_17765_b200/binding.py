@@ -728,6 +728,7 @@ def embed_backward(dy: torch.Tensor, x: torch.Tensor, V: int, *, scale: float = 
     """cpmtp_embed_backward: dE [V, d] bf16, the scaled sums of the rows of dy (x.shape + (d,), bf16 or fp32; a 2-D dy may
     have strided rows) over equal tokens.  accumulate: add to `out`, touching only the rows that occur."""
     dev = _device(dy)
+    _need(dy.dim() > 0, "dy must be x.shape + (d,)")
     T, d = x.numel(), dy.shape[-1]
     px = _int32(x, dev, "x")
     dtype = dy.dtype
@@ -1129,7 +1130,8 @@ class AdamW:
         """Step t (1 for the first) with one gradient per parameter (bf16 or fp32, contiguous; None leaves a parameter alone).
         coef: fp32 [1] on the device that multiplies the gradients (grad_norm's), or None.
         t may be a StepClock, which has the learning rate and the seed as well.  A step that is captured for replaying needs one: with a
-        number, each replay would be that step again, with the same bias corrections and rounding noise."""
+        number, each replay would be that step again, with the same bias corrections and rounding noise.  (What a graph has captured goes
+        on writing to the memory that the parameters had then.)"""
         n = len(self.params)
         _need(len(grads) == n, "one gradient per parameter")
         if n == 0:

@@ -3,7 +3,7 @@
 // The tensors' descriptors travel in the kernel's parameters (up to 32 KB), so a step is one launch with no copy to
 // the device, and can be captured; to be replayed as the steps that follow it takes what changes from step to step from a
 // clock in device memory, which a second, tiny launch advances.  Bound by bandwidth with fp32 states (133 M parameters with an
-// fp32 copy, 28 bytes each: 561 us, 6.6 TB/s), by instruction issue with 8-bit ones (10 bytes each: 286 us).  Every block takes one run
+// fp32 copy, 28 bytes each: 561 us, 6.6 TB/s), by instruction issue with 8-bit ones (10 bytes each: 290 us).  Every block takes one run
 // of elements of one tensor; a warp takes 256 elements at a time, which are also what shares an exponent in an 8-bit state.
 #pragma once
 #include "vec_io.cuh"
@@ -294,7 +294,7 @@ __device__ __forceinline__ float unit_of(int e) { return __uint_as_float(static_
 __device__ __forceinline__ float inverse_unit_of(int e) { return __uint_as_float(static_cast<uint32_t>(142 - e) << 23); }
 
 // Root and reciprocal; FLUSH: single instructions, which take subnormal numbers for zeros (668 M bf16 parameters: the
-// question which of the two a block takes costs 0.5 %; without the flush the root of a subnormal moment stays beside a small eps).
+// question which of the two a block takes costs 0.7 %; without the flush the root of a subnormal moment stays beside a small eps).
 template <bool FLUSH>
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;

@@ -4,8 +4,8 @@
 // block holds G rows at a time (W G <= 16, or G = 1).  Blocks are persistent.  Both directions move
 // 10 to 20 bytes per element and compute some tens of operations on them, so what counts is that every SM always has tens of
 // kilobytes of reads under way: rows ahead are fetched with cp.async into a ring of rows in shared memory while the
-// current row goes through its reductions.  8192 x 4096, bf16, a gate per channel: forward 58 us (5.8 TB/s), backward 104 us
-// (5.2 TB/s); a plain copy on this card reaches 6.5 TB/s.
+// current row goes through its reductions.  8192 x 4096, bf16, a gate per channel: forward 59 us (5.7 TB/s), backward 99 us
+// with the sums of the weights' gradients (5.4 TB/s); a plain copy on this card reaches 6.5 TB/s.
 #pragma once
 #include <type_traits>
 
@@ -173,9 +173,9 @@ __device__ __forceinline__ void end_sum3(float (&v)[3], float c, float (*red)[kM
 // these that are copied (the last one only as far as the row goes), so that rows of any width and stride move in whole
 // 16-byte accesses; zeros follow up to column 256 W, so that what is read needs no bounds.  VEC (rows start on a piece and
 // d % 8 == 0): a thread copies exactly what it will use itself, and no barrier is spent on the copy; what is read and written in
-// shared and global memory then are eight columns at a time (8192 x 4096: forward 58 us against 86, backward 105 against 153).
-// ALL: besides, d = 256 W and every input and output is there, which takes the questions out of the loop (57 us against 63,
-// 103 against 121).
+// shared and global memory then are eight columns at a time (8192 x 4096: forward 59 us against 83, backward 95 against 145).
+// ALL: besides, d = 256 W and every input and output is there, which takes the questions out of the loop (4096 x 8192:
+// forward 59 us against 62, backward 127 against 147; 8192 x 2048: 31 against 32, 52 against 55; 8192 x 4096: 59 against 58, 95 against 99).
 template <class T>
 __host__ __device__ constexpr int region_bytes(int threads) { return (threads * static_cast<int>(sizeof(T)) / 2 + 1) * 16; }
 

@@ -139,8 +139,8 @@ struct NormLayout {
 };
 
 // `vec`: the rows allow accesses of eight columns.  Blocks of several rows are better for those (8192 x 2048: backward 52 us
-// against 58 for blocks of one row), blocks of one row for others, whose addresses take more operations and are then common to
-// a block (8192 x 2047: 80 us against 88) -- where one row is wide enough to leave few blocks: their sums are added up afterwards.
+// against 57 for blocks of one row), blocks of one row for others, whose addresses take more operations and are then common to
+// a block (8192 x 2047: 77 us against 80; 16384 x 1023 in fp32 with row gates: 60 against 66) -- where one row is wide enough to leave few blocks: their sums are added up afterwards.
 NormLayout norm_layout(int d, bool vec) {
   NormLayout L;
   L.W = (d + 255) / 256;
