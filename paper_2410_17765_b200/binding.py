@@ -1023,12 +1023,23 @@ def _state_column(name: str):
         return tuple(None if t is None else t.detach() for t in self._states[name])
 
     def write(self, tensors) -> None:
-        _need(all(t is None or isinstance(t, torch.Tensor) for t in tensors), f"{name} takes a list of tensors")
-        # Aliases, too: another tensor given to the caller's variables changes nothing here, and the memory stays theirs and ours
-        self._states[name] = [None if t is None else t.detach() for t in tensors]
+        # Aliases, too: other memory given to the caller's tensors changes nothing here, and this memory stays
+        try:
+            self._states[name] = [None if t is None else t.detach() for t in tensors]
+        except AttributeError:
+            raise CpmtpError(f"cpmtp: {name} takes a list of tensors") from None
         self._at = None                    # the descriptors are out of date
 
     return property(read, write)
+
+
+def _same_kind(tensors, dtype, sizes: list, dev: int) -> bool:
+    """Whether these are contiguous tensors of one type, of the given sizes, on the device."""
+    try:
+        return (list(map(_size_of, tensors)) == sizes and {dtype} >= set(map(_dtype_of, tensors)) and {dev} >= set(map(_device_of, tensors))
+                and all(map(_contiguous, tensors)))
+    except TypeError:                      # (None among them)
+        return False
 
 
 class StepClock:
@@ -1054,7 +1065,7 @@ class AdamW:
     The list `params` and its tensors' memory may change between steps (`p.data = other`): every step compares their addresses
     and sizes with those it knows, and on a difference checks all tensors again as at first.  Memory that was replaced is held until
     then.  The states `m`, `v`, `m_exp`, `v_exp` and `master` are the memory that was given or made at first: read as tuples of
-    aliases, written in place, or replaced by assigning a whole list (`opt.m = tensors`)."""
+    aliases, written in place, or replaced by assigning a whole list (`opt.m = tensors`); their storages are not to be resized."""
 
     m, v, m_exp, v_exp, master = map(_state_column, ("m", "v", "m_exp", "v_exp", "master"))
 
@@ -1085,9 +1096,8 @@ class AdamW:
     def _check_params(self) -> int:
         """Index of the parameters' device."""
         dev = _device(self.params[0]) if self.params else -1
-        for p in self.params:
-            if p.dtype not in _TYPES or not p.is_contiguous() or p.get_device() != dev:
-                raise CpmtpError("cpmtp: parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
+        if not (_TYPES.keys() >= set(map(_dtype_of, self.params)) and all(map(_contiguous, self.params)) and {dev} >= set(map(_device_of, self.params))):
+            raise CpmtpError("cpmtp: parameters must be contiguous bfloat16 or float32 tensors on one CUDA device")
         return dev
 
     def _expected(self) -> dict:
@@ -1104,26 +1114,27 @@ class AdamW:
         dev, n, states = self._check_params(), len(self.params), self._states
         _need(len(self._factors) == n, "the number of parameters has changed")
         _need(len(states["master"]) == n, "master needs one entry per parameter")
-        for w, p in zip(states["master"], self.params):
-            if w is not None and (p.dtype != torch.bfloat16 or w.dtype != torch.float32 or not w.is_contiguous() or w.numel() != p.numel()
-                                  or w.get_device() != dev):
-                raise CpmtpError("cpmtp: a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
+        held = [p.detach() for p in self.params]
+        masters = [(w, p) for w, p in zip(states["master"], held) if w is not None]
+        if not (_same_kind([w for w, _ in masters], torch.float32, [p.numel() for _, p in masters], dev)
+                and all(p.dtype is torch.bfloat16 for _, p in masters)):
+            raise CpmtpError("cpmtp: a master copy is a contiguous float32 tensor of a bfloat16 parameter's size")
+        written = held + [w for w, _ in masters]
         for name, (dtype, sizes) in self._expected().items():
-            _need(len(states[name]) == n, f"{name} needs one entry per parameter")
-            for t, k in zip(states[name], sizes):
-                if t is None or t.dtype != dtype or not t.is_contiguous() or t.numel() != k or t.get_device() != dev:
-                    raise CpmtpError(f"cpmtp: {name} must be contiguous {dtype} tensors of {k} elements here")
-        written = [t for t in [*self.params, *(t for column in states.values() for t in column)] if t is not None and t.numel() > 0]
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in written)
+            if len(states[name]) != n or not _same_kind(states[name], dtype, sizes, dev):
+                raise CpmtpError(f"cpmtp: {name} must be a contiguous {dtype} tensor per parameter, of its size"
+                                 + (f" in blocks of {ADAMW_BLOCK}" if name.endswith("exp") else ""))
+            written += states[name]
+        at = list(map(_address_of, written))
+        spans = sorted((a, a + t.nbytes) for a, t in zip(at, written) if t.nbytes > 0)
         _need(all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "a tensor that a step writes is there twice, or overlaps another")
         table = _Descriptors(n)
-        held = [p.detach() for p in self.params]
         for word, tensors in ((0, held), (2, states["master"]), (3, states["m"]), (4, states["v"]), (5, states["m_exp"]), (6, states["v_exp"])):
             table.put(word, [0 if t is None else t.data_ptr() for t in tensors])
-        self._numels, self._types = [p.numel() for p in held], [_TYPES[p.dtype] for p in held]
+        self._numels, self._types = list(map(_size_of, held)), [_TYPES[k] for k in map(_dtype_of, held)]
         table.put(7, self._numels)
         table.put(9, self._factors)
-        self._table, self._held, self._at = table, held, [p.data_ptr() for p in held]
+        self._table, self._held, self._at = table, held, at[:n]
 
     def step(self, grads, t, *, lr: Optional[float] = None, betas: tuple = (0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
              coef: Optional[torch.Tensor] = None, seed: int = 0) -> None:
