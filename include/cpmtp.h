@@ -563,6 +563,136 @@ size_t cpmtp_grad_norm_workspace_bytes(const cpmtp_adamw_tensor* tensors, int32_
 int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_norm, float* norm, float* coef,
                     void* workspace, size_t workspace_bytes, cpmtp_stream stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The base model's pass over a draft: attention of its few new tokens over a paged cache of keys and values, and the step from
+ * logits to tokens and log-probabilities that cpmtp_verify_draft decides by.  The paper has no counterpart for these entry points; it
+ * measures its drafts against a base model that has them.
+ *
+ * All of them: batches of zero are allowed and enqueue nothing; statistics and sums are held in fp32 or more, in a fixed order without
+ * floating-point atomics; every output is rounded once.  What stands in device memory (lengths, tables, settings of rows) is not checked on
+ * the host: a length or page number out of range is clamped or left out, as documented, raises dev_status to 1, and never leads out of bounds.
+ */
+
+/* Widest head. */
+#define CPMTP_CACHE_MAX_D 128
+
+/*
+ * Keys and values of many sequences, in pages of `page_slots` tokens.  Element (page, slot, head, i) of the keys is
+ * k[page * k_page + slot * k_slot + head * k_head + i]; so both orders, heads within slots and slots within heads, are served.
+ * All distances are in elements; those of k and v and both addresses have to be multiples of 16 bytes.
+ * `acc`, where it is not NULL, holds the attention weight that a slot has received, for each head: acc[page * acc_page + head * acc_head + slot].
+ */
+typedef struct cpmtp_cache {
+  void *k, *v;                      /* bf16 */
+  float* acc;
+  int32_t pages;
+  int32_t page_slots;               /* a multiple of 8, <= 65536 */
+  int32_t H, D;                     /* heads; their width, a multiple of 8, <= CPMTP_CACHE_MAX_D */
+  int64_t k_page, k_slot, k_head, v_page, v_slot, v_head, acc_page, acc_head;
+} cpmtp_cache;
+
+/*
+ * The sequences of a batch.  Slot s of sequence b is slot s % page_slots of page table[b * ld_table + s / page_slots].
+ * `lens` counts the new tokens of this call, which are the last ones: token j of q sits in slot lens[b] - q + j.
+ * No page that a call writes to may be named twice.
+ */
+typedef struct cpmtp_cache_seqs {
+  const int32_t* table;
+  const int32_t* lens;              /* [B] slots in use, 0 .. width * page_slots */
+  const int32_t* q_lens;            /* [B] new tokens, 0 .. Q; NULL: Q of every sequence */
+  int64_t ld_table;
+  int32_t B, width, Q;              /* sequences; pages in a row of the table; new tokens at most */
+  int32_t unused;
+} cpmtp_cache_seqs;
+
+/* Tokens of a batch by heads: element (b, j, h, i) is data[b * seq + j * token + h * head + i].  Any alignment of elements. */
+typedef struct cpmtp_tokens {
+  void* data;
+  int64_t seq, token, head;
+} cpmtp_tokens;
+
+/*
+ * Puts the keys and values [B, Q, H, D] bf16 of the new tokens into their slots; acc of these slots (of every head) becomes 0.
+ * Rows j >= q_lens[b] are not read.  Slots out of range are left out and raise dev_status to 1.
+ */
+int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_tokens* k, const cpmtp_tokens* v,
+                       int32_t* dev_status, cpmtp_stream stream);
+
+typedef struct cpmtp_attend_args {
+  cpmtp_tokens q, out;              /* [B, Q, Hq, D] bf16 */
+  float* lse;                       /* [B, Q, Hq] or NULL */
+  int32_t Hq;                       /* a multiple of H: query head h looks at head h / (Hq / H) of the cache */
+  float scale;                      /* of the products; finite */
+} cpmtp_attend_args;
+
+/*
+ * Attention of the new tokens over the cache, which holds their own keys and values already:
+ *   s_i = scale * <q[b, j, h], k_i>  for the slots i < lens[b] - (q_lens[b] - 1 - j),
+ *   p = softmax(s),  out[b, j, h] = sum_i p_i v_i,  lse[b, j, h] = log sum_i exp(s_i).
+ * A token that sees no slot gets a row of zeros and lse -infinity.  Rows j >= q_lens[b] of out and lse are left as they were.
+ * With cache->acc, acc of slot i and head g += the sum of p_i over the new tokens and the query heads that look at g.
+ * A page number out of range stands for keys and values of zero.  Workspace: cpmtp_cache_attend_workspace_bytes, which looks at
+ * numbers alone (and at whether cache->acc is NULL).
+ */
+size_t cpmtp_cache_attend_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t Hq);
+int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_attend_args* args, void* workspace,
+                       size_t workspace_bytes, int32_t* dev_status, cpmtp_stream stream);
+
+typedef struct cpmtp_evict_args {
+  const int32_t* table_out;         /* pages that take the kept slots: slot j of sequence b is in page table_out[b * ld_table_out + j / page_slots] */
+  int64_t ld_table_out;             /* >= ceil(budget / page_slots) */
+  int32_t budget, recent;           /* 0 <= recent <= budget, budget >= 1 */
+  int32_t* lens_out;                /* [B], not lens: the new lengths, min(lens, budget) */
+  int32_t* kept;                    /* [B, H, budget]: the slots that were kept, -1 behind the last; or NULL */
+} cpmtp_evict_args;
+
+/*
+ * Cuts sequences down to `budget` slots for each head: the `recent` last slots stay, and of the others those with the largest acc (NaN
+ * counts as the least; of equals the lowest slots).  The kept slots' keys, values and acc go, in their order, to other pages, which must not be
+ * among those that the table names; a sequence that is short enough goes there whole.  Slots and pages out of range are left out.
+ * seqs->Q and q_lens are not used.  Workspace: cpmtp_cache_evict_workspace_bytes.
+ */
+size_t cpmtp_cache_evict_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t budget);
+int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_evict_args* args, void* workspace,
+                      size_t workspace_bytes, int32_t* dev_status, cpmtp_stream stream);
+
+/* Largest vocabulary of cpmtp_sample_logits. */
+#define CPMTP_SAMPLE_MAX_V (1 << 24)
+
+typedef struct cpmtp_sample_args {
+  const void* logits;               /* [N, V] of `type`, rows ld elements apart */
+  int64_t ld;
+  int32_t N, V;
+  int32_t type;                     /* CPMTP_BF16 or CPMTP_F32 */
+  int32_t top_k;                    /* settings of all rows ... */
+  float temperature, top_p, min_p;
+  int32_t unused;
+  const float* temperatures;        /* ... or of each, [N]; NULL: the number above */
+  const int32_t* top_ks;
+  const float *top_ps, *min_ps;
+  const float* uniform;             /* [N] in [0, 1) */
+  const int32_t* given;             /* [N] tokens to be scored, or NULL */
+  int32_t* tokens;                  /* [N] */
+  float* logp;                      /* [N] or NULL: log-probability of the drawn token */
+  float* logp_given;                /* [N]: of the given one; written if `given` is there */
+  int32_t* kept;                    /* [N] or NULL: entries that the filters left */
+} cpmtp_sample_args;
+
+/*
+ * A token from each row of logits, and log-probabilities of the distribution that it was drawn from.  In a row, with x a logit and m the
+ * largest, w = exp((x - m) / temperature), entries in the order of falling x and, among equals, of rising index:
+ *   top_k > 0: the first top_k entries;   top_p < 1: of these the shortest prefix that holds top_p of their mass, one entry at least;
+ *   min_p > 0: of these the entries with w >= min_p, and the first one.
+ * The token is the first entry, by index, at which the running sum of the kept w exceeds uniform * (their sum).
+ * temperature 0: the first entry, with log-probability 0.  Logits of -infinity and NaN are never kept; a row of nothing else gives token -1
+ * and log-probability -infinity; logits of +infinity share the whole mass.  A given token that was not kept, or CPMTP_EMBED_PAD, has
+ * log-probability -infinity; any other outside [0, V) does too and raises dev_status to 1.
+ * Weights are summed as 62-bit integers: the sums are exact and in no order; borders are decided in 64 bits (a weight's own relative error is below 2^-32).
+ * In rows' own settings a temperature that is not above 0 counts as 0, a top_p that is not below 1 as 1, a min_p that is not above 0 as 0; a uniform below 0 draws
+ * as 0, one not below 1 the last entry that has weight.  No workspace is needed.
+ */
+int cpmtp_sample_logits(const cpmtp_sample_args* args, int32_t* dev_status, cpmtp_stream stream);
+
 /*
  * Per-stage device timing, for benchmarks.  Between cpmtp_profile_begin() and
  * cpmtp_profile_end() every kernel launch of the entry points above is bracketed
@@ -597,6 +727,10 @@ enum {
   CPMTP_STAGE_NORM_GRAD,     /* their gradient */
   CPMTP_STAGE_GRAD_NORM,     /* norm of all gradients */
   CPMTP_STAGE_ADAMW,         /* optimiser step */
+  CPMTP_STAGE_CACHE_APPEND,  /* keys and values into the cache */
+  CPMTP_STAGE_CACHE_ATTEND,  /* attention over the cache */
+  CPMTP_STAGE_CACHE_EVICT,   /* eviction from the cache */
+  CPMTP_STAGE_SAMPLE,        /* tokens from logits */
   CPMTP_STAGE_COUNT
 };
 int cpmtp_profile_begin(void);

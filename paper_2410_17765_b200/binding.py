@@ -35,6 +35,8 @@ EXPORTS = [
     "cpmtp_embed_forward", "cpmtp_embed_workspace_bytes", "cpmtp_embed_backward",
     "cpmtp_norm_forward", "cpmtp_norm_workspace_bytes", "cpmtp_norm_backward",
     "cpmtp_adamw_step", "cpmtp_adamw_step_clocked", "cpmtp_adamw_state_values", "cpmtp_grad_norm_workspace_bytes", "cpmtp_grad_norm",
+    "cpmtp_cache_append", "cpmtp_cache_attend_workspace_bytes", "cpmtp_cache_attend", "cpmtp_cache_evict_workspace_bytes",
+    "cpmtp_cache_evict", "cpmtp_sample_logits",
 ]
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -42,10 +44,12 @@ BF16, F32 = 0, 1
 EMBED_PAD = -1
 GATE_NONE, GATE_ROW, GATE_CHANNEL = 0, 1, 2
 ADAMW_BLOCK = 256
+CACHE_MAX_D = 128
+SAMPLE_MAX_V = 1 << 24
 
 STAGES = ["gate", "proj", "lse", "mixture", "finalize", "coeff", "logit_grad", "dz", "de", "de_convert",
           "dw_head", "dh", "dw_g", "draft_step", "teacher_lse", "kl", "embed", "embed_grad", "norm", "norm_grad", "grad_norm",
-          "adamw"]
+          "adamw", "cache_append", "cache_attend", "cache_evict", "sample"]
 
 
 class CShape(ctypes.Structure):
@@ -98,6 +102,37 @@ class CAdamWHyper(ctypes.Structure):
 class CAdamWClock(ctypes.Structure):
     _fields_ = [("step", ctypes.c_int64), ("lr", ctypes.c_double), ("seed", ctypes.c_uint32), ("key", ctypes.c_uint32), ("bc1", ctypes.c_double),
                 ("rsqrt_bc2", ctypes.c_float), ("unused", ctypes.c_float)]
+
+
+class CCache(ctypes.Structure):
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("acc", ctypes.c_void_p), ("pages", ctypes.c_int32),
+                 ("page_slots", ctypes.c_int32), ("H", ctypes.c_int32), ("D", ctypes.c_int32)]
+                + [(n, ctypes.c_int64) for n in ("k_page", "k_slot", "k_head", "v_page", "v_slot", "v_head", "acc_page", "acc_head")])
+
+
+class CCacheSeqs(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("q_lens", ctypes.c_void_p), ("ld_table", ctypes.c_int64),
+                ("B", ctypes.c_int32), ("width", ctypes.c_int32), ("Q", ctypes.c_int32), ("unused", ctypes.c_int32)]
+
+
+class CTokens(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class CAttendArgs(ctypes.Structure):
+    _fields_ = [("q", CTokens), ("out", CTokens), ("lse", ctypes.c_void_p), ("Hq", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class CEvictArgs(ctypes.Structure):
+    _fields_ = [("table_out", ctypes.c_void_p), ("ld_table_out", ctypes.c_int64), ("budget", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("lens_out", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
+
+
+class CSampleArgs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("ld", ctypes.c_int64), ("N", ctypes.c_int32), ("V", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("unused", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in (
+                    "temperatures", "top_ks", "top_ps", "min_ps", "uniform", "given", "tokens", "logp", "logp_given", "kept")]
 
 
 _lib = None
@@ -174,6 +209,19 @@ def load_library() -> ctypes.CDLL:
     lib.cpmtp_grad_norm_workspace_bytes.argtypes = [atp, ctypes.c_int32]
     lib.cpmtp_grad_norm.restype = ctypes.c_int
     lib.cpmtp_grad_norm.argtypes = [atp, ctypes.c_int32, ctypes.c_float, fp, fp, vp, sz, vp]
+    csp, cqp, tkp = ctypes.POINTER(CCache), ctypes.POINTER(CCacheSeqs), ctypes.POINTER(CTokens)
+    lib.cpmtp_cache_append.restype = ctypes.c_int
+    lib.cpmtp_cache_append.argtypes = [csp, cqp, tkp, tkp, i32p, vp]
+    lib.cpmtp_cache_attend_workspace_bytes.restype = sz
+    lib.cpmtp_cache_attend_workspace_bytes.argtypes = [csp, cqp, ctypes.c_int32]
+    lib.cpmtp_cache_attend.restype = ctypes.c_int
+    lib.cpmtp_cache_attend.argtypes = [csp, cqp, ctypes.POINTER(CAttendArgs), vp, sz, i32p, vp]
+    lib.cpmtp_cache_evict_workspace_bytes.restype = sz
+    lib.cpmtp_cache_evict_workspace_bytes.argtypes = [csp, cqp, ctypes.c_int32]
+    lib.cpmtp_cache_evict.restype = ctypes.c_int
+    lib.cpmtp_cache_evict.argtypes = [csp, cqp, ctypes.POINTER(CEvictArgs), vp, sz, i32p, vp]
+    lib.cpmtp_sample_logits.restype = ctypes.c_int
+    lib.cpmtp_sample_logits.argtypes = [ctypes.POINTER(CSampleArgs), i32p, vp]
     lib.cpmtp_reload_knobs.restype = ctypes.c_int
     lib.cpmtp_debug_status.restype = ctypes.c_int
     lib.cpmtp_profile_begin.restype = ctypes.c_int
@@ -1181,3 +1229,218 @@ def adamw_state_values(codes: torch.Tensor, exps: torch.Tensor, *, second: bool,
     if rc:
         _check(rc)
     return out
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# The base model's pass over a draft: paged cache of keys and values, attention over it, sampling from logits.
+
+class PagedCache:
+    """Keys and values of many sequences in pages, as the cache_* functions take them.
+
+    k, v: [pages, page_slots, H, D] bf16 with any strides that keep rows of D contiguous (a cache kept as [pages, H, page_slots, D] is
+    passed as its transpose(1, 2)); acc: [pages, H, page_slots] fp32, the attention weight that each slot has received, or None.
+    The object holds the tensors, so that their memory stays theirs."""
+
+    __slots__ = ("k", "v", "acc", "device", "_dev", "_c", "_plain")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, acc: Optional[torch.Tensor] = None):
+        _need(k.dim() == 4 and k.dtype is torch.bfloat16, "k must be [pages, page_slots, H, D] bfloat16")
+        _need(v.shape == k.shape and v.dtype is torch.bfloat16, "v must have k's shape and type")
+        dev = k.get_device()
+        _need(v.get_device() == dev, "v is on another device")
+        P, S, H, D = k.shape
+        _need(min(P, S, H, D) > 0, "a cache has one page, slot, head and column at least")
+        _need(S % 8 == 0 and S <= 65536, "page_slots must be a multiple of 8, at most 65536")
+        _need(D % 8 == 0 and D <= CACHE_MAX_D, f"D must be a multiple of 8, at most {CACHE_MAX_D}")
+        a = CCache(k.data_ptr(), v.data_ptr(), None, P, S, H, D)
+        for name, t in (("k", k), ("v", v)):
+            _need(t.stride(3) == 1, f"{name}: the elements of a head must be contiguous")
+            for d, part in ((0, "page"), (1, "slot"), (2, "head")):
+                stride = t.stride(d) if t.shape[d] > 1 else D
+                _need(stride % 8 == 0, f"{name}: distances must be multiples of 8 elements")
+                setattr(a, f"{name}_{part}", stride)
+            _need(t.data_ptr() % 16 == 0, f"{name} must start on a 16-byte boundary")
+        self._plain = a
+        self._c = a
+        if acc is not None:
+            _need(acc.shape == (P, H, S) and acc.dtype is torch.float32 and acc.get_device() == dev, f"acc must be {[P, H, S]} float32 on the same device")
+            _need(acc.stride(2) == 1, "acc: the slots of a head must be contiguous")
+            self._c = CCache.from_buffer_copy(a)
+            self._c.acc = acc.data_ptr()
+            self._c.acc_page = acc.stride(0) if P > 1 else H * S
+            self._c.acc_head = acc.stride(1) if H > 1 else S
+        self.k, self.v, self.acc, self.device, self._dev = k, v, acc, k.device, dev
+
+    page_slots = property(lambda self: self._plain.page_slots)
+    heads = property(lambda self: self._plain.H)
+
+
+def _seqs(cache: PagedCache, dev: int, table: torch.Tensor, lens: torch.Tensor, q_lens: Optional[torch.Tensor], B: int, Q: int) -> CCacheSeqs:
+    if cache._dev != dev:
+        raise CpmtpError("cpmtp: the cache is on another device")
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != B or table.dtype is not torch.int32 or table.get_device() != dev or (shape[1] > 1 and table.stride(1) != 1):
+        raise CpmtpError(f"cpmtp: table must be [{B}, pages] int32 with contiguous rows on the same device")
+    ld = table.stride(0) if B > 1 else shape[1]
+    if ld < shape[1]:
+        raise CpmtpError("cpmtp: table: rows must not overlap")
+    return CCacheSeqs(table.data_ptr(), _ints(lens, B, dev, "lens"), None if q_lens is None else _ints(q_lens, B, dev, "q_lens"), ld, B, shape[1], Q, 0)
+
+
+def _ints(t: torch.Tensor, n: int, dev: int, name: str) -> int:
+    if t.shape != (n,) or t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise CpmtpError(f"cpmtp: {name} must be a contiguous [{n}] int32 on the same device")
+    return t.data_ptr()
+
+
+def _tokens(t: torch.Tensor, size: tuple, dev: int, name: str, written: bool = False) -> CTokens:
+    """[B, Q, heads, D] bf16 tokens whose heads are contiguous."""
+    if t.shape != size or t.dtype is not torch.bfloat16 or t.get_device() != dev:
+        raise CpmtpError(f"cpmtp: {name} must be {list(size)} bfloat16 on the same device, not {list(t.shape)} {t.dtype}")
+    seq, token, head, one = t.stride()
+    B, Q, H, D = size
+    if (one != 1 and D > 1) or (H > 1 and head < D) or (Q > 1 and token < D) or (written and B > 1 and seq < D):
+        raise CpmtpError(f"cpmtp: {name}: the elements of a head must be contiguous and heads must not overlap")
+    return CTokens(t.data_ptr(), seq if B > 1 else 0, token if Q > 1 else 0, head if H > 1 else 0)
+
+
+def _status(dev_status: Optional[torch.Tensor], dev: int):
+    return None if dev_status is None else _int32(dev_status, dev, "dev_status")
+
+
+def cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *,
+                 q_lens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> None:
+    """cpmtp_cache_append: the keys and values [B, Q, H, D] bf16 of new tokens into their slots, the last ones of lens [B] int32 (the new
+    tokens included); q_lens [B] int32: how many of the Q rows a sequence has (None: all).  table [B, pages] int32.  acc of the slots becomes 0."""
+    dev = _device(k)
+    _need(k.dim() == 4, "k must be [B, Q, H, D]")
+    B, Q = k.shape[0], k.shape[1]
+    size = (B, Q, cache._plain.H, cache._plain.D)
+    s = _seqs(cache, dev, table, lens, q_lens, B, Q)
+    rc = load_library().cpmtp_cache_append(cache._c, s, _tokens(k, size, dev, "k"), _tokens(v, size, dev, "v"), _status(dev_status, dev), _raw_stream(dev))
+    if rc:
+        _check(rc)
+
+
+def cache_attend_workspace_bytes(cache: PagedCache, B: int, width: int, Q: int, Hq: int) -> int:
+    """Scratch bytes of cache_attend for B sequences whose tables have `width` pages, Q new tokens and Hq query heads."""
+    return int(load_library().cpmtp_cache_attend_workspace_bytes(cache._c, CCacheSeqs(None, None, None, width, B, width, Q, 0), Hq))
+
+
+def cache_attend(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *, q_lens: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, accumulate: bool = True, want_lse: bool = False, out: Optional[dict] = None,
+                 workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> dict:
+    """cpmtp_cache_attend: attention of the new tokens q [B, Q, Hq, D] bf16 over the cache, which holds their own keys and values already
+    (cache_append); token j of q_lens[b] sees lens[b] - (q_lens[b] - 1 - j) slots.  scale: D ** -0.5 if None.  Returns {"out" [B, Q, Hq, D] bf16
+    [, "lse" [B, Q, Hq] fp32]}; rows behind q_lens are zeros, or left as they were in tensors given by `out`.  accumulate: add the
+    weights to cache.acc, if the cache has it."""
+    dev = _device(q)
+    size = q.shape
+    _need(len(size) == 4, "q must be [B, Q, Hq, D]")
+    B, Q, Hq, D = size
+    c = cache._c if accumulate else cache._plain
+    _need(D == c.D and Hq > 0 and Hq % c.H == 0, f"q must be [B, Q, a multiple of {c.H}, {c.D}]")
+    s = _seqs(cache, dev, table, lens, q_lens, B, Q)
+    res = out if out is not None else {}
+    fresh = torch.empty if q_lens is None else torch.zeros
+    if "out" not in res:
+        res["out"] = fresh(size, dtype=torch.bfloat16, device=q.device)
+    if want_lse and "lse" not in res:
+        res["lse"] = fresh((B, Q, Hq), dtype=torch.float32, device=q.device)
+    lse = res.get("lse")
+    if lse is not None and (lse.shape != (B, Q, Hq) or lse.dtype is not torch.float32 or lse.get_device() != dev or not lse.is_contiguous()):
+        raise CpmtpError(f"cpmtp: lse must be a contiguous {[B, Q, Hq]} float32 on the same device")
+    a = CAttendArgs(_tokens(q, size, dev, "q"), _tokens(res["out"], size, dev, "out", True), None if lse is None else lse.data_ptr(), Hq,
+                    D ** -0.5 if scale is None else scale)
+    lib = load_library()
+    if workspace is None:
+        workspace = alloc_workspace(lib.cpmtp_cache_attend_workspace_bytes(c, s, Hq), q.device)
+    pw, nw = _workspace(workspace, dev)
+    rc = lib.cpmtp_cache_attend(c, s, a, pw, nw, _status(dev_status, dev), _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return res
+
+
+def cache_evict(cache: PagedCache, table: torch.Tensor, lens: torch.Tensor, table_out: torch.Tensor, budget: int, *, recent: int = 0,
+                out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> dict:
+    """cpmtp_cache_evict: cut every sequence down to `budget` slots for each head, the `recent` last ones and those of the others with the
+    largest cache.acc, and move them into the pages of table_out [B, ceil(budget / page_slots) or more] int32, which must not be among those of
+    `table`.  Returns {"lens" [B], "kept" [B, H, budget] slots (-1 behind the last)} int32."""
+    dev = _device(lens)
+    _need(cache.acc is not None, "eviction needs a cache with acc")
+    _need(budget >= 1 and 0 <= recent <= budget, "budget must be at least 1, recent between 0 and budget")
+    B, c = lens.numel(), cache._c
+    s = _seqs(cache, dev, table, lens, None, B, 0)
+    pages = -(-budget // c.page_slots)
+    if table_out.dim() != 2 or table_out.shape[0] != B or table_out.shape[1] < pages or table_out.dtype is not torch.int32 or \
+            table_out.get_device() != dev or (table_out.shape[1] > 1 and table_out.stride(1) != 1):
+        raise CpmtpError(f"cpmtp: table_out must be [{B}, {pages} or more] int32 with contiguous rows on the same device")
+    ld = table_out.stride(0) if B > 1 else table_out.shape[1]
+    _need(ld >= pages, "table_out: rows must not overlap")
+    res = out if out is not None else {}
+    if "lens" not in res:
+        res["lens"] = torch.empty_like(lens)
+    if "kept" not in res:
+        res["kept"] = torch.empty((B, c.H, budget), dtype=torch.int32, device=lens.device)
+    kept = res["kept"]
+    if kept.shape != (B, c.H, budget) or kept.dtype is not torch.int32 or kept.get_device() != dev or not kept.is_contiguous():
+        raise CpmtpError(f"cpmtp: kept must be a contiguous {[B, c.H, budget]} int32 on the same device")
+    a = CEvictArgs(table_out.data_ptr(), ld, budget, recent, _ints(res["lens"], B, dev, "out lens"), kept.data_ptr())
+    lib = load_library()
+    if workspace is None:
+        workspace = alloc_workspace(lib.cpmtp_cache_evict_workspace_bytes(c, s, budget), lens.device)
+    pw, nw = _workspace(workspace, dev)
+    rc = lib.cpmtp_cache_evict(c, s, a, pw, nw, _status(dev_status, dev), _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return res
+
+
+_INT_MAX = (1 << 31) - 1
+
+
+def _setting(v, N: int, dtype, dev: int, name: str) -> tuple:
+    """(number for all rows, address of the rows' own numbers)"""
+    if isinstance(v, torch.Tensor):
+        if v.shape != (N,) or v.dtype is not dtype or v.get_device() != dev or not v.is_contiguous():
+            raise CpmtpError(f"cpmtp: {name} must be a number or a contiguous [{N}] {dtype} on the same device")
+        return 0, v.data_ptr()
+    if not v >= 0:
+        raise CpmtpError(f"cpmtp: {name} must not be negative")
+    return min(v, _INT_MAX) if dtype is torch.int32 else v, None
+
+
+def sample_logits(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                  given: Optional[torch.Tensor] = None, want_kept: bool = False, out: Optional[dict] = None,
+                  dev_status: Optional[torch.Tensor] = None) -> dict:
+    """cpmtp_sample_logits: a token from each row of logits [N, V] (bf16 or fp32, rows may be strided) by uniform [N] fp32 in [0, 1).
+    temperature, top_k, top_p, min_p: numbers, or tensors [N] (fp32, int32, fp32, fp32) with a setting for each row; 0, 0, 1 and 0 mean
+    greedy and no filter.  given [N] int32: tokens to be scored, EMBED_PAD for none.  Returns {"tokens" [N] int32, "logp" [N] fp32
+    [, "logp_given" [N] fp32][, "kept" [N] int32]}: log-probabilities under the filtered distribution."""
+    dev = _device(logits)
+    size, dtype = logits.shape, logits.dtype
+    _need(len(size) == 2 and dtype in _TYPES, "logits must be [N, V] bfloat16 or float32")
+    N, V = size
+    pl, ld = _rows(logits, size, dtype, dev, "logits")
+    (t, pt), (k, pk) = _setting(temperature, N, torch.float32, dev, "temperature"), _setting(top_k, N, torch.int32, dev, "top_k")
+    (p, pp), (m, pm) = _setting(top_p, N, torch.float32, dev, "top_p"), _setting(min_p, N, torch.float32, dev, "min_p")
+    res = out if out is not None else {}
+    new = dict(device=logits.device)
+    if "tokens" not in res:
+        res["tokens"] = torch.empty(N, dtype=torch.int32, **new)
+    if "logp" not in res:
+        res["logp"] = torch.empty(N, dtype=torch.float32, **new)
+    if given is not None and "logp_given" not in res:
+        res["logp_given"] = torch.empty(N, dtype=torch.float32, **new)
+    if want_kept and "kept" not in res:
+        res["kept"] = torch.empty(N, dtype=torch.int32, **new)
+    f32 = torch.float32
+    a = CSampleArgs(pl, ld, N, V, _TYPES[dtype], k, t, p, m, 0, pt, pk, pp, pm, _vector(uniform, N, f32, dev, "uniform"),
+                    None if given is None else _ints(given, N, dev, "given"), _ints(res["tokens"], N, dev, "tokens"), _vector(res["logp"], N, f32, dev, "logp"),
+                    None if given is None else _vector(res["logp_given"], N, f32, dev, "logp_given"),
+                    _ints(res["kept"], N, dev, "kept") if "kept" in res else None)
+    rc = load_library().cpmtp_sample_logits(a, _status(dev_status, dev), _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return res

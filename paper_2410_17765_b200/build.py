@@ -10,10 +10,10 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libcpmtp.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libcpmtp_debug.so")   # the same sources with -DCPMTP_DEBUG (index checks)
-SOURCES = ["cpmtp_api.cu", "train_api.cu"]
+SOURCES = ["cpmtp_api.cu", "train_api.cu", "serve_api.cu"]
 HEADERS = ["ptx.cuh", "tmap.cuh", "tc_gemm.cuh", "epilogues.cuh", "small_kernels.cuh", "sampler_kernels.cuh",
            "distill_epilogues.cuh", "distill_kernels.cuh", "host_util.cuh", "vec_io.cuh", "embed_kernels.cuh", "norm_kernels.cuh",
-           "adamw_kernels.cuh"]
+           "adamw_kernels.cuh", "cache_kernels.cuh", "attend_kernels.cuh", "sample_kernels.cuh"]
 
 
 def _nvcc() -> str:
