@@ -444,8 +444,9 @@ cudaError_t launch_gemm(const void* A, uint64_t a_rows, uint64_t a_ld, const voi
   Sched sched = sched_in;
   // every wait inside the kernel gives up after this long (default 4 s; the knob exists so that a test can
   // watch the give-up path finish in milliseconds)
-  sched.wait_limit_us = knobs().wait_limit_us > 0 ? static_cast<unsigned>(knobs().wait_limit_us) : 4000000u;
-  sched.test_skip_load = static_cast<int>(knobs().test_skip_load);
+  const WaitKnobs wait = wait_knobs();
+  sched.wait_limit_us = wait.limit_us;
+  sched.test_skip_load = wait.skip_load;
   const int grid = sched.units < sms ? sched.units : sms;
   return launch_pdl(tc_gemm_kernel<Cfg, Epi>, dim3(grid), dim3(Cfg::THREADS), smem, stream, tA, tB, sched, ep,
                     dev_status);
@@ -590,6 +591,12 @@ int check_saved(const cpmtp_saved* sv, bool need_z = true) {
 }
 
 }  // namespace
+
+WaitKnobs wait_knobs() {
+  const Knobs& k = knobs();
+  return WaitKnobs{k.wait_limit_us > 0 ? static_cast<unsigned>(k.wait_limit_us) : 4000000u, static_cast<int>(k.test_skip_load)};
+}
+
 }  // namespace cpmtp
 
 // Scratch of cpmtp_score_draft_static: lives in the library image, one copy per GPU.
@@ -769,7 +776,7 @@ static int backward_impl(const cpmtp_shape* shape, const void* h, const void* W_
 
 extern "C" {
 
-int cpmtp_version(void) { return 140; }   // 1.4: optimiser steps by a clock on the device
+int cpmtp_version(void) { return 150; }   // 1.5: paged cache, sampling from logits
 
 int cpmtp_reload_knobs(void) {
   knobs();   // make sure the one-time read has happened, then read again

@@ -42,6 +42,13 @@ inline DeviceInfo* device_info() {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// How long a wait inside a kernel may last, and the test hook that leaves out a load: of the environment knobs.
+struct WaitKnobs {
+  unsigned limit_us;
+  int skip_load;
+};
+WaitKnobs wait_knobs();
+
 // Optional per-stage timing: events bracket each launch while profiling is on.
 struct Profiler {
   bool on = false;
@@ -66,6 +73,33 @@ struct ProfScope {
     if (active) cudaEventRecord(g_prof.events.back(), st);
   }
 };
+
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+template <class K>
+cudaError_t allow_smem(K* kernel, bool (&done)[64], int bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_cache_mutex);
+  if (done[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+
+// The device that the caller has made current, if this library runs on it.
+inline int check_device(DeviceInfo** out) {
+  DeviceInfo* di = device_info();
+  if (di == nullptr) return CPMTP_ERR_LAUNCH;
+  if (di->cc_major != 10) return CPMTP_ERR_ARCH;
+  *out = di;
+  return CPMTP_OK;
+}
+
+// The current device's number of SMs; without a device that of the one this is written for.
+inline int sm_count() {
+  const DeviceInfo* di = device_info();
+  return di != nullptr && di->sms > 0 ? di->sms : 148;
+}
 
 // Launch with programmatic stream serialization: the kernel may be scheduled while the one before it in
 // the stream drains; it calls ptx::grid_dep_wait() before it touches anything that kernel produced.

@@ -11,19 +11,12 @@
 #include "cache_kernels.cuh"
 #include "host_util.cuh"
 #include "sample_kernels.cuh"
+#include "tmap.cuh"
 
 namespace cpmtp {
 namespace {
 
 using io::bf16_t;
-
-int check_device(DeviceInfo** out) {
-  DeviceInfo* di = device_info();
-  if (di == nullptr) return CPMTP_ERR_LAUNCH;
-  if (di->cc_major != 10) return CPMTP_ERR_ARCH;
-  *out = di;
-  return CPMTP_OK;
-}
 
 constexpr int64_t kMaxStride = int64_t{1} << 38;       // elements: what a tensor map's strides hold
 
@@ -82,9 +75,63 @@ int blocks_for(long long items, int threads, int sms) {
   return static_cast<int>(blocks < most ? blocks : most);
 }
 
-size_t attend_bytes(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
-  return align_up(sizeof(float) * static_cast<size_t>(s.B) * s.Q * Hq + kAlign);
+// Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.
+int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
+  const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
+
+struct AttendLayout {
+  int nt, chunks, tiles;
+  size_t part_o, part_ml, unit_ctas, whole_ml, scores, total;
+};
+AttendLayout attend_layout(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
+  AttendLayout L;
+  L.nt = attend_columns(c, s, Hq);
+  L.chunks = static_cast<int>((static_cast<long long>(s.Q) * (Hq / c.H) + L.nt - 1) / L.nt);
+  const long long slots = static_cast<long long>(s.width) * c.page_slots;
+  L.tiles = static_cast<int>(slots > 0 ? (slots + attend::kTile - 1) / attend::kTile : 1);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes); return o; };
+  const size_t parts = 2 * static_cast<size_t>(sm_count()) * L.nt, units = static_cast<size_t>(s.B) * c.H * L.chunks;
+  L.part_o = take(parts * 128 * sizeof(float));
+  L.part_ml = take(parts * sizeof(float2));
+  L.unit_ctas = take(units * sizeof(int2));
+  L.whole_ml = take(c.acc != nullptr ? units * L.nt * sizeof(float2) : 0);
+  L.scores = take(c.acc != nullptr ? units * L.tiles * L.nt * attend::kTile * sizeof(float) : 0);
+  L.total = off;
+  return L;
+}
+// Whether the list of all tiles can be counted in 31 bits.
+bool attend_fits(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
+  if (static_cast<long long>(s.Q) * (Hq / c.H) > (1 << 24)) return false;
+  const AttendLayout L = attend_layout(c, s, Hq);
+  return static_cast<double>(s.B) * c.H * L.chunks * L.tiles < 2147483648.0;
+}
+
+// Slots of a TMA box: they have to lie in one page, and a tile has to be made of whole boxes.
+int piece_slots(int page_slots) {
+  int piece = attend::kTile;
+  while (page_slots % piece != 0) piece /= 2;
+  return piece;
+}
+
+template <int NT>
+cudaError_t launch_attend(const CUtensorMap& tk, const CUtensorMap& tv, attend::Params& p, int sms, int* dev_status, cudaStream_t st) {
+  constexpr int kMost = 232448;
+  p.slots = (kMost - attend::Layout<NT>::kFixed) / (p.halves * attend::kHalfBytes);
+  if (p.slots > attend::kMaxSlots) p.slots = attend::kMaxSlots;
+  p.ctas = sms;
+  static bool done[64] = {};
+  cudaError_t e = allow_smem(attend::attend_kernel<NT>, done, kMost);
+  if (e != cudaSuccess) return e;
+  const int bytes = attend::Layout<NT>::kFixed + p.slots * p.halves * attend::kHalfBytes;
+  e = launch_pdl(attend::attend_kernel<NT>, dim3(sms), dim3(attend::kThreads), bytes, st, tk, tv, p, dev_status);
+  if (e != cudaSuccess) return e;
+  const int adders = p.scores != nullptr ? p.c.H * ((p.tiles + attend::kJoinTiles - 1) / attend::kJoinTiles) : 0;
+  return launch_pdl(attend::join_kernel<NT>, dim3(p.c.H * p.chunks + adders, p.s.B), dim3(attend::kJoinThreads), 0, st, p);
+}
+
 size_t evict_bytes(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int budget) {
   return align_up(sizeof(int) * static_cast<size_t>(s.B) * c.H * budget + kAlign);
 }
@@ -118,7 +165,7 @@ int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
 
 size_t cpmtp_cache_attend_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t Hq) {
   if (check_cache(cache) != CPMTP_OK || check_seqs(*cache, seqs) != CPMTP_OK || Hq < 1 || Hq % cache->H != 0) return 0;
-  return attend_bytes(*cache, *seqs, Hq);
+  return attend_fits(*cache, *seqs, Hq) ? attend_layout(*cache, *seqs, Hq).total : 0;
 }
 
 int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_attend_args* args, void* workspace,
@@ -130,23 +177,44 @@ int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
   const cpmtp_cache_seqs& s = *seqs;
   const cpmtp_attend_args& a = *args;
   if (a.Hq < 1 || a.Hq % c.H != 0 || !std::isfinite(a.scale)) return CPMTP_ERR_SHAPE;
-  if (static_cast<long long>(s.Q) * a.Hq > (1 << 24)) return CPMTP_ERR_LIMIT;
+  if (!attend_fits(c, s, a.Hq)) return CPMTP_ERR_LIMIT;
   if (s.B == 0 || s.Q == 0) return CPMTP_OK;
   if ((rc = check_cache_data(c)) != CPMTP_OK || (rc = check_seqs_data(s)) != CPMTP_OK) return rc;
   if ((rc = check_tokens(&a.q, s.Q, a.Hq, c.D)) != CPMTP_OK || (rc = check_tokens(&a.out, s.Q, a.Hq, c.D)) != CPMTP_OK) return rc;
   if (workspace == nullptr) return CPMTP_ERR_NULL;
   if (!aligned(a.lse, 4) || !aligned(dev_status, 4) || !aligned(workspace, kAlign)) return CPMTP_ERR_ALIGN;
-  if (workspace_bytes < attend_bytes(c, s, a.Hq)) return CPMTP_ERR_WORKSPACE;
+  const AttendLayout L = attend_layout(c, s, a.Hq);
+  if (workspace_bytes < L.total) return CPMTP_ERR_WORKSPACE;
   DeviceInfo* di = nullptr;
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_CACHE_ATTEND, st);
-  float* lse = static_cast<float*>(workspace);
-  CPMTP_TRY(launch_pdl(attend::attend_kernel, dim3(s.Q * a.Hq, s.B), dim3(attend::kThreads), 0, st, c, s, a, lse, dev_status));
+  attend::Params p = {};
+  p.c = c; p.s = s; p.a = a;
+  p.G = a.Hq / c.H; p.chunks = L.chunks; p.tiles = L.tiles;
+  p.piece = piece_slots(c.page_slots);
+  p.halves = c.D > 64 ? 2 : 1;
+  p.ksteps = (c.D + 15) / 16;
+  p.q_vec = tokens_vec(a.q);
+  p.scale2 = a.scale * attend::kLog2e;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.part_o = reinterpret_cast<float*>(ws + L.part_o);
+  p.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);
+  p.unit_ctas = reinterpret_cast<int2*>(ws + L.unit_ctas);
   if (c.acc != nullptr) {
-    const int blocks = (s.width * c.page_slots + attend::kThreads - 1) / attend::kThreads;
-    CPMTP_TRY(launch_pdl(attend::weight_kernel, dim3(blocks, c.H, s.B), dim3(attend::kThreads), 0, st, c, s, a, lse, dev_status));
+    p.whole_ml = reinterpret_cast<float2*>(ws + L.whole_ml);
+    p.scores = reinterpret_cast<float*>(ws + L.scores);
   }
+  const WaitKnobs wait = wait_knobs();
+  p.wait_limit_us = wait.limit_us;
+  p.test_skip_load = wait.skip_load;
+  CUtensorMap tk, tv;
+  if (!make_paged_tmap_bf16(&tk, c.k, c.D, c.page_slots, c.H, c.pages, c.k_slot, c.k_head, c.k_page, p.piece) ||
+      !make_paged_tmap_bf16(&tv, c.v, c.D, c.page_slots, c.H, c.pages, c.v_slot, c.v_head, c.v_page, p.piece))
+    return CPMTP_ERR_LAUNCH;
+  if (L.nt == 16) CPMTP_TRY(launch_attend<16>(tk, tv, p, di->sms, dev_status, st));
+  else if (L.nt == 32) CPMTP_TRY(launch_attend<32>(tk, tv, p, di->sms, dev_status, st));
+  else CPMTP_TRY(launch_attend<64>(tk, tv, p, di->sms, dev_status, st));
   return CPMTP_OK;
 }
 

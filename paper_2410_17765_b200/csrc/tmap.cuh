@@ -62,6 +62,21 @@ inline bool make_grouped_tmap_bf16(CUtensorMap* out, const void* base, uint64_t 
   return rc == CUDA_SUCCESS;
 }
 
+// A paged cache [pages][heads][slots][D] with any distances (elements) between pages, heads and slots, read in boxes of 64 columns of
+// `piece` slots of one head of one page.  Columns past D, and pages out of range, read as zero.
+inline bool make_paged_tmap_bf16(CUtensorMap* out, const void* base, uint64_t D, uint64_t slots, uint64_t heads, uint64_t pages, uint64_t slot_stride,
+                                 uint64_t head_stride, uint64_t page_stride, uint32_t piece) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[4] = {D, slots, heads, pages};
+  // (the distance of a dimension of size one is never used, but has to be a valid one)
+  cuuint64_t strides[3] = {slot_stride * 2, (heads > 1 ? head_stride : D) * 2, (pages > 1 ? page_stride : D) * 2};
+  cuuint32_t box[4] = {64, piece, 1, 1};
+  cuuint32_t elem[4] = {1, 1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Operand of D = A * B^T as the GEMM engine reads it.
 //   K-major : matrix [rows, K] with K contiguous; tile box = 64 (K) x tile_rows
 //   MN-major: matrix [K, rows] with the row index contiguous; tile box = 64 (rows) x 64 (K)

@@ -19,28 +19,8 @@ namespace {
 
 using io::bf16_t;
 
-int check_device(DeviceInfo** out) {
-  DeviceInfo* di = device_info();
-  if (di == nullptr) return CPMTP_ERR_LAUNCH;
-  if (di->cc_major != 10) return CPMTP_ERR_ARCH;
-  *out = di;
-  return CPMTP_OK;
-}
-
 bool known_type(int t) { return t == CPMTP_BF16 || t == CPMTP_F32; }
 size_t type_bytes(int t) { return t == CPMTP_F32 ? 4 : 2; }
-
-// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
-template <class K>
-cudaError_t allow_smem(K* kernel, bool (&done)[64], int bytes) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  std::lock_guard<std::mutex> lock(g_cache_mutex);
-  if (done[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  done[dev] = e == cudaSuccess;
-  return e;
-}
 
 // ------------------------------------------------------------------------------------------- embedding
 int check_embed(const cpmtp_embed_shape* s) {
@@ -55,12 +35,6 @@ struct EmbedLayout {
   int slabs, chunk, chunks;      // columns and sorted positions that the summing warps take
   size_t hist, keys, head, tail, total;
 };
-
-// The current device's number of SMs; without a device that of the one this is written for.
-int sm_count() {
-  const DeviceInfo* di = device_info();
-  return di != nullptr && di->sms > 0 ? di->sms : 148;
-}
 
 // Short chunks of the sums: up to this many tokens, if long ones make fewer warps than this on each SM.
 constexpr long long kShortTokens = 2048, kWarpsWanted = 8;
