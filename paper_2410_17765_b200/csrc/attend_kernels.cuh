@@ -5,16 +5,18 @@
 // Every key and value is read once and used for a few rows only (the new tokens times the query heads that share a head of the
 // cache), so the time is that of reading the cache.  The products run on the tensor cores with the cache's tile as the operand of
 // 128 rows and the queries as the narrow one:
-//   S^T [128 slots, NT rows] = K_tile [128, D] Q^T,   O^T [D, NT] = V_tile^T [D, 128] P^T
-// in TMEM: a lane is a slot in the first and a column of the head in the second, and nothing is padded to 128 but D.
+//   S^T [128 slots, NT rows] = K_tile [128, D] Q^T,   O^T [D, 2 NT] = V_tile^T [D, 128] [P_high; P_low]^T
+// in TMEM: a lane is a slot in the first and a column of the head in the second, and nothing is padded to 128 but D.  A product this
+// narrow takes the time of reading its wide operand from shared memory, so the low parts of the weights ride along.
 //
 // The tiles of 128 slots of all (sequence, head, chunk of NT rows) form one list, which is cut into equal shares, one for each
 // SM, whatever the lengths.  A share that ends inside a unit leaves (max, sum, unnormalised out) behind; join_kernel joins them.
 //
-//   warp 0      TMA: pages into a ring of K and V tiles in turn
-//   warp 1      tcgen05.mma: S of tile g, then O of tile g - 1
-//   warps 2-5   a thread is a slot: weights; then a column: sums O in registers
-//   warp 6      queries of the next unit into shared memory
+//   warps 0, 1   TMA: pages into a ring of K tiles and one of V tiles, a warp to each
+//   warp 2       tcgen05.mma: S of tile g, then O of tile g - 2
+//   warp 3       queries of the next unit into shared memory
+//   warps 4-11   two groups of 128 threads take tiles in turn: a thread is a slot and makes weights, then a column and sums O in
+//                registers.  Each group has a reference, sums and an O of its own; the one with a unit's last tile joins them
 #pragma once
 #include <cuda.h>
 
@@ -26,7 +28,7 @@ namespace attend {
 using io::bf16_t;
 
 constexpr int kTile = 128;                  // slots of a tile
-constexpr int kThreads = 7 * 32;
+constexpr int kThreads = 12 * 32;
 constexpr int kHalfBytes = kTile * 128;     // 128 slots of 64 columns
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -1.7e38f;           // the reference of a row that has seen nothing yet
@@ -42,7 +44,7 @@ struct Params {
   int chunks;                  // chunks of NT rows that Q new tokens make
   int piece;                   // slots that one TMA box covers: they lie in one page, and pieces tile a tile
   int halves, ksteps;          // 64-column halves and 16-column steps of a head
-  int slots;                   // of the ring; a slot holds one K or V tile
+  int k_slots, v_slots;        // tiles of the two rings
   int tiles;                   // most tiles of a sequence
   int ctas;                    // of the launch
   int q_vec;                   // queries can be read 16 bytes at a time
@@ -169,22 +171,23 @@ __device__ __forceinline__ int cta_of(const Start& s, int i) {
 template <int NT>
 struct Layout {
   static constexpr int kQ = NT * 256;                // queries of a unit: two halves of NT rows of 128 bytes
-  static constexpr int kP = NT * 256;                // weights of a tile: 128 slots of NT rows, bf16
-  static constexpr int kQueries = NT < 64 ? 2 : 1;   // units whose queries are held: one where two would cost the ring a slot
+  static constexpr int kP = NT * 256;                // weights of a tile: 128 slots of NT rows, bf16; two make NT x 128 fp32
   static constexpr int kBars = 512;
-  static constexpr int kSmall = 11 * NT * 4 + 128;
-  static constexpr int kFixed = 1024 + kQueries * kQ + 4 * kP + kBars + kSmall;
-  static constexpr int kTmem = 4 * NT;               // two S and two O accumulators
+  static constexpr int kGroup = 11 * NT;             // words of a group's small arrays
+  static constexpr int kSmall = 2 * kGroup * 4 + 128;
+  static constexpr int kFixed = 1024 + 2 * kQ + 4 * kP + kBars + kSmall;
+  static constexpr int kTmem = 8 * NT;               // four S accumulators and two O, of the high and the low parts of the weights
 };
 constexpr int kMaxSlots = 12;
 
-__device__ __forceinline__ bool any_of_group(bool v) {      // of the 128 softmax threads; a barrier
+// Barriers of a group's 128 threads.
+__device__ __forceinline__ bool any_of_group(int group, bool v) {
   int r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, 1, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"(static_cast<int>(v)) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, %2, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(static_cast<int>(v)), "r"(group + 1) : "memory");
   return r != 0;
 }
-__device__ __forceinline__ void group_sync() { asm volatile("barrier.cta.sync.aligned 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync.aligned %0, 128;" ::"r"(group + 1) : "memory"); }
 __device__ __forceinline__ float warp_max(float v) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -210,66 +213,63 @@ template <int NT>
 __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                                                              const __grid_constant__ Params p, int* dev_status) {
   using L = Layout<NT>;
-  constexpr int CH = NT < 32 ? NT : 32, NCH = NT / CH;        // columns of an accumulator handled at a time
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u;
   const uint32_t slot_bytes = p.halves * kHalfBytes;
-  // [ring][queries x 2][weights: two tiles of (high, low)][barriers][small arrays]
-  const uint32_t ring = raw + pad, qbuf = ring + p.slots * slot_bytes, pbuf = qbuf + L::kQueries * L::kQ, bars = pbuf + 4 * L::kP;
-  uint8_t* small = smem_raw + (bars + L::kBars - raw);
-  int* bound = reinterpret_cast<int*>(small);                 // [NT] slots that a row sees
-  float* wmax = reinterpret_cast<float*>(bound + NT);     // [4][NT] the warps' maxima
-  float* ref = wmax + 4 * NT;                                 // [NT]
-  float* alpha = ref + NT;                                    // [NT]
-  float* lsum = alpha + NT;                                   // [4][NT]
-  int* misc = reinterpret_cast<int*>(lsum + 4 * NT);          // [0..6] scan, [8..14] start, [16] TMEM address, [17], [18] abort flags
-  Start* start_sh = reinterpret_cast<Start*>(misc + 8);
-  volatile int* abort_flag = misc + 17;
-  volatile int* group_abort = misc + 18;
+  // [ring of K][ring of V][queries x 2][weights: two tiles of (high, low)][barriers][small arrays]
+  const uint32_t ring = raw + pad, qbuf = ring + (p.k_slots + p.v_slots) * slot_bytes, pbuf = qbuf + 2 * L::kQ, bars = pbuf + 4 * L::kP;
+  float* small = reinterpret_cast<float*>(smem_raw + (bars + L::kBars - raw));
+  int* misc = reinterpret_cast<int*>(small + 2 * L::kGroup);  // [0..11] scan, [12..18] start, [20] TMEM address, [21] abort flag, [22], [23] the groups'
+  Start* start_sh = reinterpret_cast<Start*>(misc + 12);
+  volatile int* abort_flag = misc + 21;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (kMaxSlots + s); };
-  auto qfull = [&](int s) { return bars + 8u * (2 * kMaxSlots + s); };
-  auto qfree = [&](int s) { return bars + 8u * (2 * kMaxSlots + 2 + s); };
-  auto sfull = [&](int s) { return bars + 8u * (2 * kMaxSlots + 4 + s); };
-  auto pfull = [&](int s) { return bars + 8u * (2 * kMaxSlots + 6 + s); };
-  auto ofull = [&](int s) { return bars + 8u * (2 * kMaxSlots + 8 + s); };
-  const uint32_t drain = bars + 8u * (2 * kMaxSlots + 10);
-  static_assert(8 * (2 * kMaxSlots + 11) <= L::kBars, "barriers");
+  auto bar = [&](int i) { return bars + 8u * (2 * kMaxSlots + i); };
+  auto qfull = [&](int s) { return bar(s); };
+  auto qfree = [&](int s) { return bar(2 + s); };
+  auto pfull = [&](int s) { return bar(4 + s); };
+  auto ofull = [&](int s) { return bar(6 + s); };
+  auto xfull = [&](int s) { return bar(8 + s); };
+  auto xfree = [&](int s) { return bar(10 + s); };
+  auto sfull = [&](int s) { return bar(12 + s); };
+  const uint32_t drain = bar(16);
+  static_assert(8 * (2 * kMaxSlots + 17) <= L::kBars, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint64_t wait_ns = static_cast<uint64_t>(p.wait_limit_us) * 1000ull;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < p.slots; ++s) {
+    for (int s = 0; s < p.k_slots + p.v_slots; ++s) {
       ptx::mbar_init(full(s), 1);
       ptx::mbar_init(empty(s), 1);
     }
     for (int s = 0; s < 2; ++s) {
       ptx::mbar_init(qfull(s), 32);
       ptx::mbar_init(qfree(s), 1);
-      ptx::mbar_init(sfull(s), 1);
-      ptx::mbar_init(pfull(s), 128);
+      ptx::mbar_init(pfull(s), 4);       // a lane of each of a group's warps
       ptx::mbar_init(ofull(s), 1);
+      ptx::mbar_init(xfull(s), 4);
+      ptx::mbar_init(xfree(s), 4);
     }
+    for (int s = 0; s < 4; ++s) ptx::mbar_init(sfull(s), 1);
     ptx::mbar_init(drain, 1);
-    *abort_flag = 0;
-    *group_abort = 0;
+    misc[21] = misc[22] = misc[23] = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tmap(&tm_k);
     ptx::prefetch_tmap(&tm_v);
   }
-  if (warp == 1) {
-    ptx::tmem_alloc(ptx::smem_u32(misc + 16), L::kTmem);
+  if (warp == 2) {
+    ptx::tmem_alloc(ptx::smem_u32(misc + 20), L::kTmem);
     ptx::tmem_relinquish();
   }
   ptx::grid_dep_wait();
   ptx::tc_fence_before_sync();
   find_start(p, NT, misc, start_sh, dev_status);
   ptx::tc_fence_after_sync();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(misc + 16);
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(misc + 20);
   const Start start = *start_sh;
   Walk w(p, start, NT);
 
-  if (warp == 0) {
+  if (warp < 2) {
     // ------------------------------------------------------------------------------------------ pages into the ring
     const int pieces = kTile / p.piece;
     auto page_at = [&](const Walk& x) {          // the page of this lane's piece of the tile; -1: nothing to load
@@ -278,6 +278,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       const int page = p.s.table[x.b * p.s.ld_table + slot / p.c.page_slots];
       return page >= 0 && page < p.c.pages ? page : p.c.pages;      // out of range: the box reads as zeros
     };
+    // (a ring has one warp that fills it: a second one could be a whole lap ahead, which the parity of a barrier does not tell)
+    const int base = warp == 0 ? 0 : p.k_slots, n = warp == 0 ? p.k_slots : p.v_slots;
     int it = 0, page = w.left > 0 ? page_at(w) : -1;
     bool alive = true;
     while (w.left > 0 && alive) {
@@ -289,82 +291,79 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       if (here == p.c.pages) cache::raise_status(dev_status, cache::kBadIndex);
       const uint32_t lanes = __ballot_sync(0xffffffffu, here >= 0);
       const uint32_t bytes = __popc(lanes) * p.piece * 128u * p.halves;
-      for (int kv = 0; kv < 2; ++kv, ++it) {
-        const int s = it % p.slots;
-        if (lane == 0) {
-          alive = ptx::mbar_wait(empty(s), ((it / p.slots) & 1) ^ 1u, abort_flag, wait_ns);
-          if (alive && it + 1 != p.test_skip_load) {
-            if (bytes > 0) ptx::mbar_arrive_expect_tx(full(s), bytes);
-            else ptx::mbar_arrive(full(s));
-          }
-        }
-        alive = __shfl_sync(0xffffffffu, alive, 0);
-        if (!alive) break;
-        if (here >= 0 && it + 1 != p.test_skip_load) {
-          const uint32_t dst = ring + s * slot_bytes + lane * p.piece * 128u;
-          const void* tm = kv == 0 ? &tm_k : &tm_v;
-          for (int half = 0; half < p.halves; ++half) tma_load_4d(dst + half * kHalfBytes, tm, full(s), half * 64, in_page, h, here);
+      const int s = base + it % n;
+      const bool skip = 2 * it + warp + 1 == p.test_skip_load;
+      if (lane == 0) {
+        alive = ptx::mbar_wait(empty(s), ((it / n) & 1) ^ 1u, abort_flag, wait_ns);
+        if (alive && !skip) {
+          if (bytes > 0) ptx::mbar_arrive_expect_tx(full(s), bytes);
+          else ptx::mbar_arrive(full(s));
         }
       }
+      alive = __shfl_sync(0xffffffffu, alive, 0);
+      if (!alive) break;
+      if (here >= 0 && !skip) {
+        const uint32_t dst = ring + s * slot_bytes + lane * p.piece * 128u;
+        for (int half = 0; half < p.halves; ++half) tma_load_4d(dst + half * kHalfBytes, warp == 0 ? &tm_k : &tm_v, full(s), half * 64, in_page, h, here);
+      }
+      ++it;
     }
     ptx::grid_dep_launch();
     if (lane == 0)               // what was issued has to land before the shared memory is given back
-      for (int back = 1; back <= p.slots && back <= it; ++back) ptx::mbar_wait(full((it - back) % p.slots), ((it - back) / p.slots) & 1, abort_flag, wait_ns, false);
-  } else if (warp == 1) {
+      for (int j = it - 1; j >= 0 && j >= it - n; --j) ptx::mbar_wait(full(base + j % n), (j / n) & 1, abort_flag, wait_ns, false);
+  } else if (warp == 2) {
     // ------------------------------------------------------------------------------------------ products
     if (lane == 0) {
-      constexpr uint32_t idesc_s = ptx::make_idesc_bf16(128, NT, 0, 0), idesc_o = ptx::make_idesc_bf16(128, NT, 1, 0);
+      constexpr uint32_t idesc_s = ptx::make_idesc_bf16(128, NT, 0, 0), idesc_o = ptx::make_idesc_bf16(128, 2 * NT, 1, 0);
       bool alive = true;
       int g = 0, unit = 0;
       auto second = [&](int k) {                 // O of tile k
-        const int s = (2 * k + 1) % p.slots;
-        if (!ptx::mbar_wait(full(s), ((2 * k + 1) / p.slots) & 1, abort_flag, wait_ns) || !ptx::mbar_wait(pfull(k & 1), (k >> 1) & 1, abort_flag, wait_ns)) return false;
+        const int s = p.k_slots + k % p.v_slots;
+        if (!ptx::mbar_wait(full(s), (k / p.v_slots) & 1, abort_flag, wait_ns) || !ptx::mbar_wait(pfull(k & 1), (k >> 1) & 1, abort_flag, wait_ns)) return false;
         ptx::tc_fence_after_sync();
-        const uint32_t v = ring + s * slot_bytes, pw = pbuf + (k & 1) * 2 * L::kP, d = tmem + 2 * NT + (k & 1) * NT;
+        const uint32_t v = ring + s * slot_bytes, pw = pbuf + (k & 1) * 2 * L::kP, d = tmem + 4 * NT + (k & 1) * 2 * NT;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          const uint64_t a = ptx::make_smem_desc_sw128(v + ks * 2048, kHalfBytes, 1024);
-#pragma unroll
-          for (int low = 0; low < 2; ++low)
-            ptx::umma_bf16(d, a, ptx::make_smem_desc_sw128(pw + low * L::kP + (ks >> 2) * (NT * 128) + (ks & 3) * 32, 16, 1024), idesc_o, (ks | low) != 0);
-        }
+        for (int ks = 0; ks < 8; ++ks)
+          ptx::umma_bf16(d, ptx::make_smem_desc_sw128(v + ks * 2048, kHalfBytes, 1024),
+                         ptx::make_smem_desc_sw128(pw + (ks >> 2) * (2 * NT * 128) + (ks & 3) * 32, 16, 1024), idesc_o, ks != 0);
         ptx::umma_commit(empty(s));
         ptx::umma_commit(ofull(k & 1));
         return true;
       };
       while (w.left > 0 && alive) {
         const int end = w.piece_end();
-        const int qs = unit % L::kQueries;
+        const int qs = unit & 1;
         const uint32_t qb = qbuf + qs * L::kQ;
-        if (!ptx::mbar_wait(qfull(qs), (unit / L::kQueries) & 1, abort_flag, wait_ns)) { alive = false; break; }
+        if (!ptx::mbar_wait(qfull(qs), (unit >> 1) & 1, abort_flag, wait_ns)) { alive = false; break; }
         for (int t = w.t; t < end; ++t, ++g) {
-          const int s = (2 * g) % p.slots;
-          if (!ptx::mbar_wait(full(s), ((2 * g) / p.slots) & 1, abort_flag, wait_ns)) { alive = false; break; }
+          const int s = g % p.k_slots;
+          if (!ptx::mbar_wait(full(s), (g / p.k_slots) & 1, abort_flag, wait_ns)) { alive = false; break; }
           ptx::tc_fence_after_sync();
           const uint32_t k = ring + s * slot_bytes;
           for (int ks = 0; ks < p.ksteps; ++ks)
-            ptx::umma_bf16(tmem + (g & 1) * NT, ptx::make_smem_desc_sw128(k + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
+            ptx::umma_bf16(tmem + (g & 3) * NT, ptx::make_smem_desc_sw128(k + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
                            ptx::make_smem_desc_sw128(qb + (ks >> 2) * (NT * 128) + (ks & 3) * 32, 16, 1024), idesc_s, ks != 0);
           ptx::umma_commit(empty(s));
-          ptx::umma_commit(sfull(g & 1));
+          ptx::umma_commit(sfull(g & 3));
           if (t + 1 == end) ptx::umma_commit(qfree(qs));
-          if (g > 0 && !second(g - 1)) { alive = false; break; }
+          if (g > 1 && !second(g - 2)) { alive = false; break; }
         }
         w.next_unit(p, end - w.t);
         ++unit;
       }
+      if (alive && g > 1) alive = second(g - 2);
       if (alive && g > 0) second(g - 1);
       ptx::umma_commit(drain);
       ptx::mbar_wait(drain, 0, abort_flag, wait_ns, false);
     }
-  } else if (warp == 6) {
+  } else if (warp == 3) {
     // ------------------------------------------------------------------------------------------ queries
     bool alive = true;
     for (int unit = 0; w.left > 0; ++unit) {
       const int end = w.piece_end();
       const int u_chunks = (w.q.fresh * p.G + NT - 1) / NT, h = w.u / u_chunks, row0 = (w.u % u_chunks) * NT, rows = w.q.fresh * p.G;
-      const int qs = unit % L::kQueries;
-      alive = ptx::mbar_wait(qfree(qs), ((unit / L::kQueries) & 1) ^ 1u, abort_flag, wait_ns);
+      const int qs = unit & 1;
+      alive = ptx::mbar_wait(qfree(qs), ((unit >> 1) & 1) ^ 1u, abort_flag, wait_ns);
       if (!__all_sync(0xffffffffu, alive)) break;
       const uint32_t qb = qbuf + qs * L::kQ;
       const bf16_t* q = static_cast<const bf16_t*>(p.a.q.data) + w.b * p.a.q.seq;
@@ -393,176 +392,214 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     }
   } else {
     // ------------------------------------------------------------------------------------------ weights and sums
-    const int quarter = warp & 3, x = quarter * 32 + lane;      // slot of the tile, and column of the head
+    const int group = (warp - 4) >> 2, quarter = warp & 3, x = quarter * 32 + lane;      // slot of the tile, and column of the head
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t p_at = pbuf + (x >> 6) * (NT * 128) + (x & 7) * 2;      // of row 0, without its swizzle
+    const uint32_t p_mine = pbuf + group * 2 * L::kP;
+    const uint32_t p_at = p_mine + (x >> 6) * (2 * NT * 128) + (x & 7) * 2;  // of row 0, without its swizzle; rows NT .. 2 NT - 1 are the low parts
     const uint32_t chunk = (x & 63) >> 3;
+    int* bound = reinterpret_cast<int*>(small + group * L::kGroup);          // [NT] slots that a row sees
+    float* wmax = small + group * L::kGroup + NT;                            // [4][NT] the warps' maxima
+    float* ref = wmax + 4 * NT;                                              // [NT]
+    float* alpha = ref + NT;                                                 // [NT]
+    float* lsum = alpha + NT;                                                // [4][NT]
+    volatile int* group_abort = misc + 22 + group;
     float o[NT], l[NT];
-    int g = 0, flat = start.first;
+    int g = 0, flat = start.first, given = 0, taken = 0;        // units that this group has given to the other, and taken from it
     auto fail = [&] { *abort_flag = 1; *group_abort = 1; };
-    auto add_o = [&](int k) {                    // O of tile k
-      if (!ptx::mbar_wait(ofull(k & 1), (k >> 1) & 1, abort_flag, wait_ns, false)) fail();
+    auto wait = [&](uint32_t b, int phase) {
+      if (!ptx::mbar_wait(b, phase & 1, abort_flag, wait_ns, false)) fail();
       __syncwarp();
+    };
+    auto arrive = [&](uint32_t b) {
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(b);
+    };
+    auto add_o = [&](int k) {                    // O of tile k
+      wait(ofull(group), k >> 1);
       ptx::tc_fence_after_sync();
 #pragma unroll
-      for (int ch = 0; ch < NCH; ++ch) {
-        float v[CH];
-        tmem_load(tmem + lanes + 2 * NT + (k & 1) * NT + ch * CH, v);
+      for (int low = 0; low < 2; ++low) {
+        float v[NT];
+        tmem_load(tmem + lanes + 4 * NT + (2 * group + low) * NT, v);
 #pragma unroll
-        for (int r = 0; r < CH; ++r) o[ch * CH + r] += v[r];
+        for (int r = 0; r < NT; ++r) o[r] += v[r];
       }
     };
     bool alive = true;
     while (w.left > 0) {
-      const int end = w.piece_end(), begin = w.t;
+      const int end = w.piece_end(), begin = w.t, tiles = end - begin;
       const int u_chunks = (w.q.fresh * p.G + NT - 1) / NT, h = w.u / u_chunks, chunk_no = w.u % u_chunks;
       const int rows = min(NT, w.q.fresh * p.G - chunk_no * NT);
       const long long unit_at = (static_cast<long long>(w.b) * p.c.H + h) * p.chunks + chunk_no;
       const int len = w.q.len, sure = len - (w.q.fresh - 1);    // every row sees the slots below `sure`
-      if (begin == 0 && x == 0) p.unit_ctas[unit_at] = make_int2(blockIdx.x, cta_of(start, flat + w.q.tiles - 1));
+      const bool finish = ((g + tiles - 1) & 1) == group;       // this group has the last tile
+      if (finish && begin == 0 && x == 0) p.unit_ctas[unit_at] = make_int2(blockIdx.x, cta_of(start, flat + w.q.tiles - 1));
       if (end * kTile > sure) {
         if (x < NT) bound[x] = x < rows ? len - (w.q.fresh - 1 - (chunk_no * NT + x) / p.G) : len;
-        group_sync();
+        group_sync(group);
       }
 #pragma unroll
       for (int r = 0; r < NT; ++r) o[r] = l[r] = 0.f;
-      for (int t = begin; t < end; ++t, ++g) {
-        const int slot = t * kTile + x;
-        const bool masked = (t + 1) * kTile > sure, first = t == begin;
-        if (!ptx::mbar_wait(sfull(g & 1), (g >> 1) & 1, abort_flag, wait_ns, false)) fail();
-        __syncwarp();
+      bool first = true;
+      for (int k = g + ((g & 1) != group); k < g + tiles; k += 2) {
+        const int t = begin + (k - g), slot = t * kTile + x;
+        const bool masked = (t + 1) * kTile > sure;
+        wait(sfull(k & 3), k >> 2);
         ptx::tc_fence_after_sync();
-        const uint32_t s_at = tmem + lanes + (g & 1) * NT;
-        float v[CH];
-        auto scores = [&](int ch) {
-          tmem_load(s_at + ch * CH, v);
+        float v[NT];
+        tmem_load(tmem + lanes + (k & 3) * NT, v);
 #pragma unroll
-          for (int r = 0; r < CH; ++r) v[r] *= p.scale2;
-          if (masked) {
+        for (int r = 0; r < NT; ++r) v[r] *= p.scale2;
+        if (masked) {
 #pragma unroll
-            for (int r = 0; r < CH; ++r) v[r] = slot < bound[ch * CH + r] ? v[r] : -INFINITY;
-          }
-        };
-        bool rise = first;
-#pragma unroll
-        for (int ch = 0; ch < NCH; ++ch) {
-          scores(ch);
-          if (p.scores != nullptr) {
-            float* to = p.scores + ((unit_at * p.tiles + t) * NT + ch * CH) * kTile + x;
-#pragma unroll
-            for (int r = 0; r < CH; ++r)
-              if (ch * CH + r < rows) to[r * kTile] = v[r];
-          }
-          if (!first) {
-#pragma unroll
-            for (int r = 0; r < CH; ++r) rise |= v[r] > ref[ch * CH + r] + kSlack;
-          }
+          for (int r = 0; r < NT; ++r) v[r] = slot < bound[r] ? v[r] : -INFINITY;
         }
-        rise = any_of_group(rise);
+        if (p.scores != nullptr) {
+          float* to = p.scores + (unit_at * p.tiles + t) * NT * kTile + x;
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+            if (r < rows) to[r * kTile] = v[r];
+        }
+        bool rise = first;
+        if (!first) {
+#pragma unroll
+          for (int r = 0; r < NT; ++r) rise |= v[r] > ref[r] + kSlack;
+        }
+        rise = any_of_group(group, rise);
         if (*group_abort) { alive = false; break; }
+        if (first && given > 0) wait(xfree(group), given - 1);       // the other group has read what this one left
         if (rise) {
+          float top = 0.f;
 #pragma unroll
-          for (int ch = 0; ch < NCH; ++ch) {
-            if (NCH > 1) scores(ch);
-            float top = 0.f;
-#pragma unroll
-            for (int r = 0; r < CH; ++r) {
-              const float m = warp_max(v[r]);
-              if (lane == r) top = m;
-            }
-            if (lane < CH) wmax[quarter * NT + ch * CH + lane] = top;
+          for (int r = 0; r < NT; ++r) {
+            const float m = warp_max(v[r]);
+            if (lane == r) top = m;
           }
-          group_sync();
+          if (lane < NT) wmax[quarter * NT + lane] = top;
+          group_sync(group);
           if (x < NT) {
             const float old = first ? kNone : ref[x];
             const float m = fmaxf(fmaxf(fmaxf(wmax[x], wmax[NT + x]), fmaxf(wmax[2 * NT + x], wmax[3 * NT + x])), old);
             ref[x] = m;
             alpha[x] = ptx::ex2_approx(old - m);
           }
-          group_sync();
-#pragma unroll
-          for (int r = 0; r < NT; ++r) l[r] *= alpha[r];
+          group_sync(group);
         }
+        if (!first) add_o(k - 2);                // (and then the weights' buffer is free)
+        if (rise) {
 #pragma unroll
-        for (int ch = 0; ch < NCH; ++ch) {
-          if (NCH > 1) scores(ch);
-          const uint32_t to = p_at + (g & 1) * 2 * L::kP + ch * CH * 128;
-#pragma unroll
-          for (int r = 0; r < CH; ++r) {
-            const float e = ptx::ex2_approx(v[r] - ref[ch * CH + r]);
-            l[ch * CH + r] += e;
-            // as the sum of two bf16: one would add its own rounding, 2^-9 of a weight, to that of the output
-            const uint32_t hi = ptx::pack_bf16x2(e, 0.f);
-            const uint32_t lo = ptx::pack_bf16x2(e - ptx::bf16_lo(hi), 0.f);
-            const uint32_t at = to + r * 128 + ((chunk ^ (r & 7)) << 4);
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(hi)) : "memory");
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + L::kP), "h"(static_cast<uint16_t>(lo)) : "memory");
+          for (int r = 0; r < NT; ++r) {
+            const float f = alpha[r];
+            l[r] *= f;
+            o[r] *= f;
           }
+        }
+        first = false;
+#pragma unroll
+        for (int r = 0; r < NT; ++r) {
+          const float e = ptx::ex2_approx(v[r] - ref[r]);
+          l[r] += e;
+          // as the sum of two bf16: one would add its own rounding, 2^-9 of a weight, to that of the output
+          const uint32_t hi = ptx::pack_bf16x2(e, 0.f);
+          const uint32_t lo = ptx::pack_bf16x2(e - ptx::bf16_lo(hi), 0.f);
+          const uint32_t at = p_at + r * 128 + ((chunk ^ (r & 7)) << 4);
+          asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(hi)) : "memory");
+          asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + NT * 128), "h"(static_cast<uint16_t>(lo)) : "memory");
         }
         if ((t + 1) * kTile > len) {
           // rows of V that no slot of the sequence fills: whatever lies there must not meet a weight of zero
-          const int s = (2 * g + 1) % p.slots;
-          if (!ptx::mbar_wait(full(s), ((2 * g + 1) / p.slots) & 1, abort_flag, wait_ns, false)) fail();
+          const int s = p.k_slots + k % p.v_slots;
+          wait(full(s), k / p.v_slots);
           if (slot >= len)
             for (int i = 0; i < 8 * p.halves; ++i)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + s * slot_bytes + (i >> 3) * kHalfBytes + x * 128 + (i & 7) * 16), "r"(0) : "memory");
         }
         ptx::tc_fence_before_sync();
         ptx::fence_proxy_async_smem();
-        ptx::mbar_arrive(pfull(g & 1));
-        if (!first) add_o(g - 1);
-        if (rise) {
-#pragma unroll
-          for (int r = 0; r < NT; ++r) o[r] *= alpha[r];
-        }
+        arrive(pfull(group));
       }
       if (!alive) break;
-      add_o(g - 1);
-      // sums over the slots' threads
-#pragma unroll
-      for (int ch = 0; ch < NCH; ++ch) {
+      const int last = g + tiles - 1 - (finish ? 0 : 1);         // this group's last tile, if it had one
+      if (last >= g) {
+        add_o(last);
+        // sums over the slots' threads
         float mine = 0.f;
 #pragma unroll
-        for (int r = 0; r < CH; ++r) {
-          const float sum = io::sum_lanes(l[ch * CH + r]);
+        for (int r = 0; r < NT; ++r) {
+          const float sum = io::sum_lanes(l[r]);
           if (lane == r) mine = sum;
         }
-        if (lane < CH) lsum[quarter * NT + ch * CH + lane] = mine;
-      }
-      group_sync();
-      const bool whole = begin == 0 && end == w.q.tiles;
-      float mine = 0.f;
-      if (x < NT) mine = (lsum[x] + lsum[NT + x]) + (lsum[2 * NT + x] + lsum[3 * NT + x]);
-      if (whole) {
-        bf16_t* out = static_cast<bf16_t*>(p.a.out.data) + w.b * p.a.out.seq + x;
+        if (lane < NT) lsum[quarter * NT + lane] = mine;
+        if (!finish) {
+          // to the other group, in the place of this one's weights
 #pragma unroll
-        for (int r = 0; r < NT; ++r)
-          if (r < rows) {
-            const float sum = (lsum[r] + lsum[NT + r]) + (lsum[2 * NT + r] + lsum[3 * NT + r]);
-            const int row = chunk_no * NT + r;
-            if (x < p.c.D) out[(row / p.G) * p.a.out.token + (h * p.G + row % p.G) * p.a.out.head] = io::from_f<bf16_t>(sum == 0.f ? 0.f : __fdividef(o[r], sum));
-          }
-        if (x < rows) {
-          const int row = chunk_no * NT + x;
-          if (p.a.lse != nullptr)
-            p.a.lse[(static_cast<long long>(w.b) * p.s.Q + row / p.G) * p.a.Hq + h * p.G + row % p.G] = mine == 0.f ? -INFINITY : (ref[x] + log2f(mine)) * kLn2;
-          if (p.scores != nullptr) p.whole_ml[unit_at * NT + x] = make_float2(ref[x], mine);
+          for (int r = 0; r < NT; ++r) asm volatile("st.shared.f32 [%0], %1;" ::"r"(p_mine + (r * 128 + x) * 4), "f"(o[r]) : "memory");
+          arrive(xfull(group));
+          ++given;
         }
-      } else {
-        const long long at = (blockIdx.x * 2 + (begin == 0 ? 1 : 0)) * NT;
-#pragma unroll
-        for (int r = 0; r < NT; ++r)
-          if (r < rows) p.part_o[(at + r) * 128 + x] = o[r];
-        if (x < NT) p.part_ml[at + x] = make_float2(ref[x], mine);
       }
-      flat += end - begin;
-      w.next_unit(p, end - begin);
+      if (finish) {
+        group_sync(group);
+        float mine = x < NT ? (lsum[x] + lsum[NT + x]) + (lsum[2 * NT + x] + lsum[3 * NT + x]) : 0.f;
+        float at_ref = x < NT ? ref[x] : 0.f;
+        if (tiles > 1) {
+          wait(xfull(group ^ 1), taken);
+          ++taken;
+          const float* theirs = small + (group ^ 1) * L::kGroup;                  // (the other group's arrays, laid out as these)
+          const float *their_ref = theirs + 5 * NT, *their_sum = theirs + 7 * NT;
+          float* f_mine = wmax;                                                    // [NT] factors, and those of the other's
+          float* f_theirs = wmax + NT;
+          if (x < NT) {
+            const float m = fmaxf(at_ref, their_ref[x]), a = ptx::ex2_approx(at_ref - m), b = ptx::ex2_approx(their_ref[x] - m);
+            f_mine[x] = a;
+            f_theirs[x] = b;
+            mine = mine * a + ((their_sum[x] + their_sum[NT + x]) + (their_sum[2 * NT + x] + their_sum[3 * NT + x])) * b;
+            at_ref = m;
+          }
+          group_sync(group);
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(pbuf + (group ^ 1) * 2 * L::kP + (r * 128 + x) * 4));
+            o[r] = o[r] * f_mine[r] + v * f_theirs[r];
+          }
+          arrive(xfree(group ^ 1));
+        }
+        if (begin == 0 && end == w.q.tiles) {
+          float* sums = wmax + 2 * NT;
+          if (x < NT) sums[x] = mine;
+          group_sync(group);
+          bf16_t* out = static_cast<bf16_t*>(p.a.out.data) + w.b * p.a.out.seq + x;
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+            if (r < rows) {
+              const float sum = sums[r];
+              const int row = chunk_no * NT + r;
+              if (x < p.c.D) out[(row / p.G) * p.a.out.token + (h * p.G + row % p.G) * p.a.out.head] = io::from_f<bf16_t>(sum == 0.f ? 0.f : __fdividef(o[r], sum));
+            }
+          if (x < rows) {
+            const int row = chunk_no * NT + x;
+            if (p.a.lse != nullptr)
+              p.a.lse[(static_cast<long long>(w.b) * p.s.Q + row / p.G) * p.a.Hq + h * p.G + row % p.G] = mine == 0.f ? -INFINITY : (at_ref + log2f(mine)) * kLn2;
+            if (p.scores != nullptr) p.whole_ml[unit_at * NT + x] = make_float2(at_ref, mine);
+          }
+        } else {
+          const long long at = (blockIdx.x * 2 + (begin == 0 ? 1 : 0)) * NT;
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+            if (r < rows) p.part_o[(at + r) * 128 + x] = o[r];
+          if (x < NT) p.part_ml[at + x] = make_float2(at_ref, mine);
+        }
+      }
+      g += tiles;
+      flat += tiles;
+      w.next_unit(p, tiles);
     }
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
-  if (warp == 1) ptx::tmem_dealloc(tmem, L::kTmem);
+  if (warp == 2) ptx::tmem_dealloc(tmem, L::kTmem);
   if (threadIdx.x == 0 && *abort_flag != 0) cache::raise_status(dev_status, cache::kWaitTimeout);
 }
 

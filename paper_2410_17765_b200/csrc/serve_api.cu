@@ -78,7 +78,7 @@ int blocks_for(long long items, int threads, int sms) {
 // Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.
 int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
   const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 16 ? 16 : 32;
 }
 
 struct AttendLayout {
@@ -119,13 +119,14 @@ int piece_slots(int page_slots) {
 template <int NT>
 cudaError_t launch_attend(const CUtensorMap& tk, const CUtensorMap& tv, attend::Params& p, int sms, int* dev_status, cudaStream_t st) {
   constexpr int kMost = 232448;
-  p.slots = (kMost - attend::Layout<NT>::kFixed) / (p.halves * attend::kHalfBytes);
-  if (p.slots > attend::kMaxSlots) p.slots = attend::kMaxSlots;
+  const int slots = std::min((kMost - attend::Layout<NT>::kFixed) / (p.halves * attend::kHalfBytes), attend::kMaxSlots);
+  p.k_slots = slots / 2;          // (a K tile is done with sooner than a V tile, which waits for the weights)
+  p.v_slots = slots - p.k_slots;
   p.ctas = sms;
   static bool done[64] = {};
   cudaError_t e = allow_smem(attend::attend_kernel<NT>, done, kMost);
   if (e != cudaSuccess) return e;
-  const int bytes = attend::Layout<NT>::kFixed + p.slots * p.halves * attend::kHalfBytes;
+  const int bytes = attend::Layout<NT>::kFixed + slots * p.halves * attend::kHalfBytes;
   e = launch_pdl(attend::attend_kernel<NT>, dim3(sms), dim3(attend::kThreads), bytes, st, tk, tv, p, dev_status);
   if (e != cudaSuccess) return e;
   const int adders = p.scores != nullptr ? p.c.H * ((p.tiles + attend::kJoinTiles - 1) / attend::kJoinTiles) : 0;
@@ -213,8 +214,7 @@ int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
       !make_paged_tmap_bf16(&tv, c.v, c.D, c.page_slots, c.H, c.pages, c.v_slot, c.v_head, c.v_page, p.piece))
     return CPMTP_ERR_LAUNCH;
   if (L.nt == 16) CPMTP_TRY(launch_attend<16>(tk, tv, p, di->sms, dev_status, st));
-  else if (L.nt == 32) CPMTP_TRY(launch_attend<32>(tk, tv, p, di->sms, dev_status, st));
-  else CPMTP_TRY(launch_attend<64>(tk, tv, p, di->sms, dev_status, st));
+  else CPMTP_TRY(launch_attend<32>(tk, tv, p, di->sms, dev_status, st));
   return CPMTP_OK;
 }
 
