@@ -13,10 +13,10 @@
 // SM, whatever the lengths.  A share that ends inside a unit leaves (max, sum, unnormalised out) behind; join_kernel joins them.
 //
 //   warps 0, 1   TMA: pages into a ring of K tiles and one of V tiles, a warp to each
-//   warp 2       tcgen05.mma: S of tile g, then O of tile g - 2
+//   warp 2       tcgen05.mma: S of tile g, then O of tile g - 1
 //   warp 3       queries of the next unit into shared memory
-//   warps 4-11   two groups of 128 threads take tiles in turn: a thread is a slot and makes weights, then a column and sums O in
-//                registers.  Each group has a reference, sums and an O of its own; the one with a unit's last tile joins them
+//   warps 4-11   two groups of 128 threads, half of the rows to each: a thread is a slot and makes its weights, then a column and
+//                sums O in registers
 #pragma once
 #include <cuda.h>
 
@@ -171,12 +171,13 @@ __device__ __forceinline__ int cta_of(const Start& s, int i) {
 template <int NT>
 struct Layout {
   static constexpr int kQ = NT * 256;                // queries of a unit: two halves of NT rows of 128 bytes
-  static constexpr int kP = NT * 256;                // weights of a tile: 128 slots of NT rows, bf16; two make NT x 128 fp32
+  static constexpr int kP = 2 * NT * 256;            // weights of a tile: 128 slots of NT rows, bf16, high and low parts
   static constexpr int kBars = 512;
-  static constexpr int kGroup = 11 * NT;             // words of a group's small arrays
+  static constexpr int kRows = NT / 2;               // of a group
+  static constexpr int kGroup = 11 * kRows;          // words of a group's small arrays
   static constexpr int kSmall = 2 * kGroup * 4 + 128;
-  static constexpr int kFixed = 1024 + 2 * kQ + 4 * kP + kBars + kSmall;
-  static constexpr int kTmem = 8 * NT;               // four S accumulators and two O, of the high and the low parts of the weights
+  static constexpr int kFixed = 1024 + 2 * kQ + 2 * kP + kBars + kSmall;
+  static constexpr int kTmem = 8 * NT;               // two S accumulators and two O, of the high and the low parts of the weights (6 NT)
 };
 constexpr int kMaxSlots = 12;
 
@@ -188,6 +189,9 @@ __device__ __forceinline__ bool any_of_group(int group, bool v) {
   return r != 0;
 }
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync.aligned %0, 128;" ::"r"(group + 1) : "memory"); }
+// The same number in every lane, and known to be.
+__device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 __device__ __forceinline__ float warp_max(float v) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -204,9 +208,12 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
                : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
                  "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[32]) {
-  ptx::tmem_ld_32x32(addr, v);
-  ptx::tmem_ld_wait_for(v);
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[8]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
 }
 
 template <int NT>
@@ -217,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   const uint32_t raw = ptx::smem_u32(smem_raw), pad = (1024u - (raw & 1023u)) & 1023u;
   const uint32_t slot_bytes = p.halves * kHalfBytes;
   // [ring of K][ring of V][queries x 2][weights: two tiles of (high, low)][barriers][small arrays]
-  const uint32_t ring = raw + pad, qbuf = ring + (p.k_slots + p.v_slots) * slot_bytes, pbuf = qbuf + 2 * L::kQ, bars = pbuf + 4 * L::kP;
+  const uint32_t ring = raw + pad, qbuf = ring + (p.k_slots + p.v_slots) * slot_bytes, pbuf = qbuf + 2 * L::kQ, bars = pbuf + 2 * L::kP;
   float* small = reinterpret_cast<float*>(smem_raw + (bars + L::kBars - raw));
   int* misc = reinterpret_cast<int*>(small + 2 * L::kGroup);  // [0..11] scan, [12..18] start, [20] TMEM address, [21] abort flag, [22], [23] the groups'
   Start* start_sh = reinterpret_cast<Start*>(misc + 12);
@@ -229,11 +236,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   auto qfree = [&](int s) { return bar(2 + s); };
   auto pfull = [&](int s) { return bar(4 + s); };
   auto ofull = [&](int s) { return bar(6 + s); };
-  auto xfull = [&](int s) { return bar(8 + s); };
-  auto xfree = [&](int s) { return bar(10 + s); };
-  auto sfull = [&](int s) { return bar(12 + s); };
-  const uint32_t drain = bar(16);
-  static_assert(8 * (2 * kMaxSlots + 17) <= L::kBars, "barriers");
+  auto sfull = [&](int s) { return bar(8 + s); };
+  const uint32_t drain = bar(10);
+  static_assert(8 * (2 * kMaxSlots + 11) <= L::kBars, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint64_t wait_ns = static_cast<uint64_t>(p.wait_limit_us) * 1000ull;
@@ -245,12 +250,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     for (int s = 0; s < 2; ++s) {
       ptx::mbar_init(qfull(s), 32);
       ptx::mbar_init(qfree(s), 1);
-      ptx::mbar_init(pfull(s), 4);       // a lane of each of a group's warps
+      ptx::mbar_init(pfull(s), 8);       // a lane of each of the groups' warps
       ptx::mbar_init(ofull(s), 1);
-      ptx::mbar_init(xfull(s), 4);
-      ptx::mbar_init(xfree(s), 4);
+      ptx::mbar_init(sfull(s), 1);
     }
-    for (int s = 0; s < 4; ++s) ptx::mbar_init(sfull(s), 1);
     ptx::mbar_init(drain, 1);
     misc[21] = misc[22] = misc[23] = 0;
     ptx::fence_mbar_init();
@@ -313,49 +316,64 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       for (int j = it - 1; j >= 0 && j >= it - n; --j) ptx::mbar_wait(full(base + j % n), (j / n) & 1, abort_flag, wait_ns, false);
   } else if (warp == 2) {
     // ------------------------------------------------------------------------------------------ products
-    if (lane == 0) {
-      constexpr uint32_t idesc_s = ptx::make_idesc_bf16(128, NT, 0, 0), idesc_o = ptx::make_idesc_bf16(128, 2 * NT, 1, 0);
-      bool alive = true;
-      int g = 0, unit = 0;
-      auto second = [&](int k) {                 // O of tile k
-        const int s = p.k_slots + k % p.v_slots;
-        if (!ptx::mbar_wait(full(s), (k / p.v_slots) & 1, abort_flag, wait_ns) || !ptx::mbar_wait(pfull(k & 1), (k >> 1) & 1, abort_flag, wait_ns)) return false;
-        ptx::tc_fence_after_sync();
-        const uint32_t v = ring + s * slot_bytes, pw = pbuf + (k & 1) * 2 * L::kP, d = tmem + 4 * NT + (k & 1) * 2 * NT;
+    // The whole warp runs this, in step, with one lane that issues: what the products need is then the same in every lane for the
+    // compiler too and stays in uniform registers.  (With one lane alone in a branch a product took 80 clocks to issue.)
+    constexpr uint32_t idesc_s = ptx::make_idesc_bf16(128, NT, 0, 0), idesc_o = ptx::make_idesc_bf16(128, 2 * NT, 1, 0);
+    const uint32_t one = ptx::elect_one(), d_base = uniform(tmem);
+    const uint64_t k_desc = ptx::make_smem_desc_sw128(ring, 16, 1024), q_desc = ptx::make_smem_desc_sw128(qbuf, 16, 1024);
+    const uint64_t v_desc = ptx::make_smem_desc_sw128(ring + p.k_slots * slot_bytes, kHalfBytes, 1024), p_desc = ptx::make_smem_desc_sw128(pbuf, 16, 1024);
+    int g = 0, unit = 0, ks = 0, vs = 0;
+    uint32_t k_phase = 0, v_phase = 0;
+    bool alive = true;
+    auto ready = [&](uint32_t b, uint32_t phase) {
+      if (!ptx::mbar_wait(b, phase & 1u, abort_flag, wait_ns)) alive = false;
+      alive = __all_sync(0xffffffffu, alive);
+      ptx::tc_fence_after_sync();
+    };
+    auto second = [&](int k) {                 // O of tile k
+      ready(full(p.k_slots + vs), v_phase);
+      ready(pfull(k & 1), k >> 1);
+      if (!alive) return;
+      const uint64_t a = v_desc + vs * (slot_bytes >> 4), w_at = p_desc + (k & 1) * (L::kP >> 4);
+      const uint32_t d = d_base + 2 * NT + (k & 1) * 2 * NT;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          ptx::umma_bf16(d, ptx::make_smem_desc_sw128(v + ks * 2048, kHalfBytes, 1024),
-                         ptx::make_smem_desc_sw128(pw + (ks >> 2) * (2 * NT * 128) + (ks & 3) * 32, 16, 1024), idesc_o, ks != 0);
-        ptx::umma_commit(empty(s));
-        ptx::umma_commit(ofull(k & 1));
-        return true;
-      };
-      while (w.left > 0 && alive) {
-        const int end = w.piece_end();
-        const int qs = unit & 1;
-        const uint32_t qb = qbuf + qs * L::kQ;
-        if (!ptx::mbar_wait(qfull(qs), (unit >> 1) & 1, abort_flag, wait_ns)) { alive = false; break; }
-        for (int t = w.t; t < end; ++t, ++g) {
-          const int s = g % p.k_slots;
-          if (!ptx::mbar_wait(full(s), (g / p.k_slots) & 1, abort_flag, wait_ns)) { alive = false; break; }
-          ptx::tc_fence_after_sync();
-          const uint32_t k = ring + s * slot_bytes;
-          for (int ks = 0; ks < p.ksteps; ++ks)
-            ptx::umma_bf16(tmem + (g & 3) * NT, ptx::make_smem_desc_sw128(k + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
-                           ptx::make_smem_desc_sw128(qb + (ks >> 2) * (NT * 128) + (ks & 3) * 32, 16, 1024), idesc_s, ks != 0);
-          ptx::umma_commit(empty(s));
-          ptx::umma_commit(sfull(g & 3));
-          if (t + 1 == end) ptx::umma_commit(qfree(qs));
-          if (g > 1 && !second(g - 2)) { alive = false; break; }
-        }
-        w.next_unit(p, end - w.t);
-        ++unit;
+      for (int s = 0; s < 8; ++s) ptx::umma_bf16_if(one, d, a + s * (2048 >> 4), w_at + (((s >> 2) * (2 * NT * 128) + (s & 3) * 32) >> 4), idesc_o, s != 0);
+      ptx::umma_commit_if(one, empty(p.k_slots + vs));
+      ptx::umma_commit_if(one, ofull(k & 1));
+      if (++vs == p.v_slots) {
+        vs = 0;
+        v_phase ^= 1u;
       }
-      if (alive && g > 1) alive = second(g - 2);
-      if (alive && g > 0) second(g - 1);
-      ptx::umma_commit(drain);
-      ptx::mbar_wait(drain, 0, abort_flag, wait_ns, false);
+    };
+    int left = uniform(w.left);
+    while (left > 0 && alive) {
+      const int tiles = uniform(w.piece_end() - w.t), qs = unit & 1;
+      ready(qfull(qs), unit >> 1);
+      for (int i = 0; i < tiles && alive; ++i, ++g) {
+        ready(full(ks), k_phase);
+        if (!alive) break;
+        const uint64_t a = k_desc + ks * (slot_bytes >> 4), q_at = q_desc + qs * (L::kQ >> 4);
+        const uint32_t d = d_base + (g & 1) * NT;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+          if (s < p.ksteps)
+            ptx::umma_bf16_if(one, d, a + (((s >> 2) * kHalfBytes + (s & 3) * 32) >> 4), q_at + (((s >> 2) * (NT * 128) + (s & 3) * 32) >> 4), idesc_s, s != 0);
+        ptx::umma_commit_if(one, empty(ks));
+        ptx::umma_commit_if(one, sfull(g & 1));
+        if (i + 1 == tiles) ptx::umma_commit_if(one, qfree(qs));
+        if (++ks == p.k_slots) {
+          ks = 0;
+          k_phase ^= 1u;
+        }
+        if (g > 0) second(g - 1);
+      }
+      w.next_unit(p, tiles);
+      left = uniform(w.left);
+      ++unit;
     }
+    if (alive && g > 0) second(g - 1);
+    ptx::umma_commit_if(one, drain);
+    ptx::mbar_wait(drain, 0, abort_flag, wait_ns, false);
   } else if (warp == 3) {
     // ------------------------------------------------------------------------------------------ queries
     bool alive = true;
@@ -392,206 +410,187 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     }
   } else {
     // ------------------------------------------------------------------------------------------ weights and sums
+    constexpr int R = L::kRows;
     const int group = (warp - 4) >> 2, quarter = warp & 3, x = quarter * 32 + lane;      // slot of the tile, and column of the head
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t p_mine = pbuf + group * 2 * L::kP;
-    const uint32_t p_at = p_mine + (x >> 6) * (2 * NT * 128) + (x & 7) * 2;  // of row 0, without its swizzle; rows NT .. 2 NT - 1 are the low parts
-    const uint32_t chunk = (x & 63) >> 3;
-    int* bound = reinterpret_cast<int*>(small + group * L::kGroup);          // [NT] slots that a row sees
-    float* wmax = small + group * L::kGroup + NT;                            // [4][NT] the warps' maxima
-    float* ref = wmax + 4 * NT;                                              // [NT]
-    float* alpha = ref + NT;                                                 // [NT]
-    float* lsum = alpha + NT;                                                // [4][NT]
+    // of this group's first row, without its swizzle; rows NT .. 2 NT - 1 are the low parts
+    const uint32_t p_at = pbuf + (x >> 6) * (2 * NT * 128) + group * R * 128 + (x & 7) * 2, chunk = (x & 63) >> 3;
+    float* wmax = small + group * L::kGroup;                                 // [4][R] the warps' maxima
+    float* lsum = wmax + 4 * R;                                              // [4][R]
+    float* ref = lsum + 4 * R;                                               // [R]
+    float* alpha = ref + R;                                                  // [R]
+    int* bound = reinterpret_cast<int*>(alpha + R);                          // [R] slots that a row sees
     volatile int* group_abort = misc + 22 + group;
-    float o[NT], l[NT];
-    int g = 0, flat = start.first, given = 0, taken = 0;        // units that this group has given to the other, and taken from it
+    float o[R], l[R];
+    int g = 0, flat = start.first;
     auto fail = [&] { *abort_flag = 1; *group_abort = 1; };
     auto wait = [&](uint32_t b, int phase) {
       if (!ptx::mbar_wait(b, phase & 1, abort_flag, wait_ns, false)) fail();
       __syncwarp();
     };
-    auto arrive = [&](uint32_t b) {
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(b);
+    auto read_row = [&](const float* from, float (&to)[R]) {
+#pragma unroll
+      for (int r = 0; r < R; r += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(from + r);
+        to[r] = q.x; to[r + 1] = q.y; to[r + 2] = q.z; to[r + 3] = q.w;
+      }
     };
     auto add_o = [&](int k) {                    // O of tile k
-      wait(ofull(group), k >> 1);
+      wait(ofull(k & 1), k >> 1);
       ptx::tc_fence_after_sync();
 #pragma unroll
       for (int low = 0; low < 2; ++low) {
-        float v[NT];
-        tmem_load(tmem + lanes + 4 * NT + (2 * group + low) * NT, v);
+        float v[R];
+        tmem_load(tmem + lanes + 2 * NT + (2 * (k & 1) + low) * NT + group * R, v);
 #pragma unroll
-        for (int r = 0; r < NT; ++r) o[r] += v[r];
+        for (int r = 0; r < R; ++r) o[r] += v[r];
       }
     };
     bool alive = true;
     while (w.left > 0) {
       const int end = w.piece_end(), begin = w.t, tiles = end - begin;
-      const int u_chunks = (w.q.fresh * p.G + NT - 1) / NT, h = w.u / u_chunks, chunk_no = w.u % u_chunks;
-      const int rows = min(NT, w.q.fresh * p.G - chunk_no * NT);
-      const long long unit_at = (static_cast<long long>(w.b) * p.c.H + h) * p.chunks + chunk_no;
+      const int u_chunks = (w.q.fresh * p.G + NT - 1) / NT, h = w.u / u_chunks, row0 = (w.u % u_chunks) * NT + group * R;
+      const int rows = min(R, w.q.fresh * p.G - row0);          // of this group; none: it keeps in step, and its weights are not looked at
+      const long long unit_at = (static_cast<long long>(w.b) * p.c.H + h) * p.chunks + w.u % u_chunks;
       const int len = w.q.len, sure = len - (w.q.fresh - 1);    // every row sees the slots below `sure`
-      const bool finish = ((g + tiles - 1) & 1) == group;       // this group has the last tile
-      if (finish && begin == 0 && x == 0) p.unit_ctas[unit_at] = make_int2(blockIdx.x, cta_of(start, flat + w.q.tiles - 1));
+      if (group == 0 && begin == 0 && x == 0) p.unit_ctas[unit_at] = make_int2(blockIdx.x, cta_of(start, flat + w.q.tiles - 1));
       if (end * kTile > sure) {
-        if (x < NT) bound[x] = x < rows ? len - (w.q.fresh - 1 - (chunk_no * NT + x) / p.G) : len;
+        if (x < R) bound[x] = x < rows ? len - (w.q.fresh - 1 - (row0 + x) / p.G) : len;
         group_sync(group);
       }
 #pragma unroll
-      for (int r = 0; r < NT; ++r) o[r] = l[r] = 0.f;
-      bool first = true;
-      for (int k = g + ((g & 1) != group); k < g + tiles; k += 2) {
-        const int t = begin + (k - g), slot = t * kTile + x;
-        const bool masked = (t + 1) * kTile > sure;
-        wait(sfull(k & 3), k >> 2);
+      for (int r = 0; r < R; ++r) o[r] = l[r] = 0.f;
+      for (int t = begin; t < end; ++t, ++g) {
+        const int slot = t * kTile + x;
+        const bool masked = (t + 1) * kTile > sure, first = t == begin;
+        wait(sfull(g & 1), g >> 1);
         ptx::tc_fence_after_sync();
-        float v[NT];
-        tmem_load(tmem + lanes + (k & 3) * NT, v);
+        bool rise = false;
+        float v[R], rf[R];
+        if (rows > 0) {
+          tmem_load(tmem + lanes + (g & 1) * NT + group * R, v);
 #pragma unroll
-        for (int r = 0; r < NT; ++r) v[r] *= p.scale2;
-        if (masked) {
+          for (int r = 0; r < R; ++r) v[r] *= p.scale2;
+          if (masked) {
 #pragma unroll
-          for (int r = 0; r < NT; ++r) v[r] = slot < bound[r] ? v[r] : -INFINITY;
-        }
-        if (p.scores != nullptr) {
-          float* to = p.scores + (unit_at * p.tiles + t) * NT * kTile + x;
+            for (int r = 0; r < R; ++r) v[r] = slot < bound[r] ? v[r] : -INFINITY;
+          }
+          if (p.scores != nullptr) {
+            float* to = p.scores + ((unit_at * p.tiles + t) * NT + group * R) * kTile + x;
 #pragma unroll
-          for (int r = 0; r < NT; ++r)
-            if (r < rows) to[r * kTile] = v[r];
-        }
-        bool rise = first;
-        if (!first) {
+            for (int r = 0; r < R; ++r)
+              if (r < rows) to[r * kTile] = v[r];
+          }
+          read_row(ref, rf);
+          rise = first;
+          if (!first) {
 #pragma unroll
-          for (int r = 0; r < NT; ++r) rise |= v[r] > ref[r] + kSlack;
+            for (int r = 0; r < R; ++r) rise |= v[r] > rf[r] + kSlack;
+          }
         }
         rise = any_of_group(group, rise);
         if (*group_abort) { alive = false; break; }
-        if (first && given > 0) wait(xfree(group), given - 1);       // the other group has read what this one left
-        if (rise) {
-          float top = 0.f;
+        if (rows > 0) {
+          if (rise) {
+            float top = 0.f;
 #pragma unroll
-          for (int r = 0; r < NT; ++r) {
-            const float m = warp_max(v[r]);
-            if (lane == r) top = m;
-          }
-          if (lane < NT) wmax[quarter * NT + lane] = top;
-          group_sync(group);
-          if (x < NT) {
-            const float old = first ? kNone : ref[x];
-            const float m = fmaxf(fmaxf(fmaxf(wmax[x], wmax[NT + x]), fmaxf(wmax[2 * NT + x], wmax[3 * NT + x])), old);
-            ref[x] = m;
-            alpha[x] = ptx::ex2_approx(old - m);
-          }
-          group_sync(group);
-        }
-        if (!first) add_o(k - 2);                // (and then the weights' buffer is free)
-        if (rise) {
+            for (int r = 0; r < R; ++r) {
+              const float m = warp_max(v[r]);
+              if (lane == r) top = m;
+            }
+            if (lane < R) wmax[quarter * R + lane] = top;
+            group_sync(group);
+            if (x < R) {
+              const float old = first ? kNone : ref[x];
+              const float m = fmaxf(fmaxf(fmaxf(wmax[x], wmax[R + x]), fmaxf(wmax[2 * R + x], wmax[3 * R + x])), old);
+              ref[x] = m;
+              alpha[x] = ptx::ex2_approx(old - m);
+            }
+            group_sync(group);
+            read_row(ref, rf);
+            float f[R];
+            read_row(alpha, f);
 #pragma unroll
-          for (int r = 0; r < NT; ++r) {
-            const float f = alpha[r];
-            l[r] *= f;
-            o[r] *= f;
+            for (int r = 0; r < R; ++r) l[r] *= f[r];
+          }
+          const uint32_t to = p_at + (g & 1) * L::kP;
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float e = ptx::ex2_approx(v[r] - rf[r]);
+            l[r] += e;
+            // as the sum of two bf16: one would add its own rounding, 2^-9 of a weight, to that of the output
+            const uint32_t hi = ptx::pack_bf16x2(e, 0.f);
+            const uint32_t lo = ptx::pack_bf16x2(e - ptx::bf16_lo(hi), 0.f);
+            const uint32_t at = to + r * 128 + ((chunk ^ (r & 7)) << 4);
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(hi)));
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + NT * 128), "h"(static_cast<uint16_t>(lo)));
           }
         }
-        first = false;
-#pragma unroll
-        for (int r = 0; r < NT; ++r) {
-          const float e = ptx::ex2_approx(v[r] - ref[r]);
-          l[r] += e;
-          // as the sum of two bf16: one would add its own rounding, 2^-9 of a weight, to that of the output
-          const uint32_t hi = ptx::pack_bf16x2(e, 0.f);
-          const uint32_t lo = ptx::pack_bf16x2(e - ptx::bf16_lo(hi), 0.f);
-          const uint32_t at = p_at + r * 128 + ((chunk ^ (r & 7)) << 4);
-          asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(hi)) : "memory");
-          asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + NT * 128), "h"(static_cast<uint16_t>(lo)) : "memory");
-        }
-        if ((t + 1) * kTile > len) {
+        if ((t + 1) * kTile > len && group < p.halves) {
           // rows of V that no slot of the sequence fills: whatever lies there must not meet a weight of zero
-          const int s = p.k_slots + k % p.v_slots;
-          wait(full(s), k / p.v_slots);
+          const int s = p.k_slots + g % p.v_slots;
+          wait(full(s), g / p.v_slots);
           if (slot >= len)
-            for (int i = 0; i < 8 * p.halves; ++i)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + s * slot_bytes + (i >> 3) * kHalfBytes + x * 128 + (i & 7) * 16), "r"(0) : "memory");
+            for (int half = group; half < p.halves; half += 2)
+              for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + s * slot_bytes + half * kHalfBytes + x * 128 + i * 16), "r"(0) : "memory");
         }
         ptx::tc_fence_before_sync();
         ptx::fence_proxy_async_smem();
-        arrive(pfull(group));
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(pfull(g & 1));
+        if (rows > 0) {
+          if (!first) add_o(g - 1);
+          if (rise) {
+            float f[R];
+            read_row(alpha, f);
+#pragma unroll
+            for (int r = 0; r < R; ++r) o[r] *= f[r];
+          }
+        } else if (!first) {
+          wait(ofull((g - 1) & 1), (g - 1) >> 1);
+        }
       }
       if (!alive) break;
-      const int last = g + tiles - 1 - (finish ? 0 : 1);         // this group's last tile, if it had one
-      if (last >= g) {
-        add_o(last);
+      if (rows > 0) {
+        add_o(g - 1);
         // sums over the slots' threads
         float mine = 0.f;
 #pragma unroll
-        for (int r = 0; r < NT; ++r) {
+        for (int r = 0; r < R; ++r) {
           const float sum = io::sum_lanes(l[r]);
           if (lane == r) mine = sum;
         }
-        if (lane < NT) lsum[quarter * NT + lane] = mine;
-        if (!finish) {
-          // to the other group, in the place of this one's weights
-#pragma unroll
-          for (int r = 0; r < NT; ++r) asm volatile("st.shared.f32 [%0], %1;" ::"r"(p_mine + (r * 128 + x) * 4), "f"(o[r]) : "memory");
-          arrive(xfull(group));
-          ++given;
-        }
-      }
-      if (finish) {
+        if (lane < R) lsum[quarter * R + lane] = mine;
         group_sync(group);
-        float mine = x < NT ? (lsum[x] + lsum[NT + x]) + (lsum[2 * NT + x] + lsum[3 * NT + x]) : 0.f;
-        float at_ref = x < NT ? ref[x] : 0.f;
-        if (tiles > 1) {
-          wait(xfull(group ^ 1), taken);
-          ++taken;
-          const float* theirs = small + (group ^ 1) * L::kGroup;                  // (the other group's arrays, laid out as these)
-          const float *their_ref = theirs + 5 * NT, *their_sum = theirs + 7 * NT;
-          float* f_mine = wmax;                                                    // [NT] factors, and those of the other's
-          float* f_theirs = wmax + NT;
-          if (x < NT) {
-            const float m = fmaxf(at_ref, their_ref[x]), a = ptx::ex2_approx(at_ref - m), b = ptx::ex2_approx(their_ref[x] - m);
-            f_mine[x] = a;
-            f_theirs[x] = b;
-            mine = mine * a + ((their_sum[x] + their_sum[NT + x]) + (their_sum[2 * NT + x] + their_sum[3 * NT + x])) * b;
-            at_ref = m;
-          }
-          group_sync(group);
-#pragma unroll
-          for (int r = 0; r < NT; ++r) {
-            float v;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(pbuf + (group ^ 1) * 2 * L::kP + (r * 128 + x) * 4));
-            o[r] = o[r] * f_mine[r] + v * f_theirs[r];
-          }
-          arrive(xfree(group ^ 1));
-        }
+        mine = x < R ? (lsum[x] + lsum[R + x]) + (lsum[2 * R + x] + lsum[3 * R + x]) : 0.f;
         if (begin == 0 && end == w.q.tiles) {
-          float* sums = wmax + 2 * NT;
-          if (x < NT) sums[x] = mine;
-          group_sync(group);
           bf16_t* out = static_cast<bf16_t*>(p.a.out.data) + w.b * p.a.out.seq + x;
+          if (x < p.c.D) {
 #pragma unroll
-          for (int r = 0; r < NT; ++r)
-            if (r < rows) {
-              const float sum = sums[r];
-              const int row = chunk_no * NT + r;
-              if (x < p.c.D) out[(row / p.G) * p.a.out.token + (h * p.G + row % p.G) * p.a.out.head] = io::from_f<bf16_t>(sum == 0.f ? 0.f : __fdividef(o[r], sum));
-            }
+            for (int r = 0; r < R; ++r)
+              if (r < rows) {
+                const float sum = (lsum[r] + lsum[R + r]) + (lsum[2 * R + r] + lsum[3 * R + r]);
+                const int row = row0 + r;
+                out[(row / p.G) * p.a.out.token + (h * p.G + row % p.G) * p.a.out.head] = io::from_f<bf16_t>(sum == 0.f ? 0.f : __fdividef(o[r], sum));
+              }
+          }
           if (x < rows) {
-            const int row = chunk_no * NT + x;
+            const int row = row0 + x;
             if (p.a.lse != nullptr)
-              p.a.lse[(static_cast<long long>(w.b) * p.s.Q + row / p.G) * p.a.Hq + h * p.G + row % p.G] = mine == 0.f ? -INFINITY : (at_ref + log2f(mine)) * kLn2;
-            if (p.scores != nullptr) p.whole_ml[unit_at * NT + x] = make_float2(at_ref, mine);
+              p.a.lse[(static_cast<long long>(w.b) * p.s.Q + row / p.G) * p.a.Hq + h * p.G + row % p.G] = mine == 0.f ? -INFINITY : (ref[x] + log2f(mine)) * kLn2;
+            if (p.scores != nullptr) p.whole_ml[unit_at * NT + group * R + x] = make_float2(ref[x], mine);
           }
         } else {
-          const long long at = (blockIdx.x * 2 + (begin == 0 ? 1 : 0)) * NT;
+          const long long at = (blockIdx.x * 2 + (begin == 0 ? 1 : 0)) * NT + group * R;
 #pragma unroll
-          for (int r = 0; r < NT; ++r)
+          for (int r = 0; r < R; ++r)
             if (r < rows) p.part_o[(at + r) * 128 + x] = o[r];
-          if (x < NT) p.part_ml[at + x] = make_float2(at_ref, mine);
+          if (x < rows) p.part_ml[at + x] = make_float2(ref[x], mine);
         }
+      } else {
+        wait(ofull((g - 1) & 1), (g - 1) >> 1);
       }
-      g += tiles;
       flat += tiles;
       w.next_unit(p, tiles);
     }
