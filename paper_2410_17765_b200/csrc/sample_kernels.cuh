@@ -1,5 +1,15 @@
 // Sampling from logits with temperature, top-k, top-p and min-p by given uniform numbers.
+//
+// A row is held by the shared memory of a cluster, read once.  Its weights w = 2^z, z = (x - m) log2(e) / T, are integers (62 - log2 V
+// bits below the point) whose sums are exact in any order, so borders between kept and dropped entries, and the token that a number
+// draws, do not depend on how the row is shared out.  Where a filter ends is found in two steps: a histogram over z in steps of 1/64
+// names the few bins in which it lies, and their entries, a few hundred of 128256, are sorted in one block.  Should they be too many (long
+// runs of equal logits, flat rows), the key of the last kept entry is found by digits instead.
+//
+// What bounds it: at many rows the instructions, about 30 for a weight and 8 for its bin, each entry once or twice; at few rows the
+// latency of a dozen barriers of a cluster.
 #pragma once
+#include <cfloat>
 #include <cstdint>
 
 #include "../../include/cpmtp.h"
@@ -11,225 +21,795 @@ namespace sample {
 
 using io::bf16_t;
 typedef unsigned long long u64;
-constexpr int kThreads = 1024;
-constexpr int kWarps = kThreads / 32;
 
-struct Row {
-  double inv_t, top_p, min_p;
-  int top_k;
-  bool greedy;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMostCtas = 8;
+constexpr int kBins = 2048;            // of the histogram, 64 to a factor of two
+constexpr int kList = 2048;            // entries that one block sorts
+constexpr int kTable = 1024;           // powers of two between one and two
+
+struct Shared {
+  u64 table[kTable];
+  u64 list[kList];
+  union {
+    uint32_t hist[kBins];
+    struct {
+      u64 mass[256];
+      uint32_t count[256];
+    } digit;
+  };
+  double scan[kWarps];
+  u64 sums[kWarps];                    // kept mass of the warps' ranges
+  u64 box[8][kMostCtas];               // numbers from the blocks of the cluster; a place in turn
+  u64 word[4];
+  int listed, number[3];
 };
-__device__ __forceinline__ Row row_settings(const cpmtp_sample_args& a, int i) {
-  Row r;
-  const float t = a.temperatures != nullptr ? a.temperatures[i] : a.temperature;
-  r.greedy = !(t > 0.f);
-  r.inv_t = r.greedy ? 1.0 : 1.0 / static_cast<double>(t);
-  const float p = a.top_ps != nullptr ? a.top_ps[i] : a.top_p, mp = a.min_ps != nullptr ? a.min_ps[i] : a.min_p;
-  r.top_p = p < 1.f ? static_cast<double>(p) : 1.0;
-  r.min_p = mp > 0.f ? static_cast<double>(mp) : 0.0;
-  const int k = a.top_ks != nullptr ? a.top_ks[i] : a.top_k;
-  r.top_k = k > 0 && k < a.V ? k : a.V;
-  if (r.greedy || r.min_p > 1.0) r.top_k = 1;
+
+static_assert(sizeof(Shared) % 16 == 0, "the row's entries follow");
+
+// -------------------------------------------------------------------------------------------- cluster
+__device__ __forceinline__ void sync_row(int ctas) {
+  if (ctas == 1) {
+    __syncthreads();
+  } else {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+}
+__device__ __forceinline__ uint32_t remote(const void* p, int cta) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(ptx::smem_u32(p)), "r"(cta));
   return r;
 }
+__device__ __forceinline__ void store_remote(const void* p, int cta, u64 v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(p, cta)), "l"(v) : "memory");
+}
+__device__ __forceinline__ u64 load_remote64(const void* p, int cta) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, cta)) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t load_remote32(const void* p, int cta) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote(p, cta)) : "memory");
+  return v;
+}
 
-// Unsigned keys in the order of the logits; 0: an entry that is never kept (-infinity, NaN).
+// -------------------------------------------------------------------------------------------- keys and weights
+// Unsigned keys in the order of the logits.
 __device__ __forceinline__ uint32_t logit_key(float x) {
-  if (!(x > -INFINITY)) return 0;
   const uint32_t u = __float_as_uint(x + 0.f);     // (-0 as +0)
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-// exp((x - m) / T), and as an integer
-__device__ __forceinline__ double z_of(float x, float m, double inv_t) { return x == m ? 0.0 : (static_cast<double>(x) - static_cast<double>(m)) * inv_t; }
-__device__ __forceinline__ u64 fixed(double w, double unit) { return static_cast<u64>(w * unit); }
+constexpr long long kNoWeight = -(60ll << 32);       // z of entries that have none
 
-template <class Op>
-__device__ __forceinline__ u64 block_all(u64 v, u64* sh, Op op) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  u64 r = sh[0];
-  for (int w = 1; w < kWarps; ++w) r = op(r, sh[w]);
+struct Weigh {
+  double m, c;           // largest logit; log2(e) / T
+  float mf, cf;
+  bool inf;              // the largest logit is infinite
+  int down;              // 62 minus the bits below the point
+  const u64* table;
+
+  // (x - m) c with 32 bits below the point: the product is added to a number whose last bit is 2^-32.
+  __device__ __forceinline__ long long z(float x) const {
+    if (inf) return x == INFINITY ? 0 : kNoWeight;
+    const float about = (x - mf) * cf;
+    constexpr double kMagic = 1572864.0;               // 1.5 x 2^20
+    const long long v = __double_as_longlong(fma(static_cast<double>(x) - m, c, kMagic)) - 0x4138000000000000ll;
+    return about > -60.f ? v : kNoWeight;
+  }
+  // 2^(z - floor(z)) with 62 bits below the point.  The leading ten bits by table, the others by three terms of the series of
+  // 2^r - 1, r < 2^-10, in fp32: an error of 2^-24 of a number below 2^-10.5.  With the 2^-33 of z and the 2^-34 of its own
+  // rounding below 2^-32 in all.
+  __device__ __forceinline__ u64 mantissa(long long z) const {
+    const uint32_t f = static_cast<uint32_t>(z);
+    const u64 t = table[f >> 22];
+    const float r = __uint_as_float(0x3f800000u | (f & 0x3fffffu) << 1) - 1.f;           // in units of 2^-10
+    constexpr double kA = 0.69314718055994530942 / 1024.0, kS = 8589934592.0;            // ln 2 2^-10; 2^33
+    const float q = fmaf(r, fmaf(r, static_cast<float>(kA * kA * kA / 6.0 * kS), static_cast<float>(kA * kA / 2.0 * kS)), static_cast<float>(kA * kS));
+    const uint32_t n = __float_as_uint(fmaf(r, q, 8388608.f)) & 0x7fffffu;
+    return t + ((static_cast<u64>(static_cast<uint32_t>(t >> 32)) * n) >> 1);
+  }
+  __device__ __forceinline__ u64 fixed(u64 mantissa, long long z) const {
+    const int s = down - static_cast<int>(z >> 32);
+    return s < 64 ? mantissa >> s : 0;
+  }
+  __device__ __forceinline__ u64 weight(long long z) const { return fixed(mantissa(z), z); }
+};
+
+struct Settings {
+  double inv_t, top_p, min_p;
+  int top_k;             // V: none
+  bool one;              // the first entry alone is kept
+};
+__device__ __forceinline__ Settings settings_of(const cpmtp_sample_args& a, int i) {
+  Settings r;
+  const float t = a.temperatures != nullptr ? a.temperatures[i] : a.temperature;
+  const float p = a.top_ps != nullptr ? a.top_ps[i] : a.top_p, mp = a.min_ps != nullptr ? a.min_ps[i] : a.min_p;
+  const int k = a.top_ks != nullptr ? a.top_ks[i] : a.top_k;
+  r.inv_t = t > 0.f ? 1.0 / static_cast<double>(t) : 1.0;
+  r.top_p = p < 1.f ? static_cast<double>(p) : 1.0;
+  r.min_p = mp > 0.f ? static_cast<double>(mp) : 0.0;
+  r.top_k = k > 0 && k < a.V ? k : a.V;
+  r.one = !(t > 0.f) || r.top_p <= 0.0 || r.min_p > 1.0 || r.top_k == 1;
   return r;
 }
-__device__ __forceinline__ u64 block_sum(u64 v, u64* sh) { return block_all(v, sh, [](u64 a, u64 b) { return a + b; }); }
 
-// One block to a row, several passes over it.
-template <class T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant__ cpmtp_sample_args a, double unit, int* dev_status) {
-  __shared__ u64 sh[kWarps];
-  __shared__ u64 mass[256];
-  __shared__ int count[256];
-  __shared__ uint32_t sh_key;
-  __shared__ int sh_need, sh_token, sh_ties[kWarps];
-  __shared__ u64 sh_above;
-  ptx::grid_dep_wait();
-  const int i = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5, V = a.V;
-  const T* x = static_cast<const T*>(a.logits) + i * a.ld;
-  const Row r = row_settings(a, i);
-  auto key = [&](int v) { return logit_key(io::to_f(x[v])); };
+// -------------------------------------------------------------------------------------------- the kernel
+// A cluster of `ctas` blocks to a row; a block has `span` entries of it, its warps equal ranges of those.  HELD: in shared memory.
+template <class T, bool HELD>
+struct Row {
+  const cpmtp_sample_args& a;
+  Shared& sh;
+  const int ctas, rank, t, lane, warp;
+  int base, n;           // this block's entries
+  int w0, w1;            // this warp's, among them
+  const T* x;
+  int boxes;
 
-  uint32_t top = 0;
-  for (int v = t; v < V; v += kThreads) top = max(top, key(v));
-  top = static_cast<uint32_t>(block_all(top, sh, [](u64 p, u64 q) { return p > q ? p : q; }));
-  const int given = a.given != nullptr ? a.given[i] : CPMTP_EMBED_PAD;
-  if (t == 0 && given != CPMTP_EMBED_PAD && (given < 0 || given >= V) && dev_status != nullptr) atomicMax(dev_status, 1);
-  if (top == 0) {
-    if (t == 0) {
-      a.tokens[i] = -1;
-      if (a.logp != nullptr) a.logp[i] = -INFINITY;
-      if (a.kept != nullptr) a.kept[i] = 0;
-      if (a.given != nullptr) a.logp_given[i] = -INFINITY;
-    }
-    return;
+  __device__ __forceinline__ float at(int i) const { return io::to_f(x[i]); }
+  __device__ __forceinline__ void sync() const { sync_row(ctas); }
+
+  // Sums over the block's threads, in every thread.
+  __device__ __forceinline__ u64 block_sum(u64 v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    u64* part = reinterpret_cast<u64*>(sh.scan);
+    if (lane == 0) part[warp] = v;
+    __syncthreads();
+    v = lane < kWarps ? part[lane] : 0;
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return __shfl_sync(0xffffffffu, v, 0);
   }
-  const float m = key_logit(top);
-  auto weight = [&](uint32_t k) { return exp(z_of(key_logit(k), m, r.inv_t)); };
+  // Gives `v` (of thread 0) to every block and brings theirs: box[r] of block r.  A barrier of the cluster.
+  __device__ __forceinline__ const u64* exchange(u64 v) {
+    u64* box = sh.box[boxes++ & 7];
+    if (ctas == 1) {
+      if (t == 0) box[0] = v;
+      __syncthreads();
+    } else {
+      v = __shfl_sync(0xffffffffu, v, 0);
+      if (t < ctas) store_remote(box + rank, t, v);
+      sync();
+    }
+    return box;
+  }
+  __device__ __forceinline__ u64 row_sum(u64 v) {
+    const u64* box = exchange(block_sum(v));
+    u64 s = 0;
+    for (int r = 0; r < ctas; ++r) s += box[r];
+    return s;
+  }
 
-  // The key of the last entry that a filter keeps, and how many of the entries with that key: by their number (what = 0) or their mass (1).
-  uint32_t floor_key = 0;
-  int floor_need = 0;                      // entries with key floor_key that are kept
-  u64 total = 0;                           // mass of the entries kept so far
-  auto find = [&](bool by_mass, u64 want, uint32_t low, int low_need) {
+  // First and second bin at which the running sum of the histogram, bin b weighing scale(b), reaches `low` and `high`, and what lies
+  // before the first; the last bin where they are not reached.
+  template <class Scale>
+  __device__ __forceinline__ void find_bins(Scale scale, double low, double high, int& b1, int& b2, double& before) {
+    sync();                                            // the blocks' histograms are complete
+    const int per = kBins / ctas, each = (per + kThreads - 1) / kThreads;       // bins of this block, of a thread
+    double mine[kBins / kThreads], sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < kBins / kThreads; ++j) {
+      mine[j] = 0.0;
+      const int b = t * each + j;
+      if (j < each && b < per) {
+        u64 c = 0;
+        for (int r = 0; r < ctas; ++r) c += ctas == 1 ? sh.hist[b] : load_remote32(&sh.hist[rank * per + b], r);
+        mine[j] = static_cast<double>(c) * scale(rank * per + b);
+        sum += mine[j];
+      }
+    }
+    double upto = sum;                                 // of this thread's bins and those before them in the warp
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    __syncthreads();
+    if (lane == 31) sh.scan[warp] = upto;
+    if (t == 0) {
+      sh.number[0] = sh.number[1] = kBins - 1;
+      sh.word[0] = 0;
+    }
+    __syncthreads();
+    double all = 0.0;
+    for (int w = 0; w < kWarps; ++w) all += sh.scan[w];
+    const u64* box = exchange(__double_as_longlong(all));
+    double run = 0.0;
+    for (int r = 0; r < rank; ++r) run += __longlong_as_double(box[r]);
+    for (int w = 0; w < warp; ++w) run += sh.scan[w];
+    // a thread begins with the very number that the one before it ends with, so that no border falls between them
+    upto += run;
+    const double left = __shfl_up_sync(0xffffffffu, upto, 1);
+    if (lane > 0) run = left;
+#pragma unroll
+    for (int j = 0; j < kBins / kThreads; ++j) {
+      const double next = j + 1 == each ? upto : run + mine[j];
+      const int b = rank * per + t * each + j;
+      if (j < each && t * each + j < per) {
+        if (run < low && next >= low)
+          for (int r = 0; r < ctas; ++r) {
+            store_remote(&sh.word[0], r, __double_as_longlong(run));
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(&sh.number[0], r)), "r"(b) : "memory");
+          }
+        if (run < high && next >= high)
+          for (int r = 0; r < ctas; ++r) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(&sh.number[1], r)), "r"(b) : "memory");
+      }
+      run = next;
+    }
+    sync();
+    b1 = sh.number[0];
+    b2 = sh.number[1];
+    before = __longlong_as_double(sh.word[0]);
+  }
+
+  __device__ __forceinline__ void clear_hist() {
+    for (int b = t; b < kBins; b += kThreads) sh.hist[b] = 0;
+    if (t == 0) sh.listed = 0;
+    __syncthreads();
+  }
+
+  // Entries (logit, index) as keys that sort in falling order of the logit and rising order of the index.
+  static __device__ __forceinline__ u64 entry(float x, int index) { return static_cast<u64>(logit_key(x)) << 32 | static_cast<uint32_t>(~index); }
+  static __device__ __forceinline__ float entry_logit(u64 e) { return key_logit(static_cast<uint32_t>(e >> 32)); }
+  static __device__ __forceinline__ int entry_index(u64 e) { return static_cast<int>(~static_cast<uint32_t>(e)); }
+
+  // Adds to the block's list the entries of lanes that have `take`.
+  __device__ __forceinline__ void list_add(bool take, float v, int index) {
+    const uint32_t lanes = __ballot_sync(0xffffffffu, take);
+    if (lanes == 0) return;
+    int place = 0;
+    if (lane == 0) place = atomicAdd(&sh.listed, __popc(lanes));
+    place = __shfl_sync(0xffffffffu, place, 0) + __popc(lanes & ((1u << lane) - 1));
+    if (take && place < kList) sh.list[place] = entry(v, index);
+  }
+
+  // All blocks' lists in block 0's, and their length in every block; more than kList: not gathered.
+  __device__ __forceinline__ int gather_list() {
+    __syncthreads();
+    const u64* box = exchange(sh.listed);
+    int total = 0;
+    for (int r = 0; r < ctas; ++r) total += static_cast<int>(box[r]);
+    if (ctas > 1 && total <= kList) {
+      if (rank == 0) {
+        int to = static_cast<int>(box[0]);
+        for (int r = 1; r < ctas; ++r) {
+          const int c = static_cast<int>(box[r]);
+          for (int i = t; i < c; i += kThreads) sh.list[to + i] = load_remote64(&sh.list[i], r);
+          to += c;
+        }
+      }
+    }
+    return total;
+  }
+  // Sorts the first `count` keys of this block's list, falling.
+  __device__ __forceinline__ void sort_list(int count) {
+    int size = 2;
+    while (size < count) size *= 2;
+    __syncthreads();
+    for (int i = count + t; i < size; i += kThreads) sh.list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+      for (int j = k / 2; j > 0; j /= 2) {
+        for (int p = t; p < size / 2; p += kThreads) {
+          const int i = 2 * p - (p & (j - 1)), o = i + j;
+          const u64 u = sh.list[i], v = sh.list[o];
+          if ((u < v) == ((i & k) == 0)) {
+            sh.list[i] = v;
+            sh.list[o] = u;
+          }
+        }
+        __syncthreads();
+      }
+  }
+  // Running sums over the block of four numbers to a thread, those of entries 4 t .. 4 t + 3: v becomes the sum up to and with itself.
+  __device__ __forceinline__ void scan4(u64 (&v)[4]) {
+#pragma unroll
+    for (int j = 1; j < 4; ++j) v[j] += v[j - 1];
+    u64 upto = v[3];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 u = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += u;
+    }
+    u64* part = reinterpret_cast<u64*>(sh.scan);
+    __syncthreads();
+    if (lane == 31) part[warp] = upto;
+    __syncthreads();
+    u64 before = upto - v[3];
+    for (int w = 0; w < warp; ++w) before += part[w];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += before;
+  }
+
+  // Index of the first entry at which the running sum of f over the row exceeds `target`; sh.sums has the warps' sums of f.
+  template <class F>
+  __device__ __forceinline__ int locate(F f, u64 target) {
+    __syncthreads();
+    u64 mine = lane < kWarps ? sh.sums[lane] : 0;
+    u64 upto = mine;
+#pragma unroll
+    for (int o = 1; o < kWarps; o <<= 1) {
+      const u64 v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const u64* box = exchange(__shfl_sync(0xffffffffu, upto, kWarps - 1));
+    u64 before = 0;
+    for (int r = 0; r < rank; ++r) before += box[r];
+    if (t == 0) sh.number[2] = -1;
+    __syncthreads();
+    const u64 here = before + __shfl_sync(0xffffffffu, upto - mine, warp), end = here + __shfl_sync(0xffffffffu, mine, warp);
+    if (here <= target && target < end) {
+      // a lane's share first (an odd number of entries, so that the lanes are in different banks), then the entries of one
+      const int share = ((w1 - w0 + 31) / 32) | 1;
+      int i0 = min(w0 + lane * share, w1), i1 = min(i0 + share, w1);
+      u64 sum = 0;
+      for (int i = i0; i < i1; ++i) sum += f(at(i), base + i);
+      u64 run = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 v = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += v;
+      }
+      const int who = __ffs(__ballot_sync(0xffffffffu, here + run > target)) - 1;
+      u64 low = here + __shfl_sync(0xffffffffu, run - sum, who);
+      i0 = __shfl_sync(0xffffffffu, i0, who);
+      i1 = __shfl_sync(0xffffffffu, i1, who);
+      for (int i = i0; i < i1; i += 32) {
+        u64 v = i + lane < i1 ? f(at(i + lane), base + i + lane) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const u64 u = __shfl_up_sync(0xffffffffu, v, o);
+          if (lane >= o) v += u;
+        }
+        const uint32_t over = __ballot_sync(0xffffffffu, low + v > target);
+        if (over != 0) {
+          if (lane == 0) sh.number[2] = base + i + __ffs(over) - 1;
+          break;
+        }
+        low += __shfl_sync(0xffffffffu, v, 31);
+      }
+    }
+    __syncthreads();
+    box = exchange(static_cast<u64>(static_cast<long long>(sh.number[2]) + 1));
+    int found = -1;
+    for (int r = 0; r < ctas; ++r)
+      if (box[r] != 0) found = static_cast<int>(box[r]) - 1;
+    return found;
+  }
+
+  // The last entry that a filter keeps, by the digits of its key: of the entries with `in`, by their number (`want` of them) or by their
+  // mass (the first at which it reaches `want`).
+  template <class In>
+  __device__ __forceinline__ void find_by_digits(const Weigh& w, In in, bool by_mass, u64 want, float& tx, int& ti) {
     uint32_t prefix = 0, mask = 0;
+    u64 ties = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
+      sync();
       if (t < 256) {
-        mass[t] = 0;
-        count[t] = 0;
+        sh.digit.mass[t] = 0;
+        sh.digit.count[t] = 0;
       }
       __syncthreads();
-      for (int v = t; v < V; v += kThreads) {
-        const uint32_t k = key(v);
-        if (k == 0 || k < low || (k & mask) != prefix) continue;
-        atomicAdd(&count[(k >> shift) & 255], 1);
-        if (by_mass && k > low) atomicAdd(&mass[(k >> shift) & 255], fixed(weight(k), unit));
+      for (int i = w0 + lane; i < w1; i += 32) {
+        const float v = at(i);
+        const uint32_t k = logit_key(v);
+        if (!in(v, base + i) || (k & mask) != prefix) continue;
+        const int d = (k >> shift) & 255;
+        atomicAdd(&sh.digit.count[d], 1u);
+        if (by_mass) atomicAdd(&sh.digit.mass[d], w.weight(w.z(v)));
       }
-      __syncthreads();
-      if (by_mass && t == 0 && low > 0 && (low & mask) == prefix) mass[(low >> shift) & 255] += low_need * fixed(weight(low), unit);
+      sync();
+      u64 mass = 0, count = 0;
+      if (t < 256)
+        for (int r = 0; r < ctas; ++r) {
+          mass += load_remote64(&sh.digit.mass[t], r);
+          count += load_remote32(&sh.digit.count[t], r);
+        }
+      sync();
+      if (t < 256) {
+        sh.digit.mass[t] = by_mass ? mass : count;
+        sh.digit.count[t] = static_cast<uint32_t>(count);
+      }
       __syncthreads();
       if (t == 0) {
         int d = 255;
         u64 left = want;
-        while (d > 0 && (by_mass ? mass[d] : static_cast<u64>(count[d])) < left) left -= by_mass ? mass[d--] : static_cast<u64>(count[d--]);
-        sh_key = prefix | (static_cast<uint32_t>(d) << shift);
-        sh_above = left;
-        sh_need = count[d];
+        while (d > 0 && sh.digit.mass[d] < left) left -= sh.digit.mass[d--];
+        sh.number[0] = d;
+        sh.word[1] = left;
+        sh.word[2] = sh.digit.count[d];
       }
       __syncthreads();
-      prefix = sh_key;
-      want = sh_above;
+      prefix |= static_cast<uint32_t>(sh.number[0]) << shift;
+      want = sh.word[1];
+      ties = sh.word[2];
       mask |= 255u << shift;
     }
-    floor_key = prefix;
-    // `want` of the entries' number or mass is still missing, and they are all equal
-    if (!by_mass) {
-      floor_need = static_cast<int>(want);
-    } else {
-      const u64 w = fixed(weight(prefix), unit);
-      const int most = prefix == low ? low_need : sh_need;     // (a prefix is never 0)
-      const u64 n = w > 0 ? (want + w - 1) / w : 1;
-      floor_need = n < 1 ? 1 : n > static_cast<u64>(most) ? most : static_cast<int>(n);
+    tx = key_logit(prefix);
+    if (by_mass) {
+      const u64 one = w.weight(w.z(tx));
+      want = one > 0 ? (want + one - 1) / one : 1;
     }
-    __syncthreads();
-  };
-  u64 n = 0;
-  for (int v = t; v < V; v += kThreads) n += key(v) > 0;
-  n = block_sum(n, sh);
-  if (static_cast<u64>(r.top_k) < n) find(false, r.top_k, 0, 0);
-  if (r.top_p < 1.0 && !r.greedy) {
-    u64 sum = 0;
-    for (int v = t; v < V; v += kThreads) {
-      const uint32_t k = key(v);
-      if (k > floor_key) sum += fixed(weight(k), unit);
-    }
-    sum = block_sum(sum, sh);
-    if (floor_key > 0) sum += floor_need * fixed(weight(floor_key), unit);
-    const double w = r.top_p * static_cast<double>(sum);
-    u64 want = w > 0.0 ? static_cast<u64>(ceil(w)) : 1;
-    if (want < 1) want = 1;
-    find(true, want, floor_key, floor_need);
+    want = want < 1 ? 1 : want > ties ? ties : want;
+    // the want-th of the equal ones
+    const float x0 = tx;
+    auto tie = [&](float v, int i) -> u64 { return v == x0 && in(v, i); };
+    u64 s = 0;
+    for (int i = w0 + lane; i < w1; i += 32) s += tie(at(i), base + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) sh.sums[warp] = s;
+    ti = locate(tie, want - 1);
   }
-  // min_p: a border between weights, so between keys
-  auto passes = [&](uint32_t k) { return k == top || weight(k) >= r.min_p; };
+};
 
-  // Kept entries by index: each warp has a range of its own.
-  const int span = (V + kWarps - 1) / kWarps, begin = min(warp * span, V), end = min(begin + span, V);
-  int ties = 0;
-  for (int v = begin + lane; v < end; v += 32) ties += key(v) == floor_key;
-  ties = __reduce_add_sync(0xffffffffu, ties);
-  if (lane == 0) sh_ties[warp] = ties;
-  __syncthreads();
-  int before = 0;
-  for (int w = 0; w < warp; ++w) before += sh_ties[w];
-  u64 sum = 0;
-  int kept = 0, last = -1, seen = before;
-  bool given_kept = false;
-  for (int base = begin; base < end; base += 32) {
-    const int v = base + lane;
-    const uint32_t k = v < end ? key(v) : 0;
-    const uint32_t same = __ballot_sync(0xffffffffu, k == floor_key);
-    const int rank = seen + __popc(same & ((1u << lane) - 1));
-    seen += __popc(same);
-    if (k != 0 && (k > floor_key || (k == floor_key && rank < floor_need)) && passes(k)) {
-      const u64 w = fixed(weight(k), unit);
-      sum += w;
-      ++kept;
-      if (w > 0) last = v;
-      given_kept |= v == given;
+template <class T, bool HELD>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ cpmtp_sample_args a, int ctas, int span, int bits, int* dev_status) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int rank = static_cast<int>(blockIdx.x) % ctas, row = static_cast<int>(blockIdx.x) / ctas;
+  // between one and two, while nothing else can be done
+  for (int i = t; i < kTable; i += kThreads) sh.table[i] = static_cast<u64>(exp2(static_cast<double>(i) / kTable) * 4611686018427387904.0);
+  ptx::grid_dep_wait();
+  const T* src = static_cast<const T*>(a.logits) + row * a.ld;
+  Row<T, HELD> R{a, sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, nullptr, 0};
+  R.base = min(rank * span, a.V);
+  R.n = min(span, a.V - R.base);
+  const int range = (R.n + kWarps - 1) / kWarps;
+  R.w0 = min(warp * range, R.n);
+  R.w1 = min(R.w0 + range, R.n);
+
+  // ---- the entries, in whole 16-byte pieces that start before them if need be, and the largest
+  float top = -INFINITY;
+  {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(src + R.base);
+    const int off = static_cast<int>(first & 15) / static_cast<int>(sizeof(T));          // entries before the first in its piece
+    constexpr int kPer = 16 / sizeof(T);
+    const uint4* pieces = reinterpret_cast<const uint4*>(first & ~static_cast<uintptr_t>(15));
+    const int count = R.n > 0 ? (off + R.n + kPer - 1) / kPer : 0;
+    uint4* held = reinterpret_cast<uint4*>(smem + sizeof(Shared));
+    R.x = HELD ? reinterpret_cast<const T*>(held) + off : src + R.base;
+    constexpr int kAhead = 8;
+    for (int i0 = t; i0 < count; i0 += kAhead * kThreads) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        if (i < count) v[j] = __ldg(pieces + i);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = i0 + j * kThreads;
+        if (i >= count) break;
+        if (HELD) held[i] = v[j];
+        float e[kPer];
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (sizeof(T) == 4) {
+            e[q % kPer] = __uint_as_float(w[q]);
+          } else {
+            e[(2 * q) % kPer] = ptx::bf16_lo(w[q]);
+            e[(2 * q + 1) % kPer] = ptx::bf16_hi(w[q]);
+          }
+        }
+        if (i == 0 || i + 1 == count) {
+#pragma unroll
+          for (int q = 0; q < kPer; ++q) {
+            const int k = i * kPer + q - off;
+            if (k < 0 || k >= R.n) e[q] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) top = fmaxf(top, e[q]);       // (which passes over NaN)
+      }
     }
   }
-  const u64 mine = [&] {
-    u64 q = sum;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-    return q;
-  }();
-  total = block_sum(sum, sh);             // leaves the warps' sums in sh
-  const int all_kept = static_cast<int>(block_sum(kept, mass));
-  const int last_token = static_cast<int>(block_all(static_cast<u64>(last + 1), mass, [](u64 p, u64 q) { return p > q ? p : q; })) - 1;
-  const bool any_given = __syncthreads_or(given_kept);
-  const float u = a.uniform[i];
-  const u64 target = u > 0.f ? (u < 1.f ? static_cast<u64>(static_cast<double>(u) * static_cast<double>(total)) : total) : 0;
-  u64 low = 0;
-  for (int w = 0; w < warp; ++w) low += sh[w];
-  if (t == 0) sh_token = last_token;
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float* tops = reinterpret_cast<float*>(sh.sums);
+  if (lane == 0) tops[warp] = top;
   __syncthreads();
-  if (low <= target && target < low + mine) {
-    // this warp's range holds the token
-    int at = before;
-    for (int base = begin; base < end; base += 32) {
-      const int v = base + lane;
-      const uint32_t k = v < end ? key(v) : 0;
-      const uint32_t same = __ballot_sync(0xffffffffu, k == floor_key);
-      const int rank = at + __popc(same & ((1u << lane) - 1));
-      at += __popc(same);
-      u64 w = 0;
-      if (k != 0 && (k > floor_key || (k == floor_key && rank < floor_need)) && passes(k)) w = fixed(weight(k), unit);
+  top = tops[lane & (kWarps - 1)];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 q = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += q;
+  for (int o = kWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  {
+    const u64* box = R.exchange(__float_as_uint(top));
+    for (int r = 0; r < ctas; ++r) top = fmaxf(top, __uint_as_float(static_cast<uint32_t>(box[r])));
+  }
+  const int given = a.given != nullptr ? a.given[row] : CPMTP_EMBED_PAD;
+  const bool writer = rank == 0 && t == 0;
+  if (writer && given != CPMTP_EMBED_PAD && (given < 0 || given >= a.V) && dev_status != nullptr) atomicMax(dev_status, 1);
+  auto answer = [&](int token, float logp, int kept, float logp_given) {
+    if (!writer) return;
+    a.tokens[row] = token;
+    if (a.logp != nullptr) a.logp[row] = logp;
+    if (a.kept != nullptr) a.kept[row] = kept;
+    if (a.given != nullptr) a.logp_given[row] = logp_given;
+  };
+  if (!(top > -INFINITY)) {
+    answer(-1, -INFINITY, 0, -INFINITY);
+    return;                                  // (the same in every block of the cluster, after its barrier)
+  }
+  const Settings set = settings_of(a, row);
+  if (set.one) {
+    // the first of the largest
+    u64 none = 0;                            // 2^31 - index: the lowest is the largest
+    for (int i = R.w0 + lane; i < R.w1; i += 32)
+      if (R.at(i) == top) none = max(none, static_cast<u64>((1u << 31) - (R.base + i)));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) none = max(none, __shfl_xor_sync(0xffffffffu, none, o));
+    __syncthreads();
+    if (lane == 0) sh.sums[warp] = none;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) none = max(none, sh.sums[w]);
+    const u64* box = R.exchange(none);
+    for (int r = 0; r < ctas; ++r) none = max(none, box[r]);
+    const int token = static_cast<int>((1u << 31) - static_cast<uint32_t>(none));
+    answer(token, 0.f, 1, given == token ? 0.f : -INFINITY);
+    return;
+  }
+  Weigh w;
+  w.m = static_cast<double>(top);
+  w.c = set.inv_t * 1.4426950408889634074;
+  w.mf = top;
+  w.cf = static_cast<float>(fmin(w.c, 3e38));
+  w.inf = top == INFINITY;
+  w.down = 62 - bits;
+  w.table = sh.table;
+  const double unit = static_cast<double>(1ull << bits);
+  long long z_min = kNoWeight;               // of min_p
+  if (set.min_p > 0.0) {
+    const double l = log2(set.min_p);
+    z_min = l > -59.0 ? static_cast<long long>(ceil(l * 4294967296.0)) : kNoWeight;
+  }
+  const float u = a.uniform[row];
+  auto target_of = [&](u64 total) {
+    return u > 0.f ? (u < 1.f ? min(static_cast<u64>(static_cast<double>(u) * static_cast<double>(total)), total - 1) : total - 1) : 0;
+  };
+  auto finish = [&](int token, u64 total, int kept, float tx, int ti) {
+    if (!writer || token < 0) return;
+    const double all = log(static_cast<double>(total) / unit);
+    auto logp = [&](float v) { return static_cast<float>((v == top ? 0.0 : (static_cast<double>(v) - w.m) * set.inv_t) - all); };
+    float lg = -INFINITY;
+    if (given >= 0 && given < a.V) {
+      const float v = io::to_f(src[given]);
+      if ((v > tx || (v == tx && given <= ti)) && w.z(v) >= z_min) lg = logp(v);
+    }
+    answer(token, logp(io::to_f(src[token])), kept, lg);
+  };
+
+  // ---- entries x > tx, and x == tx up to index ti, are kept
+  float tx = -INFINITY;
+  int ti = -1;
+  auto kept_by = [&](float v, int i) { return v > tx || (v == tx && i <= ti); };
+
+  // ---- top-k
+  u64 valid = 0;
+  if (set.top_k < a.V) {
+    for (int i = R.w0 + lane; i < R.w1; i += 32) valid += R.at(i) > -INFINITY;
+    valid = R.row_sum(valid);
+  }
+  if (static_cast<u64>(set.top_k) < valid) {
+    bool found = false;
+    if (!w.inf) {
+      // bins of 1/64 in units of ln 2 of the logits themselves; the magic number rounds to integers
+      const float step = 64.f * 1.4426950408889634f;
+      auto bin_of = [&](float v) { return __float_as_uint(fminf(fmaf(top - v, step, 8388608.f), 8388608.f + (kBins - 1))) & 0x7fffffu; };
+      R.clear_hist();
+      for (int i = R.w0 + lane; i < R.w1; i += 32) {
+        const float v = R.at(i);
+        if (v > -INFINITY) atomicAdd(&sh.hist[bin_of(v)], 1u);
       }
-      const uint32_t over = __ballot_sync(0xffffffffu, low + w > target);
-      if (over != 0) {
-        if (lane == 0) sh_token = base + __ffs(over) - 1;
-        break;
+      int b, b2;
+      double before;
+      R.find_bins([](int) { return 1.0; }, set.top_k, set.top_k, b, b2, before);
+      // all entries down to that bin, if they are few; else those of the bin
+      const bool all = before + kList / 2 <= kList && b < kBins - 1;
+      const uint32_t from = all ? 0 : b;
+      for (int i0 = R.w0; i0 < R.w1; i0 += 32) {
+        const int i = i0 + lane;
+        const float v = i < R.w1 ? R.at(i) : -INFINITY;
+        const uint32_t k = bin_of(v);
+        R.list_add(v > -INFINITY && k >= from && k <= static_cast<uint32_t>(b), v, R.base + i);
       }
-      low += __shfl_sync(0xffffffffu, w, 31);
+      const int count = R.gather_list();
+      if (count <= kList && all) {
+        // the rest is block 0's alone
+        R.sync();
+        if (rank != 0) return;
+        R.sort_list(count);
+        u64 v[4];
+        long long z[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 4 * t + j;
+          z[j] = i < set.top_k ? w.z(R.entry_logit(sh.list[i])) : kNoWeight;
+          v[j] = i < set.top_k ? w.weight(z[j]) : 0;
+        }
+        u64 own[4] = {v[0], v[1], v[2], v[3]};
+        R.scan4(v);
+        if (t == kThreads - 1) sh.word[3] = v[3];
+        __syncthreads();
+        const double border = set.top_p * static_cast<double>(sh.word[3]);
+        u64 left = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 4 * t + j;
+          left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && z[j] >= z_min;
+        }
+        const int kept = static_cast<int>(R.block_sum(left));
+        if (kept - 1 >= 4 * t && kept - 1 < 4 * t + 4) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (kept - 1 == 4 * t + j) sh.word[2] = v[j];
+        }
+        __syncthreads();
+        const u64 total = sh.word[2], last = sh.list[kept - 1];
+        // by index: the keys' halves change places (and fall, so the index is inverted as it stands)
+        __syncthreads();
+        for (int i = t; i < kept; i += kThreads) sh.list[i] = sh.list[i] << 32 | sh.list[i] >> 32;
+        R.sort_list(kept);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 4 * t + j;
+          v[j] = i < kept ? w.weight(w.z(key_logit(static_cast<uint32_t>(sh.list[i])))) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) own[j] = v[j];
+        R.scan4(v);
+        const u64 target = target_of(total);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (v[j] > target && v[j] - own[j] <= target) sh.number[2] = static_cast<int>(~static_cast<uint32_t>(sh.list[4 * t + j] >> 32));
+        __syncthreads();
+        finish(sh.number[2], total, kept, R.entry_logit(last), R.entry_index(last));
+        return;
+      }
+      if (count <= kList) {
+        const int nth = set.top_k - static_cast<int>(before) - 1;          // of the bin's entries, the last that is kept
+        if (rank == 0) {
+          R.sort_list(count);
+          if (t < ctas) store_remote(&sh.word[2], t, sh.list[nth]);
+        }
+        R.sync();
+        tx = R.entry_logit(sh.word[2]);
+        ti = R.entry_index(sh.word[2]);
+        found = true;
+      }
+    }
+    if (!found) R.find_by_digits(w, [](float v, int) { return v > -INFINITY; }, false, set.top_k, tx, ti);
+  }
+
+  // ---- top-p, and the kept mass of every warp's range
+  u64 sum = 0, number = 0;
+  bool counted = false;
+  if (set.top_p < 1.0) {
+    const int less = max(0, 32 - __clz(span - 1) - 14);                    // bits that the histogram's sums have to do without
+    u64 mass = 0;
+    R.clear_hist();
+    for (int i = R.w0 + lane; i < R.w1; i += 32) {
+      const float v = R.at(i);
+      if (!kept_by(v, R.base + i)) continue;
+      const long long z = w.z(v);
+      const u64 q = w.mantissa(z);
+      mass += w.fixed(q, z);
+      if (z > kNoWeight) atomicAdd(&sh.hist[min(static_cast<int>(-(z >> 26)), kBins - 1)], static_cast<uint32_t>(q >> (45 + less)));
+    }
+    mass = R.row_sum(mass);
+    const double border = set.top_p * static_cast<double>(mass);
+    bool found = false;
+    if (!w.inf) {
+      // an entry of bin b has floor(z) = -ceil(b / 64); the sums are short by 2^(less - 17) at most
+      const double one = unit * ldexp(1.0, less - 17), slack = ldexp(1.0, less - 15);
+      int b1, b2;
+      double before;
+      R.find_bins([&](int b) { return one * exp2f(static_cast<float>(-((b + 63) >> 6))); }, border * (1.0 - slack), border * (1.0 + slack), b1, b2, before);
+      // Entries above xa lie in bins before b1, those below xb in bins behind b2; the bins' edges, rounded outwards.
+      const float xa = nextafterf(__double2float_ru(w.m - (b1 - 1) / (64.0 * w.c)), INFINITY);
+      const float xb = b2 == kBins - 1 ? -FLT_MAX : nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY);
+      u64 above = 0;
+      for (int i0 = R.w0; i0 < R.w1; i0 += 32) {
+        const int i = i0 + lane;
+        const float v = i < R.w1 ? R.at(i) : -INFINITY;
+        const bool in = v >= xb && kept_by(v, R.base + i);
+        if (in && v > xa) {
+          const long long z = w.z(v);
+          const u64 q = w.weight(z);
+          above += q;
+          if (z >= z_min) {
+            sum += q;
+            ++number;
+          }
+        }
+        R.list_add(in && !(v > xa), v, R.base + i);
+      }
+      above = R.row_sum(above);
+      const int mine = min(sh.listed, kList);
+      const int count = R.gather_list();
+      if (count <= kList) {
+        if (rank == 0) {
+          // (the keys of the other blocks lie behind this block's own, which it needs again: they are sorted in place, so its own
+          // entries' shares are found from the sorted list by index)
+          R.sort_list(count);
+          u64 v[4], own[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) own[j] = v[j] = 4 * t + j < count ? w.weight(w.z(R.entry_logit(sh.list[4 * t + j]))) : 0;
+          R.scan4(v);
+          u64 left = 0;
+          bool reached = false;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            left += 4 * t + j < count && static_cast<double>(above + v[j] - own[j]) < border;
+            reached |= 4 * t + j < count && static_cast<double>(above + v[j]) >= border;
+          }
+          const int kept = static_cast<int>(R.block_sum(left));
+          reached = __syncthreads_or(reached);
+          // the border has to lie among these entries, as the histogram said; 0: it does not
+          const u64 last = kept > 0 && (reached || b2 == kBins - 1) ? sh.list[kept - 1] : 0;
+          if (t < ctas) store_remote(&sh.word[2], t, last);
+        }
+        R.sync();
+        const u64 last = sh.word[2];
+        if (last != 0) {
+          found = counted = true;
+          tx = R.entry_logit(last);
+          ti = R.entry_index(last);
+          // the listed entries that are kept, to the sums of the ranges they lie in
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          if (lane == 0) sh.sums[warp] = sum;
+          __syncthreads();
+          for (int i = t; i < (rank == 0 ? count : mine); i += kThreads) {
+            const u64 e = sh.list[i];
+            const int index = R.entry_index(e) - R.base;
+            if (e < last || index < 0 || index >= R.n) continue;
+            const long long z = w.z(R.entry_logit(e));
+            if (z < z_min) continue;
+            ++number;
+            atomicAdd(&sh.sums[index / range], w.weight(z));
+          }
+        }
+      }
+    }
+    if (!found) {
+      const float x1 = tx;
+      const int i1 = ti;
+      sum = number = 0;
+      R.find_by_digits(w, [=](float v, int i) { return v > x1 || (v == x1 && i <= i1); }, true, max(1ull, static_cast<u64>(ceil(border))), tx, ti);
     }
   }
-  __syncthreads();
-  if (t == 0) {
-    const double log_total = log(static_cast<double>(total) / unit);
-    a.tokens[i] = sh_token;
-    if (a.logp != nullptr) a.logp[i] = static_cast<float>(z_of(key_logit(key(sh_token)), m, r.inv_t) - log_total);
-    if (a.kept != nullptr) a.kept[i] = all_kept;
-    if (a.given != nullptr) a.logp_given[i] = any_given ? static_cast<float>(z_of(key_logit(key(given)), m, r.inv_t) - log_total) : -INFINITY;
+  auto drawn = [&](float v, int i) -> u64 {
+    if (!kept_by(v, i)) return 0;
+    const long long z = w.z(v);
+    return z >= z_min ? w.weight(z) : 0;
+  };
+  if (!counted) {
+    for (int i = R.w0 + lane; i < R.w1; i += 32) {
+      const float v = R.at(i);
+      if (!kept_by(v, R.base + i)) continue;
+      const long long z = w.z(v);
+      if (z < z_min) continue;
+      sum += w.weight(z);
+      ++number;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncthreads();
+    if (lane == 0) sh.sums[warp] = sum;
   }
+  __syncthreads();
+  u64 total = R.row_sum(t < kWarps ? sh.sums[t] : 0);
+  number = R.row_sum(number);
+  const int token = R.locate(drawn, target_of(total));
+  finish(token, total, static_cast<int>(number), tx, ti);
 }
 
 }  // namespace sample

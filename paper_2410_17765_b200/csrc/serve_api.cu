@@ -137,6 +137,29 @@ size_t evict_bytes(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int budget) 
   return align_up(sizeof(int) * static_cast<size_t>(s.B) * c.H * budget + kAlign);
 }
 
+// Blocks of a cluster that share a row: enough to hold it in 64 KB of shared memory each (two blocks to an SM) and to use all SMs, as
+// long as each has some entries for its threads.
+template <class T>
+cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, cudaStream_t st) {
+  constexpr size_t kMost = 232448, kShare = 65536;
+  int ctas = 1;
+  while (ctas < sample::kMostCtas && a.V / ctas >= 4 * sample::kThreads &&
+         (static_cast<size_t>(a.V) * sizeof(T) / ctas > kShare || static_cast<long long>(a.N) * ctas < sms))
+    ctas *= 2;
+  const int span = ((a.V + ctas - 1) / ctas + 7) / 8 * 8;
+  int width = 0;
+  while ((1ll << width) < a.V) ++width;
+  const size_t held = sizeof(sample::Shared) + static_cast<size_t>(span) * sizeof(T) + 32;
+  const dim3 grid(static_cast<unsigned>(a.N) * ctas), threads(sample::kThreads);
+  static bool done[64] = {}, done_far[64] = {};
+  if (held <= kMost) {
+    const cudaError_t e = allow_smem(sample::sample_kernel<T, true>, done, kMost);
+    return e != cudaSuccess ? e : launch_clusters(ctas, sample::sample_kernel<T, true>, grid, threads, held, st, a, ctas, span, 62 - width, dev_status);
+  }
+  const cudaError_t e = allow_smem(sample::sample_kernel<T, false>, done_far, static_cast<int>(sizeof(sample::Shared)));
+  return e != cudaSuccess ? e : launch_clusters(ctas, sample::sample_kernel<T, false>, grid, threads, sizeof(sample::Shared), st, a, ctas, span, 62 - width, dev_status);
+}
+
 }  // namespace
 }  // namespace cpmtp
 
@@ -255,7 +278,7 @@ int cpmtp_sample_logits(const cpmtp_sample_args* args, int32_t* dev_status, cpmt
   if (args == nullptr) return CPMTP_ERR_NULL;
   const cpmtp_sample_args& a = *args;
   if (a.N < 0 || a.V < 1 || (a.N > 1 && a.ld < a.V) || (a.type != CPMTP_BF16 && a.type != CPMTP_F32)) return CPMTP_ERR_SHAPE;
-  if (a.V > CPMTP_SAMPLE_MAX_V) return CPMTP_ERR_LIMIT;
+  if (a.V > CPMTP_SAMPLE_MAX_V || a.N > (1 << 27)) return CPMTP_ERR_LIMIT;
   if (!(a.temperature >= 0.f) || !std::isfinite(a.temperature) || !(a.top_p >= 0.f) || !(a.min_p >= 0.f) || a.top_k < 0) return CPMTP_ERR_SHAPE;
   if (a.N == 0) return CPMTP_OK;
   if (!a.logits || !a.uniform || !a.tokens || (a.given && !a.logp_given)) return CPMTP_ERR_NULL;
@@ -270,11 +293,8 @@ int cpmtp_sample_logits(const cpmtp_sample_args* args, int32_t* dev_status, cpmt
   if (rc != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_SAMPLE, st);
-  int bits = 0;
-  while ((1ll << bits) < a.V) ++bits;
-  const double unit = std::ldexp(1.0, 62 - bits);      // V weights of at most one sum to less than 2^63
-  if (a.type == CPMTP_F32) CPMTP_TRY(launch_pdl(sample::sample_kernel<float>, dim3(a.N), dim3(sample::kThreads), 0, st, a, unit, dev_status));
-  else CPMTP_TRY(launch_pdl(sample::sample_kernel<bf16_t>, dim3(a.N), dim3(sample::kThreads), 0, st, a, unit, dev_status));
+  if (a.type == CPMTP_F32) CPMTP_TRY(launch_sample<float>(a, di->sms, dev_status, st));
+  else CPMTP_TRY(launch_sample<bf16_t>(a, di->sms, dev_status, st));
   return CPMTP_OK;
 }
 
