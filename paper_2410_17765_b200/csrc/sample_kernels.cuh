@@ -10,6 +10,7 @@
 // latency of a dozen barriers of a cluster.
 #pragma once
 #include <cfloat>
+#include <climits>
 #include <cstdint>
 
 #include "../../include/cpmtp.h"
@@ -40,7 +41,7 @@ struct Shared {
   };
   double scan[kWarps];
   u64 sums[kWarps];                    // kept mass of the warps' ranges
-  u64 box[8][kMostCtas];               // numbers from the blocks of the cluster; a place in turn
+  u64 box[8][kMostCtas];               // numbers from the blocks of the cluster; two places in turn
   u64 word[4];
   int listed, number[3];
 };
@@ -84,22 +85,32 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-constexpr long long kNoWeight = -(60ll << 32);       // z of entries that have none
+constexpr long long kNoWeight = -(160ll << 32);      // z of entries that have none: below that of the least min_p (2^-149)
 
 struct Weigh {
   double m, c;           // largest logit; log2(e) / T
+  float x_min;           // logits below it have no weight
   float mf, cf;
-  bool inf;              // the largest logit is infinite
+  bool odd;              // the largest logit is infinite, or the next one below it is out of the range of z
   int down;              // 62 minus the bits below the point
   const u64* table;
 
   // (x - m) c with 32 bits below the point: the product is added to a number whose last bit is 2^-32.
   __device__ __forceinline__ long long z(float x) const {
-    if (inf) return x == INFINITY ? 0 : kNoWeight;
-    const float about = (x - mf) * cf;
     constexpr double kMagic = 1572864.0;               // 1.5 x 2^20
-    const long long v = __double_as_longlong(fma(static_cast<double>(x) - m, c, kMagic)) - 0x4138000000000000ll;
-    return about > -60.f ? v : kNoWeight;
+    if (odd && !(x == mf || (x - mf) * cf > -160.f)) return kNoWeight;
+    if (odd && x == mf) return 0;
+    return __double_as_longlong(fma(static_cast<double>(fmaxf(x, x_min)) - m, c, kMagic)) - 0x4138000000000000ll;
+  }
+  __device__ __forceinline__ void set(float top, double inv_t, int bits) {
+    m = static_cast<double>(top);
+    c = inv_t * 1.4426950408889634074;
+    mf = top;
+    cf = static_cast<float>(fmin(c, 3e38));
+    const double low = m - 160.0 / c;                  // (c may be 0: minus infinity)
+    x_min = low > -FLT_MAX ? __double2float_rd(low) : -FLT_MAX;
+    odd = !(x_min < top) || !((m - static_cast<double>(x_min)) * c < 1000.0);
+    down = 62 - bits;
   }
   // 2^(z - floor(z)) with 62 bits below the point.  The leading ten bits by table, the others by three terms of the series of
   // 2^r - 1, r < 2^-10, in fp32: an error of 2^-24 of a number below 2^-10.5.  With the 2^-33 of z and the 2^-34 of its own
@@ -139,24 +150,63 @@ __device__ __forceinline__ Settings settings_of(const cpmtp_sample_args& a, int 
 }
 
 // -------------------------------------------------------------------------------------------- the kernel
-// A cluster of `ctas` blocks to a row; a block has `span` entries of it, its warps equal ranges of those.  HELD: in shared memory.
+// A cluster of `ctas` blocks to a row.  A block's entries are read in whole 16-byte pieces, the first and last of which may reach beyond
+// them; its warps have equal ranges of pieces.  HELD: in shared memory.
 template <class T, bool HELD>
 struct Row {
-  const cpmtp_sample_args& a;
+  static constexpr int kPer = 16 / sizeof(T);
   Shared& sh;
   const int ctas, rank, t, lane, warp;
   int base, n;           // this block's entries
-  int w0, w1;            // this warp's, among them
-  const T* x;
+  int off;               // entries of the first piece that lie before them
+  int pieces, each;      // pieces of the block, of a warp
+  const uint4* data;
   int boxes;
 
-  __device__ __forceinline__ float at(int i) const { return io::to_f(x[i]); }
   __device__ __forceinline__ void sync() const { sync_row(ctas); }
 
-  // Sums over the block's threads, in every thread.
-  __device__ __forceinline__ u64 block_sum(u64 v) {
+  __device__ __forceinline__ void unpack(int piece, const uint4& raw, float (&v)[kPer]) const {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (sizeof(T) == 4) {
+        v[q % kPer] = __uint_as_float(w[q]);
+      } else {
+        v[(2 * q) % kPer] = ptx::bf16_lo(w[q]);
+        v[(2 * q + 1) % kPer] = ptx::bf16_hi(w[q]);
+      }
+    }
+    if (piece == 0 || piece + 1 == pieces) {           // what does not belong to them counts as never kept
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) {
+        const int i = piece * kPer + q - off;
+        if (i < 0 || i >= n) v[q] = -INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const { unpack(piece, HELD ? data[piece] : __ldg(data + piece), v); }
+  // f(logit, index in the row) for the entries of this warp's pieces.
+  template <class F>
+  __device__ __forceinline__ void for_each(F f) const {
+    const int end = min((warp + 1) * each, pieces);
+#pragma unroll 2
+    for (int p = warp * each + lane; p < end; p += 32) {
+      float v[kPer];
+      load(p, v);
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) f(v[q], base + p * kPer + q - off);
+    }
+  }
+  __device__ __forceinline__ int warp_of(int index) const { return (index - base + off) / kPer / each; }
+
+  __device__ __forceinline__ u64 warp_sum(u64 v) const {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
+  // Sum over the block's threads, in every thread.
+  __device__ __forceinline__ u64 block_sum(u64 v) {
+    v = warp_sum(v);
     __syncthreads();
     u64* part = reinterpret_cast<u64*>(sh.scan);
     if (lane == 0) part[warp] = v;
@@ -166,40 +216,67 @@ struct Row {
     for (int o = kWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return __shfl_sync(0xffffffffu, v, 0);
   }
-  // Gives `v` (of thread 0) to every block and brings theirs: box[r] of block r.  A barrier of the cluster.
-  __device__ __forceinline__ const u64* exchange(u64 v) {
-    u64* box = sh.box[boxes++ & 7];
-    if (ctas == 1) {
-      if (t == 0) box[0] = v;
-      __syncthreads();
-    } else {
-      v = __shfl_sync(0xffffffffu, v, 0);
-      if (t < ctas) store_remote(box + rank, t, v);
-      sync();
+  // Sums up to and with each thread's v over the block.
+  __device__ __forceinline__ u64 block_scan(u64 v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
     }
+    u64* part = reinterpret_cast<u64*>(sh.scan);
+    __syncthreads();
+    if (lane == 31) part[warp] = v;
+    __syncthreads();
+    u64 before = lane < warp ? part[lane & (kWarps - 1)] : 0;
+    return v + warp_sum(before);
+  }
+  // Gives numbers (of the first warp's threads) to every block and brings theirs: box[r] of block r.  A barrier of the cluster.
+  __device__ __forceinline__ const u64* exchange(u64 v) { return exchange(v, 0, 1); }
+  __device__ __forceinline__ const u64* exchange(u64 v, u64 second, int boxes_used = 2) {
+    u64* box = sh.box[boxes];
+    boxes = (boxes + 2) & 7;
+    if (t < ctas) {
+      if (ctas == 1) {
+        box[0] = v;
+        box[kMostCtas] = second;
+      } else {
+        store_remote(box + rank, t, v);
+        if (boxes_used > 1) store_remote(box + kMostCtas + rank, t, second);
+      }
+    }
+    sync();
     return box;
   }
-  __device__ __forceinline__ u64 row_sum(u64 v) {
-    const u64* box = exchange(block_sum(v));
+  __device__ __forceinline__ u64 sum_of(const u64* box) const {
     u64 s = 0;
     for (int r = 0; r < ctas; ++r) s += box[r];
     return s;
   }
+  __device__ __forceinline__ u64 row_sum(u64 v) { return sum_of(exchange(block_sum(v))); }
 
   // First and second bin at which the running sum of the histogram, bin b weighing scale(b), reaches `low` and `high`, and what lies
-  // before the first; the last bin where they are not reached.
+  // before the first; the last bin where they are not reached.  Returns the whole sum.
   template <class Scale>
-  __device__ __forceinline__ void find_bins(Scale scale, double low, double high, int& b1, int& b2, double& before) {
+  __device__ __forceinline__ double find_bins(Scale scale, double low, double high, int& b1, int& b2, double& before) {
+    constexpr int kOwn = kBins / kThreads;
     sync();                                            // the blocks' histograms are complete
-    const int per = kBins / ctas, each = (per + kThreads - 1) / kThreads;       // bins of this block, of a thread
-    double mine[kBins / kThreads], sum = 0.0;
+    const int per = kBins / ctas, mine_of = (per + kThreads - 1) / kThreads;       // bins of this block, of a thread
+    double mine[kOwn], sum = 0.0;
 #pragma unroll
-    for (int j = 0; j < kBins / kThreads; ++j) {
+    for (int j = 0; j < kOwn; ++j) {
       mine[j] = 0.0;
-      const int b = t * each + j;
-      if (j < each && b < per) {
+      const int b = t * mine_of + j;
+      if (j < mine_of && b < per) {
         u64 c = 0;
-        for (int r = 0; r < ctas; ++r) c += ctas == 1 ? sh.hist[b] : load_remote32(&sh.hist[rank * per + b], r);
+        if (ctas == 1) {
+          c = sh.hist[b];
+        } else {
+          uint32_t h[kMostCtas];
+#pragma unroll
+          for (int r = 0; r < kMostCtas; ++r) h[r] = r < ctas ? load_remote32(&sh.hist[rank * per + b], r) : 0;
+#pragma unroll
+          for (int r = 0; r < kMostCtas; ++r) c += h[r];
+        }
         mine[j] = static_cast<double>(c) * scale(rank * per + b);
         sum += mine[j];
       }
@@ -220,18 +297,21 @@ struct Row {
     double all = 0.0;
     for (int w = 0; w < kWarps; ++w) all += sh.scan[w];
     const u64* box = exchange(__double_as_longlong(all));
-    double run = 0.0;
-    for (int r = 0; r < rank; ++r) run += __longlong_as_double(box[r]);
+    double run = 0.0, total = 0.0;
+    for (int r = 0; r < ctas; ++r) {
+      if (r == rank) run = total;
+      total += __longlong_as_double(box[r]);
+    }
     for (int w = 0; w < warp; ++w) run += sh.scan[w];
     // a thread begins with the very number that the one before it ends with, so that no border falls between them
     upto += run;
     const double left = __shfl_up_sync(0xffffffffu, upto, 1);
     if (lane > 0) run = left;
 #pragma unroll
-    for (int j = 0; j < kBins / kThreads; ++j) {
-      const double next = j + 1 == each ? upto : run + mine[j];
-      const int b = rank * per + t * each + j;
-      if (j < each && t * each + j < per) {
+    for (int j = 0; j < kOwn; ++j) {
+      const double next = j + 1 == mine_of ? upto : run + mine[j];
+      const int b = rank * per + t * mine_of + j;
+      if (j < mine_of && t * mine_of + j < per) {
         if (run < low && next >= low)
           for (int r = 0; r < ctas; ++r) {
             store_remote(&sh.word[0], r, __double_as_longlong(run));
@@ -246,6 +326,7 @@ struct Row {
     b1 = sh.number[0];
     b2 = sh.number[1];
     before = __longlong_as_double(sh.word[0]);
+    return total;
   }
 
   __device__ __forceinline__ void clear_hist() {
@@ -259,39 +340,40 @@ struct Row {
   static __device__ __forceinline__ float entry_logit(u64 e) { return key_logit(static_cast<uint32_t>(e >> 32)); }
   static __device__ __forceinline__ int entry_index(u64 e) { return static_cast<int>(~static_cast<uint32_t>(e)); }
 
-  // Adds to the block's list the entries of lanes that have `take`.
-  __device__ __forceinline__ void list_add(bool take, float v, int index) {
-    const uint32_t lanes = __ballot_sync(0xffffffffu, take);
-    if (lanes == 0) return;
-    int place = 0;
-    if (lane == 0) place = atomicAdd(&sh.listed, __popc(lanes));
-    place = __shfl_sync(0xffffffffu, place, 0) + __popc(lanes & ((1u << lane) - 1));
-    if (take && place < kList) sh.list[place] = entry(v, index);
+  // Into the block's list, in any order: it is sorted later.
+  __device__ __forceinline__ void list_add(float v, int index) {
+    const int place = atomicAdd(&sh.listed, 1);
+    if (place < kList) sh.list[place] = entry(v, index);
   }
-
-  // All blocks' lists in block 0's, and their length in every block; more than kList: not gathered.
-  __device__ __forceinline__ int gather_list() {
-    __syncthreads();
-    const u64* box = exchange(sh.listed);
-    int total = 0;
-    for (int r = 0; r < ctas; ++r) total += static_cast<int>(box[r]);
-    if (ctas > 1 && total <= kList) {
-      if (rank == 0) {
-        int to = static_cast<int>(box[0]);
-        for (int r = 1; r < ctas; ++r) {
-          const int c = static_cast<int>(box[r]);
-          for (int i = t; i < c; i += kThreads) sh.list[to + i] = load_remote64(&sh.list[i], r);
-          to += c;
-        }
-      }
+  // All blocks' lists in block 0's, and their length in every block; more than kList: not gathered.  box: the lists' lengths.
+  __device__ __forceinline__ int gather_list(const u64* box) {
+    const int total = static_cast<int>(sum_of(box));
+    if (ctas > 1 && total <= kList && rank == 0 && warp > 0 && warp < ctas) {
+      int to = 0;
+      for (int r = 0; r < warp; ++r) to += static_cast<int>(box[r]);
+      const int c = static_cast<int>(box[warp]);
+      for (int i = lane; i < c; i += 32) sh.list[to + i] = load_remote64(&sh.list[i], warp);
     }
     return total;
   }
-  // Sorts the first `count` keys of this block's list, falling.
+  // Sorts the first `count` keys of this block's list, falling; they are all different.
   __device__ __forceinline__ void sort_list(int count) {
+    __syncthreads();
+    if (count <= kThreads) {
+      // a key's place is the number of larger ones
+      const u64 mine = t < count ? sh.list[t] : 0;
+      int place = 0;
+      if (warp * 32 < count) {
+#pragma unroll 4
+        for (int j = 0; j < count; ++j) place += sh.list[j] > mine;
+      }
+      __syncthreads();
+      if (t < count) sh.list[place] = mine;
+      __syncthreads();
+      return;
+    }
     int size = 2;
     while (size < count) size *= 2;
-    __syncthreads();
     for (int i = count + t; i < size; i += kThreads) sh.list[i] = 0;
     __syncthreads();
     for (int k = 2; k <= size; k *= 2)
@@ -311,82 +393,67 @@ struct Row {
   __device__ __forceinline__ void scan4(u64 (&v)[4]) {
 #pragma unroll
     for (int j = 1; j < 4; ++j) v[j] += v[j - 1];
-    u64 upto = v[3];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 u = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += u;
-    }
-    u64* part = reinterpret_cast<u64*>(sh.scan);
-    __syncthreads();
-    if (lane == 31) part[warp] = upto;
-    __syncthreads();
-    u64 before = upto - v[3];
-    for (int w = 0; w < warp; ++w) before += part[w];
+    const u64 before = block_scan(v[3]) - v[3];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] += before;
   }
 
-  // Index of the first entry at which the running sum of f over the row exceeds `target`; sh.sums has the warps' sums of f.
+  // The first entry at which the running sum of f over the row exceeds `target`, as (index + 1) << 32 | logit; sh.sums has the warps'
+  // sums of f, box those of the blocks.
   template <class F>
-  __device__ __forceinline__ int locate(F f, u64 target) {
+  __device__ __forceinline__ u64 locate(F f, u64 target, const u64* box) {
+    u64 here = 0;
+    for (int r = 0; r < rank; ++r) here += box[r];
+    if (t == 0) sh.word[1] = 0;
     __syncthreads();
-    u64 mine = lane < kWarps ? sh.sums[lane] : 0;
-    u64 upto = mine;
+    if (here <= target && target < here + box[rank]) {       // (the same for the whole block)
+      int w = 0;
+      while (target >= here + sh.sums[w]) here += sh.sums[w++];
+      // this warp's pieces, by all threads of the block
+      const int end = min((w + 1) * each, pieces);
+      for (int p0 = w * each; p0 < end; p0 += kThreads) {
+        const int p = p0 + t;
+        float v[kPer];
+        u64 g[kPer], sum = 0;
+        if (p < end) load(p, v);
 #pragma unroll
-    for (int o = 1; o < kWarps; o <<= 1) {
-      const u64 v = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += v;
-    }
-    const u64* box = exchange(__shfl_sync(0xffffffffu, upto, kWarps - 1));
-    u64 before = 0;
-    for (int r = 0; r < rank; ++r) before += box[r];
-    if (t == 0) sh.number[2] = -1;
-    __syncthreads();
-    const u64 here = before + __shfl_sync(0xffffffffu, upto - mine, warp), end = here + __shfl_sync(0xffffffffu, mine, warp);
-    if (here <= target && target < end) {
-      // a lane's share first (an odd number of entries, so that the lanes are in different banks), then the entries of one
-      const int share = ((w1 - w0 + 31) / 32) | 1;
-      int i0 = min(w0 + lane * share, w1), i1 = min(i0 + share, w1);
-      u64 sum = 0;
-      for (int i = i0; i < i1; ++i) sum += f(at(i), base + i);
-      u64 run = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 v = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += v;
-      }
-      const int who = __ffs(__ballot_sync(0xffffffffu, here + run > target)) - 1;
-      u64 low = here + __shfl_sync(0xffffffffu, run - sum, who);
-      i0 = __shfl_sync(0xffffffffu, i0, who);
-      i1 = __shfl_sync(0xffffffffu, i1, who);
-      for (int i = i0; i < i1; i += 32) {
-        u64 v = i + lane < i1 ? f(at(i + lane), base + i + lane) : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const u64 u = __shfl_up_sync(0xffffffffu, v, o);
-          if (lane >= o) v += u;
+        for (int q = 0; q < kPer; ++q) {
+          g[q] = p < end ? f(v[q], base + p * kPer + q - off) : 0;
+          sum += g[q];
         }
-        const uint32_t over = __ballot_sync(0xffffffffu, low + v > target);
-        if (over != 0) {
-          if (lane == 0) sh.number[2] = base + i + __ffs(over) - 1;
-          break;
+        const u64 upto = here + block_scan(sum);
+        u64 run = upto - sum;
+        if (run <= target && target < upto) {
+#pragma unroll
+          for (int q = 0; q < kPer; ++q) {
+            if (run <= target && target < run + g[q])
+              sh.word[1] = static_cast<u64>(base + p * kPer + q - off + 1) << 32 | __float_as_uint(v[q]);
+            run += g[q];
+          }
         }
-        low += __shfl_sync(0xffffffffu, v, 31);
+        __syncthreads();
+        here += block_total();
+        if (sh.word[1] != 0) break;
       }
     }
     __syncthreads();
-    box = exchange(static_cast<u64>(static_cast<long long>(sh.number[2]) + 1));
-    int found = -1;
-    for (int r = 0; r < ctas; ++r)
-      if (box[r] != 0) found = static_cast<int>(box[r]) - 1;
-    return found;
+    const u64* found = exchange(sh.word[1]);
+    u64 r = 0;
+    for (int i = 0; i < ctas; ++i) r |= found[i];
+    return r;
+  }
+  // What the last block_scan has summed in all.
+  __device__ __forceinline__ u64 block_total() const {
+    const u64* part = reinterpret_cast<const u64*>(sh.scan);
+    u64 s = 0;
+    for (int w = 0; w < kWarps; ++w) s += part[w];
+    return s;
   }
 
   // The last entry that a filter keeps, by the digits of its key: of the entries with `in`, by their number (`want` of them) or by their
   // mass (the first at which it reaches `want`).
   template <class In>
-  __device__ __forceinline__ void find_by_digits(const Weigh& w, In in, bool by_mass, u64 want, float& tx, int& ti) {
+  __device__ __noinline__ void find_by_digits(const Weigh& w, In in, bool by_mass, u64 want, float& tx, int& ti) {
     uint32_t prefix = 0, mask = 0;
     u64 ties = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -396,14 +463,13 @@ struct Row {
         sh.digit.count[t] = 0;
       }
       __syncthreads();
-      for (int i = w0 + lane; i < w1; i += 32) {
-        const float v = at(i);
+      for_each([&](float v, int i) {
         const uint32_t k = logit_key(v);
-        if (!in(v, base + i) || (k & mask) != prefix) continue;
+        if (!in(v, i) || (k & mask) != prefix) return;
         const int d = (k >> shift) & 255;
         atomicAdd(&sh.digit.count[d], 1u);
         if (by_mass) atomicAdd(&sh.digit.mass[d], w.weight(w.z(v)));
-      }
+      });
       sync();
       u64 mass = 0, count = 0;
       if (t < 256)
@@ -441,11 +507,13 @@ struct Row {
     const float x0 = tx;
     auto tie = [&](float v, int i) -> u64 { return v == x0 && in(v, i); };
     u64 s = 0;
-    for (int i = w0 + lane; i < w1; i += 32) s += tie(at(i), base + i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    for_each([&](float v, int i) { s += tie(v, i); });
+    s = warp_sum(s);
+    __syncthreads();
     if (lane == 0) sh.sums[warp] = s;
-    ti = locate(tie, want - 1);
+    __syncthreads();
+    const u64* box = exchange(block_sum(t < kWarps ? sh.sums[t] : 0));
+    ti = static_cast<int>(locate(tie, want - 1, box) >> 32) - 1;
   }
 };
 
@@ -458,57 +526,44 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   // between one and two, while nothing else can be done
   for (int i = t; i < kTable; i += kThreads) sh.table[i] = static_cast<u64>(exp2(static_cast<double>(i) / kTable) * 4611686018427387904.0);
   ptx::grid_dep_wait();
+  using R_t = Row<T, HELD>;
+  constexpr int kPer = R_t::kPer;
   const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-  Row<T, HELD> R{a, sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, nullptr, 0};
+  R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0};
   R.base = min(rank * span, a.V);
   R.n = min(span, a.V - R.base);
-  const int range = (R.n + kWarps - 1) / kWarps;
-  R.w0 = min(warp * range, R.n);
-  R.w1 = min(R.w0 + range, R.n);
+  const uintptr_t first = reinterpret_cast<uintptr_t>(src + R.base);
+  R.off = static_cast<int>(first & 15) / static_cast<int>(sizeof(T));
+  R.pieces = R.n > 0 ? (R.off + R.n + kPer - 1) / kPer : 0;
+  R.each = max(1, (R.pieces + kWarps - 1) / kWarps);
+  const Settings set = settings_of(a, row);
+  const int given = a.given != nullptr ? a.given[row] : CPMTP_EMBED_PAD;
+  const float u = a.uniform[row];
+  const bool writer = rank == 0 && t == 0;
+  float x_given = -INFINITY;
+  if (writer && given >= 0 && given < a.V) x_given = io::to_f(src[given]);
 
-  // ---- the entries, in whole 16-byte pieces that start before them if need be, and the largest
+  // ---- the entries, and the largest
   float top = -INFINITY;
   {
-    const uintptr_t first = reinterpret_cast<uintptr_t>(src + R.base);
-    const int off = static_cast<int>(first & 15) / static_cast<int>(sizeof(T));          // entries before the first in its piece
-    constexpr int kPer = 16 / sizeof(T);
-    const uint4* pieces = reinterpret_cast<const uint4*>(first & ~static_cast<uintptr_t>(15));
-    const int count = R.n > 0 ? (off + R.n + kPer - 1) / kPer : 0;
+    const uint4* from = reinterpret_cast<const uint4*>(first & ~static_cast<uintptr_t>(15));
     uint4* held = reinterpret_cast<uint4*>(smem + sizeof(Shared));
-    R.x = HELD ? reinterpret_cast<const T*>(held) + off : src + R.base;
+    R.data = HELD ? held : from;
     constexpr int kAhead = 8;
-    for (int i0 = t; i0 < count; i0 += kAhead * kThreads) {
-      uint4 v[kAhead];
+    for (int p0 = t; p0 < R.pieces; p0 += kAhead * kThreads) {
+      uint4 raw[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (p0 + j * kThreads < R.pieces) raw[j] = __ldg(from + p0 + j * kThreads);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + j * kThreads;
-        if (i < count) v[j] = __ldg(pieces + i);
-      }
+        const int p = p0 + j * kThreads;
+        if (p >= R.pieces) break;
+        if (HELD) held[p] = raw[j];
+        float v[kPer];
+        R.unpack(p, raw[j], v);
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + j * kThreads;
-        if (i >= count) break;
-        if (HELD) held[i] = v[j];
-        float e[kPer];
-        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (sizeof(T) == 4) {
-            e[q % kPer] = __uint_as_float(w[q]);
-          } else {
-            e[(2 * q) % kPer] = ptx::bf16_lo(w[q]);
-            e[(2 * q + 1) % kPer] = ptx::bf16_hi(w[q]);
-          }
-        }
-        if (i == 0 || i + 1 == count) {
-#pragma unroll
-          for (int q = 0; q < kPer; ++q) {
-            const int k = i * kPer + q - off;
-            if (k < 0 || k >= R.n) e[q] = -INFINITY;
-          }
-        }
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) top = fmaxf(top, e[q]);       // (which passes over NaN)
+        for (int q = 0; q < kPer; ++q) top = fmaxf(top, v[q]);       // (which passes over NaN)
       }
     }
   }
@@ -524,8 +579,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const u64* box = R.exchange(__float_as_uint(top));
     for (int r = 0; r < ctas; ++r) top = fmaxf(top, __uint_as_float(static_cast<uint32_t>(box[r])));
   }
-  const int given = a.given != nullptr ? a.given[row] : CPMTP_EMBED_PAD;
-  const bool writer = rank == 0 && t == 0;
   if (writer && given != CPMTP_EMBED_PAD && (given < 0 || given >= a.V) && dev_status != nullptr) atomicMax(dev_status, 1);
   auto answer = [&](int token, float logp, int kept, float logp_given) {
     if (!writer) return;
@@ -538,154 +591,136 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     answer(-1, -INFINITY, 0, -INFINITY);
     return;                                  // (the same in every block of the cluster, after its barrier)
   }
-  const Settings set = settings_of(a, row);
   if (set.one) {
     // the first of the largest
-    u64 none = 0;                            // 2^31 - index: the lowest is the largest
-    for (int i = R.w0 + lane; i < R.w1; i += 32)
-      if (R.at(i) == top) none = max(none, static_cast<u64>((1u << 31) - (R.base + i)));
+    u64 best = 0;                            // 2^31 - index: the lowest is the largest
+    R.for_each([&](float v, int i) {
+      if (v == top) best = max(best, static_cast<u64>((1u << 31) - i));
+    });
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) none = max(none, __shfl_xor_sync(0xffffffffu, none, o));
+    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
     __syncthreads();
-    if (lane == 0) sh.sums[warp] = none;
+    if (lane == 0) sh.sums[warp] = best;
     __syncthreads();
-    for (int w = 0; w < kWarps; ++w) none = max(none, sh.sums[w]);
-    const u64* box = R.exchange(none);
-    for (int r = 0; r < ctas; ++r) none = max(none, box[r]);
-    const int token = static_cast<int>((1u << 31) - static_cast<uint32_t>(none));
+    for (int w = 0; w < kWarps; ++w) best = max(best, sh.sums[w]);
+    const u64* box = R.exchange(best);
+    for (int r = 0; r < ctas; ++r) best = max(best, box[r]);
+    const int token = static_cast<int>((1u << 31) - static_cast<uint32_t>(best));
     answer(token, 0.f, 1, given == token ? 0.f : -INFINITY);
     return;
   }
   Weigh w;
-  w.m = static_cast<double>(top);
-  w.c = set.inv_t * 1.4426950408889634074;
-  w.mf = top;
-  w.cf = static_cast<float>(fmin(w.c, 3e38));
-  w.inf = top == INFINITY;
-  w.down = 62 - bits;
+  w.set(top, set.inv_t, bits);
   w.table = sh.table;
   const double unit = static_cast<double>(1ull << bits);
-  long long z_min = kNoWeight;               // of min_p
-  if (set.min_p > 0.0) {
-    const double l = log2(set.min_p);
-    z_min = l > -59.0 ? static_cast<long long>(ceil(l * 4294967296.0)) : kNoWeight;
-  }
-  const float u = a.uniform[row];
+  const long long z_min = set.min_p > 0.0 ? static_cast<long long>(ceil(log2(set.min_p) * 4294967296.0)) : -(1ll << 62);
   auto target_of = [&](u64 total) {
     return u > 0.f ? (u < 1.f ? min(static_cast<u64>(static_cast<double>(u) * static_cast<double>(total)), total - 1) : total - 1) : 0;
   };
-  auto finish = [&](int token, u64 total, int kept, float tx, int ti) {
+  auto finish = [&](int token, float x_token, u64 total, int kept, float tx, int ti) {
     if (!writer || token < 0) return;
     const double all = log(static_cast<double>(total) / unit);
     auto logp = [&](float v) { return static_cast<float>((v == top ? 0.0 : (static_cast<double>(v) - w.m) * set.inv_t) - all); };
-    float lg = -INFINITY;
-    if (given >= 0 && given < a.V) {
-      const float v = io::to_f(src[given]);
-      if ((v > tx || (v == tx && given <= ti)) && w.z(v) >= z_min) lg = logp(v);
-    }
-    answer(token, logp(io::to_f(src[token])), kept, lg);
+    const bool in = x_given > -INFINITY && (x_given > tx || (x_given == tx && given <= ti)) && w.z(x_given) >= z_min;
+    answer(token, logp(x_token), kept, in ? logp(x_given) : -INFINITY);
   };
 
   // ---- entries x > tx, and x == tx up to index ti, are kept
   float tx = -INFINITY;
-  int ti = -1;
+  int ti = INT_MIN;                          // (nothing: places before a piece's first entry have negative numbers)
   auto kept_by = [&](float v, int i) { return v > tx || (v == tx && i <= ti); };
 
   // ---- top-k
-  u64 valid = 0;
   if (set.top_k < a.V) {
-    for (int i = R.w0 + lane; i < R.w1; i += 32) valid += R.at(i) > -INFINITY;
-    valid = R.row_sum(valid);
-  }
-  if (static_cast<u64>(set.top_k) < valid) {
     bool found = false;
-    if (!w.inf) {
+    u64 valid = 0;
+    if (!w.odd) {
       // bins of 1/64 in units of ln 2 of the logits themselves; the magic number rounds to integers
       const float step = 64.f * 1.4426950408889634f;
       auto bin_of = [&](float v) { return __float_as_uint(fminf(fmaf(top - v, step, 8388608.f), 8388608.f + (kBins - 1))) & 0x7fffffu; };
       R.clear_hist();
-      for (int i = R.w0 + lane; i < R.w1; i += 32) {
-        const float v = R.at(i);
+      R.for_each([&](float v, int) {
         if (v > -INFINITY) atomicAdd(&sh.hist[bin_of(v)], 1u);
-      }
+      });
       int b, b2;
       double before;
-      R.find_bins([](int) { return 1.0; }, set.top_k, set.top_k, b, b2, before);
-      // all entries down to that bin, if they are few; else those of the bin
-      const bool all = before + kList / 2 <= kList && b < kBins - 1;
-      const uint32_t from = all ? 0 : b;
-      for (int i0 = R.w0; i0 < R.w1; i0 += 32) {
-        const int i = i0 + lane;
-        const float v = i < R.w1 ? R.at(i) : -INFINITY;
-        const uint32_t k = bin_of(v);
-        R.list_add(v > -INFINITY && k >= from && k <= static_cast<uint32_t>(b), v, R.base + i);
-      }
-      const int count = R.gather_list();
-      if (count <= kList && all) {
-        // the rest is block 0's alone
-        R.sync();
-        if (rank != 0) return;
-        R.sort_list(count);
-        u64 v[4];
-        long long z[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * t + j;
-          z[j] = i < set.top_k ? w.z(R.entry_logit(sh.list[i])) : kNoWeight;
-          v[j] = i < set.top_k ? w.weight(z[j]) : 0;
-        }
-        u64 own[4] = {v[0], v[1], v[2], v[3]};
-        R.scan4(v);
-        if (t == kThreads - 1) sh.word[3] = v[3];
+      valid = static_cast<u64>(R.find_bins([](int) { return 1.0; }, set.top_k, set.top_k, b, b2, before));
+      if (static_cast<u64>(set.top_k) < valid) {
+        // all entries down to that bin, if they are few; else those of the bin
+        const bool all = before + kList / 2 <= kList && b < kBins - 1;
+        const uint32_t from = all ? 0 : b;
+        R.for_each([&](float v, int i) {
+          const uint32_t k = bin_of(v);
+          if (k <= static_cast<uint32_t>(b) && k >= from && v > -INFINITY) R.list_add(v, i);
+        });
         __syncthreads();
-        const double border = set.top_p * static_cast<double>(sh.word[3]);
-        u64 left = 0;
+        const int count = R.gather_list(R.exchange(sh.listed));
+        if (count <= kList && all) {
+          // the rest is block 0's alone
+          R.sync();
+          if (rank != 0) return;
+          R.sort_list(count);
+          u64 v[4], own[4];
+          long long z[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * t + j;
-          left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && z[j] >= z_min;
-        }
-        const int kept = static_cast<int>(R.block_sum(left));
-        if (kept - 1 >= 4 * t && kept - 1 < 4 * t + 4) {
+          for (int j = 0; j < 4; ++j) {
+            const int i = 4 * t + j;
+            z[j] = i < set.top_k ? w.z(R.entry_logit(sh.list[i])) : 0;
+            own[j] = v[j] = i < set.top_k ? w.weight(z[j]) : 0;
+          }
+          R.scan4(v);
+          const double border = set.top_p * static_cast<double>(R.block_total());
+          u64 left = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 4 * t + j;
+            left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && z[j] >= z_min;
+          }
+          const int kept = static_cast<int>(R.block_sum(left));
+          if (kept - 1 >= 4 * t && kept - 1 < 4 * t + 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (kept - 1 == 4 * t + j) sh.word[2] = v[j];
+          }
+          __syncthreads();
+          const u64 total = sh.word[2], last = sh.list[kept - 1];
+          // by index: the keys' halves change places (and fall, so the index is inverted as it stands)
+          __syncthreads();
+          for (int i = t; i < kept; i += kThreads) sh.list[i] = sh.list[i] << 32 | sh.list[i] >> 32;
+          R.sort_list(kept);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 4 * t + j;
+            own[j] = v[j] = i < kept ? w.weight(w.z(key_logit(static_cast<uint32_t>(sh.list[i])))) : 0;
+          }
+          R.scan4(v);
+          const u64 target = target_of(total);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (kept - 1 == 4 * t + j) sh.word[2] = v[j];
+            if (v[j] > target && v[j] - own[j] <= target) sh.word[3] = sh.list[4 * t + j];
+          __syncthreads();
+          finish(static_cast<int>(~static_cast<uint32_t>(sh.word[3] >> 32)), key_logit(static_cast<uint32_t>(sh.word[3])), total, kept,
+                 R.entry_logit(last), R.entry_index(last));
+          return;
         }
-        __syncthreads();
-        const u64 total = sh.word[2], last = sh.list[kept - 1];
-        // by index: the keys' halves change places (and fall, so the index is inverted as it stands)
-        __syncthreads();
-        for (int i = t; i < kept; i += kThreads) sh.list[i] = sh.list[i] << 32 | sh.list[i] >> 32;
-        R.sort_list(kept);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * t + j;
-          v[j] = i < kept ? w.weight(w.z(key_logit(static_cast<uint32_t>(sh.list[i])))) : 0;
+        if (count <= kList) {
+          const int nth = set.top_k - static_cast<int>(before) - 1;          // of the bin's entries, the last that is kept
+          if (rank == 0) {
+            R.sort_list(count);
+            if (t < ctas) store_remote(&sh.word[2], t, sh.list[nth]);
+          }
+          R.sync();
+          tx = R.entry_logit(sh.word[2]);
+          ti = R.entry_index(sh.word[2]);
+          found = true;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) own[j] = v[j];
-        R.scan4(v);
-        const u64 target = target_of(total);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (v[j] > target && v[j] - own[j] <= target) sh.number[2] = static_cast<int>(~static_cast<uint32_t>(sh.list[4 * t + j] >> 32));
-        __syncthreads();
-        finish(sh.number[2], total, kept, R.entry_logit(last), R.entry_index(last));
-        return;
       }
-      if (count <= kList) {
-        const int nth = set.top_k - static_cast<int>(before) - 1;          // of the bin's entries, the last that is kept
-        if (rank == 0) {
-          R.sort_list(count);
-          if (t < ctas) store_remote(&sh.word[2], t, sh.list[nth]);
-        }
-        R.sync();
-        tx = R.entry_logit(sh.word[2]);
-        ti = R.entry_index(sh.word[2]);
-        found = true;
-      }
+    } else {
+      R.for_each([&](float v, int) { valid += v > -INFINITY; });
+      valid = R.row_sum(valid);
     }
-    if (!found) R.find_by_digits(w, [](float v, int) { return v > -INFINITY; }, false, set.top_k, tx, ti);
+    if (!found && static_cast<u64>(set.top_k) < valid)
+      R.find_by_digits(w, [](float v, int) { return v > -INFINITY; }, false, set.top_k, tx, ti);
   }
 
   // ---- top-p, and the kept mass of every warp's range
@@ -695,18 +730,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int less = max(0, 32 - __clz(span - 1) - 14);                    // bits that the histogram's sums have to do without
     u64 mass = 0;
     R.clear_hist();
-    for (int i = R.w0 + lane; i < R.w1; i += 32) {
-      const float v = R.at(i);
-      if (!kept_by(v, R.base + i)) continue;
+    R.for_each([&](float v, int i) {
+      if (!kept_by(v, i)) return;
       const long long z = w.z(v);
       const u64 q = w.mantissa(z);
       mass += w.fixed(q, z);
-      if (z > kNoWeight) atomicAdd(&sh.hist[min(static_cast<int>(-(z >> 26)), kBins - 1)], static_cast<uint32_t>(q >> (45 + less)));
-    }
+      atomicAdd(&sh.hist[min(static_cast<int>(-(z >> 26)), kBins - 1)], static_cast<uint32_t>(q >> (45 + less)));
+    });
     mass = R.row_sum(mass);
     const double border = set.top_p * static_cast<double>(mass);
     bool found = false;
-    if (!w.inf) {
+    if (!w.odd) {
       // an entry of bin b has floor(z) = -ceil(b / 64); the sums are short by 2^(less - 17) at most
       const double one = unit * ldexp(1.0, less - 17), slack = ldexp(1.0, less - 15);
       int b1, b2;
@@ -716,11 +750,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       const float xa = nextafterf(__double2float_ru(w.m - (b1 - 1) / (64.0 * w.c)), INFINITY);
       const float xb = b2 == kBins - 1 ? -FLT_MAX : nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY);
       u64 above = 0;
-      for (int i0 = R.w0; i0 < R.w1; i0 += 32) {
-        const int i = i0 + lane;
-        const float v = i < R.w1 ? R.at(i) : -INFINITY;
-        const bool in = v >= xb && kept_by(v, R.base + i);
-        if (in && v > xa) {
+      R.for_each([&](float v, int i) {
+        if (!(v >= xb && kept_by(v, i))) return;
+        if (v > xa) {
           const long long z = w.z(v);
           const u64 q = w.weight(z);
           above += q;
@@ -728,16 +760,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             sum += q;
             ++number;
           }
+        } else {
+          R.list_add(v, i);
         }
-        R.list_add(in && !(v > xa), v, R.base + i);
-      }
-      above = R.row_sum(above);
-      const int mine = min(sh.listed, kList);
-      const int count = R.gather_list();
+      });
+      above = R.block_sum(above);
+      const int mine = sh.listed;
+      const u64* box = R.exchange(above, mine);
+      above = R.sum_of(box);
+      const int count = R.gather_list(box + kMostCtas);
       if (count <= kList) {
         if (rank == 0) {
-          // (the keys of the other blocks lie behind this block's own, which it needs again: they are sorted in place, so its own
-          // entries' shares are found from the sorted list by index)
+          // (its own entries stay in the list: their shares are found by index)
           R.sort_list(count);
           u64 v[4], own[4];
 #pragma unroll
@@ -763,18 +797,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           tx = R.entry_logit(last);
           ti = R.entry_index(last);
           // the listed entries that are kept, to the sums of the ranges they lie in
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          sum = R.warp_sum(sum);
           if (lane == 0) sh.sums[warp] = sum;
           __syncthreads();
           for (int i = t; i < (rank == 0 ? count : mine); i += kThreads) {
             const u64 e = sh.list[i];
-            const int index = R.entry_index(e) - R.base;
-            if (e < last || index < 0 || index >= R.n) continue;
+            const int index = R.entry_index(e);
+            if (e < last || index < R.base || index >= R.base + R.n) continue;
             const long long z = w.z(R.entry_logit(e));
             if (z < z_min) continue;
             ++number;
-            atomicAdd(&sh.sums[index / range], w.weight(z));
+            atomicAdd(&sh.sums[R.warp_of(index)], w.weight(z));
           }
         }
       }
@@ -792,24 +825,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return z >= z_min ? w.weight(z) : 0;
   };
   if (!counted) {
-    for (int i = R.w0 + lane; i < R.w1; i += 32) {
-      const float v = R.at(i);
-      if (!kept_by(v, R.base + i)) continue;
+    R.for_each([&](float v, int i) {
+      if (!kept_by(v, i)) return;
       const long long z = w.z(v);
-      if (z < z_min) continue;
+      if (z < z_min) return;
       sum += w.weight(z);
       ++number;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    });
+    sum = R.warp_sum(sum);
     __syncthreads();
     if (lane == 0) sh.sums[warp] = sum;
   }
-  __syncthreads();
-  u64 total = R.row_sum(t < kWarps ? sh.sums[t] : 0);
-  number = R.row_sum(number);
-  const int token = R.locate(drawn, target_of(total));
-  finish(token, total, static_cast<int>(number), tx, ti);
+  number = R.block_sum(number);                        // (a barrier: the warps' sums are complete)
+  const u64 here = R.block_sum(t < kWarps ? sh.sums[t] : 0);
+  const u64* box = R.exchange(here, number);
+  const u64 total = R.sum_of(box);
+  number = R.sum_of(box + kMostCtas);
+  const u64 token = R.locate(drawn, target_of(total), box);
+  finish(static_cast<int>(token >> 32) - 1, __uint_as_float(static_cast<uint32_t>(token)), total, static_cast<int>(number), tx, ti);
 }
 
 }  // namespace sample
