@@ -85,50 +85,59 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-constexpr long long kNoWeight = -(160ll << 32);      // z of entries that have none: below that of the least min_p (2^-149)
+// z <= 0 with 32 bits below the point, in two words.
+struct Fixed {
+  int whole;             // floor(z)
+  uint32_t part;         // z - floor(z)
+};
+// Conditions of the inner loops are put together without branches, which would cost more than what they skip.
+__device__ __forceinline__ bool at_least(Fixed z, Fixed least) {
+  return (static_cast<long long>(z.whole) << 32 | z.part) >= (static_cast<long long>(least.whole) << 32 | least.part);
+}
+__device__ __forceinline__ u64 only_if(bool c, u64 v) { return v & -static_cast<u64>(c); }
 
 struct Weigh {
   double m, c;           // largest logit; log2(e) / T
-  float x_min;           // logits below it have no weight
-  float mf, cf;
-  bool odd;              // the largest logit is infinite, or the next one below it is out of the range of z
+  float x_min, x_max;    // what logits are limited to: below the one is no weight, above the other is nothing
   int down;              // 62 minus the bits below the point
-  const u64* table;
+  uint32_t table;        // address in shared memory
 
-  // (x - m) c with 32 bits below the point: the product is added to a number whose last bit is 2^-32.
-  __device__ __forceinline__ long long z(float x) const {
-    constexpr double kMagic = 1572864.0;               // 1.5 x 2^20
-    if (odd && !(x == mf || (x - mf) * cf > -160.f)) return kNoWeight;
-    if (odd && x == mf) return 0;
-    return __double_as_longlong(fma(static_cast<double>(fmaxf(x, x_min)) - m, c, kMagic)) - 0x4138000000000000ll;
-  }
+  // A weight below 2^-160 is none (the least min_p is 2^-149).  Where the next number below the largest logit is further away
+  // than that, it is put at 2^-1000, so that z has always few enough digits before the point; so is everything below an infinite one, for
+  // which the largest finite number stands.
   __device__ __forceinline__ void set(float top, double inv_t, int bits) {
-    m = static_cast<double>(top);
+    x_max = fminf(top, FLT_MAX);
+    m = static_cast<double>(x_max);
     c = inv_t * 1.4426950408889634074;
-    mf = top;
-    cf = static_cast<float>(fmin(c, 3e38));
     const double low = m - 160.0 / c;                  // (c may be 0: minus infinity)
     x_min = low > -FLT_MAX ? __double2float_rd(low) : -FLT_MAX;
-    odd = !(x_min < top) || !((m - static_cast<double>(x_min)) * c < 1000.0);
+    if (top > x_max || !(x_min < top) || !((m - static_cast<double>(x_min)) * c < 1000.0)) {
+      x_min = nextafterf(x_max, -INFINITY);
+      if (x_min >= -FLT_MAX) c = 1000.0 / (m - static_cast<double>(x_min));
+    }
     down = 62 - bits;
+  }
+  // (x - m) c: the product is added to a number whose last bit is 2^-32.
+  __device__ __forceinline__ Fixed z(float x) const {
+    constexpr double kMagic = 1572864.0;               // 1.5 x 2^20
+    const double v = fma(static_cast<double>(fminf(fmaxf(x, x_min), x_max)) - m, c, kMagic);
+    return Fixed{__double2hiint(v) - 0x41380000, static_cast<uint32_t>(__double2loint(v))};
   }
   // 2^(z - floor(z)) with 62 bits below the point.  The leading ten bits by table, the others by three terms of the series of
   // 2^r - 1, r < 2^-10, in fp32: an error of 2^-24 of a number below 2^-10.5.  With the 2^-33 of z and the 2^-34 of its own
   // rounding below 2^-32 in all.
-  __device__ __forceinline__ u64 mantissa(long long z) const {
-    const uint32_t f = static_cast<uint32_t>(z);
-    const u64 t = table[f >> 22];
-    const float r = __uint_as_float(0x3f800000u | (f & 0x3fffffu) << 1) - 1.f;           // in units of 2^-10
-    constexpr double kA = 0.69314718055994530942 / 1024.0, kS = 8589934592.0;            // ln 2 2^-10; 2^33
+  __device__ __forceinline__ u64 mantissa(Fixed z) const {
+    u64 e;
+    asm("ld.shared.u64 %0, [%1];" : "=l"(e) : "r"(table + ((z.part >> 22) << 3)));
+    const float r = __uint_as_float(0x3f800000u | (z.part & 0x3fffffu) << 1) - 1.f;           // in units of 2^-10
+    constexpr double kA = 0.69314718055994530942 / 1024.0, kS = 8589934592.0;                 // ln 2 2^-10; 2^33
     const float q = fmaf(r, fmaf(r, static_cast<float>(kA * kA * kA / 6.0 * kS), static_cast<float>(kA * kA / 2.0 * kS)), static_cast<float>(kA * kS));
     const uint32_t n = __float_as_uint(fmaf(r, q, 8388608.f)) & 0x7fffffu;
-    return t + ((static_cast<u64>(static_cast<uint32_t>(t >> 32)) * n) >> 1);
+    return e + static_cast<u64>(static_cast<uint32_t>(e >> 33)) * n;
   }
-  __device__ __forceinline__ u64 fixed(u64 mantissa, long long z) const {
-    const int s = down - static_cast<int>(z >> 32);
-    return s < 64 ? mantissa >> s : 0;
-  }
-  __device__ __forceinline__ u64 weight(long long z) const { return fixed(mantissa(z), z); }
+  __device__ __forceinline__ u64 fixed(u64 mantissa, Fixed z) const { return mantissa >> min(down - z.whole, 63); }
+  __device__ __forceinline__ u64 weight(Fixed z) const { return fixed(mantissa(z), z); }
+  __device__ __forceinline__ u64 weight(float x) const { return weight(z(x)); }
 };
 
 struct Settings {
@@ -160,7 +169,8 @@ struct Row {
   int base, n;           // this block's entries
   int off;               // entries of the first piece that lie before them
   int pieces, each;      // pieces of the block, of a warp
-  const uint4* data;
+  const uint4* data;     // the pieces: in memory, or ...
+  uint32_t held;         // ... their address in shared memory
   int boxes;
 
   __device__ __forceinline__ void sync() const { sync_row(ctas); }
@@ -184,12 +194,17 @@ struct Row {
       }
     }
   }
-  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const { unpack(piece, HELD ? data[piece] : __ldg(data + piece), v); }
+  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const {
+    uint4 raw;
+    if (HELD) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(held + piece * 16));
+    else raw = __ldg(data + piece);
+    unpack(piece, raw, v);
+  }
   // f(logit, index in the row) for the entries of this warp's pieces.
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
     const int end = min((warp + 1) * each, pieces);
-#pragma unroll 2
+#pragma unroll 1
     for (int p = warp * each + lane; p < end; p += 32) {
       float v[kPer];
       load(p, v);
@@ -468,7 +483,7 @@ struct Row {
         if (!in(v, i) || (k & mask) != prefix) return;
         const int d = (k >> shift) & 255;
         atomicAdd(&sh.digit.count[d], 1u);
-        if (by_mass) atomicAdd(&sh.digit.mass[d], w.weight(w.z(v)));
+        if (by_mass) atomicAdd(&sh.digit.mass[d], w.weight(v));
       });
       sync();
       u64 mass = 0, count = 0;
@@ -499,7 +514,7 @@ struct Row {
     }
     tx = key_logit(prefix);
     if (by_mass) {
-      const u64 one = w.weight(w.z(tx));
+      const u64 one = w.weight(tx);
       want = one > 0 ? (want + one - 1) / one : 1;
     }
     want = want < 1 ? 1 : want > ties ? ties : want;
@@ -529,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   using R_t = Row<T, HELD>;
   constexpr int kPer = R_t::kPer;
   const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-  R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0};
+  R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0, 0};
   R.base = min(rank * span, a.V);
   R.n = min(span, a.V - R.base);
   const uintptr_t first = reinterpret_cast<uintptr_t>(src + R.base);
@@ -548,7 +563,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   {
     const uint4* from = reinterpret_cast<const uint4*>(first & ~static_cast<uintptr_t>(15));
     uint4* held = reinterpret_cast<uint4*>(smem + sizeof(Shared));
-    R.data = HELD ? held : from;
+    R.data = from;
+    R.held = ptx::smem_u32(held);
     constexpr int kAhead = 8;
     for (int p0 = t; p0 < R.pieces; p0 += kAhead * kThreads) {
       uint4 raw[kAhead];
@@ -611,9 +627,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
   Weigh w;
   w.set(top, set.inv_t, bits);
-  w.table = sh.table;
+  w.table = ptx::smem_u32(sh.table);
   const double unit = static_cast<double>(1ull << bits);
-  const long long z_min = set.min_p > 0.0 ? static_cast<long long>(ceil(log2(set.min_p) * 4294967296.0)) : -(1ll << 62);
+  const long long z_least = set.min_p > 0.0 ? static_cast<long long>(ceil(log2(set.min_p) * 4294967296.0)) : -(1ll << 62);
+  const Fixed z_min{static_cast<int>(z_least >> 32), static_cast<uint32_t>(z_least)};
   auto target_of = [&](u64 total) {
     return u > 0.f ? (u < 1.f ? min(static_cast<u64>(static_cast<double>(u) * static_cast<double>(total)), total - 1) : total - 1) : 0;
   };
@@ -621,20 +638,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (!writer || token < 0) return;
     const double all = log(static_cast<double>(total) / unit);
     auto logp = [&](float v) { return static_cast<float>((v == top ? 0.0 : (static_cast<double>(v) - w.m) * set.inv_t) - all); };
-    const bool in = x_given > -INFINITY && (x_given > tx || (x_given == tx && given <= ti)) && w.z(x_given) >= z_min;
+    const bool in = x_given > -INFINITY && (x_given > tx || (x_given == tx && given <= ti)) && at_least(w.z(x_given), z_min);
     answer(token, logp(x_token), kept, in ? logp(x_given) : -INFINITY);
   };
 
   // ---- entries x > tx, and x == tx up to index ti, are kept
   float tx = -INFINITY;
   int ti = INT_MIN;                          // (nothing: places before a piece's first entry have negative numbers)
-  auto kept_by = [&](float v, int i) { return v > tx || (v == tx && i <= ti); };
+  auto kept_by = [&](float v, int i) { return (v > tx) | ((v == tx) & (i <= ti)); };
 
   // ---- top-k
   if (set.top_k < a.V) {
     bool found = false;
     u64 valid = 0;
-    if (!w.odd) {
+    if (top < INFINITY) {
       // bins of 1/64 in units of ln 2 of the logits themselves; the magic number rounds to integers
       const float step = 64.f * 1.4426950408889634f;
       auto bin_of = [&](float v) { return __float_as_uint(fminf(fmaf(top - v, step, 8388608.f), 8388608.f + (kBins - 1))) & 0x7fffffu; };
@@ -661,11 +678,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           if (rank != 0) return;
           R.sort_list(count);
           u64 v[4], own[4];
-          long long z[4];
+          Fixed z[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int i = 4 * t + j;
-            z[j] = i < set.top_k ? w.z(R.entry_logit(sh.list[i])) : 0;
+            z[j] = w.z(i < set.top_k ? R.entry_logit(sh.list[i]) : top);
             own[j] = v[j] = i < set.top_k ? w.weight(z[j]) : 0;
           }
           R.scan4(v);
@@ -674,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int i = 4 * t + j;
-            left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && z[j] >= z_min;
+            left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && at_least(z[j], z_min);
           }
           const int kept = static_cast<int>(R.block_sum(left));
           if (kept - 1 >= 4 * t && kept - 1 < 4 * t + 4) {
@@ -691,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int i = 4 * t + j;
-            own[j] = v[j] = i < kept ? w.weight(w.z(key_logit(static_cast<uint32_t>(sh.list[i])))) : 0;
+            own[j] = v[j] = i < kept ? w.weight(key_logit(static_cast<uint32_t>(sh.list[i]))) : 0;
           }
           R.scan4(v);
           const u64 target = target_of(total);
@@ -724,23 +741,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
 
   // ---- top-p, and the kept mass of every warp's range
-  u64 sum = 0, number = 0;
+  u64 sum = 0;
+  uint32_t number = 0;
   bool counted = false;
   if (set.top_p < 1.0) {
     const int less = max(0, 32 - __clz(span - 1) - 14);                    // bits that the histogram's sums have to do without
     u64 mass = 0;
     R.clear_hist();
     R.for_each([&](float v, int i) {
-      if (!kept_by(v, i)) return;
-      const long long z = w.z(v);
+      const bool in = kept_by(v, i);
+      const Fixed z = w.z(v);
       const u64 q = w.mantissa(z);
-      mass += w.fixed(q, z);
-      atomicAdd(&sh.hist[min(static_cast<int>(-(z >> 26)), kBins - 1)], static_cast<uint32_t>(q >> (45 + less)));
+      mass += only_if(in, w.fixed(q, z));
+      // (an entry of bin b has -b <= 64 z < 1 - b)
+      if (in) atomicAdd(&sh.hist[min(-(z.whole * 64 + static_cast<int>(z.part >> 26)), kBins - 1)], static_cast<uint32_t>(q >> 45) >> less);
     });
     mass = R.row_sum(mass);
     const double border = set.top_p * static_cast<double>(mass);
     bool found = false;
-    if (!w.odd) {
+    {
       // an entry of bin b has floor(z) = -ceil(b / 64); the sums are short by 2^(less - 17) at most
       const double one = unit * ldexp(1.0, less - 17), slack = ldexp(1.0, less - 15);
       int b1, b2;
@@ -753,13 +772,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       R.for_each([&](float v, int i) {
         if (!(v >= xb && kept_by(v, i))) return;
         if (v > xa) {
-          const long long z = w.z(v);
+          const Fixed z = w.z(v);
           const u64 q = w.weight(z);
+          const bool in = at_least(z, z_min);
           above += q;
-          if (z >= z_min) {
-            sum += q;
-            ++number;
-          }
+          sum += only_if(in, q);
+          number += in;
         } else {
           R.list_add(v, i);
         }
@@ -775,7 +793,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           R.sort_list(count);
           u64 v[4], own[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) own[j] = v[j] = 4 * t + j < count ? w.weight(w.z(R.entry_logit(sh.list[4 * t + j]))) : 0;
+          for (int j = 0; j < 4; ++j) own[j] = v[j] = 4 * t + j < count ? w.weight(R.entry_logit(sh.list[4 * t + j])) : 0;
           R.scan4(v);
           u64 left = 0;
           bool reached = false;
@@ -804,8 +822,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             const u64 e = sh.list[i];
             const int index = R.entry_index(e);
             if (e < last || index < R.base || index >= R.base + R.n) continue;
-            const long long z = w.z(R.entry_logit(e));
-            if (z < z_min) continue;
+            const Fixed z = w.z(R.entry_logit(e));
+            if (!at_least(z, z_min)) continue;
             ++number;
             atomicAdd(&sh.sums[R.warp_of(index)], w.weight(z));
           }
@@ -820,29 +838,27 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
   }
   auto drawn = [&](float v, int i) -> u64 {
-    if (!kept_by(v, i)) return 0;
-    const long long z = w.z(v);
-    return z >= z_min ? w.weight(z) : 0;
+    const Fixed z = w.z(v);
+    return only_if(kept_by(v, i) & at_least(z, z_min), w.weight(z));
   };
   if (!counted) {
     R.for_each([&](float v, int i) {
-      if (!kept_by(v, i)) return;
-      const long long z = w.z(v);
-      if (z < z_min) return;
-      sum += w.weight(z);
-      ++number;
+      const Fixed z = w.z(v);
+      const bool in = kept_by(v, i) & at_least(z, z_min);
+      sum += only_if(in, w.weight(z));
+      number += in;
     });
     sum = R.warp_sum(sum);
     __syncthreads();
     if (lane == 0) sh.sums[warp] = sum;
   }
-  number = R.block_sum(number);                        // (a barrier: the warps' sums are complete)
+  const u64 numbers = R.block_sum(number);             // (a barrier: the warps' sums are complete)
   const u64 here = R.block_sum(t < kWarps ? sh.sums[t] : 0);
-  const u64* box = R.exchange(here, number);
+  const u64* box = R.exchange(here, numbers);
   const u64 total = R.sum_of(box);
-  number = R.sum_of(box + kMostCtas);
+  const int kept = static_cast<int>(R.sum_of(box + kMostCtas));
   const u64 token = R.locate(drawn, target_of(total), box);
-  finish(static_cast<int>(token >> 32) - 1, __uint_as_float(static_cast<uint32_t>(token)), total, static_cast<int>(number), tx, ti);
+  finish(static_cast<int>(token >> 32) - 1, __uint_as_float(static_cast<uint32_t>(token)), total, kept, tx, ti);
 }
 
 }  // namespace sample
