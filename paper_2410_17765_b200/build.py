@@ -13,7 +13,7 @@ DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libcpmtp_debug.so")   # the same sources
 SOURCES = ["cpmtp_api.cu", "train_api.cu", "serve_api.cu"]
 HEADERS = ["ptx.cuh", "tmap.cuh", "tc_gemm.cuh", "epilogues.cuh", "small_kernels.cuh", "sampler_kernels.cuh",
            "distill_epilogues.cuh", "distill_kernels.cuh", "host_util.cuh", "vec_io.cuh", "embed_kernels.cuh", "norm_kernels.cuh",
-           "adamw_kernels.cuh", "cache_kernels.cuh", "attend_kernels.cuh", "sample_kernels.cuh"]
+           "adamw_kernels.cuh", "cluster.cuh", "cache_kernels.cuh", "attend_kernels.cuh", "sample_kernels.cuh"]
 
 
 def _nvcc() -> str:

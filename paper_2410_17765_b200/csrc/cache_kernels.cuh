@@ -3,6 +3,7 @@
 #include <cstdint>
 
 #include "../../include/cpmtp.h"
+#include "cluster.cuh"
 #include "ptx.cuh"
 #include "vec_io.cuh"
 
@@ -37,156 +38,269 @@ __device__ __forceinline__ int page_of(int page, int pages, int* dev_status) {
 }
 
 constexpr int kThreads = 256;
+constexpr int kRows = 32;              // rows (a key and a value) that a warp moves: one for each lane to look up
+constexpr int kAhead = 8;              // 16-byte pieces that a lane has under way
 
-// One thread for each piece of eight elements of a new token's key and value in one head.
+// A warp moves the keys and values of rows 0 .. count - 1 of one head, a piece of eight elements to a lane: the lanes of a row have
+// its key's pieces, then its value's.  from(row), to(row): addresses of row `row`, which lane `row` has looked up; row_ok: what lane `row` found.
+struct Place {
+  int page, slot;        // page < 0: nothing
+};
+template <class From, class To, class Move>
+__device__ __forceinline__ void move_rows(int pieces, Place src, Place dst, From from, To to, Move move) {
+  const int lane = threadIdx.x & 31, width = 2 * pieces, at_once = 32 / width;
+  const int sub = lane / width, piece = lane % width;
+  const bool value = piece >= pieces, on = sub < at_once;
+  const int col = 8 * (value ? piece - pieces : piece);
+  const uint32_t some = __ballot_sync(0xffffffffu, src.page >= 0 && dst.page >= 0);
+  for (int r0 = 0; r0 < kRows && (some >> r0) != 0; r0 += kAhead * at_once) {
+    uint4 v[kAhead];
+    bool ok[kAhead];
+    Place d[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int r = r0 + i * at_once + sub, who = r & 31;
+      const Place s{__shfl_sync(0xffffffffu, src.page, who), __shfl_sync(0xffffffffu, src.slot, who)};
+      d[i] = Place{__shfl_sync(0xffffffffu, dst.page, who), __shfl_sync(0xffffffffu, dst.slot, who)};
+      ok[i] = on && r < kRows && (some >> who & 1);
+      if (ok[i]) v[i] = move(from(value, s, col));
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (ok[i]) *reinterpret_cast<uint4*>(to(value, d[i], col)) = v[i];
+  }
+}
+__device__ __forceinline__ bf16_t* cached(const cpmtp_cache& c, bool value, Place p, int h) {
+  return value ? static_cast<bf16_t*>(c.v) + p.page * c.v_page + p.slot * c.v_slot + h * c.v_head
+               : static_cast<bf16_t*>(c.k) + p.page * c.k_page + p.slot * c.k_slot + h * c.k_head;
+}
+
+// A warp for each 32 new tokens of a sequence and head.  It is the cache lines that bound it: 8192 tokens of 8 x 128 move 101 MB.
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
                                                           const __grid_constant__ cpmtp_tokens k, const __grid_constant__ cpmtp_tokens v,
                                                           int* dev_status) {
+  const int lane = threadIdx.x & 31, groups = (s.Q + kRows - 1) / kRows;
+  const long long unit = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   ptx::grid_dep_wait();
-  const int pieces = c.D / 8;
-  const long long items = static_cast<long long>(s.B) * s.Q * c.H * pieces;
-  for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<long long>(gridDim.x) * kThreads) {
-    const int piece = static_cast<int>(i % pieces);
-    long long r = i / pieces;
-    const int h = static_cast<int>(r % c.H);
-    r /= c.H;
-    const int j = static_cast<int>(r % s.Q), b = static_cast<int>(r / s.Q);
-    const int fresh = seq_new(s, b, dev_status);
-    if (j >= fresh) continue;
-    const int len = seq_len(c, s, b, dev_status), slot = len - fresh + j;
+  if (unit >= static_cast<long long>(s.B) * groups * c.H) return;
+  // (heads next to one another: they lie next to one another in the projection and often in the cache)
+  const int h = static_cast<int>(unit % c.H), b = static_cast<int>(unit / c.H / groups), j = static_cast<int>(unit / c.H % groups) * kRows + lane;
+  const int fresh = seq_new(s, b, dev_status);
+  Place src{-1, 0}, dst{-1, 0};
+  if (j < fresh) {
+    const int slot = seq_len(c, s, b, dev_status) - fresh + j;
     if (slot < 0) {
       raise_status(dev_status, kBadIndex);
-      continue;
-    }
-    const int page = page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status);
-    if (page < 0) continue;
-    const int at = slot % c.page_slots, col = 8 * piece;
-    const bf16_t* kp = static_cast<const bf16_t*>(k.data) + b * k.seq + j * k.token + h * k.head + col;
-    const bf16_t* vp = static_cast<const bf16_t*>(v.data) + b * v.seq + j * v.token + h * v.head + col;
-    bf16_t* ko = static_cast<bf16_t*>(c.k) + page * c.k_page + at * c.k_slot + h * c.k_head + col;
-    bf16_t* vo = static_cast<bf16_t*>(c.v) + page * c.v_page + at * c.v_slot + h * c.v_head + col;
-    if (VEC) {
-      const uint4 a = *reinterpret_cast<const uint4*>(kp), d = *reinterpret_cast<const uint4*>(vp);
-      *reinterpret_cast<uint4*>(ko) = a;
-      *reinterpret_cast<uint4*>(vo) = d;
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        ko[e] = kp[e];
-        vo[e] = vp[e];
-      }
+      src = Place{0, j};
+      dst = Place{page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status), slot % c.page_slots};
     }
-    if (piece == 0 && c.acc != nullptr) c.acc[page * c.acc_page + h * c.acc_head + at] = 0.f;
   }
+  move_rows(c.D / 8, src, dst,
+            [&](bool value, Place p, int col) {
+              return value ? static_cast<const bf16_t*>(v.data) + b * v.seq + p.slot * v.token + h * v.head + col
+                           : static_cast<const bf16_t*>(k.data) + b * k.seq + p.slot * k.token + h * k.head + col;
+            },
+            [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
+            [](const bf16_t* p) {
+              if (VEC) return *reinterpret_cast<const uint4*>(p);
+              return make_uint4(p[0] | static_cast<uint32_t>(p[1]) << 16, p[2] | static_cast<uint32_t>(p[3]) << 16, p[4] | static_cast<uint32_t>(p[5]) << 16,
+                                p[6] | static_cast<uint32_t>(p[7]) << 16);
+            });
+  if (c.acc != nullptr && dst.page >= 0) c.acc[dst.page * c.acc_page + h * c.acc_head + dst.slot] = 0.f;
 }
 
 // ---------------------------------------------------------------------------------------------- eviction
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kDigits = 2048;                    // eleven bits at a time
 
-// The order in which slots are kept: the last `recent` ones before all others, then by accumulated weight.
-__device__ __forceinline__ uint32_t keep_key(float acc) {
-  if (acc != acc) return 0;                                    // NaN: the least
-  const uint32_t u = __float_as_uint(acc + 0.f);               // (-0 as +0)
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ uint32_t slot_key(const cpmtp_cache& c, const int* row, int h, int slot, int recent_from, int* dev_status) {
-  if (slot >= recent_from) return 0xffffffffu;
-  const int page = page_of(row[slot / c.page_slots], c.pages, dev_status);
-  return page < 0 ? 0 : keep_key(c.acc[page * c.acc_page + h * c.acc_head + slot % c.page_slots]);
-}
+struct Select {
+  uint32_t hist[kDigits];
+  uint32_t scan[kSelectWarps], scan2[kSelectWarps];
+  cluster::u64 box[4][cluster::kMostCtas];
+  uint32_t digit, left;
+};
 
-// One block for each head of each sequence: the key of the last slot to be kept by four passes over eight bits each, then the kept slots in their
-// order.  kept [B, H, budget].
+// The order in which slots are kept: the last `recent` ones before all others, then by accumulated weight; NaN is the least.
+__device__ __forceinline__ uint32_t keep_key(float acc) { return acc != acc ? 0u : cluster::order_key(acc); }
+
+// A cluster for each head of each sequence, a block for `span` of its slots.  The last key to be kept is found by its digits, eleven bits at
+// a time from histograms; then every warp numbers the kept slots of its range.  Keys stay in shared memory (HELD).
+template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
-                                                                int budget, int recent, int* lens_out, int* kept, int* dev_status) {
-  __shared__ int hist[256];
-  __shared__ uint32_t sh_prefix;
-  __shared__ int sh_need, warp_sums[32], warp_ties[32];
+                                                                int ctas, int span, int budget, int recent, int* lens_out, int* kept, int* dev_status) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Select& sh = *reinterpret_cast<Select*>(smem);
+  uint32_t* keys = reinterpret_cast<uint32_t*>(smem + sizeof(Select));
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int rank = static_cast<int>(blockIdx.x) % ctas, h = static_cast<int>(blockIdx.x) / ctas, b = blockIdx.y;
   ptx::grid_dep_wait();
-  const int h = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int len = seq_len(c, s, b, dev_status);
   const int* row = s.table + b * s.ld_table;
   int* out = kept + (static_cast<long long>(b) * c.H + h) * budget;
-  if (h == 0 && t == 0) lens_out[b] = min(len, budget);
+  if (h == 0 && rank == 0 && t == 0) lens_out[b] = min(len, budget);
   if (len <= budget) {
-    for (int i = t; i < budget; i += kSelectThreads) out[i] = i < len ? i : -1;
-    return;
+    for (int i = rank * kSelectThreads + t; i < budget; i += ctas * kSelectThreads) out[i] = i < len ? i : -1;
+    ptx::grid_dep_launch();
+    return;                                      // (all blocks of the cluster do)
   }
-  const int from = len - recent;
-  uint32_t prefix = 0, mask = 0;
-  int need = budget;                             // how many of the keys with this prefix are kept, the largest first
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (t < 256) hist[t] = 0;
-    __syncthreads();
-    for (int i = t; i < len; i += kSelectThreads) {
-      const uint32_t key = slot_key(c, row, h, i, from, dev_status);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1);
+  const int from = len - recent, base = min(rank * span, len), n = min(span, len - base);
+  auto read = [&](int i) {                       // of the i-th slot of this block
+    const int slot = base + i;
+    if (slot >= from) return 0xffffffffu;
+    const int page = page_of(row[slot / c.page_slots], c.pages, dev_status);
+    return page < 0 ? 0u : keep_key(c.acc[page * c.acc_page + h * c.acc_head + slot % c.page_slots]);
+  };
+  auto key = [&](int i) { return HELD ? keys[i] : read(i); };
+  auto sync = [&] { cluster::sync_row(ctas); };
+  int boxes = 0;
+  auto exchange = [&](cluster::u64 v) {          // v of thread 0 to every block, and theirs
+    cluster::u64* box = sh.box[boxes++ & 3];
+    v = __shfl_sync(0xffffffffu, v, 0);
+    if (t < ctas) {
+      if (ctas == 1) box[0] = v;
+      else cluster::store_remote(box + rank, t, v);
+    }
+    sync();
+    return box;
+  };
+  for (int i = t; i < kDigits; i += kSelectThreads) sh.hist[i] = 0;
+  __syncthreads();
+  uint32_t prefix = 0, mask = 0, need = budget;  // how many of the keys with this prefix are kept, the largest first
+#pragma unroll 1
+  for (int d = 0; d < 3; ++d) {
+    const int shift = d == 0 ? 21 : d == 1 ? 10 : 0;
+    const uint32_t digits = d < 2 ? kDigits - 1 : 1023;
+    if (d == 0) {
+#pragma unroll 8
+      for (int i = t; i < n; i += kSelectThreads) {
+        const uint32_t k = read(i);
+        if (HELD) keys[i] = k;
+        atomicAdd(&sh.hist[k >> 21], 1u);
+      }
+    } else {
+#pragma unroll 4
+      for (int i = t; i < n; i += kSelectThreads) {
+        const uint32_t k = key(i);
+        if ((k & mask) == prefix) atomicAdd(&sh.hist[k >> shift & digits], 1u);
+      }
+    }
+    sync();
+    // this block's share of the digits, the largest first; four to a thread at most
+    const int per = kDigits / ctas, each = (per + kSelectThreads - 1) / kSelectThreads;
+    uint32_t mine[kDigits / kSelectThreads], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kDigits / kSelectThreads; ++j) {
+      mine[j] = 0;
+      const int at = t * each + j;
+      if (j < each && at < per) {
+        const int digit = kDigits - 1 - (rank * per + at);
+        uint32_t v[cluster::kMostCtas];
+#pragma unroll
+        for (int r = 0; r < cluster::kMostCtas; ++r) v[r] = r < ctas ? (ctas == 1 ? sh.hist[digit] : cluster::load_remote32(&sh.hist[digit], r)) : 0;
+#pragma unroll
+        for (int r = 0; r < cluster::kMostCtas; ++r) mine[j] += v[r];
+        sum += mine[j];
+      }
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
     }
     __syncthreads();
-    if (t == 0) {
-      int left = need, d = 255;
-      while (d > 0 && hist[d] < left) left -= hist[d--];
-      sh_prefix = prefix | (static_cast<uint32_t>(d) << shift);
-      sh_need = left;
-    }
+    if (lane == 31) sh.scan[warp] = upto;
     __syncthreads();
-    prefix = sh_prefix;
-    need = sh_need;
-    mask |= 255u << shift;
+    uint32_t all = 0;
+    for (int w = 0; w < kSelectWarps; ++w) {
+      if (w < warp) upto += sh.scan[w];
+      all += sh.scan[w];
+    }
+    const cluster::u64* box = exchange(all);     // (and the histograms have been read)
+    uint32_t run = upto - sum;
+    for (int r = 0; r < rank; ++r) run += static_cast<uint32_t>(box[r]);
+#pragma unroll
+    for (int j = 0; j < kDigits / kSelectThreads; ++j) {
+      if (run < need && run + mine[j] >= need) {
+        const uint32_t digit = kDigits - 1 - (rank * per + t * each + j);
+        for (int r = 0; r < ctas; ++r) {
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster::remote(&sh.digit, r)), "r"(digit) : "memory");
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster::remote(&sh.left, r)), "r"(need - run) : "memory");
+        }
+      }
+      run += mine[j];
+    }
+    for (int i = t; i < kDigits; i += kSelectThreads) sh.hist[i] = 0;
+    sync();
+    prefix |= sh.digit << shift;
+    need = sh.left;
+    mask |= digits << shift;
   }
   // keys above `prefix`, and the first `need` equal to it
-  int done = 0, ties = 0;
-  for (int base = 0; base < len; base += kSelectThreads) {
-    const int i = base + t;
-    const uint32_t key = i < len ? slot_key(c, row, h, i, from, dev_status) : 0;
-    const bool tie = i < len && key == prefix;
-    const uint32_t tie_lanes = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) warp_ties[warp] = __popc(tie_lanes);
-    __syncthreads();
-    int rank = ties + __popc(tie_lanes & ((1u << lane) - 1));
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) rank += warp_ties[w];
-      ties += warp_ties[w];
-    }
-    const bool keep = i < len && (key > prefix || (tie && rank < need));
-    const uint32_t lanes = __ballot_sync(0xffffffffu, keep);
-    if (lane == 0) warp_sums[warp] = __popc(lanes);
-    __syncthreads();
-    int at = done + __popc(lanes & ((1u << lane) - 1));
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) at += warp_sums[w];
-      done += warp_sums[w];
-    }
-    if (keep) out[at] = i;
-    __syncthreads();
+  const int range = ((n + kSelectWarps - 1) / kSelectWarps + 31) / 32 * 32, w0 = min(warp * range, n), w1 = min(w0 + range, n);
+  uint32_t above = 0, ties = 0;
+  for (int i = w0 + lane; i < w1; i += 32) {
+    const uint32_t k = key(i);
+    above += k > prefix;
+    ties += k == prefix;
   }
+  above = __reduce_add_sync(0xffffffffu, above);
+  ties = __reduce_add_sync(0xffffffffu, ties);
+  __syncthreads();
+  if (lane == 0) {
+    sh.scan[warp] = above;
+    sh.scan2[warp] = ties;
+  }
+  __syncthreads();
+  uint32_t all = 0, all_ties = 0;
+  above = ties = 0;
+  for (int w = 0; w < kSelectWarps; ++w) {
+    if (w < warp) {
+      above += sh.scan[w];
+      ties += sh.scan2[w];
+    }
+    all += sh.scan[w];
+    all_ties += sh.scan2[w];
+  }
+  const cluster::u64* box = exchange(static_cast<cluster::u64>(all) << 32 | all_ties);
+  for (int r = 0; r < rank; ++r) {
+    above += static_cast<uint32_t>(box[r] >> 32);
+    ties += static_cast<uint32_t>(box[r]);
+  }
+  for (int i0 = w0; i0 < w1; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t k = i < w1 ? key(i) : 0;
+    const uint32_t tie = __ballot_sync(0xffffffffu, i < w1 && k == prefix), over = __ballot_sync(0xffffffffu, i < w1 && k > prefix), below = (1u << lane) - 1;
+    const uint32_t nth = ties + __popc(tie & below);
+    if (i < w1 && (k > prefix || (k == prefix && nth < need))) out[above + __popc(over & below) + min(nth, need)] = base + i;
+    above += __popc(over);
+    ties += __popc(tie);
+  }
+  ptx::grid_dep_launch();
 }
 
-// One thread for each piece of eight elements of a kept key and value.
+// A warp for each 32 kept slots of a head.
 __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
                                                         const int* table_out, long long ld_table_out, int budget, const int* kept, int* dev_status) {
+  const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z;
+  const int j = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kRows + lane;
   ptx::grid_dep_wait();
-  const int pieces = c.D / 8;
-  const long long items = static_cast<long long>(s.B) * c.H * budget * pieces;
-  for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<long long>(gridDim.x) * kThreads) {
-    const int piece = static_cast<int>(i % pieces);
-    const long long r = i / pieces;
-    const int j = static_cast<int>(r % budget), h = static_cast<int>(r / budget % c.H), b = static_cast<int>(r / budget / c.H);
-    const int slot = kept[r];
-    if (slot < 0) continue;
-    const int from = page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status);
-    const int to = page_of(table_out[b * ld_table_out + j / c.page_slots], c.pages, dev_status);
-    if (from < 0 || to < 0) continue;
-    const int at = slot % c.page_slots, in = j % c.page_slots;
-    bf16_t *k = static_cast<bf16_t*>(c.k) + h * c.k_head + 8 * piece, *v = static_cast<bf16_t*>(c.v) + h * c.v_head + 8 * piece;
-    const uint4 a = *reinterpret_cast<const uint4*>(k + from * c.k_page + at * c.k_slot);
-    const uint4 d = *reinterpret_cast<const uint4*>(v + from * c.v_page + at * c.v_slot);
-    *reinterpret_cast<uint4*>(k + to * c.k_page + in * c.k_slot) = a;
-    *reinterpret_cast<uint4*>(v + to * c.v_page + in * c.v_slot) = d;
-    if (piece == 0) c.acc[to * c.acc_page + h * c.acc_head + in] = c.acc[from * c.acc_page + h * c.acc_head + at];
+  const int slot = j < budget ? kept[(static_cast<long long>(b) * c.H + h) * budget + j] : -1;
+  Place src{-1, 0}, dst{-1, 0};
+  if (slot >= 0) {
+    src = Place{page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status), slot % c.page_slots};
+    dst = Place{page_of(table_out[b * ld_table_out + j / c.page_slots], c.pages, dev_status), j % c.page_slots};
   }
+  float acc = 0.f;
+  const bool ok = src.page >= 0 && dst.page >= 0;
+  if (ok) acc = c.acc[src.page * c.acc_page + h * c.acc_head + src.slot];
+  move_rows(c.D / 8, src, dst, [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
+            [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
+            [](const bf16_t* p) { return *reinterpret_cast<const uint4*>(p); });
+  if (ok) c.acc[dst.page * c.acc_page + h * c.acc_head + dst.slot] = acc;
 }
 
 }  // namespace cache

@@ -14,6 +14,7 @@
 #include <cstdint>
 
 #include "../../include/cpmtp.h"
+#include "cluster.cuh"
 #include "ptx.cuh"
 #include "vec_io.cuh"
 
@@ -21,10 +22,15 @@ namespace cpmtp {
 namespace sample {
 
 using io::bf16_t;
-typedef unsigned long long u64;
+using cluster::load_remote32;
+using cluster::load_remote64;
+using cluster::remote;
+using cluster::store_remote;
+using cluster::sync_row;
+using cluster::u64;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMostCtas = 8;
+using cluster::kMostCtas;
 constexpr int kBins = 2048;            // of the histogram, 64 to a factor of two
 constexpr int kList = 2048;            // entries that one block sorts
 constexpr int kTable = 1024;           // powers of two between one and two
@@ -48,41 +54,9 @@ struct Shared {
 
 static_assert(sizeof(Shared) % 16 == 0, "the row's entries follow");
 
-// -------------------------------------------------------------------------------------------- cluster
-__device__ __forceinline__ void sync_row(int ctas) {
-  if (ctas == 1) {
-    __syncthreads();
-  } else {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  }
-}
-__device__ __forceinline__ uint32_t remote(const void* p, int cta) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(ptx::smem_u32(p)), "r"(cta));
-  return r;
-}
-__device__ __forceinline__ void store_remote(const void* p, int cta, u64 v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(p, cta)), "l"(v) : "memory");
-}
-__device__ __forceinline__ u64 load_remote64(const void* p, int cta) {
-  u64 v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, cta)) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t load_remote32(const void* p, int cta) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote(p, cta)) : "memory");
-  return v;
-}
-
 // -------------------------------------------------------------------------------------------- keys and weights
 // Unsigned keys in the order of the logits.
-__device__ __forceinline__ uint32_t logit_key(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);     // (-0 as +0)
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
+__device__ __forceinline__ uint32_t logit_key(float x) { return cluster::order_key(x); }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // z <= 0 with 32 bits below the point, in two words.

@@ -70,11 +70,6 @@ int check_tokens(const cpmtp_tokens* t, int64_t Q, int64_t H, int D) {
 }
 bool tokens_vec(const cpmtp_tokens& t) { return aligned(t.data, 16) && t.seq % 8 == 0 && t.token % 8 == 0 && t.head % 8 == 0; }
 
-int blocks_for(long long items, int threads, int sms) {
-  const long long blocks = (items + threads - 1) / threads, most = 64ll * sms;
-  return static_cast<int>(blocks < most ? blocks : most);
-}
-
 // Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.
 int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
   const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
@@ -137,13 +132,34 @@ size_t evict_bytes(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int budget) 
   return align_up(sizeof(int) * static_cast<size_t>(s.B) * c.H * budget + kAlign);
 }
 
+// Blocks of a cluster that share the slots of a head: enough to use all SMs and to hold the keys in half of an SM's shared memory, as long as
+// each has some slots for its threads.
+cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const cpmtp_evict_args& e, int* kept, int sms, int* dev_status, cudaStream_t st) {
+  constexpr size_t kMost = 232448, kShare = 110000;
+  const int slots = s.width * c.page_slots;
+  int ctas = 1;
+  while (ctas < cluster::kMostCtas && slots / ctas >= 4 * cache::kSelectThreads &&
+         (static_cast<size_t>(slots) * 4 / ctas > kShare || static_cast<long long>(s.B) * c.H * ctas < 2ll * sms))
+    ctas *= 2;
+  const int span = ((slots + ctas - 1) / ctas + 31) / 32 * 32;
+  const size_t held = sizeof(cache::Select) + static_cast<size_t>(span) * 4;
+  const dim3 grid(c.H * ctas, s.B), threads(cache::kSelectThreads);
+  static bool done[64] = {}, done_far[64] = {};
+  if (held <= kMost) {
+    const cudaError_t rc = allow_smem(cache::select_kernel<true>, done, kMost);
+    return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<true>, grid, threads, held, st, c, s, ctas, span, e.budget, e.recent, e.lens_out, kept, dev_status);
+  }
+  const cudaError_t rc = allow_smem(cache::select_kernel<false>, done_far, static_cast<int>(sizeof(cache::Select)));
+  return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, e.budget, e.recent, e.lens_out, kept, dev_status);
+}
+
 // Blocks of a cluster that share a row: enough to hold it in 64 KB of shared memory each (two blocks to an SM) and to use all SMs, as
 // long as each has some entries for its threads.
 template <class T>
 cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, cudaStream_t st) {
   constexpr size_t kMost = 232448, kShare = 65536;
   int ctas = 1;
-  while (ctas < sample::kMostCtas && a.V / ctas >= 4 * sample::kThreads &&
+  while (ctas < cluster::kMostCtas && a.V / ctas >= 4 * sample::kThreads &&
          (static_cast<size_t>(a.V) * sizeof(T) / ctas > kShare || static_cast<long long>(a.N) * ctas < sms))
     ctas *= 2;
   const int span = ((a.V + ctas - 1) / ctas + 7) / 8 * 8;
@@ -181,7 +197,9 @@ int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_CACHE_APPEND, st);
-  const dim3 grid(blocks_for(static_cast<long long>(s.B) * s.Q * c.H * (c.D / 8), cache::kThreads, di->sms));
+  const long long units = static_cast<long long>(s.B) * ((s.Q + cache::kRows - 1) / cache::kRows) * c.H, per = cache::kThreads / 32;
+  if (units > 2147483647ll) return CPMTP_ERR_LIMIT;
+  const dim3 grid(static_cast<unsigned>((units + per - 1) / per));
   if (tokens_vec(*k) && tokens_vec(*v)) CPMTP_TRY(launch_pdl(cache::append_kernel<true>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   else CPMTP_TRY(launch_pdl(cache::append_kernel<false>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   return CPMTP_OK;
@@ -268,8 +286,8 @@ int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, co
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_CACHE_EVICT, st);
   int* kept = e.kept != nullptr ? e.kept : static_cast<int*>(workspace);
-  CPMTP_TRY(launch_pdl(cache::select_kernel, dim3(c.H, s.B), dim3(cache::kSelectThreads), 0, st, c, s, e.budget, e.recent, e.lens_out, kept, dev_status));
-  const dim3 grid(blocks_for(static_cast<long long>(s.B) * c.H * e.budget * (c.D / 8), cache::kThreads, di->sms));
+  CPMTP_TRY(launch_select(c, s, e, kept, di->sms, dev_status, st));
+  const dim3 grid((e.budget + cache::kThreads - 1) / cache::kThreads, c.H, s.B);
   CPMTP_TRY(launch_pdl(cache::move_kernel, grid, dim3(cache::kThreads), 0, st, c, s, e.table_out, e.ld_table_out, e.budget, kept, dev_status));
   return CPMTP_OK;
 }
