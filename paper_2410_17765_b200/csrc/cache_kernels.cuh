@@ -38,77 +38,48 @@ __device__ __forceinline__ int page_of(int page, int pages, int* dev_status) {
 }
 
 constexpr int kThreads = 256;
-constexpr int kRows = 32;              // rows (a key and a value) that a warp moves: one for each lane to look up
-constexpr int kAhead = 8;              // 16-byte pieces that a lane has under way
-
-// A warp moves the keys and values of rows 0 .. count - 1 of one head, a piece of eight elements to a lane: the lanes of a row have
-// its key's pieces, then its value's.  from(row), to(row): addresses of row `row`, which lane `row` has looked up; row_ok: what lane `row` found.
-struct Place {
-  int page, slot;        // page < 0: nothing
-};
-template <class From, class To, class Move>
-__device__ __forceinline__ void move_rows(int pieces, Place src, Place dst, From from, To to, Move move) {
-  const int lane = threadIdx.x & 31, width = 2 * pieces, at_once = 32 / width;
-  const int sub = lane / width, piece = lane % width;
-  const bool value = piece >= pieces, on = sub < at_once;
-  const int col = 8 * (value ? piece - pieces : piece);
-  const uint32_t some = __ballot_sync(0xffffffffu, src.page >= 0 && dst.page >= 0);
-  for (int r0 = 0; r0 < kRows && (some >> r0) != 0; r0 += kAhead * at_once) {
-    uint4 v[kAhead];
-    bool ok[kAhead];
-    Place d[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int r = r0 + i * at_once + sub, who = r & 31;
-      const Place s{__shfl_sync(0xffffffffu, src.page, who), __shfl_sync(0xffffffffu, src.slot, who)};
-      d[i] = Place{__shfl_sync(0xffffffffu, dst.page, who), __shfl_sync(0xffffffffu, dst.slot, who)};
-      ok[i] = on && r < kRows && (some >> who & 1);
-      if (ok[i]) v[i] = move(from(value, s, col));
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (ok[i]) *reinterpret_cast<uint4*>(to(value, d[i], col)) = v[i];
-  }
-}
-__device__ __forceinline__ bf16_t* cached(const cpmtp_cache& c, bool value, Place p, int h) {
-  return value ? static_cast<bf16_t*>(c.v) + p.page * c.v_page + p.slot * c.v_slot + h * c.v_head
-               : static_cast<bf16_t*>(c.k) + p.page * c.k_page + p.slot * c.k_slot + h * c.k_head;
-}
-
-// A warp for each 32 new tokens of a sequence and head.  It is the cache lines that bound it: 8192 tokens of 8 x 128 move 101 MB.
+// One thread for each piece of eight elements of a new token's key and value in one head: 8192 tokens of 8 x 128 (50 MB read and written) in
+// 12 us, against 14 for warps that look a row's page up once.
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
                                                           const __grid_constant__ cpmtp_tokens k, const __grid_constant__ cpmtp_tokens v,
                                                           int* dev_status) {
-  const int lane = threadIdx.x & 31, groups = (s.Q + kRows - 1) / kRows;
-  const long long unit = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   ptx::grid_dep_wait();
-  if (unit >= static_cast<long long>(s.B) * groups * c.H) return;
-  // (heads next to one another: they lie next to one another in the projection and often in the cache)
-  const int h = static_cast<int>(unit % c.H), b = static_cast<int>(unit / c.H / groups), j = static_cast<int>(unit / c.H % groups) * kRows + lane;
-  const int fresh = seq_new(s, b, dev_status);
-  Place src{-1, 0}, dst{-1, 0};
-  if (j < fresh) {
-    const int slot = seq_len(c, s, b, dev_status) - fresh + j;
+  const int pieces = c.D / 8;
+  const long long items = static_cast<long long>(s.B) * s.Q * c.H * pieces;
+  for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < items; i += static_cast<long long>(gridDim.x) * kThreads) {
+    const int piece = static_cast<int>(i % pieces);
+    long long r = i / pieces;
+    const int h = static_cast<int>(r % c.H);
+    r /= c.H;
+    const int j = static_cast<int>(r % s.Q), b = static_cast<int>(r / s.Q);
+    const int fresh = seq_new(s, b, dev_status);
+    if (j >= fresh) continue;
+    const int len = seq_len(c, s, b, dev_status), slot = len - fresh + j;
     if (slot < 0) {
       raise_status(dev_status, kBadIndex);
-    } else {
-      src = Place{0, j};
-      dst = Place{page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status), slot % c.page_slots};
+      continue;
     }
+    const int page = page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status);
+    if (page < 0) continue;
+    const int at = slot % c.page_slots, col = 8 * piece;
+    const bf16_t* kp = static_cast<const bf16_t*>(k.data) + b * k.seq + j * k.token + h * k.head + col;
+    const bf16_t* vp = static_cast<const bf16_t*>(v.data) + b * v.seq + j * v.token + h * v.head + col;
+    bf16_t* ko = static_cast<bf16_t*>(c.k) + page * c.k_page + at * c.k_slot + h * c.k_head + col;
+    bf16_t* vo = static_cast<bf16_t*>(c.v) + page * c.v_page + at * c.v_slot + h * c.v_head + col;
+    if (VEC) {
+      const uint4 a = *reinterpret_cast<const uint4*>(kp), d = *reinterpret_cast<const uint4*>(vp);
+      *reinterpret_cast<uint4*>(ko) = a;
+      *reinterpret_cast<uint4*>(vo) = d;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ko[e] = kp[e];
+        vo[e] = vp[e];
+      }
+    }
+    if (piece == 0 && c.acc != nullptr) c.acc[page * c.acc_page + h * c.acc_head + at] = 0.f;
   }
-  move_rows(c.D / 8, src, dst,
-            [&](bool value, Place p, int col) {
-              return value ? static_cast<const bf16_t*>(v.data) + b * v.seq + p.slot * v.token + h * v.head + col
-                           : static_cast<const bf16_t*>(k.data) + b * k.seq + p.slot * k.token + h * k.head + col;
-            },
-            [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
-            [](const bf16_t* p) {
-              if (VEC) return *reinterpret_cast<const uint4*>(p);
-              return make_uint4(p[0] | static_cast<uint32_t>(p[1]) << 16, p[2] | static_cast<uint32_t>(p[3]) << 16, p[4] | static_cast<uint32_t>(p[5]) << 16,
-                                p[6] | static_cast<uint32_t>(p[7]) << 16);
-            });
-  if (c.acc != nullptr && dst.page >= 0) c.acc[dst.page * c.acc_page + h * c.acc_head + dst.slot] = 0.f;
 }
 
 // ---------------------------------------------------------------------------------------------- eviction
@@ -282,25 +253,50 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
   ptx::grid_dep_launch();
 }
 
-// A warp for each 32 kept slots of a head.
+// A warp for `rows` kept slots of a head: a lane looks one of them up, then has a 16-byte piece of a row, kAhead rows at a time; the lanes of a
+// row have its key's pieces and then its value's.  Many rows to a warp save lookups (16 x 4096 slots: 32 take 75 us, 16 take 85); few rows in all
+// want more warps instead (2 x 2048 slots: 8 take 11 us, 32 take 15).
+constexpr int kAhead = 8;
+__host__ __device__ constexpr int rows_at_once(int D) { return 32 / (D / 4); }
+inline int least_rows(int D) { return kAhead * rows_at_once(D) < 32 ? kAhead * rows_at_once(D) : 32; }
+
 __global__ void __launch_bounds__(kThreads) move_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
-                                                        const int* table_out, long long ld_table_out, int budget, const int* kept, int* dev_status) {
+                                                        const int* table_out, long long ld_table_out, int budget, int rows, const int* kept, int* dev_status) {
   const int lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z;
-  const int j = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kRows + lane;
+  const int j = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * rows + lane;
   ptx::grid_dep_wait();
-  const int slot = j < budget ? kept[(static_cast<long long>(b) * c.H + h) * budget + j] : -1;
-  Place src{-1, 0}, dst{-1, 0};
+  const int slot = lane < rows && j < budget ? kept[(static_cast<long long>(b) * c.H + h) * budget + j] : -1;
+  int src_page = -1, src_slot = 0, dst_page = -1, dst_slot = 0;
   if (slot >= 0) {
-    src = Place{page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status), slot % c.page_slots};
-    dst = Place{page_of(table_out[b * ld_table_out + j / c.page_slots], c.pages, dev_status), j % c.page_slots};
+    src_page = page_of(s.table[b * s.ld_table + slot / c.page_slots], c.pages, dev_status);
+    src_slot = slot % c.page_slots;
+    dst_page = page_of(table_out[b * ld_table_out + j / c.page_slots], c.pages, dev_status);
+    dst_slot = j % c.page_slots;
   }
+  const bool both = src_page >= 0 && dst_page >= 0;
   float acc = 0.f;
-  const bool ok = src.page >= 0 && dst.page >= 0;
-  if (ok) acc = c.acc[src.page * c.acc_page + h * c.acc_head + src.slot];
-  move_rows(c.D / 8, src, dst, [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
-            [&](bool value, Place p, int col) { return cached(c, value, p, h) + col; },
-            [](const bf16_t* p) { return *reinterpret_cast<const uint4*>(p); });
-  if (ok) c.acc[dst.page * c.acc_page + h * c.acc_head + dst.slot] = acc;
+  if (both) acc = c.acc[src_page * c.acc_page + h * c.acc_head + src_slot];
+  const uint32_t some = __ballot_sync(0xffffffffu, both);
+  const int pieces = c.D / 8, width = 2 * pieces, at_once = rows_at_once(c.D), sub = lane / width, piece = lane % width;
+  const bool value = piece >= pieces;
+  const int64_t page = value ? c.v_page : c.k_page, step = value ? c.v_slot : c.k_slot;
+  bf16_t* data = value ? static_cast<bf16_t*>(c.v) + h * c.v_head + 8 * (piece - pieces) : static_cast<bf16_t*>(c.k) + h * c.k_head + 8 * piece;
+  for (int r0 = 0; r0 < rows && (some >> r0) != 0; r0 += kAhead * at_once) {
+    uint4 v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int r = r0 + i * at_once + sub;
+      const int64_t from = __shfl_sync(0xffffffffu, src_page, r & 31) * page + __shfl_sync(0xffffffffu, src_slot, r & 31) * step;
+      if (sub < at_once && r < rows && (some >> r & 1)) v[i] = *reinterpret_cast<const uint4*>(data + from);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int r = r0 + i * at_once + sub;
+      const int64_t to = __shfl_sync(0xffffffffu, dst_page, r & 31) * page + __shfl_sync(0xffffffffu, dst_slot, r & 31) * step;
+      if (sub < at_once && r < rows && (some >> r & 1)) *reinterpret_cast<uint4*>(data + to) = v[i];
+    }
+  }
+  if (both) c.acc[dst_page * c.acc_page + h * c.acc_head + dst_slot] = acc;
 }
 
 }  // namespace cache

@@ -70,6 +70,11 @@ int check_tokens(const cpmtp_tokens* t, int64_t Q, int64_t H, int D) {
 }
 bool tokens_vec(const cpmtp_tokens& t) { return aligned(t.data, 16) && t.seq % 8 == 0 && t.token % 8 == 0 && t.head % 8 == 0; }
 
+int blocks_for(long long items, int threads, int sms) {
+  const long long blocks = (items + threads - 1) / threads, most = 64ll * sms;
+  return static_cast<int>(blocks < most ? blocks : most);
+}
+
 // Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.
 int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
   const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
@@ -197,9 +202,7 @@ int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_CACHE_APPEND, st);
-  const long long units = static_cast<long long>(s.B) * ((s.Q + cache::kRows - 1) / cache::kRows) * c.H, per = cache::kThreads / 32;
-  if (units > 2147483647ll) return CPMTP_ERR_LIMIT;
-  const dim3 grid(static_cast<unsigned>((units + per - 1) / per));
+  const dim3 grid(blocks_for(static_cast<long long>(s.B) * s.Q * c.H * (c.D / 8), cache::kThreads, di->sms));
   if (tokens_vec(*k) && tokens_vec(*v)) CPMTP_TRY(launch_pdl(cache::append_kernel<true>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   else CPMTP_TRY(launch_pdl(cache::append_kernel<false>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   return CPMTP_OK;
@@ -287,8 +290,9 @@ int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, co
   ProfScope prof(CPMTP_STAGE_CACHE_EVICT, st);
   int* kept = e.kept != nullptr ? e.kept : static_cast<int*>(workspace);
   CPMTP_TRY(launch_select(c, s, e, kept, di->sms, dev_status, st));
-  const dim3 grid((e.budget + cache::kThreads - 1) / cache::kThreads, c.H, s.B);
-  CPMTP_TRY(launch_pdl(cache::move_kernel, grid, dim3(cache::kThreads), 0, st, c, s, e.table_out, e.ld_table_out, e.budget, kept, dev_status));
+  const int rows = static_cast<long long>(s.B) * c.H * e.budget >= 32ll * 64 * di->sms ? 32 : cache::least_rows(c.D), per = cache::kThreads / 32 * rows;
+  const dim3 grid((e.budget + per - 1) / per, c.H, s.B);
+  CPMTP_TRY(launch_pdl(cache::move_kernel, grid, dim3(cache::kThreads), 0, st, c, s, e.table_out, e.ld_table_out, e.budget, rows, kept, dev_status));
   return CPMTP_OK;
 }
 
