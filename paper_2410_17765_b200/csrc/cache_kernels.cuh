@@ -91,17 +91,19 @@ struct Select {
   uint32_t hist[kDigits];
   uint32_t scan[kSelectWarps], scan2[kSelectWarps];
   cluster::u64 box[4][cluster::kMostCtas];
-  uint32_t digit, left;
+  uint32_t digit, left, unused[2];
 };
+static_assert(sizeof(Select) % 16 == 0, "the keys follow");
 
 // The order in which slots are kept: the last `recent` ones before all others, then by accumulated weight; NaN is the least.
 __device__ __forceinline__ uint32_t keep_key(float acc) { return acc != acc ? 0u : cluster::order_key(acc); }
 
 // A cluster for each head of each sequence, a block for `span` of its slots.  The last key to be kept is found by its digits, eleven bits at
-// a time from histograms; then every warp numbers the kept slots of its range.  Keys stay in shared memory (HELD).
+// a time from histograms; then every warp numbers the kept slots of its range.  Keys stay in shared memory (HELD).  `vec`: acc can be read
+// 16 bytes at a time.  Latency bounds it, of barriers of the cluster above all: three to a digit.
 template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
-                                                                int ctas, int span, int budget, int recent, int* lens_out, int* kept, int* dev_status) {
+                                                                int ctas, int span, int vec, int budget, int recent, int* lens_out, int* kept, int* dev_status) {
   extern __shared__ __align__(16) uint8_t smem[];
   Select& sh = *reinterpret_cast<Select*>(smem);
   uint32_t* keys = reinterpret_cast<uint32_t*>(smem + sizeof(Select));
@@ -145,11 +147,33 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
     const int shift = d == 0 ? 21 : d == 1 ? 10 : 0;
     const uint32_t digits = d < 2 ? kDigits - 1 : 1023;
     if (d == 0) {
-#pragma unroll 8
-      for (int i = t; i < n; i += kSelectThreads) {
-        const uint32_t k = read(i);
-        if (HELD) keys[i] = k;
-        atomicAdd(&sh.hist[k >> 21], 1u);
+      // eight slots at a time, which lie in one page: one lookup, and the next one's under way
+      int page = -1;
+      auto look = [&](int i) { return i < n ? row[(base + i) / c.page_slots] : 0; };
+      int next = look(8 * t);
+      for (int i = 8 * t; i < n; i += 8 * kSelectThreads) {
+        page = page_of(next, c.pages, dev_status);
+        next = look(i + 8 * kSelectThreads);
+        const float* acc = c.acc + (page < 0 ? 0 : page * c.acc_page + h * c.acc_head + (base + i) % c.page_slots);
+        float v[8];
+        if (vec) {
+          const float4 x = *reinterpret_cast<const float4*>(acc), y = *reinterpret_cast<const float4*>(acc + 4);
+          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+          v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = acc[q];
+        }
+        uint32_t k[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          k[q] = base + i + q >= from ? 0xffffffffu : page < 0 ? 0u : keep_key(v[q]);
+          if (i + q < n) atomicAdd(&sh.hist[k[q] >> 21], 1u);
+        }
+        if (HELD) {
+          *reinterpret_cast<uint4*>(keys + i) = make_uint4(k[0], k[1], k[2], k[3]);
+          *reinterpret_cast<uint4*>(keys + i + 4) = make_uint4(k[4], k[5], k[6], k[7]);
+        }
       }
     } else {
 #pragma unroll 4
@@ -241,6 +265,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
     above += static_cast<uint32_t>(box[r] >> 32);
     ties += static_cast<uint32_t>(box[r]);
   }
+#pragma unroll 4
   for (int i0 = w0; i0 < w1; i0 += 32) {
     const int i = i0 + lane;
     const uint32_t k = i < w1 ? key(i) : 0;

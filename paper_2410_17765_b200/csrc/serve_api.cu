@@ -147,15 +147,16 @@ cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const
          (static_cast<size_t>(slots) * 4 / ctas > kShare || static_cast<long long>(s.B) * c.H * ctas < 2ll * sms))
     ctas *= 2;
   const int span = ((slots + ctas - 1) / ctas + 31) / 32 * 32;
+  const int vec = aligned(c.acc, 16) && c.acc_page % 4 == 0 && c.acc_head % 4 == 0;
   const size_t held = sizeof(cache::Select) + static_cast<size_t>(span) * 4;
   const dim3 grid(c.H * ctas, s.B), threads(cache::kSelectThreads);
   static bool done[64] = {}, done_far[64] = {};
   if (held <= kMost) {
     const cudaError_t rc = allow_smem(cache::select_kernel<true>, done, kMost);
-    return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<true>, grid, threads, held, st, c, s, ctas, span, e.budget, e.recent, e.lens_out, kept, dev_status);
+    return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<true>, grid, threads, held, st, c, s, ctas, span, vec, e.budget, e.recent, e.lens_out, kept, dev_status);
   }
   const cudaError_t rc = allow_smem(cache::select_kernel<false>, done_far, static_cast<int>(sizeof(cache::Select)));
-  return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, e.budget, e.recent, e.lens_out, kept, dev_status);
+  return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, vec, e.budget, e.recent, e.lens_out, kept, dev_status);
 }
 
 // Blocks of a cluster that share a row: enough to hold it in 64 KB of shared memory each (two blocks to an SM) and to use all SMs, as
