@@ -1,13 +1,14 @@
 // Sampling from logits with temperature, top-k, top-p and min-p by given uniform numbers.
 //
-// A row is held by the shared memory of a cluster, read once.  Its weights w = 2^z, z = (x - m) log2(e) / T, are integers (62 - log2 V
-// bits below the point) whose sums are exact in any order, so borders between kept and dropped entries, and the token that a number
-// draws, do not depend on how the row is shared out.  Where a filter ends is found in two steps: a histogram over z in steps of 1/64
-// names the few bins in which it lies, and their entries, a few hundred of 128256, are sorted in one block.  Should they be too many (long
-// runs of equal logits, flat rows), the key of the last kept entry is found by digits instead.
+// A row is shared out over the blocks of a cluster, which pass over it one to three times (after the first time it comes from L2).  Its weights
+// w = 2^z, z = (x - m) log2(e) / T, are integers (62 - log2 V bits below the point) whose sums are exact in any order, so borders between
+// kept and dropped entries, and the token that a number draws, do not depend on how the row is shared out.  Where a filter ends is found in two
+// steps: a histogram over z in steps of 1/64 names the few bins in which it lies, and their entries, a few hundred of 128256, are sorted in one
+// block.  Should they be too many (long runs of equal logits, flat rows), the key of the last kept entry is found by digits instead.
 //
-// What bounds it: at many rows the instructions, about 30 for a weight and 8 for its bin, each entry once or twice; at few rows the
-// latency of a dozen barriers of a cluster.
+// What bounds it: at many rows the instructions, about 35 for a weight and 8 for its bin; at few rows the latency of a dozen barriers of a
+// cluster.  Holding the row in shared memory was slower at many rows (512 x 128256 in bf16 with top-p: 473 us against 357), since it
+// leaves room for fewer blocks, and 1 us faster at few.
 #pragma once
 #include <cfloat>
 #include <climits>
@@ -34,6 +35,7 @@ using cluster::kMostCtas;
 constexpr int kBins = 2048;            // of the histogram, 64 to a factor of two
 constexpr int kList = 2048;            // entries that one block sorts
 constexpr int kTable = 1024;           // powers of two between one and two
+constexpr int kQueue = 9 * 32;         // logits that a warp collects before it weighs them
 
 struct Shared {
   u64 table[kTable];
@@ -45,6 +47,7 @@ struct Shared {
       uint32_t count[256];
     } digit;
   };
+  float queue[kWarps][kQueue];
   double scan[kWarps];
   u64 sums[kWarps];                    // kept mass of the warps' ranges
   u64 box[8][kMostCtas];               // numbers from the blocks of the cluster; two places in turn
@@ -134,8 +137,8 @@ __device__ __forceinline__ Settings settings_of(const cpmtp_sample_args& a, int 
 
 // -------------------------------------------------------------------------------------------- the kernel
 // A cluster of `ctas` blocks to a row.  A block's entries are read in whole 16-byte pieces, the first and last of which may reach beyond
-// them; its warps have equal ranges of pieces.  HELD: in shared memory.
-template <class T, bool HELD>
+// them; its warps have equal ranges of pieces.
+template <class T>
 struct Row {
   static constexpr int kPer = 16 / sizeof(T);
   Shared& sh;
@@ -143,8 +146,7 @@ struct Row {
   int base, n;           // this block's entries
   int off;               // entries of the first piece that lie before them
   int pieces, each;      // pieces of the block, of a warp
-  const uint4* data;     // the pieces: in memory, or ...
-  uint32_t held;         // ... their address in shared memory
+  const uint4* data;
   int boxes;
 
   __device__ __forceinline__ void sync() const { sync_row(ctas); }
@@ -168,12 +170,7 @@ struct Row {
       }
     }
   }
-  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const {
-    uint4 raw;
-    if (HELD) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(held + piece * 16));
-    else raw = __ldg(data + piece);
-    unpack(piece, raw, v);
-  }
+  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const { unpack(piece, __ldg(data + piece), v); }
   // f(logit, index in the row) for the entries of this warp's pieces.
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
@@ -506,7 +503,7 @@ struct Row {
   }
 };
 
-template <class T, bool HELD>
+template <class T>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ cpmtp_sample_args a, int ctas, int span, int bits, int* dev_status) {
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
@@ -515,10 +512,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   // between one and two, while nothing else can be done
   for (int i = t; i < kTable; i += kThreads) sh.table[i] = static_cast<u64>(exp2(static_cast<double>(i) / kTable) * 4611686018427387904.0);
   ptx::grid_dep_wait();
-  using R_t = Row<T, HELD>;
+  using R_t = Row<T>;
   constexpr int kPer = R_t::kPer;
   const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-  R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0, 0};
+  R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0};
   R.base = min(rank * span, a.V);
   R.n = min(span, a.V - R.base);
   const uintptr_t first = reinterpret_cast<uintptr_t>(src + R.base);
@@ -536,9 +533,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   float top = -INFINITY;
   {
     const uint4* from = reinterpret_cast<const uint4*>(first & ~static_cast<uintptr_t>(15));
-    uint4* held = reinterpret_cast<uint4*>(smem + sizeof(Shared));
     R.data = from;
-    R.held = ptx::smem_u32(held);
     constexpr int kAhead = 8;
     for (int p0 = t; p0 < R.pieces; p0 += kAhead * kThreads) {
       uint4 raw[kAhead];
@@ -549,7 +544,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       for (int j = 0; j < kAhead; ++j) {
         const int p = p0 + j * kThreads;
         if (p >= R.pieces) break;
-        if (HELD) held[p] = raw[j];
         float v[kPer];
         R.unpack(p, raw[j], v);
 #pragma unroll
@@ -743,19 +737,46 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       const float xa = nextafterf(__double2float_ru(w.m - (b1 - 1) / (64.0 * w.c)), INFINITY);
       const float xb = b2 == kBins - 1 ? -FLT_MAX : nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY);
       u64 above = 0;
-      R.for_each([&](float v, int i) {
-        if (!(v >= xb && kept_by(v, i))) return;
-        if (v > xa) {
-          const Fixed z = w.z(v);
-          const u64 q = w.weight(z);
-          const bool in = at_least(z, z_min);
-          above += q;
-          sum += only_if(in, q);
-          number += in;
-        } else {
-          R.list_add(v, i);
+      // few entries are that large: a warp collects them, and weighs 32 at a time
+      float* queue = sh.queue[warp];
+      int queued = 0;
+      auto weigh = [&](float v, bool on) {
+        const Fixed z = w.z(v);
+        const u64 q = only_if(on, w.weight(z));
+        const bool in = on & at_least(z, z_min);
+        above += q;
+        sum += only_if(in, q);
+        number += in;
+      };
+      const int last_piece = min((warp + 1) * R.each, R.pieces);
+#pragma unroll 1
+      for (int p0 = warp * R.each; p0 < last_piece; p0 += 32) {
+        const int p = p0 + lane;
+        float v[kPer];
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) v[q] = -INFINITY;
+        if (p < last_piece) R.load(p, v);
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+          const int i = R.base + p * kPer + q - R.off;
+          const bool in = (v[q] >= xb) & kept_by(v[q], i), over = in & (v[q] > xa);
+          const uint32_t lanes = __ballot_sync(0xffffffffu, over);
+          if (over) queue[queued + __popc(lanes & ((1u << lane) - 1))] = v[q];
+          queued += __popc(lanes);
+          if (in & !over) R.list_add(v[q], i);
         }
-      });
+        __syncwarp();
+        int done = 0;
+        for (; queued - done >= 32; done += 32) weigh(queue[done + lane], true);
+        if (done > 0) {
+          const float rest = lane < queued - done ? queue[done + lane] : 0.f;
+          __syncwarp();
+          queue[lane] = rest;
+          queued -= done;
+        }
+        __syncwarp();
+      }
+      weigh(lane < queued ? queue[lane] : top, lane < queued);
       above = R.block_sum(above);
       const int mine = sh.listed;
       const u64* box = R.exchange(above, mine);

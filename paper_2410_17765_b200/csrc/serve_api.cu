@@ -159,27 +159,28 @@ cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const
   return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, vec, e.budget, e.recent, e.lens_out, kept, dev_status);
 }
 
-// Blocks of a cluster that share a row: enough to hold it in 64 KB of shared memory each (two blocks to an SM) and to use all SMs, as
-// long as each has some entries for its threads.
+// Blocks of a cluster that share a row: what takes the least time if two blocks fit on an SM and a block takes 20 us and 1 ns an entry, or 1.5 where the
+// rows under way do not fit in L2 (measured with 1, 2, 4 and 8 blocks to each of 512 rows of 128256: 354, 323, 354 and 503 us; of 8 rows: 48, 34, 25
+// and 21).
 template <class T>
 cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, cudaStream_t st) {
-  constexpr size_t kMost = 232448, kShare = 65536;
   int ctas = 1;
-  while (ctas < cluster::kMostCtas && a.V / ctas >= 4 * sample::kThreads &&
-         (static_cast<size_t>(a.V) * sizeof(T) / ctas > kShare || static_cast<long long>(a.N) * ctas < sms))
-    ctas *= 2;
+  long long best = 0;
+  for (int n = 1; n <= cluster::kMostCtas; n *= 2) {
+    const long long waves = (static_cast<long long>(a.N) * n + 2 * sms - 1) / (2 * sms), rows = std::min<long long>(a.N, 2 * sms / n);
+    const long long entry = rows * a.V * static_cast<long long>(sizeof(T)) > (100ll << 20) ? 3 : 2, time = waves * (40000 + entry * (a.V / n));
+    if (n > 1 && time >= best) continue;
+    best = time;
+    ctas = n;
+  }
   const int span = ((a.V + ctas - 1) / ctas + 7) / 8 * 8;
   int width = 0;
   while ((1ll << width) < a.V) ++width;
-  const size_t held = sizeof(sample::Shared) + static_cast<size_t>(span) * sizeof(T) + 32;
-  const dim3 grid(static_cast<unsigned>(a.N) * ctas), threads(sample::kThreads);
-  static bool done[64] = {}, done_far[64] = {};
-  if (held <= kMost) {
-    const cudaError_t e = allow_smem(sample::sample_kernel<T, true>, done, kMost);
-    return e != cudaSuccess ? e : launch_clusters(ctas, sample::sample_kernel<T, true>, grid, threads, held, st, a, ctas, span, 62 - width, dev_status);
-  }
-  const cudaError_t e = allow_smem(sample::sample_kernel<T, false>, done_far, static_cast<int>(sizeof(sample::Shared)));
-  return e != cudaSuccess ? e : launch_clusters(ctas, sample::sample_kernel<T, false>, grid, threads, sizeof(sample::Shared), st, a, ctas, span, 62 - width, dev_status);
+  static bool done[64] = {};
+  const cudaError_t e = allow_smem(sample::sample_kernel<T>, done, static_cast<int>(sizeof(sample::Shared)));
+  if (e != cudaSuccess) return e;
+  return launch_clusters(ctas, sample::sample_kernel<T>, dim3(static_cast<unsigned>(a.N) * ctas), dim3(sample::kThreads), sizeof(sample::Shared), st, a, ctas, span, 62 - width,
+                         dev_status);
 }
 
 }  // namespace
