@@ -708,6 +708,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       R.find_by_digits(w, [](float v, int) { return v > -INFINITY; }, false, set.top_k, tx, ti);
   }
 
+  const bool floor = tx > -INFINITY;         // (without one the passes ask for less)
+
   // ---- top-p, and the kept mass of every warp's range
   u64 sum = 0;
   uint32_t number = 0;
@@ -716,14 +718,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int less = max(0, 32 - __clz(span - 1) - 14);                    // bits that the histogram's sums have to do without
     u64 mass = 0;
     R.clear_hist();
-    R.for_each([&](float v, int i) {
-      const bool in = kept_by(v, i);
+    auto measure = [&](float v, bool in) {
       const Fixed z = w.z(v);
       const u64 q = w.mantissa(z);
       mass += only_if(in, w.fixed(q, z));
-      // (an entry of bin b has -b <= 64 z < 1 - b)
-      if (in) atomicAdd(&sh.hist[min(-(z.whole * 64 + static_cast<int>(z.part >> 26)), kBins - 1)], static_cast<uint32_t>(q >> 45) >> less);
-    });
+      // (an entry of bin b has -b <= 64 z < 1 - b; one that is not kept adds nothing to its bin)
+      const int bin = min(-(z.whole * 64 + static_cast<int>(z.part >> 26)), kBins - 1);
+      atomicAdd(&sh.hist[bin & (kBins - 1)], in ? static_cast<uint32_t>(q >> 32) >> (13 + less) : 0u);
+    };
+    if (floor) R.for_each([&](float v, int i) { measure(v, kept_by(v, i)); });
+    else R.for_each([&](float v, int) { measure(v, v > -INFINITY); });
     mass = R.row_sum(mass);
     const double border = set.top_p * static_cast<double>(mass);
     bool found = false;
@@ -739,6 +743,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       u64 above = 0;
       // few entries are that large: a warp collects them, and weighs 32 at a time
       float* queue = sh.queue[warp];
+      const uint32_t below = (1u << lane) - 1, queue_at = ptx::smem_u32(queue);
       int queued = 0;
       auto weigh = [&](float v, bool on) {
         const Fixed z = w.z(v);
@@ -756,14 +761,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
         for (int q = 0; q < kPer; ++q) v[q] = -INFINITY;
         if (p < last_piece) R.load(p, v);
+        uint32_t to_list = 0;
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
-          const int i = R.base + p * kPer + q - R.off;
-          const bool in = (v[q] >= xb) & kept_by(v[q], i), over = in & (v[q] > xa);
+          bool in = v[q] >= xb;
+          if (floor) in &= kept_by(v[q], R.base + p * kPer + q - R.off);
+          const bool over = in & (v[q] > xa);
           const uint32_t lanes = __ballot_sync(0xffffffffu, over);
-          if (over) queue[queued + __popc(lanes & ((1u << lane) - 1))] = v[q];
+          // (a store under a predicate: the compiler would branch)
+          asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %0, 0;\n\t@p st.shared.f32 [%1], %2;\n\t}" ::"r"(static_cast<int>(over)),
+                       "r"(queue_at + 4 * (queued + __popc(lanes & below))), "f"(v[q]) : "memory");
           queued += __popc(lanes);
-          if (in & !over) R.list_add(v[q], i);
+          to_list |= static_cast<uint32_t>(in & !over) << q;
+        }
+        if (to_list != 0) {
+#pragma unroll
+          for (int q = 0; q < kPer; ++q)
+            if (to_list >> q & 1) R.list_add(v[q], R.base + p * kPer + q - R.off);
         }
         __syncwarp();
         int done = 0;
@@ -837,12 +851,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return only_if(kept_by(v, i) & at_least(z, z_min), w.weight(z));
   };
   if (!counted) {
-    R.for_each([&](float v, int i) {
-      const Fixed z = w.z(v);
-      const bool in = kept_by(v, i) & at_least(z, z_min);
-      sum += only_if(in, w.weight(z));
-      number += in;
-    });
+    if ((tx > -INFINITY) | (set.min_p > 0.0)) {
+      R.for_each([&](float v, int i) {
+        const Fixed z = w.z(v);
+        const bool in = kept_by(v, i) & at_least(z, z_min);
+        sum += only_if(in, w.weight(z));
+        number += in;
+      });
+    } else {
+      R.for_each([&](float v, int) {
+        const bool in = v > -INFINITY;
+        sum += only_if(in, w.weight(v));
+        number += in;
+      });
+    }
     sum = R.warp_sum(sum);
     __syncthreads();
     if (lane == 0) sh.sums[warp] = sum;
