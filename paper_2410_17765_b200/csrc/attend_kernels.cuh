@@ -604,7 +604,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
 
 // ------------------------------------------------------------------------------------------ joining the shares
 constexpr int kJoinThreads = 256;
-constexpr int kJoinTiles = 8;            // tiles whose weights one block adds to acc
+constexpr int kJoinTiles = 8;            // tiles whose weights one block adds to acc: four slots to a thread
+constexpr int kFewParts = 6;
 
 // (A CTA that has given up on a wait leaves its units' numbers unwritten.)
 __device__ __forceinline__ bool parts_known(const Params& p, int2 ctas) { return ctas.x >= 0 && ctas.x <= ctas.y && ctas.y < p.ctas; }
@@ -626,7 +627,7 @@ __device__ __forceinline__ float2 joined(const Params& p, int2 ctas, long long u
 }
 
 // Blocks [0, H * chunks) of a sequence join a unit's parts, a warp to a row; the others, with acc, add the weights of kJoinTiles
-// tiles of a head to acc, a thread to a slot.
+// tiles of a head to acc.
 template <int NT>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Params p) {
   __shared__ float sh[NT];
@@ -664,39 +665,63 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     }
     return;
   }
+  // a thread has four slots next to one another: scores are read 16 bytes at a time, and eight rows at once
   const int rest = blockIdx.x - p.c.H * p.chunks, h = rest % p.c.H, tile0 = rest / p.c.H * kJoinTiles;
   if (chunks == 0 || tile0 * kTile >= q.len) return;
-  constexpr int kPer = kJoinTiles * kTile / kJoinThreads;
-  float sum[kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) sum[i] = 0.f;
+  const int first = tile0 * kTile + 4 * threadIdx.x;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const long long unit_at = (static_cast<long long>(b) * p.c.H + h) * p.chunks + chunk;
     const int2 ctas = p.unit_ctas[unit_at];
     if (!parts_known(p, ctas)) return;
     const int rows = min(NT, all_rows - chunk * NT);
     __syncthreads();
-    for (int r = warp; r < rows; r += kJoinThreads / 32) {
-      const float2 ml = joined<NT>(p, ctas, unit_at, r);
-      if (lane == 0) sh[r] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+    if (ctas.y - ctas.x < kFewParts) {
+      // few parts: a thread to a row
+      if (threadIdx.x < NT) {
+        float m = kNone, l = 0.f;
+        if (threadIdx.x < rows) {
+          float2 ml[kFewParts];
+#pragma unroll
+          for (int i = 0; i < kFewParts; ++i) {
+            ml[i] = make_float2(kNone, 0.f);
+            if (ctas.x == ctas.y && i == 0) ml[i] = p.whole_ml[unit_at * NT + threadIdx.x];
+            else if (ctas.x + i <= ctas.y) ml[i] = p.part_ml[((ctas.x + i) * 2 + (i == 0 ? 1 : 0)) * NT + threadIdx.x];
+            m = fmaxf(m, ml[i].x);
+          }
+#pragma unroll
+          for (int i = 0; i < kFewParts; ++i) l += ml[i].y * ptx::ex2_approx(ml[i].x - m);
+        }
+        sh[threadIdx.x] = l == 0.f ? INFINITY : m + log2f(l);
+      }
+    } else {
+      for (int r = warp; r < rows; r += kJoinThreads / 32) {
+        const float2 ml = joined<NT>(p, ctas, unit_at, r);
+        if (lane == 0) sh[r] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+      }
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int slot = tile0 * kTile + i * kJoinThreads + threadIdx.x;
-      if (slot >= q.len) continue;
-      const float* s = p.scores + (unit_at * p.tiles + slot / kTile) * NT * kTile + slot % kTile;
-#pragma unroll 4
-      for (int r = 0; r < rows; ++r) sum[i] += ptx::ex2_approx(s[r * kTile] - sh[r]);
+    if (first >= q.len) continue;
+    const float4* s = reinterpret_cast<const float4*>(p.scores + (unit_at * p.tiles + first / kTile) * NT * kTile + first % kTile);
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r) {
+      const float4 v = s[r * (kTile / 4)];
+      const float f = sh[r];
+      sum.x += ptx::ex2_approx(v.x - f);
+      sum.y += ptx::ex2_approx(v.y - f);
+      sum.z += ptx::ex2_approx(v.z - f);
+      sum.w += ptx::ex2_approx(v.w - f);
     }
   }
+  if (first >= q.len) return;
+  // (pages are multiples of eight slots: the four lie in one)
+  const int page = p.s.table[b * p.s.ld_table + first / p.c.page_slots];
+  if (page < 0 || page >= p.c.pages) return;
+  float* acc = p.c.acc + page * p.c.acc_page + h * p.c.acc_head + first % p.c.page_slots;
+  const float add[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int slot = tile0 * kTile + i * kJoinThreads + threadIdx.x;
-    if (slot >= q.len) continue;
-    const int page = p.s.table[b * p.s.ld_table + slot / p.c.page_slots];
-    if (page >= 0 && page < p.c.pages) p.c.acc[page * p.c.acc_page + h * p.c.acc_head + slot % p.c.page_slots] += sum[i];
-  }
+  for (int i = 0; i < 4; ++i)
+    if (first + i < q.len) acc[i] += add[i];
 }
 
 }  // namespace attend
