@@ -631,8 +631,12 @@ typedef struct cpmtp_attend_args {
  *   p = softmax(s),  out[b, j, h] = sum_i p_i v_i,  lse[b, j, h] = log sum_i exp(s_i).
  * A token that sees no slot gets a row of zeros and lse -infinity.  Rows j >= q_lens[b] of out and lse are left as they were.
  * With cache->acc, acc of slot i and head g += the sum of p_i over the new tokens and the query heads that look at g.
- * A page number out of range stands for keys and values of zero.  Workspace: cpmtp_cache_attend_workspace_bytes, which looks at
- * numbers alone (and at whether cache->acc is NULL).
+ * A page number out of range stands for keys and values of zero.  A slot that only some of a call's tokens see has to hold finite values: its
+ * weight of zero for the others multiplies them (whatever lies in slots that none of them sees is not looked at).
+ * Sequences are shared out over the SMs by their tiles of 128 slots, whatever their lengths, and joined in a second launch: the last bits of
+ * out, lse and acc depend on the batch, and repeat for the same one.  Workspace: cpmtp_cache_attend_workspace_bytes, which looks at
+ * numbers alone (and at whether cache->acc is NULL), on the device of the call; with acc it holds a score for every row and slot.
+ * Limit: B * H * ceil(Q * Hq / H / 16 or 32) * ceil(width * page_slots / 128) < 2^31.
  */
 size_t cpmtp_cache_attend_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t Hq);
 int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_attend_args* args, void* workspace,
@@ -687,8 +691,11 @@ typedef struct cpmtp_sample_args {
  * temperature 0: the first entry, with log-probability 0.  Logits of -infinity and NaN are never kept; a row of nothing else gives token -1
  * and log-probability -infinity; logits of +infinity share the whole mass.  A given token that was not kept, or CPMTP_EMBED_PAD, has
  * log-probability -infinity; any other outside [0, V) does too and raises dev_status to 1.
- * Weights are summed as 62-bit integers: the sums are exact and in no order; borders are decided in 64 bits (a weight's own relative error is below 2^-32).
- * In rows' own settings a temperature that is not above 0 counts as 0, a top_p that is not below 1 as 1, a min_p that is not above 0 as 0; a uniform below 0 draws
+ * Weights are summed as integers with 62 - ceil(log2 V) bits below the point: the sums are exact in any order, so results do not depend on the batch.  A weight's
+ * own relative error is below 2^-32, and what it loses below its last bit.  Next to a logit of +infinity the largest finite number counts as infinite.
+ * Rows that do not start on a 16-byte boundary are read from the boundary before on and to the one behind their end: the bytes around them, in the
+ * same 16, are read and not used.
+ * In rows' own settings a temperature that is not above 0 counts as 0, a top_p that is not below 1 as 1, a min_p that is not above 0 as 0; a uniform that is not above 0 draws
  * as 0, one not below 1 the last entry that has weight.  No workspace is needed.
  */
 int cpmtp_sample_logits(const cpmtp_sample_args* args, int32_t* dev_status, cpmtp_stream stream);

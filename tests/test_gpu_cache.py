@@ -190,7 +190,7 @@ def test_attend_of_a_cache_in_one_tensor():
     assert torch.equal(got, want)
 
 
-def test_attend_bits_repeat_and_do_not_depend_on_the_batch():
+def test_attend_bits_repeat():
     from paper_2410_17765_b200 import binding
 
     c = Case([777, 1300, 64], 2, 64, 64, Hq=8, acc=False)
