@@ -151,7 +151,7 @@ struct Row {
 
   __device__ __forceinline__ void sync() const { sync_row(ctas); }
 
-  __device__ __forceinline__ void unpack(int piece, const uint4& raw, float (&v)[kPer]) const {
+  static __device__ __forceinline__ void unpack(const uint4& raw, float (&v)[kPer]) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -162,26 +162,51 @@ struct Row {
         v[(2 * q + 1) % kPer] = ptx::bf16_hi(w[q]);
       }
     }
-    if (piece == 0 || piece + 1 == pieces) {           // what does not belong to them counts as never kept
+  }
+  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const { unpack(__ldg(data + piece), v); }
+  // What a piece has beyond the block's entries counts as never kept; only the first and the last can.
+  __device__ __forceinline__ void limit(int piece, float (&v)[kPer]) const {
 #pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        const int i = piece * kPer + q - off;
-        if (i < 0 || i >= n) v[q] = -INFINITY;
-      }
+    for (int q = 0; q < kPer; ++q) {
+      const int i = piece * kPer + q - off;
+      if (i < 0 || i >= n) v[q] = -INFINITY;
     }
   }
-  __device__ __forceinline__ void load(int piece, float (&v)[kPer]) const { unpack(piece, __ldg(data + piece), v); }
+  // f(piece, its entries) for this warp's pieces, all lanes in step (a lane without a piece gets entries that are never kept): first those that lie
+  // inside, then the block's first and last one.
+  template <class F>
+  __device__ __forceinline__ void for_pieces(F f) const {
+    const int begin = warp * each, end = min(begin + each, pieces), inner = min(end, pieces - 1);
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (max(begin, 1) + lane < inner) raw = __ldg(data + max(begin, 1) + lane);
+#pragma unroll 1
+    for (int p = max(begin, 1) + lane; p - lane < inner; p += 32) {
+      float v[kPer];
+      unpack(raw, v);
+      if (p >= inner) {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) v[q] = -INFINITY;
+      }
+      if (p + 32 < inner) raw = __ldg(data + p + 32);          // under way meanwhile
+      f(p, v);
+    }
+    const int last = pieces - 1;
+    const bool has_first = begin == 0 && end > 0, has_last = last > 0 && last >= begin && last < end;
+    if (has_first || has_last) {
+      const int p = has_first && lane == 0 ? 0 : has_last && lane == 1 ? last : -1;
+      float v[kPer];
+      if (p >= 0) load(p, v);
+      limit(p < 0 ? -8 : p, v);
+      f(p, v);
+    }
+  }
   // f(logit, index in the row) for the entries of this warp's pieces.
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
-    const int end = min((warp + 1) * each, pieces);
-#pragma unroll 1
-    for (int p = warp * each + lane; p < end; p += 32) {
-      float v[kPer];
-      load(p, v);
+    for_pieces([&](int p, const float (&v)[kPer]) {
 #pragma unroll
       for (int q = 0; q < kPer; ++q) f(v[q], base + p * kPer + q - off);
-    }
+    });
   }
   __device__ __forceinline__ int warp_of(int index) const { return (index - base + off) / kPer / each; }
 
@@ -401,7 +426,10 @@ struct Row {
         const int p = p0 + t;
         float v[kPer];
         u64 g[kPer], sum = 0;
-        if (p < end) load(p, v);
+        if (p < end) {
+          load(p, v);
+          limit(p, v);
+        }
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
           g[q] = p < end ? f(v[q], base + p * kPer + q - off) : 0;
@@ -545,7 +573,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         const int p = p0 + j * kThreads;
         if (p >= R.pieces) break;
         float v[kPer];
-        R.unpack(p, raw[j], v);
+        R.unpack(raw[j], v);
+        if (p == 0 || p + 1 == R.pieces) R.limit(p, v);
 #pragma unroll
         for (int q = 0; q < kPer; ++q) top = fmaxf(top, v[q]);       // (which passes over NaN)
       }
@@ -753,14 +782,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         sum += only_if(in, q);
         number += in;
       };
-      const int last_piece = min((warp + 1) * R.each, R.pieces);
-#pragma unroll 1
-      for (int p0 = warp * R.each; p0 < last_piece; p0 += 32) {
-        const int p = p0 + lane;
-        float v[kPer];
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) v[q] = -INFINITY;
-        if (p < last_piece) R.load(p, v);
+      R.for_pieces([&](int p, const float (&v)[kPer]) {
         uint32_t to_list = 0;
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
@@ -789,7 +811,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           queued -= done;
         }
         __syncwarp();
-      }
+      });
       weigh(lane < queued ? queue[lane] : top, lane < queued);
       above = R.block_sum(above);
       const int mine = sh.listed;
