@@ -644,6 +644,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   int ti = INT_MIN;                          // (nothing: places before a piece's first entry have negative numbers)
   auto kept_by = [&](float v, int i) { return (v > tx) | ((v == tx) & (i <= ti)); };
 
+  // (of copies: what a function that is not inlined has the address of lives in memory)
+  auto by_digits = [&](auto in, bool by_mass, u64 want) {
+    R_t row_copy = R;
+    const Weigh w_copy = w;
+    float x;
+    int i;
+    row_copy.find_by_digits(w_copy, in, by_mass, want, x, i);
+    R.boxes = row_copy.boxes;
+    tx = x;
+    ti = i;
+  };
+
   // ---- top-k
   if (set.top_k < a.V) {
     bool found = false;
@@ -733,8 +745,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       R.for_each([&](float v, int) { valid += v > -INFINITY; });
       valid = R.row_sum(valid);
     }
-    if (!found && static_cast<u64>(set.top_k) < valid)
-      R.find_by_digits(w, [](float v, int) { return v > -INFINITY; }, false, set.top_k, tx, ti);
+    if (!found && static_cast<u64>(set.top_k) < valid) by_digits([](float v, int) { return v > -INFINITY; }, false, set.top_k);
   }
 
   const bool floor = tx > -INFINITY;         // (without one the passes ask for less)
@@ -865,7 +876,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       const float x1 = tx;
       const int i1 = ti;
       sum = number = 0;
-      R.find_by_digits(w, [=](float v, int i) { return v > x1 || (v == x1 && i <= i1); }, true, max(1ull, static_cast<u64>(ceil(border))), tx, ti);
+      by_digits([=](float v, int i) { return v > x1 || (v == x1 && i <= i1); }, true, max(1ull, static_cast<u64>(ceil(border))));
     }
   }
   auto drawn = [&](float v, int i) -> u64 {
