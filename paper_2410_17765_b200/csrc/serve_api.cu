@@ -159,16 +159,18 @@ cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const
   return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, vec, e.budget, e.recent, e.lens_out, kept, dev_status);
 }
 
-// Blocks of a cluster that share a row: what takes the least time if two blocks fit on an SM and a block takes 20 us and 1 ns an entry, or 1.5 where the
-// rows under way do not fit in L2 (measured with 1, 2, 4 and 8 blocks to each of 512 rows of 128256: 354, 323, 354 and 503 us; of 8 rows: 48, 34, 25
-// and 21).
+// Blocks of a cluster that share a row: what takes the least time if two blocks fit on an SM, a block takes 17 us, 3 more for every doubling of the
+// cluster, and half a nanosecond an entry if it has an SM to itself, one if not, one and a half if the rows under way do not fit in L2.
+// (Measured with top-p and 1, 2, 4 and 8 blocks: 512 rows of 128256 316, 311, 386 and 576 us; 64 rows 90, 59, 62 and 79; 8 rows 87, 57, 41 and 32; 64 rows
+// of 1024 19, 22, 25 and 46.)
 template <class T>
 cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, cudaStream_t st) {
   int ctas = 1;
   long long best = 0;
-  for (int n = 1; n <= cluster::kMostCtas; n *= 2) {
-    const long long waves = (static_cast<long long>(a.N) * n + 2 * sms - 1) / (2 * sms), rows = std::min<long long>(a.N, 2 * sms / n);
-    const long long entry = rows * a.V * static_cast<long long>(sizeof(T)) > (100ll << 20) ? 3 : 2, time = waves * (40000 + entry * (a.V / n));
+  for (int n = 1, k = 0; n <= cluster::kMostCtas; n *= 2, ++k) {
+    const long long blocks = static_cast<long long>(a.N) * n, waves = (blocks + 2 * sms - 1) / (2 * sms), rows = std::min<long long>(a.N, 2 * sms / n);
+    const int entry = rows * a.V * static_cast<long long>(sizeof(T)) > (100ll << 20) ? 3 : blocks > sms ? 2 : 1;
+    const long long time = waves * (34000 + 6000 * k + static_cast<long long>(entry) * (a.V / n));
     if (n > 1 && time >= best) continue;
     best = time;
     ctas = n;
