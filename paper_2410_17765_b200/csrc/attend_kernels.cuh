@@ -197,9 +197,16 @@ __device__ __forceinline__ float warp_max(float v) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1, int c2, int c3) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1, int c2, int c3, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy) : "memory");
+}
+// What is read once is the first to leave L2, so that the scores and parts, which are read again, stay.
+__device__ __forceinline__ uint64_t l2_policy(bool once) {
+  uint64_t p;
+  if (once) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
 __device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
   ptx::tmem_ld_32x16(addr, v);
@@ -283,6 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     };
     // (a ring has one warp that fills it: a second one could be a whole lap ahead, which the parity of a barrier does not tell)
     const int base = warp == 0 ? 0 : p.k_slots, n = warp == 0 ? p.k_slots : p.v_slots;
+    const uint64_t policy = l2_policy(p.chunks == 1);      // (another chunk of rows reads the same tiles, at about the same time)
     int it = 0, page = w.left > 0 ? page_at(w) : -1;
     bool alive = true;
     while (w.left > 0 && alive) {
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       if (!alive) break;
       if (here >= 0 && !skip) {
         const uint32_t dst = ring + s * slot_bytes + lane * p.piece * 128u;
-        for (int half = 0; half < p.halves; ++half) tma_load_4d(dst + half * kHalfBytes, warp == 0 ? &tm_k : &tm_v, full(s), half * 64, in_page, h, here);
+        for (int half = 0; half < p.halves; ++half) tma_load_4d(dst + half * kHalfBytes, warp == 0 ? &tm_k : &tm_v, full(s), half * 64, in_page, h, here, policy);
       }
       ++it;
     }
