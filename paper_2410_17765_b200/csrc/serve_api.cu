@@ -138,13 +138,13 @@ size_t evict_bytes(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int budget) 
 }
 
 // Blocks of a cluster that share the slots of a head: enough to use all SMs and to hold the keys in half of an SM's shared memory, as long as
-// each has some slots for its threads.
+// each has some slots for its threads (128 heads of 4352 slots with 1, 2, 4 and 8 blocks: 83, 82, 84 and 84 us; 16 of 65536 with 2, 4 and 8: 40, 29 and 28).
 cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const cpmtp_evict_args& e, int* kept, int sms, int* dev_status, cudaStream_t st) {
   constexpr size_t kMost = 232448, kShare = 110000;
   const int slots = s.width * c.page_slots;
   int ctas = 1;
   while (ctas < cluster::kMostCtas && slots / ctas >= 4 * cache::kSelectThreads &&
-         (static_cast<size_t>(slots) * 4 / ctas > kShare || static_cast<long long>(s.B) * c.H * ctas < 2ll * sms))
+         (static_cast<size_t>(slots) * 4 / ctas > kShare || static_cast<long long>(s.B) * c.H * ctas < sms))
     ctas *= 2;
   const int span = ((slots + ctas - 1) / ctas + 31) / 32 * 32;
   const int vec = aligned(c.acc, 16) && c.acc_page % 4 == 0 && c.acc_head % 4 == 0;
