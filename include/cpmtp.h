@@ -654,7 +654,7 @@ typedef struct cpmtp_evict_args {
  * Cuts sequences down to `budget` slots for each head: the `recent` last slots stay, and of the others those with the largest acc (NaN
  * counts as the least; of equals the lowest slots).  The kept slots' keys, values and acc go, in their order, to other pages, which must not be
  * among those that the table names; a sequence that is short enough goes there whole.  Slots and pages out of range are left out.
- * seqs->Q and q_lens are not used.  Workspace: cpmtp_cache_evict_workspace_bytes.
+ * seqs->Q and q_lens are not used.  Workspace: cpmtp_cache_evict_workspace_bytes; none is needed where `kept` is given.
  */
 size_t cpmtp_cache_evict_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t budget);
 int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_evict_args* args, void* workspace,

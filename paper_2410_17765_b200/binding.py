@@ -1363,7 +1363,7 @@ def cache_attend(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: 
 
 
 def cache_evict(cache: PagedCache, table: torch.Tensor, lens: torch.Tensor, table_out: torch.Tensor, budget: int, *, recent: int = 0,
-                out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> dict:
+                out: Optional[dict] = None, dev_status: Optional[torch.Tensor] = None) -> dict:
     """cpmtp_cache_evict: cut every sequence down to `budget` slots for each head, the `recent` last ones and those of the others with the
     largest cache.acc, and move them into the pages of table_out [B, ceil(budget / page_slots) or more] int32, which must not be among those of
     `table`.  Returns {"lens" [B], "kept" [B, H, budget] slots (-1 behind the last)} int32."""
@@ -1387,11 +1387,7 @@ def cache_evict(cache: PagedCache, table: torch.Tensor, lens: torch.Tensor, tabl
     if kept.shape != (B, c.H, budget) or kept.dtype is not torch.int32 or kept.get_device() != dev or not kept.is_contiguous():
         raise CpmtpError(f"cpmtp: kept must be a contiguous {[B, c.H, budget]} int32 on the same device")
     a = CEvictArgs(table_out.data_ptr(), ld, budget, recent, _ints(res["lens"], B, dev, "out lens"), kept.data_ptr())
-    lib = load_library()
-    if workspace is None:
-        workspace = alloc_workspace(lib.cpmtp_cache_evict_workspace_bytes(c, s, budget), lens.device)
-    pw, nw = _workspace(workspace, dev)
-    rc = lib.cpmtp_cache_evict(c, s, a, pw, nw, _status(dev_status, dev), _raw_stream(dev))
+    rc = load_library().cpmtp_cache_evict(c, s, a, None, 0, _status(dev_status, dev), _raw_stream(dev))
     if rc:
         _check(rc)
     return res
@@ -1426,17 +1422,17 @@ def sample_logits(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.
     (t, pt), (k, pk) = _setting(temperature, N, torch.float32, dev, "temperature"), _setting(top_k, N, torch.int32, dev, "top_k")
     (p, pp), (m, pm) = _setting(top_p, N, torch.float32, dev, "top_p"), _setting(min_p, N, torch.float32, dev, "min_p")
     res = out if out is not None else {}
-    new = dict(device=logits.device)
+    f32, i32 = torch.float32, torch.int32
+    pu = _vector(uniform, N, f32, dev, "uniform")
     if "tokens" not in res:
-        res["tokens"] = torch.empty(N, dtype=torch.int32, **new)
+        res["tokens"] = torch.empty_like(uniform, dtype=i32)
     if "logp" not in res:
-        res["logp"] = torch.empty(N, dtype=torch.float32, **new)
+        res["logp"] = torch.empty_like(uniform)
     if given is not None and "logp_given" not in res:
-        res["logp_given"] = torch.empty(N, dtype=torch.float32, **new)
+        res["logp_given"] = torch.empty_like(uniform)
     if want_kept and "kept" not in res:
-        res["kept"] = torch.empty(N, dtype=torch.int32, **new)
-    f32 = torch.float32
-    a = CSampleArgs(pl, ld, N, V, _TYPES[dtype], k, t, p, m, 0, pt, pk, pp, pm, _vector(uniform, N, f32, dev, "uniform"),
+        res["kept"] = torch.empty_like(uniform, dtype=i32)
+    a = CSampleArgs(pl, ld, N, V, _TYPES[dtype], k, t, p, m, 0, pt, pk, pp, pm, pu,
                     None if given is None else _ints(given, N, dev, "given"), _ints(res["tokens"], N, dev, "tokens"), _vector(res["logp"], N, f32, dev, "logp"),
                     None if given is None else _vector(res["logp_given"], N, f32, dev, "logp_given"),
                     _ints(res["kept"], N, dev, "kept") if "kept" in res else None)

@@ -206,7 +206,7 @@ int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   ProfScope prof(CPMTP_STAGE_CACHE_APPEND, st);
-  const dim3 grid(blocks_for(static_cast<long long>(s.B) * s.Q * c.H * (c.D / 8), cache::kThreads, di->sms));
+  const dim3 grid(blocks_for(static_cast<long long>(s.B) * ((s.Q + cache::kTokens - 1) / cache::kTokens) * c.H * (c.D / 8), cache::kThreads, di->sms));
   if (tokens_vec(*k) && tokens_vec(*v)) CPMTP_TRY(launch_pdl(cache::append_kernel<true>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   else CPMTP_TRY(launch_pdl(cache::append_kernel<false>, grid, dim3(cache::kThreads), 0, st, c, s, *k, *v, dev_status));
   return CPMTP_OK;
@@ -283,11 +283,11 @@ int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, co
   if (e.ld_table_out < (e.budget + c.page_slots - 1) / c.page_slots) return CPMTP_ERR_SHAPE;
   if (s.B == 0) return CPMTP_OK;
   if ((rc = check_cache_data(c)) != CPMTP_OK || (rc = check_seqs_data(s)) != CPMTP_OK) return rc;
-  if (c.acc == nullptr || e.table_out == nullptr || e.lens_out == nullptr || workspace == nullptr) return CPMTP_ERR_NULL;
+  if (c.acc == nullptr || e.table_out == nullptr || e.lens_out == nullptr || (workspace == nullptr && e.kept == nullptr)) return CPMTP_ERR_NULL;
   if (e.lens_out == s.lens) return CPMTP_ERR_SHAPE;
   if (!aligned(e.table_out, 4) || !aligned(e.lens_out, 4) || !aligned(e.kept, 4) || !aligned(dev_status, 4) || !aligned(workspace, kAlign))
     return CPMTP_ERR_ALIGN;
-  if (workspace_bytes < evict_bytes(c, s, e.budget)) return CPMTP_ERR_WORKSPACE;
+  if (e.kept == nullptr && workspace_bytes < evict_bytes(c, s, e.budget)) return CPMTP_ERR_WORKSPACE;
   DeviceInfo* di = nullptr;
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

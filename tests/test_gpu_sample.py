@@ -135,6 +135,26 @@ def test_peaked_and_flat_rows():
     check(x, u)
 
 
+@pytest.mark.parametrize("how", [dict(p=0.9), dict(k=30), dict(k=5000, p=0.7), dict(min_p=0.01)], ids=str)
+def test_results_do_not_depend_on_the_batch(how):
+    """Rows alone, in a few and in many: shared out over 8, 4, 2 and 1 blocks."""
+    from paper_2410_17765_b200 import binding
+
+    names = dict(p="top_p", k="top_k", min_p="min_p")
+    x, u = draw(400, 50000, 12, torch.float32)
+    args = {names[k]: v for k, v in how.items()}
+    want = binding.sample_logits(x, u, want_kept=True, **args)
+    for n in (1, 3, 20, 60, 140, 200):
+        got = binding.sample_logits(x[:n], u[:n], want_kept=True, **args)
+        assert all(torch.equal(got[k], want[k][:n]) for k in want)
+
+
+@pytest.mark.parametrize("how", [dict(p=0.9), dict(k=100000, p=0.8), dict(min_p=0.5), dict()], ids=str)
+def test_a_vocabulary_of_millions(how):
+    x, u = draw(1, 3000001, 5, torch.float32)
+    check(x, u, sure=False, **how)
+
+
 def test_shares_of_draws():
     """20000 draws of one row: each count within five standard deviations of its mean."""
     from paper_2410_17765_b200 import binding

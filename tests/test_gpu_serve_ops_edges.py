@@ -86,12 +86,11 @@ def test_evict_and_sample_replay_from_a_graph():
 
     c = Case([500, 90, 300], 2, 16, 16, more=4, seed=6)
     cache, out, drawn = c.cache(), {}, {}
-    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
     x, u = torch.randn(5, 3001, device="cuda"), torch.rand(5, device="cuda")
     T = torch.full((5,), 0.7, device="cuda")
 
     def step():
-        binding.cache_evict(cache, c.table, c.lens_t, c.table_out, 64, recent=9, out=out, workspace=ws)
+        binding.cache_evict(cache, c.table, c.lens_t, c.table_out, 64, recent=9, out=out)
         binding.sample_logits(x, u, temperature=T, top_k=40, top_p=0.9, want_kept=True, out=drawn)
 
     step()

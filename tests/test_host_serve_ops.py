@@ -156,6 +156,8 @@ def test_evict_arguments_are_checked(lib):
     assert lib.cpmtp_cache_evict(cache(acc=None), s, evict(), P, need, None, None) == -1
     assert lib.cpmtp_cache_evict(c, s, evict(), P, need - 1, None, None) == -4
     assert lib.cpmtp_cache_evict(c, s, evict(), None, need, None, None) == -1
+    if NO_GPU:                                   # with `kept` none is needed
+        assert lib.cpmtp_cache_evict(c, s, evict(kept=P), None, 0, None, None) in (-5, -6)
     assert lib.cpmtp_cache_evict(c, seqs(B=0), evict(), None, 0, None, None) == 0
 
 
