@@ -30,14 +30,16 @@ using cluster::store_remote;
 using cluster::sync_row;
 using cluster::u64;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 using cluster::kMostCtas;
 constexpr int kBins = 2048;            // of the histogram, 64 to a factor of two
-constexpr int kList = 2048;            // entries that one block sorts
+constexpr int kList = 2048;            // entries that one block sorts ...
+constexpr int kCounted = 192;          // ... by counting the larger ones for each (more: by a bitonic network)
 constexpr int kTable = 1024;           // powers of two between one and two
 constexpr int kQueue = 9 * 32;         // logits that a warp collects before it weighs them
 
+template <int THREADS>
 struct Shared {
+  static constexpr int kWarps = THREADS / 32;
   u64 table[kTable];
   u64 list[kList];
   union {
@@ -54,8 +56,6 @@ struct Shared {
   u64 word[4];
   int listed, number[3];
 };
-
-static_assert(sizeof(Shared) % 16 == 0, "the row's entries follow");
 
 // -------------------------------------------------------------------------------------------- keys and weights
 // Unsigned keys in the order of the logits.
@@ -138,10 +138,12 @@ __device__ __forceinline__ Settings settings_of(const cpmtp_sample_args& a, int 
 // -------------------------------------------------------------------------------------------- the kernel
 // A cluster of `ctas` blocks to a row.  A block's entries are read in whole 16-byte pieces, the first and last of which may reach beyond
 // them; its warps have equal ranges of pieces.
-template <class T>
+template <class T, int THREADS>
 struct Row {
+  static constexpr int kThreads = THREADS, kWarps = THREADS / 32;
+  static constexpr int kEach = kList / THREADS;        // entries of a full list to a thread
   static constexpr int kPer = 16 / sizeof(T);
-  Shared& sh;
+  Shared<THREADS>& sh;
   const int ctas, rank, t, lane, warp;
   int base, n;           // this block's entries
   int off;               // entries of the first piece that lie before them
@@ -269,7 +271,7 @@ struct Row {
   // before the first; the last bin where they are not reached.  Returns the whole sum.
   template <class Scale>
   __device__ __forceinline__ double find_bins(Scale scale, double low, double high, int& b1, int& b2, double& before) {
-    constexpr int kOwn = kBins / kThreads;
+    constexpr int kOwn = kBins / kThreads > 0 ? kBins / kThreads : 1;
     sync();                                            // the blocks' histograms are complete
     const int per = kBins / ctas, mine_of = (per + kThreads - 1) / kThreads;       // bins of this block, of a thread
     double mine[kOwn], sum = 0.0;
@@ -370,7 +372,7 @@ struct Row {
   // Sorts the first `count` keys of this block's list, falling; they are all different.
   __device__ __forceinline__ void sort_list(int count) {
     __syncthreads();
-    if (count <= kThreads) {
+    if (count <= kThreads && count <= kCounted) {
       // a key's place is the number of larger ones
       const u64 mine = t < count ? sh.list[t] : 0;
       int place = 0;
@@ -400,13 +402,13 @@ struct Row {
         __syncthreads();
       }
   }
-  // Running sums over the block of four numbers to a thread, those of entries 4 t .. 4 t + 3: v becomes the sum up to and with itself.
-  __device__ __forceinline__ void scan4(u64 (&v)[4]) {
+  // Running sums over the block of kEach numbers to a thread, those of entries kEach t and on: v becomes the sum up to and with itself.
+  __device__ __forceinline__ void scan_list(u64 (&v)[kEach]) {
 #pragma unroll
-    for (int j = 1; j < 4; ++j) v[j] += v[j - 1];
-    const u64 before = block_scan(v[3]) - v[3];
+    for (int j = 1; j < kEach; ++j) v[j] += v[j - 1];
+    const u64 before = block_scan(v[kEach - 1]) - v[kEach - 1];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += before;
+    for (int j = 0; j < kEach; ++j) v[j] += before;
   }
 
   // The first entry at which the running sum of f over the row exceeds `target`, as (index + 1) << 32 | logit; sh.sums has the warps'
@@ -531,17 +533,18 @@ struct Row {
   }
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ cpmtp_sample_args a, int ctas, int span, int bits, int* dev_status) {
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const __grid_constant__ cpmtp_sample_args a, int ctas, int span, int bits, int* dev_status) {
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  constexpr int kThreads = THREADS, kWarps = THREADS / 32;
+  Shared<THREADS>& sh = *reinterpret_cast<Shared<THREADS>*>(smem);
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int rank = static_cast<int>(blockIdx.x) % ctas, row = static_cast<int>(blockIdx.x) / ctas;
   // between one and two, while nothing else can be done
   for (int i = t; i < kTable; i += kThreads) sh.table[i] = static_cast<u64>(exp2(static_cast<double>(i) / kTable) * 4611686018427387904.0);
   ptx::grid_dep_wait();
-  using R_t = Row<T>;
-  constexpr int kPer = R_t::kPer;
+  using R_t = Row<T, THREADS>;
+  constexpr int kPer = R_t::kPer, kEach = R_t::kEach;
   const T* src = static_cast<const T*>(a.logits) + row * a.ld;
   R_t R{sh, ctas, rank, t, lane, warp, 0, 0, 0, 0, 1, nullptr, 0};
   R.base = min(rank * span, a.V);
@@ -686,27 +689,27 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           R.sync();
           if (rank != 0) return;
           R.sort_list(count);
-          u64 v[4], own[4];
-          Fixed z[4];
+          u64 v[kEach], own[kEach];
+          Fixed z[kEach];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 4 * t + j;
+          for (int j = 0; j < kEach; ++j) {
+            const int i = kEach * t + j;
             z[j] = w.z(i < set.top_k ? R.entry_logit(sh.list[i]) : top);
             own[j] = v[j] = i < set.top_k ? w.weight(z[j]) : 0;
           }
-          R.scan4(v);
+          R.scan_list(v);
           const double border = set.top_p * static_cast<double>(R.block_total());
           u64 left = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 4 * t + j;
+          for (int j = 0; j < kEach; ++j) {
+            const int i = kEach * t + j;
             left += i < set.top_k && (set.top_p >= 1.0 || i == 0 || static_cast<double>(v[j] - own[j]) < border) && at_least(z[j], z_min);
           }
           const int kept = static_cast<int>(R.block_sum(left));
-          if (kept - 1 >= 4 * t && kept - 1 < 4 * t + 4) {
+          if (kept - 1 >= kEach * t && kept - 1 < kEach * (t + 1)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (kept - 1 == 4 * t + j) sh.word[2] = v[j];
+            for (int j = 0; j < kEach; ++j)
+              if (kept - 1 == kEach * t + j) sh.word[2] = v[j];
           }
           __syncthreads();
           const u64 total = sh.word[2], last = sh.list[kept - 1];
@@ -715,15 +718,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           for (int i = t; i < kept; i += kThreads) sh.list[i] = sh.list[i] << 32 | sh.list[i] >> 32;
           R.sort_list(kept);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 4 * t + j;
+          for (int j = 0; j < kEach; ++j) {
+            const int i = kEach * t + j;
             own[j] = v[j] = i < kept ? w.weight(key_logit(static_cast<uint32_t>(sh.list[i]))) : 0;
           }
-          R.scan4(v);
+          R.scan_list(v);
           const u64 target = target_of(total);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (v[j] > target && v[j] - own[j] <= target) sh.word[3] = sh.list[4 * t + j];
+          for (int j = 0; j < kEach; ++j)
+            if (v[j] > target && v[j] - own[j] <= target) sh.word[3] = sh.list[kEach * t + j];
           __syncthreads();
           finish(static_cast<int>(~static_cast<uint32_t>(sh.word[3] >> 32)), key_logit(static_cast<uint32_t>(sh.word[3])), total, kept,
                  R.entry_logit(last), R.entry_index(last));
@@ -833,16 +836,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         if (rank == 0) {
           // (its own entries stay in the list: their shares are found by index)
           R.sort_list(count);
-          u64 v[4], own[4];
+          u64 v[kEach], own[kEach];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) own[j] = v[j] = 4 * t + j < count ? w.weight(R.entry_logit(sh.list[4 * t + j])) : 0;
-          R.scan4(v);
+          for (int j = 0; j < kEach; ++j) own[j] = v[j] = kEach * t + j < count ? w.weight(R.entry_logit(sh.list[kEach * t + j])) : 0;
+          R.scan_list(v);
           u64 left = 0;
           bool reached = false;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            left += 4 * t + j < count && static_cast<double>(above + v[j] - own[j]) < border;
-            reached |= 4 * t + j < count && static_cast<double>(above + v[j]) >= border;
+          for (int j = 0; j < kEach; ++j) {
+            left += kEach * t + j < count && static_cast<double>(above + v[j] - own[j]) < border;
+            reached |= kEach * t + j < count && static_cast<double>(above + v[j]) >= border;
           }
           const int kept = static_cast<int>(R.block_sum(left));
           reached = __syncthreads_or(reached);

@@ -159,12 +159,25 @@ cudaError_t launch_select(const cpmtp_cache& c, const cpmtp_cache_seqs& s, const
   return rc != cudaSuccess ? rc : launch_clusters(ctas, cache::select_kernel<false>, grid, threads, sizeof(cache::Select), st, c, s, ctas, span, vec, e.budget, e.recent, e.lens_out, kept, dev_status);
 }
 
+template <class T, int THREADS>
+cudaError_t launch_sample(const cpmtp_sample_args& a, int ctas, int* dev_status, cudaStream_t st) {
+  const int span = ((a.V + ctas - 1) / ctas + 7) / 8 * 8;
+  int width = 0;
+  while ((1ll << width) < a.V) ++width;
+  constexpr int kBytes = static_cast<int>(sizeof(sample::Shared<THREADS>));
+  static bool done[64] = {};
+  const cudaError_t e = allow_smem(sample::sample_kernel<T, THREADS>, done, kBytes);
+  if (e != cudaSuccess) return e;
+  return launch_clusters(ctas, sample::sample_kernel<T, THREADS>, dim3(static_cast<unsigned>(a.N) * ctas), dim3(THREADS), kBytes, st, a, ctas, span, 62 - width, dev_status);
+}
 // Blocks of a cluster that share a row: what takes the least time if two blocks fit on an SM, a block takes 17 us, 3 more for every doubling of the
 // cluster, and half a nanosecond an entry if it has an SM to itself, one if not, one and a half if the rows under way do not fit in L2.
-// (Measured with top-p and 1, 2, 4 and 8 blocks: 512 rows of 128256 316, 311, 386 and 576 us; 64 rows 90, 59, 62 and 79; 8 rows 87, 57, 41 and 32; 64 rows
-// of 1024 19, 22, 25 and 46.)
+// (Measured with top-p and 1, 2, 4 and 8 blocks: 512 rows of 128256 311, 306, 381 and 572 us; 64 rows 89, 60, 62 and 79; 8 rows 88, 56, 42 and 32; 64 rows
+// of 1024 18, 22, 24 and 47.)  Many rows of few entries get blocks of half the size, four to an SM: 1000 x 1024 45 us against 67, 2000 x 32000 295 against
+// 319, but 512 x 128256 327 against 311.
 template <class T>
 cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, cudaStream_t st) {
+  if (a.N > 2 * sms && a.V <= 32768) return launch_sample<T, 256>(a, 1, dev_status, st);
   int ctas = 1;
   long long best = 0;
   for (int n = 1, k = 0; n <= cluster::kMostCtas; n *= 2, ++k) {
@@ -175,14 +188,7 @@ cudaError_t launch_sample(const cpmtp_sample_args& a, int sms, int* dev_status, 
     best = time;
     ctas = n;
   }
-  const int span = ((a.V + ctas - 1) / ctas + 7) / 8 * 8;
-  int width = 0;
-  while ((1ll << width) < a.V) ++width;
-  static bool done[64] = {};
-  const cudaError_t e = allow_smem(sample::sample_kernel<T>, done, static_cast<int>(sizeof(sample::Shared)));
-  if (e != cudaSuccess) return e;
-  return launch_clusters(ctas, sample::sample_kernel<T>, dim3(static_cast<unsigned>(a.N) * ctas), dim3(sample::kThreads), sizeof(sample::Shared), st, a, ctas, span, 62 - width,
-                         dev_status);
+  return launch_sample<T, 512>(a, ctas, dev_status, st);
 }
 
 }  // namespace

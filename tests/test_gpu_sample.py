@@ -122,9 +122,18 @@ def test_strided_rows(V, ld, shift, dtype):
 
 
 @pytest.mark.parametrize("N", [1, 8, 40, 150, 700])
-def test_numbers_of_rows(N):
+@pytest.mark.parametrize("how", [dict(k=30, p=0.9), dict(p=0.8), dict(k=1500, min_p=1e-4)], ids=str)
+def test_numbers_of_rows(N, how):
     x, u = draw(N, 2049, N, torch.bfloat16)
-    check(x, u, k=30, p=0.9, sure=False)
+    check(x, u, sure=False, **how)
+
+
+def test_many_rows_of_equals():
+    """Long runs of equal logits in rows that small blocks take."""
+    x = (torch.arange(320 * 3000, device="cuda") % 7).view(320, 3000).float()
+    u = torch.rand(320, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    for how in (dict(k=1100), dict(p=0.6), dict(k=2900, p=0.99)):
+        check(x, u, sure=False, **how)
 
 
 def test_peaked_and_flat_rows():
