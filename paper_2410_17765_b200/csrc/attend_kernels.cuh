@@ -677,6 +677,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const int rest = blockIdx.x - p.c.H * p.chunks, h = rest % p.c.H, tile0 = rest / p.c.H * kJoinTiles;
   if (chunks == 0 || tile0 * kTile >= q.len) return;
   const int first = tile0 * kTile + 4 * threadIdx.x;
+  // (pages are multiples of eight slots: the four lie in one; what acc holds is read while the rows' sums are)
+  const int page = first < q.len ? p.s.table[b * p.s.ld_table + first / p.c.page_slots] : -1;
+  const bool known = page >= 0 && page < p.c.pages;
+  float* acc = p.c.acc + (known ? page * p.c.acc_page + h * p.c.acc_head + first % p.c.page_slots : 0);
+  float old[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) old[i] = known && first + i < q.len ? acc[i] : 0.f;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const long long unit_at = (static_cast<long long>(b) * p.c.H + h) * p.chunks + chunk;
@@ -721,15 +728,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
       sum.w += ptx::ex2_approx(v.w - f);
     }
   }
-  if (first >= q.len) return;
-  // (pages are multiples of eight slots: the four lie in one)
-  const int page = p.s.table[b * p.s.ld_table + first / p.c.page_slots];
-  if (page < 0 || page >= p.c.pages) return;
-  float* acc = p.c.acc + page * p.c.acc_page + h * p.c.acc_head + first % p.c.page_slots;
   const float add[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (first + i < q.len) acc[i] += add[i];
+    if (known && first + i < q.len) acc[i] = old[i] + add[i];
 }
 
 }  // namespace attend
