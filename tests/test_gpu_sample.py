@@ -108,6 +108,8 @@ def test_infinities_and_nan(dtype):
     given = torch.tensor([1, 2, 0, 1, 3, 1], dtype=torch.int32, device="cuda")
     for how in (dict(), dict(k=2), dict(p=0.6), dict(min_p=0.1), dict(T=0.0), dict(T=1e-30)):
         check(x, u, given=given, sure=False, **how)
+        for others in ([2, 4, 1, 4, 1, 3], [3, 3, 4, 2, 0, 4]):
+            check(x, u, given=torch.tensor(others, dtype=torch.int32, device="cuda"), sure=False, **how)
     r = check(x[:1], u[:1])
     assert r["tokens"].tolist() == [-1] and r["kept"].tolist() == [0] and r["logp"].tolist() == [-inf]
 
