@@ -20,6 +20,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <climits>
+
 #include "cache_kernels.cuh"
 
 namespace cpmtp {
@@ -175,7 +177,8 @@ struct Layout {
   static constexpr int kBars = 512;
   static constexpr int kRows = NT / 2;               // of a group
   static constexpr int kGroup = 11 * kRows;          // words of a group's small arrays
-  static constexpr int kSmall = 2 * kGroup * 4 + 128;
+  static constexpr int kOdd = 2 * 2 * 128;           // words: of two units, the first slots with infinities of either sign in each column
+  static constexpr int kSmall = (2 * kGroup + kOdd) * 4 + 128;
   static constexpr int kFixed = 1024 + 2 * kQ + 2 * kP + kBars + kSmall;
   static constexpr int kTmem = 8 * NT;               // two S accumulators and two O, of the high and the low parts of the weights (6 NT)
 };
@@ -233,7 +236,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   // [ring of K][ring of V][queries x 2][weights: two tiles of (high, low)][barriers][small arrays]
   const uint32_t ring = raw + pad, qbuf = ring + (p.k_slots + p.v_slots) * slot_bytes, pbuf = qbuf + 2 * L::kQ, bars = pbuf + 2 * L::kP;
   float* small = reinterpret_cast<float*>(smem_raw + (bars + L::kBars - raw));
-  int* misc = reinterpret_cast<int*>(small + 2 * L::kGroup);  // [0..11] scan, [12..18] start, [20] TMEM address, [21] abort flag, [22], [23] the groups'
+  int* odd_sh = reinterpret_cast<int*>(small + 2 * L::kGroup);
+  int* misc = odd_sh + L::kOdd;  // [0..11] scan, [12..18] start, [20] TMEM address, [21] abort flag, [22], [23] the groups'
   Start* start_sh = reinterpret_cast<Start*>(misc + 12);
   volatile int* abort_flag = misc + 21;
   auto full = [&](int s) { return bars + 8u * s; };
@@ -430,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     int* bound = reinterpret_cast<int*>(alpha + R);                          // [R] slots that a row sees
     volatile int* group_abort = misc + 22 + group;
     float o[R], l[R];
-    int g = 0, flat = start.first;
+    int g = 0, flat = start.first, unit = 0;
     auto fail = [&] { *abort_flag = 1; *group_abort = 1; };
     auto wait = [&](uint32_t b, int phase) {
       if (!ptx::mbar_wait(b, phase & 1, abort_flag, wait_ns, false)) fail();
@@ -454,15 +458,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
         for (int r = 0; r < R; ++r) o[r] += v[r];
       }
     };
+    // A slot that some of the new tokens see must not reach the others by way of a weight of zero: infinities and NaN are taken out of its
+    // value, and `odd` keeps the first slot with each (NaN counts as both signs), for the sums of the rows that see it.
+    auto set_apart = [&](uint32_t row, int slot, int* odd) {
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t at = row + ((i ^ (x & 7)) << 4);
+        uint32_t e[4];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(e[0]), "=r"(e[1]), "=r"(e[2]), "=r"(e[3]) : "r"(at) : "memory");
+        bool some = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) some |= (~e[q] & 0x7f80u) == 0 || (~e[q] & 0x7f800000u) == 0;
+        if (!some) continue;
+        for (int q = 0; q < 8; ++q) {
+          uint16_t bits;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(at + 2 * q) : "memory");
+          if ((~bits & 0x7f80) != 0) continue;
+          const bool nan = (bits & 0x7f) != 0, negative = (bits & 0x8000) != 0;
+          int* first = odd + group * 64 + i * 8 + q;
+          if (nan || !negative) atomicMin(first, slot);
+          if (nan || negative) atomicMin(first + 128, slot);
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + 2 * q), "h"(static_cast<uint16_t>(0)) : "memory");
+        }
+      }
+    };
     bool alive = true;
-    while (w.left > 0) {
+    for (; w.left > 0; ++unit) {
       const int end = w.piece_end(), begin = w.t, tiles = end - begin;
       const int u_chunks = (w.q.fresh * p.G + NT - 1) / NT, h = w.u / u_chunks, row0 = (w.u % u_chunks) * NT + group * R;
       const int rows = min(R, w.q.fresh * p.G - row0);          // of this group; none: it keeps in step, and its weights are not looked at
       const long long unit_at = (static_cast<long long>(w.b) * p.c.H + h) * p.chunks + w.u % u_chunks;
       const int len = w.q.len, sure = len - (w.q.fresh - 1);    // every row sees the slots below `sure`
       if (group == 0 && begin == 0 && x == 0) p.unit_ctas[unit_at] = make_int2(blockIdx.x, cta_of(start, flat + w.q.tiles - 1));
-      if (end * kTile > sure) {
+      const bool ragged = end * kTile > sure;
+      int* odd = odd_sh + (unit & 1) * 256;                     // [sign][column] (the other group may still read the last unit's)
+      if (ragged) {
+        if (group < p.halves) odd[(x >> 6) * 128 + group * 64 + (x & 63)] = INT_MAX;
         if (x < R) bound[x] = x < rows ? len - (w.q.fresh - 1 - (row0 + x) / p.G) : len;
         group_sync(group);
       }
@@ -534,14 +564,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
             asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + NT * 128), "h"(static_cast<uint16_t>(lo)));
           }
         }
-        if ((t + 1) * kTile > len && group < p.halves) {
+        if (masked && group < p.halves) {
           // rows of V that no slot of the sequence fills: whatever lies there must not meet a weight of zero
           const int s = p.k_slots + g % p.v_slots;
           wait(full(s), g / p.v_slots);
-          if (slot >= len)
-            for (int half = group; half < p.halves; half += 2)
-              for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + s * slot_bytes + half * kHalfBytes + x * 128 + i * 16), "r"(0) : "memory");
+          const uint32_t row = ring + s * slot_bytes + group * kHalfBytes + x * 128;
+          if (slot >= len) {
+            for (int i = 0; i < 8; ++i) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(row + i * 16), "r"(0) : "memory");
+          } else if (slot >= sure) {
+            set_apart(row, slot, odd);
+          }
         }
         ptx::tc_fence_before_sync();
         ptx::fence_proxy_async_smem();
@@ -562,6 +594,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       if (!alive) break;
       if (rows > 0) {
         add_o(g - 1);
+        if (ragged && w.q.fresh > 1 && x < 64 * p.halves) {
+          const int above = odd[x], below = odd[128 + x];
+          if (min(above, below) != INT_MAX) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) o[r] += (above < bound[r] ? INFINITY : 0.f) + (below < bound[r] ? -INFINITY : 0.f);
+          }
+        }
         // sums over the slots' threads
         float mine = 0.f;
 #pragma unroll

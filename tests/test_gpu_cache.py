@@ -140,6 +140,52 @@ def test_attend_without_weights():
     check_attend(Case([100, 300], 2, 64, 16, Hq=4), want_acc=False)
 
 
+@pytest.mark.parametrize("H,Hq,D,lens,Q", [(2, 4, 128, [300, 131, 3], 5), (1, 1, 64, [258, 129, 40], 3), (2, 6, 72, [5000, 130, 0], 7), (1, 8, 40, [700, 300, 64], 45)])
+@pytest.mark.parametrize("of", ["keys", "values"])
+def test_attend_infinities_and_nan_reach_the_tokens_that_see_them(H, Hq, D, lens, Q, of):
+    """Slots of the new tokens hold them; some of the tokens see none of these slots, some one, some more.
+
+    Values leave the scores alone, so that the other tokens' bits stay.  Keys that are infinite may move the references that weights are taken
+    relative to: a weight is then off by 2^-20 + 2^-16, a sum of 5000 by 2 * 5000 * 2^-24 of mass <= 5, which is below 2^-7, and each result by 2^-8."""
+    from paper_2410_17765_b200 import binding
+
+    c = Case(lens, H, D, 16, Hq=Hq, Q=Q, seed=Q)
+    rng = np.random.default_rng(D)
+    where = []
+    for b, n in enumerate(lens):
+        for value in (float("inf"), float("-inf"), float("nan")):
+            slot, h, col = n - 1 - int(rng.integers(0, Q - 1)), int(rng.integers(0, H)), int(rng.integers(0, D))
+            if slot < 0:
+                continue
+            page, at = S.places(c.table_np[b], c.page, n)
+            where.append((h, col, value, int(page[slot]), int(at[slot])))
+    plain = check_attend(c, want_acc=False)
+    target = c.k if of == "keys" else c.v
+    for h, col, value, page, at in where:
+        target[page, at, h, col] = value
+    c.acc.zero_()
+    got = binding.cache_attend(c.cache(), c.q, c.table, c.lens_t, accumulate=True, dev_status=c.status)
+    assert int(c.status.item()) == 0
+    got, plain, acc, G = numbers(got["out"]), numbers(plain["out"]), numbers(c.acc), Hq // H
+    for b, n in enumerate(lens):
+        K, V = c.of(c.k, b), c.of(c.v, b)
+        for j in range(Q):
+            seen = max(0, n - (Q - 1 - j))
+            for hq in range(Hq):
+                h = hq // G
+                row, was = got[b, j, hq], plain[b, j, hq]
+                if np.isfinite(K[:seen, h]).all() and np.isfinite(V[:seen, h]).all():
+                    assert np.array_equal(row, was) if of == "values" else (np.abs(row - was) <= 2.0 ** -7 * np.abs(was) + 2.0 ** -7).all()
+                elif of == "values":
+                    want = np.where(np.isfinite(V[:seen, h]), 0.0, V[:seen, h]).sum(0)        # inf - inf is NaN
+                    assert np.array_equal(np.isnan(row), np.isnan(want))
+                    assert np.array_equal(row[np.isinf(want)], want[np.isinf(want)])
+                    assert np.array_equal(row[want == 0], was[want == 0])
+        if of == "values" and n:
+            page, at = S.places(c.table_np[b], c.page, n)
+            assert np.allclose(acc[page, :, at].sum(0), G * min(n, Q), rtol=2.0 ** -10)
+
+
 @pytest.mark.parametrize("std", [1e-3, 8.0, 60.0])
 def test_attend_scales(std):
     """Flat maps, and maps of one slot; a scale of its own, also a negative one."""
