@@ -7,8 +7,9 @@
 // block.  Should they be too many (long runs of equal logits, flat rows), the key of the last kept entry is found by digits instead.
 //
 // What bounds it: at many rows the instructions, about 35 for a weight and 8 for its bin; at few rows the latency of a dozen barriers of a
-// cluster.  Holding the row in shared memory was slower at many rows (512 x 128256 in bf16 with top-p: 473 us against 357), since it
-// leaves room for fewer blocks, and 1 us faster at few.
+// cluster.  512 x 128256 in fp32 (263 MB): greedy 62 us, top-k of 50 113, no filter 157, top-p 309; 8 rows in bf16: 6, 17, 19 and 31.  Holding the
+// row in shared memory was slower at many rows (512 x 128256 in bf16 with top-p: 473 us against 357 then), since it leaves room for fewer
+// blocks, and 1 us faster at few.
 #pragma once
 #include <cfloat>
 #include <climits>
@@ -267,10 +268,11 @@ struct Row {
   }
   __device__ __forceinline__ u64 row_sum(u64 v) { return sum_of(exchange(block_sum(v))); }
 
-  // First and second bin at which the running sum of the histogram, bin b weighing scale(b), reaches `low` and `high`, and what lies
-  // before the first; the last bin where they are not reached.  Returns the whole sum.
+  // The first bin at which the running sum of the histogram, bin b weighing scale(b), reaches `low` and leaves no more than low_left behind it, what lies
+  // before that bin, and the first bin at which the sum reaches `high` or leaves no more than high_left; the last bin where there is none.  Returns
+  // the whole sum.
   template <class Scale>
-  __device__ __forceinline__ double find_bins(Scale scale, double low, double high, int& b1, int& b2, double& before) {
+  __device__ __forceinline__ double find_bins(Scale scale, double low, double high, double low_left, double high_left, int& b1, int& b2, double& before) {
     constexpr int kOwn = kBins / kThreads > 0 ? kBins / kThreads : 1;
     sync();                                            // the blocks' histograms are complete
     const int per = kBins / ctas, mine_of = (per + kThreads - 1) / kThreads;       // bins of this block, of a thread
@@ -316,6 +318,8 @@ struct Row {
       total += __longlong_as_double(box[r]);
     }
     for (int w = 0; w < warp; ++w) run += sh.scan[w];
+    low = fmax(low, total - low_left);
+    high = fmin(high, total - high_left);
     // a thread begins with the very number that the one before it ends with, so that no border falls between them
     upto += run;
     const double left = __shfl_up_sync(0xffffffffu, upto, 1);
@@ -693,7 +697,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
         }
         int b, b2;
         double before;
-        valid = static_cast<u64>(R.find_bins([](int) { return 1.0; }, set.top_k, set.top_k, b, b2, before));
+        valid = static_cast<u64>(R.find_bins([](int) { return 1.0; }, set.top_k, set.top_k, INFINITY, -INFINITY, b, b2, before));
         if (counted ? static_cast<u64>(set.top_k) >= valid : static_cast<u64>(set.top_k) > valid || b == kBins - 1) continue;
         // all entries down to that bin, if they are few; else those of the bin
         const bool all = !counted || (before + kList / 2 <= kList && b < kBins - 1);
@@ -831,11 +835,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
     const double border = set.top_p * static_cast<double>(mass);
     bool found = false;
     {
-      // an entry of bin b has floor(z) = -ceil(b / 64); the sums are short by 2^(less - 17) at most
-      const double one = unit * ldexp(1.0, less - 17), slack = ldexp(1.0, less - 15);
+      // An entry of bin b has floor(z) = -ceil(b / 64).  A sum is short by 2^(less - 17) of itself at most, which bounds what lies before a border and
+      // what lies behind it: with top_p near one that is little, and so is then the doubt.  (A border by what lies before it alone: a row with
+      // top_p = 0.9996 took 140 us, a list too long.)  The last bin, where smaller weights are too, has no sum.
+      const double one = unit * ldexp(1.0, less - 17), slack = ldexp(1.0, less - 15), behind = static_cast<double>(mass) - border;
+      const double tiny = ldexp(static_cast<double>(mass), -45), least = static_cast<double>(a.V) * unit * ldexp(1.0, -31);
       int b1, b2;
       double before;
-      R.find_bins([&](int b) { return one * exp2f(static_cast<float>(-((b + 63) >> 6))); }, border * (1.0 - slack), border * (1.0 + slack), b1, b2, before);
+      R.find_bins([&](int b) { return b == kBins - 1 ? 0.0 : one * exp2f(static_cast<float>(-((b + 63) >> 6))); }, border * (1.0 - slack), border * (1.0 + slack),
+                  behind + tiny, (behind - least) * (1.0 - slack) - tiny, b1, b2, before);
       // Entries above xa lie in bins before b1, those below xb in bins behind b2; the bins' edges, rounded outwards.
       const float xa = nextafterf(__double2float_ru(w.m - (b1 - 1) / (64.0 * w.c)), INFINITY);
       const float xb = b2 == kBins - 1 ? -FLT_MAX : nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY);

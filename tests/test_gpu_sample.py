@@ -138,6 +138,16 @@ def test_many_rows_of_equals():
         check(x, u, sure=False, **how)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1000, 50001, 128256])
+def test_top_p_near_one(V, dtype):
+    """Borders with little mass behind them, and with little before them."""
+    x, u = draw(20, V, V, dtype)
+    near = [1 - 2.0 ** -k for k in range(4, 20)] + [2.0 ** -k for k in (3, 7, 11, 20)]
+    for min_p in (0.0, 1e-4):
+        check(x, u, p=torch.tensor(near, dtype=torch.float32, device="cuda"), min_p=min_p, given=x.argmax(1).int(), sure=False)
+
+
 def test_peaked_and_flat_rows():
     x, u = draw(6, 50000, 8, torch.float32, std=1e-3)
     check(x, u, p=0.8, sure=False)
