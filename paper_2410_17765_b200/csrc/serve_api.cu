@@ -75,7 +75,8 @@ int blocks_for(long long items, int threads, int sms) {
   return static_cast<int>(blocks < most ? blocks : most);
 }
 
-// Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.
+// Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.  16 rows with 16 and 32
+// columns: one sequence of 1024 slots 10.7 and 11.7 us, 64 ragged ones 226 and 232; 20 rows: 16 sequences of 4096 with acc 66 and 53, 32 of 8192 327 and 168.
 int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
   const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
   return rows <= 16 ? 16 : 32;
@@ -119,7 +120,7 @@ int piece_slots(int page_slots) {
 template <int NT>
 cudaError_t launch_attend(const CUtensorMap& tk, const CUtensorMap& tv, attend::Params& p, int sms, int* dev_status, cudaStream_t st) {
   constexpr int kMost = 232448;
-  const int slots = std::min((kMost - attend::Layout<NT>::kFixed) / (p.halves * attend::kHalfBytes), attend::kMaxSlots);
+  const int slots = std::min(kMost - attend::Layout<NT>::kFixed, attend::kMaxSlots * attend::kHalfBytes) / (p.halves * attend::kHalfBytes);
   p.k_slots = slots / 2;          // (a K tile is done with sooner than a V tile, which waits for the weights)
   p.v_slots = slots - p.k_slots;
   p.ctas = sms;
