@@ -148,6 +148,23 @@ def test_top_p_near_one(V, dtype):
         check(x, u, p=torch.tensor(near, dtype=torch.float32, device="cuda"), min_p=min_p, given=x.argmax(1).int(), sure=False)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,V", [(5, 128256), (5, 20011), (300, 20011), (5, 700)])
+def test_top_k_wherever_the_largest_lie(N, V, dtype):
+    """In order, in one thread's pieces, in few values, at the ends: the borders that a part of the row gives are too low then, or too long runs lie above them."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x, u = draw(5, V, N, torch.float32)
+    at = torch.arange(V, device="cuda")
+    x[0] = x[0].sort().values
+    x[1] = x[1].sort(descending=True).values
+    x[2] += 20.0 * ((at // 8) % 256 == 5)
+    x[3] = torch.randint(0, 3, (V,), generator=g, device="cuda").float() * (at < V - 3) + 5.0 * (at >= V - 2)
+    x[4, V // 2:] = float("-inf")
+    x, u = x.repeat(N // 5, 1).to(dtype), torch.rand(N, generator=g, device="cuda")
+    for k in (2, 50, 224, 225, 448, 449, 2048):
+        check(x, u, k=k, p=0.9 if k % 2 == 0 else 1.0, given=x.argmin(1).int(), sure=False)
+
+
 def test_peaked_and_flat_rows():
     x, u = draw(6, 50000, 8, torch.float32, std=1e-3)
     check(x, u, p=0.8, sure=False)
