@@ -10,6 +10,17 @@ namespace cluster {
 typedef unsigned long long u64;
 constexpr int kMostCtas = 8;
 
+// Shared memory of another block may be touched once that block has begun.  A kernel whose first access to it has no barrier of the cluster before it
+// tells the others that it is there, does what it can alone, and waits for them before that access.
+__device__ __forceinline__ void tell_begun(int ctas) {
+  if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void await_begun(int ctas) {
+  if (ctas > 1) {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+}
 __device__ __forceinline__ void sync_row(int ctas) {
   if (ctas == 1) {
     __syncthreads();

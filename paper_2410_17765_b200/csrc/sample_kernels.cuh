@@ -544,6 +544,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
   Shared<THREADS>& sh = *reinterpret_cast<Shared<THREADS>*>(smem);
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int rank = static_cast<int>(blockIdx.x) % ctas, row = static_cast<int>(blockIdx.x) / ctas;
+  cluster::tell_begun(ctas);
   // between one and two, while nothing else can be done
   for (int i = t; i < kTable; i += kThreads) sh.table[i] = static_cast<u64>(exp2(static_cast<double>(i) / kTable) * 4611686018427387904.0);
   ptx::grid_dep_wait();
@@ -602,6 +603,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
   top = tops[lane & (kWarps - 1)];
 #pragma unroll
   for (int o = kWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  cluster::await_begun(ctas);                // (told before the table, so the pass has covered the wait)
   {
     const u64* box = R.exchange(__float_as_uint(top));
     for (int r = 0; r < ctas; ++r) top = fmaxf(top, __uint_as_float(static_cast<uint32_t>(box[r])));
