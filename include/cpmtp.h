@@ -632,8 +632,8 @@ typedef struct cpmtp_attend_args {
  *   p = softmax(s),  out[b, j, h] = sum_i p_i v_i,  lse[b, j, h] = log sum_i exp(s_i).
  * A token that sees no slot gets a row of zeros and lse -infinity.  Rows j >= q_lens[b] of out and lse are left as they were.
  * With cache->acc, acc of slot i and head g += the sum of p_i over the new tokens and the query heads that look at g.
- * A page number out of range stands for keys and values of zero.  Infinities and NaN in a slot reach the tokens that see it and no others;
- * whatever lies in slots that no token sees is not looked at.
+ * A page number out of range stands for keys and values of zero.  Infinities and NaN in a slot reach the tokens that see it and no others: a value
+ * that is infinite counts so however small its weight (values of both signs give NaN).  Whatever lies in slots that no token sees is not looked at.
  * Sequences are shared out over the SMs by their tiles of 128 slots, whatever their lengths, and joined in a second launch: the last bits of
  * out, lse and acc depend on the batch, and repeat for the same one.  Workspace: cpmtp_cache_attend_workspace_bytes, which looks at
  * numbers alone (and at whether cache->acc is NULL), on the device of the call; with acc it holds a score for every row and slot.

@@ -26,6 +26,7 @@
 #pragma once
 #include <cuda.h>
 
+#include <cfloat>
 #include <climits>
 
 #include "cache_kernels.cuh"
@@ -489,6 +490,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
         }
       }
     };
+    // Whether this thread's column has +infinity (1), -infinity (2) or NaN (3) among the values of slots [s0, s1).
+    auto column_kinds = [&](int b, int h, int s0, int s1) {
+      const uint16_t* col = static_cast<const uint16_t*>(p.c.v) + h * p.c.v_head + x;
+      const int* pages = p.s.table + b * p.s.ld_table;
+      int kinds = 0;
+      for (int s = s0; s < s1 && kinds != 3; s += 8) {          // (pages are multiples of eight slots)
+        const int page = pages[s / p.c.page_slots];
+        if (page < 0 || page >= p.c.pages) continue;
+        const uint16_t* at = col + page * p.c.v_page + s % p.c.page_slots * p.c.v_slot;
+        uint16_t bits[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bits[i] = s + i < s1 ? at[i * p.c.v_slot] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((~bits[i] & 0x7f80) == 0) kinds |= (bits[i] & 0x7f) != 0 ? 3 : (bits[i] & 0x8000) != 0 ? 2 : 1;
+      }
+      return kinds;
+    };
     bool alive = true;
     for (; w.left > 0; ++unit) {
       const int end = w.piece_end(), begin = w.t, tiles = end - begin;
@@ -602,6 +621,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       if (!alive) break;
       if (rows > 0) {
         add_o(g - 1);
+        // A value that is infinite or NaN in a slot that every row sees has made all of this column so, but rarely of the right kind: the low part of its weight may be
+        // zero or negative.  Then the column's values say what it is (which takes nothing elsewhere: sums that have overflowed, or weights of NaN, stay).
+        if (x < p.c.D && !(fabsf(o[0]) <= FLT_MAX)) {
+          const int kinds = column_kinds(w.b, h, begin * kTile, min(end * kTile, sure));
+          if (kinds != 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) o[r] = (kinds & 1 ? INFINITY : 0.f) + (kinds & 2 ? -INFINITY : 0.f);
+          }
+        }
         if (ragged && w.q.fresh > 1 && x < 64 * p.halves) {
           const int above = odd[x], below = odd[128 + x];
           if (min(above, below) != INT_MAX) {
@@ -704,7 +732,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         const long long at = (c * 2 + (c == ctas.x ? 1 : 0)) * NT + r;
         const float f = ptx::ex2_approx(p.part_ml[at].x - ml.x);
         const float4 v = reinterpret_cast<const float4*>(p.part_o + at * 128)[lane];
-        sum.x += f * v.x; sum.y += f * v.y; sum.z += f * v.z; sum.w += f * v.w;
+        // (what is infinite is so with any factor, also one that has underflown)
+        sum.x += fabsf(v.x) <= FLT_MAX ? f * v.x : v.x;
+        sum.y += fabsf(v.y) <= FLT_MAX ? f * v.y : v.y;
+        sum.z += fabsf(v.z) <= FLT_MAX ? f * v.z : v.z;
+        sum.w += fabsf(v.w) <= FLT_MAX ? f * v.w : v.w;
       }
       const float inv = ml.y == 0.f ? 0.f : __fdividef(1.f, ml.y);
       const int row = chunk * NT + r, j = row / p.G, hq = h * p.G + row % p.G;

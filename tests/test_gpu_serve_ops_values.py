@@ -1,0 +1,67 @@
+"""Values at the ends of their range in the serving operators: what infinities, NaN and the largest scores come out as."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serve_ops as S
+from test_gpu_cache import Case, check_attend, numbers
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("std", [1.0, 60.0])           # (60: nearly all weights underflow)
+@pytest.mark.parametrize("H,Hq,D,page,lens,Q", [(2, 4, 128, 16, [300, 131, 1], 1), (1, 1, 64, 8, [258, 129, 40], 1), (2, 6, 72, 24, [5000, 130, 0], 7), (1, 8, 40, 64, [700, 300, 64], 45),
+                                                (1, 2, 128, 64, [40000], 3), (1, 20, 128, 256, [30000, 513], 1)])
+def test_infinite_values_of_older_slots_come_out_as_they_are(H, Hq, D, page, lens, Q, std):
+    """Every token sees these slots: the columns that hold them are infinite or NaN for all tokens, as their sum is, whatever the weights; all other bits stay."""
+    from paper_2410_17765_b200 import binding
+
+    c = Case(lens, H, D, page, Hq=Hq, Q=Q, seed=Q + D, std=std, acc=False)
+    plain = check_attend(c)
+    rng = np.random.default_rng(D)
+    for b, n in enumerate(lens):
+        old = n - Q + 1                                  # slots that all tokens see
+        if old <= 0:
+            continue
+        page_of, at = S.places(c.table_np[b], page, n)
+        slots = [0, old - 1] + [int(s) for s in rng.integers(0, old, 6)]
+        for col, kinds in enumerate([(INF,), (-INF,), (NAN,), (INF, -INF), (INF, INF), (-INF, -INF), (INF, NAN)]):
+            for value in kinds:
+                slot = slots[int(rng.integers(0, len(slots)))]
+                c.v[int(page_of[slot]), int(at[slot]), int(rng.integers(0, H)), col] = value
+        if Q > 1:                                        # one of both kinds, and in the slots of the draft as well
+            c.v[int(page_of[0]), int(at[0]), 0, D - 1] = INF
+            c.v[int(page_of[n - 1]), int(at[n - 1]), 0, D - 1] = -INF
+    out = {"lse": torch.zeros(len(lens), Q, Hq, device="cuda")}
+    got = numbers(binding.cache_attend(c.cache(), c.q, c.table, c.lens_t, out=out, dev_status=c.status)["out"])
+    assert int(c.status.item()) == 0 and torch.equal(out["lse"], plain["lse"])
+    was = numbers(plain["out"])
+    met = set()
+    for b, n in enumerate(lens):
+        V = c.of(c.v, b)
+        for j in range(Q):
+            seen = max(0, n - (Q - 1 - j))
+            for hq in range(Hq):
+                v = V[:seen, hq // (Hq // H)]
+                with np.errstate(invalid="ignore"):
+                    want = np.where(np.isfinite(v), 0.0, v).sum(0)
+                row = got[b, j, hq]
+                met |= set(want[want != 0].tolist())
+                assert np.array_equal(np.isnan(row), np.isnan(want)), (b, j, hq)
+                assert np.array_equal(row[np.isinf(want)], want[np.isinf(want)])
+                assert np.array_equal(row[want == 0], was[b, j, hq][want == 0])
+    assert INF in met and -INF in met
+
+
+def test_values_that_overflow_or_are_nan_by_their_weights_stay_so():
+    """A key of NaN: its row's results are NaN in every column, with and without an infinite value beside it."""
+    from paper_2410_17765_b200 import binding
+
+    c = Case([200, 90], 1, 64, 16, Hq=4, seed=1, acc=False)
+    page, at = S.places(c.table_np[0], 16, 200)
+    c.k[int(page[5]), int(at[5]), 0, 3] = NAN
+    c.v[int(page[9]), int(at[9]), 0, 7] = INF
+    got = numbers(binding.cache_attend(c.cache(), c.q, c.table, c.lens_t)["out"])
+    assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
