@@ -581,6 +581,8 @@ int cpmtp_grad_norm(const cpmtp_adamw_tensor* tensors, int32_t count, float max_
  * k[page * k_page + slot * k_slot + head * k_head + i]; so both orders, heads within slots and slots within heads, are served.
  * All distances are in elements; those of k and v and both addresses have to be multiples of 16 bytes.
  * `acc`, where it is not NULL, holds the attention weight that a slot has received, for each head: acc[page * acc_page + head * acc_head + slot].
+ * Neither rows of the keys, nor those of the values, nor runs of page_slots numbers of acc may overlap: of two distances the larger has to reach
+ * over all that the smaller spans.
  */
 typedef struct cpmtp_cache {
   void *k, *v;                      /* bf16 */

@@ -20,20 +20,37 @@ using io::bf16_t;
 
 constexpr int64_t kMaxStride = int64_t{1} << 38;       // elements: what a tensor map's strides hold
 
+// Whether rows of `extent` elements at all places of some dimensions lie apart from one another.  (Sorts the dimensions.)
+struct Dim { int64_t stride, size; };
+template <int N>
+bool apart(Dim (&d)[N], int64_t extent) {
+  std::sort(d, d + N, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  for (const Dim& x : d) {
+    if (x.size <= 1) continue;
+    if (x.stride < extent) return false;
+    extent += x.stride * (x.size - 1);
+  }
+  return true;
+}
+
 // Distances of a cache's pages, slots and heads: rows of D elements must not overlap.
 int check_strides(const cpmtp_cache& c, int64_t page, int64_t slot, int64_t head) {
-  struct Dim { int64_t stride, size; } d[3] = {{page, c.pages}, {slot, c.page_slots}, {head, c.H}};
-  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
-  int64_t extent = c.D;
+  Dim d[3] = {{page, c.pages}, {slot, c.page_slots}, {head, c.H}};
   for (const Dim& x : d) {
     if (x.stride < 0) return CPMTP_ERR_SHAPE;
     if (x.stride >= kMaxStride) return CPMTP_ERR_LIMIT;
     if (x.stride % 8 != 0) return CPMTP_ERR_ALIGN;
-    if (x.size == 1) continue;
-    if (x.stride < extent) return CPMTP_ERR_SHAPE;
-    extent += x.stride * (x.size - 1);
   }
-  return CPMTP_OK;
+  return apart(d, c.D) ? CPMTP_OK : CPMTP_ERR_SHAPE;
+}
+// Those of the pages and heads of acc, whose slots lie next to one another.
+int check_acc(const cpmtp_cache& c) {
+  Dim d[2] = {{c.acc_page, c.pages}, {c.acc_head, c.H}};
+  for (const Dim& x : d) {
+    if (x.stride < c.page_slots) return CPMTP_ERR_SHAPE;
+    if (x.stride >= kMaxStride) return CPMTP_ERR_LIMIT;
+  }
+  return apart(d, c.page_slots) ? CPMTP_OK : CPMTP_ERR_SHAPE;
 }
 
 int check_cache(const cpmtp_cache* c) {
@@ -44,8 +61,7 @@ int check_cache(const cpmtp_cache* c) {
   int rc;
   if ((rc = check_strides(*c, c->k_page, c->k_slot, c->k_head)) != CPMTP_OK || (rc = check_strides(*c, c->v_page, c->v_slot, c->v_head)) != CPMTP_OK)
     return rc;
-  if (c->acc != nullptr && (c->acc_head < c->page_slots || c->acc_page < c->page_slots)) return CPMTP_ERR_SHAPE;
-  return CPMTP_OK;
+  return c->acc != nullptr ? check_acc(*c) : CPMTP_OK;
 }
 int check_cache_data(const cpmtp_cache& c) {
   if (c.k == nullptr || c.v == nullptr) return CPMTP_ERR_NULL;
