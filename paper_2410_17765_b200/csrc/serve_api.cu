@@ -20,17 +20,20 @@ using io::bf16_t;
 
 constexpr int64_t kMaxStride = int64_t{1} << 38;       // elements: what a tensor map's strides hold
 
-// Whether rows of `extent` elements at all places of some dimensions lie apart from one another.  (Sorts the dimensions.)
+// Whether rows of `extent` elements at all places of some dimensions lie apart from one another, within what an offset can count.
+// (Sorts the dimensions.)
 struct Dim { int64_t stride, size; };
 template <int N>
-bool apart(Dim (&d)[N], int64_t extent) {
+int check_apart(Dim (&d)[N], int64_t extent) {
+  constexpr int64_t kMost = int64_t{1} << 60;
   std::sort(d, d + N, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
   for (const Dim& x : d) {
     if (x.size <= 1) continue;
-    if (x.stride < extent) return false;
+    if (x.stride < extent) return CPMTP_ERR_SHAPE;
+    if (x.stride > (kMost - extent) / (x.size - 1)) return CPMTP_ERR_LIMIT;
     extent += x.stride * (x.size - 1);
   }
-  return true;
+  return CPMTP_OK;
 }
 
 // Distances of a cache's pages, slots and heads: rows of D elements must not overlap.
@@ -41,7 +44,7 @@ int check_strides(const cpmtp_cache& c, int64_t page, int64_t slot, int64_t head
     if (x.stride >= kMaxStride) return CPMTP_ERR_LIMIT;
     if (x.stride % 8 != 0) return CPMTP_ERR_ALIGN;
   }
-  return apart(d, c.D) ? CPMTP_OK : CPMTP_ERR_SHAPE;
+  return check_apart(d, c.D);
 }
 // Those of the pages and heads of acc, whose slots lie next to one another.
 int check_acc(const cpmtp_cache& c) {
@@ -50,7 +53,7 @@ int check_acc(const cpmtp_cache& c) {
     if (x.stride < c.page_slots) return CPMTP_ERR_SHAPE;
     if (x.stride >= kMaxStride) return CPMTP_ERR_LIMIT;
   }
-  return apart(d, c.page_slots) ? CPMTP_OK : CPMTP_ERR_SHAPE;
+  return check_apart(d, c.page_slots);
 }
 
 int check_cache(const cpmtp_cache* c) {

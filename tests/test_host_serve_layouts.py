@@ -25,3 +25,14 @@ def test_pages_and_heads_of_acc_must_not_overlap(lib, layout):
 @pytest.mark.parametrize("layout", APART_ACC, ids=str)
 def test_pages_and_heads_of_acc_that_lie_apart_are_taken(lib, layout):
     assert lib.cpmtp_cache_attend_workspace_bytes(cache(**layout), seqs(), 4) > 0
+
+
+FAR = 1 << 37
+
+
+@pytest.mark.parametrize("layout", [dict(pages=2 ** 31 - 1, k_page=FAR, k_head=FAR + 64), dict(pages=2 ** 31 - 1, v_page=FAR), dict(pages=2 ** 31 - 1, acc_page=FAR, acc_head=FAR + 16),
+                                    dict(pages=2 ** 31 - 1, H=65535, k_page=FAR, k_head=FAR + 128)], ids=str)
+def test_spans_beyond_64_bits_are_refused(lib, layout):
+    """Offsets of the last pages would not fit, and what the pages span is not known to overlap or not."""
+    assert set(calls(lib, cache(**layout), seqs())) == {-7}
+    assert lib.cpmtp_cache_attend_workspace_bytes(cache(**layout), seqs(), 4) == 0
