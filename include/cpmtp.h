@@ -616,7 +616,8 @@ typedef struct cpmtp_tokens {
 
 /*
  * Puts the keys and values [B, Q, H, D] bf16 of the new tokens into their slots; acc of these slots (of every head) becomes 0.
- * Rows j >= q_lens[b] are not read.  Slots out of range are left out and raise dev_status to 1.
+ * Rows j >= q_lens[b] are not read.  Slots out of range are left out and raise dev_status to 1: of a sequence that is too long the tokens that still have
+ * a slot go there.
  */
 int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, const cpmtp_tokens* k, const cpmtp_tokens* v,
                        int32_t* dev_status, cpmtp_stream stream);

@@ -54,7 +54,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     const int h = in / pieces, col = 8 * (in % pieces), b = static_cast<int>(r / runs), j0 = static_cast<int>(r - static_cast<long long>(b) * runs) * kTokens;
     const int fresh = seq_new(s, b, dev_status);
     if (j0 >= fresh) continue;
-    const int slot0 = seq_len(c, s, b, dev_status) - fresh + j0;
+    // (a length that is too large is not clamped: the tokens that have slots keep them, and the others are left out)
+    const int len = s.lens[b], most = s.width * c.page_slots, slot0 = min(max(len, 0), most + fresh) - fresh + j0;
+    if (len < 0 || len > most) raise_status(dev_status, kBadIndex);
     const bf16_t* kp = static_cast<const bf16_t*>(k.data) + b * k.seq + h * k.head + col;
     const bf16_t* vp = static_cast<const bf16_t*>(v.data) + b * v.seq + h * v.head + col;
     uint4 x[kTokens], y[kTokens];
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
       const int j = j0 + q, slot = slot0 + q;
       page[q] = -1;
       if (j >= fresh) continue;
-      if (slot < 0) {
+      if (slot < 0 || slot >= most) {
         raise_status(dev_status, kBadIndex);
         continue;
       }
