@@ -769,6 +769,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const int2 ctas = p.unit_ctas[unit_at];
     if (!parts_known(p, ctas)) return;
     const int rows = min(NT, all_rows - chunk * NT);
+    bool nan = false;
     __syncthreads();
     if (ctas.y - ctas.x < kFewParts) {
       // few parts: a thread to a row
@@ -787,24 +788,40 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
           for (int i = 0; i < kFewParts; ++i) l += ml[i].y * ptx::ex2_approx(ml[i].x - m);
         }
         sh[threadIdx.x] = l == 0.f ? INFINITY : m + log2f(l);
+        nan = l != l;
       }
     } else {
       for (int r = warp; r < rows; r += kJoinThreads / 32) {
         const float2 ml = joined<NT>(p, ctas, unit_at, r);
         if (lane == 0) sh[r] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+        nan |= ml.y != ml.y;
       }
     }
-    __syncthreads();
+    const bool broken = __syncthreads_or(nan);
     if (first >= q.len) continue;
     const float4* s = reinterpret_cast<const float4*>(p.scores + (unit_at * p.tiles + first / kTile) * NT * kTile + first % kTile);
+    if (!broken) {
 #pragma unroll 8
-    for (int r = 0; r < rows; ++r) {
-      const float4 v = s[r * (kTile / 4)];
-      const float f = sh[r];
-      sum.x += ptx::ex2_approx(v.x - f);
-      sum.y += ptx::ex2_approx(v.y - f);
-      sum.z += ptx::ex2_approx(v.z - f);
-      sum.w += ptx::ex2_approx(v.w - f);
+      for (int r = 0; r < rows; ++r) {
+        const float4 v = s[r * (kTile / 4)];
+        const float f = sh[r];
+        sum.x += ptx::ex2_approx(v.x - f);
+        sum.y += ptx::ex2_approx(v.y - f);
+        sum.z += ptx::ex2_approx(v.z - f);
+        sum.w += ptx::ex2_approx(v.w - f);
+      }
+    } else {
+      // a row whose sum is NaN has no weight, not even that, for the slots that it does not see
+#pragma unroll 1
+      for (int r = 0; r < rows; ++r) {
+        const float4 v = s[r * (kTile / 4)];
+        const float f = sh[r];
+        const int seen = q.len - (q.fresh - 1 - (chunk * NT + r) / p.G) - first;
+        sum.x += seen > 0 ? ptx::ex2_approx(v.x - f) : 0.f;
+        sum.y += seen > 1 ? ptx::ex2_approx(v.y - f) : 0.f;
+        sum.z += seen > 2 ? ptx::ex2_approx(v.z - f) : 0.f;
+        sum.w += seen > 3 ? ptx::ex2_approx(v.w - f) : 0.f;
+      }
     }
   }
   const float add[4] = {sum.x, sum.y, sum.z, sum.w};

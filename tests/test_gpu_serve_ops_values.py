@@ -65,3 +65,28 @@ def test_values_that_overflow_or_are_nan_by_their_weights_stay_so():
     c.v[int(page[9]), int(at[9]), 0, 7] = INF
     got = numbers(binding.cache_attend(c.cache(), c.q, c.table, c.lens_t)["out"])
     assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("H,Hq,D,page,lens,Q", [(2, 4, 64, 16, [300, 131, 6], 5), (1, 8, 128, 64, [20000, 64], 9), (1, 2, 40, 8, [129], 3)])
+@pytest.mark.parametrize("bad", [NAN, INF])
+def test_a_broken_query_adds_to_the_slots_that_it_sees_alone(bad, H, Hq, D, page, lens, Q):
+    """The query of one token is NaN or infinite: its weights are NaN.  Slots behind it get the later tokens' weights, within the bounds of the others."""
+    from paper_2410_17765_b200 import binding
+
+    c = Case(lens, H, D, page, Hq=Hq, Q=Q, seed=D)
+    broken = Q // 2 - 1
+    c.q[:, broken, :, 1] = bad
+    before = numbers(c.acc)
+    binding.cache_attend(c.cache(), c.q, c.table, c.lens_t, dev_status=c.status)
+    assert int(c.status.item()) == 0
+    after = numbers(c.acc)
+    for b, n in enumerate(lens):
+        page_of, at = S.places(c.table_np[b], page, n)
+        sees = max(0, n - (Q - 1 - broken))
+        got, was = after[page_of, :, at], before[page_of, :, at]
+        assert np.isnan(got[:sees]).all()
+        # the tokens behind the broken one alone: its own rows and those before it have no weight there
+        later = S.attend(numbers(c.q[b, broken + 1:]), c.of(c.k, b), c.of(c.v, b), Q - 1 - broken, D ** -0.5)
+        p_rel = 2 * (D + 4) * 2.0 ** -24 * later["terms"].max() + 2.0 ** -20 + n * 2.0 ** -24
+        want = was[sees:] + later["weights"].T[sees:]
+        assert len(want) and (np.abs(got[sees:] - want) <= later["weights"].T[sees:] * p_rel + 2.0 ** -23 * np.abs(want)).all()
