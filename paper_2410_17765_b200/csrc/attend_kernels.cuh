@@ -40,7 +40,7 @@ constexpr int kTile = 128;                  // slots of a tile
 constexpr int kThreads = 12 * 32;
 constexpr int kHalfBytes = kTile * 128;     // 128 slots of 64 columns
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNone = -1.7e38f;           // the reference of a row that has seen nothing yet
+constexpr float kNone = -FLT_MAX;           // the reference of a row that has seen nothing yet; no finite score lies below it
 // The reference that weights are taken relative to follows the running maximum only when that has risen by so much (a factor of
 // 256 in the weights, which costs neither fp32 nor bf16 a digit): nearly every tile then leaves the sums as they are.
 constexpr float kSlack = 8.f;

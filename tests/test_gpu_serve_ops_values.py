@@ -90,3 +90,34 @@ def test_a_broken_query_adds_to_the_slots_that_it_sees_alone(bad, H, Hq, D, page
         p_rel = 2 * (D + 4) * 2.0 ** -24 * later["terms"].max() + 2.0 ** -20 + n * 2.0 ** -24
         want = was[sees:] + later["weights"].T[sees:]
         assert len(want) and (np.abs(got[sees:] - want) <= later["weights"].T[sees:] * p_rel + 2.0 ** -23 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("n,Q", [(1, 1), (40, 3), (300, 1), (20000, 2)])
+@pytest.mark.parametrize("top", [126, -126])
+def test_scores_near_the_ends_of_fp32(top, n, Q):
+    """Scores of about +-2^126.9 (in units of log 2 +-2^127.4, still finite), one of them nearer to zero by a factor that leaves the others no weight: its value comes
+    out, rounded by 2^-24 for the product of a weight of one and its sum, and 2^-8."""
+    from paper_2410_17765_b200 import binding
+
+    c = Case([n], 1, 8, 16, Hq=2, Q=Q, seed=n)
+    page, at = S.places(c.table_np[0], 16, n)
+    page, at = torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(at).cuda()
+    c.q.zero_()
+    c.q[..., 0] = 2.0 ** 63
+    c.k[page, at] = 0.0
+    big = 1.875 * 2.0 ** (abs(top) - 63)
+    best = 0 if top < 0 or n == 1 else n // 2
+    c.k[page, at, 0, 0] = -big
+    c.k[page[best], at[best], 0, 0] = (big if top > 0 else -big) * 0.9375
+    before = c.acc.clone()
+    r = binding.cache_attend(c.cache(), c.q, c.table, c.lens_t, scale=1.0, want_lse=True, dev_status=c.status)
+    assert int(c.status.item()) == 0
+    got, value = numbers(r["out"])[0], numbers(c.v)[int(page[best]), int(at[best]), 0]
+    score = 2.0 ** 63 * float(c.k[page[best], at[best], 0, 0])
+    for j in range(Q):
+        if best < n - (Q - 1 - j):
+            assert (np.abs(got[j] - value) <= (2.0 ** -8 + 2.0 ** -20) * np.abs(value)).all()
+            assert (np.abs(r["lse"][0, j].cpu().numpy().astype(np.float64) - score) <= 2.0 ** -21 * abs(score)).all()
+    acc = numbers(c.acc - before)[page.cpu().numpy(), 0, at.cpu().numpy()]
+    seen = sum(best < n - (Q - 1 - j) for j in range(Q))
+    assert abs(acc[best] - 2 * seen) <= 2.0 ** -18 and (np.delete(acc, best) == 0).all()
