@@ -121,3 +121,25 @@ def test_scores_near_the_ends_of_fp32(top, n, Q):
     acc = numbers(c.acc - before)[page.cpu().numpy(), 0, at.cpu().numpy()]
     seen = sum(best < n - (Q - 1 - j) for j in range(Q))
     assert abs(acc[best] - 2 * seen) <= 2.0 ** -18 and (np.delete(acc, best) == 0).all()
+
+
+@pytest.mark.parametrize("how,left", [(dict(), None), (dict(top_p=0.9), 3), (dict(top_k=3), 3), (dict(min_p=0.5), 3), (dict(top_k=4, top_p=0.6), 2), (dict(top_k=2), 2)], ids=str)
+@pytest.mark.parametrize("V", [5, 3001])
+def test_the_largest_number_beside_an_infinite_logit_counts_as_infinite(V, how, left):
+    """Three entries share the mass: `left` of them, and nothing else, are left by a filter (without one every entry is).  Drawn and given tokens have the log-probability of the share that they were drawn with."""
+    from paper_2410_17765_b200 import binding
+
+    big = torch.finfo(torch.float32).max
+    x = torch.zeros(8, V, device="cuda")
+    x[:, 1], x[:, 2], x[:, 4] = big, INF, big
+    u = (torch.arange(8, device="cuda") + 0.5) / 8
+    given = torch.tensor([1, 2, 4, 0, 1, 2, 4, 3], dtype=torch.int32, device="cuda")
+    r = binding.sample_logits(x, u, given=given, want_kept=True, **how)
+    assert r["kept"].tolist() == [V if left is None else left] * 8
+    kept = 3 if left is None else left
+    order = [2, 1, 4][:kept]                               # by falling logits, of equals the first
+    assert set(r["tokens"].tolist()) == set(order)
+    want = torch.full((8,), -float(np.log(kept)), device="cuda")
+    assert (r["logp"] - want).abs().max() <= 2.0 ** -22
+    for g, got in zip(given.tolist(), r["logp_given"].tolist()):
+        assert abs(got + np.log(kept)) <= 2.0 ** -22 if g in order else got == -INF
