@@ -623,7 +623,7 @@ int cpmtp_cache_append(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
                        int32_t* dev_status, cpmtp_stream stream);
 
 typedef struct cpmtp_attend_args {
-  cpmtp_tokens q, out;              /* [B, Q, Hq, D] bf16 */
+  cpmtp_tokens q, out;              /* [B, Q, Hq, D] bf16; rows of out must not overlap (as those of a cache) */
   float* lse;                       /* [B, Q, Hq] or NULL */
   int32_t Hq;                       /* a multiple of H: query head h looks at head h / (Hq / H) of the cache */
   float scale;                      /* of the products; finite */

@@ -87,6 +87,13 @@ int check_tokens(const cpmtp_tokens* t, int64_t Q, int64_t H, int D) {
   if (t->seq < 0 || (Q > 1 && t->token < D) || (H > 1 && t->head < D)) return CPMTP_ERR_SHAPE;
   return aligned(t->data, 2) ? CPMTP_OK : CPMTP_ERR_ALIGN;
 }
+// Those that are written: no two of them in one place.
+int check_written(const cpmtp_tokens* t, int64_t B, int64_t Q, int64_t H, int D) {
+  const int rc = check_tokens(t, Q, H, D);
+  if (rc != CPMTP_OK) return rc;
+  Dim d[3] = {{t->seq, B}, {t->token, Q}, {t->head, H}};
+  return check_apart(d, D);
+}
 bool tokens_vec(const cpmtp_tokens& t) { return aligned(t.data, 16) && t.seq % 8 == 0 && t.token % 8 == 0 && t.head % 8 == 0; }
 
 int blocks_for(long long items, int threads, int sms) {
@@ -255,7 +262,7 @@ int cpmtp_cache_attend(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, c
   if (!attend_fits(c, s, a.Hq)) return CPMTP_ERR_LIMIT;
   if (s.B == 0 || s.Q == 0) return CPMTP_OK;
   if ((rc = check_cache_data(c)) != CPMTP_OK || (rc = check_seqs_data(s)) != CPMTP_OK) return rc;
-  if ((rc = check_tokens(&a.q, s.Q, a.Hq, c.D)) != CPMTP_OK || (rc = check_tokens(&a.out, s.Q, a.Hq, c.D)) != CPMTP_OK) return rc;
+  if ((rc = check_tokens(&a.q, s.Q, a.Hq, c.D)) != CPMTP_OK || (rc = check_written(&a.out, s.B, s.Q, a.Hq, c.D)) != CPMTP_OK) return rc;
   if (workspace == nullptr) return CPMTP_ERR_NULL;
   if (!aligned(a.lse, 4) || !aligned(dev_status, 4) || !aligned(workspace, kAlign)) return CPMTP_ERR_ALIGN;
   const AttendLayout L = attend_layout(c, s, a.Hq);

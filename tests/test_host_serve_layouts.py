@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2410_17765_b200 import binding
-from test_host_serve_ops import attend, cache, calls, evict, lib, seqs, tokens  # noqa: F401
+from test_host_serve_ops import P, attend, cache, calls, evict, lib, seqs, tokens  # noqa: F401
 
 NO_GPU = not torch.cuda.is_available()
 
@@ -36,3 +36,22 @@ def test_spans_beyond_64_bits_are_refused(lib, layout):
     """Offsets of the last pages would not fit, and what the pages span is not known to overlap or not."""
     assert set(calls(lib, cache(**layout), seqs())) == {-7}
     assert lib.cpmtp_cache_attend_workspace_bytes(cache(**layout), seqs(), 4) == 0
+
+
+@pytest.mark.parametrize("layout,code", [(dict(seq=0), -2), (dict(seq=256), -2), (dict(token=128), -2), (dict(token=64, head=64), -2), (dict(seq=511), -2), (dict(seq=64, token=192, head=320), -2),
+                                         (dict(seq=1 << 60), -7)], ids=str)
+def test_outputs_must_not_overlap(lib, layout, code):
+    """Three sequences of two tokens of four heads of 64; queries may overlap (a batch of one row expanded)."""
+    c, s = cache(), seqs()
+    need = lib.cpmtp_cache_attend_workspace_bytes(c, s, 4)
+    assert lib.cpmtp_cache_attend(c, s, attend(out=tokens(**layout)), P, need, None, None) == code
+    if NO_GPU:
+        assert lib.cpmtp_cache_attend(c, s, attend(q=tokens(seq=0)), P, need, None, None) in (-5, -6)
+
+
+@pytest.mark.skipif(not NO_GPU, reason="the addresses are made up")
+@pytest.mark.parametrize("layout", [dict(), dict(seq=1024), dict(seq=2048, token=64, head=128), dict(seq=64, token=192, head=384)], ids=str)
+def test_outputs_that_lie_apart_are_taken(lib, layout):
+    c, s = cache(), seqs()
+    need = lib.cpmtp_cache_attend_workspace_bytes(c, s, 4)
+    assert lib.cpmtp_cache_attend(c, s, attend(out=tokens(**layout)), P, need, None, None) in (-5, -6)
