@@ -650,7 +650,7 @@ typedef struct cpmtp_evict_args {
   const int32_t* table_out;         /* pages that take the kept slots: slot j of sequence b is in page table_out[b * ld_table_out + j / page_slots] */
   int64_t ld_table_out;             /* >= ceil(budget / page_slots) */
   int32_t budget, recent;           /* 0 <= recent <= budget, budget >= 1 */
-  int32_t* lens_out;                /* [B], not lens: the new lengths, min(lens, budget) */
+  int32_t* lens_out;                /* [B], no part of lens: the new lengths, min(lens, budget) */
   int32_t* kept;                    /* [B, H, budget]: the slots that were kept, -1 behind the last; or NULL */
 } cpmtp_evict_args;
 

@@ -55,3 +55,13 @@ def test_outputs_that_lie_apart_are_taken(lib, layout):
     c, s = cache(), seqs()
     need = lib.cpmtp_cache_attend_workspace_bytes(c, s, 4)
     assert lib.cpmtp_cache_attend(c, s, attend(out=tokens(**layout)), P, need, None, None) in (-5, -6)
+
+
+@pytest.mark.parametrize("off", [-8, -4, 0, 4, 8])
+def test_new_lengths_must_not_overlap_the_old_ones(lib, off):
+    c, s = cache(), seqs()
+    need = lib.cpmtp_cache_evict_workspace_bytes(c, s, 32)
+    assert lib.cpmtp_cache_evict(c, s, evict(lens_out=P + off), P, need, None, None) == -2
+    if NO_GPU:
+        for apart in (-12, 12):
+            assert lib.cpmtp_cache_evict(c, s, evict(lens_out=P + apart), P, need, None, None) in (-5, -6)
