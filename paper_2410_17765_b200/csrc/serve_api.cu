@@ -317,9 +317,9 @@ int cpmtp_cache_evict(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, co
   if (s.B == 0) return CPMTP_OK;
   if ((rc = check_cache_data(c)) != CPMTP_OK || (rc = check_seqs_data(s)) != CPMTP_OK) return rc;
   if (c.acc == nullptr || e.table_out == nullptr || e.lens_out == nullptr || (workspace == nullptr && e.kept == nullptr)) return CPMTP_ERR_NULL;
-  if (e.lens_out < s.lens + s.B && s.lens < e.lens_out + s.B) return CPMTP_ERR_SHAPE;      // (read by other blocks than the one that writes)
   if (!aligned(e.table_out, 4) || !aligned(e.lens_out, 4) || !aligned(e.kept, 4) || !aligned(dev_status, 4) || !aligned(workspace, kAlign))
     return CPMTP_ERR_ALIGN;
+  if (e.lens_out < s.lens + s.B && s.lens < e.lens_out + s.B) return CPMTP_ERR_SHAPE;      // (read by other blocks than the one that writes)
   if (e.kept == nullptr && workspace_bytes < evict_bytes(c, s, e.budget)) return CPMTP_ERR_WORKSPACE;
   DeviceInfo* di = nullptr;
   if ((rc = check_device(&di)) != CPMTP_OK) return rc;
