@@ -134,10 +134,11 @@ class Server:
 
 def generate(cfg: Config = Config(), *, batch: int = 8, prompt: int = 24, steps: int = 40, seed: int = 0, budget: int = 0, recent: int = 16,
              every: int = 8, **how) -> tuple:
-    """(tokens of each sequence as lists, tokens gained per round) of `steps` rounds on random prompts of ragged lengths."""
+    """(tokens of each sequence as lists, tokens gained per round) of `steps` rounds on random prompts of ragged lengths.
+    Of a budget, the last `recent` slots stay whatever their weight; all of it where it is smaller."""
     gen = torch.Generator(device="cuda").manual_seed(seed + 1)
     slots = (budget + every * cfg.n if budget else prompt + steps * cfg.n) + cfg.n + prompt
-    server = Server(Base(cfg, seed), batch, slots, budget=budget, recent=recent)
+    server = Server(Base(cfg, seed), batch, slots, budget=budget, recent=min(recent, budget))
     prompts = torch.randint(0, cfg.V, (batch, prompt), generator=gen, device="cuda").to(torch.int32)
     lengths = torch.randint(1, prompt + 1, (batch,), generator=gen, device="cuda").to(torch.int32)
     first = server.start(prompts, lengths, torch.rand(batch, generator=gen, device="cuda"), **how)
