@@ -848,7 +848,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
                   behind + tiny, (behind - least) * (1.0 - slack) - tiny, b1, b2, before);
       // Entries above xa lie in bins before b1, those below xb in bins behind b2; the bins' edges, rounded outwards.
       const float xa = nextafterf(__double2float_ru(w.m - (b1 - 1) / (64.0 * w.c)), INFINITY);
-      const float xb = b2 == kBins - 1 ? -FLT_MAX : nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY);
+      // (-infinity, which stands for what is not kept, must not reach xb)
+      const float xb = b2 == kBins - 1 ? -FLT_MAX : fmaxf(nextafterf(__double2float_rd(w.m - b2 / (64.0 * w.c)), -INFINITY), -FLT_MAX);
       u64 above = 0;
       // few entries are that large: a warp collects them, and weighs 32 at a time
       float* queue = sh.queue[warp];

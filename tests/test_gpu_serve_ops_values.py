@@ -143,3 +143,21 @@ def test_the_largest_number_beside_an_infinite_logit_counts_as_infinite(V, how, 
     assert (r["logp"] - want).abs().max() <= 2.0 ** -22
     for g, got in zip(given.tolist(), r["logp_given"].tolist()):
         assert abs(got + np.log(kept)) <= 2.0 ** -22 if g in order else got == -INF
+
+
+@pytest.mark.parametrize("how", [dict(p=0.95), dict(p=0.3), dict(p=0.999, T=1e-3), dict(p=0.9, min_p=0.5), dict(p=0.9, k=700), dict(T=1e20, p=0.6)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 2, 3, 8, 1001, 60000])
+def test_rows_that_hold_the_lowest_number_alone(V, dtype, how):
+    """Rows that a mask of the type's lowest value leaves nothing of: their entries share the mass, and nothing beside the row counts."""
+    from test_gpu_sample import check
+
+    low = torch.finfo(dtype).min
+    wide = torch.full((6, V + 5), 3.0, device="cuda", dtype=dtype)
+    x = wide[:, 1:1 + V]
+    x[:] = low
+    x[3, V // 2:] = -INF
+    x[4, ::2] = NAN
+    x[5, V - 1] = 0.5
+    u = torch.tensor([0.0, 0.4, 0.99, 0.7, 0.2, 0.6], device="cuda")
+    check(x, u, sure=False, given=torch.full((6,), V - 1, dtype=torch.int32, device="cuda"), **how)
