@@ -654,7 +654,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const _
   auto finish = [&](int token, float x_token, u64 total, int kept, float tx, int ti) {
     if (!writer || token < 0) return;
     const double all = log(static_cast<double>(total) / unit);
-    auto logp = [&](float v) { return static_cast<float>((v >= w.x_max ? 0.0 : (static_cast<double>(v) - static_cast<double>(top)) * set.inv_t) - all); };
+    // (a temperature of a row's own may be infinite: its inverse is 0)
+    auto logp = [&](float v) {
+      return static_cast<float>((v >= w.x_max ? 0.0 : top > w.x_max ? -INFINITY : (static_cast<double>(v) - static_cast<double>(top)) * set.inv_t) - all);
+    };
     const bool in = x_given > -INFINITY && (x_given > tx || (x_given == tx && given <= ti)) && at_least(w.z(x_given), z_min);
     answer(token, logp(x_token), kept, in ? logp(x_given) : -INFINITY);
   };

@@ -161,3 +161,19 @@ def test_rows_that_hold_the_lowest_number_alone(V, dtype, how):
     x[5, V - 1] = 0.5
     u = torch.tensor([0.0, 0.4, 0.99, 0.7, 0.2, 0.6], device="cuda")
     check(x, u, sure=False, given=torch.full((6,), V - 1, dtype=torch.int32, device="cuda"), **how)
+
+
+@pytest.mark.parametrize("V", [6, 4001])
+def test_infinite_temperatures_of_rows(V):
+    """Every kept entry has the same share; beside infinite logits no finite one has any."""
+    from paper_2410_17765_b200 import binding
+
+    x = torch.randn(4, V, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda")
+    x[2:, 1] = x[2:, 3] = INF
+    x[1, 0] = -INF
+    given = torch.tensor([V - 1, V - 1, 2, 3], dtype=torch.int32, device="cuda")
+    r = binding.sample_logits(x, torch.full((4,), 0.6, device="cuda"), temperature=torch.full((4,), INF, device="cuda"), given=given, want_kept=True)
+    assert r["tokens"][2:].tolist() == [3, 3] and r["kept"].tolist() == [V, V - 1, V, V]
+    for got, share in ((r["logp"], [V, V - 1, 2, 2]), (r["logp_given"], [V, V - 1, INF, 2])):
+        for value, n in zip(got.tolist(), share):
+            assert value == -INF if n == INF else abs(value + np.log(n)) <= 2.0 ** -24 * np.log(n) + 2.0 ** -30
