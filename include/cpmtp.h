@@ -634,12 +634,14 @@ typedef struct cpmtp_attend_args {
  *   s_i = scale * <q[b, j, h], k_i>  for the slots i < lens[b] - (q_lens[b] - 1 - j),
  *   p = softmax(s),  out[b, j, h] = sum_i p_i v_i,  lse[b, j, h] = log sum_i exp(s_i).
  * A token that sees no slot gets a row of zeros and lse -infinity.  Rows j >= q_lens[b] of out and lse are left as they were.
- * With cache->acc, acc of slot i and head g += the sum of p_i over the new tokens and the query heads that look at g.
+ * With cache->acc, acc of slot i and head g += the sum of p_i over the new tokens and the query heads that look at g.  A draft's tokens count whether they are kept
+ * afterwards or not: giving up their slots by a smaller lens takes nothing back from the slots before them.
  * A page number out of range stands for keys and values of zero.  Infinities and NaN in a slot reach the tokens that see it and no others: a value
  * that is infinite counts so however small its weight (values of both signs give NaN).  Whatever lies in slots that no token sees is not looked at.
  * Sequences are shared out over the SMs by their tiles of 128 slots, whatever their lengths, and joined in a second launch: the last bits of
  * out, lse and acc depend on the batch, and repeat for the same one.  Workspace: cpmtp_cache_attend_workspace_bytes, which looks at
- * numbers alone (and at whether cache->acc is NULL), on the device of the call; with acc it holds a score for every row and slot.
+ * numbers alone (and at whether cache->acc is NULL), on the device of the call.  With acc it holds the scores of all slots that the table has room for, those in use or not:
+ * B * H * ceil(width * page_slots / 128) tiles of 128 slots, of 16 or 32 rows in fp32, for every 16 or 32 of the Q * Hq / H (16 sequences, 8 heads, 20 rows and 131072 slots: 2.1 GB).
  * Limit: B * H * ceil(Q * Hq / H / 16 or 32) * ceil(width * page_slots / 128) < 2^31.
  */
 size_t cpmtp_cache_attend_workspace_bytes(const cpmtp_cache* cache, const cpmtp_cache_seqs* seqs, int32_t Hq);

@@ -1333,7 +1333,8 @@ def cache_attend(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: 
     """cpmtp_cache_attend: attention of the new tokens q [B, Q, Hq, D] bf16 over the cache, which holds their own keys and values already
     (cache_append); token j of q_lens[b] sees lens[b] - (q_lens[b] - 1 - j) slots.  scale: D ** -0.5 if None.  Returns {"out" [B, Q, Hq, D] bf16
     [, "lse" [B, Q, Hq] fp32]}; rows behind q_lens are zeros, or left as they were in tensors given by `out`.  accumulate: add the
-    weights to cache.acc, if the cache has it."""
+    weights to cache.acc, if the cache has it.  The dictionary `out` is the one that is returned: tensors that it lacks are made and put there, so a call with the same one
+    writes over them."""
     dev = _device(q)
     size = q.shape
     _need(len(size) == 4, "q must be [B, Q, Hq, D]")
@@ -1366,7 +1367,7 @@ def cache_evict(cache: PagedCache, table: torch.Tensor, lens: torch.Tensor, tabl
                 out: Optional[dict] = None, dev_status: Optional[torch.Tensor] = None) -> dict:
     """cpmtp_cache_evict: cut every sequence down to `budget` slots for each head, the `recent` last ones and those of the others with the
     largest cache.acc, and move them into the pages of table_out [B, ceil(budget / page_slots) or more] int32, which must not be among those of
-    `table`.  Returns {"lens" [B], "kept" [B, H, budget] slots (-1 behind the last)} int32."""
+    `table`.  Returns {"lens" [B], "kept" [B, H, budget] slots (-1 behind the last)} int32: the dictionary `out`, if given, which tensors that it lacks are put into."""
     dev = _device(lens)
     _need(cache.acc is not None, "eviction needs a cache with acc")
     _need(budget >= 1 and 0 <= recent <= budget, "budget must be at least 1, recent between 0 and budget")
@@ -1413,7 +1414,8 @@ def sample_logits(logits: torch.Tensor, uniform: torch.Tensor, *, temperature=1.
     """cpmtp_sample_logits: a token from each row of logits [N, V] (bf16 or fp32, rows may be strided) by uniform [N] fp32 in [0, 1).
     temperature, top_k, top_p, min_p: numbers, or tensors [N] (fp32, int32, fp32, fp32) with a setting for each row; 0, 0, 1 and 0 mean
     greedy and no filter.  given [N] int32: tokens to be scored, EMBED_PAD for none.  Returns {"tokens" [N] int32, "logp" [N] fp32
-    [, "logp_given" [N] fp32][, "kept" [N] int32]}: log-probabilities under the filtered distribution."""
+    [, "logp_given" [N] fp32][, "kept" [N] int32]}: log-probabilities under the filtered distribution.  The dictionary `out`, if given, is the one
+    that is returned, and tensors that it lacks are put there."""
     dev = _device(logits)
     size, dtype = logits.shape, logits.dtype
     _need(len(size) == 2 and dtype in _TYPES, "logits must be [N, V] bfloat16 or float32")

@@ -18,11 +18,12 @@
 //   warps 4-11   two groups of 128 threads, half of the rows to each: a thread is a slot and makes its weights, then a column and
 //                sums O in registers
 //
-// What bounds it: bandwidth where there is enough to read (32 sequences of 8192 slots, 8 heads of 128 for 32 queries, 1.07 GB: 158 to 164 us in pages of 32
-// slots and more, 6.5 to 6.8 TB/s); the start, the last tiles and the joining, 11 us in all, where there are few tiles for each SM.  Pages of 16 and 8
-// slots take 182 and 235 us: a TMA box costs its warp the same whatever it holds.  (A second warp to each ring: pages of 8 201 us, but 240 against
-// 238 for 64 ragged sequences and 63 against 62 with acc.)  Heads of 64 take 111 us for half the bytes: a tile costs its products, barriers and weights.  Rows
-// above 32 read the cache again: 16 tokens 337 us, 8 tokens 172.
+// What bounds it (times in captured graphs): bandwidth where there is enough to read (32 sequences of 8192 slots, 8 heads of 128 for 32 queries, 1.07 GB: 161 to 171 us in pages of 32
+// slots and more, 6.3 to 6.7 TB/s); the start, the last tiles and the joining, 11 us in all, where there are few tiles for each SM.  Pages of 16 and 8
+// slots take 180 to 192 and 235 us: a TMA box costs its warp the same whatever it holds.  (A second warp to each ring: pages of 8 201 us, but 240 against
+// 238 for 64 ragged sequences and 63 against 62 with acc.)  Heads of 64 take 114 us (131 where heads lie within slots) for half the bytes: a tile costs its products, barriers and weights.
+// Heads of 80 take 122 us, but 210 where heads lie within slots: rows of 160 bytes, 1280 apart, are fetched in pieces of 256.  Rows above 32 read the cache again, and every chunk of rows
+// all tiles of its sequence: 8 tokens 177 us, 16 355, 64 1456; four prompts of 2048 tokens over their own slots 2147, 84 of which are operations.
 #pragma once
 #include <cuda.h>
 
@@ -189,7 +190,7 @@ struct Layout {
   static constexpr int kFixed = 1024 + 2 * kQ + 2 * kP + kBars + kSmall;
   static constexpr int kTmem = 8 * NT;               // two S accumulators and two O, of the high and the low parts of the weights (6 NT)
 };
-// Half tiles of both rings.  There is room for twelve, but with that much under way memory answers more slowly: 1.07 GB of heads of 128 columns take 168 us
+// Half tiles of both rings.  With 16 columns there is room for twelve (with 32 for ten), but with that much under way memory answers more slowly: 1.07 GB of heads of 128 columns take 168 us
 // with six tiles, 161 with five, 160 with four and 180 with three; ragged 1.4 GB in small pages 226 with four and more.
 constexpr int kMaxSlots = 10;
 

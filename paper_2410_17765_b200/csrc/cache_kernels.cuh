@@ -117,7 +117,8 @@ __device__ __forceinline__ uint32_t keep_key(float acc) { return acc != acc ? 0u
 
 // A cluster for each head of each sequence, a block for `span` of its slots.  The last key to be kept is found by its digits, eleven bits at
 // a time from histograms; then every warp numbers the kept slots of its range.  Keys stay in shared memory (HELD).  `vec`: acc can be read
-// 16 bytes at a time.  Latency bounds it, of barriers of the cluster above all: three to a digit (128 heads of 4352 slots: 16 us; 16 of 65536: 24).
+// 16 bytes at a time.  Latency bounds it, of barriers of the cluster above all: three to a digit (under the profiler, cold: 128 heads of 4352 slots 16 us, 16 of 65536 24).
+// Slots are shared out by the width of the table: 16 sequences of 4352 slots, eviction in all, take 105 us in a table of their own, 145 in one for 131072 and 188 in one for 2^20.
 template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ cpmtp_cache c, const __grid_constant__ cpmtp_cache_seqs s,
                                                                 int ctas, int span, int vec, int budget, int recent, int* lens_out, int* kept, int* dev_status) {
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
 // A warp for `rows` kept slots of a head: a lane looks one of them up, then has a 16-byte piece of a row, kAhead rows at a time; the lanes of a
 // row have its key's pieces and then its value's.  Many rows to a warp save lookups (16 x 4096 slots: 32 take 75 us, 16 take 85); few rows in all
 // want more warps instead (2 x 2048 slots: 8 take 11 us, 32 take 15).  Bandwidth bounds many rows: 16 x 4096 slots of 8 heads of 128 (537 MB read
-// and written) take 63 us; few rows the latency of three loads, each of which needs the one before.
+// and written) take 63 us (under the profiler 67); few rows the latency of three loads, each of which needs the one before.
 constexpr int kAhead = 8;
 __host__ __device__ constexpr int rows_at_once(int D) { return 32 / (D / 4); }
 inline int least_rows(int D) { return kAhead * rows_at_once(D) < 32 ? kAhead * rows_at_once(D) : 32; }

@@ -7,7 +7,7 @@
 // block.  Should they be too many (long runs of equal logits, flat rows), the key of the last kept entry is found by digits instead.
 //
 // What bounds it: at many rows the instructions, about 35 for a weight and 8 for its bin; at few rows the latency of a dozen barriers of a
-// cluster.  512 x 128256 in fp32 (263 MB): greedy 62 us, top-k of 50 113, no filter 157, top-p 309; 8 rows in bf16: 6, 17, 19 and 31.  Holding the
+// cluster.  512 x 128256 in fp32 (263 MB): greedy 62 us, top-k of 50 113, no filter 160, top-p 313; 8 rows in bf16: 5, 16, 13 and 31 (in captured graphs).  Holding the
 // row in shared memory was slower at many rows (512 x 128256 in bf16 with top-p: 473 us against 357 then), since it leaves room for fewer
 // blocks, and 1 us faster at few.
 #pragma once

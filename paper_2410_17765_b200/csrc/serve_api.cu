@@ -102,7 +102,7 @@ int blocks_for(long long items, int threads, int sms) {
 }
 
 // Columns of the narrow operand: the new tokens times the query heads that share a head, rounded up to a size there is a kernel for.  16 rows with 16 and 32
-// columns: one sequence of 1024 slots 10.7 and 11.7 us, 64 ragged ones 226 and 232; 20 rows: 16 sequences of 4096 with acc 66 and 53, 32 of 8192 327 and 168.
+// columns: one sequence of 1024 slots 10.7 and 11.7 us, 64 ragged ones 226 and 232; 20 rows: 16 sequences of 4096 with acc 66 and 53, 32 of 8192 327 and 168 (in captured graphs).
 int attend_columns(const cpmtp_cache& c, const cpmtp_cache_seqs& s, int Hq) {
   const long long rows = static_cast<long long>(s.Q) * (Hq / c.H);
   return rows <= 16 ? 16 : 32;

@@ -6,7 +6,7 @@ The base model is a small pre-norm trunk with grouped-query attention and no pos
 states.  A round runs the base model once over the last token and the draft behind it: lookup, norms, attention over the paged cache that
 the tokens have been appended to, logits, a token from each row.  The draft is kept as far as the base model agrees with it, the rejected
 tokens' slots are given up by their length alone, and the base model's own token follows.  Every so often the cache is cut down to a
-budget by the attention weight that its slots have received.  The matrix products between the library's kernels are torch's; nothing
+budget by the attention weight that its slots have received (from drafted tokens too that were not kept).  The matrix products between the library's kernels are torch's; nothing
 waits for the host within a round.
 """
 from __future__ import annotations
